@@ -1,7 +1,8 @@
 /*
  * ardiff.h -- C ABI of the entropy-gated few-step diffusion-head hot path (B200, sm_100a).
  *
- * Two calls make the path:
+ * Two calls make the path (others stand beside it: thresholds, accepted prefixes, the draft model's tokens, cache
+ * and training):
  *   ardiff_entropy_gate  per-token entropy of the softmax-normalised shallow-feature row,
  *                        threshold, stream-compacted ascending list of surviving token ids;
  *   ardiff_head_sample   K Euler flow steps of the AdaLN residual-MLP head, conditioned on
@@ -381,7 +382,96 @@ int ardiff_pipeline_submit(ardiff_pipeline* pipeline, int32_t slot, const void* 
 int ardiff_pipeline_wait(ardiff_pipeline* pipeline, int32_t slot);
 int ardiff_pipeline_join(ardiff_pipeline* pipeline, void* stream);
 
-/* Number of kernel launches the last ardiff_head_sample / ardiff_entropy_gate call on this
+/* ---------------------------------------------------------------------------------------
+ * Pages of a cache, kept on the device. (The paper's Algorithm 1 lets a draft grow token by token and cuts it
+ * where the early stop or the verification ends it; with an attention cache in pages this is what has to happen to
+ * the cache around it. No call reads or writes the cache itself.)
+ *
+ * A cache is a pool of pages of `page` tokens. Request r holds length[r] tokens; token p of it lies in page
+ * table[r][p / page] at place p % page, i.e. in slot table[r][p / page] * page + p % page. The first *free_count
+ * entries of free_pages are the ids of the pages that nobody holds; ids are the caller's and may be any int32.
+ *
+ * ardiff_pages_extend gives request r add[r] more tokens. Pages come from the end of the free list, requests in
+ * ascending order; tokens are listed in order of request and position.
+ *   requests    0 <= requests <= ARDIFF_PAGES_MAX_REQUESTS;  page >= 1;  width: pages a row of the table holds
+ *   length, add     dev int32 [requests]       (add[r] == 0 is valid: an idle request, a padded batch)
+ *   table           dev int32 [requests][width]  in: the pages held; out: the new ones behind them. Entries behind
+ *                   those are neither read nor written
+ *   free_pages      dev int32 [free_capacity], not changed;  free_count  dev int32 [1]
+ *   max_tokens      tokens that slot, position and request have room for (below 2^31)
+ *   slot            dev int64 [max_tokens] out: slot of every new token
+ *   position        dev int32 [max_tokens] out, or NULL: its position in its request
+ *   request         dev int32 [max_tokens] out, or NULL: its request
+ *   offset          dev int32 [requests + 1] out: request r's new tokens are offset[r] .. offset[r + 1] - 1 of these;
+ *                   places from offset[requests] on are left as they were
+ *   new_length      dev int32 [requests] out; may be `length` itself
+ *   new_free_count  dev int32 [1] out; may be free_count itself
+ *   status          dev int32 [1] out: ARDIFF_OK; ARDIFF_ERR_SHAPE where a length or an add is negative, a request
+ *                   gets longer than its row of the table or than 2^31 - 1, there are more than max_tokens new tokens, or
+ *                   *free_count is not within 0 .. free_capacity; ARDIFF_ERR_NOMEM where the free pages do not suffice.
+ *                   Then nothing is taken: new_length = length, new_free_count = free_count, offset all 0, slot,
+ *                   position, request and table as they were
+ * ardiff_pages_truncate leaves request r its first target[r] tokens (e.g. the length before the draft plus what
+ * ardiff_accept_prefix accepted) and puts the pages that none of them needs on the free list, in the order in which the next
+ * extend gives them out as an earlier one did. The table is not changed.
+ *   length, target  dev int32 [requests], 0 <= target[r] <= length[r] <= width * page
+ *   free_pages      dev int32 [free_capacity] in/out;  free_count, new_free_count  dev int32 [1] (may be the same)
+ *   status          ARDIFF_ERR_SHAPE where a length or target is out of range, or the free list has no room; then
+ *                   nothing is given back
+ * Neither call allocates or keeps anything; calls on different streams are independent. Buffers other than those
+ * named as such must not overlap. Page ids are not checked.
+ * ------------------------------------------------------------------------------------- */
+#define ARDIFF_PAGES_MAX_REQUESTS (1 << 20)
+int ardiff_pages_extend(int32_t requests, int32_t page, int32_t width, const int32_t* length, const int32_t* add,
+                        int32_t* table, const int32_t* free_pages, int64_t free_capacity, const int32_t* free_count,
+                        int64_t max_tokens, int64_t* slot, int32_t* position, int32_t* request, int32_t* offset,
+                        int32_t* new_length, int32_t* new_free_count, int32_t* status, void* stream);
+int ardiff_pages_truncate(int32_t requests, int32_t page, int32_t width, const int32_t* length, const int32_t* target,
+                          const int32_t* table, int32_t* free_pages, int64_t free_capacity, const int32_t* free_count,
+                          int32_t* new_free_count, int32_t* status, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Distillation of a draft model from its target's largest logits. (The drafts of speculative decoding are accepted
+ * as often as the two agree; the paper trains its draft on its target's outputs.)
+ *
+ * Operation, row by row: over the entries j of the teacher that count (0 <= ids[j] < V and a logit above -inf; others,
+ * e.g. ids of -1 behind a shorter list, do not) q = softmax(teacher / T); p = softmax(logits / T) over all V;
+ *   loss = sum_j q_j (ln q_j - ln p[ids_j]);   grad_i = weight (p_i - sum_{j: ids_j = i} q_j) / T.
+ * An id may occur more than once. A row without entries has loss 0, stats 0 and gradient 0, and its logits are not
+ * read. A masked logit (-inf) has p = 0; loss = +inf where the teacher has a share there. A row of logits with NaN or
+ * +inf, or of only -inf, and a teacher's entry of NaN or +inf, give NaN (a row of logits in loss, stats and gradient,
+ * an entry in the loss and at the row's entries).
+ *
+ *   logits   dev  [n][V], rows `ld` >= V values apart, of type dtype (ARDIFF_BF16, ARDIFF_F16 or ARDIFF_F32), at any
+ *            multiple of its size
+ *   n        0 <= n < 2^28;  1 <= V <= ARDIFF_DISTILL_MAX_V
+ *   teacher  dev  [n][k] of type teacher_dtype (any of the three);  ids dev int32 [n][k];  1 <= k <= ARDIFF_DISTILL_MAX_K
+ *   temperature   T > 0 (and 1 / T > 0), the same for both sides; the usual factor T^2 is the caller's, in `weight`
+ *   loss     dev float [n] out
+ *   stats    dev float [n][2]: out (of the loss): the row's largest logit m and ln sum_i exp((logits_i - m) / T); in
+ *            (of the backward pass)
+ *   weight   dev float [n]: the gradient of what is minimised with respect to loss[row]
+ *   grad     dev  [n][V] out, rows ld_grad >= V values apart, of type dtype; may be the logits themselves (same ld)
+ * ardiff_distill_topk gives loss and stats; ardiff_distill_topk_backward the gradient from stats, as a graph of automatic
+ * differentiation asks for it; ardiff_distill_topk_step all three at once, for rows whose weight is known.
+ * Arithmetic is fp32 (fp32 sums in a fixed order: equal calls give equal bits); a gradient is rounded once.
+ * ------------------------------------------------------------------------------------- */
+#define ARDIFF_BF16 0
+#define ARDIFF_F16 1
+#define ARDIFF_F32 2
+#define ARDIFF_DISTILL_MAX_V (1 << 24)
+#define ARDIFF_DISTILL_MAX_K 1024
+int ardiff_distill_topk(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld, const void* teacher,
+                        int32_t teacher_dtype, const int32_t* ids, int32_t k, float temperature, float* loss, float* stats,
+                        void* stream);
+int ardiff_distill_topk_backward(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld, const void* teacher,
+                                 int32_t teacher_dtype, const int32_t* ids, int32_t k, float temperature,
+                                 const float* stats, const float* weight, void* grad, int64_t ld_grad, void* stream);
+int ardiff_distill_topk_step(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld, const void* teacher,
+                             int32_t teacher_dtype, const int32_t* ids, int32_t k, float temperature, const float* weight,
+                             float* loss, float* stats, void* grad, int64_t ld_grad, void* stream);
+
+/* Number of kernel launches the last call of the gate, the head, the cache's pages or the rows of logits on this
  * thread enqueued (for launch accounting by benchmarks). */
 int ardiff_last_launch_count(void);
 

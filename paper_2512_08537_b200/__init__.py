@@ -19,6 +19,7 @@ _STAY = contextlib.nullcontext()
 ARDIFF_OK = 0
 ARDIFF_ERR_NULL, ARDIFF_ERR_SHAPE, ARDIFF_ERR_ALIGN, ARDIFF_ERR_UNSUPPORTED = -1, -2, -3, -4
 ARDIFF_ERR_CUDA, ARDIFF_ERR_TIMEOUT, ARDIFF_ERR_NOMEM = -5, -6, -7
+ARDIFF_BF16, ARDIFF_F16, ARDIFF_F32 = 0, 1, 2
 
 _WEIGHT_FIELDS = ["Wc", "bc", "Wt1", "bt1", "Wt2", "bt2", "Win", "bin", "Wmod", "bmod",
                   "W1", "b1", "W2", "b2", "Wfm", "bfm", "Wout", "bout"]
@@ -106,6 +107,16 @@ def lib() -> ctypes.CDLL:
         L.ardiff_pipeline_wait.argtypes = [vp, i32]
         L.ardiff_pipeline_join.restype = ctypes.c_int
         L.ardiff_pipeline_join.argtypes = [vp, vp]
+        L.ardiff_pages_extend.restype = ctypes.c_int
+        L.ardiff_pages_extend.argtypes = [i32, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.ardiff_pages_truncate.restype = ctypes.c_int
+        L.ardiff_pages_truncate.argtypes = [i32, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, vp]
+        L.ardiff_distill_topk.restype = ctypes.c_int
+        L.ardiff_distill_topk.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, i32, f32, vp, vp, vp]
+        L.ardiff_distill_topk_backward.restype = ctypes.c_int
+        L.ardiff_distill_topk_backward.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, i32, f32, vp, vp, vp, i64, vp]
+        L.ardiff_distill_topk_step.restype = ctypes.c_int
+        L.ardiff_distill_topk_step.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, i32, f32, vp, vp, vp, vp, i64, vp]
         _lib = L
     return _lib
 
@@ -247,6 +258,162 @@ def ardiff_accept_prefix(r, ratio, gamma: int, block_len=None, stream=None):
                 out.data_ptr(), _stream_ptr(stream))
     _check(rc, "ardiff_accept_prefix")
     return out[:(n + gamma - 1) // gamma]
+
+
+_DTYPES = None
+
+
+def _dtype(t) -> int:
+    """A tensor's type by the library's number; one that it has no number for is refused there."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.bfloat16: ARDIFF_BF16, torch.float16: ARDIFF_F16, torch.float32: ARDIFF_F32}
+    return _DTYPES.get(t.dtype, -1)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rows(x) -> int:
+    """Distance of the rows of a matrix whose rows are contiguous (one row, or one column, may have any)."""
+    n, V = x.shape
+    assert V <= 1 or x.stride(1) == 1, "rows must be contiguous"
+    ld = x.stride(0) if n > 1 else V
+    assert ld >= V, "rows must not overlap"
+    return ld
+
+
+def _int32(t, shape, dev):
+    import torch
+    assert t.dtype == torch.int32 and t.device == dev and t.is_contiguous() and t.shape == shape, (t.dtype, t.shape, shape)
+
+
+def ardiff_pages_extend(length, add, table, free_pages, free_count, page: int, slot, position=None, request=None, offset=None,
+                        new_length=None, new_free_count=None, status=None, stream=None):
+    """add[r] new tokens for request r of a paged cache: pages from the end of the free list, the block table lengthened in
+    place, slot / position / request of every new token (as many as fit in slot; position and request are written if
+    passed). int32 CUDA tensors, slot int64. new_length may be `length` and new_free_count `free_count`; what is not passed is
+    allocated. Returns (offset [R + 1], new_length [R], new_free_count [1], status [1]); status is not looked at here."""
+    import torch
+    dev, R = length.device, length.shape[0]
+    assert length.is_cuda and table.dim() == 2
+    for t, shape in ((length, (R,)), (add, (R,)), (table, (R, table.shape[1])), (free_count, (1,))):
+        _int32(t, shape, dev)
+    _int32(free_pages, (free_pages.shape[0],), dev)
+    assert slot.dtype == torch.int64 and slot.device == dev and slot.is_contiguous() and slot.dim() == 1
+    tokens = slot.shape[0]
+    for t in (position, request):
+        if t is not None:
+            _int32(t, (tokens,), dev)
+    made = []
+    for t, size in ((offset, R + 1), (new_length, R), (new_free_count, 1), (status, 1)):
+        if t is None:
+            t = torch.empty((size,), dtype=torch.int32, device=dev)
+        else:
+            _int32(t, (size,), dev)
+        made.append(t)
+    with _on(dev):
+        rc = lib().ardiff_pages_extend(R, page, table.shape[1], length.data_ptr(), add.data_ptr(), table.data_ptr(),
+                                       free_pages.data_ptr(), free_pages.shape[0], free_count.data_ptr(), tokens,
+                                       slot.data_ptr(), _ptr(position), _ptr(request), made[0].data_ptr(),
+                                       made[1].data_ptr(), made[2].data_ptr(), made[3].data_ptr(), _stream_ptr(stream))
+    _check(rc, "ardiff_pages_extend")
+    return tuple(made)
+
+
+def ardiff_pages_truncate(length, target, table, free_pages, free_count, page: int, new_free_count=None, status=None,
+                          stream=None):
+    """Leaves request r of a paged cache its first target[r] tokens; the pages that none of them needs go back to the free list
+    (in place). int32 CUDA tensors; new_free_count may be `free_count`. Returns (new_free_count [1], status [1])."""
+    import torch
+    dev, R = length.device, length.shape[0]
+    assert length.is_cuda and table.dim() == 2
+    for t, shape in ((length, (R,)), (target, (R,)), (table, (R, table.shape[1])), (free_count, (1,))):
+        _int32(t, shape, dev)
+    _int32(free_pages, (free_pages.shape[0],), dev)
+    made = []
+    for t in (new_free_count, status):
+        if t is None:
+            t = torch.empty((1,), dtype=torch.int32, device=dev)
+        else:
+            _int32(t, (1,), dev)
+        made.append(t)
+    with _on(dev):
+        rc = lib().ardiff_pages_truncate(R, page, table.shape[1], length.data_ptr(), target.data_ptr(), table.data_ptr(),
+                                         free_pages.data_ptr(), free_pages.shape[0], free_count.data_ptr(),
+                                         made[0].data_ptr(), made[1].data_ptr(), _stream_ptr(stream))
+    _check(rc, "ardiff_pages_truncate")
+    return tuple(made)
+
+
+def _distill_args(logits, teacher, ids):
+    assert logits.is_cuda and logits.dim() == 2 and teacher.dim() == 2
+    assert teacher.is_contiguous() and teacher.device == logits.device and teacher.shape[0] == logits.shape[0]
+    _int32(ids, teacher.shape, logits.device)
+    return (logits.data_ptr(), _dtype(logits), logits.shape[0], logits.shape[1], _rows(logits), teacher.data_ptr(),
+            _dtype(teacher), ids.data_ptr(), teacher.shape[1])
+
+
+def _float_rows(t, shape, dev):
+    import torch
+    if t is None:
+        return torch.empty(shape, dtype=torch.float32, device=dev)
+    assert t.dtype == torch.float32 and t.device == dev and t.is_contiguous() and t.shape == shape, (t.dtype, t.shape, shape)
+    return t
+
+
+def _grad_rows(grad, logits):
+    import torch
+    if grad is None:
+        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    assert grad.dtype == logits.dtype and grad.device == logits.device and grad.shape == logits.shape
+    return grad
+
+
+def ardiff_distill_topk(logits, teacher, ids, temperature: float = 1.0, loss=None, stats=None, stream=None):
+    """Divergence of every row of a student's logits [n, V] (bf16, f16 or f32, rows contiguous) from the softmax of the teacher's
+    entries (teacher [n, k] at ids [n, k] int32; ids outside 0 .. V - 1 are no entries).
+    Returns (loss f32 [n], stats f32 [n, 2]: what ardiff_distill_topk_backward needs of the rows)."""
+    args = _distill_args(logits, teacher, ids)
+    n, dev = logits.shape[0], logits.device
+    loss, stats = _float_rows(loss, (n,), dev), _float_rows(stats, (n, 2), dev)
+    with _on(dev):
+        rc = lib().ardiff_distill_topk(*args, temperature, loss.data_ptr(), stats.data_ptr(), _stream_ptr(stream))
+    _check(rc, "ardiff_distill_topk")
+    return loss, stats
+
+
+def ardiff_distill_topk_backward(logits, teacher, ids, stats, weight, temperature: float = 1.0, grad=None, stream=None):
+    """Gradient of sum(weight * loss) with respect to the logits, from the stats that ardiff_distill_topk gave for the same
+    inputs; in the logits' type. `grad` may be `logits`."""
+    args = _distill_args(logits, teacher, ids)
+    n, dev = logits.shape[0], logits.device
+    assert stats is not None and weight is not None
+    grad = _grad_rows(grad, logits)
+    stats, weight = _float_rows(stats, (n, 2), dev), _float_rows(weight, (n,), dev)
+    with _on(dev):
+        rc = lib().ardiff_distill_topk_backward(*args, temperature, stats.data_ptr(), weight.data_ptr(), grad.data_ptr(),
+                                                _rows(grad), _stream_ptr(stream))
+    _check(rc, "ardiff_distill_topk_backward")
+    return grad
+
+
+def ardiff_distill_topk_step(logits, teacher, ids, weight, temperature: float = 1.0, loss=None, stats=None, grad=None,
+                             stream=None):
+    """Loss, stats and the gradient of sum(weight * loss) in one pass. `grad` may be `logits`. Returns (loss, stats, grad)."""
+    args = _distill_args(logits, teacher, ids)
+    n, dev = logits.shape[0], logits.device
+    assert weight is not None
+    grad = _grad_rows(grad, logits)
+    loss, stats = _float_rows(loss, (n,), dev), _float_rows(stats, (n, 2), dev)
+    weight = _float_rows(weight, (n,), dev)
+    with _on(dev):
+        rc = lib().ardiff_distill_topk_step(*args, temperature, weight.data_ptr(), loss.data_ptr(), stats.data_ptr(),
+                                            grad.data_ptr(), _rows(grad), _stream_ptr(stream))
+    _check(rc, "ardiff_distill_topk_step")
+    return loss, stats, grad
 
 
 GATE_NOALLOC_MAX_BLOCKS = 1024

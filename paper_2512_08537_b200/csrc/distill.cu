@@ -1,0 +1,316 @@
+// Distillation of a draft model from the largest logits that its target kept: for every row, with q the softmax of the
+// teacher's entries over the temperature and p the softmax of the student's whole row over it,
+//   loss = sum_j q_j (ln q_j - ln p[id_j]),      d loss / d x_i = (p_i [row has entries] - sum_{j: id_j = i} q_j) / T.
+// Statistics kept for a backward pass are the row's largest value m and ln Z, Z = sum_i exp((x_i - m) / T): p_i is formed from
+// x_i - m and not from x_i / T minus one rounded number, so that large logits cost no accuracy.
+//
+// A row belongs to a cluster of one to eight CTAs, a contiguous part each; their (m, Z) meet through distributed shared memory.
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <atomic>
+
+#include "../../include/ardiff.h"
+#include "common.cuh"
+#include "rows.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+enum Mode { FORWARD, STEP, BACKWARD };
+
+struct Args {
+    const void* x;
+    const void* teacher;
+    const int32_t* ids;
+    const float* weight;         // STEP, BACKWARD
+    float* loss;                 // FORWARD, STEP
+    float* stats;                // out, or in for BACKWARD
+    void* grad;                  // STEP, BACKWARD
+    int64_t ld, ld_grad;
+    int32_t teacher_type, V, k, parts;
+    float inv_t;                 // 1 / T
+};
+
+__device__ __forceinline__ float load_teacher(const Args& a, int64_t i) {
+    if (a.teacher_type == ARDIFF_F32) return static_cast<const float*>(a.teacher)[i];
+    if (a.teacher_type == ARDIFF_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(a.teacher)[i]);
+    return __half2float(static_cast<const __half*>(a.teacher)[i]);
+}
+
+struct MaxSum { float m, z; };   // largest value, sum of exp((x - m) / T)
+
+// c = log2(e) / T. -inf is the largest value of nothing: its sum is 0 and it counts for nothing beside another.
+__device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, float c) {
+    const float m = fmaxf(a.m, b.m);
+    const float at = m == -INFINITY ? 0.f : m;
+    return MaxSum{m, a.z * ardiff::ex2((a.m - at) * c) + b.z * ardiff::ex2((b.m - at) * c)};
+}
+
+template <typename T>
+__device__ __forceinline__ void take(MaxSum& s, const uint4& p, float c) {
+    constexpr int N = ardiff::Piece<T>::N;
+    float v[N];
+    ardiff::unpack(p, v, T());
+    float top = v[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+    if (top > s.m) {
+        s.z *= ardiff::ex2((s.m - top) * c);       // from -inf: 0
+        s.m = top;
+    }
+    const float at = s.m == -INFINITY ? 0.f : s.m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s.z += ardiff::ex2((v[i] - at) * c);
+}
+
+template <typename T, int MODE>
+__global__ void __launch_bounds__(kThreads) distill_kernel(const Args a) {
+    using ardiff::Row;
+    constexpr int N = ardiff::Piece<T>::N;
+    extern __shared__ __align__(16) unsigned char smem[];
+    float* s_q = reinterpret_cast<float*>(smem);             // [k] teacher's logits, then probabilities
+    float* s_x = s_q + a.k;                                  // [k] the student's logits there
+    int32_t* s_id = reinterpret_cast<int32_t*>(s_x + a.k);   // [k] -1: no entry
+    __shared__ MaxSum s_part[kWarps];
+    __shared__ MaxSum s_own;
+    __shared__ float s_loss[kWarps];
+    __shared__ float s_top, s_ln;                            // of the teacher
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t row = blockIdx.x / a.parts;
+    const int part = blockIdx.x % a.parts;
+    const float c = a.inv_t * 1.4426950408889634f;
+    const Row<T> x(static_cast<const T*>(a.x) + row * a.ld, a.V);
+    const int per = (x.pieces + a.parts - 1) / a.parts;
+    const int p0 = min(x.pieces, part * per), p1 = min(x.pieces, p0 + per);
+    // the values of this part, as a range: what is before the first piece goes with the first part, what is behind with the last
+    const int v0 = part == 0 ? 0 : x.lead + p0 * N, v1 = part == a.parts - 1 ? a.V : x.lead + p1 * N;
+    T* grad = MODE == FORWARD ? nullptr : static_cast<T*>(a.grad) + row * a.ld_grad;
+
+    bool some = false;
+    for (int j = tid; j < a.k; j += kThreads) {
+        int id = a.ids[row * a.k + j];
+        const float t = load_teacher(a, row * a.k + j);
+        if (id < 0 || id >= a.V || t == -INFINITY) id = -1;
+        s_id[j] = id;
+        s_q[j] = t;
+        s_x[j] = id >= 0 && (MODE != BACKWARD || (id >= v0 && id < v1)) ? ardiff::to_float(x.x[id]) : 0.f;
+        some |= id >= 0;
+    }
+    some = __syncthreads_or(some);
+    if (!some) {                                             // nothing to learn from this row: it is not read
+        if (MODE != FORWARD)
+            for (int i = v0 + tid; i < v1; i += kThreads) grad[i] = ardiff::from_float<T>(0.f);
+        if (MODE != BACKWARD && part == 0 && tid == 0) {
+            a.loss[row] = 0.f;
+            a.stats[2 * row] = 0.f;
+            a.stats[2 * row + 1] = 0.f;
+        }
+        return;                                              // every CTA of the cluster alike
+    }
+    if (warp == 0) {
+        float top = -INFINITY;
+        for (int j = lane; j < a.k; j += 32)
+            if (s_id[j] >= 0) top = s_q[j] > top || s_q[j] != s_q[j] ? s_q[j] : top;     // a NaN stays
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const float b = __shfl_xor_sync(0xffffffffu, top, o);
+            top = b > top || b != b ? b : top;
+        }
+        float sum = 0.f;
+        for (int j = lane; j < a.k; j += 32) {
+            const float e = s_id[j] >= 0 ? expf((s_q[j] - top) * a.inv_t) : 0.f;
+            sum += e;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) {
+            s_top = top;
+            s_ln = logf(sum);
+        }
+    }
+
+    const uint4* body = x.body();
+    float m, ln_z, scale;
+    if (MODE != BACKWARD) {
+        MaxSum s{-INFINITY, 0.f};
+        int p = p0 + tid;
+        for (; p + 3 * kThreads < p1; p += 4 * kThreads) {
+            uint4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __ldg(body + p + i * kThreads);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) take<T>(s, v[i], c);
+        }
+        for (; p < p1; p += kThreads) take<T>(s, __ldg(body + p), c);
+        const int edge = part == 0 && tid < x.lead ? tid : part == a.parts - 1 && x.tail() + tid < a.V ? x.tail() + tid : -1;
+        const int both = part == 0 && tid < x.lead && part == a.parts - 1 && x.tail() + tid < a.V ? x.tail() + tid : -1;
+        if (edge >= 0) {
+            const float v = ardiff::to_float(x.x[edge]);
+            s = merge(s, MaxSum{v, 1.f}, c);
+        }
+        if (both >= 0) {
+            const float v = ardiff::to_float(x.x[both]);
+            s = merge(s, MaxSum{v, 1.f}, c);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            s = merge(s, MaxSum{__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.z, o)}, c);
+        if (lane == 0) s_part[warp] = s;
+        __syncthreads();
+        s = s_part[0];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) s = merge(s, s_part[w], c);
+        if (a.parts > 1) {
+            cg::cluster_group cl = cg::this_cluster();
+            if (tid == 0) s_own = s;
+            cl.sync();
+            s = *cl.map_shared_rank(&s_own, 0);
+            for (int r = 1; r < a.parts; ++r) s = merge(s, *cl.map_shared_rank(&s_own, r), c);
+        }
+        m = s.m;
+        if (m == -INFINITY || s.z != s.z) m = s.z = NAN;     // a row of nothing, or with NaN or +inf, has no softmax
+        ln_z = logf(s.z);
+        if (MODE == STEP) scale = a.weight[row] * a.inv_t / s.z;
+    } else {
+        m = a.stats[2 * row];
+        ln_z = a.stats[2 * row + 1];
+        scale = a.weight[row] * a.inv_t;
+        __syncthreads();                                     // s_top, s_ln
+    }
+    const float top = s_top, ln = s_ln;
+    // the teacher's probabilities; this row's loss
+    float loss = 0.f;
+    for (int j = tid; j < a.k; j += kThreads) {
+        const float t = (s_q[j] - top) * a.inv_t - ln;
+        const float q = s_id[j] >= 0 ? expf(t) : 0.f;
+        if (MODE != BACKWARD && (q > 0.f || q != q)) loss += q * (t - ((s_x[j] - m) * a.inv_t - ln_z));
+        s_q[j] = q;
+    }
+    if (MODE != BACKWARD) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
+        if (lane == 0) s_loss[warp] = loss;
+    }
+    __syncthreads();
+    if (MODE != BACKWARD && part == 0 && tid == 0) {
+        float all = s_loss[0];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) all += s_loss[w];
+        a.loss[row] = all;
+        a.stats[2 * row] = m;
+        a.stats[2 * row + 1] = ln_z;
+    }
+    if (MODE != FORWARD) {
+        const float l2 = MODE == BACKWARD ? ln_z * 1.4426950408889634f : 0.f;
+        auto prob = [&](float v) { return ardiff::ex2((v - m) * c - l2); };
+        T* out = grad + x.lead;
+        const bool wide = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
+        for (int p = p0 + tid; p < p1; p += kThreads) {
+            float v[N];
+            ardiff::unpack(__ldcg(body + p), v, T());        // (may lie where grad does)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = prob(v[i]) * scale;
+            if (wide) {
+                reinterpret_cast<uint4*>(out)[p] = ardiff::pack(v, T());
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) out[p * N + i] = ardiff::from_float<T>(v[i]);
+            }
+        }
+        if (part == 0 && tid < x.lead) grad[tid] = ardiff::from_float<T>(prob(ardiff::to_float(x.x[tid])) * scale);
+        if (part == a.parts - 1 && x.tail() + tid < a.V) {
+            const int i = x.tail() + tid;
+            grad[i] = ardiff::from_float<T>(prob(ardiff::to_float(x.x[i])) * scale);
+        }
+        __syncthreads();
+        // the entries' places once more, with the teacher's share in the sum before it is rounded; an id that occurs again has
+        // the sum of its shares in order of the entries, and every one of them writes the same
+        const float share = a.weight[row] * a.inv_t;
+        for (int j = tid; j < a.k; j += kThreads) {
+            const int id = s_id[j];
+            if (id < v0 || id >= v1) continue;
+            float q = 0.f;
+            for (int i = 0; i < a.k; ++i) q += s_id[i] == id ? s_q[i] : 0.f;
+            grad[id] = ardiff::from_float<T>(prob(s_x[j]) * scale - q * share);
+        }
+    }
+    if (MODE != BACKWARD && a.parts > 1) cg::this_cluster().sync();      // a CTA leaves when its part has been read
+}
+
+template <typename T, int MODE>
+int launch(const Args& a, int64_t n, cudaStream_t st) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = MODE == BACKWARD ? 1 : a.parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(n * a.parts)); cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)a.k * 12; cfg.stream = st;
+    cfg.attrs = at; cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, distill_kernel<T, MODE>, a);
+    ardiff::set_launch_count(1);
+    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+}
+
+template <int MODE>
+int dispatch(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld, const void* teacher, int32_t teacher_type,
+             const int32_t* ids, int32_t k, float temperature, const float* weight, float* loss, float* stats, void* grad,
+             int64_t ld_grad, void* stream) {
+    const int size = ardiff::value_size(dtype);
+    if (!size || !ardiff::value_size(teacher_type)) return ARDIFF_ERR_UNSUPPORTED;
+    if (n < 0 || n >= (int64_t)1 << 28 || V < 1 || V > ARDIFF_DISTILL_MAX_V || k < 1 || k > ARDIFF_DISTILL_MAX_K || ld < V)
+        return ARDIFF_ERR_SHAPE;
+    if (MODE != FORWARD && ld_grad < V) return ARDIFF_ERR_SHAPE;
+    if (!(temperature > 0.f) || !isfinite(1.0f / temperature) || !(1.0f / temperature > 0.f)) return ARDIFF_ERR_SHAPE;
+    if (n == 0) {
+        ardiff::set_launch_count(0);
+        return ARDIFF_OK;
+    }
+    if (!logits || !teacher || !ids || !stats) return ARDIFF_ERR_NULL;
+    if (MODE != BACKWARD && !loss) return ARDIFF_ERR_NULL;
+    if (MODE != FORWARD && (!weight || !grad)) return ARDIFF_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(grad)) % size) return ARDIFF_ERR_ALIGN;
+    Args a;
+    memset(&a, 0, sizeof(a));
+    a.x = logits; a.teacher = teacher; a.ids = ids; a.weight = weight; a.loss = loss; a.stats = stats; a.grad = grad;
+    a.ld = ld; a.ld_grad = ld_grad; a.teacher_type = teacher_type; a.V = V; a.k = k; a.inv_t = 1.0f / temperature;
+    // more CTAs a row while there are SMs without one and each keeps two pieces a thread
+    a.parts = 1;
+    while (a.parts < 8 && n * a.parts < 148 && (int64_t)V * size / 16 >= (int64_t)4 * kThreads * a.parts) a.parts *= 2;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == ARDIFF_F32) return launch<float, MODE>(a, n, st);
+    if (dtype == ARDIFF_F16) return launch<__half, MODE>(a, n, st);
+    return launch<__nv_bfloat16, MODE>(a, n, st);
+}
+
+}  // namespace
+
+extern "C" int ardiff_distill_topk(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld, const void* teacher,
+                                   int32_t teacher_dtype, const int32_t* ids, int32_t k, float temperature, float* loss,
+                                   float* stats, void* stream) {
+    return dispatch<FORWARD>(logits, dtype, n, V, ld, teacher, teacher_dtype, ids, k, temperature, nullptr, loss, stats,
+                             nullptr, 0, stream);
+}
+
+extern "C" int ardiff_distill_topk_backward(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld,
+                                            const void* teacher, int32_t teacher_dtype, const int32_t* ids, int32_t k,
+                                            float temperature, const float* stats, const float* weight, void* grad,
+                                            int64_t ld_grad, void* stream) {
+    return dispatch<BACKWARD>(logits, dtype, n, V, ld, teacher, teacher_dtype, ids, k, temperature, weight, nullptr,
+                              const_cast<float*>(stats), grad, ld_grad, stream);
+}
+
+extern "C" int ardiff_distill_topk_step(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld,
+                                        const void* teacher, int32_t teacher_dtype, const int32_t* ids, int32_t k,
+                                        float temperature, const float* weight, float* loss, float* stats, void* grad,
+                                        int64_t ld_grad, void* stream) {
+    return dispatch<STEP>(logits, dtype, n, V, ld, teacher, teacher_dtype, ids, k, temperature, weight, loss, stats, grad,
+                          ld_grad, stream);
+}

@@ -1,0 +1,79 @@
+"""Refusals of the language-model operators: every one is made before anything is launched, so they need no GPU."""
+import math
+
+import pytest
+
+import paper_2512_08537_b200 as ardiff
+
+NULL, SHAPE, ALIGN, UNSUPPORTED = (ardiff.ARDIFF_ERR_NULL, ardiff.ARDIFF_ERR_SHAPE, ardiff.ARDIFF_ERR_ALIGN,
+                                   ardiff.ARDIFF_ERR_UNSUPPORTED)
+P = 4096                                   # an address that nothing is read from
+
+
+def extend(**kw):
+    a = dict(requests=4, page=16, width=8, length=P, add=P, table=P, free_pages=P, free_capacity=32, free_count=P, max_tokens=64,
+             slot=P, position=P, request=P, offset=P, new_length=P, new_free_count=P, status=P, stream=None)
+    assert set(kw) <= set(a)
+    return ardiff.lib().ardiff_pages_extend(*{**a, **kw}.values())
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(requests=-1), SHAPE), (dict(requests=(1 << 20) + 1), SHAPE), (dict(page=0), SHAPE), (dict(width=-1), SHAPE),
+    (dict(free_capacity=-1), SHAPE), (dict(free_capacity=1 << 31), SHAPE), (dict(max_tokens=-1), SHAPE),
+    (dict(max_tokens=1 << 31), SHAPE)] +
+    [(dict([(name, None)]), NULL) for name in ("length", "add", "table", "free_pages", "free_count", "slot", "offset",
+                                               "new_length", "new_free_count", "status")])
+def test_pages_extend_refuses(kw, code):
+    assert extend(**kw) == code
+
+
+def truncate(**kw):
+    a = dict(requests=4, page=16, width=8, length=P, target=P, table=P, free_pages=P, free_capacity=32, free_count=P,
+             new_free_count=P, status=P, stream=None)
+    assert set(kw) <= set(a)
+    return ardiff.lib().ardiff_pages_truncate(*{**a, **kw}.values())
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(requests=-1), SHAPE), (dict(requests=(1 << 20) + 1), SHAPE), (dict(page=0), SHAPE), (dict(page=-16), SHAPE),
+    (dict(width=-1), SHAPE), (dict(free_capacity=-1), SHAPE), (dict(free_capacity=1 << 31), SHAPE)] +
+    [(dict([(name, None)]), NULL) for name in ("length", "target", "table", "free_pages", "free_count", "new_free_count",
+                                               "status")])
+def test_pages_truncate_refuses(kw, code):
+    assert truncate(**kw) == code
+
+
+def distill(part, **kw):
+    a = dict(logits=P, dtype=ardiff.ARDIFF_BF16, n=4, V=100, ld=100, teacher=P, teacher_dtype=ardiff.ARDIFF_F32, ids=P, k=8,
+             temperature=1.0)
+    a.update({"": dict(loss=P, stats=P), "_backward": dict(stats=P, weight=P, grad=P, ld_grad=100),
+              "_step": dict(weight=P, loss=P, stats=P, grad=P, ld_grad=100)}[part])
+    a["stream"] = None
+    assert set(kw) <= set(a)
+    return getattr(ardiff.lib(), "ardiff_distill_topk" + part)(*{**a, **kw}.values())
+
+
+@pytest.mark.parametrize("part", ["", "_backward", "_step"])
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=-1), SHAPE), (dict(n=1 << 28), SHAPE), (dict(V=0), SHAPE), (dict(V=(1 << 24) + 1, ld=1 << 25), SHAPE),
+    (dict(ld=99), SHAPE), (dict(k=0), SHAPE), (dict(k=1025), SHAPE), (dict(temperature=0.0), SHAPE),
+    (dict(temperature=-1.0), SHAPE), (dict(temperature=math.nan), SHAPE), (dict(temperature=math.inf), SHAPE),
+    (dict(temperature=1e-39), SHAPE), (dict(dtype=3), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED),
+    (dict(teacher_dtype=7), UNSUPPORTED), (dict(logits=P + 1), ALIGN),
+    (dict(dtype=ardiff.ARDIFF_F32, logits=P + 2), ALIGN), (dict(logits=None), NULL), (dict(teacher=None), NULL),
+    (dict(ids=None), NULL), (dict(stats=None), NULL)])
+def test_distill_refuses(part, kw, code):
+    assert distill(part, **kw) == code
+
+
+@pytest.mark.parametrize("part,kw,code", [
+    ("", dict(loss=None), NULL), ("_step", dict(loss=None), NULL), ("_step", dict(weight=None), NULL),
+    ("_step", dict(grad=None), NULL), ("_backward", dict(weight=None), NULL), ("_backward", dict(grad=None), NULL),
+    ("_step", dict(ld_grad=99), SHAPE), ("_backward", dict(ld_grad=99), SHAPE), ("_step", dict(grad=P + 1), ALIGN)])
+def test_distill_refuses_what_one_part_needs(part, kw, code):
+    assert distill(part, **kw) == code
+
+
+@pytest.mark.parametrize("part", ["", "_backward", "_step"])
+def test_distill_of_no_rows_is_nothing(part):
+    assert distill(part, n=0, logits=None, teacher=None, ids=None, stats=None) == ardiff.ARDIFF_OK
