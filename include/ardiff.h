@@ -35,6 +35,11 @@ extern "C" {
 #define ARDIFF_ERR_TIMEOUT (-6)     /* a bounded device-side wait ran out (results invalid)  */
 #define ARDIFF_ERR_NOMEM (-7)       /* an allocation inside a create call failed             */
 
+/* types of the rows of logits that the draft model's calls take */
+#define ARDIFF_BF16 0
+#define ARDIFF_F16 1
+#define ARDIFF_F32 2
+
 const char* ardiff_strerror(int code);
 /* major*10000 + minor*100 + patch */
 int ardiff_version(void);
@@ -383,6 +388,37 @@ int ardiff_pipeline_wait(ardiff_pipeline* pipeline, int32_t slot);
 int ardiff_pipeline_join(ardiff_pipeline* pipeline, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * The draft's (or target's) next tokens from rows of logits. (Algorithm 1 draws every draft token x_i from q_i; its discrete
+ * tokens, e.g. the text around an image's tokens, come from logits like these. logprob is ln q_i, of the ratio
+ * p_i / q_i that ardiff_accept_prefix takes.)
+ *
+ * Operation, row by row, with w_i = exp((logits_i - max) / T) and the order "larger logit first, lower index first where
+ * equal":
+ *   T == 0          token = the first in the order; logprob 0. The other settings mean nothing
+ *   top_k           the first top_k of the order are kept (<= 0 or >= V: all)
+ *   top_p           of these the shortest prefix whose sum of w reaches top_p times theirs, at least one (>= 1: all)
+ *   min_p           of these the ones with w >= min_p (<= 0: all; above 1 as 1)
+ *   token           the kept one of the lowest index i at which the sum of w over the kept ones up to i is above u times the
+ *                   sum over all kept ones;  logprob = ln(w_token / that sum)
+ * Masked logits (-inf) are never drawn. A row of logits with NaN or +inf or of only -inf, a temperature that is negative, NaN
+ * or inf, a NaN in top_p or min_p, or u outside 0 <= u < 1, gives token -1 and logprob NaN.
+ * Weights and sums are fp64 where they decide between tokens, in an order fixed by V, n and the type: equal calls give
+ * equal bits.
+ *
+ *   logits   dev  [n][V], rows `ld` >= V values apart, of type dtype (ARDIFF_BF16, ARDIFF_F16 or ARDIFF_F32), at any
+ *            multiple of its size; read once
+ *   n        0 <= n < 2^28;  1 <= V <= ARDIFF_SAMPLE_MAX_V
+ *   u        dev float [n]: uniform numbers
+ *   temperature, top_p, min_p  dev float [n], top_k dev int32 [n], each or NULL: every row's own settings (NULL: 1, 1, 0, 0)
+ *   token    dev int32 [n] out;  logprob  dev float [n] out
+ * Nothing is allocated or kept; calls on different streams are independent.
+ * ------------------------------------------------------------------------------------- */
+#define ARDIFF_SAMPLE_MAX_V (1 << 18)
+int ardiff_sample_tokens(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld, const float* u,
+                         const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                         int32_t* token, float* logprob, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Pages of a cache, kept on the device. (The paper's Algorithm 1 lets a draft grow token by token and cuts it
  * where the early stop or the verification ends it; with an attention cache in pages this is what has to happen to
  * the cache around it. No call reads or writes the cache itself.)
@@ -456,9 +492,6 @@ int ardiff_pages_truncate(int32_t requests, int32_t page, int32_t width, const i
  * differentiation asks for it; ardiff_distill_topk_step all three at once, for rows whose weight is known.
  * Arithmetic is fp32 (fp32 sums in a fixed order: equal calls give equal bits); a gradient is rounded once.
  * ------------------------------------------------------------------------------------- */
-#define ARDIFF_BF16 0
-#define ARDIFF_F16 1
-#define ARDIFF_F32 2
 #define ARDIFF_DISTILL_MAX_V (1 << 24)
 #define ARDIFF_DISTILL_MAX_K 1024
 int ardiff_distill_topk(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld, const void* teacher,

@@ -107,6 +107,8 @@ def lib() -> ctypes.CDLL:
         L.ardiff_pipeline_wait.argtypes = [vp, i32]
         L.ardiff_pipeline_join.restype = ctypes.c_int
         L.ardiff_pipeline_join.argtypes = [vp, vp]
+        L.ardiff_sample_tokens.restype = ctypes.c_int
+        L.ardiff_sample_tokens.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp]
         L.ardiff_pages_extend.restype = ctypes.c_int
         L.ardiff_pages_extend.argtypes = [i32, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
         L.ardiff_pages_truncate.restype = ctypes.c_int
@@ -288,6 +290,32 @@ def _rows(x) -> int:
 def _int32(t, shape, dev):
     import torch
     assert t.dtype == torch.int32 and t.device == dev and t.is_contiguous() and t.shape == shape, (t.dtype, t.shape, shape)
+
+
+def ardiff_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None, stream=None):
+    """The next token of every row of logits [n, V] (bf16, f16 or f32 CUDA tensor, rows contiguous) by the uniform numbers u
+    (f32 [n], 0 <= u < 1). temperature, top_p, min_p (f32 [n]) and top_k (int32 [n]) are every row's own, or None (off).
+    Returns (token int32 [n], logprob f32 [n]); -1 and NaN for rows that have no softmax or bad settings."""
+    import torch
+    n, V = logits.shape
+    dev = logits.device
+    assert logits.is_cuda
+    for t in (u, temperature, top_p, min_p):
+        if t is not None:
+            assert t.dtype == torch.float32 and t.device == dev and t.is_contiguous() and t.shape == (n,)
+    if top_k is not None:
+        _int32(top_k, (n,), dev)
+    if token is None:
+        token = torch.empty((n,), dtype=torch.int32, device=dev)
+    else:
+        _int32(token, (n,), dev)
+    logprob = _float_rows(logprob, (n,), dev)
+    with _on(dev):
+        rc = lib().ardiff_sample_tokens(logits.data_ptr(), _dtype(logits), n, V, _rows(logits), u.data_ptr(), _ptr(temperature),
+                                        _ptr(top_k), _ptr(top_p), _ptr(min_p), token.data_ptr(), logprob.data_ptr(),
+                                        _stream_ptr(stream))
+    _check(rc, "ardiff_sample_tokens")
+    return token, logprob
 
 
 def ardiff_pages_extend(length, add, table, free_pages, free_count, page: int, slot, position=None, request=None, offset=None,

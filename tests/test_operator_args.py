@@ -77,3 +77,23 @@ def test_distill_refuses_what_one_part_needs(part, kw, code):
 @pytest.mark.parametrize("part", ["", "_backward", "_step"])
 def test_distill_of_no_rows_is_nothing(part):
     assert distill(part, n=0, logits=None, teacher=None, ids=None, stats=None) == ardiff.ARDIFF_OK
+
+
+def sample(**kw):
+    a = dict(logits=P, dtype=ardiff.ARDIFF_BF16, n=4, V=100, ld=100, u=P, temperature=P, top_k=P, top_p=P, min_p=P, token=P,
+             logprob=P, stream=None)
+    assert set(kw) <= set(a)
+    return ardiff.lib().ardiff_sample_tokens(*{**a, **kw}.values())
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=-1), SHAPE), (dict(n=1 << 28), SHAPE), (dict(V=0), SHAPE), (dict(V=(1 << 18) + 1, ld=1 << 19), SHAPE),
+    (dict(ld=99), SHAPE), (dict(dtype=3), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED), (dict(logits=P + 1), ALIGN),
+    (dict(dtype=ardiff.ARDIFF_F32, logits=P + 2), ALIGN), (dict(logits=None), NULL), (dict(u=None), NULL),
+    (dict(token=None), NULL), (dict(logprob=None), NULL)])
+def test_sample_refuses(kw, code):
+    assert sample(**kw) == code
+
+
+def test_sample_of_no_rows_is_nothing():
+    assert sample(n=0, logits=None, u=None, token=None, logprob=None) == ardiff.ARDIFF_OK
