@@ -40,6 +40,33 @@ __device__ __forceinline__ void unpack(const uint4& p, float (&v)[8], __half) {
         v[2 * i + 1] = f.y;
     }
 }
+// The largest value of a piece; NaN if one is.
+__device__ __forceinline__ float piece_max(const uint4& p, float) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(p.x)), "f"(__uint_as_float(p.y)));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(r) : "f"(__uint_as_float(p.z)));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(r) : "f"(__uint_as_float(p.w)));
+    return r;
+}
+__device__ __forceinline__ float piece_max(const uint4& p, __nv_bfloat16) {
+    uint32_t a, b;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(p.x), "r"(p.y));
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(p.z), "r"(p.w));
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(a << 16)), "f"(__uint_as_float(a & 0xffff0000u)));
+    return r;
+}
+__device__ __forceinline__ float piece_max(const uint4& p, __half) {
+    uint32_t a, b;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(a) : "r"(p.x), "r"(p.y));
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(b) : "r"(p.z), "r"(p.w));
+    asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&a));
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(f.x), "f"(f.y));
+    return r;
+}
 __device__ __forceinline__ uint4 pack(const float (&v)[4], float) {
     return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
 }

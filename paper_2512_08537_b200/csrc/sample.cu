@@ -24,8 +24,6 @@
 #include <stdint.h>
 #include <string.h>
 
-#include <atomic>
-
 #include "../../include/ardiff.h"
 #include "common.cuh"
 #include "rows.cuh"
@@ -34,10 +32,14 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kBins = 2 * kThreads;      // of a histogram, two a thread
-constexpr int kList = 2 * kThreads;      // logits that the first CTA sorts, two a thread
+constexpr int kGroups = 4;               // of a thread's pieces, each with its largest logit kept
+constexpr int kBins = 4 * kThreads;      // of a histogram, four a thread
+constexpr int kCopies = 4;               // of a histogram over all elements: neighbouring lanes count in different ones
+constexpr int kList = 4 * kThreads;      // logits that the first CTA sorts, four a thread
+constexpr int kEach = 4;                 // list entries, bins a thread
+constexpr int kSegments = 4 * kWarps;    // of a CTA's part, four a warp
 constexpr int kMaxParts = 8;
 constexpr double kFar = -100.0;          // weights below 2^kFar count as nothing: all of a row's add up to less than 2^-75 of its sum
 
@@ -52,17 +54,17 @@ struct Args {
 };
 
 struct Shared {
-    float thread_max[kThreads];
+    float top[kGroups][kThreads];        // the groups' largest logits
     float warp_max[kWarps];
-    int warp_first[kWarps];
-    double seg[2][kWarps];               // sums of the warps' segments; two, so that one may still be read by another CTA
+    double seg[2][kSegments];            // sums of the segments; two, so that one may still be read by another CTA
     double scan[kWarps];
     unsigned uscan[kWarps];
     double total, before;
     int owner;                           // segment in which a sum passes its target, of all CTAs'
     int found, last;
     float cta_max;
-    int cta_first;
+    int first;                           // lowest index of the part's largest logit
+    unsigned groups;                     // entries of `group`
     unsigned count;                      // entries of `list` (of the first CTA)
     unsigned kmin, kmax;
     int pick_first, pick_last;
@@ -71,9 +73,10 @@ struct Shared {
     unsigned cut_key;
     int cut_index;
     double mass_above, mass_in;
+    unsigned short group[kGroups * kThreads];
     unsigned long long list[kList];
     union {
-        unsigned hist[kBins];
+        unsigned hist[kBins * kCopies];
         double w[kList];
     };
 };
@@ -126,9 +129,10 @@ __device__ __noinline__ double pow2_far(double d, double a) { return d == -INFIN
 template <typename T>
 struct Part {                            // this CTA's part of its row
     static constexpr int N = ardiff::Piece<T>::N;
-    const uint4* piece;                  // in shared memory; -inf in the places outside the row
-    int pieces, segment;                 // pieces, and pieces a warp
+    const T* x;                          // the row
+    int pieces, segment;                 // pieces (aligned, 16 bytes), and pieces a segment
     int first;                           // index of the part's first value in the row (negative in front of the row)
+    int whole0, whole1;                  // pieces that lie in the row as a whole
     int rank, parts, V;
     float m;
     double a;                            // log2(e) / T
@@ -136,10 +140,10 @@ struct Part {                            // this CTA's part of its row
     bool tiny;                           // u = 0
     Shared* s;
 
-    __device__ __forceinline__ double weight(float x) const { return pow2((double)x - (double)m, a); }
-    __device__ __forceinline__ double weight_drawn(float x) const {        // of a draw that may end at any weight above 0
-        const double w = weight(x);
-        return tiny && w == 0.0 ? pow2_far((double)x - (double)m, a) : w;
+    __device__ __forceinline__ double weight(float v) const { return pow2((double)v - (double)m, a); }
+    __device__ __forceinline__ double weight_drawn(float v) const {        // of a draw that may end at any weight above 0
+        const double w = weight(v);
+        return tiny && w == 0.0 ? pow2_far((double)v - (double)m, a) : w;
     }
     __device__ __forceinline__ void sync() const {
         if (parts > 1) cg::this_cluster().sync(); else __syncthreads();
@@ -147,15 +151,56 @@ struct Part {                            // this CTA's part of its row
     template <typename U> __device__ __forceinline__ U* at(U* p, int r) const {
         return parts > 1 ? cg::this_cluster().map_shared_rank(p, r) : p;
     }
-    // f(value, index) for every value of the calling warp's segment, lanes taking pieces in turn
+    // a piece at either end of the row: -inf in the places outside it
+    __device__ __noinline__ uint4 edge(int p) const {
+        float v[N];
+        const int e = first + p * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = e + i >= 0 && e + i < V ? ardiff::to_float(x[e + i]) : -INFINITY;
+        return ardiff::pack(v, T());
+    }
+    // f(values, piece) for pieces begin, begin + step, ... below end; four loads at a time
+    template <typename F> __device__ __forceinline__ void scan(int begin, int end, int step, F&& f) const {
+        const uint4* base = reinterpret_cast<const uint4*>(x + first);     // (aligned; pieces whole0 .. whole1 - 1 are read)
+        auto one = [&](uint4 q, int p) {
+            if (p < whole0 || p >= whole1) q = edge(p);
+            float v[N];
+            ardiff::unpack(q, v, T());
+            f(v, p);
+        };
+        const int most = whole1 - 1;
+        int p = begin;
+        for (; p + 3 * step < end; p += 4 * step) {
+            uint4 q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = __ldg(base + max(whole0, min(p + i * step, most)));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) one(q[i], p + i * step);
+        }
+        for (; p < end; p += step) one(whole0 <= most ? __ldg(base + max(whole0, min(p, most))) : uint4(), p);
+    }
+    // f(value, index) for every value of the calling warp's segments
     template <typename F> __device__ __forceinline__ void each(F&& f) const {
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        const int end = min(pieces, (warp + 1) * segment);
-        for (int p = warp * segment + lane; p < end; p += 32) {
-            float v[N];
-            ardiff::unpack(piece[p], v, T());
+        scan(warp * 4 * segment + lane, min(pieces, (warp + 1) * 4 * segment), 32, [&](const float (&v)[N], int p) {
 #pragma unroll
             for (int i = 0; i < N; ++i) f(v[i], first + p * N + i);
+        });
+    }
+    // f(value, index) for every value of the groups whose largest logit `any` accepts: a warp a group, lanes its pieces. All threads.
+    template <typename G, typename F> __device__ __forceinline__ void each_of(G&& any, F&& f) const {
+        if (threadIdx.x == 0) s->groups = 0u;
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+            if (any(s->top[g][threadIdx.x])) s->group[atomicAdd(&s->groups, 1u)] = (unsigned short)(g * kThreads + threadIdx.x);
+        __syncthreads();
+        const int n = (int)s->groups, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        for (int i = warp; i < n; i += kWarps) {
+            scan(s->group[i] + lane * kGroups * kThreads, pieces, 32 * kGroups * kThreads, [&](const float (&v)[N], int p) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) f(v[j], first + p * N + j);
+            });
         }
     }
 };
@@ -210,31 +255,32 @@ __device__ __forceinline__ unsigned cta_scan(Shared& s, unsigned v, unsigned* to
     return before + inc - v;
 }
 
-// Sums of f(value, index) over the segments, in s.seg[buf]; afterwards every CTA knows their sum (returned) and, with target >= 0, the
-// first segment at whose end the running sum is above the target (the last one with anything, if none is: s.owner) and the
-// sum before it (s.before). Two calls in a row use different buffers.
+// Sums of f(value, index) over the segments; afterwards every CTA knows their sum (returned) and the first segment at whose end the
+// running sum is above `share` of it (the last one with anything, if none is: s.owner), and the sum before that (s.before). Two
+// calls in a row use different buffers: buf is turned.
 template <typename T, typename F>
-__device__ __forceinline__ double sum_segments(const Part<T>& a, int buf, double share, F&& f) {
+__device__ __forceinline__ double sum_segments(const Part<T>& a, int& buf, double share, F&& f) {
+    constexpr int N = Part<T>::N;
     Shared& s = *a.s;
-    double acc[4] = {0.0, 0.0, 0.0, 0.0};
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int end = min(a.pieces, (warp + 1) * a.segment);
-    for (int p = warp * a.segment + lane; p < end; p += 32) {
-        float v[Part<T>::N];
-        ardiff::unpack(a.piece[p], v, T());
+#pragma unroll 1
+    for (int g = warp * 4; g < warp * 4 + 4; ++g) {
+        double acc[2] = {0.0, 0.0};
+        a.scan(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const float (&v)[N], int p) {
 #pragma unroll
-        for (int i = 0; i < Part<T>::N; ++i) acc[i & 3] += f(v[i], a.first + p * Part<T>::N + i);
+            for (int i = 0; i < N; ++i) acc[i & 1] += f(v[i], a.first + p * N + i);
+        });
+        const double mine = warp_sum(acc[0] + acc[1]);
+        if (lane == 0) s.seg[buf][g] = mine;
     }
-    const double mine = warp_sum((acc[0] + acc[1]) + (acc[2] + acc[3]));
-    if (lane == 0) s.seg[buf][warp] = mine;
     a.sync();
     if (warp == 0) {
-        constexpr int kPer = kMaxParts * kWarps / 32;
+        constexpr int kPer = kMaxParts * kSegments / 32;
         double v[kPer], own = 0.0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int g = lane * kPer + i;
-            v[i] = g < a.parts * kWarps ? *a.at(&s.seg[buf][g % kWarps], g / kWarps) : 0.0;
+            v[i] = g < a.parts * kSegments ? *a.at(&s.seg[buf][g % kSegments], g / kSegments) : 0.0;
             own += v[i];
         }
         double inc = own;
@@ -274,15 +320,17 @@ __device__ __forceinline__ double sum_segments(const Part<T>& a, int buf, double
         }
     }
     __syncthreads();
+    buf ^= 1;
     return s.total;
 }
 
-// In the CTA that owns segment s.owner: the index of the first value at which the running sum of f passes share * total (the last value
-// with anything, if none does). All threads of that CTA call it.
+// In the CTA that owns segment s.owner: the index of the first value at which the running sum of f passes `target` (the last value
+// with anything, if none does), and that value. All threads of that CTA call it.
 template <typename T, typename F>
 __device__ __forceinline__ int locate(const Part<T>& a, double target, F&& f) {
+    constexpr int N = Part<T>::N;
     Shared& s = *a.s;
-    const int g = s.owner % kWarps;
+    const int g = s.owner % kSegments;
     const int begin = g * a.segment, end = min(a.pieces, begin + a.segment);
     double carry = s.before;
     if (threadIdx.x == 0) {
@@ -290,23 +338,20 @@ __device__ __forceinline__ int locate(const Part<T>& a, double target, F&& f) {
         s.last = -1;
     }
     for (int p0 = begin; p0 < end; p0 += kThreads) {
-        const int p = p0 + threadIdx.x;
-        double w[Part<T>::N], own = 0.0;
-        const int e = a.first + p * Part<T>::N;
-        if (p < end) {
-            float v[Part<T>::N];
-            ardiff::unpack(a.piece[p], v, T());
+        const int p = p0 + threadIdx.x, e = a.first + p * N;
+        double w[N], own = 0.0;
+        a.scan(p, min(end, p + 1), 1, [&](const float (&v)[N], int) {
 #pragma unroll
-            for (int i = 0; i < Part<T>::N; ++i) {
+            for (int i = 0; i < N; ++i) {
                 w[i] = f(v[i], e + i);
                 own += w[i];
             }
-        }
+        });
         double total;
         double run = carry + cta_scan(s, own, &total);             // (its barriers put s.found's start before its use)
-        if (p < end && own > 0.0) {
+        if (own > 0.0) {
 #pragma unroll
-            for (int i = 0; i < Part<T>::N; ++i) {
+            for (int i = 0; i < N; ++i) {
                 run += w[i];
                 if (w[i] > 0.0) {
                     atomicMax(&s.last, e + i);
@@ -332,8 +377,7 @@ __device__ __forceinline__ void sort_list(Shared& s, int n) {
     if (!one_warp || threadIdx.x < 32) {
         for (int span = 2; span <= size; span *= 2) {
             for (int step = span / 2; step > 0; step /= 2) {
-                const int i = threadIdx.x;
-                if (i < pairs) {
+                for (int i = threadIdx.x; i < pairs; i += kThreads) {
                     const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
                     const unsigned long long x = s.list[lo], y = s.list[hi];
                     if ((x > y) == ((lo & span) == 0)) {
@@ -364,71 +408,101 @@ __device__ __forceinline__ void answer(const Args& a, int64_t row, int token, fl
     a.logprob[row] = logprob;
 }
 
-// The first CTA alone: s.list[0 .. n) holds every logit that may be kept (and no other CTA's memory is needed). `whole`: the mass that
-// top-p is a share of, where no top-k makes it the list's own.
+// The first CTA alone: s.list[0 .. n) holds every logit that may be kept. `whole`: the mass that top-p is a share of, where it is not
+// the list's own (negative). False, and nothing done, if the list ends before the nucleus does.
 template <typename T>
-__device__ __forceinline__ void finish_list(const Args& args, int64_t row, const Part<T>& a, const Settings& o, int n, double whole,
-                                            bool all_listed) {
+__device__ __forceinline__ bool finish_list(const Args& args, int64_t row, const Part<T>& a, const Settings& o, int n, double whole) {
     Shared& s = *a.s;
     sort_list(s, n);
-    const int j0 = 2 * threadIdx.x, j1 = j0 + 1;
+    const int j0 = kEach * threadIdx.x;
     const int limit = o.use_k ? min(o.k, n) : n;
-    unsigned long long e0 = ~0ull, e1 = ~0ull;
-    double w0 = 0.0, w1 = 0.0, total;
-    if (j0 < limit) e0 = s.list[j0], w0 = a.weight_drawn(entry_value(e0));
-    if (j1 < limit) e1 = s.list[j1], w1 = a.weight_drawn(entry_value(e1));
-    const double before = cta_scan(s, w0 + w1, &total);
-    bool keep0 = j0 < limit, keep1 = j1 < limit;
-    if (o.use_p) {
-        const double enough = (double)o.p * (o.use_k || all_listed ? total : whole);
-        keep0 = keep0 && (j0 == 0 || before < enough);
-        keep1 = keep1 && before + w0 < enough;
+    unsigned long long e[kEach];
+    double w[kEach], own = 0.0, total;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        e[i] = ~0ull;
+        w[i] = 0.0;
+        if (j0 + i < limit) e[i] = s.list[j0 + i], w[i] = a.weight_drawn(entry_value(e[i]));
+        own += w[i];
     }
-    if (o.use_m) {
-        keep0 = keep0 && w0 >= (double)o.mp;
-        keep1 = keep1 && w1 >= (double)o.mp;
+    double before = cta_scan(s, own, &total);
+    const double enough = (double)o.p * (whole >= 0.0 ? whole : total);
+    if (o.use_p && whole >= 0.0 && total < enough) return false;
+    bool keep[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        keep[i] = j0 + i < limit && (!o.use_p || j0 + i == 0 || before < enough) && (!o.use_m || w[i] >= (double)o.mp);
+        before += w[i];
     }
     if (threadIdx.x == 0) {
         s.found = INT_MAX;
         s.last = -1;
     }
+    __syncthreads();                                         // the list has been read
     // what is kept, in order of index
-    const int kept = __syncthreads_count(keep0) + __syncthreads_count(keep1);
-    s.list[j0] = keep0 ? (e0 & 0xffffffffull) << 32 | (unsigned)j0 : ~0ull;
-    s.list[j1] = keep1 ? (e1 & 0xffffffffull) << 32 | (unsigned)j1 : ~0ull;
-    s.w[j0] = keep0 ? w0 : 0.0;
-    s.w[j1] = keep1 ? w1 : 0.0;
-    const float x0 = entry_value(e0), x1 = entry_value(e1);
-    sort_list(s, limit);
-    double v0 = 0.0, v1 = 0.0;
-    if (j0 < kept) v0 = s.w[(unsigned)s.list[j0]];
-    if (j1 < kept) v1 = s.w[(unsigned)s.list[j1]];
-    const double run = cta_scan(s, v0 + v1, &total);
-    const double target = (double)o.u * total;
-    if (v0 > 0.0) {
-        atomicMax(&s.last, j0);
-        if (run + v0 > target) atomicMin(&s.found, j0);
-    }
-    if (v1 > 0.0) {
-        atomicMax(&s.last, j1);
-        if (run + v0 + v1 > target) atomicMin(&s.found, j1);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        s.list[j0 + i] = keep[i] ? (e[i] & 0xffffffffull) << 32 | (unsigned)(j0 + i) : ~0ull;
+        s.w[j0 + i] = keep[i] ? w[i] : 0.0;
     }
     __syncthreads();
-    const int at = s.found != INT_MAX ? s.found : s.last;
-    const unsigned long long e = s.list[at];
-    const int j = (int)(unsigned)e;
-    if (j == j0 || j == j1) {
-        const double y = ((double)(j == j0 ? x0 : x1) - (double)a.m) * a.a;
-        answer(args, row, (int)(e >> 32), (float)(y * 0.69314718055994530942 - log(total)));
+    sort_list(s, limit);
+    own = 0.0;
+    unsigned at[kEach];
+    double v[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        at[i] = j0 + i < limit ? (unsigned)s.list[j0 + i] : ~0u;
+        v[i] = at[i] != ~0u ? s.w[at[i]] : 0.0;
+        own += v[i];
     }
+    double run = cta_scan(s, own, &total);
+    const double target = (double)o.u * total;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        run += v[i];
+        if (v[i] > 0.0) {
+            atomicMax(&s.last, j0 + i);
+            if (run > target) atomicMin(&s.found, j0 + i);
+        }
+    }
+    __syncthreads();
+    const unsigned long long drawn = s.list[s.found != INT_MAX ? s.found : s.last];
+    const int j = (int)(unsigned)drawn;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if (j == j0 + i) {
+            const double y = ((double)entry_value(e[i]) - (double)a.m) * a.a;
+            answer(args, row, (int)(drawn >> 32), (float)(y * 0.69314718055994530942 - log(total)));
+        }
+    }
+    return true;
 }
 
-// Logits at a distance d below the largest, by the bits of d: 32 bins an octave, from 2^-16 to 2^16; the last bin is beyond them.
+// Bins of logits by their distance d below the largest. By the bits of d: 32 bins an octave, from 2^-16 to 2^16, the last bin beyond.
 __device__ __forceinline__ int distance_bin(float d) {
     const int b = (int)(__float_as_uint(d) >> 18) - (int)(111u << 5);
     return min(max(b, 0), kBins - 1);
 }
 __device__ __forceinline__ float distance_edge(int b) { return __uint_as_float((unsigned)(b + (111 << 5)) << 18); }
+// By the weight, 16 bins an octave, 64 octaves (to the nearest whole number: adding 2^23 leaves it in the last bits).
+__device__ __forceinline__ int weight_bin(float d, float a32) {
+    return __float_as_int(fminf(d * a32 * 16.0f, (float)(kBins - 1)) + 8388608.0f) - __float_as_int(8388608.0f);
+}
+
+__device__ __forceinline__ void clear_bins(Shared& s) {
+#pragma unroll
+    for (int i = 0; i < kBins * kCopies / 4 / kThreads; ++i) reinterpret_cast<uint4*>(s.hist)[i * kThreads + threadIdx.x] = uint4();
+}
+__device__ __forceinline__ void count_bin(Shared& s, int b) { atomicAdd(&s.hist[b * kCopies + (threadIdx.x & (kCopies - 1))], 1u); }
+// The calling thread's bins of one histogram, kEach * threadIdx.x and the ones behind it.
+__device__ __forceinline__ void add_bins(const unsigned* hist, unsigned (&c)[kEach]) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const uint4 q = reinterpret_cast<const uint4*>(hist)[kEach * threadIdx.x + i];
+        c[i] += (q.x + q.y) + (q.z + q.w);
+    }
+}
 
 // What a histogram says about where a prefix ends: the bins, first to last (larger logits first), that hold its last element, the
 // elements before them and in them, and the mass before them by the bins' middles.
@@ -439,64 +513,81 @@ struct Range {
 };
 
 // Adds up the CTAs' histograms and picks the bin in which the count passes k (COUNT), the estimated mass `enough`, or the count half of
-// all (HALF: where estimates did not help). A bin that was found by an estimate comes with its neighbours, as far as the list
+// all (half: where estimates did not help). A bin that was found by an estimate comes with its neighbours, as far as the list
 // has room. before, mass: in front of the histogram. middle(b): a weight of bin b. False: there is nothing.
 template <typename T, bool COUNT, typename F>
 __device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough, bool half, unsigned before, double mass, F&& middle,
                                      Range& r) {
     Shared& s = *a.s;
-    const int b0 = 2 * threadIdx.x, b1 = b0 + 1;
-    unsigned c0 = 0, c1 = 0, total;
-    for (int p = 0; p < a.parts; ++p) {
-        const unsigned* h = a.at(s.hist, p);
-        c0 += h[b0];
-        c1 += h[b1];
-    }
+    const int b0 = kEach * threadIdx.x;
+    unsigned c[kEach] = {}, own = 0, total;
+    for (int p = 0; p < a.parts; ++p) add_bins(a.at(s.hist, p), c);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) own += c[i];
     if (threadIdx.x == 0) {
         s.found = s.pick_first = INT_MAX;
         s.last = s.pick_last = -1;
     }
-    const unsigned n0 = before + cta_scan(s, c0 + c1, &total), n1 = n0 + c0, n2 = n1 + c1;
+    unsigned n[kEach + 1];
+    double m[kEach + 1];
+    n[0] = before + cta_scan(s, own, &total);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) n[i + 1] = n[i] + c[i];
+    m[0] = mass;
     if (total == 0u) return false;
     if (COUNT && before + total < k) {                       // not as many
         r = Range{0, 0, before, total, 0.0};
         return true;
     }
-    double m0 = mass, m1 = mass;
     if (COUNT || half) {
         const unsigned goal = COUNT ? k : before + (total + 1) / 2;
-        if (n0 < goal && n1 >= goal) s.found = b0;
-        else if (n1 < goal && n2 >= goal) s.found = b1;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (n[i] < goal && n[i + 1] >= goal) s.found = b0 + i;
+            m[i + 1] = mass;
+        }
     } else {
-        double w0 = 0.0, w1 = 0.0, all;
-        if (c0) w0 = c0 * middle(b0);
-        if (c1) w1 = c1 * middle(b1);
-        m0 = mass + cta_scan(s, w0 + w1, &all);
-        m1 = m0 + w0;
-        if (c0 && m1 >= enough) atomicMin(&s.found, b0);
-        else if (c1 && m1 + w1 >= enough) atomicMin(&s.found, b1);
-        if (c0 | c1) atomicMax(&s.last, c1 ? b1 : b0);
+        double w[kEach], sum = 0.0, all;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            w[i] = c[i] ? c[i] * middle(b0 + i) : 0.0;
+            sum += w[i];
+        }
+        m[0] = mass + cta_scan(s, sum, &all);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            m[i + 1] = m[i] + w[i];
+            if (c[i]) {
+                atomicMax(&s.last, b0 + i);
+                if (m[i + 1] >= enough) atomicMin(&s.found, b0 + i);
+            }
+        }
     }
     __syncthreads();
     const int found = s.found != INT_MAX ? s.found : s.last;
-    if (found == b0) s.pick_before = n0, s.pick_after = n1;
-    else if (found == b1) s.pick_before = n1, s.pick_after = n2;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (found == b0 + i) s.pick_before = n[i], s.pick_after = n[i + 1];
     __syncthreads();
     const unsigned lo = s.pick_before, hi = s.pick_after, in = hi - lo;
     const unsigned more = COUNT || in > (unsigned)kList ? 0u : ((unsigned)kList - in) / 2;
     if (more == 0u) {
         if (threadIdx.x == 0) s.pick_first = s.pick_last = found;
-    } else if (b0 <= found && n0 + more >= lo) atomicMin(&s.pick_first, b0);
-    else if (b1 <= found && n1 + more >= lo) atomicMin(&s.pick_first, b1);
-    if (more != 0u && b1 >= found && n2 <= hi + more) atomicMax(&s.pick_last, b1);
-    else if (more != 0u && b0 >= found && n1 <= hi + more) atomicMax(&s.pick_last, b0);
+    } else {                                                 // (empty bins at either end come along)
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (b0 + i <= found && n[i] + more >= lo) atomicMin(&s.pick_first, b0 + i);
+            if (b0 + i >= found && n[i + 1] <= hi + more) atomicMax(&s.pick_last, b0 + i);
+        }
+    }
     __syncthreads();
     r.first = s.pick_first;
     r.last = s.pick_last;
-    if (r.first == b0) s.pick_before = n0, s.mass_above = m0;
-    else if (r.first == b1) s.pick_before = n1, s.mass_above = m1;
-    if (r.last == b0) s.pick_after = n1;
-    else if (r.last == b1) s.pick_after = n2;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if (r.first == b0 + i) s.pick_before = n[i], s.mass_above = m[i];
+        if (r.last == b0 + i) s.pick_after = n[i + 1];
+    }
     __syncthreads();
     r.before = s.pick_before;
     r.in = s.pick_after - r.before;
@@ -504,42 +595,41 @@ __device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough
     return true;
 }
 
-// The search for a prefix's last element among what `cut` keeps: the k-th (COUNT), or the first at which the mass reaches `enough`.
+// The search for a prefix's last element among what `cut` keeps: the k-th (COUNT), or the first at which the mass reaches `enough`; then
+// r is the range of weight_bin's bins that a histogram over the same elements pointed to.
 template <typename T, bool COUNT>
-__device__ __noinline__ Cut search(const Part<T>& a, const Cut cut, unsigned k, double enough, int& buf) {
+__device__ __noinline__ Cut search(const Part<T>& a, const Cut cut, unsigned k, double enough, Range r, int& buf) {
     Shared& s = *a.s;
     const float cut_value = value_of(cut.key);
     auto kept = [&](float x, int i) { return x > cut_value || (x == cut_value && i <= cut.index) || cut.key == 0u; };
     const float a32 = a.a32;
     unsigned lo_key = key_of(-INFINITY) + 1, hi_key = key_of(a.m);       // where the element can be; masked logits are none
     double hi_mass = 0.0;                                                // above hi_key
-    // a first histogram by the distance from the largest: its logarithm where elements are counted, linear over 64 octaves of the
-    // weight where their mass is
-    const float width = 64.0f / (float)kBins / a32;
-    auto bin_of = [&](float d) { return COUNT ? distance_bin(d) : (int)fminf(d / width, (float)(kBins - 1)); };
     __syncthreads();                                                     // s.found and the histogram have been read
-    s.hist[2 * threadIdx.x] = s.hist[2 * threadIdx.x + 1] = 0u;
+    if (COUNT) {
+        clear_bins(s);
+        __syncthreads();
+        a.each([&](float x, int i) {
+            if (x > -INFINITY && kept(x, i)) count_bin(s, distance_bin(a.m - x));
+        });
+        a.sync();
+        pick<T, true>(a, k, enough, false, 0u, 0.0, [](int) { return 0.0; }, r);
+        if (r.before + r.in < k) {                                       // there are no more than k
+            a.sync();
+            return cut;
+        }
+    }
+    // the range as keys: those of its elements' extremes
     if (threadIdx.x == 0) {
         s.kmin = UINT_MAX;
         s.kmax = 0u;
     }
     __syncthreads();
-    a.each([&](float x, int i) {
-        if (x > -INFINITY && kept(x, i)) atomicAdd(&s.hist[bin_of(a.m - x)], 1u);
-    });
-    a.sync();
-    Range r;
-    pick<T, COUNT>(a, k, enough, false, 0u, 0.0, [&](int b) { return (double)ardiff::ex2(-((float)b + 0.5f) * width * a32); }, r);
-    if (COUNT && r.before + r.in < k) {                                  // there are no more than k
-        a.sync();
-        return cut;
-    }
-    // the range as keys: those of its elements' extremes
     {
         unsigned lo = UINT_MAX, hi = 0u;
         a.each([&](float x, int i) {
             if (x > -INFINITY && kept(x, i)) {
-                const int b = bin_of(a.m - x);
+                const int b = COUNT ? distance_bin(a.m - x) : weight_bin(a.m - x, a32);
                 if (b >= r.first && b <= r.last) {
                     const unsigned q = key_of(x);
                     lo = min(lo, q);
@@ -568,11 +658,11 @@ __device__ __noinline__ Cut search(const Part<T>& a, const Cut cut, unsigned k, 
         while (r.in == UINT_MAX || (r.in > (unsigned)kList && kmin < kmax)) {
             int shift = 0;
             while (((kmax - kmin) >> shift) >= (unsigned)kBins) ++shift;
-            s.hist[2 * threadIdx.x] = s.hist[2 * threadIdx.x + 1] = 0u;
+            clear_bins(s);
             __syncthreads();
             a.each([&](float x, int i) {
                 const unsigned q = key_of(x);
-                if (q >= kmin && q <= kmax && kept(x, i)) atomicAdd(&s.hist[(kmax - q) >> shift], 1u);     // largest first
+                if (q >= kmin && q <= kmax && kept(x, i)) count_bin(s, (int)((kmax - q) >> shift));        // largest first
             });
             a.sync();
             const bool any = pick<T, COUNT>(a, k, enough, turn > 2, r.before, r.mass, [&](int b) {
@@ -592,10 +682,7 @@ __device__ __noinline__ Cut search(const Part<T>& a, const Cut cut, unsigned k, 
         if (threadIdx.x == 0) s.count = 0u;
         a.sync();
         double sure = 0.0;
-        if (!COUNT) {
-            sure = sum_segments(a, buf, 2.0, [&](float x, int i) { return x > top && kept(x, i) ? a.weight(x) : 0.0; });
-            buf ^= 1;
-        }
+        if (!COUNT) sure = sum_segments(a, buf, 2.0, [&](float x, int i) { return x > top && kept(x, i) ? a.weight(x) : 0.0; });
         if (!ties) {
             a.each([&](float x, int i) {
                 if (x >= bottom && x <= top && kept(x, i)) {
@@ -616,13 +703,19 @@ __device__ __noinline__ Cut search(const Part<T>& a, const Cut cut, unsigned k, 
                     }
                 } else {
                     if (threadIdx.x == 0) s.found = INT_MAX;
-                    const int j0 = 2 * threadIdx.x;
-                    double w0 = 0.0, w1 = 0.0, all;
-                    if (j0 < n) w0 = a.weight(entry_value(s.list[j0]));
-                    if (j0 + 1 < n) w1 = a.weight(entry_value(s.list[j0 + 1]));
-                    const double run = sure + cta_scan(s, w0 + w1, &all);
-                    if (j0 < n && run + w0 >= enough) atomicMin(&s.found, j0);
-                    else if (j0 + 1 < n && run + w0 + w1 >= enough) atomicMin(&s.found, j0 + 1);
+                    const int j0 = kEach * threadIdx.x;
+                    double w[kEach], own = 0.0, all;
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) {
+                        w[i] = j0 + i < n ? a.weight(entry_value(s.list[j0 + i])) : 0.0;
+                        own += w[i];
+                    }
+                    double run = sure + cta_scan(s, own, &all);
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) {
+                        run += w[i];
+                        if (j0 + i < n && run >= enough) atomicMin(&s.found, j0 + i);
+                    }
                     __syncthreads();
                     if (threadIdx.x == 0) {
                         s.mass_in = sure + all;
@@ -653,8 +746,7 @@ __device__ __noinline__ Cut search(const Part<T>& a, const Cut cut, unsigned k, 
             auto one = [&](float x, int i) { return x == top && kept(x, i) ? 1.0 : 0.0; };
             // (the sum over all is r.in: the share of it is a whole number less a half, up to rounding)
             sum_segments(a, buf, (need - 0.5) / (double)r.in, one);
-            buf ^= 1;
-            const int owner = s.owner / kWarps;
+            const int owner = s.owner / kSegments;
             if (verdict == 0 && owner == a.rank) {
                 const int at = locate(a, need - 0.5, one);
                 if (threadIdx.x == 0) s.cut_index = at;
@@ -691,9 +783,8 @@ __device__ __noinline__ Cut search(const Part<T>& a, const Cut cut, unsigned k, 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const Args args) {
+__global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     constexpr int N = ardiff::Piece<T>::N;
-    extern __shared__ __align__(16) uint4 s_piece[];
     __shared__ Shared s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row = blockIdx.x / args.parts;
@@ -714,65 +805,66 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Args args) {
     a.rank = blockIdx.x % args.parts;
     a.parts = args.parts;
     a.V = args.V;
-    a.piece = s_piece;
     a.tiny = o.u == 0.f;
     // the aligned pieces that cover the row; `shift` places in front of it belong to none of them
-    const T* x = static_cast<const T*>(args.x) + row * args.ld;
-    const int shift = (int)((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T));
+    a.x = static_cast<const T*>(args.x) + row * args.ld;
+    const int shift = (int)((reinterpret_cast<uintptr_t>(a.x) & 15u) / sizeof(T));
     const int pieces = (shift + args.V + N - 1) / N;
     const int per = (pieces + a.parts - 1) / a.parts;
     const int p0 = min(pieces, a.rank * per);
     a.pieces = min(pieces, p0 + per) - p0;
-    a.segment = (a.pieces + kWarps - 1) / kWarps;
+    a.segment = (a.pieces + kSegments - 1) / kSegments;
     a.first = p0 * N - shift;
-    float top = -INFINITY;
+    a.whole0 = a.first < 0 ? 1 : 0;
+    a.whole1 = max(a.whole0, min(a.pieces, (args.V - a.first) / N));
+    float top[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) top[g] = -INFINITY;
     {
-        const int end = min(a.pieces, (warp + 1) * a.segment);
-        for (int p = warp * a.segment + lane; p < end; p += 32) {
-            const int e = a.first + p * N;
-            uint4 v;
-            if (e >= 0 && e + N <= args.V) {
-                v = __ldg(reinterpret_cast<const uint4*>(x + e));
-            } else {
-                T t[N];
+        const uint4* base = reinterpret_cast<const uint4*>(a.x + a.first);
+        const int most = a.whole1 - 1;
+        if (a.whole0 <= most) {
+            for (int p = tid; p < a.pieces; p += kGroups * kThreads) {
+                uint4 q[kGroups];
+                // (beyond the whole pieces the nearest of them once more, which changes no maximum but that group's)
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    t[i] = e + i >= 0 && e + i < args.V ? x[e + i] : ardiff::from_float<T>(-INFINITY);
-                float f[N];
+                for (int g = 0; g < kGroups; ++g) q[g] = __ldg(base + max(a.whole0, min(p + g * kThreads, most)));
 #pragma unroll
-                for (int i = 0; i < N; ++i) f[i] = ardiff::to_float(t[i]);
-                v = ardiff::pack(f, T());
+                for (int g = 0; g < kGroups; ++g) {
+                    const int i = p + g * kThreads;
+                    if (i >= a.whole0 && i <= most) top[g] = max_nan(top[g], ardiff::piece_max(q[g], T()));
+                }
             }
-            s_piece[p] = v;
-            float f[N];
-            ardiff::unpack(v, f, T());
+        }
+        // the pieces that only partly lie in the row: their group's maximum has them too
 #pragma unroll
-            for (int i = 0; i < N; ++i) top = max_nan(top, f[i]);
+        for (int g = 0; g < kGroups; ++g) {
+            const int group = g * kThreads + tid;
+            if (a.whole0 == 1 && group == 0 && a.pieces > 0) top[g] = max_nan(top[g], ardiff::piece_max(a.edge(0), T()));
+            if (a.whole1 < a.pieces && (a.whole1 & (kGroups * kThreads - 1)) == group)
+                top[g] = max_nan(top[g], ardiff::piece_max(a.edge(a.whole1), T()));
         }
     }
-    s.thread_max[tid] = top;
-    float wtop = top;
+    float own = top[0];
 #pragma unroll
-    for (int q = 16; q > 0; q >>= 1) wtop = max_nan(wtop, __shfl_xor_sync(0xffffffffu, wtop, q));
-    if (lane == 0) s.warp_max[warp] = wtop;
-    if (tid == 0) s.count = 0u;
+    for (int g = 0; g < kGroups; ++g) {
+        s.top[g][tid] = top[g];
+        own = max_nan(own, top[g]);
+    }
+#pragma unroll
+    for (int q = 16; q > 0; q >>= 1) own = max_nan(own, __shfl_xor_sync(0xffffffffu, own, q));
+    if (lane == 0) s.warp_max[warp] = own;
+    if (tid == 0) {
+        s.count = 0u;
+        s.first = INT_MAX;
+    }
     __syncthreads();
-    float own = s.warp_max[0];
+    own = s.warp_max[0];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) own = max_nan(own, s.warp_max[w]);
     const bool greedy = o.T == 0.f;
-    if (greedy) {                                            // the lowest index of this part's largest
-        int first = INT_MAX;
-        if (top == own)
-            a.each([&](float v, int i) { if (v == own) first = min(first, i); });
-        first = __reduce_min_sync(0xffffffffu, first);
-        if (lane == 0) s.warp_first[warp] = first;
-        __syncthreads();
-        if (tid == 0) {
-            for (int w = 1; w < kWarps; ++w) first = min(first, s.warp_first[w]);
-            s.cta_first = first;
-        }
-    }
+    if (greedy)                                              // the lowest index of this part's largest
+        a.each_of([&](float v) { return v == own; }, [&](float v, int i) { if (v == own) atomicMin(&s.first, i); });
     if (tid == 0) s.cta_max = own;
     a.sync();
     a.m = own;
@@ -783,7 +875,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Args args) {
             if (valid && fabsf(a.m) < INFINITY) {
                 token = INT_MAX;
                 for (int r = 0; r < a.parts; ++r)
-                    if (*a.at(&s.cta_max, r) == a.m) token = min(token, *a.at(&s.cta_first, r));
+                    if (*a.at(&s.cta_max, r) == a.m) token = min(token, *a.at(&s.first, r));
             }
             answer(args, row, token, token >= 0 ? 0.f : NAN);
         }
@@ -792,130 +884,142 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Args args) {
     }
     a.a = 1.4426950408889634074 / (double)o.T;
     a.a32 = (float)fmin(a.a, 3e38);
+    const float half = 0.5f * a.m;                           // (halves: a difference of two logits can pass fp32's range)
+    const float floor_ = o.use_m ? 0.5f * (log2f(o.mp) - 0.01f) : -INFINITY;
     int buf = 0;
     Cut cut = no_cut();
-    if (o.use_k || o.use_p) {
-        // a distance below the largest logit within which everything that is kept lies, but few others
-        float reach = -1.f;
-        double whole = 0.0;
-        const bool all = args.V <= kList;
-        if (all) {
-            reach = INFINITY;
-        } else {
-            if (!o.use_k) {
-                whole = sum_segments(a, buf, 2.0, [&](float v, int) { return a.weight(v); });
-                buf ^= 1;
-            }
-            s.hist[2 * tid] = s.hist[2 * tid + 1] = 0u;
+    if (o.use_k || o.use_p || o.use_m) {
+        // which logits a list of all that may be kept has to hold, if there is a list
+        enum { ALL, REACH, WEIGHT, SHARE, NONE } which = NONE;
+        float reach = 0.f;
+        Range r;
+        double whole = -1.0;
+        if (args.V <= kList) {
+            which = ALL;
+        } else if (o.use_k) {
+            // by the groups' largest logits: at least k logits are not below the k-th of them
+            clear_bins(s);
             if (tid == 0) s.found = INT_MAX;
             __syncthreads();
-            for (int r = 0; r < a.parts; ++r) {
-                const float d = a.m - *a.at(&s.thread_max[tid], r);
-                const int b = distance_bin(d);
-                if (b < kBins - 1) atomicAdd(&s.hist[b], 1u);
+            for (int p = 0; p < a.parts; ++p) {
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    const int b = distance_bin(a.m - *a.at(&s.top[g][tid], p));
+                    if (b < kBins - 1) count_bin(s, b);
+                }
             }
             __syncthreads();
-            const unsigned c0 = s.hist[2 * tid], c1 = s.hist[2 * tid + 1];
-            unsigned total;
-            const unsigned before = cta_scan(s, c0 + c1, &total);
-            if (o.use_k) {
-                if (before < (unsigned)o.k && before + c0 >= (unsigned)o.k) s.found = 2 * tid;
-                else if (before + c0 < (unsigned)o.k && before + c0 + c1 >= (unsigned)o.k) s.found = 2 * tid + 1;
-            } else {
-                // weights at the bins' far edges, less what fp32 may have added to them: no more than the logits have
-                const double m0 = c0 * 0.9999 * (double)ardiff::ex2(-distance_edge(2 * tid + 1) * a.a32);
-                const double m1 = c1 * 0.9999 * (double)ardiff::ex2(-distance_edge(2 * tid + 2) * a.a32);
-                double sum;
-                const double run = cta_scan(s, m0 + m1, &sum);
-                const double enough = (double)o.p * whole;
-                if (c0 && run + m0 >= enough) atomicMin(&s.found, 2 * tid);
-                else if (c1 && run + m0 + m1 >= enough) atomicMin(&s.found, 2 * tid + 1);
+            unsigned c[kEach] = {}, total;
+            add_bins(s.hist, c);
+            unsigned n = cta_scan(s, (c[0] + c[1]) + (c[2] + c[3]), &total);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                if (n < (unsigned)o.k && n + c[i] >= (unsigned)o.k) s.found = kEach * tid + i;
+                n += c[i];
             }
             __syncthreads();
-            if (s.found != INT_MAX) reach = distance_edge(s.found + 1);
+            if (s.found != INT_MAX) {
+                which = REACH;
+                reach = distance_edge(s.found + 1);
+            }
+        } else if (o.use_p) {
+            // the whole mass, and a histogram that says about where the nucleus ends
+            clear_bins(s);
+            __syncthreads();
+            whole = sum_segments(a, buf, 2.0, [&](float v, int) {
+                const int b = weight_bin(a.m - v, a.a32);
+                if (b < kBins - 1) count_bin(s, b);
+                return a.weight(v);
+            });
+            pick<T, false>(a, 0u, (double)o.p * whole, false, 0u, 0.0,
+                           [&](int b) { return (double)ardiff::ex2(-0.0625f * (float)b); }, r);
+            r.last = min(r.last, kBins - 2);                 // (the last bin was not counted)
+            if (r.before + r.in <= (unsigned)kList) which = SHARE;
+        } else {
+            which = WEIGHT;
         }
-        if (reach >= 0.f) {
-            if (a.m - top < reach || (all && top > -INFINITY))
-                a.each([&](float v, int i) {
-                    if (v > -INFINITY && (all || a.m - v < reach)) {
-                        const unsigned at = atomicAdd(a.at(&s.count, 0), 1u);
-                        if (at < (unsigned)kList) *a.at(&s.list[at], 0) = entry(v, i);
-                    }
-                });
+        if (which != NONE) {
+            auto listed = [&](float v) {
+                if (which == REACH) return a.m - v < reach;
+                if (which == WEIGHT) return (0.5f * v - half) * a.a32 >= floor_;
+                if (which == SHARE) return v > -INFINITY && weight_bin(a.m - v, a.a32) <= r.last;
+                return v > -INFINITY;
+            };
+            a.each_of(listed, [&](float v, int i) {
+                if (listed(v) && v > -INFINITY) {
+                    const unsigned at = atomicAdd(a.at(&s.count, 0), 1u);
+                    if (at < (unsigned)kList) *a.at(&s.list[at], 0) = entry(v, i);
+                }
+            });
             a.sync();
             const unsigned n = *a.at(&s.count, 0);
+            bool done = n <= (unsigned)kList;
+            if (done && a.rank == 0) {
+                done = finish_list(args, row, a, o, (int)n, whole);
+                if (tid == 0) s.verdict = done;
+            }
+            if (which == SHARE && n <= (unsigned)kList) {    // an estimate's list: it may have been too short
+                a.sync();
+                done = *a.at(&s.verdict, 0);
+            }
             a.sync();
-            if (n <= (unsigned)kList) {
-                if (a.rank == 0) finish_list(args, row, a, o, (int)n, whole, all);
-                return;
-            }
+            if (done) return;
         }
-        if (o.use_k) cut = search<T, true>(a, cut, (unsigned)o.k, 0.0, buf);
+        if (o.use_k) cut = search<T, true>(a, cut, (unsigned)o.k, 0.0, r, buf);
         if (o.use_p) {
-            const float c = value_of(cut.key);
             if (o.use_k) {
+                const float c = value_of(cut.key);
+                __syncthreads();
+                clear_bins(s);
+                __syncthreads();
                 whole = sum_segments(a, buf, 2.0, [&](float v, int i) {
-                    return cut.key == 0u || v > c || (v == c && i <= cut.index) ? a.weight(v) : 0.0;
+                    if (!(cut.key == 0u || v > c || (v == c && i <= cut.index))) return 0.0;
+                    const int b = weight_bin(a.m - v, a.a32);
+                    if (b < kBins - 1) count_bin(s, b);
+                    return a.weight(v);
                 });
-                buf ^= 1;
+                pick<T, false>(a, 0u, (double)o.p * whole, false, 0u, 0.0,
+                               [&](int b) { return (double)ardiff::ex2(-0.0625f * (float)b); }, r);
+                r.last = min(r.last, kBins - 2);                 // (the last bin was not counted)
+                a.sync();                                    // the histograms have been read
             }
-            cut = search<T, false>(a, cut, 0u, fmax((double)o.p * whole, 1e-300), buf);       // at least one
+            cut = search<T, false>(a, cut, 0u, fmax((double)o.p * whole, 1e-300), r, buf);       // at least one
         }
     }
     // the draw among what the cut keeps
     const float c = value_of(cut.key);
-    const float half = 0.5f * a.m;                           // (halves: a difference of two logits can pass fp32's range)
-    const float floor_ = o.use_m ? 0.5f * (log2f(o.mp) - 0.01f) : -INFINITY;
     auto kept = [&](float v, int i) {
         return (cut.key == 0u || v > c || (v == c && i <= cut.index)) && (!o.use_m || (0.5f * v - half) * a.a32 >= floor_);
     };
     auto weight = [&](float v, int i) {
         if (!kept(v, i)) return 0.0;
-        const double w = a.weight(v);
+        const double w = a.tiny ? a.weight_drawn(v) : a.weight(v);
         return o.use_m && w < (double)o.mp ? 0.0 : w;
     };
-    auto weight_drawn = [&](float v, int i) {
-        if (!kept(v, i)) return 0.0;
-        const double w = a.weight_drawn(v);
-        return o.use_m && w < (double)o.mp ? 0.0 : w;
-    };
-    const double total = a.tiny ? sum_segments(a, buf, (double)o.u, weight_drawn) : sum_segments(a, buf, (double)o.u, weight);
+    const double total = sum_segments(a, buf, (double)o.u, weight);
     a.sync();                                                // every CTA has read the others' sums
-    if (s.owner / kWarps != a.rank) return;
-    const int token = locate(a, (double)o.u * total, weight_drawn);
+    if (s.owner / kSegments != a.rank) return;
+    const int token = locate(a, (double)o.u * total, weight);
     if (tid == 0) {
-        const float v = ardiff::to_float(reinterpret_cast<const T*>(s_piece)[token - a.first]);
-        const double y = ((double)v - (double)a.m) * a.a;
+        const double y = ((double)ardiff::to_float(a.x[token]) - (double)a.m) * a.a;
         answer(args, row, token, (float)(y * 0.69314718055994530942 - log(total)));
     }
 }
 
 template <typename T>
 int launch(Args a, int64_t n, cudaStream_t st) {
-    static std::atomic<unsigned long long> ready{0};
-    const void* fn = reinterpret_cast<const void*>(&sample_kernel<T>);
-    constexpr int kMostBytes = 160 * 1024;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return ARDIFF_ERR_CUDA;
-    if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
-        if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostBytes) != cudaSuccess) return ARDIFF_ERR_CUDA;
-        if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
-    }
-    // parts of at most 64 KB where that is possible; more parts while there are SMs without one and parts of 16 KB
-    const int64_t pieces = ((int64_t)a.V + 2 * ardiff::Piece<T>::N - 2) / ardiff::Piece<T>::N;
+    // more CTAs a row while not all find room at once and each keeps 512 pieces
+    const int64_t pieces = ((int64_t)a.V + ardiff::Piece<T>::N - 1) / ardiff::Piece<T>::N;
     int parts = 1;
-    while (parts < kMaxParts && (pieces * 16 > (int64_t)parts * 65536 || (n * parts < 148 && pieces * 16 > (int64_t)parts * 16384)))
-        parts *= 2;
+    while (parts < kMaxParts && n * parts < 148 * 2 && pieces >= (int64_t)parts * 1024) parts *= 2;
     a.parts = parts;
-    const int64_t bytes = (pieces + parts - 1) / parts * 16;
-    if (bytes > kMostBytes) return ARDIFF_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)(n * parts)); cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)bytes; cfg.stream = st;
+    cfg.stream = st;
     cfg.attrs = at; cfg.numAttrs = 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, sample_kernel<T>, (const Args)a);
     ardiff::set_launch_count(1);
