@@ -53,6 +53,14 @@ struct Args {
     int32_t V, parts;
 };
 
+// Kept: everything before this element in the order (descending, lowest index first), and it.
+struct Cut {
+    float value;
+    int index;
+    __device__ __forceinline__ bool keeps(float v, int i) const { return v > value || (v == value && i <= index); }
+};
+__device__ __forceinline__ Cut no_cut() { return Cut{-INFINITY, INT_MAX}; }
+
 struct Shared {
     float top[kGroups][kThreads];        // the groups' largest logits
     float warp_max[kWarps];
@@ -70,8 +78,7 @@ struct Shared {
     int pick_first, pick_last;
     unsigned pick_before, pick_after;
     int verdict;
-    unsigned cut_key;
-    int cut_index;
+    Cut cut;
     double mass_above, mass_in;
     unsigned short group[kGroups * kThreads];
     unsigned long long list[kList];
@@ -90,13 +97,6 @@ __device__ __forceinline__ float value_of(unsigned k) {
     return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// Kept: everything before this element in the order (descending, lowest index first), and it.
-struct Cut {
-    unsigned key;
-    int index;
-};
-__device__ __forceinline__ Cut no_cut() { return Cut{0u, INT_MAX}; }
-
 __device__ __forceinline__ float max_nan(float a, float b) {       // NaN if either is
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -104,12 +104,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {       // NaN if eit
 }
 
 // 2^y of y = d a, d <= 0: y = k + r, |r| <= 1/2, 2^r = 1 + r P(r), P of degree 8 by interpolation at the Chebyshev nodes (3.7e-14
-// relative; exactly 1 at 0). 0 below 2^kFar, also for d = -inf.
+// relative; exactly 1 at 0). y > -1000.
 __device__ __forceinline__ double pow2(double d, double a) {
     constexpr double kRound = 6755399441055744.0;                  // 1.5 2^52: adding it leaves the nearest integer
     const double t = fma(d, a, kRound);
-    const double k = t - kRound;
-    const double r = fma(d, a, -k);
+    const double r = fma(d, a, kRound - t);
     double p = 1.0203121063391729e-07;
     p = fma(p, r, 1.3255224878668817e-06);
     p = fma(p, r, 1.525268684626772e-05);
@@ -120,11 +119,24 @@ __device__ __forceinline__ double pow2(double d, double a) {
     p = fma(p, r, 0.2402265069581299);
     p = fma(p, r, 0.6931471805599453);
     p = fma(p, r, 1.0);
-    const double v = __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
-    return k >= kFar ? v : 0.0;
+    return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
 }
-// u = 0 asks for the first kept token with any weight at all, down to fp64's smallest.
-__device__ __noinline__ double pow2_far(double d, double a) { return d == -INFINITY ? 0.0 : exp2(d * a); }
+
+// The weights of a row. Sums over many use bulk(): logits below `lowest` count as 2^-100 each, which is nothing beside the largest
+// one's 1 (2^18 of them are 2^-82; at most 2^-57 where fp32 had to round `lowest`). One that may be drawn has its own() weight, down to
+// fp64's smallest.
+struct Weights {
+    double m, a;                         // the largest logit, log2(e) / T
+    float lowest;
+    bool far;                            // bulk() will not do: u = 0 asks for the first token of any weight at all; temperatures
+                                         // so high, or so low, that fp32 has no such `lowest`
+    __device__ __forceinline__ double bulk(float v) const { return pow2((double)fmaxf(v, lowest) - m, a); }
+    __device__ __noinline__ static double exact(double y) { return y >= -1100.0 ? exp2(y) : 0.0; }
+    __device__ __forceinline__ double own(float v) const {
+        const double d = (double)v - m, y = d * a;
+        return y >= -100.0 ? pow2(d, a) : exact(y);                // (-inf: 0)
+    }
+};
 
 template <typename T>
 struct Part {                            // this CTA's part of its row
@@ -134,27 +146,17 @@ struct Part {                            // this CTA's part of its row
     int first;                           // index of the part's first value in the row (negative in front of the row)
     int whole0, whole1;                  // pieces that lie in the row as a whole
     int rank, parts, V;
-    float m;
-    double a;                            // log2(e) / T
-    float a32;                           // the same in fp32, finite
-    bool tiny;                           // u = 0
     Shared* s;
 
-    __device__ __forceinline__ double weight(float v) const { return pow2((double)v - (double)m, a); }
-    __device__ __forceinline__ double weight_drawn(float v) const {        // of a draw that may end at any weight above 0
-        const double w = weight(v);
-        return tiny && w == 0.0 ? pow2_far((double)v - (double)m, a) : w;
-    }
     __device__ __forceinline__ void sync() const {
         if (parts > 1) cg::this_cluster().sync(); else __syncthreads();
     }
     template <typename U> __device__ __forceinline__ U* at(U* p, int r) const {
         return parts > 1 ? cg::this_cluster().map_shared_rank(p, r) : p;
     }
-    // a piece at either end of the row: -inf in the places outside it
-    __device__ __noinline__ uint4 edge(int p) const {
+    // the piece of the values e, e + 1, ... at either end of a row: -inf in the places outside it
+    __device__ __noinline__ static uint4 edge(const T* x, int e, int V) {
         float v[N];
-        const int e = first + p * N;
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = e + i >= 0 && e + i < V ? ardiff::to_float(x[e + i]) : -INFINITY;
         return ardiff::pack(v, T());
@@ -163,7 +165,7 @@ struct Part {                            // this CTA's part of its row
     template <typename F> __device__ __forceinline__ void scan(int begin, int end, int step, F&& f) const {
         const uint4* base = reinterpret_cast<const uint4*>(x + first);     // (aligned; pieces whole0 .. whole1 - 1 are read)
         auto one = [&](uint4 q, int p) {
-            if (p < whole0 || p >= whole1) q = edge(p);
+            if (p < whole0 || p >= whole1) q = edge(x, first + p * N, V);
             float v[N];
             ardiff::unpack(q, v, T());
             f(v, p);
@@ -324,15 +326,14 @@ __device__ __forceinline__ double sum_segments(const Part<T>& a, int& buf, doubl
     return s.total;
 }
 
-// In the CTA that owns segment s.owner: the index of the first value at which the running sum of f passes `target` (the last value
-// with anything, if none does), and that value. All threads of that CTA call it.
+// In the CTA that owns segment g: the index of the first value at which the running sum of f, `carry` before the segment, passes
+// `target` (the last value with anything, if none does). All threads of that CTA call it.
 template <typename T, typename F>
-__device__ __forceinline__ int locate(const Part<T>& a, double target, F&& f) {
+__device__ __forceinline__ int locate(const Part<T>& a, int g, double carry, double target, F&& f) {
     constexpr int N = Part<T>::N;
     Shared& s = *a.s;
-    const int g = s.owner % kSegments;
-    const int begin = g * a.segment, end = min(a.pieces, begin + a.segment);
-    double carry = s.before;
+    const int begin = g % kSegments * a.segment, end = min(a.pieces, begin + a.segment);
+    __syncthreads();
     if (threadIdx.x == 0) {
         s.found = INT_MAX;
         s.last = -1;
@@ -410,9 +411,7 @@ __device__ __forceinline__ void answer(const Args& a, int64_t row, int token, fl
 
 // The first CTA alone: s.list[0 .. n) holds every logit that may be kept. `whole`: the mass that top-p is a share of, where it is not
 // the list's own (negative). False, and nothing done, if the list ends before the nucleus does.
-template <typename T>
-__device__ __forceinline__ bool finish_list(const Args& args, int64_t row, const Part<T>& a, const Settings& o, int n, double whole) {
-    Shared& s = *a.s;
+__device__ __forceinline__ bool finish_list(const Args& args, int64_t row, Shared& s, const Weights& wt, const Settings& o, int n, double whole) {
     sort_list(s, n);
     const int j0 = kEach * threadIdx.x;
     const int limit = o.use_k ? min(o.k, n) : n;
@@ -422,7 +421,7 @@ __device__ __forceinline__ bool finish_list(const Args& args, int64_t row, const
     for (int i = 0; i < kEach; ++i) {
         e[i] = ~0ull;
         w[i] = 0.0;
-        if (j0 + i < limit) e[i] = s.list[j0 + i], w[i] = a.weight_drawn(entry_value(e[i]));
+        if (j0 + i < limit) e[i] = s.list[j0 + i], w[i] = wt.own(entry_value(e[i]));
         own += w[i];
     }
     double before = cta_scan(s, own, &total);
@@ -472,7 +471,7 @@ __device__ __forceinline__ bool finish_list(const Args& args, int64_t row, const
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         if (j == j0 + i) {
-            const double y = ((double)entry_value(e[i]) - (double)a.m) * a.a;
+            const double y = ((double)entry_value(e[i]) - wt.m) * wt.a;
             answer(args, row, (int)(drawn >> 32), (float)(y * 0.69314718055994530942 - log(total)));
         }
     }
@@ -489,6 +488,8 @@ __device__ __forceinline__ float distance_edge(int b) { return __uint_as_float((
 __device__ __forceinline__ int weight_bin(float d, float a32) {
     return __float_as_int(fminf(d * a32 * 16.0f, (float)(kBins - 1)) + 8388608.0f) - __float_as_int(8388608.0f);
 }
+
+__device__ __forceinline__ double weight_of_bin(int b) { return (double)ardiff::ex2(-0.0625f * (float)b); }
 
 __device__ __forceinline__ void clear_bins(Shared& s) {
 #pragma unroll
@@ -595,82 +596,77 @@ __device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough
     return true;
 }
 
-// The search for a prefix's last element among what `cut` keeps: the k-th (COUNT), or the first at which the mass reaches `enough`; then
-// r is the range of weight_bin's bins that a histogram over the same elements pointed to.
-template <typename T, bool COUNT>
-__device__ __noinline__ Cut search(const Part<T>& a, const Cut cut, unsigned k, double enough, Range r, int& buf) {
-    Shared& s = *a.s;
-    const float cut_value = value_of(cut.key);
-    auto kept = [&](float x, int i) { return x > cut_value || (x == cut_value && i <= cut.index) || cut.key == 0u; };
-    const float a32 = a.a32;
-    unsigned lo_key = key_of(-INFINITY) + 1, hi_key = key_of(a.m);       // where the element can be; masked logits are none
-    double hi_mass = 0.0;                                                // above hi_key
-    __syncthreads();                                                     // s.found and the histogram have been read
+// The first CTA alone: where in the sorted list (n entries, the elements next to `sure` in mass, or to `before` in number) the prefix
+// ends. s.verdict: 0 and s.cut its last element; 1, it lies above the list; 2, below.
+template <bool COUNT>
+__device__ __forceinline__ void end_in_list(Shared& s, const Weights& wt, int n, unsigned nth, double sure, double enough) {
+    sort_list(s, n);
     if (COUNT) {
-        clear_bins(s);
-        __syncthreads();
-        a.each([&](float x, int i) {
-            if (x > -INFINITY && kept(x, i)) count_bin(s, distance_bin(a.m - x));
-        });
-        a.sync();
-        pick<T, true>(a, k, enough, false, 0u, 0.0, [](int) { return 0.0; }, r);
-        if (r.before + r.in < k) {                                       // there are no more than k
-            a.sync();
-            return cut;
+        if (threadIdx.x == 0) {
+            const unsigned long long e = s.list[nth];
+            s.cut = Cut{entry_value(e), (int)(unsigned)e};
+            s.verdict = 0;
         }
+        return;
     }
-    // the range as keys: those of its elements' extremes
-    if (threadIdx.x == 0) {
-        s.kmin = UINT_MAX;
-        s.kmax = 0u;
+    if (threadIdx.x == 0) s.found = INT_MAX;
+    const int j0 = kEach * threadIdx.x;
+    double w[kEach], own = 0.0, all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        w[i] = j0 + i < n ? wt.own(entry_value(s.list[j0 + i])) : 0.0;
+        own += w[i];
+    }
+    double run = sure + cta_scan(s, own, &all);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        run += w[i];
+        if (j0 + i < n && run >= enough) atomicMin(&s.found, j0 + i);
     }
     __syncthreads();
-    {
-        unsigned lo = UINT_MAX, hi = 0u;
-        a.each([&](float x, int i) {
-            if (x > -INFINITY && kept(x, i)) {
-                const int b = COUNT ? distance_bin(a.m - x) : weight_bin(a.m - x, a32);
-                if (b >= r.first && b <= r.last) {
-                    const unsigned q = key_of(x);
-                    lo = min(lo, q);
-                    hi = max(hi, q);
-                }
-            }
-        });
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        if ((threadIdx.x & 31) == 0) {
-            atomicMin(&s.kmin, lo);
-            atomicMax(&s.kmax, hi);
+    if (threadIdx.x == 0) {
+        s.mass_in = sure + all;
+        s.verdict = sure >= enough ? 1 : s.found == INT_MAX ? 2 : 0;
+        if (s.verdict == 0) {
+            const unsigned long long e = s.list[s.found];
+            s.cut = Cut{entry_value(e), (int)(unsigned)e};
         }
     }
-    a.sync();
-    unsigned kmin = UINT_MAX, kmax = 0u;
-    for (int p = 0; p < a.parts; ++p) {
-        kmin = min(kmin, *a.at(&s.kmin, p));
-        kmax = max(kmax, *a.at(&s.kmax, p));
-    }
-    a.sync();
-    // The range shrinks to one bin of the histogram before it, or fits the list, at every step of the inner loop; with a wrong
-    // estimate everything on one side of it is done with, from the third time on half of the elements or more.
+}
+
+// The search for a prefix's last element among what `cut` keeps, by the logits as whole numbers: the k-th (COUNT), or the first at which
+// the mass reaches `enough`. Histograms narrow the range of numbers until few elements are in it or all are equal; an exact pass
+// sums what lies above, and a range that an estimate got wrong is done with, together with everything on its far side.
+template <typename T, bool COUNT>
+__device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32, const Cut cut, unsigned k, double enough, int& buf) {
+    Shared& s = *a.s;
+    const float m = (float)wt.m;
+    unsigned lo_key = key_of(-INFINITY) + 1, hi_key = key_of(m);         // where the element can be; masked logits are none
+    double hi_mass = 0.0;                                                // above hi_key
+    // The range shrinks to one bin of the histogram before it, or fits the list, at every step of the inner loop; of the outer one
+    // half of the elements or more are done with, from the third time on.
     for (int turn = 0; turn < 64; ++turn) {
-        // histograms over the keys, until few are left or all are equal
+        unsigned kmin = lo_key, kmax = hi_key;
+        Range r{0, 0, 0u, UINT_MAX, hi_mass};
         while (r.in == UINT_MAX || (r.in > (unsigned)kList && kmin < kmax)) {
             int shift = 0;
             while (((kmax - kmin) >> shift) >= (unsigned)kBins) ++shift;
+            a.sync();                                        // the last histograms have been read
             clear_bins(s);
             __syncthreads();
             a.each([&](float x, int i) {
                 const unsigned q = key_of(x);
-                if (q >= kmin && q <= kmax && kept(x, i)) count_bin(s, (int)((kmax - q) >> shift));        // largest first
+                if (q >= kmin && q <= kmax && cut.keeps(x, i)) count_bin(s, (int)((kmax - q) >> shift));   // largest first
             });
             a.sync();
-            const bool any = pick<T, COUNT>(a, k, enough, turn > 2, r.before, r.mass, [&](int b) {
+            const bool any = pick<T, COUNT>(a, k, enough, turn > 1, r.before, r.mass, [&](int b) {
                 const unsigned down = ((unsigned)b << shift) + (shift ? 1u << (shift - 1) : 0u);
-                return (double)ardiff::ex2((value_of(kmax - min(down, kmax - kmin)) - a.m) * a32);
+                return (double)ardiff::ex2((value_of(kmax - min(down, kmax - kmin)) - m) * a32);
             }, r);
-            a.sync();                                        // the histograms have been read
-            if (!any) return Cut{hi_key + 1, INT_MAX};       // nothing there: by the exact sums all above it is kept
+            if (!any || (COUNT && r.before + r.in < k)) {    // nothing there: all above it is kept; or all of fewer than k
+                a.sync();
+                return COUNT ? cut : Cut{value_of(hi_key + 1), INT_MAX};
+            }
             const unsigned top = kmax - ((unsigned)r.first << shift);
             const unsigned long long below = (unsigned long long)(r.last + 1) << shift;      // (up to 2^32)
             if (kmax - kmin >= below) kmin = kmax - (unsigned)below + 1;
@@ -679,63 +675,24 @@ __device__ __noinline__ Cut search(const Part<T>& a, const Cut cut, unsigned k, 
         // the exact sum above the range; the range's elements to the first CTA
         const float top = value_of(kmax), bottom = value_of(kmin);
         const bool ties = r.in > (unsigned)kList;
+        a.sync();
         if (threadIdx.x == 0) s.count = 0u;
         a.sync();
         double sure = 0.0;
-        if (!COUNT) sure = sum_segments(a, buf, 2.0, [&](float x, int i) { return x > top && kept(x, i) ? a.weight(x) : 0.0; });
+        if (!COUNT) sure = sum_segments(a, buf, 2.0, [&](float x, int i) { return x > top && cut.keeps(x, i) ? wt.own(x) : 0.0; });
         if (!ties) {
             a.each([&](float x, int i) {
-                if (x >= bottom && x <= top && kept(x, i)) {
+                if (x >= bottom && x <= top && cut.keeps(x, i)) {
                     const unsigned at = atomicAdd(a.at(&s.count, 0), 1u);
                     if (at < (unsigned)kList) *a.at(&s.list[at], 0) = entry(x, i);
                 }
             });
             a.sync();
-            if (a.rank == 0) {
-                const int n = (int)min(s.count, (unsigned)kList);
-                sort_list(s, n);
-                if (COUNT) {
-                    if (threadIdx.x == 0) {
-                        const unsigned long long e = s.list[k - r.before - 1];
-                        s.cut_key = ~(unsigned)(e >> 32);
-                        s.cut_index = (int)(unsigned)e;
-                        s.verdict = 0;
-                    }
-                } else {
-                    if (threadIdx.x == 0) s.found = INT_MAX;
-                    const int j0 = kEach * threadIdx.x;
-                    double w[kEach], own = 0.0, all;
-#pragma unroll
-                    for (int i = 0; i < kEach; ++i) {
-                        w[i] = j0 + i < n ? a.weight(entry_value(s.list[j0 + i])) : 0.0;
-                        own += w[i];
-                    }
-                    double run = sure + cta_scan(s, own, &all);
-#pragma unroll
-                    for (int i = 0; i < kEach; ++i) {
-                        run += w[i];
-                        if (j0 + i < n && run >= enough) atomicMin(&s.found, j0 + i);
-                    }
-                    __syncthreads();
-                    if (threadIdx.x == 0) {
-                        s.mass_in = sure + all;
-                        if (sure >= enough) {
-                            s.verdict = 1;                               // it lies above
-                        } else if (s.found == INT_MAX) {
-                            s.verdict = 2;                               // below
-                        } else {
-                            const unsigned long long e = s.list[s.found];
-                            s.cut_key = ~(unsigned)(e >> 32);
-                            s.cut_index = (int)(unsigned)e;
-                            s.verdict = 0;
-                        }
-                    }
-                }
-            }
+            if (a.rank == 0) end_in_list<COUNT>(s, wt, (int)min(s.count, (unsigned)kList), k - r.before - 1, sure, enough);
         } else {
             // one value, more often than the list is long: as many of it as are needed, lowest indices first
             double need = (double)(k - r.before);
-            const double w = COUNT ? 1.0 : a.weight(top);
+            const double w = COUNT ? 1.0 : wt.own(top);
             int verdict = 0;
             if (!COUNT) {
                 need = fmin(ceil((enough - sure) / w), (double)r.in + 1.0);
@@ -743,43 +700,36 @@ __device__ __noinline__ Cut search(const Part<T>& a, const Cut cut, unsigned k, 
                 while (need <= (double)r.in && sure + need * w < enough) need += 1.0;
                 verdict = sure >= enough ? 1 : need > (double)r.in ? 2 : 0;
             }
-            auto one = [&](float x, int i) { return x == top && kept(x, i) ? 1.0 : 0.0; };
+            auto one = [&](float x, int i) { return x == top && cut.keeps(x, i) ? 1.0 : 0.0; };
             // (the sum over all is r.in: the share of it is a whole number less a half, up to rounding)
             sum_segments(a, buf, (need - 0.5) / (double)r.in, one);
             const int owner = s.owner / kSegments;
             if (verdict == 0 && owner == a.rank) {
-                const int at = locate(a, need - 0.5, one);
-                if (threadIdx.x == 0) s.cut_index = at;
+                const int at = locate(a, s.owner, s.before, need - 0.5, one);
+                if (threadIdx.x == 0) s.cut = Cut{top, at};
             }
             a.sync();
             if (a.rank == 0 && threadIdx.x == 0) {
-                s.cut_key = kmax;
-                s.cut_index = *a.at(&s.cut_index, owner);
+                if (verdict == 0) s.cut = Cut{top, a.at(&s.cut, owner)->index};
                 s.verdict = verdict;
                 s.mass_in = sure + r.in * w;
             }
         }
         a.sync();
         const int verdict = *a.at(&s.verdict, 0);
-        const Cut found{*a.at(&s.cut_key, 0), *a.at(&s.cut_index, 0)};
+        const Cut found{a.at(&s.cut, 0)->value, a.at(&s.cut, 0)->index};
         const double with = *a.at(&s.mass_in, 0);
         a.sync();
         if (verdict == 0) return found;
-        // the estimates were wrong about the range: the exact sums say on which side of it the element lies
         if (verdict == 1) {
             lo_key = kmax + 1;
         } else {
             hi_key = kmin - 1;
             hi_mass = with;
         }
-        if (lo_key > hi_key) return Cut{hi_key + 1, INT_MAX};            // sums that differ in their last bit
-        kmin = lo_key;
-        kmax = hi_key;
-        r.in = UINT_MAX;                                     // not known: a histogram at least
-        r.before = 0;
-        r.mass = hi_mass;
+        if (lo_key > hi_key) break;                          // sums that differ in their last bit
     }
-    return Cut{hi_key + 1, INT_MAX};                         // (2^18 elements are halved 18 times)
+    return Cut{value_of(hi_key + 1), INT_MAX};
 }
 
 template <typename T>
@@ -805,7 +755,6 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     a.rank = blockIdx.x % args.parts;
     a.parts = args.parts;
     a.V = args.V;
-    a.tiny = o.u == 0.f;
     // the aligned pieces that cover the row; `shift` places in front of it belong to none of them
     a.x = static_cast<const T*>(args.x) + row * args.ld;
     const int shift = (int)((reinterpret_cast<uintptr_t>(a.x) & 15u) / sizeof(T));
@@ -826,7 +775,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
         if (a.whole0 <= most) {
             for (int p = tid; p < a.pieces; p += kGroups * kThreads) {
                 uint4 q[kGroups];
-                // (beyond the whole pieces the nearest of them once more, which changes no maximum but that group's)
+                // (beyond the whole pieces the nearest of them once more, which counts for nothing)
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) q[g] = __ldg(base + max(a.whole0, min(p + g * kThreads, most)));
 #pragma unroll
@@ -840,9 +789,9 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
             const int group = g * kThreads + tid;
-            if (a.whole0 == 1 && group == 0 && a.pieces > 0) top[g] = max_nan(top[g], ardiff::piece_max(a.edge(0), T()));
+            if (a.whole0 == 1 && group == 0 && a.pieces > 0) top[g] = max_nan(top[g], ardiff::piece_max(Part<T>::edge(a.x, a.first, a.V), T()));
             if (a.whole1 < a.pieces && (a.whole1 & (kGroups * kThreads - 1)) == group)
-                top[g] = max_nan(top[g], ardiff::piece_max(a.edge(a.whole1), T()));
+                top[g] = max_nan(top[g], ardiff::piece_max(Part<T>::edge(a.x, a.first + a.whole1 * N, a.V), T()));
         }
     }
     float own = top[0];
@@ -867,24 +816,29 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
         a.each_of([&](float v) { return v == own; }, [&](float v, int i) { if (v == own) atomicMin(&s.first, i); });
     if (tid == 0) s.cta_max = own;
     a.sync();
-    a.m = own;
-    for (int r = 0; r < a.parts; ++r) a.m = max_nan(a.m, *a.at(&s.cta_max, r));
-    if (!valid || !(fabsf(a.m) < INFINITY) || greedy) {
+    float m = own;
+    for (int r = 0; r < a.parts; ++r) m = max_nan(m, *a.at(&s.cta_max, r));
+    if (!valid || !(fabsf(m) < INFINITY) || greedy) {
         if (a.rank == 0 && tid == 0) {
             int token = -1;
-            if (valid && fabsf(a.m) < INFINITY) {
+            if (valid && fabsf(m) < INFINITY) {
                 token = INT_MAX;
                 for (int r = 0; r < a.parts; ++r)
-                    if (*a.at(&s.cta_max, r) == a.m) token = min(token, *a.at(&s.first, r));
+                    if (*a.at(&s.cta_max, r) == m) token = min(token, *a.at(&s.first, r));
             }
             answer(args, row, token, token >= 0 ? 0.f : NAN);
         }
         a.sync();
         return;
     }
-    a.a = 1.4426950408889634074 / (double)o.T;
-    a.a32 = (float)fmin(a.a, 3e38);
-    const float half = 0.5f * a.m;                           // (halves: a difference of two logits can pass fp32's range)
+    Weights wt;
+    wt.m = m;
+    wt.a = 1.4426950408889634074 / (double)o.T;
+    wt.lowest = (float)fmax(wt.m - 100.0 / wt.a, -3e38);
+    const double octaves = ((double)wt.lowest - wt.m) * wt.a;
+    wt.far = o.u == 0.f || octaves > -75.0 || octaves < -900.0;
+    const float a32 = (float)fmin(wt.a, 3e38);
+    const float half = 0.5f * m;                             // (halves: a difference of two logits can pass fp32's range)
     const float floor_ = o.use_m ? 0.5f * (log2f(o.mp) - 0.01f) : -INFINITY;
     int buf = 0;
     Cut cut = no_cut();
@@ -904,7 +858,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             for (int p = 0; p < a.parts; ++p) {
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
-                    const int b = distance_bin(a.m - *a.at(&s.top[g][tid], p));
+                    const int b = distance_bin(m - *a.at(&s.top[g][tid], p));
                     if (b < kBins - 1) count_bin(s, b);
                 }
             }
@@ -926,23 +880,29 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             // the whole mass, and a histogram that says about where the nucleus ends
             clear_bins(s);
             __syncthreads();
-            whole = sum_segments(a, buf, 2.0, [&](float v, int) {
-                const int b = weight_bin(a.m - v, a.a32);
+            auto count = [&](float v) {
+                const int b = weight_bin(m - v, a32);
                 if (b < kBins - 1) count_bin(s, b);
-                return a.weight(v);
-            });
-            pick<T, false>(a, 0u, (double)o.p * whole, false, 0u, 0.0,
-                           [&](int b) { return (double)ardiff::ex2(-0.0625f * (float)b); }, r);
+            };
+            if (wt.far) whole = sum_segments(a, buf, 2.0, [&](float v, int) { count(v); return wt.own(v); });
+            else whole = sum_segments(a, buf, 2.0, [&](float v, int) { count(v); return wt.bulk(v); });
+            pick<T, false>(a, 0u, (double)o.p * whole, false, 0u, 0.0, weight_of_bin, r);
             r.last = min(r.last, kBins - 2);                 // (the last bin was not counted)
             if (r.before + r.in <= (unsigned)kList) which = SHARE;
         } else {
-            which = WEIGHT;
+            // a list has no room for more groups than it has entries
+            int n = 0;
+            for (int p = 0; p < a.parts; ++p) {
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) n += __syncthreads_count((0.5f * *a.at(&s.top[g][tid], p) - half) * a32 >= floor_);
+            }
+            if (n <= kList) which = WEIGHT;
         }
         if (which != NONE) {
             auto listed = [&](float v) {
-                if (which == REACH) return a.m - v < reach;
-                if (which == WEIGHT) return (0.5f * v - half) * a.a32 >= floor_;
-                if (which == SHARE) return v > -INFINITY && weight_bin(a.m - v, a.a32) <= r.last;
+                if (which == REACH) return m - v < reach;
+                if (which == WEIGHT) return (0.5f * v - half) * a32 >= floor_;
+                if (which == SHARE) return v > -INFINITY && weight_bin(m - v, a32) <= r.last;
                 return v > -INFINITY;
             };
             a.each_of(listed, [&](float v, int i) {
@@ -955,7 +915,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             const unsigned n = *a.at(&s.count, 0);
             bool done = n <= (unsigned)kList;
             if (done && a.rank == 0) {
-                done = finish_list(args, row, a, o, (int)n, whole);
+                done = finish_list(args, row, s, wt, o, (int)n, whole);
                 if (tid == 0) s.verdict = done;
             }
             if (which == SHARE && n <= (unsigned)kList) {    // an estimate's list: it may have been too short
@@ -965,43 +925,95 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             a.sync();
             if (done) return;
         }
-        if (o.use_k) cut = search<T, true>(a, cut, (unsigned)o.k, 0.0, r, buf);
+        if (o.use_k) {
+            // the k-th by a histogram over all logits, and a list of its bin
+            __syncthreads();
+            clear_bins(s);
+            if (tid == 0) s.count = 0u;
+            __syncthreads();
+            a.each([&](float v, int) { if (v > -INFINITY) count_bin(s, distance_bin(m - v)); });
+            a.sync();
+            pick<T, true>(a, (unsigned)o.k, 0.0, false, 0u, 0.0, weight_of_bin, r);
+            if (r.before + r.in >= (unsigned)o.k) {          // (else there are fewer than k)
+                if (r.in <= (unsigned)kList) {
+                    a.each([&](float v, int i) {
+                        if (v > -INFINITY && distance_bin(m - v) == r.first) *a.at(&s.list[atomicAdd(a.at(&s.count, 0), 1u)], 0) = entry(v, i);
+                    });
+                    a.sync();
+                    if (a.rank == 0) end_in_list<true>(s, wt, (int)r.in, (unsigned)o.k - r.before - 1, 0.0, 0.0);
+                    a.sync();
+                    cut = Cut{a.at(&s.cut, 0)->value, a.at(&s.cut, 0)->index};
+                } else {
+                    cut = search<T, true>(a, wt, a32, cut, (unsigned)o.k, 0.0, buf);
+                }
+            }
+            a.sync();
+        }
         if (o.use_p) {
             if (o.use_k) {
-                const float c = value_of(cut.key);
-                __syncthreads();
                 clear_bins(s);
                 __syncthreads();
                 whole = sum_segments(a, buf, 2.0, [&](float v, int i) {
-                    if (!(cut.key == 0u || v > c || (v == c && i <= cut.index))) return 0.0;
-                    const int b = weight_bin(a.m - v, a.a32);
+                    if (!cut.keeps(v, i)) return 0.0;
+                    const int b = weight_bin(m - v, a32);
                     if (b < kBins - 1) count_bin(s, b);
-                    return a.weight(v);
+                    return wt.own(v);
                 });
-                pick<T, false>(a, 0u, (double)o.p * whole, false, 0u, 0.0,
-                               [&](int b) { return (double)ardiff::ex2(-0.0625f * (float)b); }, r);
-                r.last = min(r.last, kBins - 2);                 // (the last bin was not counted)
-                a.sync();                                    // the histograms have been read
+                pick<T, false>(a, 0u, (double)o.p * whole, false, 0u, 0.0, weight_of_bin, r);
+                r.last = min(r.last, kBins - 2);
             }
-            cut = search<T, false>(a, cut, 0u, fmax((double)o.p * whole, 1e-300), r, buf);       // at least one
+            const double enough = fmax((double)o.p * whole, 1e-300);                  // at least one
+            bool found = false;
+            if (r.in <= (unsigned)kList && !wt.far) {
+                // the sum of what lies above the histogram's range, and a list of what lies in it
+                a.sync();
+                if (tid == 0) s.count = 0u;
+                a.sync();
+                auto above = [&](float v, int i) {
+                    const int b = weight_bin(m - v, a32);
+                    const bool in = cut.keeps(v, i);
+                    if (b >= r.first && b <= r.last && in && v > -INFINITY) {
+                        const unsigned at = atomicAdd(a.at(&s.count, 0), 1u);
+                        if (at < (unsigned)kList) *a.at(&s.list[at], 0) = entry(v, i);
+                    }
+                    const double w = wt.bulk(v);
+                    return in && b < r.first ? w : 0.0;
+                };
+                const double sure = sum_segments(a, buf, 2.0, above);
+                if (a.rank == 0) end_in_list<false>(s, wt, (int)min(s.count, (unsigned)kList), 0u, sure, enough);
+                a.sync();
+                found = *a.at(&s.verdict, 0) == 0;
+                const Cut c{a.at(&s.cut, 0)->value, a.at(&s.cut, 0)->index};
+                a.sync();
+                if (found) cut = c;
+            }
+            if (!found) cut = search<T, false>(a, wt, a32, cut, 0u, enough, buf);
         }
     }
     // the draw among what the cut keeps
-    const float c = value_of(cut.key);
-    auto kept = [&](float v, int i) {
-        return (cut.key == 0u || v > c || (v == c && i <= cut.index)) && (!o.use_m || (0.5f * v - half) * a.a32 >= floor_);
-    };
+    auto kept = [&](float v, int i) { return cut.keeps(v, i) && (0.5f * v - half) * a32 >= floor_; };
     auto weight = [&](float v, int i) {
         if (!kept(v, i)) return 0.0;
-        const double w = a.tiny ? a.weight_drawn(v) : a.weight(v);
+        const double w = wt.own(v);
         return o.use_m && w < (double)o.mp ? 0.0 : w;
     };
-    const double total = sum_segments(a, buf, (double)o.u, weight);
+    const bool all = !(o.use_k || o.use_p || o.use_m);
+    double total;
+    if (wt.far || o.use_m) {
+        total = sum_segments(a, buf, (double)o.u, weight);
+    } else if (all) {
+        total = sum_segments(a, buf, (double)o.u, [&](float v, int) { return wt.bulk(v); });
+    } else {
+        total = sum_segments(a, buf, (double)o.u, [&](float v, int i) {
+            const double w = wt.bulk(v);
+            return cut.keeps(v, i) ? w : 0.0;
+        });
+    }
     a.sync();                                                // every CTA has read the others' sums
     if (s.owner / kSegments != a.rank) return;
-    const int token = locate(a, (double)o.u * total, weight);
+    const int token = locate(a, s.owner, s.before, (double)o.u * total, weight);
     if (tid == 0) {
-        const double y = ((double)ardiff::to_float(a.x[token]) - (double)a.m) * a.a;
+        const double y = ((double)ardiff::to_float(a.x[token]) - wt.m) * wt.a;
         answer(args, row, token, (float)(y * 0.69314718055994530942 - log(total)));
     }
 }
