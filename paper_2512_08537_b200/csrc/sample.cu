@@ -36,7 +36,6 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kGroups = 4;               // of a thread's pieces, each with its largest logit kept
 constexpr int kBins = 4 * kThreads;      // of a histogram, four a thread
-constexpr int kCopies = 4;               // of a histogram over all elements: neighbouring lanes count in different ones
 constexpr int kList = 4 * kThreads;      // logits that the first CTA sorts, four a thread
 constexpr int kEach = 4;                 // list entries, bins a thread
 constexpr int kSegments = 4 * kWarps;    // of a CTA's part, four a warp
@@ -65,6 +64,7 @@ struct Shared {
     float top[kGroups][kThreads];        // the groups' largest logits
     float warp_max[kWarps];
     double seg[2][kSegments];            // sums of the segments; two, so that one may still be read by another CTA
+    unsigned seg_ties[kSegments];
     double scan[kWarps];
     unsigned uscan[kWarps];
     double total, before;
@@ -79,11 +79,12 @@ struct Shared {
     unsigned pick_before, pick_after;
     int verdict;
     Cut cut;
+    unsigned cut_ahead;
     double mass_above, mass_in;
     unsigned short group[kGroups * kThreads];
     unsigned long long list[kList];
-    union {
-        unsigned hist[kBins * kCopies];
+    union alignas(16) {                  // (read in 16-byte pieces)
+        unsigned hist[kBins];
         double w[kList];
     };
 };
@@ -189,7 +190,7 @@ struct Part {                            // this CTA's part of its row
             for (int i = 0; i < N; ++i) f(v[i], first + p * N + i);
         });
     }
-    // f(value, index) for every value of the groups whose largest logit `any` accepts: a warp a group, lanes its pieces. All threads.
+    // f(value, index) for every value of the groups whose largest logit `any` accepts. All threads.
     template <typename G, typename F> __device__ __forceinline__ void each_of(G&& any, F&& f) const {
         if (threadIdx.x == 0) s->groups = 0u;
         __syncthreads();
@@ -197,12 +198,30 @@ struct Part {                            // this CTA's part of its row
         for (int g = 0; g < kGroups; ++g)
             if (any(s->top[g][threadIdx.x])) s->group[atomicAdd(&s->groups, 1u)] = (unsigned short)(g * kThreads + threadIdx.x);
         __syncthreads();
-        const int n = (int)s->groups, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        for (int i = warp; i < n; i += kWarps) {
-            scan(s->group[i] + lane * kGroups * kThreads, pieces, 32 * kGroups * kThreads, [&](const float (&v)[N], int p) {
+        // every thread takes pieces of them in turn, four loads at a time
+        const int turns = (pieces + kGroups * kThreads - 1) / (kGroups * kThreads), items = (int)s->groups * turns;
+        const uint4* base = reinterpret_cast<const uint4*>(x + first);
+        const int most = whole1 - 1;
+        for (int i0 = threadIdx.x; i0 < items; i0 += 4 * kThreads) {
+            uint4 q[4];
+            int at[4];
 #pragma unroll
-                for (int j = 0; j < N; ++j) f(v[j], first + p * N + j);
-            });
+            for (int j = 0; j < 4; ++j) {
+                const unsigned item = (unsigned)(i0 + j * kThreads);
+                at[j] = pieces;
+                if ((int)item < items) at[j] = s->group[item / turns] + (int)(item % turns) * kGroups * kThreads;
+                q[j] = uint4();
+                if (whole0 <= most && at[j] < pieces) q[j] = __ldg(base + max(whole0, min(at[j], most)));
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (at[j] >= pieces) continue;
+                if (at[j] < whole0 || at[j] >= whole1) q[j] = edge(x, first + at[j] * N, V);
+                float v[N];
+                ardiff::unpack(q[j], v, T());
+#pragma unroll
+                for (int i = 0; i < N; ++i) f(v[i], first + at[j] * N + i);
+            }
         }
     }
 };
@@ -259,9 +278,10 @@ __device__ __forceinline__ unsigned cta_scan(Shared& s, unsigned v, unsigned* to
 
 // Sums of f(value, index) over the segments; afterwards every CTA knows their sum (returned) and the first segment at whose end the
 // running sum is above `share` of it (the last one with anything, if none is: s.owner), and the sum before that (s.before). Two
-// calls in a row use different buffers: buf is turned.
+// calls in a row use different buffers: buf is turned, and says which one the last call used. (Not inlined: these loops get all
+// registers that way, and f's values lie in them.)
 template <typename T, typename F>
-__device__ __forceinline__ double sum_segments(const Part<T>& a, int& buf, double share, F&& f) {
+__device__ __noinline__ double sum_in(const Part<T> a, const int buf, const double share, const F f) {
     constexpr int N = Part<T>::N;
     Shared& s = *a.s;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -322,14 +342,18 @@ __device__ __forceinline__ double sum_segments(const Part<T>& a, int& buf, doubl
         }
     }
     __syncthreads();
-    buf ^= 1;
     return s.total;
+}
+template <typename T, typename F>
+__device__ __forceinline__ double sum_segments(const Part<T>& a, int& buf, double share, const F& f) {
+    buf ^= 1;
+    return sum_in<T, F>(a, buf, share, f);
 }
 
 // In the CTA that owns segment g: the index of the first value at which the running sum of f, `carry` before the segment, passes
 // `target` (the last value with anything, if none does). All threads of that CTA call it.
 template <typename T, typename F>
-__device__ __forceinline__ int locate(const Part<T>& a, int g, double carry, double target, F&& f) {
+__device__ __noinline__ int locate(const Part<T> a, const int g, double carry, const double target, const F f) {
     constexpr int N = Part<T>::N;
     Shared& s = *a.s;
     const int begin = g % kSegments * a.segment, end = min(a.pieces, begin + a.segment);
@@ -484,25 +508,23 @@ __device__ __forceinline__ int distance_bin(float d) {
     return min(max(b, 0), kBins - 1);
 }
 __device__ __forceinline__ float distance_edge(int b) { return __uint_as_float((unsigned)(b + (111 << 5)) << 18); }
-// By the weight, 16 bins an octave, 64 octaves (to the nearest whole number: adding 2^23 leaves it in the last bits).
-__device__ __forceinline__ int weight_bin(float d, float a32) {
-    return __float_as_int(fminf(d * a32 * 16.0f, (float)(kBins - 1)) + 8388608.0f) - __float_as_int(8388608.0f);
+// By the weight: a code of 2^14 steps an octave, up to 64 octaves (to the nearest whole number: adding 2^23 leaves it in the last
+// bits), of which a histogram takes the upper ten bits, and one over a single bin of it the lower ten.
+constexpr int kFine = 10, kCodes = kBins << kFine;
+__device__ __forceinline__ int weight_code(float d, float a32) {
+    return __float_as_int(fminf(d * a32 * 16384.0f, (float)(kCodes - 1)) + 8388608.0f) - __float_as_int(8388608.0f);
 }
+__device__ __forceinline__ double weight_of_bin(int b) { return (double)ardiff::ex2(-0.0625f * ((float)b + 0.5f)); }
 
-__device__ __forceinline__ double weight_of_bin(int b) { return (double)ardiff::ex2(-0.0625f * (float)b); }
-
-__device__ __forceinline__ void clear_bins(Shared& s) {
-#pragma unroll
-    for (int i = 0; i < kBins * kCopies / 4 / kThreads; ++i) reinterpret_cast<uint4*>(s.hist)[i * kThreads + threadIdx.x] = uint4();
-}
-__device__ __forceinline__ void count_bin(Shared& s, int b) { atomicAdd(&s.hist[b * kCopies + (threadIdx.x & (kCopies - 1))], 1u); }
+__device__ __forceinline__ void clear_bins(Shared& s) { reinterpret_cast<uint4*>(s.hist)[threadIdx.x] = uint4(); }
+__device__ __forceinline__ void count_bin(Shared& s, int b) { atomicAdd(&s.hist[b], 1u); }
 // The calling thread's bins of one histogram, kEach * threadIdx.x and the ones behind it.
 __device__ __forceinline__ void add_bins(const unsigned* hist, unsigned (&c)[kEach]) {
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const uint4 q = reinterpret_cast<const uint4*>(hist)[kEach * threadIdx.x + i];
-        c[i] += (q.x + q.y) + (q.z + q.w);
-    }
+    const uint4 q = reinterpret_cast<const uint4*>(hist)[threadIdx.x];
+    c[0] += q.x;
+    c[1] += q.y;
+    c[2] += q.z;
+    c[3] += q.w;
 }
 
 // What a histogram says about where a prefix ends: the bins, first to last (larger logits first), that hold its last element, the
@@ -515,9 +537,11 @@ struct Range {
 
 // Adds up the CTAs' histograms and picks the bin in which the count passes k (COUNT), the estimated mass `enough`, or the count half of
 // all (half: where estimates did not help). A bin that was found by an estimate comes with its neighbours, as far as the list
-// has room. before, mass: in front of the histogram. middle(b): a weight of bin b. False: there is nothing.
+// has room; if it has none, with `spread` of them on either side. before, mass: in front of the histogram; whole: the exact mass of all
+// that was counted, if it is known (then the estimates come from behind, where bins hold many elements each and their middles err
+// little), else negative. middle(b): a weight of bin b. False: there is nothing.
 template <typename T, bool COUNT, typename F>
-__device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough, bool half, unsigned before, double mass, F&& middle,
+__device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough, bool half, int spread, unsigned before, double mass, double whole, F&& middle,
                                      Range& r) {
     Shared& s = *a.s;
     const int b0 = kEach * threadIdx.x;
@@ -554,7 +578,8 @@ __device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough
             w[i] = c[i] ? c[i] * middle(b0 + i) : 0.0;
             sum += w[i];
         }
-        m[0] = mass + cta_scan(s, sum, &all);
+        m[0] = cta_scan(s, sum, &all);
+        m[0] += whole >= 0.0 ? whole - all : mass;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             m[i + 1] = m[i] + w[i];
@@ -573,7 +598,10 @@ __device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough
     const unsigned lo = s.pick_before, hi = s.pick_after, in = hi - lo;
     const unsigned more = COUNT || in > (unsigned)kList ? 0u : ((unsigned)kList - in) / 2;
     if (more == 0u) {
-        if (threadIdx.x == 0) s.pick_first = s.pick_last = found;
+        if (threadIdx.x == 0) {
+            s.pick_first = max(found - spread, 0);
+            s.pick_last = min(found + spread, kBins - 1);
+        }
     } else {                                                 // (empty bins at either end come along)
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
@@ -596,8 +624,84 @@ __device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough
     return true;
 }
 
-// The first CTA alone: where in the sorted list (n entries, the elements next to `sure` in mass, or to `before` in number) the prefix
-// ends. s.verdict: 0 and s.cut its last element; 1, it lies above the list; 2, below.
+// What the sums over segments add up, value by value.
+struct Bulk {                            // all weights
+    Weights wt;
+    __device__ __forceinline__ double operator()(float v, int) const { return wt.bulk(v); }
+};
+struct Drawn {                           // the weights of what is kept, exactly; floor: below it none has min_p (all halved)
+    Weights wt;
+    Cut cut;
+    float half, a32, floor;
+    double mp;
+    __device__ __forceinline__ double operator()(float v, int i) const {
+        if (!cut.keeps(v, i) || !((0.5f * v - half) * a32 >= floor)) return 0.0;
+        const double w = wt.own(v);
+        return w >= mp ? w : 0.0;
+    }
+};
+struct Kept {                            // the weights of what the cut keeps
+    Weights wt;
+    Cut cut;
+    __device__ __forceinline__ double operator()(float v, int i) const {
+        const double w = wt.bulk(v);
+        return cut.keeps(v, i) ? w : 0.0;
+    }
+};
+template <bool FAR>
+struct Counted {                         // the same, with a histogram of the weights (all but the last bin)
+    Weights wt;
+    Cut cut;
+    float m, a32;
+    unsigned* hist;
+    __device__ __forceinline__ double operator()(float v, int i) const {
+        const double w = FAR ? wt.own(v) : wt.bulk(v);
+        const bool in = cut.keeps(v, i);
+        const int b = weight_code(m - v, a32) >> kFine;
+        if (in && b < kBins - 1) atomicAdd(&hist[b], 1u);
+        return in ? w : 0.0;
+    }
+};
+struct Above {                           // the weights above a range of codes; what is in it goes to the list
+    Weights wt;
+    Cut cut;
+    float m, a32;
+    int first, last;
+    unsigned* count;                     // of the first CTA; NULL: no list
+    unsigned long long* list;
+    __device__ __forceinline__ double operator()(float v, int i) const {
+        const double w = wt.bulk(v);
+        const int code = weight_code(m - v, a32);
+        const bool in = cut.keeps(v, i);
+        if (in && count && code >= first && code <= last) {
+            const unsigned at = atomicAdd(count, 1u);
+            if (at < (unsigned)kList) list[at] = entry(v, i);
+        }
+        return in && code < first ? w : 0.0;
+    }
+};
+struct AboveValue {                      // the weights above a value
+    Weights wt;
+    Cut cut;
+    float top;
+    __device__ __forceinline__ double operator()(float v, int i) const { return v > top && cut.keeps(v, i) ? wt.own(v) : 0.0; }
+};
+struct Equal {                           // the number of elements of a value
+    Cut cut;
+    float value;
+    __device__ __forceinline__ double operator()(float v, int i) const { return v == value && cut.keeps(v, i) ? 1.0 : 0.0; }
+};
+
+// How many elements of weight w, next to `sure`, it takes to reach `enough`: `in` + 1 if there are not that many.
+__device__ __forceinline__ double needed(double enough, double sure, double w, unsigned in) {
+    double need = fmin(ceil((enough - sure) / w), (double)in + 1.0);
+    while (need > 1.0 && sure + (need - 1.0) * w >= enough) need -= 1.0;
+    while (need <= (double)in && sure + need * w < enough) need += 1.0;
+    return need;
+}
+
+// The first CTA alone: where in the sorted list (n entries, the elements next to `sure` in mass, or the nth in number) the prefix ends.
+// s.verdict: 0, and s.cut its last element (COUNT = false: also s.found, its place in the list); 1, it lies above the list; 2, below.
 template <bool COUNT>
 __device__ __forceinline__ void end_in_list(Shared& s, const Weights& wt, int n, unsigned nth, double sure, double enough) {
     sort_list(s, n);
@@ -632,6 +736,7 @@ __device__ __forceinline__ void end_in_list(Shared& s, const Weights& wt, int n,
             s.cut = Cut{entry_value(e), (int)(unsigned)e};
         }
     }
+    __syncthreads();
 }
 
 // The search for a prefix's last element among what `cut` keeps, by the logits as whole numbers: the k-th (COUNT), or the first at which
@@ -659,7 +764,7 @@ __device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32,
                 if (q >= kmin && q <= kmax && cut.keeps(x, i)) count_bin(s, (int)((kmax - q) >> shift));   // largest first
             });
             a.sync();
-            const bool any = pick<T, COUNT>(a, k, enough, turn > 1, r.before, r.mass, [&](int b) {
+            const bool any = pick<T, COUNT>(a, k, enough, turn > 1, 0, r.before, r.mass, -1.0, [&](int b) {
                 const unsigned down = ((unsigned)b << shift) + (shift ? 1u << (shift - 1) : 0u);
                 return (double)ardiff::ex2((value_of(kmax - min(down, kmax - kmin)) - m) * a32);
             }, r);
@@ -679,7 +784,7 @@ __device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32,
         if (threadIdx.x == 0) s.count = 0u;
         a.sync();
         double sure = 0.0;
-        if (!COUNT) sure = sum_segments(a, buf, 2.0, [&](float x, int i) { return x > top && cut.keeps(x, i) ? wt.own(x) : 0.0; });
+        if (!COUNT) sure = sum_segments(a, buf, 2.0, AboveValue{wt, cut, top});
         if (!ties) {
             a.each([&](float x, int i) {
                 if (x >= bottom && x <= top && cut.keeps(x, i)) {
@@ -691,21 +796,14 @@ __device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32,
             if (a.rank == 0) end_in_list<COUNT>(s, wt, (int)min(s.count, (unsigned)kList), k - r.before - 1, sure, enough);
         } else {
             // one value, more often than the list is long: as many of it as are needed, lowest indices first
-            double need = (double)(k - r.before);
             const double w = COUNT ? 1.0 : wt.own(top);
-            int verdict = 0;
-            if (!COUNT) {
-                need = fmin(ceil((enough - sure) / w), (double)r.in + 1.0);
-                while (need > 1.0 && sure + (need - 1.0) * w >= enough) need -= 1.0;
-                while (need <= (double)r.in && sure + need * w < enough) need += 1.0;
-                verdict = sure >= enough ? 1 : need > (double)r.in ? 2 : 0;
-            }
-            auto one = [&](float x, int i) { return x == top && cut.keeps(x, i) ? 1.0 : 0.0; };
+            const double need = COUNT ? (double)(k - r.before) : needed(enough, sure, w, r.in);
+            const int verdict = COUNT ? 0 : sure >= enough ? 1 : need > (double)r.in ? 2 : 0;
             // (the sum over all is r.in: the share of it is a whole number less a half, up to rounding)
-            sum_segments(a, buf, (need - 0.5) / (double)r.in, one);
+            sum_segments(a, buf, (need - 0.5) / (double)r.in, Equal{cut, top});
             const int owner = s.owner / kSegments;
             if (verdict == 0 && owner == a.rank) {
-                const int at = locate(a, s.owner, s.before, need - 0.5, one);
+                const int at = locate(a, s.owner, s.before, need - 0.5, Equal{cut, top});
                 if (threadIdx.x == 0) s.cut = Cut{top, at};
             }
             a.sync();
@@ -730,6 +828,33 @@ __device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32,
         if (lo_key > hi_key) break;                          // sums that differ in their last bit
     }
     return Cut{value_of(hi_key + 1), INT_MAX};
+}
+
+// The first CTA: the draw's segment, where the sum over segment g (of all CTAs') is in_segment(g); a thread a segment.
+template <typename T, typename F>
+__device__ __forceinline__ void draw_segment(const Part<T>& a, double u, F&& in_segment) {
+    static_assert(kMaxParts * kSegments <= kThreads, "a thread a segment");
+    Shared& s = *a.s;
+    const int g = threadIdx.x;
+    const double own = g < a.parts * kSegments ? in_segment(g) : 0.0;
+    double total;
+    const double before = cta_scan(s, own, &total);
+    if (g == 0) {
+        s.found = INT_MAX;
+        s.last = -1;
+    }
+    __syncthreads();
+    if (own > 0.0) {
+        atomicMax(&s.last, g);
+        if (before + own > u * total) atomicMin(&s.found, g);
+    }
+    __syncthreads();
+    if (g == (s.found != INT_MAX ? s.found : s.last)) {
+        s.owner = g;
+        s.before = before;
+        s.total = total;
+    }
+    __syncthreads();
 }
 
 template <typename T>
@@ -841,12 +966,16 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     const float half = 0.5f * m;                             // (halves: a difference of two logits can pass fp32's range)
     const float floor_ = o.use_m ? 0.5f * (log2f(o.mp) - 0.01f) : -INFINITY;
     int buf = 0;
-    Cut cut = no_cut();
+    Drawn drawn{wt, no_cut(), half, a32, floor_, o.use_m ? (double)o.mp : 0.0};
+    Cut& cut = drawn.cut;
+    int owner = -1;                                          // the draw's segment, where the search for the cut finds it
+    double before = 0.0, total = 0.0;
     if (o.use_k || o.use_p || o.use_m) {
         // which logits a list of all that may be kept has to hold, if there is a list
         enum { ALL, REACH, WEIGHT, SHARE, NONE } which = NONE;
         float reach = 0.f;
         Range r;
+        int last_code = 0;                                   // of a nucleus' end
         double whole = -1.0;
         if (args.V <= kList) {
             which = ALL;
@@ -863,9 +992,9 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                 }
             }
             __syncthreads();
-            unsigned c[kEach] = {}, total;
+            unsigned c[kEach] = {}, all;
             add_bins(s.hist, c);
-            unsigned n = cta_scan(s, (c[0] + c[1]) + (c[2] + c[3]), &total);
+            unsigned n = cta_scan(s, (c[0] + c[1]) + (c[2] + c[3]), &all);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 if (n < (unsigned)o.k && n + c[i] >= (unsigned)o.k) s.found = kEach * tid + i;
@@ -880,14 +1009,11 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             // the whole mass, and a histogram that says about where the nucleus ends
             clear_bins(s);
             __syncthreads();
-            auto count = [&](float v) {
-                const int b = weight_bin(m - v, a32);
-                if (b < kBins - 1) count_bin(s, b);
-            };
-            if (wt.far) whole = sum_segments(a, buf, 2.0, [&](float v, int) { count(v); return wt.own(v); });
-            else whole = sum_segments(a, buf, 2.0, [&](float v, int) { count(v); return wt.bulk(v); });
-            pick<T, false>(a, 0u, (double)o.p * whole, false, 0u, 0.0, weight_of_bin, r);
+            if (wt.far) whole = sum_segments(a, buf, 2.0, Counted<true>{wt, cut, m, a32, s.hist});
+            else whole = sum_segments(a, buf, 2.0, Counted<false>{wt, cut, m, a32, s.hist});
+            pick<T, false>(a, 0u, (double)o.p * whole, false, 1, 0u, 0.0, whole, weight_of_bin, r);
             r.last = min(r.last, kBins - 2);                 // (the last bin was not counted)
+            last_code = (r.last << kFine) + (1 << kFine) - 1;
             if (r.before + r.in <= (unsigned)kList) which = SHARE;
         } else {
             // a list has no room for more groups than it has entries
@@ -902,17 +1028,19 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             auto listed = [&](float v) {
                 if (which == REACH) return m - v < reach;
                 if (which == WEIGHT) return (0.5f * v - half) * a32 >= floor_;
-                if (which == SHARE) return v > -INFINITY && weight_bin(m - v, a32) <= r.last;
+                if (which == SHARE) return v > -INFINITY && weight_code(m - v, a32) <= last_code;
                 return v > -INFINITY;
             };
+            unsigned* count = a.at(&s.count, 0);
+            unsigned long long* list = a.at(s.list, 0);
             a.each_of(listed, [&](float v, int i) {
                 if (listed(v) && v > -INFINITY) {
-                    const unsigned at = atomicAdd(a.at(&s.count, 0), 1u);
-                    if (at < (unsigned)kList) *a.at(&s.list[at], 0) = entry(v, i);
+                    const unsigned at = atomicAdd(count, 1u);
+                    if (at < (unsigned)kList) list[at] = entry(v, i);
                 }
             });
             a.sync();
-            const unsigned n = *a.at(&s.count, 0);
+            const unsigned n = *count;
             bool done = n <= (unsigned)kList;
             if (done && a.rank == 0) {
                 done = finish_list(args, row, s, wt, o, (int)n, whole);
@@ -933,11 +1061,13 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             __syncthreads();
             a.each([&](float v, int) { if (v > -INFINITY) count_bin(s, distance_bin(m - v)); });
             a.sync();
-            pick<T, true>(a, (unsigned)o.k, 0.0, false, 0u, 0.0, weight_of_bin, r);
+            pick<T, true>(a, (unsigned)o.k, 0.0, false, 0, 0u, 0.0, -1.0, weight_of_bin, r);
             if (r.before + r.in >= (unsigned)o.k) {          // (else there are fewer than k)
                 if (r.in <= (unsigned)kList) {
+                    unsigned* count = a.at(&s.count, 0);
+                    unsigned long long* list = a.at(s.list, 0);
                     a.each([&](float v, int i) {
-                        if (v > -INFINITY && distance_bin(m - v) == r.first) *a.at(&s.list[atomicAdd(a.at(&s.count, 0), 1u)], 0) = entry(v, i);
+                        if (v > -INFINITY && distance_bin(m - v) == r.first) list[atomicAdd(count, 1u)] = entry(v, i);
                     });
                     a.sync();
                     if (a.rank == 0) end_in_list<true>(s, wt, (int)r.in, (unsigned)o.k - r.before - 1, 0.0, 0.0);
@@ -953,65 +1083,165 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             if (o.use_k) {
                 clear_bins(s);
                 __syncthreads();
-                whole = sum_segments(a, buf, 2.0, [&](float v, int i) {
-                    if (!cut.keeps(v, i)) return 0.0;
-                    const int b = weight_bin(m - v, a32);
-                    if (b < kBins - 1) count_bin(s, b);
-                    return wt.own(v);
-                });
-                pick<T, false>(a, 0u, (double)o.p * whole, false, 0u, 0.0, weight_of_bin, r);
+                if (wt.far) whole = sum_segments(a, buf, 2.0, Counted<true>{wt, cut, m, a32, s.hist});
+                else whole = sum_segments(a, buf, 2.0, Counted<false>{wt, cut, m, a32, s.hist});
+                pick<T, false>(a, 0u, (double)o.p * whole, false, 1, 0u, 0.0, whole, weight_of_bin, r);
                 r.last = min(r.last, kBins - 2);
+                last_code = (r.last << kFine) + (1 << kFine) - 1;
             }
             const double enough = fmax((double)o.p * whole, 1e-300);                  // at least one
-            bool found = false;
-            if (r.in <= (unsigned)kList && !wt.far) {
-                // the sum of what lies above the histogram's range, and a list of what lies in it
+            int first_code = r.first << kFine;
+            if (r.in > (unsigned)kList) {                    // a histogram of these three bins, four codes a bin
+                a.sync();                                    // the first has been read
+                clear_bins(s);
+                __syncthreads();
+                a.each([&](float v, int i) {
+                    const int code = weight_code(m - v, a32);
+                    if (code >= first_code && code <= last_code && cut.keeps(v, i)) count_bin(s, (code - first_code) >> 2);
+                });
                 a.sync();
-                if (tid == 0) s.count = 0u;
-                a.sync();
-                auto above = [&](float v, int i) {
-                    const int b = weight_bin(m - v, a32);
-                    const bool in = cut.keeps(v, i);
-                    if (b >= r.first && b <= r.last && in && v > -INFINITY) {
-                        const unsigned at = atomicAdd(a.at(&s.count, 0), 1u);
-                        if (at < (unsigned)kList) *a.at(&s.list[at], 0) = entry(v, i);
-                    }
-                    const double w = wt.bulk(v);
-                    return in && b < r.first ? w : 0.0;
-                };
-                const double sure = sum_segments(a, buf, 2.0, above);
-                if (a.rank == 0) end_in_list<false>(s, wt, (int)min(s.count, (unsigned)kList), 0u, sure, enough);
-                a.sync();
-                found = *a.at(&s.verdict, 0) == 0;
-                const Cut c{a.at(&s.cut, 0)->value, a.at(&s.cut, 0)->index};
-                a.sync();
-                if (found) cut = c;
+                pick<T, false>(a, 0u, enough, false, 0, r.before, r.mass, -1.0,
+                               [&](int b) { return (double)ardiff::ex2(-((float)(first_code + 4 * b) + 1.5f) * 0.00006103515625f); }, r);
+                last_code = min(last_code, first_code + 4 * r.last + 3);
+                first_code += 4 * r.first;
             }
-            if (!found) cut = search<T, false>(a, wt, a32, cut, 0u, enough, buf);
+            // the sum of what lies above the range; a list of what lies in it, or, where that is more than a list holds, whether it is
+            // one value, and how often in which segment
+            const bool listed = r.in <= (unsigned)kList;
+            a.sync();
+            if (tid == 0) {
+                s.count = 0u;
+                s.kmin = UINT_MAX;
+                s.kmax = 0u;
+                s.verdict = 1;
+            }
+            a.sync();
+            const double sure = wt.far ? 0.0 : sum_segments(a, buf, 2.0, Above{wt, cut, m, a32, first_code, last_code,
+                                                                               listed ? a.at(&s.count, 0) : nullptr, a.at(s.list, 0)});
+            // verdict of the first CTA: 0, the draw's segment is known; 1, nothing is; 2, min_p ends above the range, the cut is not needed
+            if (listed && !wt.far && a.rank == 0) {
+                const int n = (int)min(s.count, (unsigned)kList);
+                end_in_list<false>(s, wt, n, 0u, sure, enough);
+                if (s.verdict == 0) {
+                    const int kept = s.found + 1;
+                    const bool above = o.use_m && wt.own(entry_value(s.list[0])) < (double)o.mp;
+                    __syncthreads();                         // s.verdict and s.found have been read
+                    // what is kept of the list, in order of index
+                    unsigned long long e[kEach];
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) e[i] = s.list[kEach * tid + i];
+                    __syncthreads();
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) {
+                        const int j = kEach * tid + i;
+                        if (j < kept) {
+                            const double w = wt.own(entry_value(e[i]));
+                            s.list[j] = (e[i] & 0xffffffffull) << 32 | (unsigned)j;
+                            s.w[j] = o.use_m && w < (double)o.mp ? 0.0 : w;
+                        }
+                    }
+                    __syncthreads();
+                    sort_list(s, kept);
+                    draw_segment(a, (double)o.u, [&](int g) {
+                        // the entries from the segment's first index on, up to the next one's
+                        const int q0 = min(pieces, g / kSegments * per), mine = min(pieces, q0 + per) - q0;
+                        const int len = (mine + kSegments - 1) / kSegments, at = g % kSegments * len;
+                        const int begin = (q0 + min(mine, at)) * N - shift, end = (q0 + min(mine, at + len)) * N - shift;
+                        int lo = 0, hi = kept;
+                        while (lo < hi) {
+                            const int mid = (lo + hi) >> 1;
+                            if ((int)(s.list[mid] >> 32) < begin) lo = mid + 1; else hi = mid;
+                        }
+                        double sum = *a.at(&s.seg[buf][g % kSegments], g / kSegments);
+                        for (; lo < kept && (int)(s.list[lo] >> 32) < end; ++lo) sum += s.w[(unsigned)s.list[lo]];
+                        return sum;
+                    });
+                    if (tid == 0) s.verdict = above ? 2 : 0;
+                } else if (tid == 0) {
+                    s.verdict = 1;
+                }
+            }
+            double need = 0.0;
+            float value = 0.f;
+            if (!listed && !wt.far) {
+                unsigned lo = UINT_MAX, hi = 0u;
+                for (int g = warp * 4; g < warp * 4 + 4; ++g) {
+                    unsigned n = 0;
+                    a.scan(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const float (&v)[N], int p) {
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const int code = weight_code(m - v[i], a32);
+                            if (code >= first_code && code <= last_code && cut.keeps(v[i], a.first + p * N + i)) {
+                                ++n;
+                                lo = min(lo, key_of(v[i]));
+                                hi = max(hi, key_of(v[i]));
+                            }
+                        }
+                    });
+                    n = __reduce_add_sync(0xffffffffu, n);
+                    if (lane == 0) s.seg_ties[g] = n;
+                }
+                lo = __reduce_min_sync(0xffffffffu, lo);
+                hi = __reduce_max_sync(0xffffffffu, hi);
+                if (lane == 0) {
+                    atomicMin(&s.kmin, lo);
+                    atomicMax(&s.kmax, hi);
+                }
+                a.sync();
+                lo = UINT_MAX, hi = 0u;
+                for (int p = 0; p < a.parts; ++p) {
+                    lo = min(lo, *a.at(&s.kmin, p));
+                    hi = max(hi, *a.at(&s.kmax, p));
+                }
+                value = value_of(lo);
+                const double w = wt.own(value);
+                need = needed(enough, sure, w, r.in);
+                if (lo == hi && sure < enough && need <= (double)r.in && a.rank == 0) {
+                    const unsigned ties = tid < a.parts * kSegments ? *a.at(&s.seg_ties[tid % kSegments], tid / kSegments) : 0u;
+                    unsigned all;
+                    const unsigned ahead = cta_scan(s, ties, &all);
+                    draw_segment(a, (double)o.u, [&](int g) {
+                        return *a.at(&s.seg[buf][g % kSegments], g / kSegments) + w * fmin(fmax(need - (double)ahead, 0.0), (double)ties);
+                    });
+                    if (tid == s.owner) s.cut_ahead = ahead;
+                    if (tid == 0) s.verdict = o.use_m && w < (double)o.mp ? 2 : 0;
+                }
+            }
+            a.sync();
+            const int verdict = *a.at(&s.verdict, 0);
+            if (verdict == 0) {
+                owner = *a.at(&s.owner, 0);
+                before = *a.at(&s.before, 0);
+                total = *a.at(&s.total, 0);
+                if (listed) {
+                    cut = Cut{a.at(&s.cut, 0)->value, a.at(&s.cut, 0)->index};
+                } else {
+                    need -= (double)*a.at(&s.cut_ahead, 0);  // of this value in the draw's segment, lowest indices first
+                }
+            }
+            a.sync();
+            if (verdict == 0 && owner / kSegments != a.rank) return;
+            if (verdict == 0 && !listed) {
+                const unsigned ties = s.seg_ties[owner % kSegments];
+                int index = need <= 0.0 ? -1 : INT_MAX;
+                if (need > 0.0 && need < (double)ties) index = locate(a, owner, 0.0, need - 0.5, Equal{cut, value});
+                // (a cut before this one keeps all of the range or is its end)
+                cut = Cut{value, cut.value == value ? min(index, cut.index) : index};
+            }
+            if (verdict == 1) cut = search<T, false>(a, wt, a32, cut, 0u, enough, buf);
         }
     }
     // the draw among what the cut keeps
-    auto kept = [&](float v, int i) { return cut.keeps(v, i) && (0.5f * v - half) * a32 >= floor_; };
-    auto weight = [&](float v, int i) {
-        if (!kept(v, i)) return 0.0;
-        const double w = wt.own(v);
-        return o.use_m && w < (double)o.mp ? 0.0 : w;
-    };
-    const bool all = !(o.use_k || o.use_p || o.use_m);
-    double total;
-    if (wt.far || o.use_m) {
-        total = sum_segments(a, buf, (double)o.u, weight);
-    } else if (all) {
-        total = sum_segments(a, buf, (double)o.u, [&](float v, int) { return wt.bulk(v); });
-    } else {
-        total = sum_segments(a, buf, (double)o.u, [&](float v, int i) {
-            const double w = wt.bulk(v);
-            return cut.keeps(v, i) ? w : 0.0;
-        });
+    if (owner < 0) {
+        if (wt.far || o.use_m) total = sum_segments(a, buf, (double)o.u, drawn);
+        else if (o.use_k || o.use_p) total = sum_segments(a, buf, (double)o.u, Kept{wt, cut});
+        else total = sum_segments(a, buf, (double)o.u, Bulk{wt});
+        owner = s.owner;
+        before = s.before;
+        a.sync();                                            // every CTA has read the others' sums
+        if (owner / kSegments != a.rank) return;
     }
-    a.sync();                                                // every CTA has read the others' sums
-    if (s.owner / kSegments != a.rank) return;
-    const int token = locate(a, s.owner, s.before, (double)o.u * total, weight);
+    const int token = locate(a, owner, before, (double)o.u * total, drawn);
     if (tid == 0) {
         const double y = ((double)ardiff::to_float(a.x[token]) - wt.m) * wt.a;
         answer(args, row, token, (float)(y * 0.69314718055994530942 - log(total)));
