@@ -34,12 +34,13 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kGroups = 4;               // of a thread's pieces, each with its largest logit kept
 constexpr int kBins = 4 * kThreads;      // of a histogram, four a thread
 constexpr int kList = 4 * kThreads;      // logits that the first CTA sorts, four a thread
 constexpr int kEach = 4;                 // list entries, bins a thread
-constexpr int kSegments = 4 * kWarps;    // of a CTA's part, four a warp
+constexpr int kGroups = 4;               // segments a warp; a thread's share of one is a group, whose largest logit is kept
+constexpr int kSegments = kGroups * kWarps;  // of a CTA's part
 constexpr int kMaxParts = 8;
+constexpr float kSane = 6e4f;            // logits up to which, at temperatures from 1e-3 to 1e3, a first pass can sum
 constexpr double kFar = -100.0;          // weights below 2^kFar count as nothing: all of a row's add up to less than 2^-75 of its sum
 
 struct Args {
@@ -71,6 +72,7 @@ struct Shared {
     int owner;                           // segment in which a sum passes its target, of all CTAs'
     int found, last;
     float cta_max;
+    float ref;                           // what the part's sums of the first pass are relative to
     int first;                           // lowest index of the part's largest logit
     unsigned groups;                     // entries of `group`
     unsigned count;                      // entries of `list` (of the first CTA)
@@ -82,7 +84,7 @@ struct Shared {
     unsigned cut_ahead;
     double mass_above, mass_in;
     unsigned short group[kGroups * kThreads];
-    unsigned long long list[kList];
+    alignas(16) unsigned long long list[kList];
     union alignas(16) {                  // (read in 16-byte pieces)
         unsigned hist[kBins];
         double w[kList];
@@ -185,7 +187,7 @@ struct Part {                            // this CTA's part of its row
     // f(value, index) for every value of the calling warp's segments
     template <typename F> __device__ __forceinline__ void each(F&& f) const {
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        scan(warp * 4 * segment + lane, min(pieces, (warp + 1) * 4 * segment), 32, [&](const float (&v)[N], int p) {
+        scan(warp * kGroups * segment + lane, min(pieces, (warp + 1) * kGroups * segment), 32, [&](const float (&v)[N], int p) {
 #pragma unroll
             for (int i = 0; i < N; ++i) f(v[i], first + p * N + i);
         });
@@ -199,7 +201,7 @@ struct Part {                            // this CTA's part of its row
             if (any(s->top[g][threadIdx.x])) s->group[atomicAdd(&s->groups, 1u)] = (unsigned short)(g * kThreads + threadIdx.x);
         __syncthreads();
         // every thread takes pieces of them in turn, four loads at a time
-        const int turns = (pieces + kGroups * kThreads - 1) / (kGroups * kThreads), items = (int)s->groups * turns;
+        const int turns = (segment + 31) / 32, items = (int)s->groups * turns;
         const uint4* base = reinterpret_cast<const uint4*>(x + first);
         const int most = whole1 - 1;
         for (int i0 = threadIdx.x; i0 < items; i0 += 4 * kThreads) {
@@ -209,7 +211,10 @@ struct Part {                            // this CTA's part of its row
             for (int j = 0; j < 4; ++j) {
                 const unsigned item = (unsigned)(i0 + j * kThreads);
                 at[j] = pieces;
-                if ((int)item < items) at[j] = s->group[item / turns] + (int)(item % turns) * kGroups * kThreads;
+                if ((int)item < items) {
+                    const int id = s->group[item / turns], t = id & (kThreads - 1), in = (t & 31) + (int)(item % turns) * 32;
+                    if (in < segment) at[j] = min(pieces, ((t >> 5) * kGroups + id / kThreads) * segment + in);
+                }
                 q[j] = uint4();
                 if (whole0 <= most && at[j] < pieces) q[j] = __ldg(base + max(whole0, min(at[j], most)));
             }
@@ -280,22 +285,15 @@ __device__ __forceinline__ unsigned cta_scan(Shared& s, unsigned v, unsigned* to
 // running sum is above `share` of it (the last one with anything, if none is: s.owner), and the sum before that (s.before). Two
 // calls in a row use different buffers: buf is turned, and says which one the last call used. (Not inlined: these loops get all
 // registers that way, and f's values lie in them.)
-template <typename T, typename F>
-__device__ __noinline__ double sum_in(const Part<T> a, const int buf, const double share, const F f) {
-    constexpr int N = Part<T>::N;
+template <typename T>
+__device__ __noinline__ double add_segments(const Part<T> a, const int buf, const double share, const bool scaled, const Weights wt) {
     Shared& s = *a.s;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll 1
-    for (int g = warp * 4; g < warp * 4 + 4; ++g) {
-        double acc[2] = {0.0, 0.0};
-        a.scan(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const float (&v)[N], int p) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) acc[i & 1] += f(v[i], a.first + p * N + i);
-        });
-        const double mine = warp_sum(acc[0] + acc[1]);
-        if (lane == 0) s.seg[buf][g] = mine;
-    }
     a.sync();
+    if (scaled) {                                            // first-pass sums: from the part's own reference to the row's largest
+        if (threadIdx.x < kSegments) s.seg[buf][threadIdx.x] *= wt.own(s.ref);
+        a.sync();
+    }
     if (warp == 0) {
         constexpr int kPer = kMaxParts * kSegments / 32;
         double v[kPer], own = 0.0;
@@ -303,8 +301,9 @@ __device__ __noinline__ double sum_in(const Part<T> a, const int buf, const doub
         for (int i = 0; i < kPer; ++i) {
             const int g = lane * kPer + i;
             v[i] = g < a.parts * kSegments ? *a.at(&s.seg[buf][g % kSegments], g / kSegments) : 0.0;
-            own += v[i];
         }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) own += v[i];
         double inc = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -343,6 +342,23 @@ __device__ __noinline__ double sum_in(const Part<T> a, const int buf, const doub
     }
     __syncthreads();
     return s.total;
+}
+template <typename T, typename F>
+__device__ __noinline__ double sum_in(const Part<T> a, const int buf, const double share, const F f) {
+    constexpr int N = Part<T>::N;
+    Shared& s = *a.s;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int g = warp * kGroups; g < (warp + 1) * kGroups; ++g) {
+        double acc[2] = {0.0, 0.0};
+        a.scan(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const float (&v)[N], int p) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) acc[i & 1] += f(v[i], a.first + p * N + i);
+        });
+        const double mine = warp_sum(acc[0] + acc[1]);
+        if (lane == 0) s.seg[buf][g] = mine;
+    }
+    return add_segments(a, buf, share, false, Weights());
 }
 template <typename T, typename F>
 __device__ __forceinline__ double sum_segments(const Part<T>& a, int& buf, double share, const F& f) {
@@ -391,28 +407,87 @@ __device__ __noinline__ int locate(const Part<T> a, const int g, double carry, c
     return s.found != INT_MAX ? s.found : s.last;
 }
 
-// Sorts s.list[0 .. n), ascending, n <= kList; entries behind are overwritten.
-__device__ __forceinline__ void sort_list(Shared& s, int n) {
-    int size = 2;
-    while (size < n) size *= 2;
-    for (int i = n + threadIdx.x; i < size; i += kThreads) s.list[i] = ~0ull;
+// Sorts s.list[0 .. n), ascending, n <= kList; all entries but those of ~0 are different. Up to kThreads of them each counts the smaller
+// ones (64 take 0.3 us, where exchanging neighbours step by step took 2.7); beyond, each warp sorts 128 in its registers and
+// every entry looks itself up in the other warps' runs.
+__device__ __noinline__ void sort_list(Shared& s, const int n) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr unsigned long long kNone = ~0ull;
     __syncthreads();
-    const int pairs = size / 2;
-    const bool one_warp = pairs <= 32;
-    if (!one_warp || threadIdx.x < 32) {
-        for (int span = 2; span <= size; span *= 2) {
-            for (int step = span / 2; step > 0; step /= 2) {
-                for (int i = threadIdx.x; i < pairs; i += kThreads) {
-                    const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
-                    const unsigned long long x = s.list[lo], y = s.list[hi];
-                    if ((x > y) == ((lo & span) == 0)) {
-                        s.list[lo] = y;
-                        s.list[hi] = x;
-                    }
-                }
-                if (one_warp) __syncwarp(); else __syncthreads();
+    if (n <= kThreads) {
+        const unsigned long long key = tid < n ? s.list[tid] : kNone;
+        int rank = 0;
+        if (warp * 32 < n) {
+            int j = 0;
+#pragma unroll 4
+            for (; j + 1 < n; j += 2) {
+                const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&s.list[j]);
+                rank += (q.x < key) + (q.y < key);
+            }
+            if (j < n) rank += s.list[j] < key;
+        }
+        const int valid = __syncthreads_count(key != kNone);
+        if (key != kNone) s.list[rank] = key;
+        if (tid >= valid && tid < n) s.list[tid] = kNone;
+        __syncthreads();
+        return;
+    }
+    unsigned long long key[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) key[i] = 4 * tid + i < n ? s.list[4 * tid + i] : kNone;
+    auto order = [](unsigned long long& x, unsigned long long& y, bool up) {
+        if ((x > y) == up) {
+            const unsigned long long t = x;
+            x = y;
+            y = t;
+        }
+    };
+    // 128 in a warp, places 4 lane .. 4 lane + 3: runs of ever longer size, upwards and downwards in turn
+    order(key[0], key[1], true);
+    order(key[2], key[3], false);
+#pragma unroll
+    for (int size = 4; size <= 128; size *= 2) {
+        const bool up = (4 * lane & size) == 0;
+#pragma unroll
+        for (int step = size / 8; step > 0; step /= 2) {
+            const bool low = ((lane & step) == 0) == up;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned long long other = __shfl_xor_sync(0xffffffffu, key[i], step);
+                key[i] = (other < key[i]) == low ? other : key[i];
             }
         }
+        order(key[0], key[2], up);
+        order(key[1], key[3], up);
+        order(key[0], key[1], up);
+        order(key[2], key[3], up);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s.list[4 * tid + i] = key[i];
+    __syncthreads();
+    int rank[4], valid = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rank[i] = 4 * lane + i;
+    for (int run = 0; run < kWarps; ++run) {
+        if (run == warp || run * 128 >= n) continue;
+        const unsigned long long* r = s.list + run * 128;
+        int below[4] = {};
+#pragma unroll
+        for (int step = 64; step > 0; step /= 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (r[below[i] + step - 1] < key[i]) below[i] += step;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rank[i] += below[i] + (r[below[i]] < key[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) valid += __syncthreads_count(key[i] != kNone);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (key[i] != kNone) s.list[rank[i]] = key[i];
+        if (4 * tid + i >= valid) s.list[4 * tid + i] = kNone;
     }
     __syncthreads();
 }
@@ -434,8 +509,8 @@ __device__ __forceinline__ void answer(const Args& a, int64_t row, int token, fl
 }
 
 // The first CTA alone: s.list[0 .. n) holds every logit that may be kept. `whole`: the mass that top-p is a share of, where it is not
-// the list's own (negative). False, and nothing done, if the list ends before the nucleus does.
-__device__ __forceinline__ bool finish_list(const Args& args, int64_t row, Shared& s, const Weights& wt, const Settings& o, int n, double whole) {
+// the list's own (negative).
+__device__ __forceinline__ void finish_list(const Args& args, int64_t row, Shared& s, const Weights& wt, const Settings& o, int n, double whole) {
     sort_list(s, n);
     const int j0 = kEach * threadIdx.x;
     const int limit = o.use_k ? min(o.k, n) : n;
@@ -450,7 +525,6 @@ __device__ __forceinline__ bool finish_list(const Args& args, int64_t row, Share
     }
     double before = cta_scan(s, own, &total);
     const double enough = (double)o.p * (whole >= 0.0 ? whole : total);
-    if (o.use_p && whole >= 0.0 && total < enough) return false;
     bool keep[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -499,7 +573,6 @@ __device__ __forceinline__ bool finish_list(const Args& args, int64_t row, Share
             answer(args, row, (int)(drawn >> 32), (float)(y * 0.69314718055994530942 - log(total)));
         }
     }
-    return true;
 }
 
 // Bins of logits by their distance d below the largest. By the bits of d: 32 bins an octave, from 2^-16 to 2^16, the last bin beyond.
@@ -830,6 +903,52 @@ __device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32,
     return Cut{value_of(hi_key + 1), INT_MAX};
 }
 
+// The first pass: the groups' largest logits and, with SUMS, the sums of the segments, relative to the largest of the first few (s.ref: the
+// part's own, so that the row is read only once; a weight may be above 1 then).
+template <typename T, bool SUMS>
+__device__ __noinline__ void first_pass(const Part<T> a, const double scale) {
+    constexpr int N = Part<T>::N;
+    Shared& s = *a.s;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    Weights wt{};
+    if (SUMS) {
+        float ref = -INFINITY;
+        a.scan(warp * kGroups * a.segment + lane, min(a.pieces, warp * kGroups * a.segment + min(32, a.segment)), 32, [&](const float (&v)[N], int) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) ref = fmaxf(ref, v[i]);
+        });
+#pragma unroll
+        for (int q = 16; q > 0; q >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, q));
+        if (lane == 0) s.warp_max[warp] = ref;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) ref = fmaxf(ref, s.warp_max[w]);
+        ref = fminf(fmaxf(ref, -kSane), kSane);
+        if (tid == 0) s.ref = ref;
+        wt.m = ref;
+        wt.a = scale;
+        wt.lowest = (float)(wt.m - 100.0 / scale);
+    }
+#pragma unroll 1
+    for (int g = 0; g < kGroups; ++g) {
+        const int at = warp * kGroups + g;
+        float top = -INFINITY;
+        double acc[2] = {0.0, 0.0};
+        a.scan(at * a.segment + lane, min(a.pieces, (at + 1) * a.segment), 32, [&](const float (&v)[N], int) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                top = max_nan(top, v[i]);
+                if (SUMS) acc[i & 1] += wt.bulk(v[i]);
+            }
+        });
+        s.top[g][tid] = top;
+        if (SUMS) {
+            const double mine = warp_sum(acc[0] + acc[1]);
+            if (lane == 0) s.seg[0][at] = mine;
+        }
+    }
+}
+
 // The first CTA: the draw's segment, where the sum over segment g (of all CTAs') is in_segment(g); a thread a segment.
 template <typename T, typename F>
 __device__ __forceinline__ void draw_segment(const Part<T>& a, double u, F&& in_segment) {
@@ -891,40 +1010,16 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     a.first = p0 * N - shift;
     a.whole0 = a.first < 0 ? 1 : 0;
     a.whole1 = max(a.whole0, min(a.pieces, (args.V - a.first) / N));
-    float top[kGroups];
+    // the first pass sums, too, where all weights count and the temperature is one for which fp32 tells which logits are far below
+    const bool greedy = o.T == 0.f;
+    const double scale = 1.4426950408889634074 / (double)o.T;
+    const bool sums = valid && o.u > 0.f && o.T >= 1e-3f && o.T <= 1e3f && !o.use_k && (o.use_p ? args.V > kList : !o.use_m);
+    if (sums) first_pass<T, true>(a, scale);
+    else first_pass<T, false>(a, scale);
+    float own = s.top[0][tid];
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) top[g] = -INFINITY;
-    {
-        const uint4* base = reinterpret_cast<const uint4*>(a.x + a.first);
-        const int most = a.whole1 - 1;
-        if (a.whole0 <= most) {
-            for (int p = tid; p < a.pieces; p += kGroups * kThreads) {
-                uint4 q[kGroups];
-                // (beyond the whole pieces the nearest of them once more, which counts for nothing)
-#pragma unroll
-                for (int g = 0; g < kGroups; ++g) q[g] = __ldg(base + max(a.whole0, min(p + g * kThreads, most)));
-#pragma unroll
-                for (int g = 0; g < kGroups; ++g) {
-                    const int i = p + g * kThreads;
-                    if (i >= a.whole0 && i <= most) top[g] = max_nan(top[g], ardiff::piece_max(q[g], T()));
-                }
-            }
-        }
-        // the pieces that only partly lie in the row: their group's maximum has them too
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            const int group = g * kThreads + tid;
-            if (a.whole0 == 1 && group == 0 && a.pieces > 0) top[g] = max_nan(top[g], ardiff::piece_max(Part<T>::edge(a.x, a.first, a.V), T()));
-            if (a.whole1 < a.pieces && (a.whole1 & (kGroups * kThreads - 1)) == group)
-                top[g] = max_nan(top[g], ardiff::piece_max(Part<T>::edge(a.x, a.first + a.whole1 * N, a.V), T()));
-        }
-    }
-    float own = top[0];
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        s.top[g][tid] = top[g];
-        own = max_nan(own, top[g]);
-    }
+    for (int g = 1; g < kGroups; ++g) own = max_nan(own, s.top[g][tid]);
+    __syncthreads();
 #pragma unroll
     for (int q = 16; q > 0; q >>= 1) own = max_nan(own, __shfl_xor_sync(0xffffffffu, own, q));
     if (lane == 0) s.warp_max[warp] = own;
@@ -936,13 +1031,15 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     own = s.warp_max[0];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) own = max_nan(own, s.warp_max[w]);
-    const bool greedy = o.T == 0.f;
     if (greedy)                                              // the lowest index of this part's largest
         a.each_of([&](float v) { return v == own; }, [&](float v, int i) { if (v == own) atomicMin(&s.first, i); });
     if (tid == 0) s.cta_max = own;
     a.sync();
-    float m = own;
-    for (int r = 0; r < a.parts; ++r) m = max_nan(m, *a.at(&s.cta_max, r));
+    float m = own, ref = sums ? s.ref : 0.f;                  // of all parts; the lowest reference
+    for (int r = 0; r < a.parts; ++r) {
+        m = max_nan(m, *a.at(&s.cta_max, r));
+        if (sums) ref = fminf(ref, *a.at(&s.ref, r));
+    }
     if (!valid || !(fabsf(m) < INFINITY) || greedy) {
         if (a.rank == 0 && tid == 0) {
             int token = -1;
@@ -958,13 +1055,15 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     }
     Weights wt;
     wt.m = m;
-    wt.a = 1.4426950408889634074 / (double)o.T;
+    wt.a = scale;
     wt.lowest = (float)fmax(wt.m - 100.0 / wt.a, -3e38);
     const double octaves = ((double)wt.lowest - wt.m) * wt.a;
     wt.far = o.u == 0.f || octaves > -75.0 || octaves < -900.0;
     const float a32 = (float)fmin(wt.a, 3e38);
     const float half = 0.5f * m;                             // (halves: a difference of two logits can pass fp32's range)
     const float floor_ = o.use_m ? 0.5f * (log2f(o.mp) - 0.01f) : -INFINITY;
+    // (what is too far above a part's reference has overflowed)
+    const bool summed = sums && fabsf(m) <= kSane && ((double)m - (double)ref) * scale <= 900.0;
     int buf = 0;
     Drawn drawn{wt, no_cut(), half, a32, floor_, o.use_m ? (double)o.mp : 0.0};
     Cut& cut = drawn.cut;
@@ -972,63 +1071,63 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     double before = 0.0, total = 0.0;
     if (o.use_k || o.use_p || o.use_m) {
         // which logits a list of all that may be kept has to hold, if there is a list
-        enum { ALL, REACH, WEIGHT, SHARE, NONE } which = NONE;
+        enum { ALL, REACH, WEIGHT, NONE } which = NONE;
         float reach = 0.f;
         Range r;
         int last_code = 0;                                   // of a nucleus' end
         double whole = -1.0;
         if (args.V <= kList) {
             which = ALL;
-        } else if (o.use_k) {
-            // by the groups' largest logits: at least k logits are not below the k-th of them
+        } else {
+            if (o.use_p && !o.use_k) {
+                if (summed) whole = add_segments(a, buf, 2.0, true, wt);
+                else if (wt.far) whole = sum_segments(a, buf, 2.0, AboveValue{wt, cut, -INFINITY});
+                else whole = sum_segments(a, buf, 2.0, Bulk{wt});
+            }
+            // by the groups' largest logits: at least k logits are not below the k-th of them, and the mass down to one of them is at
+            // least theirs (in whole steps of 2^-18, rounded down)
             clear_bins(s);
             if (tid == 0) s.found = INT_MAX;
             __syncthreads();
-            for (int p = 0; p < a.parts; ++p) {
+            unsigned groups = 0;
 #pragma unroll
-                for (int g = 0; g < kGroups; ++g) {
-                    const int b = distance_bin(m - *a.at(&s.top[g][tid], p));
-                    if (b < kBins - 1) count_bin(s, b);
+            for (int g = 0; g < kGroups; ++g) {
+                const float v = s.top[g][tid];
+                if (o.use_k || o.use_p) {
+                    const int b = distance_bin(m - v);
+                    if (b < kBins - 1)
+                        atomicAdd(&s.hist[b], o.use_k ? 1u : (unsigned)(0.9999f * 262144.0f * ardiff::ex2((v - m) * a32)));
+                } else {
+                    groups += __syncthreads_count((0.5f * v - half) * a32 >= floor_);
                 }
             }
-            __syncthreads();
-            unsigned c[kEach] = {}, all;
-            add_bins(s.hist, c);
-            unsigned n = cta_scan(s, (c[0] + c[1]) + (c[2] + c[3]), &all);
+            if (tid == 0) s.groups = groups;
+            a.sync();
+            if (o.use_k || o.use_p) {
+                unsigned c[kEach] = {}, all;
+                for (int p = 0; p < a.parts; ++p) add_bins(a.at(s.hist, p), c);
+                unsigned n = cta_scan(s, (c[0] + c[1]) + (c[2] + c[3]), &all);
+                const double goal = o.use_k ? (double)o.k : fmax((double)o.p * whole * 262144.0, 1.0);
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                if (n < (unsigned)o.k && n + c[i] >= (unsigned)o.k) s.found = kEach * tid + i;
-                n += c[i];
+                for (int i = 0; i < kEach; ++i) {
+                    if ((double)n < goal && (double)(n + c[i]) >= goal) s.found = kEach * tid + i;
+                    n += c[i];
+                }
+                __syncthreads();
+                if (s.found != INT_MAX) {
+                    which = REACH;
+                    reach = distance_edge(s.found + 1);
+                }
+            } else {                                         // a list has no room for more groups than it has entries
+                for (int p = 0; p < a.parts; ++p) groups = p == 0 ? *a.at(&s.groups, 0) : groups + *a.at(&s.groups, p);
+                if (groups <= (unsigned)kList) which = WEIGHT;
             }
-            __syncthreads();
-            if (s.found != INT_MAX) {
-                which = REACH;
-                reach = distance_edge(s.found + 1);
-            }
-        } else if (o.use_p) {
-            // the whole mass, and a histogram that says about where the nucleus ends
-            clear_bins(s);
-            __syncthreads();
-            if (wt.far) whole = sum_segments(a, buf, 2.0, Counted<true>{wt, cut, m, a32, s.hist});
-            else whole = sum_segments(a, buf, 2.0, Counted<false>{wt, cut, m, a32, s.hist});
-            pick<T, false>(a, 0u, (double)o.p * whole, false, 1, 0u, 0.0, whole, weight_of_bin, r);
-            r.last = min(r.last, kBins - 2);                 // (the last bin was not counted)
-            last_code = (r.last << kFine) + (1 << kFine) - 1;
-            if (r.before + r.in <= (unsigned)kList) which = SHARE;
-        } else {
-            // a list has no room for more groups than it has entries
-            int n = 0;
-            for (int p = 0; p < a.parts; ++p) {
-#pragma unroll
-                for (int g = 0; g < kGroups; ++g) n += __syncthreads_count((0.5f * *a.at(&s.top[g][tid], p) - half) * a32 >= floor_);
-            }
-            if (n <= kList) which = WEIGHT;
+            a.sync();                                        // the others' bins have been read
         }
         if (which != NONE) {
             auto listed = [&](float v) {
                 if (which == REACH) return m - v < reach;
                 if (which == WEIGHT) return (0.5f * v - half) * a32 >= floor_;
-                if (which == SHARE) return v > -INFINITY && weight_code(m - v, a32) <= last_code;
                 return v > -INFINITY;
             };
             unsigned* count = a.at(&s.count, 0);
@@ -1041,17 +1140,11 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             });
             a.sync();
             const unsigned n = *count;
-            bool done = n <= (unsigned)kList;
-            if (done && a.rank == 0) {
-                done = finish_list(args, row, s, wt, o, (int)n, whole);
-                if (tid == 0) s.verdict = done;
-            }
-            if (which == SHARE && n <= (unsigned)kList) {    // an estimate's list: it may have been too short
-                a.sync();
-                done = *a.at(&s.verdict, 0);
-            }
             a.sync();
-            if (done) return;
+            if (n <= (unsigned)kList) {
+                if (a.rank == 0) finish_list(args, row, s, wt, o, (int)n, whole);
+                return;
+            }
         }
         if (o.use_k) {
             // the k-th by a histogram over all logits, and a list of its bin
@@ -1080,15 +1173,22 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             a.sync();
         }
         if (o.use_p) {
+            // a histogram that says about where the nucleus ends
+            clear_bins(s);
+            __syncthreads();
             if (o.use_k) {
-                clear_bins(s);
-                __syncthreads();
                 if (wt.far) whole = sum_segments(a, buf, 2.0, Counted<true>{wt, cut, m, a32, s.hist});
                 else whole = sum_segments(a, buf, 2.0, Counted<false>{wt, cut, m, a32, s.hist});
-                pick<T, false>(a, 0u, (double)o.p * whole, false, 1, 0u, 0.0, whole, weight_of_bin, r);
-                r.last = min(r.last, kBins - 2);
-                last_code = (r.last << kFine) + (1 << kFine) - 1;
+            } else {
+                a.each([&](float v, int) {
+                    const int b = weight_code(m - v, a32) >> kFine;
+                    if (b < kBins - 1) count_bin(s, b);
+                });
+                a.sync();
             }
+            pick<T, false>(a, 0u, (double)o.p * whole, false, 1, 0u, 0.0, whole, weight_of_bin, r);
+            r.last = min(r.last, kBins - 2);                 // (the last bin was not counted)
+            last_code = (r.last << kFine) + (1 << kFine) - 1;
             const double enough = fmax((double)o.p * whole, 1e-300);                  // at least one
             int first_code = r.first << kFine;
             if (r.in > (unsigned)kList) {                    // a histogram of these three bins, four codes a bin
@@ -1235,6 +1335,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     if (owner < 0) {
         if (wt.far || o.use_m) total = sum_segments(a, buf, (double)o.u, drawn);
         else if (o.use_k || o.use_p) total = sum_segments(a, buf, (double)o.u, Kept{wt, cut});
+        else if (summed) total = add_segments(a, buf, (double)o.u, true, wt);
         else total = sum_segments(a, buf, (double)o.u, Bulk{wt});
         owner = s.owner;
         before = s.before;
