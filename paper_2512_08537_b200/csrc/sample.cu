@@ -164,70 +164,45 @@ struct Part {                            // this CTA's part of its row
         for (int i = 0; i < N; ++i) v[i] = e + i >= 0 && e + i < V ? ardiff::to_float(x[e + i]) : -INFINITY;
         return ardiff::pack(v, T());
     }
-    // f(values, piece) for pieces begin, begin + step, ... below end; four loads at a time
-    template <typename F> __device__ __forceinline__ void scan(int begin, int end, int step, F&& f) const {
+    // f(piece's bits, piece) for pieces begin, begin + step, ... below end; AHEAD loads at a time
+    template <int AHEAD, typename F> __device__ __forceinline__ void scan(int begin, int end, int step, F&& f) const {
         const uint4* base = reinterpret_cast<const uint4*>(x + first);     // (aligned; pieces whole0 .. whole1 - 1 are read)
-        auto one = [&](uint4 q, int p) {
-            if (p < whole0 || p >= whole1) q = edge(x, first + p * N, V);
-            float v[N];
-            ardiff::unpack(q, v, T());
-            f(v, p);
-        };
         const int most = whole1 - 1;
-        int p = begin;
-        for (; p + 3 * step < end; p += 4 * step) {
-            uint4 q[4];
+#pragma unroll 1
+        for (int p = begin; p < end; p += AHEAD * step) {
+            uint4 q[AHEAD];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = __ldg(base + max(whole0, min(p + i * step, most)));
+            for (int i = 0; i < AHEAD; ++i) q[i] = whole0 <= most ? __ldg(base + max(whole0, min(p + i * step, most))) : uint4();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) one(q[i], p + i * step);
+            for (int i = 0; i < AHEAD; ++i) {
+                const int at = p + i * step;
+                if (at >= end) break;
+                if (at < whole0 || at >= whole1) q[i] = edge(x, first + at * N, V);
+                f(q[i], at);
+            }
         }
-        for (; p < end; p += step) one(whole0 <= most ? __ldg(base + max(whole0, min(p, most))) : uint4(), p);
     }
-    // f(value, index) for every value of the calling warp's segments
+    // f(value, index) for every value of the calling warp's segments (once in the code: not for what has to be fast)
     template <typename F> __device__ __forceinline__ void each(F&& f) const {
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        scan(warp * kGroups * segment + lane, min(pieces, (warp + 1) * kGroups * segment), 32, [&](const float (&v)[N], int p) {
+        scan<2>(warp * kGroups * segment + lane, min(pieces, (warp + 1) * kGroups * segment), 32, [&](const uint4& q, int p) {
+            float v[N];
+            ardiff::unpack(q, v, T());
 #pragma unroll
             for (int i = 0; i < N; ++i) f(v[i], first + p * N + i);
         });
     }
-    // f(value, index) for every value of the groups whose largest logit `any` accepts. All threads.
-    template <typename G, typename F> __device__ __forceinline__ void each_of(G&& any, F&& f) const {
-        if (threadIdx.x == 0) s->groups = 0u;
-        __syncthreads();
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g)
-            if (any(s->top[g][threadIdx.x])) s->group[atomicAdd(&s->groups, 1u)] = (unsigned short)(g * kThreads + threadIdx.x);
-        __syncthreads();
-        // every thread takes pieces of them in turn, four loads at a time
-        const int turns = (segment + 31) / 32, items = (int)s->groups * turns;
-        const uint4* base = reinterpret_cast<const uint4*>(x + first);
-        const int most = whole1 - 1;
-        for (int i0 = threadIdx.x; i0 < items; i0 += 4 * kThreads) {
-            uint4 q[4];
-            int at[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const unsigned item = (unsigned)(i0 + j * kThreads);
-                at[j] = pieces;
-                if ((int)item < items) {
-                    const int id = s->group[item / turns], t = id & (kThreads - 1), in = (t & 31) + (int)(item % turns) * 32;
-                    if (in < segment) at[j] = min(pieces, ((t >> 5) * kGroups + id / kThreads) * segment + in);
-                }
-                q[j] = uint4();
-                if (whole0 <= most && at[j] < pieces) q[j] = __ldg(base + max(whole0, min(at[j], most)));
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (at[j] >= pieces) continue;
-                if (at[j] < whole0 || at[j] >= whole1) q[j] = edge(x, first + at[j] * N, V);
-                float v[N];
-                ardiff::unpack(q[j], v, T());
-#pragma unroll
-                for (int i = 0; i < N; ++i) f(v[i], first + at[j] * N + i);
-            }
-        }
+};
+
+// Which logits go on a list.
+struct Listed {
+    enum { ALL, REACH, WEIGHT, EQUAL } which;
+    float m, bound, half, a32;           // REACH: nearer to m than bound; WEIGHT: half the exponent at least bound; EQUAL: bound
+    __device__ __forceinline__ bool operator()(float v) const {
+        if (which == REACH) return m - v < bound;
+        if (which == WEIGHT) return (0.5f * v - half) * a32 >= bound;
+        if (which == EQUAL) return v == bound;
+        return v > -INFINITY;
     }
 };
 
@@ -238,7 +213,7 @@ __device__ __forceinline__ double warp_sum(double v) {
 }
 
 // Exclusive sums over the CTA's threads; *total: of all.
-__device__ __forceinline__ double cta_scan(Shared& s, double v, double* total) {
+__device__ __noinline__ double cta_scan(Shared& s, double v, double* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     double inc = v;
 #pragma unroll
@@ -260,7 +235,7 @@ __device__ __forceinline__ double cta_scan(Shared& s, double v, double* total) {
     *total = all;
     return before + ex;
 }
-__device__ __forceinline__ unsigned cta_scan(Shared& s, unsigned v, unsigned* total) {
+__device__ __noinline__ unsigned cta_scan(Shared& s, unsigned v, unsigned* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned inc = v;
 #pragma unroll
@@ -351,7 +326,9 @@ __device__ __noinline__ double sum_in(const Part<T> a, const int buf, const doub
 #pragma unroll 1
     for (int g = warp * kGroups; g < (warp + 1) * kGroups; ++g) {
         double acc[2] = {0.0, 0.0};
-        a.scan(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const float (&v)[N], int p) {
+        a.template scan<F::kHot ? 2 : 1>(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const uint4& q, int p) {
+            float v[N];
+            ardiff::unpack(q, v, T());
 #pragma unroll
             for (int i = 0; i < N; ++i) acc[i & 1] += f(v[i], a.first + p * N + i);
         });
@@ -381,7 +358,9 @@ __device__ __noinline__ int locate(const Part<T> a, const int g, double carry, c
     for (int p0 = begin; p0 < end; p0 += kThreads) {
         const int p = p0 + threadIdx.x, e = a.first + p * N;
         double w[N], own = 0.0;
-        a.scan(p, min(end, p + 1), 1, [&](const float (&v)[N], int) {
+        a.template scan<1>(p, min(end, p + 1), 1, [&](const uint4& q, int) {
+            float v[N];
+            ardiff::unpack(q, v, T());
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 w[i] = f(v[i], e + i);
@@ -497,6 +476,63 @@ __device__ __forceinline__ unsigned long long entry(float x, int index) {
 }
 __device__ __forceinline__ float entry_value(unsigned long long e) { return value_of(~(unsigned)(e >> 32)); }
 
+// Takes every value that is to be listed out of the groups whose largest logit is: to the list of the first CTA (*count, list), or, of
+// EQUAL ones, the lowest index to *lowest. All threads.
+template <typename T>
+__device__ __noinline__ void collect(const Part<T> a, const Listed listed, unsigned* count, unsigned long long* list, int* lowest) {
+    constexpr int N = Part<T>::N;
+    Shared& s = *a.s;
+    if (threadIdx.x == 0) s.groups = 0u;
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+        if (listed(s.top[g][threadIdx.x])) s.group[atomicAdd(&s.groups, 1u)] = (unsigned short)(g * kThreads + threadIdx.x);
+    __syncthreads();
+    // every thread takes pieces of them in turn, four loads at a time
+    const int turns = (a.segment + 31) / 32, items = (int)s.groups * turns;
+    const uint4* base = reinterpret_cast<const uint4*>(a.x + a.first);
+    const int most = a.whole1 - 1;
+#pragma unroll 1
+    for (int i0 = threadIdx.x; i0 < items; i0 += 4 * kThreads) {
+        uint4 q[4];
+        int at[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const unsigned item = (unsigned)(i0 + j * kThreads);
+            at[j] = a.pieces;
+            if ((int)item < items) {
+                const int id = s.group[item / turns], t = id & (kThreads - 1), in = (t & 31) + (int)(item % turns) * 32;
+                if (in < a.segment) at[j] = min(a.pieces, ((t >> 5) * kGroups + id / kThreads) * a.segment + in);
+            }
+            q[j] = a.whole0 <= most && at[j] < a.pieces ? __ldg(base + max(a.whole0, min(at[j], most))) : uint4();
+        }
+        // (one copy of what follows: the pieces move down)
+#pragma unroll 1
+        for (int j = 0; j < 4; ++j) {
+            if (at[0] < a.pieces) {
+                if (at[0] < a.whole0 || at[0] >= a.whole1) q[0] = Part<T>::edge(a.x, a.first + at[0] * N, a.V);
+                float v[N];
+                ardiff::unpack(q[0], v, T());
+                unsigned hit = 0;
+#pragma unroll
+                for (int i = 0; i < N; ++i) hit |= listed(v[i]) && v[i] > -INFINITY ? 1u << i : 0u;
+#pragma unroll 1
+                for (; hit; hit &= hit - 1) {
+                    const int i = __ffs(hit) - 1, index = a.first + at[0] * N + i;
+                    if (lowest) {
+                        atomicMin(lowest, index);
+                    } else {
+                        const unsigned place = atomicAdd(count, 1u);
+                        if (place < (unsigned)kList) list[place] = entry(ardiff::to_float(a.x[index]), index);
+                    }
+                }
+            }
+            q[0] = q[1], q[1] = q[2], q[2] = q[3];
+            at[0] = at[1], at[1] = at[2], at[2] = at[3];
+        }
+    }
+}
+
 struct Settings {
     float T, p, mp, u;
     int k;
@@ -587,17 +623,36 @@ constexpr int kFine = 10, kCodes = kBins << kFine;
 __device__ __forceinline__ int weight_code(float d, float a32) {
     return __float_as_int(fminf(d * a32 * 16384.0f, (float)(kCodes - 1)) + 8388608.0f) - __float_as_int(8388608.0f);
 }
-__device__ __forceinline__ double weight_of_bin(int b) { return (double)ardiff::ex2(-0.0625f * ((float)b + 0.5f)); }
+// Weights in the middle of bins: of codes first + b step .. first + (b + 1) step - 1; of keys from top - (b << shift) down to the next bin's.
+struct CodeBins {
+    int first, step;
+    __device__ __forceinline__ double operator()(int b) const {
+        return (double)ardiff::ex2(-((float)(first + b * step) + 0.5f * (float)(step - 1)) * 0.00006103515625f);
+    }
+};
+struct KeyBins {
+    unsigned top, bottom;
+    int shift;
+    float m, a32;
+    __device__ __forceinline__ double operator()(int b) const {
+        const unsigned down = ((unsigned)b << shift) + (shift ? 1u << (shift - 1) : 0u);
+        return (double)ardiff::ex2((value_of(top - min(down, top - bottom)) - m) * a32);
+    }
+};
 
 __device__ __forceinline__ void clear_bins(Shared& s) { reinterpret_cast<uint4*>(s.hist)[threadIdx.x] = uint4(); }
 __device__ __forceinline__ void count_bin(Shared& s, int b) { atomicAdd(&s.hist[b], 1u); }
-// The calling thread's bins of one histogram, kEach * threadIdx.x and the ones behind it.
-__device__ __forceinline__ void add_bins(const unsigned* hist, unsigned (&c)[kEach]) {
-    const uint4 q = reinterpret_cast<const uint4*>(hist)[threadIdx.x];
-    c[0] += q.x;
-    c[1] += q.y;
-    c[2] += q.z;
-    c[3] += q.w;
+// The calling thread's bins of all CTAs' histograms, kEach * threadIdx.x and the ones behind it.
+template <typename T>
+__device__ __forceinline__ void gather_bins(const Part<T>& a, unsigned (&c)[kEach]) {
+    uint4 q[kMaxParts];
+#pragma unroll
+    for (int p = 0; p < kMaxParts; ++p) {                    // (all loads before the first sum: another CTA's bins are far away)
+        q[p] = uint4();
+        if (p < a.parts) q[p] = reinterpret_cast<const uint4*>(a.at(a.s->hist, p))[threadIdx.x];
+    }
+#pragma unroll
+    for (int p = 0; p < kMaxParts; ++p) c[0] += q[p].x, c[1] += q[p].y, c[2] += q[p].z, c[3] += q[p].w;
 }
 
 // What a histogram says about where a prefix ends: the bins, first to last (larger logits first), that hold its last element, the
@@ -608,18 +663,18 @@ struct Range {
     double mass;
 };
 
-// Adds up the CTAs' histograms and picks the bin in which the count passes k (COUNT), the estimated mass `enough`, or the count half of
+// Adds up the CTAs' histograms and picks the bin in which the count passes k (count), the estimated mass `enough`, or the count half of
 // all (half: where estimates did not help). A bin that was found by an estimate comes with its neighbours, as far as the list
 // has room; if it has none, with `spread` of them on either side. before, mass: in front of the histogram; whole: the exact mass of all
 // that was counted, if it is known (then the estimates come from behind, where bins hold many elements each and their middles err
 // little), else negative. middle(b): a weight of bin b. False: there is nothing.
-template <typename T, bool COUNT, typename F>
-__device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough, bool half, int spread, unsigned before, double mass, double whole, F&& middle,
-                                     Range& r) {
+template <typename T, typename F>
+__device__ __noinline__ bool pick(const Part<T> a, const bool count, unsigned k, double enough, bool half, int spread, unsigned before,
+                                  double mass, double whole, const F middle, Range& r) {
     Shared& s = *a.s;
     const int b0 = kEach * threadIdx.x;
     unsigned c[kEach] = {}, own = 0, total;
-    for (int p = 0; p < a.parts; ++p) add_bins(a.at(s.hist, p), c);
+    gather_bins(a, c);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) own += c[i];
     if (threadIdx.x == 0) {
@@ -633,12 +688,12 @@ __device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough
     for (int i = 0; i < kEach; ++i) n[i + 1] = n[i] + c[i];
     m[0] = mass;
     if (total == 0u) return false;
-    if (COUNT && before + total < k) {                       // not as many
+    if (count && before + total < k) {                       // not as many
         r = Range{0, 0, before, total, 0.0};
         return true;
     }
-    if (COUNT || half) {
-        const unsigned goal = COUNT ? k : before + (total + 1) / 2;
+    if (count || half) {
+        const unsigned goal = count ? k : before + (total + 1) / 2;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             if (n[i] < goal && n[i + 1] >= goal) s.found = b0 + i;
@@ -669,7 +724,7 @@ __device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough
         if (found == b0 + i) s.pick_before = n[i], s.pick_after = n[i + 1];
     __syncthreads();
     const unsigned lo = s.pick_before, hi = s.pick_after, in = hi - lo;
-    const unsigned more = COUNT || in > (unsigned)kList ? 0u : ((unsigned)kList - in) / 2;
+    const unsigned more = count || in > (unsigned)kList ? 0u : min(((unsigned)kList - in) / 2, 192u);
     if (more == 0u) {
         if (threadIdx.x == 0) {
             s.pick_first = max(found - spread, 0);
@@ -699,10 +754,12 @@ __device__ __forceinline__ bool pick(const Part<T>& a, unsigned k, double enough
 
 // What the sums over segments add up, value by value.
 struct Bulk {                            // all weights
+    static constexpr bool kHot = true;
     Weights wt;
     __device__ __forceinline__ double operator()(float v, int) const { return wt.bulk(v); }
 };
 struct Drawn {                           // the weights of what is kept, exactly; floor: below it none has min_p (all halved)
+    static constexpr bool kHot = false;
     Weights wt;
     Cut cut;
     float half, a32, floor;
@@ -714,6 +771,7 @@ struct Drawn {                           // the weights of what is kept, exactly
     }
 };
 struct Kept {                            // the weights of what the cut keeps
+    static constexpr bool kHot = true;
     Weights wt;
     Cut cut;
     __device__ __forceinline__ double operator()(float v, int i) const {
@@ -723,6 +781,7 @@ struct Kept {                            // the weights of what the cut keeps
 };
 template <bool FAR>
 struct Counted {                         // the same, with a histogram of the weights (all but the last bin)
+    static constexpr bool kHot = !FAR;
     Weights wt;
     Cut cut;
     float m, a32;
@@ -736,6 +795,7 @@ struct Counted {                         // the same, with a histogram of the we
     }
 };
 struct Above {                           // the weights above a range of codes; what is in it goes to the list
+    static constexpr bool kHot = true;
     Weights wt;
     Cut cut;
     float m, a32;
@@ -754,16 +814,20 @@ struct Above {                           // the weights above a range of codes; 
     }
 };
 struct AboveValue {                      // the weights above a value
+    static constexpr bool kHot = false;
     Weights wt;
     Cut cut;
     float top;
     __device__ __forceinline__ double operator()(float v, int i) const { return v > top && cut.keeps(v, i) ? wt.own(v) : 0.0; }
 };
 struct Equal {                           // the number of elements of a value
+    static constexpr bool kHot = false;
     Cut cut;
     float value;
     __device__ __forceinline__ double operator()(float v, int i) const { return v == value && cut.keeps(v, i) ? 1.0 : 0.0; }
 };
+
+enum Verdict { kFound, kAbove, kBelow, kUnknown, kNotNeeded };
 
 // How many elements of weight w, next to `sure`, it takes to reach `enough`: `in` + 1 if there are not that many.
 __device__ __forceinline__ double needed(double enough, double sure, double w, unsigned in) {
@@ -774,15 +838,14 @@ __device__ __forceinline__ double needed(double enough, double sure, double w, u
 }
 
 // The first CTA alone: where in the sorted list (n entries, the elements next to `sure` in mass, or the nth in number) the prefix ends.
-// s.verdict: 0, and s.cut its last element (COUNT = false: also s.found, its place in the list); 1, it lies above the list; 2, below.
-template <bool COUNT>
-__device__ __forceinline__ void end_in_list(Shared& s, const Weights& wt, int n, unsigned nth, double sure, double enough) {
+// s.verdict: kFound, and s.cut its last element (count = false: also s.found, its place in the list); or it lies above the list, or below.
+__device__ __noinline__ void end_in_list(Shared& s, const Weights wt, const bool count, int n, unsigned nth, double sure, double enough) {
     sort_list(s, n);
-    if (COUNT) {
+    if (count) {
         if (threadIdx.x == 0) {
             const unsigned long long e = s.list[nth];
             s.cut = Cut{entry_value(e), (int)(unsigned)e};
-            s.verdict = 0;
+            s.verdict = kFound;
         }
         return;
     }
@@ -803,8 +866,8 @@ __device__ __forceinline__ void end_in_list(Shared& s, const Weights& wt, int n,
     __syncthreads();
     if (threadIdx.x == 0) {
         s.mass_in = sure + all;
-        s.verdict = sure >= enough ? 1 : s.found == INT_MAX ? 2 : 0;
-        if (s.verdict == 0) {
+        s.verdict = sure >= enough ? kAbove : s.found == INT_MAX ? kBelow : kFound;
+        if (s.verdict == kFound) {
             const unsigned long long e = s.list[s.found];
             s.cut = Cut{entry_value(e), (int)(unsigned)e};
         }
@@ -812,11 +875,12 @@ __device__ __forceinline__ void end_in_list(Shared& s, const Weights& wt, int n,
     __syncthreads();
 }
 
-// The search for a prefix's last element among what `cut` keeps, by the logits as whole numbers: the k-th (COUNT), or the first at which
+// The search for a prefix's last element among what `cut` keeps, by the logits as whole numbers: the k-th (count), or the first at which
 // the mass reaches `enough`. Histograms narrow the range of numbers until few elements are in it or all are equal; an exact pass
 // sums what lies above, and a range that an estimate got wrong is done with, together with everything on its far side.
-template <typename T, bool COUNT>
-__device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32, const Cut cut, unsigned k, double enough, int& buf) {
+template <typename T>
+__device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32, const Cut cut, const bool count, unsigned k, double enough,
+                                   int& buf) {
     Shared& s = *a.s;
     const float m = (float)wt.m;
     unsigned lo_key = key_of(-INFINITY) + 1, hi_key = key_of(m);         // where the element can be; masked logits are none
@@ -837,13 +901,10 @@ __device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32,
                 if (q >= kmin && q <= kmax && cut.keeps(x, i)) count_bin(s, (int)((kmax - q) >> shift));   // largest first
             });
             a.sync();
-            const bool any = pick<T, COUNT>(a, k, enough, turn > 1, 0, r.before, r.mass, -1.0, [&](int b) {
-                const unsigned down = ((unsigned)b << shift) + (shift ? 1u << (shift - 1) : 0u);
-                return (double)ardiff::ex2((value_of(kmax - min(down, kmax - kmin)) - m) * a32);
-            }, r);
-            if (!any || (COUNT && r.before + r.in < k)) {    // nothing there: all above it is kept; or all of fewer than k
+            const bool any = pick(a, count, k, enough, turn > 1, 0, r.before, r.mass, -1.0, KeyBins{kmax, kmin, shift, m, a32}, r);
+            if (!any || (count && r.before + r.in < k)) {    // nothing there: all above it is kept; or all of fewer than k
                 a.sync();
-                return COUNT ? cut : Cut{value_of(hi_key + 1), INT_MAX};
+                return count ? cut : Cut{value_of(hi_key + 1), INT_MAX};
             }
             const unsigned top = kmax - ((unsigned)r.first << shift);
             const unsigned long long below = (unsigned long long)(r.last + 1) << shift;      // (up to 2^32)
@@ -857,7 +918,7 @@ __device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32,
         if (threadIdx.x == 0) s.count = 0u;
         a.sync();
         double sure = 0.0;
-        if (!COUNT) sure = sum_segments(a, buf, 2.0, AboveValue{wt, cut, top});
+        if (!count) sure = sum_segments(a, buf, 2.0, AboveValue{wt, cut, top});
         if (!ties) {
             a.each([&](float x, int i) {
                 if (x >= bottom && x <= top && cut.keeps(x, i)) {
@@ -866,22 +927,22 @@ __device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32,
                 }
             });
             a.sync();
-            if (a.rank == 0) end_in_list<COUNT>(s, wt, (int)min(s.count, (unsigned)kList), k - r.before - 1, sure, enough);
+            if (a.rank == 0) end_in_list(s, wt, count, (int)min(s.count, (unsigned)kList), k - r.before - 1, sure, enough);
         } else {
             // one value, more often than the list is long: as many of it as are needed, lowest indices first
-            const double w = COUNT ? 1.0 : wt.own(top);
-            const double need = COUNT ? (double)(k - r.before) : needed(enough, sure, w, r.in);
-            const int verdict = COUNT ? 0 : sure >= enough ? 1 : need > (double)r.in ? 2 : 0;
+            const double w = count ? 1.0 : wt.own(top);
+            const double need = count ? (double)(k - r.before) : needed(enough, sure, w, r.in);
+            const int verdict = count ? kFound : sure >= enough ? kAbove : need > (double)r.in ? kBelow : kFound;
             // (the sum over all is r.in: the share of it is a whole number less a half, up to rounding)
             sum_segments(a, buf, (need - 0.5) / (double)r.in, Equal{cut, top});
             const int owner = s.owner / kSegments;
-            if (verdict == 0 && owner == a.rank) {
+            if (verdict == kFound && owner == a.rank) {
                 const int at = locate(a, s.owner, s.before, need - 0.5, Equal{cut, top});
                 if (threadIdx.x == 0) s.cut = Cut{top, at};
             }
             a.sync();
             if (a.rank == 0 && threadIdx.x == 0) {
-                if (verdict == 0) s.cut = Cut{top, a.at(&s.cut, owner)->index};
+                if (verdict == kFound) s.cut = Cut{top, a.at(&s.cut, owner)->index};
                 s.verdict = verdict;
                 s.mass_in = sure + r.in * w;
             }
@@ -891,8 +952,8 @@ __device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32,
         const Cut found{a.at(&s.cut, 0)->value, a.at(&s.cut, 0)->index};
         const double with = *a.at(&s.mass_in, 0);
         a.sync();
-        if (verdict == 0) return found;
-        if (verdict == 1) {
+        if (verdict == kFound) return found;
+        if (verdict == kAbove) {
             lo_key = kmax + 1;
         } else {
             hi_key = kmin - 1;
@@ -913,10 +974,8 @@ __device__ __noinline__ void first_pass(const Part<T> a, const double scale) {
     Weights wt{};
     if (SUMS) {
         float ref = -INFINITY;
-        a.scan(warp * kGroups * a.segment + lane, min(a.pieces, warp * kGroups * a.segment + min(32, a.segment)), 32, [&](const float (&v)[N], int) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) ref = fmaxf(ref, v[i]);
-        });
+        a.template scan<1>(warp * kGroups * a.segment + lane, min(a.pieces, warp * kGroups * a.segment + min(32, a.segment)), 32,
+                           [&](const uint4& q, int) { ref = fmaxf(ref, ardiff::piece_max(q, T())); });
 #pragma unroll
         for (int q = 16; q > 0; q >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, q));
         if (lane == 0) s.warp_max[warp] = ref;
@@ -934,11 +993,13 @@ __device__ __noinline__ void first_pass(const Part<T> a, const double scale) {
         const int at = warp * kGroups + g;
         float top = -INFINITY;
         double acc[2] = {0.0, 0.0};
-        a.scan(at * a.segment + lane, min(a.pieces, (at + 1) * a.segment), 32, [&](const float (&v)[N], int) {
+        a.template scan<SUMS ? 2 : 8>(at * a.segment + lane, min(a.pieces, (at + 1) * a.segment), 32, [&](const uint4& q, int) {
+            top = max_nan(top, ardiff::piece_max(q, T()));
+            if (SUMS) {
+                float v[N];
+                ardiff::unpack(q, v, T());
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                top = max_nan(top, v[i]);
-                if (SUMS) acc[i & 1] += wt.bulk(v[i]);
+                for (int i = 0; i < N; ++i) acc[i & 1] += wt.bulk(v[i]);
             }
         });
         s.top[g][tid] = top;
@@ -1032,13 +1093,16 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) own = max_nan(own, s.warp_max[w]);
     if (greedy)                                              // the lowest index of this part's largest
-        a.each_of([&](float v) { return v == own; }, [&](float v, int i) { if (v == own) atomicMin(&s.first, i); });
+        collect(a, Listed{Listed::EQUAL, 0.f, own, 0.f, 0.f}, (unsigned*)nullptr, (unsigned long long*)nullptr, &s.first);
     if (tid == 0) s.cta_max = own;
     a.sync();
     float m = own, ref = sums ? s.ref : 0.f;                  // of all parts; the lowest reference
-    for (int r = 0; r < a.parts; ++r) {
-        m = max_nan(m, *a.at(&s.cta_max, r));
-        if (sums) ref = fminf(ref, *a.at(&s.ref, r));
+#pragma unroll
+    for (int r = 0; r < kMaxParts; ++r) {
+        if (r < a.parts) {
+            m = max_nan(m, *a.at(&s.cta_max, r));
+            if (sums) ref = fminf(ref, *a.at(&s.ref, r));
+        }
     }
     if (!valid || !(fabsf(m) < INFINITY) || greedy) {
         if (a.rank == 0 && tid == 0) {
@@ -1071,14 +1135,13 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     double before = 0.0, total = 0.0;
     if (o.use_k || o.use_p || o.use_m) {
         // which logits a list of all that may be kept has to hold, if there is a list
-        enum { ALL, REACH, WEIGHT, NONE } which = NONE;
-        float reach = 0.f;
+        Listed listed{Listed::ALL, m, 0.f, half, a32};
+        bool list = true;
         Range r;
         int last_code = 0;                                   // of a nucleus' end
         double whole = -1.0;
-        if (args.V <= kList) {
-            which = ALL;
-        } else {
+        if (args.V > kList) {
+            list = false;
             if (o.use_p && !o.use_k) {
                 if (summed) whole = add_segments(a, buf, 2.0, true, wt);
                 else if (wt.far) whole = sum_segments(a, buf, 2.0, AboveValue{wt, cut, -INFINITY});
@@ -1105,7 +1168,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             a.sync();
             if (o.use_k || o.use_p) {
                 unsigned c[kEach] = {}, all;
-                for (int p = 0; p < a.parts; ++p) add_bins(a.at(s.hist, p), c);
+                gather_bins(a, c);
                 unsigned n = cta_scan(s, (c[0] + c[1]) + (c[2] + c[3]), &all);
                 const double goal = o.use_k ? (double)o.k : fmax((double)o.p * whole * 262144.0, 1.0);
 #pragma unroll
@@ -1115,29 +1178,21 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                 }
                 __syncthreads();
                 if (s.found != INT_MAX) {
-                    which = REACH;
-                    reach = distance_edge(s.found + 1);
+                    list = true;
+                    listed.which = Listed::REACH;
+                    listed.bound = distance_edge(s.found + 1);
                 }
             } else {                                         // a list has no room for more groups than it has entries
                 for (int p = 0; p < a.parts; ++p) groups = p == 0 ? *a.at(&s.groups, 0) : groups + *a.at(&s.groups, p);
-                if (groups <= (unsigned)kList) which = WEIGHT;
+                list = groups <= (unsigned)kList;
+                listed.which = Listed::WEIGHT;
+                listed.bound = floor_;
             }
             a.sync();                                        // the others' bins have been read
         }
-        if (which != NONE) {
-            auto listed = [&](float v) {
-                if (which == REACH) return m - v < reach;
-                if (which == WEIGHT) return (0.5f * v - half) * a32 >= floor_;
-                return v > -INFINITY;
-            };
-            unsigned* count = a.at(&s.count, 0);
-            unsigned long long* list = a.at(s.list, 0);
-            a.each_of(listed, [&](float v, int i) {
-                if (listed(v) && v > -INFINITY) {
-                    const unsigned at = atomicAdd(count, 1u);
-                    if (at < (unsigned)kList) list[at] = entry(v, i);
-                }
-            });
+        if (list) {
+            const unsigned* count = a.at(&s.count, 0);
+            collect(a, listed, a.at(&s.count, 0), a.at(s.list, 0), (int*)nullptr);
             a.sync();
             const unsigned n = *count;
             a.sync();
@@ -1154,7 +1209,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             __syncthreads();
             a.each([&](float v, int) { if (v > -INFINITY) count_bin(s, distance_bin(m - v)); });
             a.sync();
-            pick<T, true>(a, (unsigned)o.k, 0.0, false, 0, 0u, 0.0, -1.0, weight_of_bin, r);
+            pick(a, true, (unsigned)o.k, 0.0, false, 0, 0u, 0.0, -1.0, CodeBins{0, 1}, r);
             if (r.before + r.in >= (unsigned)o.k) {          // (else there are fewer than k)
                 if (r.in <= (unsigned)kList) {
                     unsigned* count = a.at(&s.count, 0);
@@ -1163,11 +1218,11 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                         if (v > -INFINITY && distance_bin(m - v) == r.first) list[atomicAdd(count, 1u)] = entry(v, i);
                     });
                     a.sync();
-                    if (a.rank == 0) end_in_list<true>(s, wt, (int)r.in, (unsigned)o.k - r.before - 1, 0.0, 0.0);
+                    if (a.rank == 0) end_in_list(s, wt, true, (int)r.in, (unsigned)o.k - r.before - 1, 0.0, 0.0);
                     a.sync();
                     cut = Cut{a.at(&s.cut, 0)->value, a.at(&s.cut, 0)->index};
                 } else {
-                    cut = search<T, true>(a, wt, a32, cut, (unsigned)o.k, 0.0, buf);
+                    cut = search(a, wt, a32, cut, true, (unsigned)o.k, 0.0, buf);
                 }
             }
             a.sync();
@@ -1186,13 +1241,17 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                 });
                 a.sync();
             }
-            pick<T, false>(a, 0u, (double)o.p * whole, false, 1, 0u, 0.0, whole, weight_of_bin, r);
+            pick(a, false, 0u, (double)o.p * whole, false, 1, 0u, 0.0, whole, CodeBins{0, 1 << kFine}, r);
             r.last = min(r.last, kBins - 2);                 // (the last bin was not counted)
             last_code = (r.last << kFine) + (1 << kFine) - 1;
             const double enough = fmax((double)o.p * whole, 1e-300);                  // at least one
             int first_code = r.first << kFine;
-            if (r.in > (unsigned)kList) {                    // a histogram of these three bins, four codes a bin
-                a.sync();                                    // the first has been read
+            bool window = r.in > (unsigned)kList;            // first_code .. last_code want a histogram of their own, four codes a bin
+            double base = r.mass, upto = -1.0;               // the mass in front of them, or that up to their end
+            int verdict = kAbove;
+            for (int turn = 0; (verdict == kAbove || verdict == kBelow) && turn < 6; ++turn) {
+            if (window) {
+                a.sync();                                    // the last histogram has been read
                 clear_bins(s);
                 __syncthreads();
                 a.each([&](float v, int i) {
@@ -1200,8 +1259,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                     if (code >= first_code && code <= last_code && cut.keeps(v, i)) count_bin(s, (code - first_code) >> 2);
                 });
                 a.sync();
-                pick<T, false>(a, 0u, enough, false, 0, r.before, r.mass, -1.0,
-                               [&](int b) { return (double)ardiff::ex2(-((float)(first_code + 4 * b) + 1.5f) * 0.00006103515625f); }, r);
+                if (!pick(a, false, 0u, enough, false, 0, 0u, base, upto, CodeBins{first_code, 4}, r)) break;
                 last_code = min(last_code, first_code + 4 * r.last + 3);
                 first_code += 4 * r.first;
             }
@@ -1213,16 +1271,15 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                 s.count = 0u;
                 s.kmin = UINT_MAX;
                 s.kmax = 0u;
-                s.verdict = 1;
+                s.verdict = kUnknown;
             }
             a.sync();
             const double sure = wt.far ? 0.0 : sum_segments(a, buf, 2.0, Above{wt, cut, m, a32, first_code, last_code,
                                                                                listed ? a.at(&s.count, 0) : nullptr, a.at(s.list, 0)});
-            // verdict of the first CTA: 0, the draw's segment is known; 1, nothing is; 2, min_p ends above the range, the cut is not needed
             if (listed && !wt.far && a.rank == 0) {
                 const int n = (int)min(s.count, (unsigned)kList);
-                end_in_list<false>(s, wt, n, 0u, sure, enough);
-                if (s.verdict == 0) {
+                end_in_list(s, wt, false, n, 0u, sure, enough);
+                if (s.verdict == kFound) {
                     const int kept = s.found + 1;
                     const bool above = o.use_m && wt.own(entry_value(s.list[0])) < (double)o.mp;
                     __syncthreads();                         // s.verdict and s.found have been read
@@ -1256,9 +1313,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                         for (; lo < kept && (int)(s.list[lo] >> 32) < end; ++lo) sum += s.w[(unsigned)s.list[lo]];
                         return sum;
                     });
-                    if (tid == 0) s.verdict = above ? 2 : 0;
-                } else if (tid == 0) {
-                    s.verdict = 1;
+                    if (tid == 0) s.verdict = above ? kNotNeeded : kFound;
                 }
             }
             double need = 0.0;
@@ -1267,7 +1322,9 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                 unsigned lo = UINT_MAX, hi = 0u;
                 for (int g = warp * 4; g < warp * 4 + 4; ++g) {
                     unsigned n = 0;
-                    a.scan(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const float (&v)[N], int p) {
+                    a.template scan<1>(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const uint4& q, int p) {
+                        float v[N];
+                        ardiff::unpack(q, v, T());
 #pragma unroll
                         for (int i = 0; i < N; ++i) {
                             const int code = weight_code(m - v[i], a32);
@@ -1296,6 +1353,10 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                 value = value_of(lo);
                 const double w = wt.own(value);
                 need = needed(enough, sure, w, r.in);
+                if (lo == hi && a.rank == 0 && tid == 0) {
+                    s.verdict = sure >= enough ? kAbove : need > (double)r.in ? kBelow : kFound;
+                    s.mass_in = sure + r.in * w;
+                }
                 if (lo == hi && sure < enough && need <= (double)r.in && a.rank == 0) {
                     const unsigned ties = tid < a.parts * kSegments ? *a.at(&s.seg_ties[tid % kSegments], tid / kSegments) : 0u;
                     unsigned all;
@@ -1304,12 +1365,13 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                         return *a.at(&s.seg[buf][g % kSegments], g / kSegments) + w * fmin(fmax(need - (double)ahead, 0.0), (double)ties);
                     });
                     if (tid == s.owner) s.cut_ahead = ahead;
-                    if (tid == 0) s.verdict = o.use_m && w < (double)o.mp ? 2 : 0;
+                    if (tid == 0 && o.use_m && w < (double)o.mp) s.verdict = kNotNeeded;
                 }
             }
             a.sync();
-            const int verdict = *a.at(&s.verdict, 0);
-            if (verdict == 0) {
+            verdict = *a.at(&s.verdict, 0);
+            const double with = *a.at(&s.mass_in, 0);
+            if (verdict == kFound) {
                 owner = *a.at(&s.owner, 0);
                 before = *a.at(&s.before, 0);
                 total = *a.at(&s.total, 0);
@@ -1320,15 +1382,28 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                 }
             }
             a.sync();
-            if (verdict == 0 && owner / kSegments != a.rank) return;
-            if (verdict == 0 && !listed) {
+            if (verdict == kFound && owner / kSegments != a.rank) return;
+            if (verdict == kFound && !listed) {
                 const unsigned ties = s.seg_ties[owner % kSegments];
                 int index = need <= 0.0 ? -1 : INT_MAX;
                 if (need > 0.0 && need < (double)ties) index = locate(a, owner, 0.0, need - 0.5, Equal{cut, value});
                 // (a cut before this one keeps all of the range or is its end)
                 cut = Cut{value, cut.value == value ? min(index, cut.index) : index};
             }
-            if (verdict == 1) cut = search<T, false>(a, wt, a32, cut, 0u, enough, buf);
+            // the estimate was wrong, but the sums next to the range are exact now: the same with a window beside it
+            window = true;
+            if (verdict == kAbove) {
+                upto = sure;
+                last_code = first_code - 1;
+                first_code = max(0, last_code - 4095);
+            } else {
+                upto = -1.0;
+                base = with;
+                first_code = last_code + 1;
+                last_code = min(first_code + 4095, ((kBins - 1) << kFine) - 1);
+            }
+            }
+            if (verdict != kFound && verdict != kNotNeeded) cut = search(a, wt, a32, cut, false, 0u, enough, buf);
         }
     }
     // the draw among what the cut keeps
@@ -1351,10 +1426,12 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
 
 template <typename T>
 int launch(Args a, int64_t n, cudaStream_t st) {
-    // more CTAs a row while not all find room at once and each keeps 512 pieces
+    // More CTAs a row while there is room for them and each keeps so many pieces that it gains: a list is one CTA's work, and the others
+    // cost it meetings (1 x 32768 bf16 with top-k: 18.7 us with one CTA, 22.6 with four; sums of all weights: 22.5 and 18.5).
+    const int64_t least = a.top_k ? 4096 : 1024;
     const int64_t pieces = ((int64_t)a.V + ardiff::Piece<T>::N - 1) / ardiff::Piece<T>::N;
     int parts = 1;
-    while (parts < kMaxParts && n * parts < 148 * 2 && pieces >= (int64_t)parts * 1024) parts *= 2;
+    while (parts < kMaxParts && n * parts < 148 * 2 && pieces >= 2 * parts * least) parts *= 2;
     a.parts = parts;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
