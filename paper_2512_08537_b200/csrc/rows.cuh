@@ -40,6 +40,24 @@ __device__ __forceinline__ void unpack(const uint4& p, float (&v)[8], __half) {
         v[2 * i + 1] = f.y;
     }
 }
+// Values h .. h + 3 of a piece, h a multiple of 4.
+__device__ __forceinline__ void unpack4(const uint4& p, int, float (&v)[4], float) { unpack(p, v, 0.f); }
+__device__ __forceinline__ void unpack4(const uint4& p, int h, float (&v)[4], __nv_bfloat16) {
+    const uint32_t a = h ? p.z : p.x, b = h ? p.w : p.y;
+    v[0] = __uint_as_float(a << 16);
+    v[1] = __uint_as_float(a & 0xffff0000u);
+    v[2] = __uint_as_float(b << 16);
+    v[3] = __uint_as_float(b & 0xffff0000u);
+}
+__device__ __forceinline__ void unpack4(const uint4& p, int h, float (&v)[4], __half) {
+    const uint32_t a = h ? p.z : p.x, b = h ? p.w : p.y;
+    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&a)), y = __half22float2(*reinterpret_cast<const __half2*>(&b));
+    v[0] = x.x;
+    v[1] = x.y;
+    v[2] = y.x;
+    v[3] = y.y;
+}
+
 // The largest value of a piece; NaN if one is.
 __device__ __forceinline__ float piece_max(const uint4& p, float) {
     float r;

@@ -164,15 +164,20 @@ struct Part {                            // this CTA's part of its row
         for (int i = 0; i < N; ++i) v[i] = e + i >= 0 && e + i < V ? ardiff::to_float(x[e + i]) : -INFINITY;
         return ardiff::pack(v, T());
     }
-    // f(piece's bits, piece) for pieces begin, begin + step, ... below end; AHEAD loads at a time
+    // f(piece's bits, piece) for pieces begin, begin + step, ... below end; AHEAD loads at a time, issued while the ones before are used
     template <int AHEAD, typename F> __device__ __forceinline__ void scan(int begin, int end, int step, F&& f) const {
         const uint4* base = reinterpret_cast<const uint4*>(x + first);     // (aligned; pieces whole0 .. whole1 - 1 are read)
         const int most = whole1 - 1;
+        if (begin >= end) return;
+        uint4 q[AHEAD], next[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) q[i] = next[i] = whole0 <= most ? __ldg(base + max(whole0, min(begin + i * step, most))) : uint4();
 #pragma unroll 1
         for (int p = begin; p < end; p += AHEAD * step) {
-            uint4 q[AHEAD];
+            if (p + AHEAD * step < end) {
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) q[i] = whole0 <= most ? __ldg(base + max(whole0, min(p + i * step, most))) : uint4();
+                for (int i = 0; i < AHEAD; ++i) next[i] = whole0 <= most ? __ldg(base + max(whole0, min(p + (AHEAD + i) * step, most))) : uint4();
+            }
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 const int at = p + i * step;
@@ -180,12 +185,14 @@ struct Part {                            // this CTA's part of its row
                 if (at < whole0 || at >= whole1) q[i] = edge(x, first + at * N, V);
                 f(q[i], at);
             }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) q[i] = next[i];
         }
     }
     // f(value, index) for every value of the calling warp's segments (once in the code: not for what has to be fast)
     template <typename F> __device__ __forceinline__ void each(F&& f) const {
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        scan<2>(warp * kGroups * segment + lane, min(pieces, (warp + 1) * kGroups * segment), 32, [&](const uint4& q, int p) {
+        scan<4>(warp * kGroups * segment + lane, min(pieces, (warp + 1) * kGroups * segment), 32, [&](const uint4& q, int p) {
             float v[N];
             ardiff::unpack(q, v, T());
 #pragma unroll
@@ -326,11 +333,15 @@ __device__ __noinline__ double sum_in(const Part<T> a, const int buf, const doub
 #pragma unroll 1
     for (int g = warp * kGroups; g < (warp + 1) * kGroups; ++g) {
         double acc[2] = {0.0, 0.0};
-        a.template scan<F::kHot ? 2 : 1>(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const uint4& q, int p) {
-            float v[N];
-            ardiff::unpack(q, v, T());
+        a.template scan<2>(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const uint4& q, int p) {
+            // (four weights side by side: with eight, registers run out)
+#pragma unroll 1
+            for (int h = 0; h < N; h += 4) {
+                float v[4];
+                ardiff::unpack4(q, h, v, T());
 #pragma unroll
-            for (int i = 0; i < N; ++i) acc[i & 1] += f(v[i], a.first + p * N + i);
+                for (int i = 0; i < 4; ++i) acc[i & 1] += f(v[i], a.first + p * N + h + i);
+            }
         });
         const double mine = warp_sum(acc[0] + acc[1]);
         if (lane == 0) s.seg[buf][g] = mine;
@@ -724,7 +735,7 @@ __device__ __noinline__ bool pick(const Part<T> a, const bool count, unsigned k,
         if (found == b0 + i) s.pick_before = n[i], s.pick_after = n[i + 1];
     __syncthreads();
     const unsigned lo = s.pick_before, hi = s.pick_after, in = hi - lo;
-    const unsigned more = count || in > (unsigned)kList ? 0u : min(((unsigned)kList - in) / 2, 192u);
+    const unsigned more = count || in > (unsigned)kList ? 0u : min(((unsigned)kList - in) / 2, 64u);
     if (more == 0u) {
         if (threadIdx.x == 0) {
             s.pick_first = max(found - spread, 0);
@@ -752,14 +763,16 @@ __device__ __noinline__ bool pick(const Part<T> a, const bool count, unsigned k,
     return true;
 }
 
+// w where `in`, 0 elsewhere: as a product, so that the weights of neighbouring values are formed side by side and none in a branch of its
+// own (which the compiler makes of a selection: 2.5 times as slow).
+__device__ __forceinline__ double masked(double w, bool in) { return w * __hiloint2double(in ? 0x3ff00000 : 0, 0); }
+
 // What the sums over segments add up, value by value.
 struct Bulk {                            // all weights
-    static constexpr bool kHot = true;
     Weights wt;
     __device__ __forceinline__ double operator()(float v, int) const { return wt.bulk(v); }
 };
 struct Drawn {                           // the weights of what is kept, exactly; floor: below it none has min_p (all halved)
-    static constexpr bool kHot = false;
     Weights wt;
     Cut cut;
     float half, a32, floor;
@@ -771,17 +784,14 @@ struct Drawn {                           // the weights of what is kept, exactly
     }
 };
 struct Kept {                            // the weights of what the cut keeps
-    static constexpr bool kHot = true;
     Weights wt;
     Cut cut;
     __device__ __forceinline__ double operator()(float v, int i) const {
-        const double w = wt.bulk(v);
-        return cut.keeps(v, i) ? w : 0.0;
+        return masked(wt.bulk(v), cut.keeps(v, i));
     }
 };
 template <bool FAR>
 struct Counted {                         // the same, with a histogram of the weights (all but the last bin)
-    static constexpr bool kHot = !FAR;
     Weights wt;
     Cut cut;
     float m, a32;
@@ -791,37 +801,16 @@ struct Counted {                         // the same, with a histogram of the we
         const bool in = cut.keeps(v, i);
         const int b = weight_code(m - v, a32) >> kFine;
         if (in && b < kBins - 1) atomicAdd(&hist[b], 1u);
-        return in ? w : 0.0;
-    }
-};
-struct Above {                           // the weights above a range of codes; what is in it goes to the list
-    static constexpr bool kHot = true;
-    Weights wt;
-    Cut cut;
-    float m, a32;
-    int first, last;
-    unsigned* count;                     // of the first CTA; NULL: no list
-    unsigned long long* list;
-    __device__ __forceinline__ double operator()(float v, int i) const {
-        const double w = wt.bulk(v);
-        const int code = weight_code(m - v, a32);
-        const bool in = cut.keeps(v, i);
-        if (in && count && code >= first && code <= last) {
-            const unsigned at = atomicAdd(count, 1u);
-            if (at < (unsigned)kList) list[at] = entry(v, i);
-        }
-        return in && code < first ? w : 0.0;
+        return masked(w, in);
     }
 };
 struct AboveValue {                      // the weights above a value
-    static constexpr bool kHot = false;
     Weights wt;
     Cut cut;
     float top;
     __device__ __forceinline__ double operator()(float v, int i) const { return v > top && cut.keeps(v, i) ? wt.own(v) : 0.0; }
 };
 struct Equal {                           // the number of elements of a value
-    static constexpr bool kHot = false;
     Cut cut;
     float value;
     __device__ __forceinline__ double operator()(float v, int i) const { return v == value && cut.keeps(v, i) ? 1.0 : 0.0; }
@@ -993,7 +982,7 @@ __device__ __noinline__ void first_pass(const Part<T> a, const double scale) {
         const int at = warp * kGroups + g;
         float top = -INFINITY;
         double acc[2] = {0.0, 0.0};
-        a.template scan<SUMS ? 2 : 8>(at * a.segment + lane, min(a.pieces, (at + 1) * a.segment), 32, [&](const uint4& q, int) {
+        a.template scan<SUMS ? 2 : 4>(at * a.segment + lane, min(a.pieces, (at + 1) * a.segment), 32, [&](const uint4& q, int) {
             top = max_nan(top, ardiff::piece_max(q, T()));
             if (SUMS) {
                 float v[N];
@@ -1008,6 +997,46 @@ __device__ __noinline__ void first_pass(const Part<T> a, const double scale) {
             if (lane == 0) s.seg[0][at] = mine;
         }
     }
+}
+
+// The sums of the weights above a range of codes, over the segments; what is in the range goes to the list of the first CTA (*count, list;
+// NULL: it does not).
+template <typename T>
+__device__ __noinline__ double sum_above(const Part<T> a, const int buf, const Weights wt, const Cut cut, const float m, const float a32,
+                                         const int first, const int last, unsigned* count, unsigned long long* list) {
+    constexpr int N = Part<T>::N;
+    Shared& s = *a.s;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int g = warp * kGroups; g < (warp + 1) * kGroups; ++g) {
+        double acc[2] = {0.0, 0.0};
+        a.template scan<2>(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const uint4& q, int p) {
+            unsigned hit = 0;
+#pragma unroll 1
+            for (int h = 0; h < N; h += 4) {                 // (as above)
+                float v[4];
+                ardiff::unpack4(q, h, v, T());
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int code = weight_code(m - v[i], a32);
+                    const bool in = cut.keeps(v[i], a.first + p * N + h + i);
+                    acc[i & 1] += masked(wt.bulk(v[i]), in && code < first);
+                    hit |= in && code >= first && code <= last ? 1u << (h + i) : 0u;
+                }
+            }
+            if (hit && count) {
+#pragma unroll 1
+                for (; hit; hit &= hit - 1) {
+                    const int index = a.first + p * N + __ffs(hit) - 1;
+                    const unsigned place = atomicAdd(count, 1u);
+                    if (place < (unsigned)kList) list[place] = entry(ardiff::to_float(a.x[index]), index);
+                }
+            }
+        });
+        const double mine = warp_sum(acc[0] + acc[1]);
+        if (lane == 0) s.seg[buf][g] = mine;
+    }
+    return add_segments(a, buf, 2.0, false, Weights());
 }
 
 // The first CTA: the draw's segment, where the sum over segment g (of all CTAs') is in_segment(g); a thread a segment.
@@ -1246,22 +1275,24 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             last_code = (r.last << kFine) + (1 << kFine) - 1;
             const double enough = fmax((double)o.p * whole, 1e-300);                  // at least one
             int first_code = r.first << kFine;
-            bool window = r.in > (unsigned)kList;            // first_code .. last_code want a histogram of their own, four codes a bin
+            bool window = r.in > 2 * kThreads;               // first_code .. last_code want a histogram of their own
             double base = r.mass, upto = -1.0;               // the mass in front of them, or that up to their end
             int verdict = kAbove;
             for (int turn = 0; (verdict == kAbove || verdict == kBelow) && turn < 6; ++turn) {
             if (window) {
+                int shift = 0;
+                while ((last_code - first_code) >> shift >= kBins) ++shift;
                 a.sync();                                    // the last histogram has been read
                 clear_bins(s);
                 __syncthreads();
                 a.each([&](float v, int i) {
                     const int code = weight_code(m - v, a32);
-                    if (code >= first_code && code <= last_code && cut.keeps(v, i)) count_bin(s, (code - first_code) >> 2);
+                    if (code >= first_code && code <= last_code && cut.keeps(v, i)) count_bin(s, (code - first_code) >> shift);
                 });
                 a.sync();
-                if (!pick(a, false, 0u, enough, false, 0, 0u, base, upto, CodeBins{first_code, 4}, r)) break;
-                last_code = min(last_code, first_code + 4 * r.last + 3);
-                first_code += 4 * r.first;
+                if (!pick(a, false, 0u, enough, false, 0, 0u, base, upto, CodeBins{first_code, 1 << shift}, r)) break;
+                last_code = min(last_code, first_code + ((r.last + 1) << shift) - 1);
+                first_code += r.first << shift;
             }
             // the sum of what lies above the range; a list of what lies in it, or, where that is more than a list holds, whether it is
             // one value, and how often in which segment
@@ -1274,8 +1305,11 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                 s.verdict = kUnknown;
             }
             a.sync();
-            const double sure = wt.far ? 0.0 : sum_segments(a, buf, 2.0, Above{wt, cut, m, a32, first_code, last_code,
-                                                                               listed ? a.at(&s.count, 0) : nullptr, a.at(s.list, 0)});
+            double sure = 0.0;
+            if (!wt.far) {
+                buf ^= 1;
+                sure = sum_above(a, buf, wt, cut, m, a32, first_code, last_code, listed ? a.at(&s.count, 0) : nullptr, a.at(s.list, 0));
+            }
             if (listed && !wt.far && a.rank == 0) {
                 const int n = (int)min(s.count, (unsigned)kList);
                 end_in_list(s, wt, false, n, 0u, sure, enough);
