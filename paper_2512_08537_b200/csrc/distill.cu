@@ -11,6 +11,7 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "../../include/ardiff.h"
@@ -21,9 +22,10 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
+constexpr int kCache = 60 * 1024;        // bytes of a part that are kept for the gradient: three CTAs an SM
 enum Mode { FORWARD, STEP, BACKWARD };
+template <int MODE> constexpr int kThreadsOf = MODE == FORWARD ? 256 : 512;
+template <int MODE> constexpr int kAheadOf = MODE == FORWARD ? 8 : 4;        // pieces a thread has under way
 
 struct Args {
     const void* x;
@@ -35,6 +37,7 @@ struct Args {
     void* grad;                  // STEP, BACKWARD
     int64_t ld, ld_grad;
     int32_t teacher_type, V, k, parts;
+    int32_t cached;              // STEP: pieces of a part that shared memory holds
     float inv_t;                 // 1 / T
 };
 
@@ -53,35 +56,43 @@ __device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, float c) {
     return MaxSum{m, a.z * ardiff::ex2((a.m - at) * c) + b.z * ardiff::ex2((b.m - at) * c)};
 }
 
-template <typename T>
-__device__ __forceinline__ void take(MaxSum& s, const uint4& p, float c) {
+template <typename T, int kAhead>
+__device__ __forceinline__ void take(MaxSum& s, const uint4 (&q)[kAhead], int n, float c) {
     constexpr int N = ardiff::Piece<T>::N;
-    float v[N];
-    ardiff::unpack(p, v, T());
-    float top = v[0];
+    float top = ardiff::piece_max(q[0], T());
 #pragma unroll
-    for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+    for (int j = 1; j < kAhead; ++j)
+        if (j < n) top = fmaxf(top, ardiff::piece_max(q[j], T()));
     if (top > s.m) {
         s.z *= ardiff::ex2((s.m - top) * c);       // from -inf: 0
         s.m = top;
     }
     const float at = s.m == -INFINITY ? 0.f : s.m;
 #pragma unroll
-    for (int i = 0; i < N; ++i) s.z += ardiff::ex2((v[i] - at) * c);
+    for (int j = 0; j < kAhead; ++j) {
+        if (j < n) {
+            float v[N], e = 0.f;
+            ardiff::unpack(q[j], v, T());
+#pragma unroll
+            for (int i = 0; i < N; ++i) e += ardiff::ex2((v[i] - at) * c);
+            s.z += e;
+        }
+    }
 }
 
 template <typename T, int MODE>
-__global__ void __launch_bounds__(kThreads) distill_kernel(const Args a) {
+__global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) distill_kernel(const Args a) {
+    constexpr int kThreads = kThreadsOf<MODE>, kWarps = kThreads / 32, kAhead = kAheadOf<MODE>;
     using ardiff::Row;
     constexpr int N = ardiff::Piece<T>::N;
     extern __shared__ __align__(16) unsigned char smem[];
-    float* s_q = reinterpret_cast<float*>(smem);             // [k] teacher's logits, then probabilities
+    uint4* s_cache = reinterpret_cast<uint4*>(smem);         // [cached] pieces of this part
+    float* s_q = reinterpret_cast<float*>(s_cache + a.cached);   // [k] teacher's logits, then probabilities
     float* s_x = s_q + a.k;                                  // [k] the student's logits there
     int32_t* s_id = reinterpret_cast<int32_t*>(s_x + a.k);   // [k] -1: no entry
-    __shared__ MaxSum s_part[kWarps];
+    __shared__ MaxSum s_part[kWarps], s_entries[kWarps];
     __shared__ MaxSum s_own;
     __shared__ float s_loss[kWarps];
-    __shared__ float s_top, s_ln;                            // of the teacher
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row = blockIdx.x / a.parts;
     const int part = blockIdx.x % a.parts;
@@ -93,6 +104,17 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const Args a) {
     const int v0 = part == 0 ? 0 : x.lead + p0 * N, v1 = part == a.parts - 1 ? a.V : x.lead + p1 * N;
     T* grad = MODE == FORWARD ? nullptr : static_cast<T*>(a.grad) + row * a.ld_grad;
 
+    // the first pieces are under way before anything is waited for
+    const uint4* body = x.body();
+    uint4 q[kAhead];
+    int n_q = 0;
+    auto load = [&](int p) {
+        n_q = p < p1 ? min(kAhead, (p1 - p + kThreads - 1) / kThreads) : 0;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (j < n_q) q[j] = __ldg(body + p + j * kThreads);
+    };
+    if (MODE != BACKWARD) load(p0 + tid);
     bool some = false;
     for (int j = tid; j < a.k; j += kThreads) {
         int id = a.ids[row * a.k + j];
@@ -114,41 +136,36 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const Args a) {
         }
         return;                                              // every CTA of the cluster alike
     }
-    if (warp == 0) {
-        float top = -INFINITY;
-        for (int j = lane; j < a.k; j += 32)
-            if (s_id[j] >= 0) top = s_q[j] > top || s_q[j] != s_q[j] ? s_q[j] : top;     // a NaN stays
+    // this thread's entries: their largest and the sum of their exponentials above it
+    MaxSum t{-INFINITY, 0.f};
+    for (int j = tid; j < a.k; j += kThreads)
+        if (s_id[j] >= 0) t = merge(t, MaxSum{s_q[j], 1.f}, c);
+    auto reduce_entries = [&]() {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const float b = __shfl_xor_sync(0xffffffffu, top, o);
-            top = b > top || b != b ? b : top;
-        }
-        float sum = 0.f;
-        for (int j = lane; j < a.k; j += 32) {
-            const float e = s_id[j] >= 0 ? expf((s_q[j] - top) * a.inv_t) : 0.f;
-            sum += e;
-        }
+        for (int o = 16; o > 0; o >>= 1)
+            t = merge(t, MaxSum{__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.z, o)}, c);
+        if (lane == 0) s_entries[warp] = t;
+    };
+    auto add_warps = [&](const MaxSum* w) {                  // every warp for itself, one value a lane
+        MaxSum v = lane < kWarps ? w[lane] : MaxSum{-INFINITY, 0.f};
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) {
-            s_top = top;
-            s_ln = logf(sum);
-        }
-    }
-
-    const uint4* body = x.body();
+        for (int o = kWarps / 2; o > 0; o >>= 1)
+            v = merge(v, MaxSum{__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.z, o)}, c);
+        return MaxSum{__shfl_sync(0xffffffffu, v.m, 0), __shfl_sync(0xffffffffu, v.z, 0)};
+    };
     float m, ln_z, scale;
     if (MODE != BACKWARD) {
         MaxSum s{-INFINITY, 0.f};
-        int p = p0 + tid;
-        for (; p + 3 * kThreads < p1; p += 4 * kThreads) {
-            uint4 v[4];
+#pragma unroll 1
+        for (int p = p0 + tid; n_q > 0; p += kAhead * kThreads) {
+            if (MODE == STEP) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __ldg(body + p + i * kThreads);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) take<T>(s, v[i], c);
+                for (int j = 0; j < kAhead; ++j)
+                    if (j < n_q && p - p0 + j * kThreads < a.cached) s_cache[p - p0 + j * kThreads] = q[j];
+            }
+            take<T, kAhead>(s, q, n_q, c);
+            load(p + kAhead * kThreads);
         }
-        for (; p < p1; p += kThreads) take<T>(s, __ldg(body + p), c);
         const int edge = part == 0 && tid < x.lead ? tid : part == a.parts - 1 && x.tail() + tid < a.V ? x.tail() + tid : -1;
         const int both = part == 0 && tid < x.lead && part == a.parts - 1 && x.tail() + tid < a.V ? x.tail() + tid : -1;
         if (edge >= 0) {
@@ -163,10 +180,9 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const Args a) {
         for (int o = 16; o > 0; o >>= 1)
             s = merge(s, MaxSum{__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.z, o)}, c);
         if (lane == 0) s_part[warp] = s;
+        reduce_entries();
         __syncthreads();
-        s = s_part[0];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) s = merge(s, s_part[w], c);
+        s = add_warps(s_part);
         if (a.parts > 1) {
             cg::cluster_group cl = cg::this_cluster();
             if (tid == 0) s_own = s;
@@ -182,9 +198,11 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const Args a) {
         m = a.stats[2 * row];
         ln_z = a.stats[2 * row + 1];
         scale = a.weight[row] * a.inv_t;
-        __syncthreads();                                     // s_top, s_ln
+        reduce_entries();
+        __syncthreads();
     }
-    const float top = s_top, ln = s_ln;
+    t = add_warps(s_entries);
+    const float top = t.m, ln = logf(t.z);
     // the teacher's probabilities; this row's loss
     float loss = 0.f;
     for (int j = tid; j < a.k; j += kThreads) {
@@ -212,16 +230,30 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const Args a) {
         auto prob = [&](float v) { return ardiff::ex2((v - m) * c - l2); };
         T* out = grad + x.lead;
         const bool wide = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
-        for (int p = p0 + tid; p < p1; p += kThreads) {
-            float v[N];
-            ardiff::unpack(__ldcg(body + p), v, T());        // (may lie where grad does)
+#pragma unroll 1
+        for (int p = p0 + tid; p < p1; p += 4 * kThreads) {
+            uint4 r[4];
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = prob(v[i]) * scale;
-            if (wide) {
-                reinterpret_cast<uint4*>(out)[p] = ardiff::pack(v, T());
-            } else {
+            for (int j = 0; j < 4; ++j) {
+                const int i = p + j * kThreads;
+                if (i >= p1) continue;
+                if (MODE == STEP && i - p0 < a.cached) r[j] = s_cache[i - p0];       // (each thread's own)
+                else r[j] = __ldcg(body + i);                                        // (may lie where the gradient does)
+            }
 #pragma unroll
-                for (int i = 0; i < N; ++i) out[p * N + i] = ardiff::from_float<T>(v[i]);
+            for (int j = 0; j < 4; ++j) {
+                const int i = p + j * kThreads;
+                if (i >= p1) continue;
+                float v[N];
+                ardiff::unpack(r[j], v, T());
+#pragma unroll
+                for (int l = 0; l < N; ++l) v[l] = prob(v[l]) * scale;
+                if (wide) {
+                    __stcs(reinterpret_cast<uint4*>(out) + i, ardiff::pack(v, T()));
+                } else {
+#pragma unroll
+                    for (int l = 0; l < N; ++l) out[i * N + l] = ardiff::from_float<T>(v[l]);
+                }
             }
         }
         if (part == 0 && tid < x.lead) grad[tid] = ardiff::from_float<T>(prob(ardiff::to_float(x.x[tid])) * scale);
@@ -231,14 +263,16 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const Args a) {
         }
         __syncthreads();
         // the entries' places once more, with the teacher's share in the sum before it is rounded; an id that occurs again has
-        // the sum of its shares in order of the entries, and every one of them writes the same
+        // the sum of its shares, and every one of them writes the same
         const float share = a.weight[row] * a.inv_t;
-        for (int j = tid; j < a.k; j += kThreads) {
+        for (int j = warp; j < a.k; j += kWarps) {
             const int id = s_id[j];
             if (id < v0 || id >= v1) continue;
-            float q = 0.f;
-            for (int i = 0; i < a.k; ++i) q += s_id[i] == id ? s_q[i] : 0.f;
-            grad[id] = ardiff::from_float<T>(prob(s_x[j]) * scale - q * share);
+            float q_sum = 0.f;
+            for (int i = lane; i < a.k; i += 32) q_sum += s_id[i] == id ? s_q[i] : 0.f;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) q_sum += __shfl_xor_sync(0xffffffffu, q_sum, o);
+            if (lane == 0) grad[id] = ardiff::from_float<T>(prob(s_x[j]) * scale - q_sum * share);
         }
     }
     if (MODE != BACKWARD && a.parts > 1) cg::this_cluster().sync();      // a CTA leaves when its part has been read
@@ -246,13 +280,24 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const Args a) {
 
 template <typename T, int MODE>
 int launch(const Args& a, int64_t n, cudaStream_t st) {
+    static std::atomic<unsigned long long> ready{0};         // devices on which the kernel may have its shared memory
+    if (MODE == STEP) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess) return ARDIFF_ERR_CUDA;
+        if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
+            if (cudaFuncSetAttribute(distill_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     kCache + ARDIFF_DISTILL_MAX_K * 12) != cudaSuccess)
+                return ARDIFF_ERR_CUDA;
+            if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+        }
+    }
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = MODE == BACKWARD ? 1 : a.parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(n * a.parts)); cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)a.k * 12; cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)(n * a.parts)); cfg.blockDim = dim3(kThreadsOf<MODE>);
+    cfg.dynamicSmemBytes = (size_t)a.k * 12 + (size_t)a.cached * 16; cfg.stream = st;
     cfg.attrs = at; cfg.numAttrs = 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, distill_kernel<T, MODE>, a);
     ardiff::set_launch_count(1);
@@ -281,9 +326,13 @@ int dispatch(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld
     memset(&a, 0, sizeof(a));
     a.x = logits; a.teacher = teacher; a.ids = ids; a.weight = weight; a.loss = loss; a.stats = stats; a.grad = grad;
     a.ld = ld; a.ld_grad = ld_grad; a.teacher_type = teacher_type; a.V = V; a.k = k; a.inv_t = 1.0f / temperature;
-    // more CTAs a row while there are SMs without one and each keeps two pieces a thread
+    // more CTAs a row while there is room for them and each keeps several pieces a thread; those that keep their part until the gradient
+    // is due, as many as it takes to hold it
+    const int64_t pieces = (int64_t)V * size / 16;
     a.parts = 1;
-    while (a.parts < 8 && n * a.parts < 148 && (int64_t)V * size / 16 >= (int64_t)4 * kThreads * a.parts) a.parts *= 2;
+    while (a.parts < 8 && n * a.parts < 148 * 2 && pieces >= (int64_t)8 * kThreadsOf<MODE> * a.parts)
+        a.parts *= 2;
+    if (MODE == STEP) a.cached = (int)std::min<int64_t>((pieces + a.parts - 1) / a.parts, kCache / 16);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (dtype == ARDIFF_F32) return launch<float, MODE>(a, n, st);
     if (dtype == ARDIFF_F16) return launch<__half, MODE>(a, n, st);

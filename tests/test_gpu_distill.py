@@ -92,7 +92,9 @@ def check(x, teacher, ids, weight, T):
     near(stats[:, 1], stats_w[:, 1], dlnz, "ln Z")
     near(ardiff.ardiff_distill_topk_backward(x, teacher, ids, stats, weight, T), grad_w, tol, "backward")
     loss2, stats2, grad = ardiff.ardiff_distill_topk_step(x, teacher, ids, weight, T)
-    assert torch.equal(loss.nan_to_num(-1.0), loss2.nan_to_num(-1.0)) and torch.equal(stats.nan_to_num(), stats2.nan_to_num())
+    near(loss2, loss_w, dloss, "loss of the step")             # (by other threads, so in another order of sums)
+    near(stats2[:, 0], stats_w[:, 0], torch.zeros(len(loss_w)), "largest of the step")
+    near(stats2[:, 1], stats_w[:, 1], dlnz, "ln Z of the step")
     near(grad, grad_w, tol, "step")
     return loss_w, grad_w
 
