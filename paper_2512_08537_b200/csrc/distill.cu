@@ -38,6 +38,7 @@ struct Args {
     int64_t ld, ld_grad;
     int32_t teacher_type, V, k, parts;
     int32_t cached;              // STEP: pieces of a part that shared memory holds
+    int32_t seen;                // STEP, BACKWARD: places of the ids' table, a power of two, at least twice k
     float inv_t;                 // 1 / T
 };
 
@@ -56,26 +57,35 @@ __device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, float c) {
     return MaxSum{m, a.z * ardiff::ex2((a.m - at) * c) + b.z * ardiff::ex2((b.m - at) * c)};
 }
 
+// A thread's running largest value, and two sums of every other value's exponential above it.
+struct Running {
+    float m;
+    ardiff::Two z;
+};
 template <typename T, int kAhead>
-__device__ __forceinline__ void take(MaxSum& s, const uint4 (&q)[kAhead], int n, float c) {
+__device__ __forceinline__ void take(Running& s, const uint4 (&q)[kAhead], int n, float c) {
     constexpr int N = ardiff::Piece<T>::N;
     float top = ardiff::piece_max(q[0], T());
 #pragma unroll
     for (int j = 1; j < kAhead; ++j)
         if (j < n) top = fmaxf(top, ardiff::piece_max(q[j], T()));
     if (top > s.m) {
-        s.z *= ardiff::ex2((s.m - top) * c);       // from -inf: 0
+        const float down = ardiff::ex2((s.m - top) * c);     // from -inf: 0
+        s.z = s.z * ardiff::two(down, down);
         s.m = top;
     }
     const float at = s.m == -INFINITY ? 0.f : s.m;
+    const ardiff::Two minus = ardiff::two(-at, -at), c2 = ardiff::two(c, c);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
         if (j < n) {
-            float v[N], e = 0.f;
+            float v[N];
             ardiff::unpack(q[j], v, T());
 #pragma unroll
-            for (int i = 0; i < N; ++i) e += ardiff::ex2((v[i] - at) * c);
-            s.z += e;
+            for (int i = 0; i < N; i += 2) {
+                const float2 y = ardiff::apart((ardiff::two(v[i], v[i + 1]) + minus) * c2);
+                s.z = s.z + ardiff::two(ardiff::ex2(y.x), ardiff::ex2(y.y));
+            }
         }
     }
 }
@@ -90,6 +100,8 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) dis
     float* s_q = reinterpret_cast<float*>(s_cache + a.cached);   // [k] teacher's logits, then probabilities
     float* s_x = s_q + a.k;                                  // [k] the student's logits there
     int32_t* s_id = reinterpret_cast<int32_t*>(s_x + a.k);   // [k] -1: no entry
+    int32_t* s_seen = s_id + a.k;                            // [a.seen] ids, each at or behind the place that its bits point to
+    __shared__ int s_again;                                  // whether an id occurs more than once
     __shared__ MaxSum s_part[kWarps], s_entries[kWarps];
     __shared__ MaxSum s_own;
     __shared__ float s_loss[kWarps];
@@ -115,6 +127,10 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) dis
             if (j < n_q) q[j] = __ldg(body + p + j * kThreads);
     };
     if (MODE != BACKWARD) load(p0 + tid);
+    if (MODE != FORWARD) {
+        for (int j = tid; j < a.seen; j += kThreads) s_seen[j] = -1;
+        if (tid == 0) s_again = 0;
+    }
     bool some = false;
     for (int j = tid; j < a.k; j += kThreads) {
         int id = a.ids[row * a.k + j];
@@ -138,16 +154,31 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) dis
     }
     // this thread's entries: their largest and the sum of their exponentials above it
     MaxSum t{-INFINITY, 0.f};
-    for (int j = tid; j < a.k; j += kThreads)
-        if (s_id[j] >= 0) t = merge(t, MaxSum{s_q[j], 1.f}, c);
+    const bool entries = warp * 32 < a.k;                    // this warp has some
+    for (int j = tid; j < a.k; j += kThreads) {
+        const int id = s_id[j];
+        if (id < 0) continue;
+        t = merge(t, MaxSum{s_q[j], 1.f}, c);
+        if (MODE != FORWARD) {
+            unsigned h = (unsigned)id * 2654435761u;
+            for (;;) {                                       // (more places than ids)
+                h &= (unsigned)(a.seen - 1);
+                const int there = atomicCAS(&s_seen[h], -1, id);
+                if (there == id) s_again = 1;
+                if (there == id || there == -1) break;
+                ++h;
+            }
+        }
+    }
     auto reduce_entries = [&]() {
+        if (!entries) return;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1)
             t = merge(t, MaxSum{__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.z, o)}, c);
         if (lane == 0) s_entries[warp] = t;
     };
-    auto add_warps = [&](const MaxSum* w) {                  // every warp for itself, one value a lane
-        MaxSum v = lane < kWarps ? w[lane] : MaxSum{-INFINITY, 0.f};
+    auto add_warps = [&](const MaxSum* w, int n) {           // every warp for itself, one value a lane
+        MaxSum v = lane < n ? w[lane] : MaxSum{-INFINITY, 0.f};
 #pragma unroll
         for (int o = kWarps / 2; o > 0; o >>= 1)
             v = merge(v, MaxSum{__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.z, o)}, c);
@@ -155,7 +186,7 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) dis
     };
     float m, ln_z, scale;
     if (MODE != BACKWARD) {
-        MaxSum s{-INFINITY, 0.f};
+        Running run{-INFINITY, ardiff::two(0.f, 0.f)};
 #pragma unroll 1
         for (int p = p0 + tid; n_q > 0; p += kAhead * kThreads) {
             if (MODE == STEP) {
@@ -163,9 +194,11 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) dis
                 for (int j = 0; j < kAhead; ++j)
                     if (j < n_q && p - p0 + j * kThreads < a.cached) s_cache[p - p0 + j * kThreads] = q[j];
             }
-            take<T, kAhead>(s, q, n_q, c);
+            take<T, kAhead>(run, q, n_q, c);
             load(p + kAhead * kThreads);
         }
+        const float2 sums = ardiff::apart(run.z);
+        MaxSum s{run.m, sums.x + sums.y};
         const int edge = part == 0 && tid < x.lead ? tid : part == a.parts - 1 && x.tail() + tid < a.V ? x.tail() + tid : -1;
         const int both = part == 0 && tid < x.lead && part == a.parts - 1 && x.tail() + tid < a.V ? x.tail() + tid : -1;
         if (edge >= 0) {
@@ -182,7 +215,7 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) dis
         if (lane == 0) s_part[warp] = s;
         reduce_entries();
         __syncthreads();
-        s = add_warps(s_part);
+        s = add_warps(s_part, kWarps);
         if (a.parts > 1) {
             cg::cluster_group cl = cg::this_cluster();
             if (tid == 0) s_own = s;
@@ -201,7 +234,7 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) dis
         reduce_entries();
         __syncthreads();
     }
-    t = add_warps(s_entries);
+    if (entries) t = add_warps(s_entries, min(kWarps, (a.k + 31) / 32));
     const float top = t.m, ln = logf(t.z);
     // the teacher's probabilities; this row's loss
     float loss = 0.f;
@@ -228,6 +261,7 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) dis
     if (MODE != FORWARD) {
         const float l2 = MODE == BACKWARD ? ln_z * 1.4426950408889634f : 0.f;
         auto prob = [&](float v) { return ardiff::ex2((v - m) * c - l2); };
+        const ardiff::Two minus = ardiff::two(-m, -m), c2 = ardiff::two(c, c), scale2 = ardiff::two(scale, scale);
         T* out = grad + x.lead;
         const bool wide = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
 #pragma unroll 1
@@ -247,7 +281,12 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) dis
                 float v[N];
                 ardiff::unpack(r[j], v, T());
 #pragma unroll
-                for (int l = 0; l < N; ++l) v[l] = prob(v[l]) * scale;
+                for (int l = 0; l < N; l += 2) {
+                    const float2 y = ardiff::apart((ardiff::two(v[l], v[l + 1]) + minus) * c2);
+                    const float2 e = ardiff::apart(ardiff::two(ardiff::ex2(y.x - l2), ardiff::ex2(y.y - l2)) * scale2);
+                    v[l] = e.x;
+                    v[l + 1] = e.y;
+                }
                 if (wide) {
                     __stcs(reinterpret_cast<uint4*>(out) + i, ardiff::pack(v, T()));
                 } else {
@@ -265,14 +304,21 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) dis
         // the entries' places once more, with the teacher's share in the sum before it is rounded; an id that occurs again has
         // the sum of its shares, and every one of them writes the same
         const float share = a.weight[row] * a.inv_t;
-        for (int j = warp; j < a.k; j += kWarps) {
-            const int id = s_id[j];
-            if (id < v0 || id >= v1) continue;
-            float q_sum = 0.f;
-            for (int i = lane; i < a.k; i += 32) q_sum += s_id[i] == id ? s_q[i] : 0.f;
+        if (!s_again) {
+            for (int j = tid; j < a.k; j += kThreads) {
+                const int id = s_id[j];
+                if (id >= v0 && id < v1) grad[id] = ardiff::from_float<T>(prob(s_x[j]) * scale - s_q[j] * share);
+            }
+        } else {
+            for (int j = warp; j < a.k; j += kWarps) {
+                const int id = s_id[j];
+                if (id < v0 || id >= v1) continue;
+                float q_sum = 0.f;
+                for (int i = lane; i < a.k; i += 32) q_sum += s_id[i] == id ? s_q[i] : 0.f;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) q_sum += __shfl_xor_sync(0xffffffffu, q_sum, o);
-            if (lane == 0) grad[id] = ardiff::from_float<T>(prob(s_x[j]) * scale - q_sum * share);
+                for (int o = 16; o > 0; o >>= 1) q_sum += __shfl_xor_sync(0xffffffffu, q_sum, o);
+                if (lane == 0) grad[id] = ardiff::from_float<T>(prob(s_x[j]) * scale - q_sum * share);
+            }
         }
     }
     if (MODE != BACKWARD && a.parts > 1) cg::this_cluster().sync();      // a CTA leaves when its part has been read
@@ -286,7 +332,7 @@ int launch(const Args& a, int64_t n, cudaStream_t st) {
         if (cudaGetDevice(&dev) != cudaSuccess) return ARDIFF_ERR_CUDA;
         if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
             if (cudaFuncSetAttribute(distill_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     kCache + ARDIFF_DISTILL_MAX_K * 12) != cudaSuccess)
+                                     kCache + ARDIFF_DISTILL_MAX_K * 20) != cudaSuccess)
                 return ARDIFF_ERR_CUDA;
             if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
         }
@@ -297,7 +343,7 @@ int launch(const Args& a, int64_t n, cudaStream_t st) {
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = MODE == BACKWARD ? 1 : a.parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)(n * a.parts)); cfg.blockDim = dim3(kThreadsOf<MODE>);
-    cfg.dynamicSmemBytes = (size_t)a.k * 12 + (size_t)a.cached * 16; cfg.stream = st;
+    cfg.dynamicSmemBytes = (size_t)a.k * 12 + (size_t)a.seen * 4 + (size_t)a.cached * 16; cfg.stream = st;
     cfg.attrs = at; cfg.numAttrs = 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, distill_kernel<T, MODE>, a);
     ardiff::set_launch_count(1);
@@ -332,6 +378,8 @@ int dispatch(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld
     a.parts = 1;
     while (a.parts < 8 && n * a.parts < 148 * 2 && pieces >= (int64_t)8 * kThreadsOf<MODE> * a.parts)
         a.parts *= 2;
+    if (MODE != FORWARD)
+        for (a.seen = 2; a.seen < 2 * k; a.seen *= 2) {}
     if (MODE == STEP) a.cached = (int)std::min<int64_t>((pieces + a.parts - 1) / a.parts, kCache / 16);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (dtype == ARDIFF_F32) return launch<float, MODE>(a, n, st);
