@@ -262,16 +262,38 @@ def ardiff_accept_prefix(r, ratio, gamma: int, block_len=None, stream=None):
     return out[:(n + gamma - 1) // gamma]
 
 
-_DTYPES = None
+class _Torch:
+    """What the calls below ask of torch every time, looked up once (they take microseconds in all, so lookups count)."""
 
-
-def _dtype(t) -> int:
-    """A tensor's type by the library's number; one that it has no number for is refused there."""
-    global _DTYPES
-    if _DTYPES is None:
+    def __init__(self):
         import torch
-        _DTYPES = {torch.bfloat16: ARDIFF_BF16, torch.float16: ARDIFF_F16, torch.float32: ARDIFF_F32}
-    return _DTYPES.get(t.dtype, -1)
+        self.i32, self.i64, self.f32 = torch.int32, torch.int64, torch.float32
+        self.types = {torch.bfloat16: ARDIFF_BF16, torch.float16: ARDIFF_F16, torch.float32: ARDIFF_F32}
+        self.empty, self.device = torch.empty, torch.cuda.device
+        self.current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+_torch = None
+
+
+def _t() -> _Torch:
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    return _torch
+
+
+def _run(fn, where: str, index: int, stream, *args):
+    """fn(*args, stream) with the device of the tensors current; raises on an error."""
+    t = _torch
+    if t.current() == index:
+        rc = fn(*args, t.stream(index) if stream is None else stream.cuda_stream)
+    else:
+        with t.device(index):
+            rc = fn(*args, t.stream(index) if stream is None else stream.cuda_stream)
+    if rc:
+        raise ArdiffError(rc, where)
 
 
 def _ptr(t):
@@ -281,41 +303,67 @@ def _ptr(t):
 def _rows(x) -> int:
     """Distance of the rows of a matrix whose rows are contiguous (one row, or one column, may have any)."""
     n, V = x.shape
+    if x.is_contiguous():
+        return V
     assert V <= 1 or x.stride(1) == 1, "rows must be contiguous"
     ld = x.stride(0) if n > 1 else V
     assert ld >= V, "rows must not overlap"
     return ld
 
 
-def _int32(t, shape, dev):
-    import torch
-    assert t.dtype == torch.int32 and t.device == dev and t.is_contiguous() and t.shape == shape, (t.dtype, t.shape, shape)
+def _check_i32(x, n: int, index: int):
+    assert x.dtype is _torch.i32 and x.numel() == n and x.get_device() == index and x.is_contiguous(), \
+        f"int32 tensor of {n} entries on cuda:{index} expected, got {x.dtype} {tuple(x.shape)} on {x.device}"
+
+
+def _check_f32(x, n: int, index: int):
+    assert x.dtype is _torch.f32 and x.numel() == n and x.get_device() == index and x.is_contiguous(), \
+        f"float32 tensor of {n} entries on cuda:{index} expected, got {x.dtype} {tuple(x.shape)} on {x.device}"
 
 
 def ardiff_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None, stream=None):
     """The next token of every row of logits [n, V] (bf16, f16 or f32 CUDA tensor, rows contiguous) by the uniform numbers u
     (f32 [n], 0 <= u < 1). temperature, top_p, min_p (f32 [n]) and top_k (int32 [n]) are every row's own, or None (off).
     Returns (token int32 [n], logprob f32 [n]); -1 and NaN for rows that have no softmax or bad settings."""
-    import torch
+    t = _t()
     n, V = logits.shape
-    dev = logits.device
-    assert logits.is_cuda
-    for t in (u, temperature, top_p, min_p):
-        if t is not None:
-            assert t.dtype == torch.float32 and t.device == dev and t.is_contiguous() and t.shape == (n,)
+    index = logits.get_device()
+    assert index >= 0
+    for x in (u, temperature, top_p, min_p):
+        if x is not None:
+            _check_f32(x, n, index)
     if top_k is not None:
-        _int32(top_k, (n,), dev)
+        _check_i32(top_k, n, index)
     if token is None:
-        token = torch.empty((n,), dtype=torch.int32, device=dev)
+        token = t.empty((n,), dtype=t.i32, device=logits.device)
     else:
-        _int32(token, (n,), dev)
-    logprob = _float_rows(logprob, (n,), dev)
-    with _on(dev):
-        rc = lib().ardiff_sample_tokens(logits.data_ptr(), _dtype(logits), n, V, _rows(logits), u.data_ptr(), _ptr(temperature),
-                                        _ptr(top_k), _ptr(top_p), _ptr(min_p), token.data_ptr(), logprob.data_ptr(),
-                                        _stream_ptr(stream))
-    _check(rc, "ardiff_sample_tokens")
+        _check_i32(token, n, index)
+    if logprob is None:
+        logprob = t.empty((n,), dtype=t.f32, device=logits.device)
+    else:
+        _check_f32(logprob, n, index)
+    _run(lib().ardiff_sample_tokens, "ardiff_sample_tokens", index, stream, logits.data_ptr(), t.types.get(logits.dtype, -1), n, V,
+         _rows(logits), u.data_ptr(), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), token.data_ptr(), logprob.data_ptr())
     return token, logprob
+
+
+def _pages_args(length, other, table, free_pages, free_count):
+    R, width = table.shape
+    index = length.get_device()
+    assert index >= 0
+    _check_i32(length, R, index)
+    _check_i32(other, R, index)
+    _check_i32(table, R * width, index)
+    _check_i32(free_pages, free_pages.numel(), index)
+    _check_i32(free_count, 1, index)
+    return R, width, index
+
+
+def _made_i32(x, n: int, like):
+    if x is None:
+        return _torch.empty((n,), dtype=_torch.i32, device=like.device)
+    _check_i32(x, n, like.get_device())
+    return x
 
 
 def ardiff_pages_extend(length, add, table, free_pages, free_count, page: int, slot, position=None, request=None, offset=None,
@@ -324,79 +372,60 @@ def ardiff_pages_extend(length, add, table, free_pages, free_count, page: int, s
     place, slot / position / request of every new token (as many as fit in slot; position and request are written if
     passed). int32 CUDA tensors, slot int64. new_length may be `length` and new_free_count `free_count`; what is not passed is
     allocated. Returns (offset [R + 1], new_length [R], new_free_count [1], status [1]); status is not looked at here."""
-    import torch
-    dev, R = length.device, length.shape[0]
-    assert length.is_cuda and table.dim() == 2
-    for t, shape in ((length, (R,)), (add, (R,)), (table, (R, table.shape[1])), (free_count, (1,))):
-        _int32(t, shape, dev)
-    _int32(free_pages, (free_pages.shape[0],), dev)
-    assert slot.dtype == torch.int64 and slot.device == dev and slot.is_contiguous() and slot.dim() == 1
-    tokens = slot.shape[0]
-    for t in (position, request):
-        if t is not None:
-            _int32(t, (tokens,), dev)
-    made = []
-    for t, size in ((offset, R + 1), (new_length, R), (new_free_count, 1), (status, 1)):
-        if t is None:
-            t = torch.empty((size,), dtype=torch.int32, device=dev)
-        else:
-            _int32(t, (size,), dev)
-        made.append(t)
-    with _on(dev):
-        rc = lib().ardiff_pages_extend(R, page, table.shape[1], length.data_ptr(), add.data_ptr(), table.data_ptr(),
-                                       free_pages.data_ptr(), free_pages.shape[0], free_count.data_ptr(), tokens,
-                                       slot.data_ptr(), _ptr(position), _ptr(request), made[0].data_ptr(),
-                                       made[1].data_ptr(), made[2].data_ptr(), made[3].data_ptr(), _stream_ptr(stream))
-    _check(rc, "ardiff_pages_extend")
-    return tuple(made)
+    t = _t()
+    R, width, index = _pages_args(length, add, table, free_pages, free_count)
+    tokens = slot.numel()
+    assert slot.dtype is t.i64 and slot.get_device() == index and slot.is_contiguous()
+    if position is not None:
+        _check_i32(position, tokens, index)
+    if request is not None:
+        _check_i32(request, tokens, index)
+    offset = _made_i32(offset, R + 1, length)
+    new_length = _made_i32(new_length, R, length)
+    new_free_count = _made_i32(new_free_count, 1, length)
+    status = _made_i32(status, 1, length)
+    _run(lib().ardiff_pages_extend, "ardiff_pages_extend", index, stream, R, page, width, length.data_ptr(), add.data_ptr(),
+         table.data_ptr(), free_pages.data_ptr(), free_pages.numel(), free_count.data_ptr(), tokens, slot.data_ptr(), _ptr(position),
+         _ptr(request), offset.data_ptr(), new_length.data_ptr(), new_free_count.data_ptr(), status.data_ptr())
+    return offset, new_length, new_free_count, status
 
 
 def ardiff_pages_truncate(length, target, table, free_pages, free_count, page: int, new_free_count=None, status=None,
                           stream=None):
     """Leaves request r of a paged cache its first target[r] tokens; the pages that none of them needs go back to the free list
     (in place). int32 CUDA tensors; new_free_count may be `free_count`. Returns (new_free_count [1], status [1])."""
-    import torch
-    dev, R = length.device, length.shape[0]
-    assert length.is_cuda and table.dim() == 2
-    for t, shape in ((length, (R,)), (target, (R,)), (table, (R, table.shape[1])), (free_count, (1,))):
-        _int32(t, shape, dev)
-    _int32(free_pages, (free_pages.shape[0],), dev)
-    made = []
-    for t in (new_free_count, status):
-        if t is None:
-            t = torch.empty((1,), dtype=torch.int32, device=dev)
-        else:
-            _int32(t, (1,), dev)
-        made.append(t)
-    with _on(dev):
-        rc = lib().ardiff_pages_truncate(R, page, table.shape[1], length.data_ptr(), target.data_ptr(), table.data_ptr(),
-                                         free_pages.data_ptr(), free_pages.shape[0], free_count.data_ptr(),
-                                         made[0].data_ptr(), made[1].data_ptr(), _stream_ptr(stream))
-    _check(rc, "ardiff_pages_truncate")
-    return tuple(made)
+    _t()
+    R, width, index = _pages_args(length, target, table, free_pages, free_count)
+    new_free_count = _made_i32(new_free_count, 1, length)
+    status = _made_i32(status, 1, length)
+    _run(lib().ardiff_pages_truncate, "ardiff_pages_truncate", index, stream, R, page, width, length.data_ptr(), target.data_ptr(),
+         table.data_ptr(), free_pages.data_ptr(), free_pages.numel(), free_count.data_ptr(), new_free_count.data_ptr(),
+         status.data_ptr())
+    return new_free_count, status
 
 
 def _distill_args(logits, teacher, ids):
-    assert logits.is_cuda and logits.dim() == 2 and teacher.dim() == 2
-    assert teacher.is_contiguous() and teacher.device == logits.device and teacher.shape[0] == logits.shape[0]
-    _int32(ids, teacher.shape, logits.device)
-    return (logits.data_ptr(), _dtype(logits), logits.shape[0], logits.shape[1], _rows(logits), teacher.data_ptr(),
-            _dtype(teacher), ids.data_ptr(), teacher.shape[1])
+    t = _t()
+    n, V = logits.shape
+    k = teacher.shape[1]
+    index = logits.get_device()
+    assert index >= 0 and teacher.get_device() == index and teacher.is_contiguous() and teacher.shape[0] == n
+    _check_i32(ids, n * k, index)
+    return index, (logits.data_ptr(), t.types.get(logits.dtype, -1), n, V, _rows(logits), teacher.data_ptr(),
+                   t.types.get(teacher.dtype, -1), ids.data_ptr(), k)
 
 
-def _float_rows(t, shape, dev):
-    import torch
-    if t is None:
-        return torch.empty(shape, dtype=torch.float32, device=dev)
-    assert t.dtype == torch.float32 and t.device == dev and t.is_contiguous() and t.shape == shape, (t.dtype, t.shape, shape)
-    return t
+def _made_f32(x, shape, n: int, like):
+    if x is None:
+        return _torch.empty(shape, dtype=_torch.f32, device=like.device)
+    _check_f32(x, n, like.get_device())
+    return x
 
 
-def _grad_rows(grad, logits):
-    import torch
+def _made_grad(grad, logits):
     if grad is None:
-        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    assert grad.dtype == logits.dtype and grad.device == logits.device and grad.shape == logits.shape
+        return _torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    assert grad.dtype is logits.dtype and grad.get_device() == logits.get_device() and grad.shape == logits.shape
     return grad
 
 
@@ -404,43 +433,36 @@ def ardiff_distill_topk(logits, teacher, ids, temperature: float = 1.0, loss=Non
     """Divergence of every row of a student's logits [n, V] (bf16, f16 or f32, rows contiguous) from the softmax of the teacher's
     entries (teacher [n, k] at ids [n, k] int32; ids outside 0 .. V - 1 are no entries).
     Returns (loss f32 [n], stats f32 [n, 2]: what ardiff_distill_topk_backward needs of the rows)."""
-    args = _distill_args(logits, teacher, ids)
-    n, dev = logits.shape[0], logits.device
-    loss, stats = _float_rows(loss, (n,), dev), _float_rows(stats, (n, 2), dev)
-    with _on(dev):
-        rc = lib().ardiff_distill_topk(*args, temperature, loss.data_ptr(), stats.data_ptr(), _stream_ptr(stream))
-    _check(rc, "ardiff_distill_topk")
+    index, args = _distill_args(logits, teacher, ids)
+    n = logits.shape[0]
+    loss, stats = _made_f32(loss, (n,), n, logits), _made_f32(stats, (n, 2), 2 * n, logits)
+    _run(lib().ardiff_distill_topk, "ardiff_distill_topk", index, stream, *args, temperature, loss.data_ptr(), stats.data_ptr())
     return loss, stats
 
 
 def ardiff_distill_topk_backward(logits, teacher, ids, stats, weight, temperature: float = 1.0, grad=None, stream=None):
     """Gradient of sum(weight * loss) with respect to the logits, from the stats that ardiff_distill_topk gave for the same
     inputs; in the logits' type. `grad` may be `logits`."""
-    args = _distill_args(logits, teacher, ids)
-    n, dev = logits.shape[0], logits.device
-    assert stats is not None and weight is not None
-    grad = _grad_rows(grad, logits)
-    stats, weight = _float_rows(stats, (n, 2), dev), _float_rows(weight, (n,), dev)
-    with _on(dev):
-        rc = lib().ardiff_distill_topk_backward(*args, temperature, stats.data_ptr(), weight.data_ptr(), grad.data_ptr(),
-                                                _rows(grad), _stream_ptr(stream))
-    _check(rc, "ardiff_distill_topk_backward")
+    index, args = _distill_args(logits, teacher, ids)
+    n = logits.shape[0]
+    _check_f32(stats, 2 * n, index)
+    _check_f32(weight, n, index)
+    grad = _made_grad(grad, logits)
+    _run(lib().ardiff_distill_topk_backward, "ardiff_distill_topk_backward", index, stream, *args, temperature, stats.data_ptr(),
+         weight.data_ptr(), grad.data_ptr(), _rows(grad))
     return grad
 
 
 def ardiff_distill_topk_step(logits, teacher, ids, weight, temperature: float = 1.0, loss=None, stats=None, grad=None,
                              stream=None):
     """Loss, stats and the gradient of sum(weight * loss) in one pass. `grad` may be `logits`. Returns (loss, stats, grad)."""
-    args = _distill_args(logits, teacher, ids)
-    n, dev = logits.shape[0], logits.device
-    assert weight is not None
-    grad = _grad_rows(grad, logits)
-    loss, stats = _float_rows(loss, (n,), dev), _float_rows(stats, (n, 2), dev)
-    weight = _float_rows(weight, (n,), dev)
-    with _on(dev):
-        rc = lib().ardiff_distill_topk_step(*args, temperature, weight.data_ptr(), loss.data_ptr(), stats.data_ptr(),
-                                            grad.data_ptr(), _rows(grad), _stream_ptr(stream))
-    _check(rc, "ardiff_distill_topk_step")
+    index, args = _distill_args(logits, teacher, ids)
+    n = logits.shape[0]
+    _check_f32(weight, n, index)
+    grad = _made_grad(grad, logits)
+    loss, stats = _made_f32(loss, (n,), n, logits), _made_f32(stats, (n, 2), 2 * n, logits)
+    _run(lib().ardiff_distill_topk_step, "ardiff_distill_topk_step", index, stream, *args, temperature, weight.data_ptr(),
+         loss.data_ptr(), stats.data_ptr(), grad.data_ptr(), _rows(grad))
     return loss, stats, grad
 
 
