@@ -1462,7 +1462,7 @@ template <typename T>
 int launch(Args a, int64_t n, cudaStream_t st) {
     // More CTAs a row while there is room for them and each keeps so many pieces that it gains: a list is one CTA's work, and the others
     // cost it meetings (1 x 32768 bf16 with top-k: 18.7 us with one CTA, 22.6 with four; sums of all weights: 22.5 and 18.5).
-    const int64_t least = a.top_k ? 4096 : 1024;
+    const int64_t least = a.top_k ? 2048 : 1024;
     const int64_t pieces = ((int64_t)a.V + ardiff::Piece<T>::N - 1) / ardiff::Piece<T>::N;
     int parts = 1;
     while (parts < kMaxParts && n * parts < 148 * 2 && pieces >= 2 * parts * least) parts *= 2;
