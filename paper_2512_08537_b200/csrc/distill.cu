@@ -16,6 +16,7 @@
 
 #include "../../include/ardiff.h"
 #include "common.cuh"
+#include "launch.cuh"
 #include "rows.cuh"
 
 namespace cg = cooperative_groups;
@@ -93,6 +94,7 @@ __device__ __forceinline__ void take(Running& s, const uint4 (&q)[kAhead], int n
 template <typename T, int MODE>
 __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : 3) distill_kernel(const Args a) {
     constexpr int kThreads = kThreadsOf<MODE>, kWarps = kThreads / 32, kAhead = kAheadOf<MODE>;
+    ardiff::begin_kernel();
     using ardiff::Row;
     constexpr int N = ardiff::Piece<T>::N;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -337,17 +339,11 @@ int launch(const Args& a, int64_t n, cudaStream_t st) {
             if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
         }
     }
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = MODE == BACKWARD ? 1 : a.parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(n * a.parts)); cfg.blockDim = dim3(kThreadsOf<MODE>);
-    cfg.dynamicSmemBytes = (size_t)a.k * 12 + (size_t)a.seen * 4 + (size_t)a.cached * 16; cfg.stream = st;
-    cfg.attrs = at; cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, distill_kernel<T, MODE>, a);
+    const size_t shared = (size_t)a.k * 12 + (size_t)a.seen * 4 + (size_t)a.cached * 16;
+    const bool ok = ardiff::launch_early(distill_kernel<T, MODE>, (unsigned)(n * a.parts), kThreadsOf<MODE>, MODE == BACKWARD ? 1u : (unsigned)a.parts,
+                                         shared, st, a);
     ardiff::set_launch_count(1);
-    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+    return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
 }
 
 template <int MODE>

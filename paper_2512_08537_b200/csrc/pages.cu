@@ -19,6 +19,7 @@
 
 #include "../../include/ardiff.h"
 #include "common.cuh"
+#include "launch.cuh"
 
 namespace {
 
@@ -146,6 +147,7 @@ template <bool WRITE>
 __global__ void __launch_bounds__(kThreads) extend_kernel(const Extend a) {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ Sums s_scan[32];
+    ardiff::begin_kernel();
     Tile& t = *reinterpret_cast<Tile*>(smem);
     const int tid = threadIdx.x;
     const bool one = a.requests <= kTile;
@@ -224,7 +226,7 @@ __global__ void __launch_bounds__(kThreads) extend_write_kernel(const Extend a) 
     __shared__ Sums s_scan[32];
     Tile& t = *reinterpret_cast<Tile*>(smem);
     const int tid = threadIdx.x;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    ardiff::begin_kernel();
     const int total = a.offset[a.requests];
     const int quads = (total + 3) / 4;
     const int per = (quads + gridDim.x - 1) / gridDim.x;
@@ -294,6 +296,7 @@ struct Truncate {
 __global__ void __launch_bounds__(kThreads) truncate_kernel(const Truncate a) {
     __shared__ Sums s_scan[32];
     __shared__ int s_first[kTile + 1], s_stay[kTile];
+    ardiff::begin_kernel();
     const int tid = threadIdx.x;
     const bool one = a.requests <= kTile;
     int stay[kPer], back[kPer];
@@ -403,22 +406,14 @@ extern "C" int ardiff_pages_extend(int32_t requests, int32_t page, int32_t width
     const int sms = prepare_device();
     if (sms < 1) return ARDIFF_ERR_CUDA;
     if (max_tokens <= kOneLaunchTokens) {
-        extend_kernel<true><<<1, kThreads, sizeof(Tile), st>>>(a);
+        const bool ok = ardiff::launch_early(extend_kernel<true>, 1, kThreads, 1, sizeof(Tile), st, a);
         ardiff::set_launch_count(1);
-        return cudaGetLastError() == cudaSuccess ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+        return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
     }
-    extend_kernel<false><<<1, kThreads, 0, st>>>(a);
-    if (cudaGetLastError() != cudaSuccess) return ARDIFF_ERR_CUDA;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(sms); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = sizeof(Tile); cfg.stream = st;
-    cfg.attrs = at; cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, extend_write_kernel, a);
+    const bool ok = ardiff::launch_early(extend_kernel<false>, 1, kThreads, 1, 0, st, a) &&
+                    ardiff::launch_early(extend_write_kernel, (unsigned)sms, kThreads, 1, sizeof(Tile), st, a);
     ardiff::set_launch_count(2);
-    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+    return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
 }
 
 extern "C" int ardiff_pages_truncate(int32_t requests, int32_t page, int32_t width, const int32_t* length,
@@ -436,7 +431,7 @@ extern "C" int ardiff_pages_truncate(int32_t requests, int32_t page, int32_t wid
     a.length = length; a.target = target; a.table = table; a.free_pages = free_pages; a.free_count = free_count;
     a.new_free_count = new_free_count; a.status = status; a.free_capacity = free_capacity;
     a.requests = requests; a.page = page; a.width = width;
-    truncate_kernel<<<1, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    const bool ok = ardiff::launch_early(truncate_kernel, 1, kThreads, 1, 0, static_cast<cudaStream_t>(stream), a);
     ardiff::set_launch_count(1);
-    return cudaGetLastError() == cudaSuccess ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+    return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
 }

@@ -26,6 +26,7 @@
 
 #include "../../include/ardiff.h"
 #include "common.cuh"
+#include "launch.cuh"
 #include "rows.cuh"
 
 namespace cg = cooperative_groups;
@@ -1070,6 +1071,7 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     constexpr int N = ardiff::Piece<T>::N;
     __shared__ Shared s;
+    ardiff::begin_kernel();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row = blockIdx.x / args.parts;
     Settings o;
@@ -1467,17 +1469,9 @@ int launch(Args a, int64_t n, cudaStream_t st) {
     int parts = 1;
     while (parts < kMaxParts && n * parts < 148 * 2 && pieces >= 2 * parts * least) parts *= 2;
     a.parts = parts;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(n * parts)); cfg.blockDim = dim3(kThreads);
-    cfg.stream = st;
-    cfg.attrs = at; cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, sample_kernel<T>, (const Args)a);
+    const bool ok = ardiff::launch_early(sample_kernel<T>, (unsigned)(n * parts), kThreads, (unsigned)parts, 0, st, a);
     ardiff::set_launch_count(1);
-    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+    return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
 }
 
 }  // namespace
