@@ -406,7 +406,7 @@ int ardiff_pipeline_join(ardiff_pipeline* pipeline, void* stream);
  * equal bits.
  *
  *   logits   dev  [n][V], rows `ld` >= V values apart, of type dtype (ARDIFF_BF16, ARDIFF_F16 or ARDIFF_F32), at any
- *            multiple of its size; read once
+ *            multiple of its size; read once from memory
  *   n        0 <= n < 2^28;  1 <= V <= ARDIFF_SAMPLE_MAX_V
  *   u        dev float [n]: uniform numbers
  *   temperature, top_p, min_p  dev float [n], top_k dev int32 [n], each or NULL: every row's own settings (NULL: 1, 1, 0, 0)

@@ -8,15 +8,25 @@
 // fp32 sums are exact: all weights that decide are formed and summed in fp64 (polynomial of degree 9 after splitting off the
 // integer part, 4e-14 relative), in an order that depends on sizes only.
 //
-// A row belongs to a cluster of one to eight CTAs and is read once, into shared memory, a contiguous part a CTA, of that a
-// contiguous segment a warp. What is done with it depends on its settings:
-//   T = 0                the largest logit's lowest index
-//   top-k, small nuclei  "list": the threads' own largest logits (512 a CTA) bound the k-th largest from below (at least k logits
-//                        lie above the k-th largest of them), and the mass above a bound as well; the few logits above the bound
-//                        go to the first CTA, which sorts them and does the rest alone
-//   no prefix            the segments' sums, then the one segment in which the draw ends
-//   large k or nuclei    "search" for the prefix's last element: histograms narrow a range of logits until it holds few, an exact
-//                        pass sums what lies above it and lists what lies in it, and the sums say whether the range was right
+// A row belongs to a cluster of one to eight CTAs, a contiguous part each, a part to 32 segments, four a warp. A first pass reads the row
+// from memory and keeps every thread's largest logit in every segment (a "group", 1024 a CTA); later passes, over rows that need
+// them, find it in L2. What is done with it depends on its settings:
+//   T = 0                  the largest logit's lowest index
+//   no filter              the first pass sums the segments' weights, too, relative to a reference of the CTA's own, in fp64; then the
+//                          one segment is walked in which the draw ends
+//   top-k, small nuclei,   a list: at least k logits are not below the k-th of the groups' largest, and the mass down to one of those is
+//   few with min-p         at least theirs; the groups with anything above that bound are read again, the first CTA sorts what
+//                          it finds there and does the rest alone
+//   large nuclei           a histogram of the weights says about where the nucleus ends, where a bin holds too many a second one
+//                          more closely; an exact pass sums what lies above that range and lists what lies in it; the sums
+//                          say whether the range was right, and on which side of it to look if it was not
+//   large k                a histogram counts down to the bin of the k-th, which is listed
+//   what none of these     (thousands of different logits closer together than 2^-14 octaves of the weight): a search by the logits
+//   settles                as whole numbers
+//
+// Measured on B200 (L2 flushed, us; floor: the row read once at the measured copy rate), 512 x 131072 bf16, floor 20.5: T = 0 37, top-k 50
+// with top-p 51, no filter 115 (bound by 67 million fp64 weights of 15 instructions, 60 us at 64 a clock and SM), nuclei of tens of
+// tokens 213, of tens of thousands 590. 1 x 32768 bf16 with top-k and top-p: 14, of which a dozen barriers and dependent loads are all.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 #include <limits.h>
@@ -42,7 +52,6 @@ constexpr int kGroups = 4;               // segments a warp; a thread's share of
 constexpr int kSegments = kGroups * kWarps;  // of a CTA's part
 constexpr int kMaxParts = 8;
 constexpr float kSane = 6e4f;            // logits up to which, at temperatures from 1e-3 to 1e3, a first pass can sum
-constexpr double kFar = -100.0;          // weights below 2^kFar count as nothing: all of a row's add up to less than 2^-75 of its sum
 
 struct Args {
     const void* x;
@@ -170,14 +179,16 @@ struct Part {                            // this CTA's part of its row
         const uint4* base = reinterpret_cast<const uint4*>(x + first);     // (aligned; pieces whole0 .. whole1 - 1 are read)
         const int most = whole1 - 1;
         if (begin >= end) return;
+        // (a place outside the whole pieces gives the nearest of them, which is not used)
+        auto load = [&](int p) { return whole0 <= most ? __ldg(base + max(whole0, min(p, most))) : uint4(); };
         uint4 q[AHEAD], next[AHEAD];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) q[i] = next[i] = whole0 <= most ? __ldg(base + max(whole0, min(begin + i * step, most))) : uint4();
+        for (int i = 0; i < AHEAD; ++i) q[i] = next[i] = load(begin + i * step);
 #pragma unroll 1
         for (int p = begin; p < end; p += AHEAD * step) {
             if (p + AHEAD * step < end) {
 #pragma unroll
-                for (int i = 0; i < AHEAD; ++i) next[i] = whole0 <= most ? __ldg(base + max(whole0, min(p + (AHEAD + i) * step, most))) : uint4();
+                for (int i = 0; i < AHEAD; ++i) next[i] = load(p + (AHEAD + i) * step);
             }
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
@@ -558,7 +569,8 @@ __device__ __forceinline__ void answer(const Args& a, int64_t row, int token, fl
 
 // The first CTA alone: s.list[0 .. n) holds every logit that may be kept. `whole`: the mass that top-p is a share of, where it is not
 // the list's own (negative).
-__device__ __forceinline__ void finish_list(const Args& args, int64_t row, Shared& s, const Weights& wt, const Settings& o, int n, double whole) {
+__device__ __forceinline__ void finish_list(const Args& args, int64_t row, Shared& s, const Weights& wt, const Settings& o, int n,
+                                            double whole) {
     sort_list(s, n);
     const int j0 = kEach * threadIdx.x;
     const int limit = o.use_k ? min(o.k, n) : n;
@@ -635,7 +647,8 @@ constexpr int kFine = 10, kCodes = kBins << kFine;
 __device__ __forceinline__ int weight_code(float d, float a32) {
     return __float_as_int(fminf(d * a32 * 16384.0f, (float)(kCodes - 1)) + 8388608.0f) - __float_as_int(8388608.0f);
 }
-// Weights in the middle of bins: of codes first + b step .. first + (b + 1) step - 1; of keys from top - (b << shift) down to the next bin's.
+// Weights in the middle of bins: of codes first + b step .. first + (b + 1) step - 1; of keys from top - (b << shift) down to the
+// next bin's.
 struct CodeBins {
     int first, step;
     __device__ __forceinline__ double operator()(int b) const {
@@ -1281,163 +1294,164 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             double base = r.mass, upto = -1.0;               // the mass in front of them, or that up to their end
             int verdict = kAbove;
             for (int turn = 0; (verdict == kAbove || verdict == kBelow) && turn < 6; ++turn) {
-            if (window) {
-                int shift = 0;
-                while ((last_code - first_code) >> shift >= kBins) ++shift;
-                a.sync();                                    // the last histogram has been read
-                clear_bins(s);
-                __syncthreads();
-                a.each([&](float v, int i) {
-                    const int code = weight_code(m - v, a32);
-                    if (code >= first_code && code <= last_code && cut.keeps(v, i)) count_bin(s, (code - first_code) >> shift);
-                });
-                a.sync();
-                if (!pick(a, false, 0u, enough, false, 0, 0u, base, upto, CodeBins{first_code, 1 << shift}, r)) break;
-                last_code = min(last_code, first_code + ((r.last + 1) << shift) - 1);
-                first_code += r.first << shift;
-            }
-            // the sum of what lies above the range; a list of what lies in it, or, where that is more than a list holds, whether it is
-            // one value, and how often in which segment
-            const bool listed = r.in <= (unsigned)kList;
-            a.sync();
-            if (tid == 0) {
-                s.count = 0u;
-                s.kmin = UINT_MAX;
-                s.kmax = 0u;
-                s.verdict = kUnknown;
-            }
-            a.sync();
-            double sure = 0.0;
-            if (!wt.far) {
-                buf ^= 1;
-                sure = sum_above(a, buf, wt, cut, m, a32, first_code, last_code, listed ? a.at(&s.count, 0) : nullptr, a.at(s.list, 0));
-            }
-            if (listed && !wt.far && a.rank == 0) {
-                const int n = (int)min(s.count, (unsigned)kList);
-                end_in_list(s, wt, false, n, 0u, sure, enough);
-                if (s.verdict == kFound) {
-                    const int kept = s.found + 1;
-                    const bool above = o.use_m && wt.own(entry_value(s.list[0])) < (double)o.mp;
-                    __syncthreads();                         // s.verdict and s.found have been read
-                    // what is kept of the list, in order of index
-                    unsigned long long e[kEach];
-#pragma unroll
-                    for (int i = 0; i < kEach; ++i) e[i] = s.list[kEach * tid + i];
+                if (window) {
+                    int shift = 0;
+                    while ((last_code - first_code) >> shift >= kBins) ++shift;
+                    a.sync();                                    // the last histogram has been read
+                    clear_bins(s);
                     __syncthreads();
-#pragma unroll
-                    for (int i = 0; i < kEach; ++i) {
-                        const int j = kEach * tid + i;
-                        if (j < kept) {
-                            const double w = wt.own(entry_value(e[i]));
-                            s.list[j] = (e[i] & 0xffffffffull) << 32 | (unsigned)j;
-                            s.w[j] = o.use_m && w < (double)o.mp ? 0.0 : w;
-                        }
-                    }
-                    __syncthreads();
-                    sort_list(s, kept);
-                    draw_segment(a, (double)o.u, [&](int g) {
-                        // the entries from the segment's first index on, up to the next one's
-                        const int q0 = min(pieces, g / kSegments * per), mine = min(pieces, q0 + per) - q0;
-                        const int len = (mine + kSegments - 1) / kSegments, at = g % kSegments * len;
-                        const int begin = (q0 + min(mine, at)) * N - shift, end = (q0 + min(mine, at + len)) * N - shift;
-                        int lo = 0, hi = kept;
-                        while (lo < hi) {
-                            const int mid = (lo + hi) >> 1;
-                            if ((int)(s.list[mid] >> 32) < begin) lo = mid + 1; else hi = mid;
-                        }
-                        double sum = *a.at(&s.seg[buf][g % kSegments], g / kSegments);
-                        for (; lo < kept && (int)(s.list[lo] >> 32) < end; ++lo) sum += s.w[(unsigned)s.list[lo]];
-                        return sum;
+                    a.each([&](float v, int i) {
+                        const int code = weight_code(m - v, a32);
+                        if (code >= first_code && code <= last_code && cut.keeps(v, i)) count_bin(s, (code - first_code) >> shift);
                     });
-                    if (tid == 0) s.verdict = above ? kNotNeeded : kFound;
+                    a.sync();
+                    if (!pick(a, false, 0u, enough, false, 0, 0u, base, upto, CodeBins{first_code, 1 << shift}, r)) break;
+                    last_code = min(last_code, first_code + ((r.last + 1) << shift) - 1);
+                    first_code += r.first << shift;
                 }
-            }
-            double need = 0.0;
-            float value = 0.f;
-            if (!listed && !wt.far) {
-                unsigned lo = UINT_MAX, hi = 0u;
-                for (int g = warp * 4; g < warp * 4 + 4; ++g) {
-                    unsigned n = 0;
-                    a.template scan<1>(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const uint4& q, int p) {
-                        float v[N];
-                        ardiff::unpack(q, v, T());
+                // the sum of what lies above the range; a list of what lies in it, or, where that is more than a list holds, whether it is
+                // one value, and how often in which segment
+                const bool listed = r.in <= (unsigned)kList;
+                a.sync();
+                if (tid == 0) {
+                    s.count = 0u;
+                    s.kmin = UINT_MAX;
+                    s.kmax = 0u;
+                    s.verdict = kUnknown;
+                }
+                a.sync();
+                double sure = 0.0;
+                if (!wt.far) {
+                    buf ^= 1;
+                    sure = sum_above(a, buf, wt, cut, m, a32, first_code, last_code, listed ? a.at(&s.count, 0) : nullptr, a.at(s.list, 0));
+                }
+                if (listed && !wt.far && a.rank == 0) {
+                    const int n = (int)min(s.count, (unsigned)kList);
+                    end_in_list(s, wt, false, n, 0u, sure, enough);
+                    if (s.verdict == kFound) {
+                        const int kept = s.found + 1;
+                        const bool above = o.use_m && wt.own(entry_value(s.list[0])) < (double)o.mp;
+                        __syncthreads();                         // s.verdict and s.found have been read
+                        // what is kept of the list, in order of index
+                        unsigned long long e[kEach];
 #pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            const int code = weight_code(m - v[i], a32);
-                            if (code >= first_code && code <= last_code && cut.keeps(v[i], a.first + p * N + i)) {
-                                ++n;
-                                lo = min(lo, key_of(v[i]));
-                                hi = max(hi, key_of(v[i]));
+                        for (int i = 0; i < kEach; ++i) e[i] = s.list[kEach * tid + i];
+                        __syncthreads();
+#pragma unroll
+                        for (int i = 0; i < kEach; ++i) {
+                            const int j = kEach * tid + i;
+                            if (j < kept) {
+                                const double w = wt.own(entry_value(e[i]));
+                                s.list[j] = (e[i] & 0xffffffffull) << 32 | (unsigned)j;
+                                s.w[j] = o.use_m && w < (double)o.mp ? 0.0 : w;
                             }
                         }
-                    });
-                    n = __reduce_add_sync(0xffffffffu, n);
-                    if (lane == 0) s.seg_ties[g] = n;
+                        __syncthreads();
+                        sort_list(s, kept);
+                        draw_segment(a, (double)o.u, [&](int g) {
+                            // the entries from the segment's first index on, up to the next one's
+                            const int q0 = min(pieces, g / kSegments * per), mine = min(pieces, q0 + per) - q0;
+                            const int len = (mine + kSegments - 1) / kSegments, at = g % kSegments * len;
+                            const int begin = (q0 + min(mine, at)) * N - shift, end = (q0 + min(mine, at + len)) * N - shift;
+                            int lo = 0, hi = kept;
+                            while (lo < hi) {
+                                const int mid = (lo + hi) >> 1;
+                                if ((int)(s.list[mid] >> 32) < begin) lo = mid + 1; else hi = mid;
+                            }
+                            double sum = *a.at(&s.seg[buf][g % kSegments], g / kSegments);
+                            for (; lo < kept && (int)(s.list[lo] >> 32) < end; ++lo) sum += s.w[(unsigned)s.list[lo]];
+                            return sum;
+                        });
+                        if (tid == 0) s.verdict = above ? kNotNeeded : kFound;
+                    }
                 }
-                lo = __reduce_min_sync(0xffffffffu, lo);
-                hi = __reduce_max_sync(0xffffffffu, hi);
-                if (lane == 0) {
-                    atomicMin(&s.kmin, lo);
-                    atomicMax(&s.kmax, hi);
+                double need = 0.0;
+                float value = 0.f;
+                if (!listed && !wt.far) {
+                    unsigned lo = UINT_MAX, hi = 0u;
+                    for (int g = warp * kGroups; g < (warp + 1) * kGroups; ++g) {
+                        unsigned n = 0;
+                        a.template scan<1>(g * a.segment + lane, min(a.pieces, (g + 1) * a.segment), 32, [&](const uint4& q, int p) {
+                            float v[N];
+                            ardiff::unpack(q, v, T());
+#pragma unroll
+                            for (int i = 0; i < N; ++i) {
+                                const int code = weight_code(m - v[i], a32);
+                                if (code >= first_code && code <= last_code && cut.keeps(v[i], a.first + p * N + i)) {
+                                    ++n;
+                                    lo = min(lo, key_of(v[i]));
+                                    hi = max(hi, key_of(v[i]));
+                                }
+                            }
+                        });
+                        n = __reduce_add_sync(0xffffffffu, n);
+                        if (lane == 0) s.seg_ties[g] = n;
+                    }
+                    lo = __reduce_min_sync(0xffffffffu, lo);
+                    hi = __reduce_max_sync(0xffffffffu, hi);
+                    if (lane == 0) {
+                        atomicMin(&s.kmin, lo);
+                        atomicMax(&s.kmax, hi);
+                    }
+                    a.sync();
+                    lo = UINT_MAX, hi = 0u;
+                    for (int p = 0; p < a.parts; ++p) {
+                        lo = min(lo, *a.at(&s.kmin, p));
+                        hi = max(hi, *a.at(&s.kmax, p));
+                    }
+                    value = value_of(lo);
+                    const double w = wt.own(value);
+                    need = needed(enough, sure, w, r.in);
+                    if (lo == hi && a.rank == 0 && tid == 0) {
+                        s.verdict = sure >= enough ? kAbove : need > (double)r.in ? kBelow : kFound;
+                        s.mass_in = sure + r.in * w;
+                    }
+                    if (lo == hi && sure < enough && need <= (double)r.in && a.rank == 0) {
+                        const unsigned ties = tid < a.parts * kSegments ? *a.at(&s.seg_ties[tid % kSegments], tid / kSegments) : 0u;
+                        unsigned all;
+                        const unsigned ahead = cta_scan(s, ties, &all);
+                        draw_segment(a, (double)o.u, [&](int g) {
+                            const double kept = fmin(fmax(need - (double)ahead, 0.0), (double)ties);
+                            return *a.at(&s.seg[buf][g % kSegments], g / kSegments) + w * kept;
+                        });
+                        if (tid == s.owner) s.cut_ahead = ahead;
+                        if (tid == 0 && o.use_m && w < (double)o.mp) s.verdict = kNotNeeded;
+                    }
                 }
                 a.sync();
-                lo = UINT_MAX, hi = 0u;
-                for (int p = 0; p < a.parts; ++p) {
-                    lo = min(lo, *a.at(&s.kmin, p));
-                    hi = max(hi, *a.at(&s.kmax, p));
+                verdict = *a.at(&s.verdict, 0);
+                const double with = *a.at(&s.mass_in, 0);
+                if (verdict == kFound) {
+                    owner = *a.at(&s.owner, 0);
+                    before = *a.at(&s.before, 0);
+                    total = *a.at(&s.total, 0);
+                    if (listed) {
+                        cut = Cut{a.at(&s.cut, 0)->value, a.at(&s.cut, 0)->index};
+                    } else {
+                        need -= (double)*a.at(&s.cut_ahead, 0);  // of this value in the draw's segment, lowest indices first
+                    }
                 }
-                value = value_of(lo);
-                const double w = wt.own(value);
-                need = needed(enough, sure, w, r.in);
-                if (lo == hi && a.rank == 0 && tid == 0) {
-                    s.verdict = sure >= enough ? kAbove : need > (double)r.in ? kBelow : kFound;
-                    s.mass_in = sure + r.in * w;
+                a.sync();
+                if (verdict == kFound && owner / kSegments != a.rank) return;
+                if (verdict == kFound && !listed) {
+                    const unsigned ties = s.seg_ties[owner % kSegments];
+                    int index = need <= 0.0 ? -1 : INT_MAX;
+                    if (need > 0.0 && need < (double)ties) index = locate(a, owner, 0.0, need - 0.5, Equal{cut, value});
+                    // (a cut before this one keeps all of the range or is its end)
+                    cut = Cut{value, cut.value == value ? min(index, cut.index) : index};
                 }
-                if (lo == hi && sure < enough && need <= (double)r.in && a.rank == 0) {
-                    const unsigned ties = tid < a.parts * kSegments ? *a.at(&s.seg_ties[tid % kSegments], tid / kSegments) : 0u;
-                    unsigned all;
-                    const unsigned ahead = cta_scan(s, ties, &all);
-                    draw_segment(a, (double)o.u, [&](int g) {
-                        return *a.at(&s.seg[buf][g % kSegments], g / kSegments) + w * fmin(fmax(need - (double)ahead, 0.0), (double)ties);
-                    });
-                    if (tid == s.owner) s.cut_ahead = ahead;
-                    if (tid == 0 && o.use_m && w < (double)o.mp) s.verdict = kNotNeeded;
-                }
-            }
-            a.sync();
-            verdict = *a.at(&s.verdict, 0);
-            const double with = *a.at(&s.mass_in, 0);
-            if (verdict == kFound) {
-                owner = *a.at(&s.owner, 0);
-                before = *a.at(&s.before, 0);
-                total = *a.at(&s.total, 0);
-                if (listed) {
-                    cut = Cut{a.at(&s.cut, 0)->value, a.at(&s.cut, 0)->index};
+                // the estimate was wrong, but the sums next to the range are exact now: the same with a window beside it
+                window = true;
+                if (verdict == kAbove) {
+                    upto = sure;
+                    last_code = first_code - 1;
+                    first_code = max(0, last_code - 4095);
                 } else {
-                    need -= (double)*a.at(&s.cut_ahead, 0);  // of this value in the draw's segment, lowest indices first
+                    upto = -1.0;
+                    base = with;
+                    first_code = last_code + 1;
+                    last_code = min(first_code + 4095, ((kBins - 1) << kFine) - 1);
                 }
-            }
-            a.sync();
-            if (verdict == kFound && owner / kSegments != a.rank) return;
-            if (verdict == kFound && !listed) {
-                const unsigned ties = s.seg_ties[owner % kSegments];
-                int index = need <= 0.0 ? -1 : INT_MAX;
-                if (need > 0.0 && need < (double)ties) index = locate(a, owner, 0.0, need - 0.5, Equal{cut, value});
-                // (a cut before this one keeps all of the range or is its end)
-                cut = Cut{value, cut.value == value ? min(index, cut.index) : index};
-            }
-            // the estimate was wrong, but the sums next to the range are exact now: the same with a window beside it
-            window = true;
-            if (verdict == kAbove) {
-                upto = sure;
-                last_code = first_code - 1;
-                first_code = max(0, last_code - 4095);
-            } else {
-                upto = -1.0;
-                base = with;
-                first_code = last_code + 1;
-                last_code = min(first_code + 4095, ((kBins - 1) << kFine) - 1);
-            }
             }
             if (verdict != kFound && verdict != kNotNeeded) cut = search(a, wt, a32, cut, false, 0u, enough, buf);
         }
