@@ -245,3 +245,21 @@ def test_a_few_steps_of_training_bring_the_student_to_the_teacher():
     change = (loss0 - loss1).double()
     slack = 0.25 * eta * eta * slope + 4e-6
     assert bool(((change - eta * slope).abs() <= slack).all())
+
+
+@pytest.mark.parametrize("what", ["type of ids", "stats of another size", "rows that overlap", "columns apart", "type of logits"])
+def test_tensors_that_do_not_fit_are_refused(what):
+    x, teacher, ids, weight = make(4, 100, 8, torch.float32, seed=1)
+    stats = torch.zeros((4, 2), device=x.device)
+    if what == "type of ids":
+        ids = ids.long()
+    elif what == "stats of another size":
+        stats = stats[:3]
+    elif what == "rows that overlap":
+        x = x[:1].expand(4, 100)
+    elif what == "columns apart":
+        x = x.repeat(1, 2)[:, ::2]
+    else:
+        x = x.double()
+    with pytest.raises((AssertionError, ardiff.ArdiffError)):
+        ardiff.ardiff_distill_topk_backward(x, teacher, ids, stats, weight)

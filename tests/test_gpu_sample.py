@@ -215,6 +215,35 @@ def test_rows_at_any_place(dtype, n, V, pad, offset):
     check(x, u, T=[0.0] * n)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [5e-4, 1e-3, 0.02, 900.0, 1e3, 3e3])
+@pytest.mark.parametrize("shift", [0.0, 5e4, -5e4, 7e4])
+def test_sums_of_the_first_pass_at_any_temperature_and_height(dtype, T, shift):
+    """The first pass sums relative to the first few logits of each part: those may be low, the largest far above them, all of
+    them high or low, the temperature such that most weights are nothing or nearly all are alike."""
+    n, V = 6, 40000
+    x, u = rows(n, V, torch.float32, seed=12)
+    x[1, :20000] -= 30.0                          # the reference is far below the largest
+    x[2, :30000] -= 3000.0
+    x[3, :39999] = -3e5
+    x[4, 4096:] -= 500.0
+    x = (x + shift).to(DTYPES[dtype])
+    check(x, u, T=[T] * n)
+    check(x, u, T=[T] * n, p=[0.9] * n)
+    check(x, u, T=[T] * n, p=[0.9] * n, mp=[0.2] * n)
+
+
+@pytest.mark.parametrize("n,V", [(1, 4096), (1, 20000), (40, 70000), (300, 9000), (700, 1500)])
+def test_settings_that_differ_from_row_to_row_in_one_call(n, V):
+    """Rows that are listed, walked, counted and drawn at once, by clusters of every size."""
+    g = torch.Generator().manual_seed(V)
+    x, u = rows(n, V, torch.bfloat16, seed=13)
+    flat, _ = rows(n, V, torch.bfloat16, seed=14, kind="flat")
+    x[::3] = flat[::3]
+    pick = lambda v: [v[i] for i in torch.randint(0, len(v), (n,), generator=g).tolist()]  # noqa: E731
+    check(x, u, T=pick([0.0, 0.7, 1.0, 2.0]), k=pick([0, 1, 40, 1200, V // 2]), p=pick([1.0, 0.5, 0.9, 0.99]), mp=pick([0.0, 0.0, 0.05]))
+
+
 def test_largest_of_equal_ones_and_both_zeros():
     x = torch.full((4, 4000), -1.0)
     x[0, [70, 3999, 71]] = 2.0

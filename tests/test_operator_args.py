@@ -2,6 +2,7 @@
 import math
 
 import pytest
+import torch
 
 import paper_2512_08537_b200 as ardiff
 
@@ -97,3 +98,16 @@ def test_sample_refuses(kw, code):
 
 def test_sample_of_no_rows_is_nothing():
     assert sample(n=0, logits=None, u=None, token=None, logprob=None) == ardiff.ARDIFF_OK
+
+
+def test_tensors_of_the_host_are_refused():
+    f, i = torch.zeros(4), torch.zeros(4, dtype=torch.int32)
+    table = torch.zeros((4, 2), dtype=torch.int32)
+    with pytest.raises(AssertionError):
+        ardiff.ardiff_sample_tokens(torch.zeros((4, 8)), f)
+    with pytest.raises(AssertionError):
+        ardiff.ardiff_distill_topk(torch.zeros((4, 8)), torch.zeros((4, 2)), table)
+    with pytest.raises(AssertionError):
+        ardiff.ardiff_pages_extend(i, i, table, i, i[:1], 16, torch.zeros(4, dtype=torch.int64))
+    with pytest.raises(AssertionError):
+        ardiff.ardiff_pages_truncate(i, i, table, i, i[:1], 16)
