@@ -350,7 +350,9 @@ __global__ void __launch_bounds__(kThreads) truncate_kernel(const Truncate a) {
         }
         if (tid == kThreads - 1) s_first[kTile] = (int)at.pages;
         __syncthreads();
-        for (int g = s_first[0] + tid; g < s_first[kTile]; g += kThreads) {
+        // (without a sign: the last step may pass 2^31)
+        for (unsigned next = (unsigned)s_first[0] + tid; next < (unsigned)s_first[kTile]; next += kThreads) {
+            const int g = (int)next;
             int below = 0, above = kTile;        // the last request whose first page given back is not behind g
             while (above - below > 1) {
                 const int mid = (below + above) >> 1;

@@ -277,3 +277,16 @@ def test_calls_on_another_stream_than_the_current_one():
     offset, _, _, status = ardiff.ardiff_pages_extend(d.length, more, d.table, d.free, d.count, 16, slot, stream=s)
     s.synchronize()
     assert int(status) == 0 and slot.tolist() == want[0] and offset.tolist() == want[3]
+
+
+def test_pages_given_back_up_to_the_last_number_of_32_bits():
+    """A step of the CTA past the last page would pass 2^31."""
+    W = 2**31 - 600
+    table = torch.arange(W, dtype=torch.int32, device=require_cuda()).reshape(1, W)
+    free = torch.full((W,), GAP, dtype=torch.int32, device=table.device)
+    count, status = ardiff.ardiff_pages_truncate(dev([W]), dev([0]), table, free, dev([0]), 1)
+    assert (int(count), int(status)) == (W, 0)
+    step = 1 << 28
+    for i in range(0, W, step):                   # the last page lowest
+        n = min(step, W - i)
+        assert torch.equal(free[i:i + n], table[0, W - i - n:W - i].flip(0))
