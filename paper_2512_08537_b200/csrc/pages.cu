@@ -93,9 +93,9 @@ struct Tile {
 // Writes the tokens [lo, hi) of a tile of `m` requests from `r0` on: a thread takes four consecutive ones, looks up the
 // request of the first and walks on. `free_top`: the free list's entries before the call.
 __device__ void write_tokens(const Extend& a, const Tile& t, int r0, int m, int lo, int hi, int free_top) {
-    const int q_end = (hi + 3) / 4;
+    const int q_end = (int)(((unsigned)hi + 3u) / 4u);       // (hi may be the last number of 32 bits)
     for (int q = lo / 4 + (int)threadIdx.x; q < q_end; q += kThreads) {
-        const int t0 = max(lo, 4 * q), t1 = min(hi, 4 * q + 4);
+        const int t0 = max(lo, 4 * q), t1 = (int)min((unsigned)hi, 4u * (unsigned)q + 4u);
         int below = 0, above = m;                // the last request whose first token is not behind t0
         while (above - below > 1) {
             const int mid = (below + above) >> 1;
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kThreads) extend_write_kernel(const Extend a) 
     const int tid = threadIdx.x;
     ardiff::begin_kernel();
     const int total = a.offset[a.requests];
-    const int quads = (total + 3) / 4;
+    const int quads = (int)(((unsigned)total + 3u) / 4u);
     const int per = (quads + gridDim.x - 1) / gridDim.x;
     const int lo = (int)min((long long)total, 4ll * per * blockIdx.x), hi = (int)min((long long)total, 4ll * per * (blockIdx.x + 1));
     if (lo >= hi) return;

@@ -290,3 +290,16 @@ def test_pages_given_back_up_to_the_last_number_of_32_bits():
     for i in range(0, W, step):                   # the last page lowest
         n = min(step, W - i)
         assert torch.equal(free[i:i + n], table[0, W - i - n:W - i].flip(0))
+
+
+@pytest.mark.parametrize("tokens", [2**31 - 1, 2**31 - 4])
+def test_tokens_up_to_the_last_number_of_32_bits(tokens):
+    page, width = 1 << 20, 2048
+    slot = torch.full((tokens,), GAP, dtype=torch.int64, device=require_cuda())
+    table, free = dev([[GAP] * width]), dev(list(range(7, 7 + width)))
+    offset, length, count, status = ardiff.ardiff_pages_extend(dev([0]), dev([tokens]), table, free, dev([width]), page, slot)
+    assert (offset.tolist(), int(length), int(count), int(status)) == ([0, tokens], tokens, 0, 0)
+    assert table[0].tolist() == free.tolist()[::-1]
+    for p in range(width):
+        lo, n = p * page, min(page, tokens - p * page)
+        assert torch.equal(slot[lo:lo + n], torch.arange(n, device=slot.device) + int(6 + width - p) * page)
