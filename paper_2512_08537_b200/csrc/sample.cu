@@ -51,6 +51,7 @@ constexpr int kEach = 4;                 // list entries, bins a thread
 constexpr int kGroups = 4;               // segments a warp; a thread's share of one is a group, whose largest logit is kept
 constexpr int kSegments = kGroups * kWarps;  // of a CTA's part
 constexpr int kMaxParts = 8;
+constexpr float kLeastU = 0x1p-24f;      // below it, u asks how nothing adds up: every weight counts as what it is
 constexpr float kSane = 6e4f;            // logits up to which, at temperatures from 1e-3 to 1e3, a first pass can sum
 
 struct Args {
@@ -133,12 +134,12 @@ __device__ __forceinline__ double pow2(double d, double a) {
 }
 
 // The weights of a row. Sums over many use bulk(): logits below `lowest` count as 2^-100 each, which is nothing beside the largest
-// one's 1 (2^18 of them are 2^-82; at most 2^-57 where fp32 had to round `lowest`). One that may be drawn has its own() weight, down to
-// fp64's smallest.
+// one's 1 and to the least u (2^18 of them are 2^-82; at most 2^-77 where fp32 had to round `lowest`). One that may be drawn has its own()
+// weight, down to fp64's smallest.
 struct Weights {
     double m, a;                         // the largest logit, log2(e) / T
     float lowest;
-    bool far;                            // bulk() will not do: u = 0 asks for the first token of any weight at all; temperatures
+    bool far;                            // bulk() will not do: a tiny u asks for the first tokens of any weight at all; temperatures
                                          // so high, or so low, that fp32 has no such `lowest`
     __device__ __forceinline__ double bulk(float v) const { return pow2((double)fmaxf(v, lowest) - m, a); }
     __device__ __noinline__ static double exact(double y) { return y >= -1100.0 ? exp2(y) : 0.0; }
@@ -403,6 +404,26 @@ __device__ __noinline__ int locate(const Part<T> a, const int g, double carry, c
         __syncthreads();
         if (s.found != INT_MAX) break;
     }
+    return s.found != INT_MAX ? s.found : s.last;
+}
+
+// Where the segment of a draw holds nothing (all of it masked, and the sums of the ones around it rounded differently on their two ways
+// to the border): the index of the first value of any weight from `from` on, the last one before it if there is none. All threads.
+template <typename T, typename F>
+__device__ __noinline__ int nearest(const Part<T> a, const int from, const F f) {
+    Shared& s = *a.s;
+    __syncthreads();                                         // s.found and s.last have been read
+    if (threadIdx.x == 0) {
+        s.found = INT_MAX;
+        s.last = -1;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.V; i += kThreads) {
+        if (f(ardiff::to_float(a.x[i]), i) > 0.0) {
+            if (i >= from) atomicMin(&s.found, i); else atomicMax(&s.last, i);
+        }
+    }
+    __syncthreads();
     return s.found != INT_MAX ? s.found : s.last;
 }
 
@@ -1115,7 +1136,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     // the first pass sums, too, where all weights count and the temperature is one for which fp32 tells which logits are far below
     const bool greedy = o.T == 0.f;
     const double scale = 1.4426950408889634074 / (double)o.T;
-    const bool sums = valid && o.u > 0.f && o.T >= 1e-3f && o.T <= 1e3f && !o.use_k && (o.use_p ? args.V > kList : !o.use_m);
+    const bool sums = valid && o.u >= kLeastU && o.T >= 1e-3f && o.T <= 1e3f && !o.use_k && (o.use_p ? args.V > kList : !o.use_m);
     if (sums) first_pass<T, true>(a, scale);
     else first_pass<T, false>(a, scale);
     float own = s.top[0][tid];
@@ -1163,7 +1184,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     wt.a = scale;
     wt.lowest = (float)fmax(wt.m - 100.0 / wt.a, -3e38);
     const double octaves = ((double)wt.lowest - wt.m) * wt.a;
-    wt.far = o.u == 0.f || octaves > -75.0 || octaves < -900.0;
+    wt.far = o.u < kLeastU || octaves > -95.0 || octaves < -900.0;
     const float a32 = (float)fmin(wt.a, 3e38);
     const float half = 0.5f * m;                             // (halves: a difference of two logits can pass fp32's range)
     const float floor_ = o.use_m ? 0.5f * (log2f(o.mp) - 0.01f) : -INFINITY;
@@ -1464,7 +1485,8 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
         a.sync();                                            // every CTA has read the others' sums
         if (owner / kSegments != a.rank) return;
     }
-    const int token = locate(a, owner, before, (double)o.u * total, drawn);
+    int token = locate(a, owner, before, (double)o.u * total, drawn);
+    if (token < 0) token = nearest(a, a.first + owner % kSegments * a.segment * N, drawn);
     if (tid == 0) {
         const double y = ((double)ardiff::to_float(a.x[token]) - wt.m) * wt.a;
         answer(args, row, token, (float)(y * 0.69314718055994530942 - log(total)));

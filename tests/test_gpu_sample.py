@@ -300,3 +300,33 @@ def test_no_rows():
     d = require_cuda()
     token, logprob = ardiff.ardiff_sample_tokens(torch.empty((0, 50), device=d), torch.empty((0,), device=d))
     assert token.shape == (0,) and logprob.shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [{}, {"mp": 1e-9}, {"k": 15000}, {"p": 0.999999}])
+@pytest.mark.parametrize("front", [-math.inf, -150.0, -90.0])
+def test_tiny_numbers_pass_over_what_weighs_nothing(dtype, kw, front):
+    """u below the 24 bits of a generator, in front of which lie masked logits, or ones whose weights are near u or far below it."""
+    n, V = 8, 40000
+    x, _ = rows(n, V, DTYPES[dtype], seed=15)
+    x[:, :20000] = front
+    u = [1e-45, 1e-38, 2.0**-126, 1e-30, 2.0**-100, 1e-20, 2.0**-25, 2.0**-24]
+    check(x, u, **{name: [v] * n for name, v in kw.items()})
+    check(x, u, T=[0.01] * n, **{name: [v] * n for name, v in kw.items()})
+
+
+@pytest.mark.parametrize("kw", [{}, {"k": 59999}, {"mp": 1e-9}, {"p": 0.9999999}])
+def test_draws_that_end_where_masked_logits_begin(kw):
+    """The same logits on both sides of masked ones and u = 1/2: the border lies at the masked ones but for rounding, so that the last
+    logit of weight before them and the first behind them are both right, and nothing else is."""
+    n, half, gap = 256, 10000, 20000
+    g = torch.Generator().manual_seed(16)
+    v = torch.randn((n, half), generator=g)
+    x = torch.cat([v, torch.full((n, gap), -math.inf), v, torch.full((n, gap), -math.inf)], 1)
+    if "p" in kw or "mp" in kw:                    # (the borders are kept whatever the filter)
+        x[:, [0, half - 1, half + gap, 2 * half + gap - 1]] = 3.0
+    d = require_cuda()
+    args = {"k": "top_k", "mp": "min_p", "p": "top_p"}
+    kw = {args[name]: torch.tensor([w] * n, dtype=torch.int32 if name == "k" else torch.float32, device=d) for name, w in kw.items()}
+    token, _ = ardiff.ardiff_sample_tokens(x.to(d), torch.full((n,), 0.5, device=d), **kw)
+    assert set(token.tolist()) <= {half - 1, half + gap}
