@@ -402,8 +402,8 @@ int ardiff_pipeline_join(ardiff_pipeline* pipeline, void* stream);
  *                   sum over all kept ones;  logprob = ln(w_token / that sum)
  * Masked logits (-inf) are never drawn. A row of logits with NaN or +inf or of only -inf, a temperature that is negative, NaN
  * or inf, a NaN in top_p or min_p, or u outside 0 <= u < 1, gives token -1 and logprob NaN.
- * Weights and sums are fp64 where they decide between tokens, in an order fixed by V, n and the type: equal calls give
- * equal bits.
+ * Weights and sums are fp64 where they decide between tokens, in an order fixed by V, n, the type and the row's
+ * place between 16-byte boundaries: equal calls give equal bits.
  *
  *   logits   dev  [n][V], rows `ld` >= V values apart, of type dtype (ARDIFF_BF16, ARDIFF_F16 or ARDIFF_F32), at any
  *            multiple of its size; read once from memory
@@ -473,16 +473,16 @@ int ardiff_pages_truncate(int32_t requests, int32_t page, int32_t width, const i
  * Operation, row by row: over the entries j of the teacher that count (0 <= ids[j] < V and a logit above -inf; others,
  * e.g. ids of -1 behind a shorter list, do not) q = softmax(teacher / T); p = softmax(logits / T) over all V;
  *   loss = sum_j q_j (ln q_j - ln p[ids_j]);   grad_i = weight (p_i - sum_{j: ids_j = i} q_j) / T.
- * An id may occur more than once. A row without entries has loss 0, stats 0 and gradient 0, and its logits are not
- * read. A masked logit (-inf) has p = 0; loss = +inf where the teacher has a share there. A row of logits with NaN or
+ * An id may occur more than once. A row without entries has loss 0, stats 0 and gradient 0, whatever its logits
+ * are. A masked logit (-inf) has p = 0; loss = +inf where the teacher has a share there. A row of logits with NaN or
  * +inf, or of only -inf, and a teacher's entry of NaN or +inf, give NaN (a row of logits in loss, stats and gradient,
  * an entry in the loss and at the row's entries).
  *
  *   logits   dev  [n][V], rows `ld` >= V values apart, of type dtype (ARDIFF_BF16, ARDIFF_F16 or ARDIFF_F32), at any
  *            multiple of its size
  *   n        0 <= n < 2^28;  1 <= V <= ARDIFF_DISTILL_MAX_V
- *   teacher  dev  [n][k] of type teacher_dtype (any of the three);  ids dev int32 [n][k];  1 <= k <= ARDIFF_DISTILL_MAX_K
- *   temperature   T > 0 (and 1 / T > 0), the same for both sides; the usual factor T^2 is the caller's, in `weight`
+ *   teacher  dev  [n][k] of type teacher_dtype (any of the three), at a multiple of its size;  ids dev int32 [n][k];  1 <= k <= ARDIFF_DISTILL_MAX_K
+ *   temperature   T > 0 (1 / T > 0 and 1.4427 / T within fp32), the same for both sides; the usual factor T^2 is the caller's, in `weight`
  *   loss     dev float [n] out
  *   stats    dev float [n][2]: out (of the loss): the row's largest logit m and ln sum_i exp((logits_i - m) / T); in
  *            (of the backward pass)

@@ -410,6 +410,7 @@ def _distill_args(logits, teacher, ids):
     k = teacher.shape[1]
     index = logits.get_device()
     assert index >= 0 and teacher.get_device() == index and teacher.is_contiguous() and teacher.shape[0] == n
+    assert ids.shape == teacher.shape, f"ids of {tuple(teacher.shape)} expected, got {tuple(ids.shape)}"
     _check_i32(ids, n * k, index)
     return index, (logits.data_ptr(), t.types.get(logits.dtype, -1), n, V, _rows(logits), teacher.data_ptr(),
                    t.types.get(teacher.dtype, -1), ids.data_ptr(), k)

@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : MODE =
         some |= id >= 0;
     }
     some = __syncthreads_or(some);
-    if (!some) {                                             // nothing to learn from this row: it is not read
+    if (!some) {                                             // nothing to learn from this row: its logits do not matter
         if (MODE != FORWARD)
             for (int i = v0 + tid; i < v1; i += kThreads) grad[i] = ardiff::from_float<T>(0.f);
         if (MODE != BACKWARD && part == 0 && tid == 0) {
@@ -355,7 +355,8 @@ int dispatch(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld
     if (n < 0 || n >= (int64_t)1 << 28 || V < 1 || V > ARDIFF_DISTILL_MAX_V || k < 1 || k > ARDIFF_DISTILL_MAX_K || ld < V)
         return ARDIFF_ERR_SHAPE;
     if (MODE != FORWARD && ld_grad < V) return ARDIFF_ERR_SHAPE;
-    if (!(temperature > 0.f) || !isfinite(1.0f / temperature) || !(1.0f / temperature > 0.f)) return ARDIFF_ERR_SHAPE;
+    const float inv_t = 1.0f / temperature;                   // (and its octaves a unit, which the kernel forms, too)
+    if (!(temperature > 0.f) || !isfinite(inv_t * 1.4426950408889634f) || !(inv_t > 0.f)) return ARDIFF_ERR_SHAPE;
     if (n == 0) {
         ardiff::set_launch_count(0);
         return ARDIFF_OK;
@@ -363,11 +364,13 @@ int dispatch(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld
     if (!logits || !teacher || !ids || !stats) return ARDIFF_ERR_NULL;
     if (MODE != BACKWARD && !loss) return ARDIFF_ERR_NULL;
     if (MODE != FORWARD && (!weight || !grad)) return ARDIFF_ERR_NULL;
-    if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(grad)) % size) return ARDIFF_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(grad)) % size ||
+        reinterpret_cast<uintptr_t>(teacher) % ardiff::value_size(teacher_type))
+        return ARDIFF_ERR_ALIGN;
     Args a;
     memset(&a, 0, sizeof(a));
     a.x = logits; a.teacher = teacher; a.ids = ids; a.weight = weight; a.loss = loss; a.stats = stats; a.grad = grad;
-    a.ld = ld; a.ld_grad = ld_grad; a.teacher_type = teacher_type; a.V = V; a.k = k; a.inv_t = 1.0f / temperature;
+    a.ld = ld; a.ld_grad = ld_grad; a.teacher_type = teacher_type; a.V = V; a.k = k; a.inv_t = inv_t;
     const int64_t pieces = (int64_t)V * size / 16;
     a.parts = 1;
     // A gradient's parts are strangers to each other: of 4096 pieces, so that they end one by one and not in a few waves (4096 x 131072

@@ -247,12 +247,14 @@ def test_a_few_steps_of_training_bring_the_student_to_the_teacher():
     assert bool(((change - eta * slope).abs() <= slack).all())
 
 
-@pytest.mark.parametrize("what", ["type of ids", "stats of another size", "rows that overlap", "columns apart", "type of logits"])
+@pytest.mark.parametrize("what", ["type of ids", "ids by columns", "stats of another size", "rows that overlap", "columns apart", "type of logits"])
 def test_tensors_that_do_not_fit_are_refused(what):
     x, teacher, ids, weight = make(4, 100, 8, torch.float32, seed=1)
     stats = torch.zeros((4, 2), device=x.device)
     if what == "type of ids":
         ids = ids.long()
+    elif what == "ids by columns":
+        ids = ids.t().contiguous()
     elif what == "stats of another size":
         stats = stats[:3]
     elif what == "rows that overlap":

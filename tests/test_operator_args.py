@@ -59,7 +59,7 @@ def distill(part, **kw):
     (dict(n=-1), SHAPE), (dict(n=1 << 28), SHAPE), (dict(V=0), SHAPE), (dict(V=(1 << 24) + 1, ld=1 << 25), SHAPE),
     (dict(ld=99), SHAPE), (dict(k=0), SHAPE), (dict(k=1025), SHAPE), (dict(temperature=0.0), SHAPE),
     (dict(temperature=-1.0), SHAPE), (dict(temperature=math.nan), SHAPE), (dict(temperature=math.inf), SHAPE),
-    (dict(temperature=1e-39), SHAPE), (dict(dtype=3), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED),
+    (dict(temperature=1e-39), SHAPE), (dict(temperature=4e-39), SHAPE), (dict(teacher=P + 2), ALIGN), (dict(dtype=3), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED),
     (dict(teacher_dtype=7), UNSUPPORTED), (dict(logits=P + 1), ALIGN),
     (dict(dtype=ardiff.ARDIFF_F32, logits=P + 2), ALIGN), (dict(logits=None), NULL), (dict(teacher=None), NULL),
     (dict(ids=None), NULL), (dict(stats=None), NULL)])
