@@ -481,8 +481,10 @@ int ardiff_pages_truncate(int32_t requests, int32_t page, int32_t width, const i
  *   logits   dev  [n][V], rows `ld` >= V values apart, of type dtype (ARDIFF_BF16, ARDIFF_F16 or ARDIFF_F32), at any
  *            multiple of its size
  *   n        0 <= n < 2^28;  1 <= V <= ARDIFF_DISTILL_MAX_V
- *   teacher  dev  [n][k] of type teacher_dtype (any of the three), at a multiple of its size;  ids dev int32 [n][k];  1 <= k <= ARDIFF_DISTILL_MAX_K
- *   temperature   T > 0 (1 / T > 0 and 1.4427 / T within fp32), the same for both sides; the usual factor T^2 is the caller's, in `weight`
+ *   teacher  dev  [n][k] of type teacher_dtype (any of the three), at a multiple of its size
+ *   ids      dev int32 [n][k];  1 <= k <= ARDIFF_DISTILL_MAX_K
+ *   temperature   T > 0 (1 / T > 0 and 1.4427 / T within fp32), the same for both sides; the usual factor T^2 is the
+ *            caller's, in `weight`
  *   loss     dev float [n] out
  *   stats    dev float [n][2]: out (of the loss): the row's largest logit m and ln sum_i exp((logits_i - m) / T); in
  *            (of the backward pass)
