@@ -52,6 +52,7 @@ constexpr int kGroups = 4;               // segments a warp; a thread's share of
 constexpr int kSegments = kGroups * kWarps;  // of a CTA's part
 constexpr int kMaxParts = 8;
 constexpr float kLeastU = 0x1p-24f;      // below it, u asks how nothing adds up: every weight counts as what it is
+constexpr float kLeastMin = 0x1p-60f;    // min_p from which every weight that has it is one that sums over many hold exactly
 constexpr float kSane = 6e4f;            // logits up to which, at temperatures from 1e-3 to 1e3, a first pass can sum
 
 struct Args {
@@ -530,7 +531,8 @@ __device__ __noinline__ void collect(const Part<T> a, const Listed listed, unsig
         if (listed(s.top[g][threadIdx.x])) s.group[atomicAdd(&s.groups, 1u)] = (unsigned short)(g * kThreads + threadIdx.x);
     __syncthreads();
     // every thread takes pieces of them in turn, four loads at a time
-    const int turns = (a.segment + 31) / 32, items = (int)s.groups * turns;
+    const int turns = (a.segment + 31) / 32;
+    int items = (int)s.groups * turns;
     const uint4* base = reinterpret_cast<const uint4*>(a.x + a.first);
     const int most = a.whole1 - 1;
 #pragma unroll 1
@@ -558,13 +560,19 @@ __device__ __noinline__ void collect(const Part<T> a, const Listed listed, unsig
 #pragma unroll
                 for (int i = 0; i < N; ++i) hit |= listed(v[i]) && v[i] > -INFINITY ? 1u << i : 0u;
 #pragma unroll 1
-                for (; hit; hit &= hit - 1) {
+                while (hit) {
                     const int i = __ffs(hit) - 1, index = a.first + at[0] * N + i;
+                    hit &= hit - 1;
                     if (lowest) {
                         atomicMin(lowest, index);
                     } else {
                         const unsigned place = atomicAdd(count, 1u);
-                        if (place < (unsigned)kList) list[place] = entry(ardiff::to_float(a.x[index]), index);
+                        if (place < (unsigned)kList) {
+                            list[place] = entry(ardiff::to_float(a.x[index]), index);
+                        } else {                             // there is more than the list holds, and the count says so
+                            items = hit = 0;
+                            at[1] = at[2] = at[3] = a.pieces;
+                        }
                     }
                 }
             }
@@ -820,6 +828,15 @@ struct Kept {                            // the weights of what the cut keeps
     Cut cut;
     __device__ __forceinline__ double operator()(float v, int i) const {
         return masked(wt.bulk(v), cut.keeps(v, i));
+    }
+};
+struct KeptMin {                         // the same of those that have min_p, where min_p is a weight that bulk() gives exactly
+    Weights wt;
+    Cut cut;
+    double mp;
+    __device__ __forceinline__ double operator()(float v, int i) const {
+        const double w = wt.bulk(v);
+        return masked(w, cut.keeps(v, i) && w >= mp);
     }
 };
 template <bool FAR>
@@ -1476,7 +1493,8 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
     }
     // the draw among what the cut keeps
     if (owner < 0) {
-        if (wt.far || o.use_m) total = sum_segments(a, buf, (double)o.u, drawn);
+        if (wt.far || (o.use_m && o.mp < kLeastMin)) total = sum_segments(a, buf, (double)o.u, drawn);
+        else if (o.use_m) total = sum_segments(a, buf, (double)o.u, KeptMin{wt, cut, (double)o.mp});
         else if (o.use_k || o.use_p) total = sum_segments(a, buf, (double)o.u, Kept{wt, cut});
         else if (summed) total = add_segments(a, buf, (double)o.u, true, wt);
         else total = sum_segments(a, buf, (double)o.u, Bulk{wt});

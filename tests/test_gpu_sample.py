@@ -330,3 +330,14 @@ def test_draws_that_end_where_masked_logits_begin(kw):
     kw = {args[name]: torch.tensor([w] * n, dtype=torch.int32 if name == "k" else torch.float32, device=d) for name, w in kw.items()}
     token, _ = ardiff.ardiff_sample_tokens(x.to(d), torch.full((n,), 0.5, device=d), **kw)
     assert set(token.tolist()) <= {half - 1, half + gap}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mp", [0.5, 0.01, 1e-8, 2.0**-60, 2.0**-61, 1e-30])
+@pytest.mark.parametrize("T", [1.0, 0.1])
+def test_min_p_that_keeps_more_than_a_list_holds(dtype, mp, T):
+    n, V = 4, 60000
+    x, u = rows(n, V, DTYPES[dtype], seed=17, kind="flat")
+    x *= 8.0 * T
+    check(x, u, T=[T] * n, mp=[mp] * n)
+    check(x.clamp(max=T), u, T=[T] * n, mp=[mp] * n)
