@@ -24,9 +24,9 @@
 //   what none of these     (thousands of different logits closer together than 2^-14 octaves of the weight): a search by the logits
 //   settles                as whole numbers
 //
-// Measured on B200 (L2 flushed, us; floor: the row read once at the measured copy rate), 512 x 131072 bf16, floor 20.5: T = 0 37, top-k 50
-// with top-p 51, no filter 115 (bound by 67 million fp64 weights of 15 instructions, 60 us at 64 a clock and SM), nuclei of tens of
-// tokens 213, of tens of thousands 590. 1 x 32768 bf16 with top-k and top-p: 14, of which a dozen barriers and dependent loads are all.
+// Measured on B200 (L2 flushed, us; floor: the row read once at the measured copy rate), 512 x 131072 bf16, floor 20.5: T = 0 39, top-k 50
+// with top-p 51, no filter 111 (bound by 67 million fp64 weights of 15 instructions, 60 us at 64 a clock and SM), nuclei of tens of
+// tokens 210, of tens of thousands 490 to 530, min-p that keeps thousands 230. 1 x 32768 bf16 with top-k and top-p: 14, of which a dozen barriers and dependent loads are all.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 #include <limits.h>
@@ -1326,7 +1326,6 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
             const double enough = fmax((double)o.p * whole, 1e-300);                  // at least one
             int first_code = r.first << kFine;
             bool window = r.in > 2 * kThreads;               // first_code .. last_code want a histogram of their own
-            double base = r.mass, upto = -1.0;               // the mass in front of them, or that up to their end
             int verdict = kAbove;
             for (int turn = 0; (verdict == kAbove || verdict == kBelow) && turn < 6; ++turn) {
                 if (window) {
@@ -1335,12 +1334,22 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                     a.sync();                                    // the last histogram has been read
                     clear_bins(s);
                     __syncthreads();
+                    // with it the mass in front of them, in fp32: bins' middles then err by what lies in the window alone (where many logits
+                    // are equal, middles in front of it put many rows' ends beside the right bin, and those go round again: 512 x 131072
+                    // bf16, flat nuclei, 606 -> 488 us)
+                    float sum = 0.f;
                     a.each([&](float v, int i) {
                         const int code = weight_code(m - v, a32);
-                        if (code >= first_code && code <= last_code && cut.keeps(v, i)) count_bin(s, (code - first_code) >> shift);
+                        const bool in = cut.keeps(v, i);
+                        if (in && code >= first_code && code <= last_code) count_bin(s, (code - first_code) >> shift);
+                        const float w = ardiff::ex2((v - m) * a32);
+                        sum += in && code < first_code ? w : 0.f;
                     });
-                    a.sync();
-                    if (!pick(a, false, 0u, enough, false, 0, 0u, base, upto, CodeBins{first_code, 1 << shift}, r)) break;
+                    const double mine = warp_sum(sum);
+                    buf ^= 1;
+                    if (lane < kGroups) s.seg[buf][warp * kGroups + lane] = lane == 0 ? mine : 0.0;
+                    const double base = add_segments(a, buf, 2.0, false, Weights());
+                    if (!pick(a, false, 0u, enough, false, 0, 0u, base, -1.0, CodeBins{first_code, 1 << shift}, r)) break;
                     last_code = min(last_code, first_code + ((r.last + 1) << shift) - 1);
                     first_code += r.first << shift;
                 }
@@ -1455,7 +1464,6 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                 }
                 a.sync();
                 verdict = *a.at(&s.verdict, 0);
-                const double with = *a.at(&s.mass_in, 0);
                 if (verdict == kFound) {
                     owner = *a.at(&s.owner, 0);
                     before = *a.at(&s.before, 0);
@@ -1475,15 +1483,12 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                     // (a cut before this one keeps all of the range or is its end)
                     cut = Cut{value, cut.value == value ? min(index, cut.index) : index};
                 }
-                // the estimate was wrong, but the sums next to the range are exact now: the same with a window beside it
+                // the estimate was wrong: the same with a window beside it
                 window = true;
                 if (verdict == kAbove) {
-                    upto = sure;
                     last_code = first_code - 1;
                     first_code = max(0, last_code - 4095);
                 } else {
-                    upto = -1.0;
-                    base = with;
                     first_code = last_code + 1;
                     last_code = min(first_code + 4095, ((kBins - 1) << kFine) - 1);
                 }
