@@ -37,6 +37,7 @@
 #include "../../include/ardiff.h"
 #include "common.cuh"
 #include "launch.cuh"
+#include "nucleus.h"
 #include "rows.cuh"
 
 namespace cg = cooperative_groups;
@@ -867,14 +868,6 @@ struct Equal {                           // the number of elements of a value
 
 enum Verdict { kFound, kAbove, kBelow, kUnknown, kNotNeeded };
 
-// How many elements of weight w, next to `sure`, it takes to reach `enough`: `in` + 1 if there are not that many.
-__device__ __forceinline__ double needed(double enough, double sure, double w, unsigned in) {
-    double need = fmin(ceil((enough - sure) / w), (double)in + 1.0);
-    while (need > 1.0 && sure + (need - 1.0) * w >= enough) need -= 1.0;
-    while (need <= (double)in && sure + need * w < enough) need += 1.0;
-    return need;
-}
-
 // The first CTA alone: where in the sorted list (n entries, the elements next to `sure` in mass, or the nth in number) the prefix ends.
 // s.verdict: kFound, and s.cut its last element (count = false: also s.found, its place in the list); or it lies above the list, or below.
 __device__ __noinline__ void end_in_list(Shared& s, const Weights wt, const bool count, int n, unsigned nth, double sure, double enough) {
@@ -969,7 +962,7 @@ __device__ __noinline__ Cut search(const Part<T> a, const Weights wt, float a32,
         } else {
             // one value, more often than the list is long: as many of it as are needed, lowest indices first
             const double w = count ? 1.0 : wt.own(top);
-            const double need = count ? (double)(k - r.before) : needed(enough, sure, w, r.in);
+            const double need = count ? (double)(k - r.before) : ardiff::needed(enough, sure, w, r.in);
             const int verdict = count ? kFound : sure >= enough ? kAbove : need > (double)r.in ? kBelow : kFound;
             // (the sum over all is r.in: the share of it is a whole number less a half, up to rounding)
             sum_segments(a, buf, (need - 0.5) / (double)r.in, Equal{cut, top});
@@ -1445,7 +1438,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
                     }
                     value = value_of(lo);
                     const double w = wt.own(value);
-                    need = needed(enough, sure, w, r.in);
+                    need = ardiff::needed(enough, sure, w, r.in);
                     if (lo == hi && a.rank == 0 && tid == 0) {
                         s.verdict = sure >= enough ? kAbove : need > (double)r.in ? kBelow : kFound;
                         s.mass_in = sure + r.in * w;

@@ -341,3 +341,18 @@ def test_min_p_that_keeps_more_than_a_list_holds(dtype, mp, T):
     x *= 8.0 * T
     check(x, u, T=[T] * n, mp=[mp] * n)
     check(x.clamp(max=T), u, T=[T] * n, mp=[mp] * n)
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("u", [0.0, 2.0**-26])
+def test_a_small_share_of_thousands_of_largest_ones_with_thousands_far_below(dtype, u):
+    """The search by whole numbers looks at the far ones first, with many times the mass that is asked for in front of them. Sums are whole
+    numbers, so the cut is exact."""
+    lows = [41, 48, 50, 53, 58, 60, 66, 68, 69, 71, 73, 90]
+    shares = [0.02, 0.05, 0.1, 0.35, 0.4, 0.45]
+    x = torch.empty((len(lows) * len(shares), 6000))
+    for i, low in enumerate(lows):
+        x[i * len(shares):(i + 1) * len(shares)] = 10.0 - low
+    x[:, 1000:4000] = 10.0
+    got = check(x.to(DTYPES[dtype]), [u] * len(x), p=shares * len(lows))
+    assert set(got) == {1000}
