@@ -2,6 +2,7 @@
 #pragma once
 #include <math.h>
 #include <stdint.h>
+#include <string.h>
 
 #ifdef __CUDACC__
 #define ARDIFF_BOTH __host__ __device__ __forceinline__
@@ -10,6 +11,20 @@
 #endif
 
 namespace ardiff {
+
+// Logits in their order as whole numbers, and back: key_of(x) < key_of(y) just where x < y, both zeros are one number, and no number between
+// two logits' is without a logit, so that a range of numbers and the range of the logits at its ends hold the same ones.
+ARDIFF_BOTH unsigned key_of(float x) {
+    uint32_t b;
+    memcpy(&b, &x, 4);
+    return b & 0x80000000u ? 0u - b : b | 0x80000000u;
+}
+ARDIFF_BOTH float value_of(unsigned k) {
+    const uint32_t b = k & 0x80000000u ? k & 0x7fffffffu : 0u - k;
+    float x;
+    memcpy(&x, &b, 4);
+    return x;
+}
 
 // How many elements of weight w, next to `sure`, it takes to reach `enough`: `in` + 1 if there are not that many, 1 if none is needed.
 // The first estimate is held between these before it is stepped, so that every step is one of fp64's own whole numbers: where `sure` is

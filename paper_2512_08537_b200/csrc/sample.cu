@@ -104,14 +104,8 @@ struct Shared {
     };
 };
 
-// logits in their order as whole numbers; both zeros are one
-__device__ __forceinline__ unsigned key_of(float x) {
-    const unsigned b = __float_as_uint(x + 0.0f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float value_of(unsigned k) {
-    return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
-}
+using ardiff::key_of;
+using ardiff::value_of;
 
 __device__ __forceinline__ float max_nan(float a, float b) {       // NaN if either is
     float r;

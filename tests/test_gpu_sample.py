@@ -356,3 +356,36 @@ def test_a_small_share_of_thousands_of_largest_ones_with_thousands_far_below(dty
     x[:, 1000:4000] = 10.0
     got = check(x.to(DTYPES[dtype]), [u] * len(x), p=shares * len(lows))
     assert set(got) == {1000}
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("u", [0.0, 2.0**-30, 2.0**-25])
+def test_nuclei_that_end_below_more_zeros_than_a_list_holds(dtype, u):
+    """Positive logits, thousands of zeros (of both signs), and negative ones, among which the nucleus ends."""
+    x = torch.cat([torch.linspace(-1.1, -1.0, 1000), torch.ones(1), torch.linspace(0.51, 0.511, 3000), torch.zeros(20000)])
+    x = x.repeat(8, 1)
+    x[1::2, 10000:] = -0.0
+    x[4:, :1000] *= 1e-3
+    p = [0.995, 0.99, 0.982, 0.9999, 0.995, 0.99, 0.97, 0.9999]
+    check(x.to(DTYPES[dtype]), [u] * 8, p=p)
+
+
+@pytest.mark.parametrize("u", [0.0, 2.0**-25])
+@pytest.mark.parametrize("kind", ["few values", "around zero", "flat"])
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+def test_tiny_numbers_and_nuclei_on_both_sides_of_zero(kind, dtype, u):
+    x, _ = rows(12, 30000, DTYPES[dtype], seed=18, kind=kind)
+    check(x, [u] * 12, p=[0.05, 0.2, 0.35, 0.5, 0.6, 0.7, 0.8, 0.9, 0.95, 0.98, 0.99, 0.999])
+
+
+def test_a_count_that_ends_among_the_smallest_numbers_below_zero():
+    """fp32's least negative numbers directly below thousands of zeros, and a largest logit from which steps of 2^22 numbers lead to the
+    border between them."""
+    g = torch.Generator().manual_seed(19)
+    tiny = (torch.randperm((1 << 22) - 1, generator=g)[:600] + 1).to(torch.int32).view(torch.float32)
+    top = torch.tensor([0x3fffffff], dtype=torch.int32).view(torch.float32)
+    x = torch.cat([-tiny, torch.zeros(2000), top, torch.rand((1500,), generator=g)])
+    x = x[torch.randperm(len(x), generator=g)].repeat(32, 1)
+    k = [1501 + 2000 + v for v in (1, 2, 100, 300, 333, 500, 599, 600)] * 4
+    check(x, torch.rand((32,), generator=g).tolist(), k=k)
+    check(x, [0.0] * 32, k=k, p=[0.999] * 32)

@@ -4,6 +4,7 @@ import os
 import random
 import subprocess
 
+import numpy as np
 import pytest
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2512_08537_b200", "csrc")
@@ -64,3 +65,40 @@ def test_needed_ends_where_the_mass_in_front_is_far_above(needed):
 def test_needed_of_weights_that_are_nothing(needed):
     assert needed([(0.5, 1.0, 0.0, 7), (0.5, 0.5, 0.0, 7)]) == [1.0, 1.0]
     assert needed([(0.5, 0.25, 0.0, 7), (0.5, 0.25, 5e-324, 7)]) == [8.0, 8.0]
+
+
+# of the numbers of standard input, each as the bits of a float: its key, and the bits of the value of that key and of its two neighbours
+KEYS = """
+#include "nucleus.h"
+#include <stdio.h>
+int main() {
+    unsigned b;
+    while (scanf("%u", &b) == 1) {
+        float x, v[3];
+        memcpy(&x, &b, 4);
+        const unsigned k = ardiff::key_of(x);
+        unsigned o[3];
+        for (int i = 0; i < 3; ++i) v[i] = ardiff::value_of(k - 1u + i);
+        memcpy(o, v, 12);
+        printf("%u %u %u %u\\n", k, o[0], o[1], o[2]);
+    }
+}
+"""
+
+
+def test_keys_are_the_logits_order_without_gaps(tmp_path):
+    exe = program(tmp_path, "keys", KEYS)
+    rng = np.random.default_rng(1)
+    most = np.float32(np.finfo(np.float32).max)
+    bits = [0, 1, 2, 0x7fffff, 0x800000, 0x3f800000, int(most.view(np.uint32))] + rng.integers(0, 0x7f7fffff, 4000).tolist()
+    bits = np.array([b | sign for b in bits for sign in (0, 0x80000000)], np.uint32)
+    x = bits.view(np.float32)
+    out = subprocess.run([exe], input=" ".join(map(str, bits)), capture_output=True, text=True, timeout=20, check=True).stdout
+    out = np.array(out.split(), np.uint64).reshape(-1, 4)
+    key, near = out[:, 0], out[:, 1:].astype(np.uint32).view(np.float32)
+    order = np.argsort(x, kind="stable")
+    assert np.array_equal(np.diff(x[order]) > 0, np.diff(key[order].astype(np.int64)) > 0)
+    assert np.array_equal(near[:, 1], x)                         # (-0 comes back as +0, which is equal)
+    inf = np.float32(np.inf)
+    with np.errstate(over="ignore"):
+        assert np.array_equal(near[:, 0], np.nextafter(x, -inf)) and np.array_equal(near[:, 2], np.nextafter(x, inf))
