@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : MODE =
         n_q = p < p1 ? min(kAhead, (p1 - p + kThreads - 1) / kThreads) : 0;
 #pragma unroll
         for (int j = 0; j < kAhead; ++j)
-            if (j < n_q) q[j] = __ldg(body + p + j * kThreads);
+            if (j < n_q) q[j] = ardiff::load_piece(body + p + j * kThreads);
     };
     if (MODE != BACKWARD) load(p0 + tid);
     if (MODE != FORWARD) {
@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : MODE =
                 const int i = p + j * kThreads;
                 if (i >= p1) continue;
                 if (MODE == STEP && i - p0 < a.cached) r[j] = s_cache[i - p0];       // (each thread's own)
-                else r[j] = __ldcg(body + i);                                        // (may lie where the gradient does)
+                else r[j] = ardiff::load_piece(body + i);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

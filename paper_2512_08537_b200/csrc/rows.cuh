@@ -11,6 +11,11 @@ namespace ardiff {
 
 template <typename T> struct Piece { static constexpr int N = 16 / (int)sizeof(T); };   // values a piece
 
+// A piece of a row. The kernels are launched early: the one that writes the logits may still run when they start, and the gradient may lie
+// where the logits do. So these are ordinary loads, which stay behind begin_kernel(): read-only ones (__ldg, or through __restrict__) want data
+// that does not change while the kernel runs and may be moved in front of it.
+__device__ __forceinline__ uint4 load_piece(const uint4* p) { return *p; }
+
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }

@@ -174,7 +174,7 @@ struct Part {                            // this CTA's part of its row
         const int most = whole1 - 1;
         if (begin >= end) return;
         // (a place outside the whole pieces gives the nearest of them, which is not used)
-        auto load = [&](int p) { return whole0 <= most ? __ldg(base + max(whole0, min(p, most))) : uint4(); };
+        auto load = [&](int p) { return whole0 <= most ? ardiff::load_piece(base + max(whole0, min(p, most))) : uint4(); };
         uint4 q[AHEAD], next[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) q[i] = next[i] = load(begin + i * step);
@@ -542,7 +542,7 @@ __device__ __noinline__ void collect(const Part<T> a, const Listed listed, unsig
                 const int id = s.group[item / turns], t = id & (kThreads - 1), in = (t & 31) + (int)(item % turns) * 32;
                 if (in < a.segment) at[j] = min(a.pieces, ((t >> 5) * kGroups + id / kThreads) * a.segment + in);
             }
-            q[j] = a.whole0 <= most && at[j] < a.pieces ? __ldg(base + max(a.whole0, min(at[j], most))) : uint4();
+            q[j] = a.whole0 <= most && at[j] < a.pieces ? ardiff::load_piece(base + max(a.whole0, min(at[j], most))) : uint4();
         }
         // (one copy of what follows: the pieces move down)
 #pragma unroll 1

@@ -120,3 +120,47 @@ def test_the_draft_learns_from_the_rows_it_draws_from():
     assert bool((total <= grad.double().abs().sum(1) * 2.0 ** -8).all())
     token, _ = ardiff.ardiff_sample_tokens(s.q, s.u, s.T, s.top_k)
     assert np.all(token.cpu().numpy() >= 0)
+
+
+def test_kernels_launched_early_read_what_the_kernel_before_them_wrote():
+    """A step of the distillation writes its gradient in the place of the logits, and lets the next kernel start at once; that one reads them.
+    Small and large rows, on one stream and in a captured graph, against the same calls one at a time."""
+    d = require_cuda()
+    for n, width, k in ((4, 1001, 8), (64, 40000, 32), (700, 9000, 16)):
+        g = torch.Generator(device=d).manual_seed(n)
+        x0 = (4 * torch.randn((n, width), device=d, generator=g)).to(torch.bfloat16)
+        teacher, ids = (x0.float() + 0.5 * torch.randn((n, width), device=d, generator=g)).topk(k, dim=1)
+        ids = ids.to(torch.int32)
+        weight = 50.0 + torch.rand((n,), device=d, generator=g)
+        u = torch.rand((n,), device=d, generator=g)
+        top_p = torch.full((n,), 0.95, device=d)
+        x, out = x0.clone(), {}
+
+        def calls(wait):
+            wait()
+            out["loss"], _, _ = ardiff.ardiff_distill_topk_step(x, teacher, ids, weight, grad=x)
+            wait()
+            out["token"], out["logprob"] = ardiff.ardiff_sample_tokens(x, u, top_p=top_p)
+            wait()
+            out["loss 2"], out["stats"], _ = ardiff.ardiff_distill_topk_step(x, teacher, ids, weight, 0.5, grad=x)
+            wait()
+            out["loss 3"], _ = ardiff.ardiff_distill_topk(x, teacher, ids, 2.0)
+            wait()
+            out["back"] = ardiff.ardiff_distill_topk_backward(x, teacher, ids, out["stats"], weight, grad=x).clone()
+
+        calls(torch.cuda.synchronize)
+        want = {name: v.clone() for name, v in out.items()}
+        for _ in range(5):
+            x.copy_(x0)
+            calls(lambda: None)
+            for name, v in want.items():
+                assert torch.equal(out[name], v), (n, name)
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            calls(lambda: None)
+        for _ in range(5):
+            x.copy_(x0)
+            graph.replay()
+            for name, v in want.items():
+                assert torch.equal(out[name], v), (n, name)
