@@ -3,6 +3,12 @@
 Argument marshalling only: every step of the hot path runs in the CUDA kernels of the shared
 library. torch is used for device memory and streams. There is no CPU fallback: if the library
 cannot be loaded, or a call fails, an exception is raised.
+
+Calls are enqueued on the current stream of their tensors' device, or on `stream`. What a call reads has to
+be ready on that stream, and what reads its results elsewhere has to wait for it: the caller orders the
+streams. Results that a call with `stream` allocates come from that stream's memory, and tensors may be
+dropped while it still runs. (Calls that write to tensors passed in alone, the head's and the gate's without
+allocation, leave that to the caller.)
 """
 from __future__ import annotations
 
@@ -140,6 +146,13 @@ def _check(rc: int, where: str):
         raise ArdiffError(rc, where)
 
 
+def _current_stream(index: int) -> int:
+    """The handle of a device's current stream."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+
+
 def _stream_ptr(stream) -> int:
     """The stream's handle; without one that of the current stream (asked for as a number where torch has that: a Stream object
     takes 2 us)."""
@@ -158,6 +171,27 @@ def _on(device):
     return _STAY if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
 
+def _beside(fn, stream, *args):
+    """fn(*args) on `stream`, for calls that allocate results. These come from that stream's memory, which nothing older on another
+    stream can still be using; and every tensor is marked as used by the stream that is not its own, so that its memory is not
+    given out again while a kernel reads or writes it."""
+    import torch
+    index = stream.device_index
+    assert args[0].get_device() == index, f"a stream of cuda:{index} for tensors on {args[0].device}"
+    if _current_stream(index) == stream.cuda_stream:
+        return fn(*args)
+    here = torch.cuda.current_stream(index)
+    for t in args:
+        if hasattr(t, "record_stream") and t.get_device() == index:
+            t.record_stream(stream)
+    with torch.cuda.stream(stream):
+        out = fn(*args)
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None:
+            t.record_stream(here)
+    return out
+
+
 def ardiff_entropy_gate(feat, tau: float, mask=None, idx=None, count=None, entropy=None,
                         want_entropy: bool = False, stream=None):
     """Entropy gate + compaction on `feat` (torch bf16 CUDA tensor [n, d]).
@@ -166,6 +200,8 @@ def ardiff_entropy_gate(feat, tau: float, mask=None, idx=None, count=None, entro
     allocated here unless passed in. Nothing is synchronised.
     """
     import torch
+    if stream is not None:
+        return _beside(ardiff_entropy_gate, stream, feat, tau, mask, idx, count, entropy, want_entropy)
     assert feat.is_cuda and feat.dtype == torch.bfloat16 and feat.dim() == 2 and feat.is_contiguous()
     n, d = feat.shape
     dev = feat.device
@@ -180,7 +216,7 @@ def ardiff_entropy_gate(feat, tau: float, mask=None, idx=None, count=None, entro
     with _on(dev):
         rc = lib().ardiff_entropy_gate_ex(
             feat.data_ptr(), n, d, float(tau), mask.data_ptr(), idx.data_ptr(), count.data_ptr(),
-            entropy.data_ptr() if entropy is not None else None, _stream_ptr(stream))
+            entropy.data_ptr() if entropy is not None else None, _stream_ptr(None))
     _check(rc, "ardiff_entropy_gate")
     return mask, idx, count, entropy
 
@@ -189,6 +225,8 @@ def ardiff_entropy_gate_stats(feat, tau: float = -1.0, want_entropy: bool = Fals
     """Gate + threshold statistics of its own entropies in one pass. Returns (mask, idx, count, entropy or
     None, out3 float64 CUDA tensor [3] = mean, std, 0.3 mean - 0.1 std)."""
     import torch
+    if stream is not None:
+        return _beside(ardiff_entropy_gate_stats, stream, feat, tau, want_entropy)
     assert feat.is_cuda and feat.dtype == torch.bfloat16 and feat.dim() == 2 and feat.is_contiguous()
     n, d = feat.shape
     dev = feat.device
@@ -200,7 +238,7 @@ def ardiff_entropy_gate_stats(feat, tau: float = -1.0, want_entropy: bool = Fals
     fn = lib().ardiff_entropy_gate_stats
     with _on(dev):
         rc = fn(feat.data_ptr(), n, d, float(tau), mask.data_ptr(), idx.data_ptr(), count.data_ptr(),
-                entropy.data_ptr() if entropy is not None else None, out3.data_ptr(), _stream_ptr(stream))
+                entropy.data_ptr() if entropy is not None else None, out3.data_ptr(), _stream_ptr(None))
     _check(rc, "ardiff_entropy_gate_stats")
     return mask, idx, count, entropy, out3
 
@@ -211,6 +249,8 @@ def ardiff_entropy_gate_blocks(feat, rows_per_token: int, gamma: int, tau: float
     `rows_per_token` rows of feat). Returns (mask u8 [n], idx i32 [n], count i32 [1], block_len i32
     [ceil(n/gamma)], row_entropy f32 [n*rows_per_token], token_entropy f32 [n] or None)."""
     import torch
+    if stream is not None:
+        return _beside(ardiff_entropy_gate_blocks, stream, feat, rows_per_token, gamma, tau, want_token_entropy, want_row_entropy)
     assert feat.is_cuda and feat.dtype == torch.bfloat16 and feat.dim() == 2 and feat.is_contiguous()
     rows, d = feat.shape
     assert rows % rows_per_token == 0
@@ -227,7 +267,7 @@ def ardiff_entropy_gate_blocks(feat, rows_per_token: int, gamma: int, tau: float
         rc = fn(feat.data_ptr(), n, rows_per_token, d, gamma, float(tau),
                 row_ent.data_ptr() if row_ent is not None else None,
                 tok_ent.data_ptr() if tok_ent is not None else None, mask.data_ptr(), idx.data_ptr(),
-                count.data_ptr(), block_len.data_ptr(), _stream_ptr(stream))
+                count.data_ptr(), block_len.data_ptr(), _stream_ptr(None))
     _check(rc, "ardiff_entropy_gate_blocks")
     return mask, idx, count, block_len, row_ent, tok_ent
 
@@ -235,11 +275,13 @@ def ardiff_entropy_gate_blocks(feat, rows_per_token: int, gamma: int, tau: float
 def ardiff_tau_calibrate(entropy, stream=None):
     """(mean, std, tau = 0.3 mean - 0.1 std) of a float32 CUDA tensor of entropies, as a float64 CUDA tensor [3]."""
     import torch
+    if stream is not None:
+        return _beside(ardiff_tau_calibrate, stream, entropy)
     assert entropy.is_cuda and entropy.dtype == torch.float32 and entropy.is_contiguous()
     out = torch.empty((3,), dtype=torch.float64, device=entropy.device)
     fn = lib().ardiff_tau_calibrate
     with _on(entropy.device):
-        rc = fn(entropy.data_ptr(), entropy.numel(), out.data_ptr(), _stream_ptr(stream))
+        rc = fn(entropy.data_ptr(), entropy.numel(), out.data_ptr(), _stream_ptr(None))
     _check(rc, "ardiff_tau_calibrate")
     return out
 
@@ -248,6 +290,8 @@ def ardiff_accept_prefix(r, ratio, gamma: int, block_len=None, stream=None):
     """Accepted draft length per block of `gamma`: first position with r > ratio, else the length of the
     draft (block_len[b] tokens where the early stop truncated block b; the whole block if block_len is None)."""
     import torch
+    if stream is not None:
+        return _beside(ardiff_accept_prefix, stream, r, ratio, gamma, block_len)
     assert r.is_cuda and r.dtype == torch.float32 and ratio.dtype == torch.float32 and r.shape == ratio.shape
     n = r.numel()
     nb = (n + gamma - 1) // gamma
@@ -257,7 +301,7 @@ def ardiff_accept_prefix(r, ratio, gamma: int, block_len=None, stream=None):
     fn = lib().ardiff_accept_prefix
     with _on(r.device):
         rc = fn(r.data_ptr(), ratio.data_ptr(), n, gamma, block_len.data_ptr() if block_len is not None else None,
-                out.data_ptr(), _stream_ptr(stream))
+                out.data_ptr(), _stream_ptr(None))
     _check(rc, "ardiff_accept_prefix")
     return out[:(n + gamma - 1) // gamma]
 
@@ -284,14 +328,14 @@ def _t() -> _Torch:
     return _torch
 
 
-def _run(fn, where: str, index: int, stream, *args):
-    """fn(*args, stream) with the device of the tensors current; raises on an error."""
+def _run(fn, where: str, index: int, *args):
+    """fn(*args, current stream) with the device of the tensors current; raises on an error."""
     t = _torch
     if t.current() == index:
-        rc = fn(*args, t.stream(index) if stream is None else stream.cuda_stream)
+        rc = fn(*args, t.stream(index))
     else:
         with t.device(index):
-            rc = fn(*args, t.stream(index) if stream is None else stream.cuda_stream)
+            rc = fn(*args, t.stream(index))
     if rc:
         raise ArdiffError(rc, where)
 
@@ -325,6 +369,8 @@ def ardiff_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, mi
     """The next token of every row of logits [n, V] (bf16, f16 or f32 CUDA tensor, rows contiguous) by the uniform numbers u
     (f32 [n], 0 <= u < 1). temperature, top_p, min_p (f32 [n]) and top_k (int32 [n]) are every row's own, or None (off).
     Returns (token int32 [n], logprob f32 [n]); -1 and NaN for rows that have no softmax or bad settings."""
+    if stream is not None:
+        return _beside(ardiff_sample_tokens, stream, logits, u, temperature, top_k, top_p, min_p, token, logprob)
     t = _t()
     n, V = logits.shape
     index = logits.get_device()
@@ -342,7 +388,7 @@ def ardiff_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, mi
         logprob = t.empty((n,), dtype=t.f32, device=logits.device)
     else:
         _check_f32(logprob, n, index)
-    _run(lib().ardiff_sample_tokens, "ardiff_sample_tokens", index, stream, logits.data_ptr(), t.types.get(logits.dtype, -1), n, V,
+    _run(lib().ardiff_sample_tokens, "ardiff_sample_tokens", index, logits.data_ptr(), t.types.get(logits.dtype, -1), n, V,
          _rows(logits), u.data_ptr(), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), token.data_ptr(), logprob.data_ptr())
     return token, logprob
 
@@ -372,6 +418,9 @@ def ardiff_pages_extend(length, add, table, free_pages, free_count, page: int, s
     place, slot / position / request of every new token (as many as fit in slot; position and request are written if
     passed). int32 CUDA tensors, slot int64. new_length may be `length` and new_free_count `free_count`; what is not passed is
     allocated. Returns (offset [R + 1], new_length [R], new_free_count [1], status [1]); status is not looked at here."""
+    if stream is not None:
+        return _beside(ardiff_pages_extend, stream, length, add, table, free_pages, free_count, page, slot, position, request, offset,
+                       new_length, new_free_count, status)
     t = _t()
     R, width, index = _pages_args(length, add, table, free_pages, free_count)
     tokens = slot.numel()
@@ -384,7 +433,7 @@ def ardiff_pages_extend(length, add, table, free_pages, free_count, page: int, s
     new_length = _made_i32(new_length, R, length)
     new_free_count = _made_i32(new_free_count, 1, length)
     status = _made_i32(status, 1, length)
-    _run(lib().ardiff_pages_extend, "ardiff_pages_extend", index, stream, R, page, width, length.data_ptr(), add.data_ptr(),
+    _run(lib().ardiff_pages_extend, "ardiff_pages_extend", index, R, page, width, length.data_ptr(), add.data_ptr(),
          table.data_ptr(), free_pages.data_ptr(), free_pages.numel(), free_count.data_ptr(), tokens, slot.data_ptr(), _ptr(position),
          _ptr(request), offset.data_ptr(), new_length.data_ptr(), new_free_count.data_ptr(), status.data_ptr())
     return offset, new_length, new_free_count, status
@@ -394,11 +443,13 @@ def ardiff_pages_truncate(length, target, table, free_pages, free_count, page: i
                           stream=None):
     """Leaves request r of a paged cache its first target[r] tokens; the pages that none of them needs go back to the free list
     (in place). int32 CUDA tensors; new_free_count may be `free_count`. Returns (new_free_count [1], status [1])."""
+    if stream is not None:
+        return _beside(ardiff_pages_truncate, stream, length, target, table, free_pages, free_count, page, new_free_count, status)
     _t()
     R, width, index = _pages_args(length, target, table, free_pages, free_count)
     new_free_count = _made_i32(new_free_count, 1, length)
     status = _made_i32(status, 1, length)
-    _run(lib().ardiff_pages_truncate, "ardiff_pages_truncate", index, stream, R, page, width, length.data_ptr(), target.data_ptr(),
+    _run(lib().ardiff_pages_truncate, "ardiff_pages_truncate", index, R, page, width, length.data_ptr(), target.data_ptr(),
          table.data_ptr(), free_pages.data_ptr(), free_pages.numel(), free_count.data_ptr(), new_free_count.data_ptr(),
          status.data_ptr())
     return new_free_count, status
@@ -434,22 +485,26 @@ def ardiff_distill_topk(logits, teacher, ids, temperature: float = 1.0, loss=Non
     """Divergence of every row of a student's logits [n, V] (bf16, f16 or f32, rows contiguous) from the softmax of the teacher's
     entries (teacher [n, k] at ids [n, k] int32; ids outside 0 .. V - 1 are no entries).
     Returns (loss f32 [n], stats f32 [n, 2]: what ardiff_distill_topk_backward needs of the rows)."""
+    if stream is not None:
+        return _beside(ardiff_distill_topk, stream, logits, teacher, ids, temperature, loss, stats)
     index, args = _distill_args(logits, teacher, ids)
     n = logits.shape[0]
     loss, stats = _made_f32(loss, (n,), n, logits), _made_f32(stats, (n, 2), 2 * n, logits)
-    _run(lib().ardiff_distill_topk, "ardiff_distill_topk", index, stream, *args, temperature, loss.data_ptr(), stats.data_ptr())
+    _run(lib().ardiff_distill_topk, "ardiff_distill_topk", index, *args, temperature, loss.data_ptr(), stats.data_ptr())
     return loss, stats
 
 
 def ardiff_distill_topk_backward(logits, teacher, ids, stats, weight, temperature: float = 1.0, grad=None, stream=None):
     """Gradient of sum(weight * loss) with respect to the logits, from the stats that ardiff_distill_topk gave for the same
     inputs; in the logits' type. `grad` may be `logits`."""
+    if stream is not None:
+        return _beside(ardiff_distill_topk_backward, stream, logits, teacher, ids, stats, weight, temperature, grad)
     index, args = _distill_args(logits, teacher, ids)
     n = logits.shape[0]
     _check_f32(stats, 2 * n, index)
     _check_f32(weight, n, index)
     grad = _made_grad(grad, logits)
-    _run(lib().ardiff_distill_topk_backward, "ardiff_distill_topk_backward", index, stream, *args, temperature, stats.data_ptr(),
+    _run(lib().ardiff_distill_topk_backward, "ardiff_distill_topk_backward", index, *args, temperature, stats.data_ptr(),
          weight.data_ptr(), grad.data_ptr(), _rows(grad))
     return grad
 
@@ -457,12 +512,14 @@ def ardiff_distill_topk_backward(logits, teacher, ids, stats, weight, temperatur
 def ardiff_distill_topk_step(logits, teacher, ids, weight, temperature: float = 1.0, loss=None, stats=None, grad=None,
                              stream=None):
     """Loss, stats and the gradient of sum(weight * loss) in one pass. `grad` may be `logits`. Returns (loss, stats, grad)."""
+    if stream is not None:
+        return _beside(ardiff_distill_topk_step, stream, logits, teacher, ids, weight, temperature, loss, stats, grad)
     index, args = _distill_args(logits, teacher, ids)
     n = logits.shape[0]
     _check_f32(weight, n, index)
     grad = _made_grad(grad, logits)
     loss, stats = _made_f32(loss, (n,), n, logits), _made_f32(stats, (n, 2), 2 * n, logits)
-    _run(lib().ardiff_distill_topk_step, "ardiff_distill_topk_step", index, stream, *args, temperature, weight.data_ptr(),
+    _run(lib().ardiff_distill_topk_step, "ardiff_distill_topk_step", index, *args, temperature, weight.data_ptr(),
          loss.data_ptr(), stats.data_ptr(), grad.data_ptr(), _rows(grad))
     return loss, stats, grad
 
