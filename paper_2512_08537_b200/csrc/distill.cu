@@ -58,11 +58,14 @@ __device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, float c) {
     return MaxSum{m, a.z * ardiff::ex2((a.m - at) * c) + b.z * ardiff::ex2((b.m - at) * c)};
 }
 
-// A thread's running largest value, and two sums of every other value's exponential above it.
+// A thread's running largest value m and sum of exponentials above `ref`, which follows m a few octaves late. The sum is a compensated one
+// (`lost`: what its last addition rounded off) of the pieces' sums: plain additions one after the other round the same way where
+// many logits are equal, and 8192 of them are off by 4e-5 to 8e-5. And it is scaled only where a value is kLate octaves above `ref`:
+// a row that rises slowly would else be scaled, and rounded, at every step.
 struct Running {
-    float m;
-    ardiff::Two z;
+    float m, ref, z, lost;
 };
+constexpr float kLate = 4.f;
 template <typename T, int kAhead>
 __device__ __forceinline__ void take(Running& s, const uint4 (&q)[kAhead], int n, float c) {
     constexpr int N = ardiff::Piece<T>::N;
@@ -70,13 +73,16 @@ __device__ __forceinline__ void take(Running& s, const uint4 (&q)[kAhead], int n
 #pragma unroll
     for (int j = 1; j < kAhead; ++j)
         if (j < n) top = fmaxf(top, ardiff::piece_max(q[j], T()));
-    if (top > s.m) {
-        const float down = ardiff::ex2((s.m - top) * c);     // from -inf: 0
-        s.z = s.z * ardiff::two(down, down);
-        s.m = top;
+    s.m = fmaxf(s.m, top);
+    if ((top - s.ref) * c > kLate) {
+        const float down = ardiff::ex2((s.ref - top) * c);   // from -inf: 0
+        s.z *= down;
+        s.lost *= down;
+        s.ref = top;
     }
-    const float at = s.m == -INFINITY ? 0.f : s.m;
+    const float at = s.ref == -INFINITY ? 0.f : s.ref;
     const ardiff::Two minus = ardiff::two(-at, -at), c2 = ardiff::two(c, c);
+    ardiff::Two sum = ardiff::two(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
         if (j < n) {
@@ -85,10 +91,14 @@ __device__ __forceinline__ void take(Running& s, const uint4 (&q)[kAhead], int n
 #pragma unroll
             for (int i = 0; i < N; i += 2) {
                 const float2 y = ardiff::apart((ardiff::two(v[i], v[i + 1]) + minus) * c2);
-                s.z = s.z + ardiff::two(ardiff::ex2(y.x), ardiff::ex2(y.y));
+                sum = sum + ardiff::two(ardiff::ex2(y.x), ardiff::ex2(y.y));
             }
         }
     }
+    const float2 sums = ardiff::apart(sum);
+    const float more = sums.x + sums.y - s.lost, z = s.z + more;
+    s.lost = z - s.z - more;
+    s.z = z;
 }
 
 template <typename T, int MODE>
@@ -188,7 +198,7 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : MODE =
     };
     float m, ln_z, scale;
     if (MODE != BACKWARD) {
-        Running run{-INFINITY, ardiff::two(0.f, 0.f)};
+        Running run{-INFINITY, -INFINITY, 0.f, 0.f};
 #pragma unroll 1
         for (int p = p0 + tid; n_q > 0; p += kAhead * kThreads) {
             if (MODE == STEP) {
@@ -199,8 +209,7 @@ __global__ void __launch_bounds__(kThreadsOf<MODE>, MODE == FORWARD ? 4 : MODE =
             take<T, kAhead>(run, q, n_q, c);
             load(p + kAhead * kThreads);
         }
-        const float2 sums = ardiff::apart(run.z);
-        MaxSum s{run.m, sums.x + sums.y};
+        MaxSum s = merge(MaxSum{run.m, 0.f}, MaxSum{run.ref, run.z}, c);
         const int edge = part == 0 && tid < x.lead ? tid : part == a.parts - 1 && x.tail() + tid < a.V ? x.tail() + tid : -1;
         const int both = part == 0 && tid < x.lead && part == a.parts - 1 && x.tail() + tid < a.V ? x.tail() + tid : -1;
         if (edge >= 0) {

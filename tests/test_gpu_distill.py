@@ -265,3 +265,34 @@ def test_tensors_that_do_not_fit_are_refused(what):
         x = x.double()
     with pytest.raises((AssertionError, ardiff.ArdiffError)):
         ardiff.ardiff_distill_topk_backward(x, teacher, ids, stats, weight)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["equal", "rising", "falling"])
+def test_long_rows_do_not_add_up_roundings(kind, dtype):
+    """As many rows as give each row one CTA. ln Z may be off by 32 additions of a few pieces' values and the compensated sum of those (2),
+    by exponents up to 4 octaves above 0 (4 + 3 4 ln 2 <= 13 roundings each, at most 12 times where the sum is scaled: later ones weigh 2^-48), by 16
+    merges of 13 and by the number's own rounding: all of which does not depend on V."""
+    n, V, k = 300, 1 << 22, 4
+    d = require_cuda()
+    i = torch.arange(V, device=d, dtype=torch.float64)
+    for slope in ([-0.5, -0.75, -1.0, -2.5, -3.0] if kind == "equal" else [1e-6, 3e-5]):
+        row = torch.full((V,), slope, dtype=torch.float64, device=d) if kind == "equal" else slope * (i if kind == "rising" else -i)
+        if kind == "equal":
+            row[:16384] = 0.0                                    # every thread's first pieces
+        row = row.to(DTYPES[dtype])
+        x = row.repeat(n, 1)
+        y = row.double() - row.double().max()
+        ln_z = float(torch.log(y.exp().sum()))
+        mean = float((y.abs() * y.exp()).sum() / y.exp().sum())
+        teacher = torch.zeros((n, k), device=d)
+        ids = torch.arange(k, device=d, dtype=torch.int32).repeat(n, 1) * 1000
+        weight = torch.ones(n, device=d)
+        tol = (4 + 3 * (mean + 4) + 34 + 12 * 13 + 16 * 13 + 3 + 3 * abs(ln_z)) * U
+        stats = ardiff.ardiff_distill_topk(x, teacher, ids)[1]
+        step = ardiff.ardiff_distill_topk_step(x, teacher, ids, weight, grad=x)[1]
+        for s in (stats, step):
+            assert bool((s[:, 0].double() == float(row.double().max())).all())
+            off = float((s[:, 1].double() - ln_z).abs().max())
+            assert off <= tol, (slope, off, tol)
+        del x
