@@ -46,26 +46,28 @@ def results(out):
 
 @pytest.mark.parametrize("name", sorted(CALLS))
 def test_no_memory_is_given_out_while_a_call_on_another_stream_uses_it(name):
-    """The other stream is kept busy for some tens of milliseconds in front of the call; meanwhile inputs and results are dropped and as
+    """The other stream is kept busy for a tenth of a second in front of the call; meanwhile inputs and results are dropped and as
     much is allocated and written on the current stream."""
     call, takes = CALLS[name]
     want, whole = results(call(None, *[make()[k] for k in takes.split()]))
     kept = [torch.empty_like(v, device="cpu").pin_memory() for v in want]
     side = torch.cuda.Stream()
-    t = (lambda m: [m[k] for k in takes.split()])(make())
-    torch.cuda.synchronize()
-    with torch.cuda.stream(side):
-        torch.cuda._sleep(50_000_000)
-    out, _ = results(call(side, *t))
-    with torch.cuda.stream(side):
-        for k, v in zip(kept, out):
-            k.copy_(v, non_blocking=True)
-    used = t + out
-    places, sizes = {v.data_ptr() for v in used}, [v.numel() * v.element_size() for v in used]
-    del t, out, used, v
-    others = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(2)]
-    assert not side.query()                                      # nothing of it has run yet
+    for cycles in (1000, 200_000_000):                           # the first time loads kernels and gets memory, which may wait for all streams
+        t = (lambda m: [m[k] for k in takes.split()])(make())
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(cycles)
+        out, _ = results(call(side, *t))
+        with torch.cuda.stream(side):
+            for k, v in zip(kept, out):
+                k.copy_(v, non_blocking=True)
+        used = t + out
+        places, sizes = {v.data_ptr() for v in used}, [v.numel() * v.element_size() for v in used]
+        del t, out, used, v
+        others = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(2)]
+        running = not side.query()
+        torch.cuda.synchronize()
+    assert running                                               # nothing of it had run yet
     assert not places & {o.data_ptr() for o in others}
-    torch.cuda.synchronize()
     for i in whole:
         assert torch.equal(kept[i], want[i].cpu()), i
