@@ -344,9 +344,15 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# The C calls take these sizes as int32, and ctypes would cut off what does not fit.
+_SIZES = 2**31
+_TOO_LARGE = "sizes that do not fit 32 bits"
+
+
 def _rows(x) -> int:
     """Distance of the rows of a matrix whose rows are contiguous (one row, or one column, may have any)."""
     n, V = x.shape
+    assert V < _SIZES, _TOO_LARGE
     if x.is_contiguous():
         return V
     assert V <= 1 or x.stride(1) == 1, "rows must be contiguous"
@@ -393,8 +399,9 @@ def ardiff_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, mi
     return token, logprob
 
 
-def _pages_args(length, other, table, free_pages, free_count):
+def _pages_args(length, other, table, free_pages, free_count, page):
     R, width = table.shape
+    assert R < _SIZES and width < _SIZES and -_SIZES <= page < _SIZES, _TOO_LARGE
     index = length.get_device()
     assert index >= 0
     _check_i32(length, R, index)
@@ -422,7 +429,7 @@ def ardiff_pages_extend(length, add, table, free_pages, free_count, page: int, s
         return _beside(ardiff_pages_extend, stream, length, add, table, free_pages, free_count, page, slot, position, request, offset,
                        new_length, new_free_count, status)
     t = _t()
-    R, width, index = _pages_args(length, add, table, free_pages, free_count)
+    R, width, index = _pages_args(length, add, table, free_pages, free_count, page)
     tokens = slot.numel()
     assert slot.dtype is t.i64 and slot.get_device() == index and slot.is_contiguous()
     if position is not None:
@@ -446,7 +453,7 @@ def ardiff_pages_truncate(length, target, table, free_pages, free_count, page: i
     if stream is not None:
         return _beside(ardiff_pages_truncate, stream, length, target, table, free_pages, free_count, page, new_free_count, status)
     _t()
-    R, width, index = _pages_args(length, target, table, free_pages, free_count)
+    R, width, index = _pages_args(length, target, table, free_pages, free_count, page)
     new_free_count = _made_i32(new_free_count, 1, length)
     status = _made_i32(status, 1, length)
     _run(lib().ardiff_pages_truncate, "ardiff_pages_truncate", index, R, page, width, length.data_ptr(), target.data_ptr(),
@@ -459,6 +466,7 @@ def _distill_args(logits, teacher, ids):
     t = _t()
     n, V = logits.shape
     k = teacher.shape[1]
+    assert k < _SIZES, _TOO_LARGE
     index = logits.get_device()
     assert index >= 0 and teacher.get_device() == index and teacher.is_contiguous() and teacher.shape[0] == n
     assert ids.shape == teacher.shape, f"ids of {tuple(teacher.shape)} expected, got {tuple(ids.shape)}"

@@ -111,3 +111,28 @@ def test_tensors_of_the_host_are_refused():
         ardiff.ardiff_pages_extend(i, i, table, i, i[:1], 16, torch.zeros(4, dtype=torch.int64))
     with pytest.raises(AssertionError):
         ardiff.ardiff_pages_truncate(i, i, table, i, i[:1], 16)
+
+
+@pytest.mark.parametrize("page", [2**32 + 16, 2**31, -2**32 + 16])
+def test_page_sizes_that_32_bits_cut_off_are_refused(page):
+    i = torch.zeros(4, dtype=torch.int32)
+    table = torch.zeros((4, 2), dtype=torch.int32)
+    with pytest.raises(AssertionError, match="32 bits"):
+        ardiff.ardiff_pages_extend(i, i, table, i, i[:1], page, torch.zeros(4, dtype=torch.int64))
+    with pytest.raises(AssertionError, match="32 bits"):
+        ardiff.ardiff_pages_truncate(i, i, table, i, i[:1], page)
+
+
+def test_shapes_that_32_bits_cut_off_are_refused():
+    """(Tensors without memory: a row of 2^32 + 5 logits has 8 GB.)"""
+    made = lambda *shape, t=torch.int32: torch.empty(shape, dtype=t, device="meta")  # noqa: E731
+    for V in (2**31, 2**32 + 5):
+        with pytest.raises(AssertionError, match="32 bits"):
+            ardiff._rows(made(1, V, t=torch.bfloat16))
+        with pytest.raises(AssertionError, match="32 bits"):
+            ardiff.ardiff_distill_topk(made(1, 8, t=torch.bfloat16), made(1, V, t=torch.float32), made(1, V))
+    one = made(1)
+    with pytest.raises(AssertionError, match="32 bits"):
+        ardiff.ardiff_pages_truncate(one, one, made(1, 2**32 + 4), one, one, 16)
+    with pytest.raises(AssertionError, match="32 bits"):
+        ardiff.ardiff_pages_truncate(one, one, made(2**32 + 1, 1), one, one, 16)
