@@ -402,11 +402,12 @@ int ardiff_pipeline_join(ardiff_pipeline* pipeline, void* stream);
  *                   sum over all kept ones;  logprob = ln(w_token / that sum)
  * Masked logits (-inf) are never drawn. A row of logits with NaN or +inf or of only -inf, a temperature that is negative, NaN
  * or inf, a NaN in top_p or min_p, or u outside 0 <= u < 1, gives token -1 and logprob NaN.
- * Weights and sums are fp64 where they decide between tokens, in an order fixed by V, n, the type and the row's
- * place between 16-byte boundaries: equal calls give equal bits.
+ * Weights and sums are fp64 where they decide between tokens, in an order fixed by V, n, the type, the row's place between
+ * 16-byte boundaries, the row's own settings, and whether top_k is passed at all (an array of zeros is another call than
+ * NULL: the same tokens but where a border lies within 1e-13 of the sum): equal calls give equal bits.
  *
  *   logits   dev  [n][V], rows `ld` >= V values apart, of type dtype (ARDIFF_BF16, ARDIFF_F16 or ARDIFF_F32), at any
- *            multiple of its size; read once from memory
+ *            multiple of its size; read once, or up to four times where nuclei hold more than a thousand
  *   n        0 <= n < 2^28;  1 <= V <= ARDIFF_SAMPLE_MAX_V
  *   u        dev float [n]: uniform numbers
  *   temperature, top_p, min_p  dev float [n], top_k dev int32 [n], each or NULL: every row's own settings (NULL: 1, 1, 0, 0)
@@ -467,8 +468,8 @@ int ardiff_pages_truncate(int32_t requests, int32_t page, int32_t width, const i
                           int32_t* new_free_count, int32_t* status, void* stream);
 
 /* ---------------------------------------------------------------------------------------
- * Distillation of a draft model from its target's largest logits. (The drafts of speculative decoding are accepted
- * as often as the two agree; the paper trains its draft on its target's outputs.)
+ * Distillation of a draft model from its target's largest logits. (For drafts with a vocabulary, which speculative decoding
+ * accepts as often as the two agree. The paper's own draft is trained by other losses, without one over classes.)
  *
  * Operation, row by row: over the entries j of the teacher that count (0 <= ids[j] < V and a logit above -inf; others,
  * e.g. ids of -1 behind a shorter list, do not) q = softmax(teacher / T); p = softmax(logits / T) over all V;
@@ -491,8 +492,11 @@ int ardiff_pages_truncate(int32_t requests, int32_t page, int32_t width, const i
  *   weight   dev float [n]: the gradient of what is minimised with respect to loss[row]
  *   grad     dev  [n][V] out, rows ld_grad >= V values apart, of type dtype; may be the logits themselves (same ld)
  * ardiff_distill_topk gives loss and stats; ardiff_distill_topk_backward the gradient from stats, as a graph of automatic
- * differentiation asks for it; ardiff_distill_topk_step all three at once, for rows whose weight is known.
- * Arithmetic is fp32 (fp32 sums in a fixed order: equal calls give equal bits); a gradient is rounded once.
+ * differentiation asks for it (which this library has none of); ardiff_distill_topk_step all three at once, for rows whose
+ * weight is known.
+ * Arithmetic is fp32, with exponentials good to 2^-22; sums are formed in a fixed order (equal calls give equal bits) and
+ * compensated over the row, so that ln Z is off by some 1e-6 at any V; a gradient is rounded once. Probabilities below 2^-126
+ * may count as 0 on either side, and a difference of two logits over T beyond fp32 as infinite.
  * ------------------------------------------------------------------------------------- */
 #define ARDIFF_DISTILL_MAX_V (1 << 24)
 #define ARDIFF_DISTILL_MAX_K 1024

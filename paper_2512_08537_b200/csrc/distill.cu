@@ -383,10 +383,11 @@ int dispatch(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t ld
     const int64_t pieces = (int64_t)V * size / 16;
     a.parts = 1;
     // A gradient's parts are strangers to each other: of 4096 pieces, so that they end one by one and not in a few waves (4096 x 131072
-    // bf16: 375 us with a CTA a row, 341 with four).
+    // bf16: 364 us with a CTA a row, 348 with two, 330 with four, 369 with eight).
     if (MODE == BACKWARD) a.parts = (int)std::min<int64_t>(std::max<int64_t>(1, (pieces + 4095) / 4096), (((int64_t)1 << 31) - 1) / n);
     // More CTAs a row while there is room for them and each keeps several pieces a thread; otherwise meeting costs more than a part of a
-    // row saves (2048 x 32768 bf16, loss: 45 us with one, 60 with two).
+    // row saves (us with 1 / 2 / 4 CTAs, bf16: loss 2048 x 32768 35 / 52 / 96, 296 x 32768 9.6 / 11.0 / 18.4, 64 x 32768 7.4 / 6.7 / 6.9,
+    // 16 x 8191 4.7 / 5.3 / 5.4; step 2048 x 32768 77 / 111 / 206, 64 x 131072 34 / 23 / 22, with eight 26).
     while (a.parts < 8 && n * a.parts < 148 * 2 && pieces >= (int64_t)8 * kThreadsOf<MODE> * a.parts) a.parts *= 2;
     if (MODE != FORWARD)
         for (a.seen = 2; a.seen < 2 * k; a.seen *= 2) {}

@@ -364,7 +364,9 @@ __global__ void __launch_bounds__(kThreads) truncate_kernel(const Truncate a) {
     }
 }
 
-// Buffers of at most this many tokens: one CTA writes them in the launch that sums.
+// Buffers of at most this many tokens: one CTA writes them in the launch that sums. (The host knows the buffer's size, not how much of it
+// the call fills. us with one / two launches: 256 requests with 256 tokens 7.4 / 10.4, with 8000 12.9 / 10.6; 2048 requests with 8000
+// 14.9 / 12.5; 64 with 16000 16.8 / 9.9. So a full buffer of this size loses some 5 us, a nearly empty one gains 3.)
 constexpr int64_t kOneLaunchTokens = 16384;
 
 // The current device's SM count, its kernels' shared memory granted; 0 where that fails. Asked once a device.

@@ -24,9 +24,12 @@
 //   what none of these     (thousands of different logits closer together than 2^-14 octaves of the weight): a search by the logits
 //   settles                as whole numbers
 //
-// Measured on B200 (L2 flushed, us; floor: the row read once at the measured copy rate), 512 x 131072 bf16, floor 20.5: T = 0 39, top-k 50
-// with top-p 51, no filter 111 (bound by 67 million fp64 weights of 15 instructions, 60 us at 64 a clock and SM), nuclei of tens of
-// tokens 210, of tens of thousands 490 to 530, min-p that keeps thousands 230. 1 x 32768 bf16 with top-k and top-p: 14, of which a dozen barriers and dependent loads are all.
+// Measured on B200 (one call after the other, inputs not in L2, us; floor: the row read once at the measured copy rate), 512 x 131072 bf16, floor
+// 20.5: T = 0 28, top-k below 100 with top-p 47, no filter 106 (bound by 67 million fp64 weights of 15 instructions, 60 us at 64 a clock
+// and SM), nuclei of rows that fall off steeply 420, of flat ones (tens of thousands) 610, min-p that keeps few 55, thousands 223.
+// 1 x 32768 bf16 with top-k and top-p, two CTAs: 16, of which a dozen barriers and dependent loads are all.
+// 64 registers a thread, for four CTAs an SM, cost sample_kernel 600 to 700 bytes of spills (up to 190 in the functions it calls); with
+// 80 and three CTAs sums were 10 % faster and lists 30 % slower.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 #include <limits.h>
@@ -1514,7 +1517,11 @@ __global__ void __launch_bounds__(kThreads, 4) sample_kernel(const Args args) {
 template <typename T>
 int launch(Args a, int64_t n, cudaStream_t st) {
     // More CTAs a row while there is room for them and each keeps so many pieces that it gains: a list is one CTA's work, and the others
-    // cost it meetings (1 x 32768 bf16 with top-k: 18.7 us with one CTA, 22.6 with four; sums of all weights: 22.5 and 18.5).
+    // cost it meetings. us with 1 / 2 / 4 / 8 CTAs, 8 rows of bf16: top-k with top-p 16384 14.6 / 15.9 / 16.7 / 18.6, 32768 15.7 / 17.1 /
+    // 16.2 / 17.5, 65536 19.0 / 17.7 / 17.4 / 17.1, 131072 25.6 / 20.2 / 17.8 / 18.1; no filter 8192 12.0 / 13.5 / 14.1 / 13.7, 16384 14.0 /
+    // 13.9 / 13.6 / 14.5, 32768 17.3 / 16.0 / 14.1 / 14.0; nuclei alone 16384 51.6 / 47.0 / 45.7 / 47.2, 32768 75 / 60 / 51 / 50. The lists alone
+    // would have twice as many pieces a CTA; but calls with top_k have rows without it, which lose more (64 x 65536, nuclei: 80 us
+    // with four CTAs, 100 with two). Room: 64 rows of 131072 with no filter 23.9 with four CTAs, 26.5 with eight.
     const int64_t least = a.top_k ? 2048 : 1024;
     const int64_t pieces = ((int64_t)a.V + ardiff::Piece<T>::N - 1) / ardiff::Piece<T>::N;
     int parts = 1;
