@@ -71,3 +71,27 @@ def test_no_memory_is_given_out_while_a_call_on_another_stream_uses_it(name):
     assert not places & {o.data_ptr() for o in others}
     for i in whole:
         assert torch.equal(kept[i], want[i].cpu()), i
+
+
+def test_a_captured_graph_with_a_call_on_a_second_stream():
+    """The call lies on a branch of the graph; its results are the graph's memory and follow the inputs at every replay."""
+    t = make()
+    x, u = t["x"], t["u"]
+    side = torch.cuda.Stream()
+    want = [v.clone() for v in ardiff.ardiff_sample_tokens(x, u, stream=side)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        token, logprob = ardiff.ardiff_sample_tokens(x, u, stream=side)
+        ardiff.ardiff_entropy_gate_stats(t["feat"], 5.0, stream=side)          # dropped at once
+        here.wait_stream(side)
+        twice = 2 * token
+    x0 = x.clone()
+    for flip in (False, True, False):
+        x.copy_(x0.flip(0) if flip else x0)
+        graph.replay()
+        again = want if not flip else ardiff.ardiff_sample_tokens(x, u)
+        torch.cuda.synchronize()
+        assert torch.equal(token, again[0]) and torch.equal(logprob, again[1]) and torch.equal(twice, 2 * again[0])
