@@ -510,6 +510,123 @@ int ardiff_distill_topk_step(const void* logits, int32_t dtype, int64_t n, int32
                              int32_t teacher_dtype, const int32_t* ids, int32_t k, float temperature, const float* weight,
                              float* loss, float* stats, void* grad, int64_t ld_grad, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Around a draft model's attention: rotary positions with several axes, attention over the pages of a cache, the weight that
+ * every token has got, and eviction of those that got least. (Where a draft has attention layers; the paper's own text and image
+ * tokens have one, or a row and a column, of positions. Nothing of it is read on the host.)
+ *
+ * A cache here is two pools, of keys and of values: value (pg, i, h, d) of a pool lies at pg * page_stride + i * token_stride +
+ * h * head_stride + d values, for 0 <= pg < pages, 0 <= i < page, 0 <= h < heads, 0 <= d < width (so the tokens of a page, or its
+ * heads, may lie next to each other). Tables, lengths, offsets and slots are those of ardiff_pages_extend.
+ * ------------------------------------------------------------------------------------- */
+
+/* Rotary positions. Token t turns pair i of every head by angle = position[axis[i]][t] * freq[i]:
+ *   (a, b) -> (a cos - b sin, a sin + b cos),   values i and i + pairs of the row, or 2 i and 2 i + 1 (`neighbours` != 0);
+ * values from 2 * pairs on are copied. ardiff_rotary_backward turns by the negative angle: the gradients of what ardiff_rotary
+ * returned become those of its inputs. Turns are formed in fp64, rotations in fp32 and rounded once.
+ *   q, k        dev [n][heads][width] of type dtype (ARDIFF_BF16, ARDIFF_F16 or ARDIFF_F32), width contiguous, strides in
+ *               values, at multiples of the value's size (16-byte boundaries are fastest); either may have 0 heads
+ *   q_out, k_out  the same shape; may be the inputs themselves (same strides), must not overlap them otherwise
+ *   n           0 <= n < 2^31;  heads <= ARDIFF_ROTARY_MAX_HEADS;  1 <= width <= ARDIFF_ROTARY_MAX_WIDTH;  0 <= 2 * pairs <= width
+ *   position    dev int32 [axes][n], rows position_ld apart: any numbers
+ *   freq        dev float [pairs];  axis  dev int32 [pairs], or NULL: 0. A pair of an axis outside 0 .. axes - 1 stands still
+ * ardiff_rotary_append turns q into q_out, and k into its cache, and copies v there: token t's row goes to slot[t] = page * id +
+ * place, as ardiff_pages_extend lists them.
+ *   slot        dev int64 [n], each its own; the keys and values of tokens with one outside 0 .. pages * page - 1 are not written
+ *   count       dev int32 [1], or NULL: tokens from *count on (a padded batch: offset[requests] of the extension) are not touched */
+#define ARDIFF_ROTARY_MAX_WIDTH 512
+#define ARDIFF_ROTARY_MAX_HEADS 1024
+int ardiff_rotary(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head,
+                  int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, void* k_out, int64_t k_out_token,
+                  int64_t k_out_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width, const int32_t* position,
+                  int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs, int32_t neighbours,
+                  void* stream);
+int ardiff_rotary_backward(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head,
+                           int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, void* k_out, int64_t k_out_token,
+                           int64_t k_out_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width, const int32_t* position,
+                           int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs,
+                           int32_t neighbours, void* stream);
+int ardiff_rotary_append(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head,
+                         int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, const void* v, int64_t v_token,
+                         int64_t v_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width, const int32_t* position,
+                         int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs,
+                         int32_t neighbours, const int64_t* slot, const int32_t* count, void* k_cache, int64_t k_cache_page,
+                         int64_t k_cache_token, int64_t k_cache_head, void* v_cache, int64_t v_cache_page, int64_t v_cache_token,
+                         int64_t v_cache_head, int32_t pages, int32_t page, void* stream);
+
+/* Attention of new tokens over pages. Request r's new tokens are rows offset[r] .. offset[r + 1] - 1 of q, its length[r] tokens (the new
+ * ones among them, at its end) lie in the pages of its row of the table. With G = q_heads / heads, query head h looks at head h / G:
+ *   w_p = exp(scale q.k_p);   out = sum_p w_p v_p / sum_p w_p;   lse = ln sum_p w_p
+ * over the keys p < length[r] - n + i + 1 for the i-th of its n new tokens (causal != 0), or p < length[r] for all. A query that sees
+ * no key has out 0 and lse -inf. Rows of q behind offset[requests] are not read, those of out and lse left as they were.
+ * Shared tokens: the requests group[g] .. group[g + 1] - 1 (g < groups) have their first shared[g] tokens in common, so these are read
+ * once for all of them, through the table's row group[g] alone. (The other rows must name pages that hold the same. Where a query of the group does
+ * not see all of them, only those that all see are taken as shared.)
+ *   q, out      dev [tokens][q_heads][head_width] of type dtype, ARDIFF_BF16 or ARDIFF_F16, strides in values; lse  dev float
+ *               [tokens][q_heads], rows lse_token apart.  tokens * q_heads < 2^31, q_heads <= ARDIFF_ROTARY_MAX_HEADS, a multiple of heads
+ *   caches      as above, of the same type; head_width 64, 80, 96 or 128 (others: ERR_UNSUPPORTED). Pointers on 16-byte boundaries, strides
+ *               multiples of 8 values, those of q and out too
+ *   table       dev int32 [requests][width];  length  dev int32 [requests];  offset  dev int32 [requests + 1]
+ *   group       dev int32 [groups + 1], shared  dev int32 [groups]; groups == 0: NULL
+ *   most        new tokens of a request at most, or 0 where that is not known: it only decides how the work is laid out
+ *   status      dev int32 [1] out: ARDIFF_OK; ARDIFF_ERR_SHAPE where offsets descend or pass `tokens`, a length is negative or above
+ *               width * page, groups descend or pass `requests`, or shared is negative (then nothing is computed), or where a page outside 0 .. pages - 1 was met
+ *               (then the results of the requests that have it mean nothing)
+ *   workspace   dev, 256-byte aligned, at least ardiff_attend_workspace(...) bytes, as for ardiff_pages_evict
+ * Products take 16-bit operands with fp32 sums; weights are fp32 and rounded to dtype as operands of the second product, their sum is
+ * that of the unrounded ones. The order of sums follows sizes and lengths: equal calls give equal bits. */
+int64_t ardiff_attend_workspace(int32_t requests, int32_t groups, int64_t tokens, int32_t q_heads, int32_t heads, int32_t head_width);
+int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype, const void* k_cache,
+                        int64_t k_page, int64_t k_token, int64_t k_head, const void* v_cache, int64_t v_page, int64_t v_token,
+                        int64_t v_head, int32_t pages, int32_t page, int32_t heads, int32_t head_width, const int32_t* table,
+                        int32_t width, int32_t requests, const int32_t* length, const int32_t* offset, int32_t groups,
+                        const int32_t* group, const int32_t* shared, int32_t most, float scale, int32_t causal, void* out,
+                        int64_t out_token, int64_t out_head, float* lse, int64_t lse_token, int32_t* status, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
+/* The weight that every token got, added up (what eviction goes by):
+ *   new_score[r][p] = (p < length[r] - n ? decay * score[r][p] : 0) + sum over the n new tokens that see p and all query heads of
+ *                     exp(scale q.k_p - lse)        for first[r] <= p < length[r]; other entries are left as they were.
+ * Arguments as for ardiff_attend_pages, whose lse this takes (a row with lse -inf adds nothing); q may be the last queries of a
+ * prompt alone. A request without new tokens has its scores multiplied by decay.
+ *   first       dev int32 [requests], or NULL: 0 (e.g. behind shared tokens, which are not one request's to evict)
+ *   score, new_score  dev float [requests], rows ld and new_ld apart (lengths may not pass either); may be the same
+ *   status      as above;  workspace  16-byte aligned, at least ardiff_attend_weights_workspace(requests) bytes */
+int64_t ardiff_attend_weights_workspace(int32_t requests);
+int ardiff_attend_weights(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype,
+                          const void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head, int32_t pages, int32_t page,
+                          int32_t heads, int32_t head_width, const int32_t* table, int32_t width, int32_t requests,
+                          const int32_t* length, const int32_t* offset, const int32_t* first, const float* lse, int64_t lse_token,
+                          const float* score, int64_t ld, int32_t most, float scale, float decay, int32_t causal, float* new_score,
+                          int64_t new_ld, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Eviction. Of request r's length[r] tokens keep = min(length[r], max(budget[r], first[r])) stay: those at places below first[r], and of the
+ * others those of largest score, the lowest place first where equal. Tokens whose position is at or above seen[r] - recent count as
+ * infinitely heavy, NaN as -inf. Tokens that stay keep their place where it is below keep; the others move, in order, into the places
+ * below keep that became free, and what is known of them with them. (Attention does not depend on the order of its keys, except for
+ * new ones that must not see each other; ardiff_pages_truncate with new_length as the target gives the pages back.)
+ *   requests    0 <= requests <= ARDIFF_PAGES_MAX_REQUESTS;  page >= 1, width >= 0 pages a row of the table, page * width < 2^31
+ *   length, budget, first   dev int32 [requests]; first may be NULL (0). Budgets below 0 are 0
+ *   score       dev float [requests], rows ld apart: what ardiff_attend_weights adds up
+ *   position    dev int32, the same shape, or NULL: the place.  seen  dev int32 [requests], or NULL: the length
+ *   table       dev int32 [requests][width];  k_cache, v_cache  as above, of any of the three types, head_width of them a head a
+ *               multiple of 16 bytes, strides and pointers too. A page that two requests share must lie below both their `first`
+ *   new_length  dev int32 [requests] out; may be `length`
+ *   new_score, new_position, source   dev [requests], rows new_ld apart, out, entries below new_length[r] only: score and position of the token that is
+ *               at the place now, and the place it had. The last two may be NULL; the first two may be their inputs (same distance)
+ *   status      dev int32 [1] out: ARDIFF_OK; ARDIFF_ERR_SHAPE where a length is negative or above width * page, ld or new_ld (that request
+ *               is left as it is) or a token moves from or to a page outside 0 .. pages - 1 (it is not moved)
+ *   workspace   dev, 16-byte aligned, at least ardiff_pages_evict_workspace(requests, page, width) bytes; nothing is kept in it between
+ *               calls, but calls that may run at the same time need their own */
+int64_t ardiff_pages_evict_workspace(int32_t requests, int32_t page, int32_t width);
+int ardiff_pages_evict(int32_t requests, const int32_t* length, const int32_t* budget, const int32_t* first, const float* score,
+                       int64_t ld, const int32_t* position, const int32_t* seen, int32_t recent, const int32_t* table,
+                       int32_t width, int32_t dtype, void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head,
+                       void* v_cache, int64_t v_page, int64_t v_token, int64_t v_head, int32_t pages, int32_t page,
+                       int32_t heads, int32_t head_width, int32_t* new_length, float* new_score, int32_t* new_position,
+                       int32_t* source, int64_t new_ld, int32_t* status, void* workspace, int64_t workspace_bytes,
+                       void* stream);
+
 /* Number of kernel launches the last call of the gate, the head, the cache's pages or the rows of logits on this
  * thread enqueued (for launch accounting by benchmarks). */
 int ardiff_last_launch_count(void);

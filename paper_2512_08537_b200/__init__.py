@@ -125,6 +125,29 @@ def lib() -> ctypes.CDLL:
         L.ardiff_distill_topk_backward.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, i32, f32, vp, vp, vp, i64, vp]
         L.ardiff_distill_topk_step.restype = ctypes.c_int
         L.ardiff_distill_topk_step.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, i32, f32, vp, vp, vp, vp, i64, vp]
+        turn = [vp, i64, i64, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, i32, i32, i64, i32, vp, i64, i32, vp, vp, i32, i32, vp]
+        L.ardiff_rotary.restype = ctypes.c_int
+        L.ardiff_rotary.argtypes = turn
+        L.ardiff_rotary_backward.restype = ctypes.c_int
+        L.ardiff_rotary_backward.argtypes = turn
+        L.ardiff_rotary_append.restype = ctypes.c_int
+        L.ardiff_rotary_append.argtypes = [vp, i64, i64, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, i32, i32, i64, i32, vp, i64, i32,
+                                           vp, vp, i32, i32, vp, vp, vp, i64, i64, i64, vp, i64, i64, i64, i32, i32, vp]
+        L.ardiff_attend_workspace.restype = i64
+        L.ardiff_attend_workspace.argtypes = [i32, i32, i64, i32, i32, i32]
+        L.ardiff_attend_pages.restype = ctypes.c_int
+        L.ardiff_attend_pages.argtypes = [vp, i64, i64, i32, i64, i32, vp, i64, i64, i64, vp, i64, i64, i64, i32, i32, i32, i32, vp, i32,
+                                          i32, vp, vp, i32, vp, vp, i32, f32, i32, vp, i64, i64, vp, i64, vp, vp, i64, vp]
+        L.ardiff_attend_weights_workspace.restype = i64
+        L.ardiff_attend_weights_workspace.argtypes = [i32]
+        L.ardiff_attend_weights.restype = ctypes.c_int
+        L.ardiff_attend_weights.argtypes = [vp, i64, i64, i32, i64, i32, vp, i64, i64, i64, i32, i32, i32, i32, vp, i32, i32, vp, vp, vp,
+                                            vp, i64, vp, i64, i32, f32, f32, i32, vp, i64, vp, vp, i64, vp]
+        L.ardiff_pages_evict_workspace.restype = i64
+        L.ardiff_pages_evict_workspace.argtypes = [i32, i32, i32]
+        L.ardiff_pages_evict.restype = ctypes.c_int
+        L.ardiff_pages_evict.argtypes = [i32, vp, vp, vp, vp, i64, vp, vp, i32, vp, i32, i32, vp, i64, i64, i64, vp, i64, i64, i64, i32,
+                                         i32, i32, i32, vp, vp, vp, vp, i64, vp, vp, i64, vp]
         _lib = L
     return _lib
 
@@ -313,6 +336,7 @@ class _Torch:
         import torch
         self.i32, self.i64, self.f32 = torch.int32, torch.int64, torch.float32
         self.types = {torch.bfloat16: ARDIFF_BF16, torch.float16: ARDIFF_F16, torch.float32: ARDIFF_F32}
+        self.u8 = torch.uint8
         self.empty, self.device = torch.empty, torch.cuda.device
         self.current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -530,6 +554,249 @@ def ardiff_distill_topk_step(logits, teacher, ids, weight, temperature: float = 
     _run(lib().ardiff_distill_topk_step, "ardiff_distill_topk_step", index, *args, temperature, weight.data_ptr(),
          loss.data_ptr(), stats.data_ptr(), grad.data_ptr(), _rows(grad))
     return loss, stats, grad
+
+
+def _heads(x, index: int):
+    """Address, strides of tokens and heads, and heads of a tensor [n, heads, width] whose rows are contiguous."""
+    n, heads, width = x.shape
+    assert x.get_device() == index and heads < _SIZES and width < _SIZES, f"a tensor on cuda:{index} expected, of sizes within 32 bits"
+    token, head, one = x.stride()
+    assert width <= 1 or one == 1, "rows must be contiguous"
+    return x.data_ptr(), token, head, heads
+
+
+def _out_heads(x, like, index: int):
+    """The same without the number of heads, for results of the shape and type of `like`. They must not overlap themselves."""
+    assert x.dtype is like.dtype and x.shape == like.shape, f"{like.dtype} {tuple(like.shape)} expected, got {x.dtype} {tuple(x.shape)}"
+    n, heads, width = x.shape
+    token, head = x.stride()[:2]
+    assert (heads <= 1 or head >= width) and (n <= 1 or token >= width), "rows of results must not overlap"
+    return _heads(x, index)[:3]
+
+
+def _rotary_args(q, k, position, freq, axis):
+    t = _t()
+    index = q.get_device()
+    n, _, width = q.shape
+    assert index >= 0 and k.dtype is q.dtype and k.shape[0] == n and k.shape[2] == width, "queries and keys of the same tokens, type and width expected"
+    if position.dim() == 1:
+        position = position[None]
+    axes = position.shape[0]
+    assert position.dtype is t.i32 and position.get_device() == index and position.shape[1] == n and (n <= 1 or position.stride(1) == 1), \
+        f"int32 positions [axes, {n}] on cuda:{index} expected"
+    pairs = freq.numel()
+    assert n < _SIZES and pairs < _SIZES and axes < _SIZES, _TOO_LARGE
+    _check_f32(freq, pairs, index)
+    if axis is not None:
+        _check_i32(axis, pairs, index)
+    return index, t.types.get(q.dtype, -1), n, width, (position.data_ptr(), position.stride(0) if axes > 1 else 0, axes, freq.data_ptr(), _ptr(axis), pairs)
+
+
+def _turned(fn, where, q, k, position, freq, axis, neighbours, q_out, k_out):
+    index, dtype, n, width, angles = _rotary_args(q, k, position, freq, axis)
+    if q_out is None:
+        q_out = _torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None:
+        k_out = _torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    qp, qt, qh, q_heads = _heads(q, index)
+    kp, kt, kh, k_heads = _heads(k, index)
+    _run(fn, where, index, qp, qt, qh, *_out_heads(q_out, q, index), q_heads, kp, kt, kh, *_out_heads(k_out, k, index), k_heads, dtype, n,
+         width, *angles, 1 if neighbours else 0)
+    return q_out, k_out
+
+
+def ardiff_rotary(q, k, position, freq, axis=None, neighbours: bool = False, q_out=None, k_out=None, stream=None):
+    """Queries [n, heads, width] and keys [n, kv heads, width] (bf16, f16 or f32, any strides with contiguous rows) turned by their positions:
+    pair i of token t by position[axis[i], t] * freq[i] (position int32 [axes, n] or [n], freq f32 [pairs], axis int32 [pairs] or None for the
+    first). A pair is values i and i + pairs, or 2 i and 2 i + 1 (neighbours); values from 2 * pairs on are copied. q_out and k_out may be q and k.
+    Returns (q_out, k_out)."""
+    if stream is not None:
+        return _beside(ardiff_rotary, stream, q, k, position, freq, axis, neighbours, q_out, k_out)
+    return _turned(lib().ardiff_rotary, "ardiff_rotary", q, k, position, freq, axis, neighbours, q_out, k_out)
+
+
+def ardiff_rotary_backward(grad_q, grad_k, position, freq, axis=None, neighbours: bool = False, q_out=None, k_out=None, stream=None):
+    """Gradients with respect to what ardiff_rotary was given, from those with respect to what it returned. Arguments as there."""
+    if stream is not None:
+        return _beside(ardiff_rotary_backward, stream, grad_q, grad_k, position, freq, axis, neighbours, q_out, k_out)
+    return _turned(lib().ardiff_rotary_backward, "ardiff_rotary_backward", grad_q, grad_k, position, freq, axis, neighbours, q_out, k_out)
+
+
+def _cache_args(cache, dtype, index: int):
+    """Address and strides of pages, tokens and heads of a cache [pages, page, heads, width] whose rows are contiguous."""
+    assert cache.dtype is dtype and cache.get_device() == index, f"a cache of {dtype} on cuda:{index} expected"
+    pages, page, heads, width = cache.shape
+    assert pages < _SIZES and page < _SIZES and heads < _SIZES and width < _SIZES, _TOO_LARGE
+    a, b, c, d = cache.stride()
+    assert width <= 1 or d == 1, "rows must be contiguous"
+    return cache.data_ptr(), a, b, c
+
+
+def ardiff_rotary_append(q, k, v, position, freq, slot, k_cache, v_cache, axis=None, count=None, neighbours: bool = False, q_out=None,
+                         stream=None):
+    """Queries turned as by ardiff_rotary (into q_out), keys turned and written with their values into a cache (k_cache, v_cache [pages, page,
+    kv heads, width], rows contiguous) at slot[t] (int64 [n]: page * id + place, as ardiff_pages_extend lists them; others are not written).
+    Tokens from count[0] on (int32 [1], e.g. offset[-1:]) are not touched. Returns q_out."""
+    if stream is not None:
+        return _beside(ardiff_rotary_append, stream, q, k, v, position, freq, slot, k_cache, v_cache, axis, count, neighbours, q_out)
+    index, dtype, n, width, angles = _rotary_args(q, k, position, freq, axis)
+    if q_out is None:
+        q_out = _torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert v.shape == k.shape and v.dtype is k.dtype, "keys and values of the same shape and type expected"
+    assert slot.dtype is _torch.i64 and slot.numel() == n and slot.get_device() == index and slot.is_contiguous(), f"int64 slots [{n}] on cuda:{index} expected"
+    if count is not None:
+        _check_i32(count, 1, index)
+    pages, page = k_cache.shape[:2]
+    assert k_cache.shape == v_cache.shape and k_cache.shape[2] == k.shape[1] and k_cache.shape[3] == width, "caches [pages, page, kv heads, width] expected"
+    qp, qt, qh, q_heads = _heads(q, index)
+    kp, kt, kh, k_heads = _heads(k, index)
+    _run(lib().ardiff_rotary_append, "ardiff_rotary_append", index, qp, qt, qh, *_out_heads(q_out, q, index), q_heads, kp, kt, kh,
+         *_heads(v, index)[:3], k_heads, dtype, n, width, *angles, 1 if neighbours else 0, slot.data_ptr(), _ptr(count),
+         *_cache_args(k_cache, k.dtype, index), *_cache_args(v_cache, k.dtype, index), pages, page)
+    return q_out
+
+
+def _attend_args(q, k_cache, table, length, offset):
+    t = _t()
+    R, width = table.shape
+    pages, page, heads, D = k_cache.shape
+    T, q_heads, _ = q.shape
+    assert R < _SIZES and width < _SIZES and T < _SIZES, _TOO_LARGE
+    index = q.get_device()
+    assert index >= 0 and q.shape[2] == D, "queries and keys of the same width expected"
+    _check_i32(table, R * width, index)
+    _check_i32(length, R, index)
+    _check_i32(offset, R + 1, index)
+    return index, R, width, pages, page, heads, D, T, t.types.get(q.dtype, -1)
+
+
+def _workspace(size: int, where: str, device):
+    if size < 0:
+        raise ArdiffError(size, where)
+    return _torch.empty((size,), dtype=_torch.u8, device=device)
+
+
+def _most(most) -> int:
+    most = 0 if most is None else most
+    assert 0 <= most < _SIZES, _TOO_LARGE
+    return most
+
+
+def ardiff_attend_pages(q, k_cache, v_cache, table, length, offset, group=None, shared=None, most=None, scale=None, causal: bool = True,
+                        out=None, lse=None, status=None, stream=None):
+    """Attention of every request's new tokens (rows offset[r] .. offset[r + 1] - 1 of q [tokens, heads, width], bf16 or f16) over its length[r]
+    tokens, the new ones at their end, in the pages table[r] of the caches [pages, page, kv heads, width]. Requests group[g] .. group[g + 1] - 1
+    share their first shared[g] tokens, which are read once for all of them (int32 [groups + 1] and [groups]). most: new tokens of a request at
+    most, if known. scale: 1 / sqrt(width) unless given. Returns (out like q, lse f32 [tokens, heads], status int32 [1], not looked at here); rows behind
+    offset[-1] are left as they were."""
+    if stream is not None:
+        return _beside(ardiff_attend_pages, stream, q, k_cache, v_cache, table, length, offset, group, shared, most, scale, causal, out, lse, status)
+    index, R, width, pages, page, heads, D, T, dtype = _attend_args(q, k_cache, table, length, offset)
+    assert k_cache.shape == v_cache.shape, "caches of the same shape expected"
+    assert (group is None) == (shared is None), "group and shared belong together"
+    groups = 0
+    if group is not None:
+        groups = shared.numel()
+        assert groups < _SIZES, _TOO_LARGE
+        _check_i32(group, groups + 1, index)
+        _check_i32(shared, groups, index)
+    if out is None:
+        out = _torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    qp, qt, qh, q_heads = _heads(q, index)
+    lse = _made_f32(lse, (T, q_heads), T * q_heads, q)
+    status = _made_i32(status, 1, length)
+    L = lib()
+    size = L.ardiff_attend_workspace(R, groups, T, q_heads, heads, D)
+    work = _workspace(size, "ardiff_attend_pages", q.device)
+    _run(L.ardiff_attend_pages, "ardiff_attend_pages", index, qp, qt, qh, q_heads, T, dtype, *_cache_args(k_cache, q.dtype, index),
+         *_cache_args(v_cache, q.dtype, index), pages, page, heads, D, table.data_ptr(), width, R, length.data_ptr(), offset.data_ptr(), groups,
+         _ptr(group), _ptr(shared), _most(most), D ** -0.5 if scale is None else scale, 1 if causal else 0, *_out_heads(out, q, index),
+         lse.data_ptr(), q_heads, status.data_ptr(), work.data_ptr(), size)
+    return out, lse, status
+
+
+def _scores(x, R: int, index: int) -> int:
+    """Distance of the rows of a matrix of R rows; its row length may be any."""
+    assert x.dim() == 2 and x.shape[0] == R and x.get_device() == index, f"{R} rows on cuda:{index} expected"
+    if x.is_contiguous():
+        return x.shape[1]
+    assert x.shape[1] <= 1 or x.stride(1) == 1, "rows must be contiguous"
+    assert x.stride(0) >= x.shape[1], "rows must not overlap"
+    return x.stride(0)
+
+
+def ardiff_attend_weights(q, k_cache, table, length, offset, lse, score, first=None, most=None, decay: float = 1.0, scale=None,
+                          causal: bool = True, new_score=None, status=None, stream=None):
+    """The attention weight that every token got from the new tokens' queries, added to decay * score (f32 [requests, places]): arguments as for
+    ardiff_attend_pages, whose lse it takes. Places below first[r] (int32 [requests]) and from length[r] on are left as they are in new_score, which may
+    be `score` (and is made without them being set if not given). Returns (new_score, status int32 [1])."""
+    if stream is not None:
+        return _beside(ardiff_attend_weights, stream, q, k_cache, table, length, offset, lse, score, first, most, decay, scale, causal, new_score, status)
+    index, R, width, pages, page, heads, D, T, dtype = _attend_args(q, k_cache, table, length, offset)
+    qp, qt, qh, q_heads = _heads(q, index)
+    _check_f32(lse, T * q_heads, index)
+    if first is not None:
+        _check_i32(first, R, index)
+    ld = _scores(score, R, index)
+    if new_score is None:
+        new_score = _torch.empty(score.shape, dtype=_torch.f32, device=score.device)
+    assert score.dtype is _torch.f32 and new_score.dtype is _torch.f32 and new_score.shape == score.shape, "f32 scores of the same shape expected"
+    new_ld = _scores(new_score, R, index)
+    places = score.shape[1]
+    assert width * page <= places, f"scores for the {width * page} places of a row of the table expected, got {places}"
+    status = _made_i32(status, 1, length)
+    L = lib()
+    size = L.ardiff_attend_weights_workspace(R)
+    work = _workspace(size, "ardiff_attend_weights", q.device)
+    _run(L.ardiff_attend_weights, "ardiff_attend_weights", index, qp, qt, qh, q_heads, T, dtype, *_cache_args(k_cache, q.dtype, index), pages, page,
+         heads, D, table.data_ptr(), width, R, length.data_ptr(), offset.data_ptr(), _ptr(first), lse.data_ptr(), q_heads, score.data_ptr(), ld,
+         _most(most), D ** -0.5 if scale is None else scale, decay, 1 if causal else 0, new_score.data_ptr(), new_ld, status.data_ptr(),
+         work.data_ptr(), size)
+    return new_score, status
+
+
+def ardiff_pages_evict(length, budget, score, table, k_cache, v_cache, first=None, position=None, seen=None, recent: int = 0, new_length=None,
+                       new_score=None, new_position=None, source=None, status=None, stream=None):
+    """Leaves request r its budget[r] tokens of largest score (f32 [requests, places]), those below first[r] and those whose position (int32 [requests,
+    places], or the place) is at or above seen[r] - recent before all others. Kept tokens behind the new end move, in the caches too, into the places
+    that became free. int32 CUDA tensors [requests]; new_length may be `length`, new_score `score`, new_position `position`; source (int32, like
+    score): the place that every token had. Entries behind the new length are left as they are (not set where made here). Returns
+    (new_length, new_score, new_position or None, status)."""
+    if stream is not None:
+        return _beside(ardiff_pages_evict, stream, length, budget, score, table, k_cache, v_cache, first, position, seen, recent, new_length,
+                       new_score, new_position, source, status)
+    t = _t()
+    R, width = table.shape
+    pages, page, heads, D = k_cache.shape
+    assert R < _SIZES and width < _SIZES and 0 <= recent < _SIZES, _TOO_LARGE
+    index = length.get_device()
+    assert index >= 0 and k_cache.shape == v_cache.shape, "caches of the same shape expected"
+    _check_i32(table, R * width, index)
+    for x in (length, budget, first, seen):
+        if x is not None:
+            _check_i32(x, R, index)
+    new_length = _made_i32(new_length, R, length)
+    ld = _scores(score, R, index)
+    places = score.shape[1]
+    if new_score is None:
+        new_score = t.empty(score.shape, dtype=t.f32, device=score.device)
+    if new_position is None and position is not None:
+        new_position = t.empty(score.shape, dtype=t.i32, device=score.device)
+    assert score.dtype is t.f32 and new_score.dtype is t.f32 and new_score.shape == score.shape, "f32 scores of the same shape expected"
+    assert width * page <= places, f"scores for the {width * page} places of a row of the table expected, got {places}"
+    new_ld = _scores(new_score, R, index)
+    for x, rows in ((position, ld), (new_position, new_ld), (source, new_ld)):
+        if x is not None:
+            assert x.dtype is t.i32 and x.shape == score.shape and _scores(x, R, index) == rows, "int32 positions laid out as the scores are expected"
+    status = _made_i32(status, 1, length)
+    L = lib()
+    size = L.ardiff_pages_evict_workspace(R, page, width)
+    work = _workspace(size, "ardiff_pages_evict", length.device)
+    _run(L.ardiff_pages_evict, "ardiff_pages_evict", index, R, length.data_ptr(), budget.data_ptr(), _ptr(first), score.data_ptr(), ld, _ptr(position),
+         _ptr(seen), recent, table.data_ptr(), width, t.types.get(k_cache.dtype, -1), *_cache_args(k_cache, k_cache.dtype, index),
+         *_cache_args(v_cache, k_cache.dtype, index), pages, page, heads, D, new_length.data_ptr(), new_score.data_ptr(), _ptr(new_position),
+         _ptr(source), new_ld, status.data_ptr(), work.data_ptr(), size)
+    return new_length, new_score, new_position, status
 
 
 GATE_NOALLOC_MAX_BLOCKS = 1024

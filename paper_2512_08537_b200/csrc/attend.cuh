@@ -1,0 +1,152 @@
+// What the kernels of attention over pages share: the cache, the plan of a call's work, the pieces of results that are joined.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace ardiff {
+
+struct Pages {                                   // strides in bytes
+    const char* k;
+    const char* v;
+    long long k_page, k_token, k_head, v_page, v_token, v_head;
+    const int32_t* table;
+    int width, page, pages, heads;
+};
+
+// Query rows that look at the same keys together. A segment is the new tokens of one request, or of a group of requests that share
+// their first tokens; row j of it is token token0 + j / G, query head h G + j % G (G: query heads a kv head). A block is up to kBlockRows
+// rows of a segment and the keys that they see of one row of the table. Its row j sees the keys below limit + step * (j / G).
+struct Block {
+    int token0, row0, rows, request, key0, keys, limit, step;
+};
+
+struct PlanHead {
+    long long steps;                             // of all blocks: key tiles times kv heads
+    int blocks, own;                             // blocks [0, own): shared tokens; [own, blocks): the requests' own
+};
+
+// Of a request: where its rows are among those of its group (prefix -1: no shared tokens)
+struct Share {
+    int prefix, row0;                            // first block of the shared tokens; its first row there
+};
+
+struct Plan {
+    PlanHead* head;
+    Block* block;
+    long long* steps;                            // [blocks + 1]: steps of the blocks before
+    long long* rows;                             // [blocks + 1]: rows of the blocks before
+    Share* share;                                // [requests]
+    int* shared;                                 // [requests]: shared tokens that the request does not read itself
+};
+
+struct Queries {                                 // strides in values
+    const void* q;
+    void* out;
+    float* lse;
+    long long q_token, q_head, out_token, out_head, lse_token;
+    int heads, G;
+    long long tokens;
+};
+
+// Results of a unit (a block and a kv head) in pieces: of the CTA that began it, in rows[block] * heads + head * rows, and one of every CTA that
+// went on with it, in that CTA's own place behind all those. Values are relative to the piece's maximum, in powers of two.
+struct Pieces {
+    float* o;                                    // [rows][width]
+    float2* ml;                                  // [rows]: maximum, sum
+    long long main_rows;
+};
+
+__device__ __forceinline__ long long piece_row(const Pieces& p, long long rows_before, int heads, int rows, int h, int cta, int first, int cta_rows) {
+    return cta == first ? rows_before * heads + (long long)h * rows : p.main_rows + (long long)cta * cta_rows;
+}
+
+// The last of n + 1 ascending numbers x[0] = 0 .. x[n] that is not above s < x[n]. All lanes of a warp call it with the same arguments.
+__device__ __forceinline__ int find_last(const long long* x, int n, long long s) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = n;                          // x[lo] <= s < x[hi]
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 32) / 33;
+        const int at = lo + (lane + 1) * step;
+        const bool below = at < hi && x[at] <= s;
+        const int k = __popc(__ballot_sync(0xffffffffu, below));   // probes ascend, so these are the first k
+        const int up = lo + (k + 1) * step;
+        lo += k * step;
+        hi = up < hi ? up : hi;
+    }
+    return lo;
+}
+
+template <typename T> struct Pair;
+template <> struct Pair<__nv_bfloat16> {
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ float rounded(float a) { return __bfloat162float(__float2bfloat16_rn(a)); }
+    static __device__ __forceinline__ bool not_finite(uint32_t p) { return (p & 0x7f800000u) == 0x7f800000u || (p & 0x7f80u) == 0x7f80u; }
+};
+template <> struct Pair<__half> {
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ float rounded(float a) { return __half2float(__float2half_rn(a)); }
+    static __device__ __forceinline__ bool not_finite(uint32_t p) { return (p & 0x7c000000u) == 0x7c000000u || (p & 0x7c00u) == 0x7c00u; }
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// 16-byte chunk c of row `row` of a tile of rows of D values: chunks change places with the row, or rows are a chunk longer than their values, so
+// that the eight rows of a matrix lie in different banks.
+template <int D> constexpr int kPitch = D % 64 ? 2 * D + 16 : 2 * D;
+template <int D> __device__ __forceinline__ uint32_t chunk_at(int row, int c) {
+    return row * kPitch<D> + ((D % 64 ? c : c ^ (row & 7)) << 4);
+}
+
+__device__ __forceinline__ long long warp_inclusive(long long v) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long up = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += up;
+    }
+    return v;
+}
+// Exclusive sum over a CTA's 1024 threads, and the total; `s` holds 32 values.
+__device__ __forceinline__ long long cta_scan(long long v, long long* s, long long* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long inc = warp_inclusive(v);
+    __syncthreads();
+    if (lane == 31) s[warp] = inc;
+    __syncthreads();
+    const long long w = warp_inclusive(s[lane]);
+    *total = __shfl_sync(0xffffffffu, w, 31);
+    const long long before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+    return inc - v + (warp ? before : 0);
+}
+
+// The current device's SM count; 0 where that fails. Asked once a device.
+int device_sms();
+
+}  // namespace ardiff

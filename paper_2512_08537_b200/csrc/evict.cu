@@ -1,0 +1,343 @@
+// ardiff_pages_evict: the tokens that have got least attention leave the cache.
+//
+// Of a request's `length` tokens `keep` stay: the ones in front of `first`, and of the others those of largest weight, lowest place first
+// where equal, with recent ones counted as infinitely heavy. Attention does not ask in which order keys lie (their positions are in their
+// rotations), so a token that stays keeps its place unless it lies at or behind the new end; those move, in order, into the places below it that
+// became free. So as many rows move as leave a place free below the new end, not the whole cache, and sources (>= keep) and
+// destinations (< keep) are apart: all moves run at once, in place.
+//
+// Two kernels. The first finds, by CTA a request, the keep-th largest weight by three counts of 11 bits each over whole numbers that order as
+// the weights do, then walks the places once more with a running count of heavier and equal ones: the number kept in front of a place p is
+// heavier(p) + min(equal(p), equal ones needed), which gives every hole and every token behind the end its rank. The second copies the rows.
+// Bound by the latency of those passes where few rows move, by memory where many do.
+#include <cuda_runtime.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <atomic>
+
+#include "../../include/ardiff.h"
+#include "common.cuh"
+#include "launch.cuh"
+#include "rows.cuh"
+
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kBins = 2048;
+constexpr int kPer = 4;                          // places of a thread, consecutive, in the last walk
+constexpr int kKept = 40960;                     // keys that shared memory holds; more are worked out again in every pass
+
+struct Evict {
+    const int32_t* length;
+    const int32_t* budget;
+    const int32_t* first;                        // or NULL: 0
+    const float* score;
+    const int32_t* position;                     // or NULL: the place
+    const int32_t* seen;                         // or NULL: the length
+    const int32_t* table;
+    char* k;
+    char* v;
+    int32_t* new_length;
+    float* new_score;
+    int32_t* new_position;
+    int32_t* source;
+    int32_t* status;
+    int2* move;                                  // [requests][capacity]: hole, token
+    int32_t* moves;                              // [requests]
+    long long ld, new_ld, limit;                 // limit: the longest request
+    long long k_page, k_token, k_head, v_page, v_token, v_head;   // bytes
+    int requests, recent, page, width, pages, heads, row, capacity;   // row: bytes of a head's row
+};
+
+// Whole numbers in the order of the weights: NaN as -inf, -0 as 0.
+__device__ __forceinline__ uint32_t ordered(float x) {
+    if (!(x == x)) x = -INFINITY;
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+constexpr uint32_t kInfinite = 0xff800000u;      // +inf
+
+// Exclusive sums of two 32-bit counts over the CTA, and the totals. `s` holds 32 values.
+__device__ __forceinline__ uint2 cta_scan(uint2 v, uint2* s, uint2* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint2 inc = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, inc.x, o), y = __shfl_up_sync(0xffffffffu, inc.y, o);
+        if (lane >= o) { inc.x += x; inc.y += y; }
+    }
+    __syncthreads();
+    if (lane == 31) s[warp] = inc;
+    __syncthreads();
+    uint2 w = s[lane];
+    const uint2 own = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, w.x, o), y = __shfl_up_sync(0xffffffffu, w.y, o);
+        if (lane >= o) { w.x += x; w.y += y; }
+    }
+    total->x = __shfl_sync(0xffffffffu, w.x, 31);
+    total->y = __shfl_sync(0xffffffffu, w.y, 31);
+    w.x -= own.x; w.y -= own.y;
+    return make_uint2(inc.x - v.x + __shfl_sync(0xffffffffu, w.x, warp), inc.y - v.y + __shfl_sync(0xffffffffu, w.y, warp));
+}
+
+__global__ void __launch_bounds__(kThreads) select_kernel(const Evict a) {
+    extern __shared__ uint32_t s_key[];
+    __shared__ uint32_t s_bin[kBins];
+    __shared__ uint2 s_scan[32];
+    __shared__ uint32_t s_prefix, s_rest, s_inside;
+    ardiff::begin_kernel();
+    const int tid = threadIdx.x, r = blockIdx.x;
+    if (r == 0) {
+        bool bad = false;
+        for (int i = tid; i < a.requests; i += kThreads) bad |= a.length[i] < 0 || (long long)a.length[i] > a.limit;
+        bad = __syncthreads_or(bad);
+        if (tid == 0) *a.status = bad ? ARDIFF_ERR_SHAPE : ARDIFF_OK;
+    }
+    const int length = a.length[r];
+    __syncthreads();                             // new_length may be the length itself
+    if (length < 0 || (long long)length > a.limit) {         // left as it is
+        if (tid == 0) { a.new_length[r] = length; a.moves[r] = 0; }
+        return;
+    }
+    const int first = a.first ? min(max(a.first[r], 0), length) : 0;
+    const int keep = min(length, max(max(a.budget[r], 0), first));
+    const float* score = a.score + r * a.ld;
+    const int32_t* position = a.position ? a.position + r * a.ld : nullptr;
+    const long long recent_from = (long long)(a.seen ? a.seen[r] : length) - a.recent;
+    float* new_score = a.new_score + r * a.new_ld;
+    int32_t* new_position = a.new_position ? a.new_position + r * a.new_ld : nullptr;
+    int32_t* source = a.source ? a.source + r * a.new_ld : nullptr;
+    if (tid == 0) a.new_length[r] = keep;
+    if (keep == length) {
+        if (tid == 0) a.moves[r] = 0;
+        for (int p = tid; p < length; p += kThreads) {
+            new_score[p] = score[p];
+            if (new_position) new_position[p] = position ? position[p] : p;
+            if (source) source[p] = p;
+        }
+        return;
+    }
+
+    auto work_out = [&](int p) -> uint32_t {
+        const long long pos = position ? position[p] : p;
+        return pos >= recent_from ? kInfinite : ordered(score[p]);
+    };
+    const int n = length - first;
+    auto key = [&](int i) -> uint32_t { return i < kKept ? s_key[i] : work_out(first + i); };
+    for (int i = tid; i < min(n, kKept); i += kThreads) s_key[i] = work_out(first + i);
+
+    // the need-th largest key, by its highest 11 bits, the next 11, the last 10
+    uint32_t prefix = 0, need = keep - first;
+    constexpr int shift[3] = {21, 10, 0}, above[3] = {32, 21, 10};
+    if (need > 0) {
+#pragma unroll
+        for (int round = 0; round < 3; ++round) {
+            for (int b = tid; b < kBins; b += kThreads) s_bin[b] = 0;
+            __syncthreads();
+            const uint32_t mask = round == 2 ? 1023u : 2047u;
+            for (int i = tid; i < n; i += kThreads) {
+                const uint32_t k = key(i);
+                if (round == 0 || (k >> above[round]) == (prefix >> above[round])) atomicAdd(&s_bin[(k >> shift[round]) & mask], 1u);
+            }
+            __syncthreads();
+            // bins from the top: thread t has the two from kBins - 1 - 2 t down
+            const int top = kBins - 1 - 2 * tid;
+            const uint32_t hi = s_bin[top], lo = s_bin[top - 1];
+            uint2 total;
+            const uint32_t before = cta_scan(make_uint2(hi + lo, 0u), s_scan, &total).x;
+            if (before < need && need <= before + hi + lo) {
+                const bool second = need > before + hi;
+                s_prefix = prefix | ((uint32_t)(second ? top - 1 : top) << shift[round]);
+                s_rest = need - before - (second ? hi : 0u);
+            }
+            __syncthreads();
+            prefix = s_prefix;
+            need = s_rest;                       // of those that begin like this
+            __syncthreads();
+        }
+    } else {
+        prefix = 0xffffffffu;                    // nothing is heavier or as heavy
+    }
+    const uint32_t border = prefix, equal = need;
+
+    // places in order: what is kept, its rank; holes below keep, tokens behind it
+    int2* move = a.move + (long long)r * a.capacity;
+    uint2 carry = make_uint2(0u, 0u);
+    uint32_t inside = 0;                         // kept ones of first .. keep - 1
+    for (int base = 0; base < n; base += kThreads * kPer) {
+        uint32_t k[kPer];
+        uint2 mine = make_uint2(0u, 0u);
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int i = base + tid * kPer + u;
+            k[u] = i < n ? key(i) : 0u;
+            if (i < n) { mine.x += k[u] > border; mine.y += k[u] == border; }
+        }
+        uint2 total;
+        uint2 at = cta_scan(mine, s_scan, &total);
+        at.x += carry.x; at.y += carry.y;
+        if (base <= keep - first && keep - first < base + kThreads * kPer) {
+            uint2 c = at;
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) {
+                const int i = base + tid * kPer + u;
+                if (i == keep - first) s_inside = c.x + min(c.y, equal);
+                c.x += k[u] > border; c.y += k[u] == border;
+            }
+            __syncthreads();
+            inside = s_inside;
+        }
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int i = base + tid * kPer + u, p = first + i;
+            if (i < n) {
+                const uint32_t before = at.x + min(at.y, equal);
+                const bool stays = k[u] > border || (k[u] == border && at.y < equal);
+                if (p < keep) {
+                    if (!stays) {
+                        move[i - before].x = p;
+                    } else {
+                        new_score[p] = score[p];
+                        if (new_position) new_position[p] = position ? position[p] : p;
+                        if (source) source[p] = p;
+                    }
+                } else if (stays) {
+                    move[before - inside].y = p;
+                }
+            }
+            at.x += k[u] > border; at.y += k[u] == border;
+        }
+        carry.x += total.x; carry.y += total.y;
+    }
+    for (int p = tid; p < first; p += kThreads) {
+        new_score[p] = score[p];
+        if (new_position) new_position[p] = position ? position[p] : p;
+        if (source) source[p] = p;
+    }
+    const int moves = keep - first - (int)inside;
+    if (tid == 0) a.moves[r] = moves;
+    __syncthreads();
+    for (int j = tid; j < moves; j += kThreads) {
+        const int2 m = move[j];
+        new_score[m.x] = score[m.y];
+        if (new_position) new_position[m.x] = position ? position[m.y] : m.y;
+        if (source) source[m.x] = m.y;
+    }
+}
+
+// A warp a move: the rows of all heads, keys and values, four pieces a lane under way.
+__global__ void __launch_bounds__(256) move_kernel(const Evict a, int split) {
+    ardiff::begin_kernel();
+    const int r = blockIdx.x / split, lane = threadIdx.x & 31;
+    const int2* move = a.move + (long long)r * a.capacity;
+    const int32_t* table = a.table + (long long)r * a.width;
+    const int moves = a.moves[r];
+    const int pieces = a.row / 16, all = a.heads * pieces;
+    for (int j = (blockIdx.x - r * split) * 8 + (threadIdx.x >> 5); j < moves; j += split * 8) {
+        const int2 m = move[j];
+        const int to_page = m.x / a.page, from_page = m.y / a.page;
+        const int to = table[to_page], from = table[from_page];
+        if (to < 0 || to >= a.pages || from < 0 || from >= a.pages) {
+            if (lane == 0) *a.status = ARDIFF_ERR_SHAPE;
+            continue;
+        }
+        const long long to_in = m.x - to_page * a.page, from_in = m.y - from_page * a.page;
+        const char* k_from = a.k + from * a.k_page + from_in * a.k_token;
+        const char* v_from = a.v + from * a.v_page + from_in * a.v_token;
+        char* k_to = a.k + to * a.k_page + to_in * a.k_token;
+        char* v_to = a.v + to * a.v_page + to_in * a.v_token;
+        for (int c0 = lane; c0 < all; c0 += 128) {
+            uint4 x[4], y[4];
+            long long k_off[4], v_off[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int c = c0 + 32 * u;
+                if (c >= all) continue;
+                const int h = c / pieces, in = (c - h * pieces) * 16;
+                k_off[u] = h * a.k_head + in;
+                v_off[u] = h * a.v_head + in;
+                x[u] = *reinterpret_cast<const uint4*>(k_from + k_off[u]);
+                y[u] = *reinterpret_cast<const uint4*>(v_from + v_off[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (c0 + 32 * u >= all) continue;
+                *reinterpret_cast<uint4*>(k_to + k_off[u]) = x[u];
+                *reinterpret_cast<uint4*>(v_to + v_off[u]) = y[u];
+            }
+        }
+    }
+}
+
+bool prepare_device() {
+    static std::atomic<bool> known[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    if (dev < 64 && known[dev].load(std::memory_order_relaxed)) return true;
+    if (cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKept * 4) != cudaSuccess) return false;
+    if (dev < 64) known[dev].store(true, std::memory_order_relaxed);
+    return true;
+}
+
+// moves of a request: as many as there are holes below the new end and tokens behind it
+int64_t move_capacity(int64_t limit) { return limit / 2 + 1; }
+
+}  // namespace
+
+extern "C" int64_t ardiff_pages_evict_workspace(int32_t requests, int32_t page, int32_t width) {
+    if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || page < 1 || width < 0 || (int64_t)page * width >= (int64_t)1 << 31)
+        return ARDIFF_ERR_SHAPE;
+    return (int64_t)requests * (8 * move_capacity((int64_t)page * width) + 4) + 16;
+}
+
+extern "C" int ardiff_pages_evict(int32_t requests, const int32_t* length, const int32_t* budget, const int32_t* first, const float* score,
+                                  int64_t ld, const int32_t* position, const int32_t* seen, int32_t recent, const int32_t* table,
+                                  int32_t width, int32_t dtype, void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head,
+                                  void* v_cache, int64_t v_page, int64_t v_token, int64_t v_head, int32_t pages, int32_t page,
+                                  int32_t heads, int32_t head_width, int32_t* new_length, float* new_score, int32_t* new_position,
+                                  int32_t* source, int64_t new_ld, int32_t* status, void* workspace, int64_t workspace_bytes,
+                                  void* stream) {
+    const int size = ardiff::value_size(dtype);
+    if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || page < 1 || width < 0 || pages < 0 || heads < 1 || heads > 65535 ||
+        head_width < 1 || head_width > ARDIFF_ROTARY_MAX_WIDTH || recent < 0 || ld < 0 || new_ld < 0 || (int64_t)page * width >= (int64_t)1 << 31)
+        return ARDIFF_ERR_SHAPE;
+    if (!size || head_width * size % 16) return ARDIFF_ERR_UNSUPPORTED;
+    if (!status) return ARDIFF_ERR_NULL;
+    if (requests > 0 && (!length || !budget || !score || !new_length || !new_score || !workspace || (width > 0 && !table) || !k_cache || !v_cache))
+        return ARDIFF_ERR_NULL;
+    if (((reinterpret_cast<uintptr_t>(k_cache) | reinterpret_cast<uintptr_t>(v_cache)) & 15u) ||
+        ((k_page | k_token | k_head | v_page | v_token | v_head) * size & 15) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
+        return ARDIFF_ERR_ALIGN;
+    const int64_t limit = (int64_t)page * width;
+    if (workspace_bytes < ardiff_pages_evict_workspace(requests, page, width) && requests > 0) return ARDIFF_ERR_SHAPE;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!prepare_device()) return ARDIFF_ERR_CUDA;
+    Evict a;
+    memset(&a, 0, sizeof(a));
+    a.length = length; a.budget = budget; a.first = first; a.score = score; a.position = position; a.seen = seen; a.table = table;
+    a.k = static_cast<char*>(k_cache); a.v = static_cast<char*>(v_cache);
+    a.new_length = new_length; a.new_score = new_score; a.new_position = new_position; a.source = source; a.status = status;
+    a.capacity = (int)move_capacity(limit);
+    a.move = static_cast<int2*>(workspace);
+    a.moves = reinterpret_cast<int32_t*>(a.move + (int64_t)requests * a.capacity);
+    a.ld = ld; a.new_ld = new_ld;
+    a.limit = limit < ld ? limit : ld;
+    a.limit = a.limit < new_ld ? a.limit : new_ld;
+    a.k_page = k_page * size; a.k_token = k_token * size; a.k_head = k_head * size;
+    a.v_page = v_page * size; a.v_token = v_token * size; a.v_head = v_head * size;
+    a.requests = requests; a.recent = recent; a.page = page; a.width = width; a.pages = pages; a.heads = heads; a.row = head_width * size;
+    if (requests == 0) {
+        const bool ok = cudaMemsetAsync(status, 0, 4, st) == cudaSuccess;
+        ardiff::set_launch_count(0);
+        return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+    }
+    const int64_t keys = limit < kKept ? limit : kKept;
+    const int split = requests >= 592 ? 1 : (592 + requests - 1) / requests;
+    const bool ok = ardiff::launch_early(select_kernel, (unsigned)requests, kThreads, 1, (size_t)keys * 4, st, a) &&
+                    ardiff::launch_early(move_kernel, (unsigned)(requests * split), 256, 1, 0, st, a, split);
+    ardiff::set_launch_count(2);
+    return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+}

@@ -1,0 +1,290 @@
+// Rotary positions with several axes:
+//   ardiff_rotary           queries and keys turned by their positions (forward);
+//   ardiff_rotary_backward  their gradients turned back (a rotation's transpose is the rotation by the negative angle);
+//   ardiff_rotary_append    queries turned, keys turned and written with their values into the slots of a paged cache.
+//
+// Token t turns pair i of every head by angle(t, i) = position[axis_i][t] * freq_i. The angle belongs to the token and the pair alone, so a
+// CTA works out cosine and sine of its tokens once, into shared memory, and uses them for all heads. A far position has an angle of
+// 10^5 turns and more, of which fp32 would keep no fraction; so turns are formed and reduced in fp64 (three operations a token and pair,
+// against 2 x 40 heads that use them) and only the fraction, at most half a turn, goes on in fp32. Rotations are fp32, rounded once.
+//
+// Bound by memory: every value is read once and written once. An item is a chunk of VEC pairs (two loads and two stores of up to 16 bytes),
+// or a chunk of VEC values that no pair covers. VEC is the widest that the alignment of rows, halves and pointers allows. Four items a
+// thread are under way at once.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "../../include/ardiff.h"
+#include "common.cuh"
+#include "launch.cuh"
+#include "rows.cuh"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kItems = 4;                        // items of a thread under way together
+
+// n / d for n * d < 2^32, by the number 2^32 / d rounded up (here n < 2^20, since a CTA has at most 2048 items or one token's, and d <= 1024)
+struct Divide {
+    uint32_t d, m;
+};
+Divide divide_by(uint32_t d) { return Divide{d, d > 1 ? (uint32_t)((((uint64_t)1 << 32) + d - 1) / d) : 0u}; }
+__device__ __forceinline__ uint32_t quotient(uint32_t n, Divide by) { return by.d > 1 ? __umulhi(n, by.m) : n; }
+
+struct Side {                                    // queries, keys or values: strides in values
+    const void* in;
+    void* out;
+    long long in_token, in_head, out_token, out_head;
+    int heads;
+};
+
+struct Rotary {
+    Side q, k, v;                                // v: copied, only with a cache
+    const int32_t* position;                     // [axes][n], rows position_ld apart
+    long long position_ld;
+    const float* freq;
+    const int32_t* axis;
+    const int64_t* slot;                         // the cache's: place of every token
+    const int32_t* count;
+    long long n, slots;
+    long long k_page, v_page;                    // strides of the cache's pages; out_token is that of tokens in a page
+    int page, axes, width, pairs, tokens;        // tokens: of a CTA
+    Divide by_chunks, by_copies, by_q, by_k, by_token;   // chunks of a row, of a value's row; heads; pairs
+    float sign;
+};
+
+template <typename T, int VEC> struct alignas(sizeof(T) * VEC) Chunk { T x[VEC]; };
+
+// With a cache, keys and values of token t go to page slot / page, place slot % page.
+template <typename T, int VEC, bool kNeighbours, bool kAppend>
+__global__ void __launch_bounds__(kThreads) rotary_kernel(const Rotary a) {
+    extern __shared__ char smem[];
+    float2* cs = reinterpret_cast<float2*>(smem);                                   // [tokens][pairs]
+    long long* k_at = reinterpret_cast<long long*>(cs + (size_t)a.tokens * a.pairs);    // [tokens], -1: not written
+    long long* v_at = k_at + a.tokens;
+    ardiff::begin_kernel();
+    const long long t0 = (long long)blockIdx.x * a.tokens;
+    long long n = a.n;
+    if (kAppend && a.count) n = min(n, (long long)*a.count);
+    const int tokens = (int)max(0ll, min((long long)a.tokens, n - t0));
+    if (tokens == 0) return;
+
+    for (uint32_t j = threadIdx.x; j < (uint32_t)(tokens * a.pairs); j += kThreads) {
+        const uint32_t t = quotient(j, a.by_token), i = j - t * a.pairs;
+        const int axis = a.axis ? a.axis[i] : 0;
+        float s = 0.f, c = 1.f;                  // a pair of no axis stands still
+        if (axis >= 0 && axis < a.axes) {
+            double turns = (double)a.position[axis * a.position_ld + t0 + t] * ((double)a.freq[i] * 0.15915494309189533577);
+            turns -= rint(turns);
+            sincospif(2.f * (float)turns, &s, &c);
+        }
+        cs[j] = make_float2(c, s * a.sign);
+    }
+    if (kAppend) {
+        for (int t = threadIdx.x; t < tokens; t += kThreads) {
+            const long long slot = a.slot[t0 + t];
+            long long k = -1, v = -1;
+            if (slot >= 0 && slot < a.slots) {
+                const long long pg = slot / a.page, in = slot - pg * a.page;
+                k = pg * a.k_page + in * a.k.out_token;
+                v = pg * a.v_page + in * a.v.out_token;
+            }
+            k_at[t] = k;
+            v_at[t] = v;
+        }
+    }
+    __syncthreads();
+
+    using C = Chunk<T, VEC>;
+    const uint32_t pair_chunks = a.pairs / VEC, chunks = a.by_chunks.d;             // chunks of a row of queries or keys
+    const uint32_t queries = tokens * a.q.heads * chunks, turned = queries + tokens * a.k.heads * chunks;
+    const uint32_t items = turned + (kAppend ? tokens * a.k.heads * a.by_copies.d : 0u);
+    for (uint32_t base = threadIdx.x; base < items; base += kThreads * kItems) {
+        C lo[kItems], hi[kItems];
+        T* to[kItems];
+        int32_t table[kItems];                   // place of the cosines of an item that turns; -1: copied
+#pragma unroll
+        for (int u = 0; u < kItems; ++u) {
+            const uint32_t item = base + u * kThreads;
+            to[u] = nullptr;
+            table[u] = -1;
+            if (item >= items) continue;
+            // all tokens' queries, then all tokens' keys, then, with a cache, all tokens' values
+            const bool is_q = item < queries, is_v = kAppend && item >= turned;
+            const uint32_t at = is_q ? item : is_v ? item - turned : item - queries;
+            uint32_t row = quotient(at, is_v ? a.by_copies : a.by_chunks);
+            const uint32_t c = at - row * (is_v ? a.by_copies.d : chunks);
+            const uint32_t t = quotient(row, is_q ? a.by_q : a.by_k);
+            row -= t * (is_q ? a.by_q.d : a.by_k.d);
+            const T* in = static_cast<const T*>(is_q ? a.q.in : is_v ? a.v.in : a.k.in) +
+                          (t0 + t) * (is_q ? a.q.in_token : is_v ? a.v.in_token : a.k.in_token) +
+                          (long long)row * (is_q ? a.q.in_head : is_v ? a.v.in_head : a.k.in_head);
+            T* out = static_cast<T*>(is_q ? a.q.out : is_v ? a.v.out : a.k.out) +
+                     (long long)row * (is_q ? a.q.out_head : is_v ? a.v.out_head : a.k.out_head);
+            if (kAppend && !is_q) {
+                const long long place = is_v ? v_at[t] : k_at[t];
+                if (place < 0) continue;
+                out += place;
+            } else {
+                out += (t0 + t) * (is_q ? a.q.out_token : a.k.out_token);
+            }
+            if (!is_v && c < pair_chunks) {
+                const int first = kNeighbours ? 2 * c * VEC : c * VEC;
+                lo[u] = *reinterpret_cast<const C*>(in + first);
+                hi[u] = *reinterpret_cast<const C*>(in + (kNeighbours ? first + VEC : first + a.pairs));
+                to[u] = out + first;
+                table[u] = t * a.pairs + c * VEC;
+            } else {
+                const int first = is_v ? c * VEC : 2 * a.pairs + (c - pair_chunks) * VEC;
+                lo[u] = *reinterpret_cast<const C*>(in + first);
+                to[u] = out + first;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kItems; ++u) {
+            if (!to[u]) continue;
+            if (table[u] >= 0) {
+                const float2* p = cs + table[u];
+                T v[2 * VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float2 w = p[e];
+                    T &a0 = kNeighbours ? (2 * e < VEC ? lo[u].x[2 * e < VEC ? 2 * e : 0] : hi[u].x[2 * e >= VEC ? 2 * e - VEC : 0]) : lo[u].x[e];
+                    T &b0 = kNeighbours ? (2 * e + 1 < VEC ? lo[u].x[2 * e + 1 < VEC ? 2 * e + 1 : 0] : hi[u].x[2 * e + 1 >= VEC ? 2 * e + 1 - VEC : 0]) : hi[u].x[e];
+                    const float x = ardiff::to_float(a0), y = ardiff::to_float(b0);
+                    v[2 * e] = ardiff::from_float<T>(x * w.x - y * w.y);
+                    v[2 * e + 1] = ardiff::from_float<T>(x * w.y + y * w.x);
+                }
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    lo[u].x[e] = kNeighbours ? v[e] : v[2 * e];
+                    hi[u].x[e] = kNeighbours ? v[VEC + e] : v[2 * e + 1];
+                }
+                *reinterpret_cast<C*>(to[u] + (kNeighbours ? VEC : a.pairs)) = hi[u];
+            }
+            *reinterpret_cast<C*>(to[u]) = lo[u];
+        }
+    }
+}
+
+template <typename T, int VEC> bool launch(const Rotary& a, bool neighbours, bool append, unsigned grid, size_t smem, cudaStream_t st) {
+    if (append) {
+        return neighbours ? ardiff::launch_early(rotary_kernel<T, VEC, true, true>, grid, kThreads, 1, smem, st, a)
+                          : ardiff::launch_early(rotary_kernel<T, VEC, false, true>, grid, kThreads, 1, smem, st, a);
+    }
+    return neighbours ? ardiff::launch_early(rotary_kernel<T, VEC, true, false>, grid, kThreads, 1, smem, st, a)
+                      : ardiff::launch_early(rotary_kernel<T, VEC, false, false>, grid, kThreads, 1, smem, st, a);
+}
+
+template <typename T> bool launch_type(const Rotary& a, int vec, bool neighbours, bool append, unsigned grid, size_t smem, cudaStream_t st) {
+    if (sizeof(T) == 2 && vec == 8) return launch<T, sizeof(T) == 2 ? 8 : 4>(a, neighbours, append, grid, smem, st);
+    if (vec >= 4) return launch<T, 4>(a, neighbours, append, grid, smem, st);
+    if (vec >= 2) return launch<T, 2>(a, neighbours, append, grid, smem, st);
+    return launch<T, 1>(a, neighbours, append, grid, smem, st);
+}
+
+// The strides and the pointer of rows, as far as their alignment goes: what a power of two that divides all of them divides.
+uint64_t places(const void* p, int size, long long token, long long head) {
+    return (uint64_t)reinterpret_cast<uintptr_t>(p) / size | (uint64_t)token | (uint64_t)head;
+}
+
+int rotary(Rotary& a, int32_t dtype, int32_t neighbours, bool append, cudaStream_t st) {
+    const int size = ardiff::value_size(dtype);
+    if (a.n < 0 || a.n >= (int64_t)1 << 31 || a.q.heads < 0 || a.k.heads < 0 || a.q.heads > ARDIFF_ROTARY_MAX_HEADS || a.k.heads > ARDIFF_ROTARY_MAX_HEADS || a.width < 1 ||
+        a.width > ARDIFF_ROTARY_MAX_WIDTH || a.pairs < 0 || 2 * a.pairs > a.width || a.axes < 1 || a.axes > 65535 || a.position_ld < 0)
+        return ARDIFF_ERR_SHAPE;
+    if (!size) return ARDIFF_ERR_UNSUPPORTED;
+    ardiff::set_launch_count(0);
+    if (a.n == 0 || (a.q.heads == 0 && a.k.heads == 0)) return ARDIFF_OK;
+    if (!a.position || (a.pairs > 0 && !a.freq) || (append && !a.slot)) return ARDIFF_ERR_NULL;
+    uint64_t bits = (uint64_t)a.width | (uint64_t)a.pairs;
+    const Side* sides[3] = {&a.q, &a.k, &a.v};
+    for (int i = 0; i < (append ? 3 : 2); ++i) {
+        const Side& s = *sides[i];
+        if (s.heads == 0) continue;
+        if (!s.in || !s.out) return ARDIFF_ERR_NULL;
+        if ((reinterpret_cast<uintptr_t>(s.in) | reinterpret_cast<uintptr_t>(s.out)) & (size - 1)) return ARDIFF_ERR_ALIGN;
+        bits |= places(s.in, size, s.in_token, s.heads > 1 ? s.in_head : 0) | places(s.out, size, s.out_token, s.heads > 1 ? s.out_head : 0);
+    }
+    if (append) bits |= (uint64_t)a.k_page | (uint64_t)a.v_page;
+    int vec = 16 / size;
+    while (vec > 1 && (bits & (vec - 1))) vec >>= 1;
+    const uint32_t chunks = a.pairs / vec + (a.width - 2 * a.pairs) / vec;
+    const long long copies = append ? (long long)a.k.heads * (a.width / vec) : 0;
+    const long long of_token = (long long)(a.q.heads + a.k.heads) * chunks + copies;
+    // About 2048 items a CTA: two rounds of its threads, so that loads of one are under way while the other computes; few tokens spread
+    // over as many CTAs as there are.
+    long long tokens = 2048 / of_token;
+    if (tokens > a.n / 296) tokens = a.n / 296;
+    a.tokens = (int)(tokens < 1 ? 1 : tokens > 16 ? 16 : tokens);
+    a.by_chunks = divide_by(chunks);
+    a.by_q = divide_by(a.q.heads > 0 ? a.q.heads : 1);
+    a.by_k = divide_by(a.k.heads > 0 ? a.k.heads : 1);
+    a.by_copies = divide_by((uint32_t)(a.width / vec));
+    a.by_token = divide_by(a.pairs > 0 ? a.pairs : 1);
+    const size_t smem = (size_t)a.tokens * (a.pairs * sizeof(float2) + 16);
+    const unsigned grid = (unsigned)((a.n + a.tokens - 1) / a.tokens);
+    const bool ok = dtype == ARDIFF_F32 ? launch_type<float>(a, vec, neighbours != 0, append, grid, smem, st)
+                  : dtype == ARDIFF_F16 ? launch_type<__half>(a, vec, neighbours != 0, append, grid, smem, st)
+                                        : launch_type<__nv_bfloat16>(a, vec, neighbours != 0, append, grid, smem, st);
+    ardiff::set_launch_count(1);
+    return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+}
+
+Rotary arguments(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head, int32_t q_heads,
+                 const void* k, int64_t k_token, int64_t k_head, int32_t k_heads, int64_t n, int32_t width, const int32_t* position,
+                 int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs) {
+    Rotary a;
+    memset(&a, 0, sizeof(a));
+    a.q = Side{q, q_out, q_token, q_head, q_out_token, q_out_head, q_heads};
+    a.k.in = k; a.k.in_token = k_token; a.k.in_head = k_head; a.k.heads = k_heads;
+    a.n = n; a.width = width; a.position = position; a.position_ld = position_ld; a.axes = axes; a.freq = freq; a.axis = axis;
+    a.pairs = pairs; a.sign = 1.f;
+    return a;
+}
+
+}  // namespace
+
+extern "C" int ardiff_rotary(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head,
+                             int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, void* k_out, int64_t k_out_token,
+                             int64_t k_out_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width, const int32_t* position,
+                             int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs,
+                             int32_t neighbours, void* stream) {
+    Rotary a = arguments(q, q_token, q_head, q_out, q_out_token, q_out_head, q_heads, k, k_token, k_head, k_heads, n, width, position,
+                         position_ld, axes, freq, axis, pairs);
+    a.k.out = k_out; a.k.out_token = k_out_token; a.k.out_head = k_out_head;
+    return rotary(a, dtype, neighbours, false, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int ardiff_rotary_backward(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token,
+                                      int64_t q_out_head, int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, void* k_out,
+                                      int64_t k_out_token, int64_t k_out_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width,
+                                      const int32_t* position, int64_t position_ld, int32_t axes, const float* freq,
+                                      const int32_t* axis, int32_t pairs, int32_t neighbours, void* stream) {
+    Rotary a = arguments(q, q_token, q_head, q_out, q_out_token, q_out_head, q_heads, k, k_token, k_head, k_heads, n, width, position,
+                         position_ld, axes, freq, axis, pairs);
+    a.k.out = k_out; a.k.out_token = k_out_token; a.k.out_head = k_out_head;
+    a.sign = -1.f;
+    return rotary(a, dtype, neighbours, false, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int ardiff_rotary_append(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token,
+                                    int64_t q_out_head, int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                                    int64_t v_token, int64_t v_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width,
+                                    const int32_t* position, int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis,
+                                    int32_t pairs, int32_t neighbours, const int64_t* slot, const int32_t* count, void* k_cache,
+                                    int64_t k_cache_page, int64_t k_cache_token, int64_t k_cache_head, void* v_cache,
+                                    int64_t v_cache_page, int64_t v_cache_token, int64_t v_cache_head, int32_t pages, int32_t page,
+                                    void* stream) {
+    if (pages < 0 || page < 1) return ARDIFF_ERR_SHAPE;
+    Rotary a = arguments(q, q_token, q_head, q_out, q_out_token, q_out_head, q_heads, k, k_token, k_head, k_heads, n, width, position,
+                         position_ld, axes, freq, axis, pairs);
+    a.k.out = k_cache; a.k.out_token = k_cache_token; a.k.out_head = k_cache_head; a.k_page = k_cache_page;
+    a.v = Side{v, v_cache, v_token, v_head, v_cache_token, v_cache_head, k_heads};
+    a.v_page = v_cache_page;
+    a.slot = slot; a.count = count; a.page = page; a.slots = (long long)pages * page;
+    return rotary(a, dtype, neighbours, true, static_cast<cudaStream_t>(stream));
+}

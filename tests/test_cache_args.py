@@ -1,0 +1,127 @@
+"""Refusals of the operators around a draft model's cache: every one is made before anything is launched, so they need no GPU."""
+import math
+
+import pytest
+
+import paper_2512_08537_b200 as ardiff
+
+NULL, SHAPE, ALIGN, UNSUPPORTED = (ardiff.ARDIFF_ERR_NULL, ardiff.ARDIFF_ERR_SHAPE, ardiff.ARDIFF_ERR_ALIGN,
+                                   ardiff.ARDIFF_ERR_UNSUPPORTED)
+P = 4096                                   # an address that nothing is read from
+BIG = 1 << 40
+
+
+def call(name, defaults, kw):
+    assert set(kw) <= set(defaults), kw
+    return getattr(ardiff.lib(), name)(*{**defaults, **kw}.values())
+
+
+def turn(**kw):
+    return dict(q=P, q_token=512, q_head=64, q_out=P, q_out_token=512, q_out_head=64, q_heads=8, k=P, k_token=128, k_head=64, k_out=P,
+                k_out_token=128, k_out_head=64, k_heads=2, dtype=ardiff.ARDIFF_BF16, n=4, width=64, position=P, position_ld=4, axes=1, freq=P, axis=None,
+                pairs=32, neighbours=0, stream=None)
+
+
+ROTARY = [(dict(n=-1), SHAPE), (dict(n=1 << 31), SHAPE), (dict(width=0), SHAPE), (dict(width=513), SHAPE), (dict(pairs=33), SHAPE), (dict(pairs=-1), SHAPE),
+          (dict(axes=0), SHAPE), (dict(q_heads=-1), SHAPE), (dict(q_heads=1025), SHAPE), (dict(k_heads=1025), SHAPE), (dict(dtype=3), UNSUPPORTED),
+          (dict(dtype=-1), UNSUPPORTED), (dict(q=None), NULL), (dict(k=None), NULL), (dict(q_out=None), NULL), (dict(position=None), NULL), (dict(freq=None), NULL),
+          (dict(q=P + 1), ALIGN), (dict(q_out=P + 1), ALIGN), (dict(position_ld=-1), SHAPE)]
+
+
+@pytest.mark.parametrize("name", ["ardiff_rotary", "ardiff_rotary_backward"])
+@pytest.mark.parametrize("kw,code", ROTARY + [(dict(k_out=None), NULL), (dict(dtype=ardiff.ARDIFF_F32, k=P + 2), ALIGN)])
+def test_rotary_refuses(name, kw, code):
+    assert call(name, turn(), kw) == code
+
+
+@pytest.mark.parametrize("name", ["ardiff_rotary", "ardiff_rotary_backward"])
+def test_rotary_of_nothing(name):
+    assert call(name, turn(), dict(n=0, q=None, k=None)) == 0
+    assert call(name, turn(), dict(q_heads=0, k_heads=0, q=None, k=None)) == 0
+
+
+def append():
+    return dict(q=P, q_token=512, q_head=64, q_out=P, q_out_token=512, q_out_head=64, q_heads=8, k=P, k_token=128, k_head=64, v=P, v_token=128, v_head=64,
+                k_heads=2, dtype=ardiff.ARDIFF_BF16, n=4, width=64, position=P, position_ld=4, axes=1, freq=P, axis=None, pairs=32, neighbours=0, slot=P,
+                count=None, k_cache=P, k_cache_page=2048, k_cache_token=128, k_cache_head=64, v_cache=P, v_cache_page=2048, v_cache_token=128,
+                v_cache_head=64, pages=4, page=16, stream=None)
+
+
+@pytest.mark.parametrize("kw,code", ROTARY + [(dict(slot=None), NULL), (dict(v=None), NULL), (dict(k_cache=None), NULL), (dict(v_cache=None), NULL),
+                                              (dict(page=0), SHAPE), (dict(pages=-1), SHAPE), (dict(v_cache=P + 1), ALIGN)])
+def test_rotary_append_refuses(kw, code):
+    assert call("ardiff_rotary_append", append(), kw) == code
+
+
+CACHE = dict(k_cache=P, k_page=2048, k_token=128, k_head=64)
+
+
+def attend():
+    return dict(q=P, q_token=512, q_head=64, q_heads=8, tokens=4, dtype=ardiff.ARDIFF_BF16, **CACHE, v_cache=P, v_page=2048, v_token=128, v_head=64, pages=4,
+                page=16, heads=2, head_width=64, table=P, width=4, requests=2, length=P, offset=P, groups=1, group=P, shared=P, most=1, scale=0.125, causal=1,
+                out=P, out_token=512, out_head=64, lse=P, lse_token=8, status=P, workspace=P, workspace_bytes=BIG, stream=None)
+
+
+ATTEND = [(dict(requests=-1), SHAPE), (dict(requests=(1 << 20) + 1), SHAPE), (dict(tokens=-1), SHAPE), (dict(tokens=1 << 28), SHAPE), (dict(heads=0), SHAPE),
+          (dict(q_heads=9), SHAPE), (dict(q_heads=1), SHAPE), (dict(q_heads=2048), SHAPE), (dict(pages=-1), SHAPE), (dict(page=0), SHAPE), (dict(width=-1), SHAPE),
+          (dict(page=1 << 16, width=1 << 15), SHAPE), (dict(most=-1), SHAPE), (dict(scale=math.inf), SHAPE), (dict(scale=math.nan), SHAPE),
+          (dict(dtype=ardiff.ARDIFF_F32), UNSUPPORTED), (dict(dtype=7), UNSUPPORTED), (dict(head_width=72), UNSUPPORTED), (dict(head_width=256), UNSUPPORTED),
+          (dict(workspace_bytes=8), SHAPE), (dict(workspace_bytes=0), SHAPE), (dict(k_token=124), ALIGN), (dict(k_head=4), ALIGN), (dict(k_page=1), ALIGN),
+          (dict(q_token=513), ALIGN), (dict(q_head=68), ALIGN), (dict(q=P + 8), ALIGN), (dict(k_cache=P + 8), ALIGN), (dict(workspace=P + 8), ALIGN)] + \
+    [(dict([(name, None)]), NULL) for name in ("q", "k_cache", "table", "length", "offset", "lse", "status", "workspace")]
+
+
+@pytest.mark.parametrize("kw,code", ATTEND + [(dict(groups=-1), SHAPE), (dict(groups=(1 << 20) + 1), SHAPE), (dict(v_token=4), ALIGN), (dict(out_token=4), ALIGN),
+                                              (dict(out_head=1), ALIGN), (dict(out=P + 2), ALIGN), (dict(v_cache=P + 2), ALIGN)] +
+                         [(dict([(name, None)]), NULL) for name in ("v_cache", "out", "group", "shared")])
+def test_attend_refuses(kw, code):
+    assert call("ardiff_attend_pages", attend(), kw) == code
+
+
+def weights():
+    return dict(q=P, q_token=512, q_head=64, q_heads=8, tokens=4, dtype=ardiff.ARDIFF_BF16, **CACHE, pages=4, page=16, heads=2, head_width=64, table=P, width=4,
+                requests=2, length=P, offset=P, first=None, lse=P, lse_token=8, score=P, ld=64, most=1, scale=0.125, decay=1.0, causal=1, new_score=P, new_ld=64,
+                status=P, workspace=P, workspace_bytes=BIG, stream=None)
+
+
+@pytest.mark.parametrize("kw,code", ATTEND + [(dict(decay=math.nan), SHAPE), (dict(decay=math.inf), SHAPE), (dict(ld=-1), SHAPE), (dict(new_ld=-1), SHAPE),
+                                              (dict(score=None), NULL), (dict(new_score=None), NULL)])
+def test_weights_refuse(kw, code):
+    assert call("ardiff_attend_weights", weights(), kw) == code
+
+
+def evict():
+    return dict(requests=2, length=P, budget=P, first=None, score=P, ld=64, position=None, seen=None, recent=0, table=P, width=4, dtype=ardiff.ARDIFF_F16,
+                **CACHE, v_cache=P, v_page=2048, v_token=128, v_head=64, pages=4, page=16, heads=2, head_width=64, new_length=P, new_score=P, new_position=None,
+                source=None, new_ld=64, status=P, workspace=P, workspace_bytes=BIG, stream=None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(requests=-1), SHAPE), (dict(requests=(1 << 20) + 1), SHAPE), (dict(page=0), SHAPE), (dict(width=-1), SHAPE), (dict(page=1 << 16, width=1 << 15), SHAPE),
+    (dict(pages=-1), SHAPE), (dict(heads=0), SHAPE), (dict(head_width=0), SHAPE), (dict(head_width=1 << 20), SHAPE), (dict(recent=-1), SHAPE), (dict(ld=-1), SHAPE),
+    (dict(new_ld=-1), SHAPE), (dict(dtype=5), UNSUPPORTED), (dict(head_width=4), UNSUPPORTED), (dict(k_token=4), ALIGN), (dict(v_head=12), ALIGN),
+    (dict(k_cache=P + 8), ALIGN), (dict(workspace=P + 4), ALIGN), (dict(workspace_bytes=16), SHAPE)] +
+    [(dict([(name, None)]), NULL) for name in ("length", "budget", "score", "table", "k_cache", "v_cache", "new_length", "new_score", "status", "workspace")])
+def test_evict_refuses(kw, code):
+    assert call("ardiff_pages_evict", evict(), kw) == code
+
+
+def test_workspaces():
+    L = ardiff.lib()
+    assert L.ardiff_attend_workspace(-1, 0, 1, 1, 1, 64) == SHAPE and L.ardiff_attend_workspace(1, 0, 1, 3, 2, 64) == SHAPE
+    assert L.ardiff_attend_workspace(1, 0, 1 << 31, 8, 1, 64) == SHAPE and L.ardiff_pages_evict_workspace(4, 16, -1) == SHAPE
+    assert L.ardiff_attend_weights_workspace(-1) == SHAPE
+    small, large = L.ardiff_attend_workspace(1, 0, 1, 8, 2, 64), L.ardiff_attend_workspace(500, 3, 4000, 8, 2, 64)
+    assert 0 < small < large
+    assert L.ardiff_pages_evict_workspace(3, 16, 5) > 0 and L.ardiff_attend_weights_workspace(3) >= 32
+
+
+def test_what_32_bits_do_not_hold_is_refused_before_the_call():
+    """The binding checks what ctypes would cut off (tensors without memory of their own stand in for the sizes)."""
+    import torch
+    with pytest.raises(AssertionError):
+        ardiff.ardiff_attend_pages(torch.zeros(1, 1, 64), torch.zeros(1, 1, 1, 64), torch.zeros(1, 1, 1, 64), torch.zeros((1, 1), dtype=torch.int32),
+                                   torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), most=1 << 32)
+    with pytest.raises(AssertionError):
+        ardiff.ardiff_pages_evict(torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1), torch.zeros((1, 1), dtype=torch.int32),
+                                  torch.zeros(1, 1, 1, 64), torch.zeros(1, 1, 1, 64), recent=1 << 33)
