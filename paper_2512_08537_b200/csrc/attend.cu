@@ -28,28 +28,18 @@ namespace {
 
 using namespace ardiff;
 
-constexpr int kBlockRows = 64;
-constexpr int kTileKeys = 64;
-constexpr int kMaxCtas = 512;                    // CTAs that have a place for pieces
+constexpr int kMaxCtas = 512, kMaxWideCtas = 256;    // CTAs that have a place for pieces
 constexpr int kPlanThreads = 1024;
 // Fewer shared tokens are read by every request itself: a block of its own and the pieces to join cost more than they take.
 constexpr int kLeastShared = 64;
 
-struct Call {
-    Pages cache;
-    Queries x;
-    Plan plan;
-    Pieces pieces;
-    const int32_t* length;
-    const int32_t* offset;
-    const int32_t* group;
-    const int32_t* shared;
-    int32_t* status;
-    float scale;                                 // times log2 e
-    int requests, groups, causal;
-};
-
 // ---- the plan -----------------------------------------------------------------------------------
+// Blocks of a segment: of which list, how many.
+__device__ __forceinline__ bool is_wide(long long rows) { return rows > kNarrowRows; }
+__device__ __forceinline__ int blocks_of(long long rows) {
+    return (int)(is_wide(rows) ? (rows + kWideRows - 1) / kWideRows : (rows + kNarrowRows - 1) / kNarrowRows);
+}
+
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
     __shared__ long long s_scan[32];
     ardiff::begin_kernel();
@@ -59,8 +49,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
     for (int r = tid; r < R; r += kPlanThreads) {
         const int a = c.offset[r], b = c.offset[r + 1], len = c.length[r];
         bad |= a < 0 || b < a || b > c.x.tokens || len < 0 || len > limit;
-        c.plan.shared[r] = 0;
-        c.plan.share[r] = Share{-1, 0};
+        c.plan.share[r] = Share{-1, 0, 0, 0, 0, r, 0, 0};
     }
     for (int g = tid; g < c.groups; g += kPlanThreads) {
         const int a = c.group[g], b = c.group[g + 1];
@@ -69,193 +58,174 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
     bad = __syncthreads_or(bad);
     if (tid == 0) *c.status = bad ? ARDIFF_ERR_SHAPE : ARDIFF_OK;
     if (bad) {
-        if (tid == 0) { c.plan.head->steps = 0; c.plan.head->blocks = 0; c.plan.head->own = 0; }
+        if (tid < 2) *(tid ? c.plan.wide : c.plan.narrow).head = PlanHead{0, 0, 0, 0};
         return;
     }
-    // the tokens that all queries of a group see; nothing is gained where one request has queries
+    // The tokens that all queries of a group see are found through its first row of the table, and read once for all, unless
+    // one request has queries, or all have so many that each fills its blocks of rows: then the same work is done, and there are no pieces to join.
     for (int g = tid >> 5; g < c.groups; g += kPlanThreads / 32) {
         const int r0 = c.group[g], r1 = c.group[g + 1];
-        int least = c.shared[g], active = 0;
+        int least = c.shared[g], active = 0, fewest = 0x7fffffff;
         for (int r = r0 + lane; r < r1; r += 32) {
             const int n = c.offset[r + 1] - c.offset[r];
             if (n == 0) continue;
             ++active;
+            fewest = min(fewest, n);
             least = min(least, max(0, c.causal ? c.length[r] - n + 1 : c.length[r]));
         }
         least = __reduce_min_sync(0xffffffffu, least);
+        fewest = __reduce_min_sync(0xffffffffu, fewest);
         active = __reduce_add_sync(0xffffffffu, active);
-        if (active < 2 || least < kLeastShared) least = 0;
-        for (int r = r0 + lane; r < r1; r += 32) c.plan.shared[r] = least;
+        const bool once = active > 1 && least >= kLeastShared && (long long)fewest * G < kWideRows;
+        for (int r = r0 + lane; r < r1; r += 32) c.plan.share[r] = Share{-1, 0, 0, once ? least : 0, least, r0, 0, 0};
     }
     __syncthreads();
 
-    long long blocks = 0;
+    long long blocks[2] = {0, 0};                // narrow, wide
     // shared tokens: blocks of the group's rows
     for (int g0 = 0; g0 < c.groups; g0 += kPlanThreads) {
         const int g = g0 + tid;
-        int n = 0, r0 = 0, r1 = 0, keys = 0, token0 = 0;
+        int n = 0, r0 = 0, keys = 0, token0 = 0;
         long long rows = 0;
         if (g < c.groups) {
-            r0 = c.group[g]; r1 = c.group[g + 1];
+            r0 = c.group[g];
+            const int r1 = c.group[g + 1];
             if (r1 > r0) {
-                keys = c.plan.shared[r0];
+                keys = c.plan.share[r0].shared;
                 token0 = c.offset[r0];
                 rows = keys > 0 ? (long long)(c.offset[r1] - token0) * G : 0;
             }
-            n = (int)((rows + kBlockRows - 1) / kBlockRows);
+            n = blocks_of(rows);
         }
+        const bool wide = is_wide(rows);
         long long total;
-        const long long at = blocks + cta_scan(n, s_scan, &total);
+        const long long packed = cta_scan((long long)(wide ? 0 : n) << 32 | (wide ? n : 0), s_scan, &total);
+        const long long at = wide ? blocks[1] + (int)packed : blocks[0] + (packed >> 32);
+        const int per = wide ? kWideRows : kNarrowRows;
         for (int j = 0; j < n; ++j) {
             Block b;
-            b.token0 = token0; b.row0 = j * kBlockRows; b.rows = (int)min((long long)kBlockRows, rows - b.row0);
-            b.request = r0; b.key0 = 0; b.keys = keys; b.limit = keys; b.step = 0;
-            c.plan.block[at + j] = b;
+            b.token0 = token0; b.row0 = j * per; b.rows = (int)min((long long)per, rows - b.row0);
+            b.request = r0; b.key0 = 0; b.keys = keys; b.limit = keys; b.step = 0; b.split = 0; b.front = r0; b.pad0 = b.pad1 = 0;
+            (wide ? c.plan.wide : c.plan.narrow).block[at + j] = b;
         }
-        if (n > 0) c.plan.share[r0].prefix = (int)at;
-        blocks += total;
+        if (n > 0) { c.plan.share[r0].prefix = (int)at; c.plan.share[r0].wide = wide; }
+        blocks[0] += total >> 32;
+        blocks[1] += (int)total;
     }
+    const int own[2] = {(int)blocks[0], (int)blocks[1]};
     __syncthreads();
     for (int g = tid >> 5; g < c.groups; g += kPlanThreads / 32) {
         const int r0 = c.group[g], r1 = c.group[g + 1];
         if (r0 == r1) continue;
-        const int prefix = c.plan.share[r0].prefix, token0 = c.offset[r0];
+        const Share first = c.plan.share[r0];
+        const int token0 = c.offset[r0];
         __syncwarp();
-        for (int r = r0 + lane; r < r1 && prefix >= 0; r += 32) c.plan.share[r] = Share{prefix, (c.offset[r] - token0) * G};
+        for (int r = r0 + lane; r < r1 && first.prefix >= 0; r += 32) {
+            Share s = first;
+            s.row0 = (c.offset[r] - token0) * G;
+            c.plan.share[r] = s;
+        }
     }
-    const long long own = blocks;
+    __syncthreads();
     for (int first = 0; first < R; first += kPlanThreads) {
         const int r = first + tid;
-        int n = 0, token0 = 0, keys0 = 0, len = 0, news = 0;
+        int n = 0, token0 = 0, len = 0, news = 0;
         long long rows = 0;
+        Share share{-1, 0, 0, 0, 0, 0, 0, 0};
         if (r < R) {
             token0 = c.offset[r];
             news = c.offset[r + 1] - token0;
             len = c.length[r];
-            keys0 = c.plan.shared[r];
+            share = c.plan.share[r];
             rows = (long long)news * G;
-            n = (int)((rows + kBlockRows - 1) / kBlockRows);
+            n = blocks_of(rows);
         }
+        const bool wide = is_wide(rows);
         long long total;
-        const long long at = blocks + cta_scan(n, s_scan, &total);
+        const long long packed = cta_scan((long long)(wide ? 0 : n) << 32 | (wide ? n : 0), s_scan, &total);
+        const long long at = wide ? blocks[1] + (int)packed : blocks[0] + (packed >> 32);
+        const int per = wide ? kWideRows : kNarrowRows;
         for (int j = 0; j < n; ++j) {
             Block b;
-            b.token0 = token0; b.row0 = j * kBlockRows; b.rows = (int)min((long long)kBlockRows, rows - b.row0);
-            b.request = r; b.key0 = keys0;
+            b.token0 = token0; b.row0 = j * per; b.rows = (int)min((long long)per, rows - b.row0);
+            b.request = r; b.key0 = share.shared; b.split = share.split; b.front = share.front; b.pad0 = b.pad1 = 0;
             b.step = c.causal ? 1 : 0;
             b.limit = c.causal ? len - news + 1 : len;
             const int last = min(len, b.limit + b.step * ((b.row0 + b.rows - 1) / G));
-            b.keys = max(0, last - keys0);
-            c.plan.block[at + j] = b;
+            b.keys = max(0, last - b.key0);
+            (wide ? c.plan.wide : c.plan.narrow).block[at + j] = b;
         }
-        blocks += total;
+        blocks[0] += total >> 32;
+        blocks[1] += (int)total;
     }
     __syncthreads();
-    long long steps = 0, rows = 0;
-    for (int first = 0; first < blocks; first += kPlanThreads) {
-        const int b = first + tid;
-        long long s = 0, w = 0;
-        if (b < blocks) {
-            s = (long long)((c.plan.block[b].keys + kTileKeys - 1) / kTileKeys) * c.cache.heads;
-            w = c.plan.block[b].rows;
+    long long before = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const List& l = i ? c.plan.wide : c.plan.narrow;
+        const int keys = i ? kWideKeys : kNarrowKeys;
+        long long steps = 0, rows = 0;
+        for (int first = 0; first < blocks[i]; first += kPlanThreads) {
+            const int b = first + tid;
+            long long s = 0, w = 0;
+            if (b < blocks[i]) {
+                s = (long long)((l.block[b].keys + keys - 1) / keys) * c.cache.heads;
+                w = l.block[b].rows;
+            }
+            long long total;
+            const long long at = steps + cta_scan(s, s_scan, &total);
+            steps += total;
+            const long long rows_at = rows + cta_scan(w, s_scan, &total);
+            rows += total;
+            if (b < blocks[i]) { l.steps[b] = at; l.rows[b] = rows_at; }
         }
-        long long total;
-        const long long at = steps + cta_scan(s, s_scan, &total);
-        steps += total;
-        const long long rows_at = rows + cta_scan(w, s_scan, &total);
-        rows += total;
-        if (b < blocks) { c.plan.steps[b] = at; c.plan.rows[b] = rows_at; }
-    }
-    if (tid == 0) {
-        c.plan.steps[blocks] = steps;
-        c.plan.rows[blocks] = rows;
-        c.plan.head->steps = steps;
-        c.plan.head->blocks = (int)blocks;
-        c.plan.head->own = (int)own;
+        if (tid == 0) {
+            l.steps[blocks[i]] = steps;
+            l.rows[blocks[i]] = rows;
+            *l.head = PlanHead{steps, before, (int)blocks[i], own[i]};
+        }
+        before = rows;
     }
 }
-
-// The steps of a CTA: the same number for all but the last ones.
-__device__ __forceinline__ long long steps_each(long long steps, int ctas) { return max(1ll, (steps + ctas - 1) / ctas); }
 
 // ---- up to 64 query rows ------------------------------------------------------------------------
 constexpr int kThreads = 128;
 constexpr int kStages = 3;
 
-template <int D> constexpr int kTileBytes = kTileKeys * kPitch<D>;
-template <int D> constexpr int kNarrowShared = kStages * 2 * kTileBytes<D> + 16 * D * 4 + kStages * kTileKeys * 16 + 4 * 16 * 8;
-
-// Where a CTA is in the line of steps: block, head, tile of keys.
-struct Cursor {
-    int b, h, tile, tiles;
-    Block at;
-    __device__ __forceinline__ void enter(const Plan& p) {
-        at = p.block[b];
-        tiles = (at.keys + kTileKeys - 1) / kTileKeys;
-    }
-    // (only called while there is a next step)
-    __device__ __forceinline__ void next(const Plan& p, int heads) {
-        if (++tile < tiles) return;
-        tile = 0;
-        if (++h < heads) return;
-        h = 0;
-        do {
-            ++b;
-            enter(p);
-        } while (tiles == 0);
-    }
-};
+template <int D> constexpr int kTileBytes = kNarrowKeys * kPitch<D>;
+template <int D> constexpr int kNarrowShared = kStages * 2 * kTileBytes<D> + 16 * D * 4 + kStages * kNarrowKeys * 16 + 4 * 16 * 8;
 
 // Four warps. Those that share 16 query rows (all four where the block has up to 16 rows, two up to 32) take turns at groups of 16 keys, each
 // with a running maximum, sum and weighted values of its own, joined in shared memory when the unit ends. Keys and values come by asynchronous copies,
 // two tiles ahead, through offsets that are looked up in the table a step before that.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 2) narrow_kernel(const Call c, int ctas) {
+__global__ void __launch_bounds__(kThreads, 2) narrow_kernel(const Call c) {
     extern __shared__ __align__(128) char smem[];
     char* tiles = smem;
     float* joined = reinterpret_cast<float*>(smem + kStages * 2 * kTileBytes<D>);
     longlong2* place = reinterpret_cast<longlong2*>(joined + 16 * D);                // [stages][keys]
-    float2* part = reinterpret_cast<float2*>(place + kStages * kTileKeys);           // [warps][16]
+    float2* part = reinterpret_cast<float2*>(place + kStages * kNarrowKeys);           // [warps][16]
     ardiff::begin_kernel();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const long long steps = c.plan.head->steps, each = steps_each(steps, ctas);
+    const List& list = c.plan.narrow;
+    const long long steps = list.head->steps, each = steps_each(steps, list.ctas);
     const long long begin = each * blockIdx.x;
     if (begin >= steps) return;
-    const int n = (int)(min(steps, begin + each) - begin);
-    const int blocks = c.plan.head->blocks;
+    const int n = (int)(min(steps, begin + each) - begin), own = list.head->own;
     const uint32_t tiles_at = ptx::smem_u32(tiles);
 
-    Cursor now;
-    now.b = find_last(c.plan.steps, blocks, begin);
-    now.enter(c.plan);
-    {
-        const long long in = begin - c.plan.steps[now.b];
-        now.h = (int)(in / now.tiles);
-        now.tile = (int)(in - (long long)now.h * now.tiles);
-    }
-    Cursor load = now;                           // the step whose places are looked up next
+    Cursor<false> now;
+    now.start(c, find_last(list.steps, list.head->blocks, begin), begin);
+    Cursor<false> load = now;                    // the step whose places are looked up next
 
-    // the offsets of key `j` of the step at `load`, -1 for none
-    auto look_up = [&](int j) -> longlong2 {
-        const int in = load.tile * kTileKeys + j;
-        if (in >= load.at.keys) return make_longlong2(-1, -1);
-        const unsigned key = load.at.key0 + in, pg = key / (unsigned)c.cache.page, row = key - pg * c.cache.page;
-        const int id = c.cache.table[(long long)load.at.request * c.cache.width + pg];
-        if (id < 0 || id >= c.cache.pages) {
-            *c.status = ARDIFF_ERR_SHAPE;
-            return make_longlong2(-1, -1);
-        }
-        return make_longlong2(id * c.cache.k_page + row * c.cache.k_token + load.h * c.cache.k_head,
-                              id * c.cache.v_page + row * c.cache.v_token + load.h * c.cache.v_head);
-    };
     auto fetch = [&](int step) {
         if (step < n) {
             const int stage = step % kStages;
             const uint32_t k_to = tiles_at + stage * 2 * kTileBytes<D>, v_to = k_to + kTileBytes<D>;
             constexpr int kChunks = D / 8;
-            for (int i = tid; i < kTileKeys * kChunks; i += kThreads) {
+            for (int i = tid; i < kNarrowKeys * kChunks; i += kThreads) {
                 const int row = i / kChunks, ch = i - row * kChunks;
-                const longlong2 p = place[stage * kTileKeys + row];
+                const longlong2 p = place[stage * kNarrowKeys + row];
                 cp_async16(k_to + chunk_at<D>(row, ch), c.cache.k + (p.x < 0 ? 0 : p.x + ch * 16), p.x < 0 ? 0 : 16);
                 cp_async16(v_to + chunk_at<D>(row, ch), c.cache.v + (p.x < 0 ? 0 : p.y + ch * 16), p.x < 0 ? 0 : 16);
             }
@@ -265,8 +235,8 @@ __global__ void __launch_bounds__(kThreads, 2) narrow_kernel(const Call c, int c
 
     // places of the first three steps, copies of the first two
     for (int s = 0; s < kStages && s < n; ++s) {
-        if (tid < kTileKeys) place[s * kTileKeys + tid] = look_up(tid);
-        if (s + 1 < n) load.next(c.plan, c.cache.heads);
+        if (tid < kNarrowKeys) place[s * kNarrowKeys + tid] = place_of<false>(c, load, tid);
+        if (s + 1 < n) load.next(c);
     }
     __syncthreads();
     for (int s = 0; s < kStages - 1; ++s) fetch(s);
@@ -316,12 +286,12 @@ __global__ void __launch_bounds__(kThreads, 2) narrow_kernel(const Call c, int c
         fetch(i + kStages - 1);
         const int ahead = i + kStages;
         longlong2 found;
-        if (ahead < n && tid < kTileKeys) found = look_up(tid);
+        if (ahead < n && tid < kNarrowKeys) found = place_of<false>(c, load, tid);
 
         const uint32_t k_tile = tiles_at + (i % kStages) * 2 * kTileBytes<D>, v_tile = k_tile + kTileBytes<D>;
-        const int left = now.at.keys - now.tile * kTileKeys;
-        const int key0 = now.at.key0 + now.tile * kTileKeys;
-        for (int g = wk; g < kTileKeys / 16 && g * 16 < left; g += groups_k) {
+        const int left = now.at.keys - now.tile * kNarrowKeys;
+        const int key0 = now.at.key0 + now.tile * kNarrowKeys;
+        for (int g = wk; g < kNarrowKeys / 16 && g * 16 < left; g += groups_k) {
             float s[2][4];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -416,8 +386,8 @@ __global__ void __launch_bounds__(kThreads, 2) narrow_kernel(const Call c, int c
                 mma_16816(o[j + 1], p, b[2], b[3], T());
             }
         }
-        if (ahead < n && tid < kTileKeys) place[(ahead % kStages) * kTileKeys + tid] = found;
-        if (ahead + 1 < n) load.next(c.plan, c.cache.heads);
+        if (ahead < n && tid < kNarrowKeys) place[(ahead % kStages) * kNarrowKeys + tid] = found;
+        if (ahead + 1 < n) load.next(c);
 
         const bool ends = now.tile + 1 == now.tiles;
         if (ends || i + 1 == n) {
@@ -475,10 +445,9 @@ __global__ void __launch_bounds__(kThreads, 2) narrow_kernel(const Call c, int c
                 }
             }
             if (wk == groups_k - 1) {
-                const long long unit_begin = c.plan.steps[now.b] + (long long)now.h * now.tiles;   // among all steps
-                const bool direct = whole && ends && now.b >= c.plan.head->own && c.plan.share[b.request].prefix < 0;
-                const int first_cta = (int)(unit_begin / each);
-                const long long at = direct ? 0 : piece_row(c.pieces, c.plan.rows[now.b], c.cache.heads, b.rows, now.h, blockIdx.x, first_cta, kBlockRows);
+                const long long unit = list.steps[now.b] + (long long)now.h * now.tiles;       // its first step
+                const bool direct = whole && ends && now.b >= own && c.plan.share[b.request].prefix < 0;
+                const long long at = direct ? 0 : piece_row<false>(c, now.b, b, now.h, blockIdx.x, (int)(unit / each));
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const int in = wm * 16 + row8 + 8 * u;
@@ -503,121 +472,147 @@ __global__ void __launch_bounds__(kThreads, 2) narrow_kernel(const Call c, int c
             fresh = true;
             whole = true;
         }
-        if (i + 1 < n) now.next(c.plan, c.cache.heads);
+        if (i + 1 < n) now.next(c);
     }
     cp_async_wait<0>();
 }
 
 // ---- pieces -------------------------------------------------------------------------------------
+// The pieces of a unit: of CTAs first .. first + count - 1.
+struct Cut {
+    int first, count;
+};
+template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, int b, const Block& k, int h) {
+    const List& l = list_of<kWide>(c);
+    const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
+    if (tiles == 0) return Cut{0, 0};
+    const long long each = steps_each(l.head->steps, l.ctas), s0 = l.steps[b] + (long long)h * tiles;
+    const int first = (int)(s0 / each);
+    return Cut{first, (int)((s0 + tiles - 1) / each) - first + 1};
+}
+
 // A CTA a unit of the requests' own tokens, a warp a row: the pieces of the unit and those of the same row among its group's shared tokens.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) join_kernel(const Call c, int ctas) {
-    ardiff::begin_kernel();
-    const int lane = threadIdx.x & 31, H = c.cache.heads, G = c.x.G;
-    const PlanHead head = *c.plan.head;
-    const long long each = steps_each(head.steps, ctas), units = (long long)(head.blocks - head.own) * H;
-    for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const int b = head.own + (int)(unit / H), h = (int)(unit % H);
-        const Block k = c.plan.block[b];
-        const Share share = c.plan.share[k.request];
-        const int tiles = (k.keys + kTileKeys - 1) / kTileKeys;
-        const long long s0 = c.plan.steps[b] + (long long)h * tiles;
-        const int c0 = (int)(s0 / each), mine = tiles ? (int)((s0 + tiles - 1) / each) - c0 + 1 : 0;
-        if (mine == 1 && share.prefix < 0) continue;                                // written already
-        for (int in = threadIdx.x >> 5; in < k.rows; in += 8) {
-            int theirs = 0, t0 = 0, t_in = 0, t_rows = 0;
-            long long t_before = 0;
-            if (share.prefix >= 0) {
-                const int row = share.row0 + k.row0 + in, pb = share.prefix + row / kBlockRows;
-                const Block p = c.plan.block[pb];
-                const int p_tiles = (p.keys + kTileKeys - 1) / kTileKeys;
-                const long long p0 = c.plan.steps[pb] + (long long)h * p_tiles;
-                t0 = (int)(p0 / each);
-                theirs = (int)((p0 + p_tiles - 1) / each) - t0 + 1;
-                t_in = row % kBlockRows;
-                t_rows = p.rows;
-                t_before = c.plan.rows[pb];
-            }
-            auto row_of = [&](int i) -> long long {
-                return i < mine ? piece_row(c.pieces, c.plan.rows[b], H, k.rows, h, c0 + i, c0, kBlockRows) + in
-                                : piece_row(c.pieces, t_before, H, t_rows, h, t0 + i - mine, t0, kBlockRows) + t_in;
-            };
-            const int all = mine + theirs;
-            float top = -INFINITY;
-            for (int i = lane; i < all; i += 32) top = fmaxf(top, c.pieces.ml[row_of(i)].x);
-#pragma unroll
-            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const float base = top == -INFINITY ? 0.f : top;
-            constexpr int kValues = (D + 31) / 32;
-            float acc[kValues], sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < kValues; ++j) acc[j] = 0.f;
-            for (int i0 = 0; i0 < all; i0 += 32) {
-                float w = 0.f;
-                long long at = 0;
-                if (i0 + lane < all) {
-                    at = row_of(i0 + lane);
-                    const float2 ml = c.pieces.ml[at];
-                    w = ex2(ml.x - base);
-                    sum += w * ml.y;
-                }
-                for (int i = 0; i < min(32, all - i0); ++i) {
-                    const float f = __shfl_sync(0xffffffffu, w, i);
-                    const float* from = c.pieces.o + __shfl_sync(0xffffffffu, at, i) * D;
-#pragma unroll
-                    for (int j = 0; j < kValues; ++j)
-                        if (lane + 32 * j < D) acc[j] += f * from[lane + 32 * j];
-                }
-            }
-#pragma unroll
-            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const float f = sum > 0.f ? 1.f / sum : sum;                             // no key: 0, and lse -inf
-            const int row = k.row0 + in, tok = row / G, qh = h * G + row - tok * G;
-            T* to = static_cast<T*>(c.x.out) + (k.token0 + (long long)tok) * c.x.out_token + qh * c.x.out_head;
-#pragma unroll
-            for (int j = 0; j < kValues; ++j)
-                if (lane + 32 * j < D) to[lane + 32 * j] = from_float<T>(acc[j] * f);
-            if (lane == 0) c.x.lse[(k.token0 + (long long)tok) * c.x.lse_token + qh] = (base + log2f(sum)) * 0.6931471805599453f;
+template <typename T, int D, bool kWide>
+__device__ __forceinline__ void join_unit(const Call& c, int b, int h) {
+    const int lane = threadIdx.x & 31, G = c.x.G;
+    const Block k = list_of<kWide>(c).block[b];
+    const Share share = c.plan.share[k.request];
+    const Cut mine = cut_of<kWide>(c, b, k, h);
+    if (mine.count == 1 && share.prefix < 0) return;                                // written already
+    for (int in = threadIdx.x >> 5; in < k.rows; in += 8) {
+        Cut theirs{0, 0};
+        Block p = k;
+        int pb = 0, p_in = 0;
+        if (share.prefix >= 0) {
+            const int row = share.row0 + k.row0 + in, per = share.wide ? kWideRows : kNarrowRows;
+            pb = share.prefix + row / per;
+            p_in = row % per;
+            p = (share.wide ? c.plan.wide : c.plan.narrow).block[pb];
+            theirs = share.wide ? cut_of<true>(c, pb, p, h) : cut_of<false>(c, pb, p, h);
         }
+        auto row_of = [&](int i) -> long long {
+            if (i < mine.count) return piece_row<kWide>(c, b, k, h, mine.first + i, mine.first) + in;
+            const int cta = theirs.first + i - mine.count;
+            return (share.wide ? piece_row<true>(c, pb, p, h, cta, theirs.first) : piece_row<false>(c, pb, p, h, cta, theirs.first)) + p_in;
+        };
+        const int all = mine.count + theirs.count;
+        float top = -INFINITY;
+        for (int i = lane; i < all; i += 32) top = fmaxf(top, c.pieces.ml[row_of(i)].x);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float base = top == -INFINITY ? 0.f : top;
+        constexpr int kValues = (D + 31) / 32;
+        float acc[kValues], sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < kValues; ++j) acc[j] = 0.f;
+        for (int i0 = 0; i0 < all; i0 += 32) {
+            float w = 0.f;
+            long long at = 0;
+            if (i0 + lane < all) {
+                at = row_of(i0 + lane);
+                const float2 ml = c.pieces.ml[at];
+                w = ex2(ml.x - base);
+                sum += w * ml.y;
+            }
+            for (int i = 0; i < min(32, all - i0); ++i) {
+                const float f = __shfl_sync(0xffffffffu, w, i);
+                const float* from = c.pieces.o + __shfl_sync(0xffffffffu, at, i) * D;
+#pragma unroll
+                for (int j = 0; j < kValues; ++j)
+                    if (lane + 32 * j < D) acc[j] += f * from[lane + 32 * j];
+            }
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const float f = sum > 0.f ? 1.f / sum : sum;                             // no key: 0, and lse -inf
+        const int row = k.row0 + in, tok = row / G, qh = h * G + row - tok * G;
+        T* to = static_cast<T*>(c.x.out) + (k.token0 + (long long)tok) * c.x.out_token + qh * c.x.out_head;
+#pragma unroll
+        for (int j = 0; j < kValues; ++j)
+            if (lane + 32 * j < D) to[lane + 32 * j] = from_float<T>(acc[j] * f);
+        if (lane == 0) c.x.lse[(k.token0 + (long long)tok) * c.x.lse_token + qh] = (base + log2f(sum)) * 0.6931471805599453f;
+    }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) join_kernel(const Call c) {
+    ardiff::begin_kernel();
+    const int H = c.cache.heads;
+    const PlanHead narrow = *c.plan.narrow.head, wide = *c.plan.wide.head;
+    const long long narrow_units = (long long)(narrow.blocks - narrow.own) * H, units = narrow_units + (long long)(wide.blocks - wide.own) * H;
+    for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        if (unit < narrow_units) join_unit<T, D, false>(c, narrow.own + (int)(unit / H), (int)(unit % H));
+        else join_unit<T, D, true>(c, wide.own + (int)((unit - narrow_units) / H), (int)((unit - narrow_units) % H));
     }
 }
 
 // ---- the call -----------------------------------------------------------------------------------
-struct Sizes {
-    long long blocks, main_rows, bytes, block_at, steps_at, rows_at, share_at, shared_at, ml_at, o_at;
+struct Layout {
+    long long narrow_blocks, wide_blocks, main_rows, bytes, block_at[2], steps_at[2], rows_at[2], share_at, ml_at, o_at;
 };
-Sizes sizes(long long requests, long long groups, long long tokens, long long q_heads, long long heads, long long width) {
-    Sizes s;
-    const long long G = q_heads / heads;
-    // blocks of requests or groups: one each for their ends, and the full ones
-    s.blocks = requests + tokens * G / kBlockRows + (groups > 0 ? (groups < requests ? groups : requests) + tokens * G / kBlockRows : 0) + 1;
-    s.main_rows = tokens * q_heads * (groups > 0 ? 2 : 1);
+Layout layout(long long requests, long long groups, long long tokens, long long q_heads, long long heads, long long width) {
+    Layout s;
+    const long long rows = tokens * (q_heads / heads), parts = groups > 0 ? 2 : 1, ends = requests + (groups < requests ? groups : requests);
+    // narrow: a segment of 1 to 64 rows each; wide: the full blocks, and one for the end of every segment of more than 64 rows
+    s.narrow_blocks = (ends < parts * rows ? ends : parts * rows) + 1;
+    s.wide_blocks = parts * (rows / kWideRows + (rows / kNarrowRows < requests ? rows / kNarrowRows : requests)) + 1;
+    s.main_rows = tokens * q_heads * parts;
     auto up = [](long long v) { return (v + 255) / 256 * 256; };
     long long at = 256;
-    s.block_at = at; at = up(at + s.blocks * (long long)sizeof(Block));
-    s.steps_at = at; at = up(at + (s.blocks + 1) * 8);
-    s.rows_at = at; at = up(at + (s.blocks + 1) * 8);
+    for (int i = 0; i < 2; ++i) {
+        const long long blocks = i ? s.wide_blocks : s.narrow_blocks;
+        s.block_at[i] = at; at = up(at + blocks * (long long)sizeof(Block));
+        s.steps_at[i] = at; at = up(at + (blocks + 1) * 8);
+        s.rows_at[i] = at; at = up(at + (blocks + 1) * 8);
+    }
     s.share_at = at; at = up(at + requests * (long long)sizeof(Share));
-    s.shared_at = at; at = up(at + requests * 4);
-    const long long rows = s.main_rows + (long long)kMaxCtas * kBlockRows;
-    s.ml_at = at; at = up(at + rows * 8);
-    s.o_at = at; at = up(at + rows * width * 4);
+    const long long pieces = s.main_rows + (long long)kMaxCtas * kNarrowRows + (long long)kMaxWideCtas * kWideRows;
+    s.ml_at = at; at = up(at + pieces * 8);
+    s.o_at = at; at = up(at + pieces * width * 4);
     s.bytes = at;
     return s;
 }
 
-template <typename T, int D> bool launch(const Call& c, int sms, cudaStream_t st) {
-    const int ctas = 2 * sms < kMaxCtas ? 2 * sms : kMaxCtas;
-    if (cudaFuncSetAttribute(narrow_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kNarrowShared<D>) != cudaSuccess) return false;
-    return launch_early(plan_kernel, 1, kPlanThreads, 1, 0, st, c) && launch_early(narrow_kernel<T, D>, ctas, kThreads, 1, kNarrowShared<D>, st, c, ctas) &&
-           launch_early(join_kernel<T, D>, 8 * sms, 256, 1, 0, st, c, ctas);
+// Whether a block may have more than 64 rows: `most` and the number of tokens say what they can.
+bool may_be_wide(const Call& c, int most) {
+    const long long news = most > 0 && most < c.x.tokens ? most : c.x.tokens;
+    return (c.groups > 0 ? c.x.tokens : news) * c.x.G > kNarrowRows;
 }
-template <typename T> bool launch_width(const Call& c, int width, int sms, cudaStream_t st) {
+
+template <typename T, int D> bool launch(const Call& c, int32_t dtype, int most, int sms, cudaStream_t st) {
+    if (cudaFuncSetAttribute(narrow_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kNarrowShared<D>) != cudaSuccess) return false;
+    const bool wide = may_be_wide(c, most);
+    ardiff::set_launch_count(wide ? 4 : 3);
+    return launch_early(plan_kernel, 1, kPlanThreads, 1, 0, st, c) && (!wide || launch_wide(c, dtype, D, st)) &&
+           launch_early(narrow_kernel<T, D>, c.plan.narrow.ctas, kThreads, 1, kNarrowShared<D>, st, c) &&
+           launch_early(join_kernel<T, D>, 8 * sms, 256, 1, 0, st, c);
+}
+template <typename T> bool launch_width(const Call& c, int32_t dtype, int width, int most, int sms, cudaStream_t st) {
     switch (width) {
-        case 64: return launch<T, 64>(c, sms, st);
-        case 80: return launch<T, 80>(c, sms, st);
-        case 96: return launch<T, 96>(c, sms, st);
-        default: return launch<T, 128>(c, sms, st);
+        case 64: return launch<T, 64>(c, dtype, most, sms, st);
+        case 80: return launch<T, 80>(c, dtype, most, sms, st);
+        case 96: return launch<T, 96>(c, dtype, most, sms, st);
+        default: return launch<T, 128>(c, dtype, most, sms, st);
     }
 }
 
@@ -641,7 +636,7 @@ int ardiff::device_sms() {
 
 extern "C" int64_t ardiff_attend_workspace(int32_t requests, int32_t groups, int64_t tokens, int32_t q_heads, int32_t heads, int32_t head_width) {
     if (!shape(requests, groups, tokens, q_heads, heads) || head_width < 1 || head_width > ARDIFF_ROTARY_MAX_WIDTH) return ARDIFF_ERR_SHAPE;
-    return sizes(requests, groups, tokens, q_heads, heads, head_width).bytes;
+    return layout(requests, groups, tokens, q_heads, heads, head_width).bytes;
 }
 
 extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype, const void* k_cache,
@@ -664,7 +659,7 @@ extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_hea
     if (((low(q) | low(out) | low(k_cache) | low(v_cache)) & 15u) || (low(workspace) & 255u) ||
         ((q_token | q_head | out_token | out_head | k_page | k_token | k_head | v_page | v_token | v_head) & 7))
         return ARDIFF_ERR_ALIGN;
-    const Sizes s = sizes(requests, groups, tokens, q_heads, heads, head_width);
+    const Layout s = layout(requests, groups, tokens, q_heads, heads, head_width);
     if (workspace_bytes < s.bytes) return ARDIFF_ERR_SHAPE;
     const int sms = device_sms();
     if (sms < 1) return ARDIFF_ERR_CUDA;
@@ -675,20 +670,25 @@ extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_hea
     c.x.q = q; c.x.out = out; c.x.lse = lse; c.x.q_token = q_token; c.x.q_head = q_head; c.x.out_token = out_token; c.x.out_head = out_head;
     c.x.lse_token = lse_token; c.x.heads = q_heads; c.x.G = q_heads / heads; c.x.tokens = tokens;
     char* w = static_cast<char*>(workspace);
-    c.plan.head = reinterpret_cast<PlanHead*>(w);
-    c.plan.block = reinterpret_cast<Block*>(w + s.block_at);
-    c.plan.steps = reinterpret_cast<long long*>(w + s.steps_at);
-    c.plan.rows = reinterpret_cast<long long*>(w + s.rows_at);
+    for (int i = 0; i < 2; ++i) {
+        List& l = i ? c.plan.wide : c.plan.narrow;
+        l.head = reinterpret_cast<PlanHead*>(w) + i;
+        l.block = reinterpret_cast<Block*>(w + s.block_at[i]);
+        l.steps = reinterpret_cast<long long*>(w + s.steps_at[i]);
+        l.rows = reinterpret_cast<long long*>(w + s.rows_at[i]);
+    }
+    c.plan.narrow.ctas = 2 * sms < kMaxCtas ? 2 * sms : kMaxCtas;
+    c.plan.wide.ctas = sms < kMaxWideCtas ? sms : kMaxWideCtas;
     c.plan.share = reinterpret_cast<Share*>(w + s.share_at);
-    c.plan.shared = reinterpret_cast<int*>(w + s.shared_at);
     c.pieces.ml = reinterpret_cast<float2*>(w + s.ml_at);
     c.pieces.o = reinterpret_cast<float*>(w + s.o_at);
-    c.pieces.main_rows = s.main_rows;
+    c.pieces.narrow_rows = s.main_rows;
+    c.pieces.wide_rows = s.main_rows + (long long)kMaxCtas * kNarrowRows;
     c.length = length; c.offset = offset; c.group = group; c.shared = shared; c.status = status;
     c.scale = scale * 1.4426950408889634f;
     c.requests = requests; c.groups = groups; c.causal = causal != 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool ok = dtype == ARDIFF_F16 ? launch_width<__half>(c, head_width, sms, st) : launch_width<__nv_bfloat16>(c, head_width, sms, st);
-    ardiff::set_launch_count(3);
+    const bool ok = dtype == ARDIFF_F16 ? launch_width<__half>(c, dtype, head_width, most, sms, st)
+                                        : launch_width<__nv_bfloat16>(c, dtype, head_width, most, sms, st);
     return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
 }

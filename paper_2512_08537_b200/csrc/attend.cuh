@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "../../include/ardiff.h"
+
 namespace ardiff {
 
 struct Pages {                                   // strides in bytes
@@ -16,29 +18,41 @@ struct Pages {                                   // strides in bytes
 };
 
 // Query rows that look at the same keys together. A segment is the new tokens of one request, or of a group of requests that share
-// their first tokens; row j of it is token token0 + j / G, query head h G + j % G (G: query heads a kv head). A block is up to kBlockRows
-// rows of a segment and the keys that they see of one row of the table. Its row j sees the keys below limit + step * (j / G).
+// their first tokens; row j of it is token token0 + j / G, query head h G + j % G (G: query heads a kv head). A block is some rows of a segment, 64 in
+// the list of narrow blocks, 256 in that of wide ones, and the keys that they see. Its row j sees the keys below limit + step * (j / G). Keys below
+// `split` are found through row `front` of the table, the others through row `request`.
 struct Block {
-    int token0, row0, rows, request, key0, keys, limit, step;
+    int token0, row0, rows, request, key0, keys, limit, step, split, front, pad0, pad1;
 };
 
 struct PlanHead {
     long long steps;                             // of all blocks: key tiles times kv heads
+    long long rows_before;                       // rows of the other list's blocks, in front of this one's among the pieces
     int blocks, own;                             // blocks [0, own): shared tokens; [own, blocks): the requests' own
 };
 
-// Of a request: where its rows are among those of its group (prefix -1: no shared tokens)
+// Of a request: the first block of its group's shared tokens (-1: none), in which list, and its first row there; how many shared tokens it does not read
+// itself; how many it finds through another row of the table.
 struct Share {
-    int prefix, row0;                            // first block of the shared tokens; its first row there
+    int prefix, wide, row0, shared, split, front, pad0, pad1;
 };
 
-struct Plan {
+constexpr int kNarrowRows = 64, kNarrowKeys = 64, kWideRows = 256, kWideKeys = 128;
+template <bool kWide> struct Sizes {
+    static constexpr int rows = kWide ? kWideRows : kNarrowRows, keys = kWide ? kWideKeys : kNarrowKeys;
+};
+
+struct List {
     PlanHead* head;
     Block* block;
     long long* steps;                            // [blocks + 1]: steps of the blocks before
     long long* rows;                             // [blocks + 1]: rows of the blocks before
+    int ctas;                                    // that share its steps
+};
+
+struct Plan {
+    List narrow, wide;
     Share* share;                                // [requests]
-    int* shared;                                 // [requests]: shared tokens that the request does not read itself
 };
 
 struct Queries {                                 // strides in values
@@ -50,17 +64,84 @@ struct Queries {                                 // strides in values
     long long tokens;
 };
 
-// Results of a unit (a block and a kv head) in pieces: of the CTA that began it, in rows[block] * heads + head * rows, and one of every CTA that
-// went on with it, in that CTA's own place behind all those. Values are relative to the piece's maximum, in powers of two.
+// Results of a unit (a block and a kv head) in pieces: of the CTA that began it, in its rows' own place (narrow blocks' rows, then wide ones'), and
+// one of every CTA that went on with it, in that CTA's place behind all those. Values are relative to the piece's maximum, in powers of two.
 struct Pieces {
     float* o;                                    // [rows][width]
     float2* ml;                                  // [rows]: maximum, sum
-    long long main_rows;
+    long long narrow_rows, wide_rows;            // where the CTAs' places begin
 };
 
-__device__ __forceinline__ long long piece_row(const Pieces& p, long long rows_before, int heads, int rows, int h, int cta, int first, int cta_rows) {
-    return cta == first ? rows_before * heads + (long long)h * rows : p.main_rows + (long long)cta * cta_rows;
+struct Call {
+    Pages cache;
+    Queries x;
+    Plan plan;
+    Pieces pieces;
+    const int32_t* length;
+    const int32_t* offset;
+    const int32_t* group;
+    const int32_t* shared;
+    int32_t* status;
+    float scale;                                 // times log2 e
+    int requests, groups, causal;
+};
+
+template <bool kWide> __device__ __forceinline__ const List& list_of(const Call& c) { return kWide ? c.plan.wide : c.plan.narrow; }
+
+// The steps of a CTA: the same number for all but the last ones.
+__device__ __forceinline__ long long steps_each(long long steps, int ctas) { return max(1ll, (steps + ctas - 1) / ctas); }
+
+template <bool kWide> __device__ __forceinline__ long long piece_row(const Call& c, int b, const Block& k, int h, int cta, int first) {
+    const List& l = list_of<kWide>(c);
+    return cta != first ? (kWide ? c.pieces.wide_rows : c.pieces.narrow_rows) + (long long)cta * Sizes<kWide>::rows
+                        : (l.head->rows_before + l.rows[b]) * c.cache.heads + (long long)h * k.rows;
 }
+
+// Where a CTA is in the line of steps: block, head, tile of keys.
+template <bool kWide> struct Cursor {
+    int b, h, tile, tiles;
+    Block at;
+    __device__ __forceinline__ void enter(const Call& c) {
+        at = list_of<kWide>(c).block[b];
+        tiles = (at.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
+    }
+    __device__ __forceinline__ void start(const Call& c, int block, long long step) {
+        b = block;
+        enter(c);
+        const int in = (int)(step - list_of<kWide>(c).steps[b]);          // heads times tiles of a block: below 2^31
+        h = in / tiles;
+        tile = in - h * tiles;
+    }
+    // (only called while there is a next step)
+    __device__ __forceinline__ void next(const Call& c) {
+        if (++tile < tiles) return;
+        tile = 0;
+        if (++h < c.cache.heads) return;
+        h = 0;
+        do {
+            ++b;
+            enter(c);
+        } while (tiles == 0);
+    }
+};
+
+// The offsets of key `j` of the tile at `load` in the caches of keys and values, -1 for none.
+template <bool kWide> __device__ __forceinline__ longlong2 place_of(const Call& c, const Cursor<kWide>& load, int j) {
+    const int in = load.tile * Sizes<kWide>::keys + j;
+    if (in >= load.at.keys) return make_longlong2(-1, -1);
+    const unsigned key = load.at.key0 + in, pg = key / (unsigned)c.cache.page, row = key - pg * c.cache.page;
+    const int r = (int)key < load.at.split ? load.at.front : load.at.request;
+    const int id = c.cache.table[(long long)r * c.cache.width + pg];
+    if (id < 0 || id >= c.cache.pages) {
+        *c.status = ARDIFF_ERR_SHAPE;
+        return make_longlong2(-1, -1);
+    }
+    return make_longlong2(id * c.cache.k_page + row * c.cache.k_token + load.h * c.cache.k_head,
+                          id * c.cache.v_page + row * c.cache.v_token + load.h * c.cache.v_head);
+}
+
+// Blocks of more than 64 rows (attend_wide.cu).
+bool launch_wide(const Call& c, int32_t dtype, int width, cudaStream_t st);
 
 // The last of n + 1 ascending numbers x[0] = 0 .. x[n] that is not above s < x[n]. All lanes of a warp call it with the same arguments.
 __device__ __forceinline__ int find_last(const long long* x, int n, long long s) {
@@ -80,6 +161,7 @@ __device__ __forceinline__ int find_last(const long long* x, int n, long long s)
 
 template <typename T> struct Pair;
 template <> struct Pair<__nv_bfloat16> {
+    static constexpr bool kBf16 = true;
     static __device__ __forceinline__ uint32_t pack(float a, float b) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);
@@ -88,6 +170,7 @@ template <> struct Pair<__nv_bfloat16> {
     static __device__ __forceinline__ bool not_finite(uint32_t p) { return (p & 0x7f800000u) == 0x7f800000u || (p & 0x7f80u) == 0x7f80u; }
 };
 template <> struct Pair<__half> {
+    static constexpr bool kBf16 = false;
     static __device__ __forceinline__ uint32_t pack(float a, float b) {
         const __half2 h = __floats2half2_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);

@@ -217,6 +217,29 @@ def test_bad_pages_are_told_and_touch_no_other_request():
     assert int(status) == SHAPE
 
 
+def test_what_is_not_finite_in_blocks_of_many_rows():
+    """The same where 256 rows, and 300 keys in three tiles, are worked on together."""
+    for D, dtype in ((64, "bf16"), (80, "f16"), (128, "bf16")):
+        c = Case([200, 70], [300, 75], 4, 2, D, 16, dtype, seed=13)
+        want, want_lse, _ = c.attend()
+        for at_new in (0, 30, 150, 199):
+            p = 100 + at_new
+            at = int(c.table[0, p // 16]), p % 16
+            for cache, bad in ((c.k, math.nan), (c.v, math.nan), (c.v, math.inf)):
+                old = cache[at].clone()
+                cache[at] = bad
+                out, lse, status = c.attend()
+                cache[at] = old
+                assert int(status) == 0
+                same = list(range(at_new)) + list(range(200, 270))
+                assert torch.equal(lse[same], want_lse[same])
+                # the same operands in another order of fp32 sums (of at most 300 terms: 300 2^-23 of the largest value), rounded once each
+                off = (out[same].double() - want[same].double()).abs()
+                tol = torch.finfo(out.dtype).eps * want[same].double().abs() + 300 * 2.0 ** -23 * float(c.values[0].abs().max())
+                assert bool((off <= tol).all()) and torch.equal(out[200:], want[200:])
+                assert not bool(torch.isfinite(out[at_new:200].float()).all(-1).any())
+
+
 # ---- weights ------------------------------------------------------------------------------------
 @pytest.mark.parametrize("n,length,Hq,Hkv,page", MIXES)
 @pytest.mark.parametrize("D,dtype,layout", [(64, "f16", "nhd"), (80, "bf16", "hnd"), (96, "bf16", "nhd"), (128, "bf16", "nhd")])
