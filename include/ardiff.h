@@ -560,8 +560,8 @@ int ardiff_rotary_append(const void* q, int64_t q_token, int64_t q_head, void* q
  * over the keys p < length[r] - n + i + 1 for the i-th of its n new tokens (causal != 0), or p < length[r] for all. A query that sees
  * no key has out 0 and lse -inf. Rows of q behind offset[requests] are not read, those of out and lse left as they were.
  * Shared tokens: the requests group[g] .. group[g + 1] - 1 (g < groups) have their first shared[g] tokens in common, so these are read
- * once for all of them, through the table's row group[g] alone. (The other rows must name pages that hold the same. Where a query of the group does
- * not see all of them, only those that all see are taken as shared.)
+ * once for all of them, and whole pages of them through the table's row group[g] alone. (The page in which they end is every request's own
+ * and holds the same. Where a query of the group does not see all of them, only those that all see are taken as shared.)
  *   q, out      dev [tokens][q_heads][head_width] of type dtype, ARDIFF_BF16 or ARDIFF_F16, strides in values; lse  dev float
  *               [tokens][q_heads], rows lse_token apart.  tokens * q_heads < 2^31, q_heads <= ARDIFF_ROTARY_MAX_HEADS, a multiple of heads
  *   caches      as above, of the same type; head_width 64, 80, 96 or 128 (others: ERR_UNSUPPORTED). Pointers on 16-byte boundaries, strides

@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
         for (int j = 0; j < n; ++j) {
             Block b;
             b.token0 = token0; b.row0 = j * per; b.rows = (int)min((long long)per, rows - b.row0);
-            b.request = r0; b.key0 = 0; b.keys = keys; b.limit = keys; b.step = 0; b.split = 0; b.front = r0; b.pad0 = b.pad1 = 0;
+            b.request = r0; b.key0 = b.low = 0; b.keys = keys; b.limit = keys; b.step = 0; b.split = 0; b.front = r0; b.pad = 0;
             (wide ? c.plan.wide : c.plan.narrow).block[at + j] = b;
         }
         if (n > 0) { c.plan.share[r0].prefix = (int)at; c.plan.share[r0].wide = wide; }
@@ -148,11 +148,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
         for (int j = 0; j < n; ++j) {
             Block b;
             b.token0 = token0; b.row0 = j * per; b.rows = (int)min((long long)per, rows - b.row0);
-            b.request = r; b.key0 = share.shared; b.split = share.split; b.front = share.front; b.pad0 = b.pad1 = 0;
+            b.request = r; b.low = share.shared; b.split = share.split; b.front = share.front; b.pad = 0;
+            b.key0 = wide ? b.low / kWideKeys * kWideKeys : b.low;
             b.step = c.causal ? 1 : 0;
             b.limit = c.causal ? len - news + 1 : len;
             const int last = min(len, b.limit + b.step * ((b.row0 + b.rows - 1) / G));
-            b.keys = max(0, last - b.key0);
+            b.keys = last > b.low ? last - b.key0 : 0;
             (wide ? c.plan.wide : c.plan.narrow).block[at + j] = b;
         }
         blocks[0] += total >> 32;
@@ -669,6 +670,7 @@ extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_hea
                     v_token * 2, v_head * 2, table, width, page, pages, heads};
     c.x.q = q; c.x.out = out; c.x.lse = lse; c.x.q_token = q_token; c.x.q_head = q_head; c.x.out_token = out_token; c.x.out_head = out_head;
     c.x.lse_token = lse_token; c.x.heads = q_heads; c.x.G = q_heads / heads; c.x.tokens = tokens;
+    c.x.by_G = divide_by(q_heads / heads);
     char* w = static_cast<char*>(workspace);
     for (int i = 0; i < 2; ++i) {
         List& l = i ? c.plan.wide : c.plan.narrow;

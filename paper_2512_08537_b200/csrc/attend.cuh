@@ -19,10 +19,10 @@ struct Pages {                                   // strides in bytes
 
 // Query rows that look at the same keys together. A segment is the new tokens of one request, or of a group of requests that share
 // their first tokens; row j of it is token token0 + j / G, query head h G + j % G (G: query heads a kv head). A block is some rows of a segment, 64 in
-// the list of narrow blocks, 256 in that of wide ones, and the keys that they see. Its row j sees the keys below limit + step * (j / G). Keys below
-// `split` are found through row `front` of the table, the others through row `request`.
+// the list of narrow blocks, 256 in that of wide ones, and the keys that they see, key0 .. key0 + keys - 1. Its row j sees those from `low` on (wide
+// blocks begin at a multiple of their tiles) and below limit + step * (j / G). Pages of keys all below `split` are found through row `front` of the table, the others through row `request`.
 struct Block {
-    int token0, row0, rows, request, key0, keys, limit, step, split, front, pad0, pad1;
+    int token0, row0, rows, request, key0, keys, low, limit, step, split, front, pad;
 };
 
 struct PlanHead {
@@ -55,6 +55,18 @@ struct Plan {
     Share* share;                                // [requests]
 };
 
+// n / d for n < 2^31
+struct Divide {
+    uint32_t d, m, s;
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return d == 1 ? n : __umulhi(n, m) >> s; }
+};
+// m = 2^(32 + s) / d rounded up with 2^s < d <= 2^(s + 1): exact for n < 2^31, since m d - 2^(32 + s) < d <= 2^(s + 1)
+inline Divide divide_by(uint32_t d) {
+    uint32_t s = 0;
+    while (d > 1 && (2u << s) < d) ++s;
+    return Divide{d, d > 1 ? (uint32_t)((((uint64_t)1 << (32 + s)) + d - 1) / d) : 0u, s};
+}
+
 struct Queries {                                 // strides in values
     const void* q;
     void* out;
@@ -62,6 +74,7 @@ struct Queries {                                 // strides in values
     long long q_token, q_head, out_token, out_head, lse_token;
     int heads, G;
     long long tokens;
+    Divide by_G;
 };
 
 // Results of a unit (a block and a kv head) in pieces: of the CTA that began it, in its rows' own place (narrow blocks' rows, then wide ones'), and
@@ -130,7 +143,7 @@ template <bool kWide> __device__ __forceinline__ longlong2 place_of(const Call& 
     const int in = load.tile * Sizes<kWide>::keys + j;
     if (in >= load.at.keys) return make_longlong2(-1, -1);
     const unsigned key = load.at.key0 + in, pg = key / (unsigned)c.cache.page, row = key - pg * c.cache.page;
-    const int r = (int)key < load.at.split ? load.at.front : load.at.request;
+    const int r = pg < (unsigned)load.at.split / (unsigned)c.cache.page ? load.at.front : load.at.request;
     const int id = c.cache.table[(long long)r * c.cache.width + pg];
     if (id < 0 || id >= c.cache.pages) {
         *c.status = ARDIFF_ERR_SHAPE;

@@ -10,12 +10,17 @@
 // The maximum only moves when it would grow by more than 8 (a factor 256 that P and the sums hold easily): then O is rescaled in
 // tensor memory, which is rare; the product that last wrote O is done by then, since its successor S_t is issued after it.
 //
-// Warps: 0-3 and 4-7 the rows of tile 0 and 1 (a thread a row), 8 issues products, 9-11 copy. Queries, keys and values come by asynchronous 16-byte
-// copies through places looked up in the table, into the 128-byte-swizzled layout that the products read; pages may have any size and strides.
+// Warps: 0-3 and 4-7 the rows of tile 0 and 1 (a thread a row), 8 issues products, 9 copies keys, 10 values, 11 queries. Pages of a multiple of 8 tokens
+// come by TMA, in boxes of the largest power of two of tokens that divides a page (a lane looks up and copies a box). Others come by asynchronous
+// 16-byte copies, 64 a lane and tile, into the same 128-byte-swizzled layout; their places warp 11 looks up, up to four steps ahead. Those
+// copies tell of themselves when they have landed, and the issuing warp puts the fence between the proxies.
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
 #include <string.h>
+
+#include <atomic>
 
 #include "../../include/ardiff.h"
 #include "attend.cuh"
@@ -29,7 +34,7 @@ namespace {
 using namespace ardiff;
 
 constexpr int kThreads = 12 * 32;               // three warps a quarter of the SM: 168 registers each
-constexpr int kLoaders = 96;                    // threads that copy
+constexpr int kPlaces = 4;                       // steps whose places are known
 constexpr int kRows = 128;                       // of a tile
 constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemColumns = 512;
 constexpr float kSlack = 8.f;
@@ -37,10 +42,10 @@ constexpr unsigned long long kWaitLimit = 4000000000ull;   // ns
 
 template <int D> constexpr int kSub = (D + 63) / 64;                       // blocks of 64 values of a row
 template <int D> constexpr int kTile = kSub<D> * 128 * 128;                // bytes of 128 rows
-template <int D> constexpr int kShared = 1024 + 6 * kTile<D> + 2 * 128 * 16;
+template <int D> constexpr int kShared = 1024 + 6 * kTile<D> + kPlaces * kWideKeys * 16;
 
 enum Bar { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + 2, kVFull = kKEmpty + 2, kVEmpty = kVFull + 2, kSFull = kVEmpty + 2, kPFull = kSFull + 2,
-           kOFull = kPFull + 2, kDrained = kOFull + 2, kBars };
+           kOFull = kPFull + 2, kVLanded = kOFull + 2, kDrained = kVLanded + 2, kPlaceFull, kPlaceEmpty = kPlaceFull + kPlaces, kBars = kPlaceEmpty + kPlaces };
 
 // Waits give up after kWaitLimit, tell the status and make all others give up.
 struct Waits {
@@ -76,15 +81,85 @@ __device__ __forceinline__ uint32_t swizzled(int row, int c) {
     return (uint32_t)((c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
 }
 
+// The caches as arrays of four dimensions, copied by boxes of `tokens` tokens of a page and 64 values of a head; 0: not that way.
+struct Boxes {
+    CUtensorMap k, v;
+    int tokens;
+};
+
+// 2^x of two numbers, x <= 8, by the nearest whole number and a polynomial for the rest f, |f| <= 1/2 (fitted to 2^f for the least relative
+// error, 2.1e-7 in fp32): a quarter of the exponentials go this way, through pipes that have room, so that the special-function unit's 16 a
+// clock are not the bound. Numbers below -125 count as that; NaN and infinities are not taken here.
+__device__ __forceinline__ float2 exp2_by_products(float2 x) {
+    const Two y = two(fmaxf(x.x, -125.f), fmaxf(x.y, -125.f));
+    const Two t = y + two(12582912.f, 12582912.f);             // 1.5 2^23: the whole number in the low bits
+    const Two f = fma2(t + two(-12582912.f, -12582912.f), two(-1.f, -1.f), y);
+    Two v = fma2(two(1.32764725e-3f, 1.32764725e-3f), f, two(9.67554096e-3f, 9.67554096e-3f));
+    v = fma2(v, f, two(5.55071309e-2f, 5.55071309e-2f));
+    v = fma2(v, f, two(0.240221202f, 0.240221202f));
+    v = fma2(v, f, two(0.693146944f, 0.693146944f));
+    v = fma2(v, f, two(1.00000012f, 1.00000012f));
+    const float2 a = apart(v), n = apart(t);
+    return make_float2(__int_as_float(__float_as_int(n.x) * (1 << 23) + __float_as_int(a.x)),
+                       __int_as_float(__float_as_int(n.y) * (1 << 23) + __float_as_int(a.y)));
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {                  // NaN if one is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// A row's 128 scores from tensor memory: weights 2^(s scale - base), packed; their sum; the highest score (NaN if one is). Careful: only
+// those from `hidden` on and below `seen` count, and every exponential is the special-function unit's, infinities and NaN as they come.
+template <typename T, bool kCareful>
+__device__ __forceinline__ void weights(uint32_t s_at, float scale, float base, int hidden, int seen, uint32_t (&p)[64], Two& sum, float& top) {
+    const Two scale2 = two(scale, scale), base2 = two(-base, -base);
+    uint32_t r[2][32];
+    float high[2] = {-INFINITY, -INFINITY};
+    Two part[2] = {two(0.f, 0.f), two(0.f, 0.f)};
+    ptx::tmem_ld_32x32b_x32(s_at, r[0]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        ptx::tmem_ld_wait_for(r[q & 1]);
+        if (q < 3) ptx::tmem_ld_32x32b_x32(s_at + 32 * (q + 1), r[(q + 1) & 1]);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            float a = __uint_as_float(r[q & 1][2 * j]), b = __uint_as_float(r[q & 1][2 * j + 1]);
+            if (kCareful) {
+                a = 32 * q + 2 * j < seen && 32 * q + 2 * j >= hidden ? a : -INFINITY;
+                b = 32 * q + 2 * j + 1 < seen && 32 * q + 2 * j + 1 >= hidden ? b : -INFINITY;
+            }
+            high[j & 1] = max3(high[j & 1], a, b);
+            const float2 x = apart(fma2(two(a, b), scale2, base2));
+            const float2 w = !kCareful && (j & 3) == 3 ? exp2_by_products(x) : make_float2(ex2(x.x), ex2(x.y));
+            part[j & 1] = part[j & 1] + two(w.x, w.y);
+            p[16 * q + j] = Pair<T>::pack(w.x, w.y);
+        }
+    }
+    sum = part[0] + part[1];
+    top = max3(high[0], high[1], high[1]);
+}
+
+// an arrival on the barrier once this thread's copies so far have landed
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// Keys below this are seen by all rows of a block.
+__device__ __forceinline__ int least_seen(const Block& b, int G) { return min(b.key0 + b.keys, b.limit + b.step * (b.row0 / G)); }
+
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c) {
+__global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const __grid_constant__ Boxes boxes) {
     extern __shared__ char raw[];
     char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     constexpr int kQ = 0, kK = 2 * kTile<D>, kV = 4 * kTile<D>;
-    longlong2* place = reinterpret_cast<longlong2*>(smem + 6 * kTile<D>);            // [2][128]
+    // offsets of keys and of values: [2][steps][128]; odd: there is none
+    long long* place = reinterpret_cast<long long*>(smem + 6 * kTile<D>);
     __shared__ __align__(8) uint64_t s_bar[kBars];
     __shared__ uint32_t s_tmem;
     __shared__ int s_stop;
+    __shared__ int s_whole[kPlaces];             // whether all 128 keys of the step have a place
     __shared__ int s_odd[2];                     // values of the stage that are not finite, where some row does not see them
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t bars = ptx::smem_u32(s_bar), at = ptx::smem_u32(smem);
@@ -95,8 +170,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c) {
     const int n = (int)(min(steps, begin + each) - begin), own = list.head->own, G = c.x.G;
     if (tid == 0) {
         for (int i = 0; i < kBars; ++i) {
-            const bool loaders = i == kQFull || i == kKFull || i == kKFull + 1 || i == kVFull || i == kVFull + 1;
-            ptx::mbar_init(bars + i * 8, loaders ? kLoaders : i == kPFull || i == kPFull + 1 ? 128 : 1);
+            const bool a_warp = i == kQFull || i == kKFull || i == kKFull + 1 || i == kVFull || i == kVFull + 1 || (i >= kPlaceFull && i < kPlaceEmpty);
+            ptx::mbar_init(bars + i * 8, a_warp ? (boxes.tokens && i != kQFull ? 1 : 32) : i >= kPlaceEmpty ? 2 : i == kPFull || i == kPFull + 1 ? 128 : 1);
         }
         s_stop = 0;
         ptx::fence_mbar_init();
@@ -113,159 +188,262 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c) {
     Cursor<true> now;
     now.start(c, find_last(list.steps, list.head->blocks, begin), begin);
 
-    if (warp >= 9) {
-        // ---- copies
-        const int t = tid - 9 * 32;
-        constexpr int kChunks = D / 8;
-        longlong2 found[2];                      // of keys t and t + 96 of the step that is copied next
-        auto look_up = [&](const Cursor<true>& x) {
-            found[0] = place_of<true>(c, x, t);
-            if (t + kLoaders < kWideKeys) found[1] = place_of<true>(c, x, t + kLoaders);
-        };
-        look_up(now);
-        Cursor<true> load = now;                 // of the places looked up last
+    if (warp == 11) {
+        // ---- places and queries
+        constexpr int kLanes = D / 8 <= 8 ? 8 : 16;                         // a row
+        const int ch = lane % kLanes;
+        const bool mine = ch < D / 8;
         uint32_t unit = 0;
         bool fresh = true;
-        auto signal_v = [&](int i, const Cursor<true>& x) {
-            // the keys that some row of the block does not see must not reach it as 0 times a value that is not finite
-            const int least = min(x.at.key0 + x.at.keys, x.at.limit + x.at.step * (x.at.row0 / G));
-            const int stage = i & 1;
-            if (x.at.key0 + (x.tile + 1) * kWideKeys > least) {
-                bool odd = false;
-                for (int j = t; j < kWideKeys * kChunks; j += kLoaders) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(smem + kV + stage * kTile<D> + swizzled(j / kChunks, j % kChunks));
-                    odd |= Pair<T>::not_finite(v.x) || Pair<T>::not_finite(v.y) || Pair<T>::not_finite(v.z) || Pair<T>::not_finite(v.w);
-                }
-                if (odd) s_odd[stage] = 1;
+        for (int i = 0; i < n; ++i) {
+            const int slot = i % kPlaces;
+            longlong2 found[4];
+            bool whole = true;
+            if (!boxes.tokens) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                found[u] = place_of<true>(c, now, u * 32 + lane);
+                whole &= found[u].x >= 0;
             }
-            ptx::fence_proxy_async_smem();
-            ptx::mbar_arrive(bars + (kVFull + stage) * 8);
-        };
-        Cursor<true> last = now;                 // of step i - 1
-        auto copy = [&](int i) -> bool {
-            const int stage = i & 1;
-            const uint32_t parity = (((uint32_t)i >> 1) & 1) ^ 1;
+            whole = __all_sync(0xffffffffu, whole);
+            if (!__all_sync(0xffffffffu, wait(kPlaceEmpty + slot, ((i / kPlaces) & 1) ^ 1))) break;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                place[slot * kWideKeys + u * 32 + lane] = found[u].x < 0 ? 1 : found[u].x;
+                place[(kPlaces + slot) * kWideKeys + u * 32 + lane] = found[u].x < 0 ? 1 : found[u].y;
+            }
+            if (lane == 0) s_whole[slot] = whole;
+            ptx::mbar_arrive(bars + (kPlaceFull + slot) * 8);
+            }
             if (fresh) {
-                if (!wait(kQEmpty, (unit & 1) ^ 1)) return false;
-                for (int j = t; j < 2 * kRows * kChunks; j += kLoaders) {
-                    const int in = j / kChunks, ch = j - in * kChunks;
+                if (!__all_sync(0xffffffffu, wait(kQEmpty, (unit & 1) ^ 1))) break;
+                const int rows = now.at.rows > kRows ? 2 * kRows : kRows;
+                const T* base = static_cast<const T*>(c.x.q) + (long long)now.at.token0 * c.x.q_token + (long long)now.h * G * c.x.q_head + ch * 8;
+#pragma unroll 4
+                for (int in = lane / kLanes; in < rows; in += 32 / kLanes) {
                     const bool there = in < now.at.rows;
-                    const int row = now.at.row0 + in, tok = row / G;
-                    const T* from = static_cast<const T*>(c.x.q);
-                    if (there) from += (now.at.token0 + (long long)tok) * c.x.q_token + (now.h * G + row - tok * G) * c.x.q_head + ch * 8;
-                    cp_async16(at + kQ + (in >> 7) * kTile<D> + swizzled(in & 127, ch), from, there ? 16 : 0);
+                    const unsigned row = now.at.row0 + in, tok = c.x.by_G.quotient(row);
+                    const T* from = base + (there ? tok * c.x.q_token + (row - tok * G) * c.x.q_head : 0);
+                    if (mine) cp_async16(at + kQ + (in >> 7) * kTile<D> + swizzled(in & 127, ch), from, there ? 16 : 0);
                 }
+                cp_async_arrive(bars + kQFull * 8);
             }
-            if (!wait(kKEmpty + stage, parity)) return false;
-            for (int j = t; j < kWideKeys * kChunks; j += kLoaders) {
-                const int row = j / kChunks, ch = j - row * kChunks;
-                const long long p = place[stage * 128 + row].x;
-                cp_async16(at + kK + stage * kTile<D> + swizzled(row, ch), c.cache.k + (p < 0 ? 0 : p + ch * 16), p < 0 ? 0 : 16);
-            }
-            cp_async_commit();
-            if (i > 0) {
-                cp_async_wait<1>();
-                signal_v(i - 1, last);
-            }
-            if (!wait(kVEmpty + stage, parity)) return false;
-            if (t == 0) s_odd[stage] = 0;
-            for (int j = t; j < kWideKeys * kChunks; j += kLoaders) {
-                const int row = j / kChunks, ch = j - row * kChunks;
-                const longlong2 p = place[stage * 128 + row];
-                cp_async16(at + kV + stage * kTile<D> + swizzled(row, ch), c.cache.v + (p.x < 0 ? 0 : p.y + ch * 16), p.x < 0 ? 0 : 16);
-            }
-            cp_async_commit();
-            if (i + 1 < n) {
-                load.next(c);
-                look_up(load);
-            }
-            cp_async_wait<1>();
-            ptx::fence_proxy_async_smem();
-            if (fresh) ptx::mbar_arrive(bars + kQFull * 8);
-            ptx::mbar_arrive(bars + (kKFull + stage) * 8);
             fresh = now.tile + 1 == now.tiles;
             if (fresh) ++unit;
-            last = now;
             if (i + 1 < n) now.next(c);
-            return true;
-        };
-        bool good = true;                        // (the copying warps meet n + 1 times whether they gave up or not)
-        for (int i = 0; i < n; ++i) {
-            place[(i & 1) * 128 + t] = found[0];
-            if (t + kLoaders < kWideKeys) place[(i & 1) * 128 + t + kLoaders] = found[1];
-            ptx::bar_sync(1, kLoaders);
-            good = good && copy(i);
         }
+        cp_async_commit();
         cp_async_wait<0>();
-        ptx::bar_sync(1, kLoaders);              // s_odd's zero comes before any one
-        if (good) signal_v(n - 1, last);
+    } else if (warp >= 9 && boxes.tokens) {
+        // ---- keys or values, by boxes
+        const bool v = warp == 10;
+        const int full = v ? kVFull : kKFull, empty = v ? kVEmpty : kKEmpty, tokens = boxes.tokens;
+        const CUtensorMap* map = v ? &boxes.v : &boxes.k;
+        const uint32_t to = at + (v ? kV : kK) + lane * tokens * 128;
+        Cursor<true> load = now;                 // of the box that is looked up next
+        struct Box { int id, row, head; } next;
+        auto look_up = [&]() {
+            const int in = load.tile * kWideKeys + lane * tokens, key = load.at.key0 + in;
+            next.id = -1;
+            next.head = load.h;
+            if (lane * tokens < kWideKeys && in < load.at.keys) {
+                const int pg = (unsigned)key / (unsigned)c.cache.page;
+                next.row = key - pg * c.cache.page;
+                next.id = c.cache.table[(long long)(pg < load.at.split / c.cache.page ? load.at.front : load.at.request) * c.cache.width + pg];
+                if (next.id < 0 || next.id >= c.cache.pages) {
+                    *c.status = ARDIFF_ERR_SHAPE;
+                    next.id = -1;
+                }
+            }
+        };
+        look_up();
+        uint32_t landed[2] = {0, 0};
+        for (int i = 0; i < n; ++i) {
+            const int stage = i & 1;
+            const Box box = next;
+            if (!__all_sync(0xffffffffu, wait(empty + stage, ((i >> 1) & 1) ^ 1))) break;
+            const bool zone = v && now.at.key0 + (now.tile + 1) * kWideKeys > least_seen(now.at, G);
+            const uint32_t bar = bars + ((zone ? kVLanded : full) + stage) * 8;
+            const uint32_t there = __ballot_sync(0xffffffffu, box.id >= 0);
+            if (lane == 0) ptx::mbar_arrive_expect_tx(bar, __popc(there) * tokens * 128 * kSub<D>);
+            __syncwarp();
+            if (box.id >= 0) {
+#pragma unroll
+                for (int b = 0; b < kSub<D>; ++b)
+                    ptx::tma_load_4d(to + stage * kTile<D> + b * 16384, map, bar, b * 64, box.row, box.head, box.id);
+            }
+            if (i + 1 < n) {
+                load.next(c);
+                look_up();
+            }
+            if (zone) {
+                // keys that some row of the block does not see must not reach it as 0 times a value that is not finite; those behind the
+                // last one, whatever they are, become zeros
+                if (!__all_sync(0xffffffffu, wait(kVLanded + stage, landed[stage]++ & 1))) break;
+                const int left = now.at.keys - now.tile * kWideKeys;
+                bool odd = false;
+                for (int j = lane; j < kWideKeys * 8 * kSub<D>; j += 32) {
+                    const int row = j & 127;
+                    uint4* w = reinterpret_cast<uint4*>(smem + kV + stage * kTile<D> + swizzled(row, j >> 7));
+                    if (row >= left) *w = make_uint4(0u, 0u, 0u, 0u);
+                    else odd |= Pair<T>::not_finite(w->x) || Pair<T>::not_finite(w->y) || Pair<T>::not_finite(w->z) || Pair<T>::not_finite(w->w);
+                }
+                odd = __any_sync(0xffffffffu, odd);
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    s_odd[stage] = odd;
+                    ptx::mbar_arrive(bars + (kVFull + stage) * 8);
+                }
+            }
+            if (i + 1 < n) now.next(c);
+        }
+    } else if (warp >= 9) {
+        // ---- keys or values, by 16 bytes
+        const bool v = warp == 10;
+        const int full = v ? kVFull : kKFull, empty = v ? kVEmpty : kKEmpty;
+        constexpr int kLanes = D / 8 <= 8 ? 8 : 16, kAtOnce = 32 / kLanes, kPeriod = 8 / kAtOnce;    // lanes a row, rows at once, before they repeat
+        const int ch = lane % kLanes, row0 = lane / kLanes;
+        const bool mine = ch < D / 8;
+        const char* from = (v ? c.cache.v : c.cache.k) + ch * 16;
+        uint32_t to[kPeriod];
+#pragma unroll
+        for (int u = 0; u < kPeriod; ++u) to[u] = at + (v ? kV : kK) + swizzled(row0 + u * kAtOnce, ch);
+        for (int i = 0; i < n; ++i) {
+            const int slot = i % kPlaces, stage = i & 1;
+            if (!__all_sync(0xffffffffu, wait(kPlaceFull + slot, (i / kPlaces) & 1) && wait(empty + stage, ((i >> 1) & 1) ^ 1))) break;
+            const long long* p = place + (v ? kPlaces + slot : slot) * kWideKeys + row0;
+            const uint32_t in = stage * kTile<D>;
+            // (offsets of 16 rows first: nothing is read past a copy that has been issued)
+            const bool whole = s_whole[slot];
+#pragma unroll 1
+            for (int j = 0; j < kWideKeys / kAtOnce; j += 16) {
+                long long o[16];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) o[u] = p[(j + u) * kAtOnce];
+                const uint32_t base = in + (j / kPeriod) * 1024;
+                if (whole) {
+#pragma unroll
+                    for (int u = 0; u < 16; ++u)
+                        if (mine) cp_async16(to[u % kPeriod] + base + (u / kPeriod) * 1024, from + o[u], 16);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 16; ++u)
+                        if (mine) cp_async16(to[u % kPeriod] + base + (u / kPeriod) * 1024, from + (o[u] & 1 ? 0 : o[u]), o[u] & 1 ? 0 : 16);
+                }
+            }
+            if (v && now.at.key0 + (now.tile + 1) * kWideKeys > least_seen(now.at, G)) {
+                // keys that some row of the block does not see must not reach it as 0 times a value that is not finite
+                cp_async_commit();
+                cp_async_wait<0>();
+                __syncwarp();
+                bool odd = false;
+                for (int row = row0; mine && row < kWideKeys; row += kAtOnce) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(smem + kV + in + swizzled(row, ch));
+                    odd |= Pair<T>::not_finite(w.x) || Pair<T>::not_finite(w.y) || Pair<T>::not_finite(w.z) || Pair<T>::not_finite(w.w);
+                }
+                odd = __any_sync(0xffffffffu, odd);
+                if (lane == 0) s_odd[stage] = odd;
+                ptx::mbar_arrive(bars + (full + stage) * 8);
+            } else {
+                cp_async_arrive(bars + (full + stage) * 8);
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bars + (kPlaceEmpty + slot) * 8);
+            if (i + 1 < n) now.next(c);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
     } else if (warp == 8) {
-        // ---- products
-        if (ptx::elect_one()) {
-            const uint32_t idesc_s = ptx::idesc_16(Pair<T>::kBf16, 128, 128, false, c.scale < 0.f);
-            const uint32_t idesc_o = ptx::idesc_16(Pair<T>::kBf16, 128, D, true, false);
-            uint32_t unit = 0, p_count[2] = {0, 0};
-            bool fresh = true;
-            auto scores = [&](int tile, int stage) {
+        // ---- products. The whole warp goes through the steps, so that addresses stay in uniform registers; one lane issues.
+        const uint32_t idesc_s = ptx::idesc_16(Pair<T>::kBf16, 128, 128, false, c.scale < 0.f);
+        const uint32_t idesc_o = ptx::idesc_16(Pair<T>::kBf16, 128, D, true, false);
+        const uint64_t q_desc = ptx::smem_desc_sw128(at + kQ), k_desc = ptx::smem_desc_sw128(at + kK);
+        const uint64_t v_desc = ptx::smem_desc_mn_sw128(at + kV, 16384, 1024);
+        uint32_t unit = 0, p_count[2] = {0, 0};
+        bool fresh = true, good = true;
+        auto all = [](bool ok) { return __all_sync(0xffffffffu, ok) != 0; };
+        auto commit = [&](int bar) {
+            if (ptx::elect_one()) ptx::mma_commit(bars + bar * 8);
+            __syncwarp();
+        };
+        // (a descriptor counts in 16 bytes)
+        auto scores = [&](int tile, int stage) {
+            const uint64_t a = q_desc + tile * (kTile<D> / 16), b = k_desc + stage * (kTile<D> / 16);
+            const uint32_t to = tmem + kTmemS + tile * 128;
+            if (ptx::elect_one()) {
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
-                    const uint32_t in = (ks >> 2) * 16384 + (ks & 3) * 32;
-                    ptx::mma_f16_ss(tmem + kTmemS + tile * 128, ptx::smem_desc_sw128(at + kQ + tile * kTile<D> + in),
-                                    ptx::smem_desc_sw128(at + kK + stage * kTile<D> + in), idesc_s, ks > 0);
+                    const uint32_t in = (ks >> 2) * 1024 + (ks & 3) * 2;
+                    ptx::mma_f16_ss(to, a + in, b + in, idesc_s, ks > 0);
                 }
                 ptx::mma_commit(bars + (kSFull + tile) * 8);
-            };
-            auto values = [&](int tile, int stage, bool first) {
+            }
+            __syncwarp();
+        };
+        auto values = [&](int tile, int stage, bool first) {
+            const uint64_t b = v_desc + stage * (kTile<D> / 16);
+            const uint32_t to = tmem + kTmemO + tile * 128, p = tmem + kTmemS + tile * 128;
+            if (ptx::elect_one()) {
 #pragma unroll
-                for (int ks = 0; ks < kWideKeys / 16; ++ks)
-                    ptx::mma_f16_ts(tmem + kTmemO + tile * 128, tmem + kTmemS + tile * 128 + ks * 8,
-                                    ptx::smem_desc_mn_sw128(at + kV + stage * kTile<D> + ks * 2048, 16384, 1024), idesc_o, !first || ks > 0);
-            };
-            bool good = true;
-            for (int i = 0; i < n && good; ++i) {
-                const int stage = i & 1;
-                const uint32_t parity = ((uint32_t)i >> 1) & 1;
-                const bool two = now.at.rows > kRows, ends = now.tile + 1 == now.tiles || i + 1 == n;
-                if (fresh) {
-                    good = wait(kQFull, unit & 1) && wait(kKFull + stage, parity);
-                    if (!good) break;
-                    ptx::tc_fence_after();
-                    scores(0, stage);
-                    if (two) scores(1, stage);
-                    ptx::mma_commit(bars + (kKEmpty + stage) * 8);
-                    if (ends) ptx::mma_commit(bars + kQEmpty * 8);
-                }
-                const int stage1 = (i + 1) & 1;
-                const uint32_t parity1 = ((uint32_t)(i + 1) >> 1) & 1;
-                const bool first = fresh;
-                for (int tile = 0; tile < (two ? 2 : 1); ++tile) {
-                    good = wait(kPFull + tile, p_count[tile]++ & 1) && wait(kVFull + stage, parity);
-                    if (!good) break;
-                    ptx::tc_fence_after();
-                    if (!*(volatile int*)&s_odd[stage]) values(tile, stage, first);
-                    if (ends) ptx::mma_commit(bars + (kOFull + tile) * 8);
-                    if (tile == (two ? 1 : 0)) ptx::mma_commit(bars + (kVEmpty + stage) * 8);
-                    if (!ends) {
-                        good = wait(kKFull + stage1, parity1);
-                        if (!good) break;
-                        ptx::tc_fence_after();
-                        scores(tile, stage1);
-                    }
-                }
+                for (int ks = 0; ks < kWideKeys / 16; ++ks) ptx::mma_f16_ts(to, p + ks * 8, b + ks * 128, idesc_o, !first || ks > 0);
+            }
+            __syncwarp();
+        };
+        for (int i = 0; i < n; ++i) {
+            const int stage = i & 1;
+            const uint32_t parity = ((uint32_t)i >> 1) & 1;
+            const bool two = now.at.rows > kRows, ends = now.tile + 1 == now.tiles || i + 1 == n;
+            if (fresh) {
+                good = all(wait(kQFull, unit & 1) && wait(kKFull + stage, parity));
                 if (!good) break;
-                if (!ends) {
-                    ptx::mma_commit(bars + (kKEmpty + stage1) * 8);
-                    if (now.tile + 2 == now.tiles || i + 2 == n) ptx::mma_commit(bars + kQEmpty * 8);
+                ptx::fence_proxy_async_smem();
+                ptx::tc_fence_after();
+                scores(0, stage);
+                if (two) scores(1, stage);
+                commit(kKEmpty + stage);
+                if (ends) commit(kQEmpty);
+            }
+            const int stage1 = (i + 1) & 1;
+            const uint32_t parity1 = ((uint32_t)(i + 1) >> 1) & 1;
+            const bool zone = now.at.key0 + (now.tile + 1) * kWideKeys > least_seen(now.at, G);
+#pragma unroll
+            for (int tile = 0; tile < 2; ++tile) {
+                if (tile == 1 && !two) break;
+                if (tile == 0) {
+                    good = all(wait(kVFull + stage, parity));
+                    ptx::fence_proxy_async_smem();
                 }
-                fresh = ends;
-                if (ends) ++unit;
-                if (i + 1 < n) now.next(c);
+                good = good && all(wait(kPFull + tile, p_count[tile] & 1));
+                ++p_count[tile];
+                if (!good) break;
+                ptx::tc_fence_after();
+                if (!zone || !*(volatile int*)&s_odd[stage]) values(tile, stage, fresh);
+                if (ends) commit(kOFull + tile);
+                if (tile == (two ? 1 : 0)) commit(kVEmpty + stage);
+                if (!ends) {
+                    if (tile == 0) {
+                        good = all(wait(kKFull + stage1, parity1));
+                        if (!good) break;
+                        ptx::fence_proxy_async_smem();
+                        ptx::tc_fence_after();
+                    }
+                    scores(tile, stage1);
+                }
             }
-            if (!good) {
-                // products in flight end before tensor memory is given back
-                ptx::mma_commit(bars + kDrained * 8);
-                for (int i = 0; i < 1 << 20 && !ptx::mbar_try_wait(bars + kDrained * 8, 0); ++i) {}
+            if (!good) break;
+            if (!ends) {
+                commit(kKEmpty + stage1);
+                if (now.tile + 2 == now.tiles || i + 2 == n) commit(kQEmpty);
             }
+            fresh = ends;
+            if (ends) ++unit;
+            if (i + 1 < n) now.next(c);
+        }
+        if (!good) {
+            // products in flight end before tensor memory is given back
+            commit(kDrained);
+            for (int i = 0; i < 1 << 20 && !ptx::mbar_try_wait(bars + kDrained * 8, 0); ++i) {}
         }
         __syncwarp();
     } else {
@@ -286,37 +464,31 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c) {
                 if (fresh) {
                     m = -INFINITY;
                     l = 0.f;
-                    least = min(now.at.key0 + now.at.keys, now.at.limit + now.at.step * (now.at.row0 / G));
+                    least = least_seen(now.at, G);
                     lim = in < now.at.rows ? min(now.at.key0 + now.at.keys, now.at.limit + now.at.step * tok) : now.at.key0 + now.at.keys;
                 }
                 if (!all(wait(kSFull + tile, s_count++ & 1))) break;
                 ptx::tc_fence_after();
                 const int key0 = now.at.key0 + now.tile * kWideKeys;
-                const int seen = lim - key0;                               // of the tile's keys
-                const bool masked = __any_sync(0xffffffffu, seen < kWideKeys);
-                auto hide = [&](uint32_t (&r)[32], int first) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (first + j >= seen) r[j] = 0xff800000u;
-                };
-                uint32_t r[2][32];
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                ptx::tmem_ld_32x32b_x32(s_at, r[0]);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    ptx::tmem_ld_wait_for(r[q & 1]);
-                    if (q < 3) ptx::tmem_ld_32x32b_x32(s_at + 32 * (q + 1), r[(q + 1) & 1]);
-                    if (masked) hide(r[q & 1], 32 * q);
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], __uint_as_float(r[q & 1][j + e]));
+                const int seen = lim - key0, hidden = now.at.low - key0;   // of the tile's keys
+                const bool masked = __any_sync(0xffffffffu, seen < kWideKeys || hidden > 0);
+                // Weights by the maximum so far, in the hope that it holds, and kept in registers until it is known to: S is still there for another
+                // try with a higher one (the first tile's always, later ones' rarely).
+                uint32_t p[64];
+                bool careful = masked;
+                for (bool again = false;;) {
+                    const float base = m == -INFINITY ? 0.f : m;
+                    Two sum = two(0.f, 0.f);
+                    float top = -INFINITY;
+                    if (careful) weights<T, true>(s_at, scale, base, hidden, seen, p, sum, top);
+                    else weights<T, false>(s_at, scale, base, hidden, seen, p, sum, top);
+                    const float highest = top * scale;
+                    const bool holds = highest <= m + kSlack || highest == -INFINITY;         // (not where it is NaN)
+                    if (again || __all_sync(0xffffffffu, holds)) {
+                        const float2 total = apart(sum);
+                        l += total.x + total.y;
+                        break;
                     }
-                }
-                const float highest = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
-                ptx::tmem_ld_32x32b_x32(s_at, r[0]);
-                bool odd = false;
-                if (__any_sync(0xffffffffu, highest > m + kSlack)) {
                     const float higher = fmaxf(m, highest), alpha = m == higher ? 1.f : ex2(m - higher);
                     m = higher;
                     l *= alpha;
@@ -331,31 +503,22 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c) {
                             ptx::tmem_st_32x32b_x16(o_at + 16 * q, o);
                         }
                     }
+                    careful = again = true;
                 }
-                const float base = m == -INFINITY ? 0.f : m;
+                bool odd = false;
                 if (now.at.key0 + (now.tile + 1) * kWideKeys > least) {
                     if (!all(wait(kVFull + (i & 1), ((uint32_t)i >> 1) & 1))) break;
                     odd = *(volatile int*)&s_odd[i & 1] != 0;
                 }
-                const Two scale2 = two(scale, scale), base2 = two(-base, -base);
-                Two sum[2] = {two(0.f, 0.f), two(0.f, 0.f)};
+                if (!odd) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    ptx::tmem_ld_wait_for(r[q & 1]);
-                    if (q < 3) ptx::tmem_ld_32x32b_x32(s_at + 32 * (q + 1), r[(q + 1) & 1]);
-                    if (masked) hide(r[q & 1], 32 * q);
-                    uint32_t p[16];
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t part[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float2 x = apart(fma2(two(__uint_as_float(r[q & 1][2 * j]), __uint_as_float(r[q & 1][2 * j + 1])), scale2, base2));
-                        const float2 w = make_float2(ex2(x.x), ex2(x.y));
-                        sum[j & 1] = sum[j & 1] + two(w.x, w.y);
-                        p[j] = Pair<T>::pack(w.x, w.y);
+                        for (int j = 0; j < 16; ++j) part[j] = p[16 * q + j];
+                        ptx::tmem_st_32x32b_x16(s_at + 16 * q, part);
                     }
-                    if (!odd) ptx::tmem_st_32x32b_x16(s_at + 16 * q, p);
                 }
-                const float2 total = apart(sum[0] + sum[1]);
-                l += total.x + total.y;
                 if (odd) {
                     // (rare) the product without the keys that a row does not see, key by key
                     const char* v_at = smem + kV + (i & 1) * kTile<D>;
@@ -373,8 +536,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c) {
                             ptx::tmem_ld_wait_for(s);
 #pragma unroll
                             for (int k = 0; k < 16; ++k) {
-                                if (k0 + k >= seen) continue;
-                                const float w = Pair<T>::rounded(ex2(fmaf(__uint_as_float(s[k]), scale, -base)));
+                                if (k0 + k >= seen || k0 + k < hidden) continue;
+                                const float w = Pair<T>::rounded(ex2(fmaf(__uint_as_float(s[k]), scale, m == -INFINITY ? 0.f : -m)));
 #pragma unroll
                                 for (int j = 0; j < 16; ++j) {
                                     const T* v = reinterpret_cast<const T*>(v_at + swizzled(k0 + k, 2 * q + (j >> 3))) + (j & 7);
@@ -432,21 +595,59 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c) {
     if (warp == 8) ptx::tmem_dealloc(tmem, kTmemColumns);
 }
 
-template <typename T, int D> bool launch(const Call& c, cudaStream_t st) {
+template <typename T, int D> bool launch(const Call& c, const Boxes& boxes, cudaStream_t st) {
     if (cudaFuncSetAttribute(wide_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared<D>) != cudaSuccess) return false;
-    return launch_early(wide_kernel<T, D>, c.plan.wide.ctas, kThreads, 1, kShared<D>, st, c);
+    return launch_early(wide_kernel<T, D>, c.plan.wide.ctas, kThreads, 1, kShared<D>, st, c, boxes);
 }
-template <typename T> bool launch_width(const Call& c, int width, cudaStream_t st) {
+template <typename T> bool launch_width(const Call& c, int width, const Boxes& boxes, cudaStream_t st) {
     switch (width) {
-        case 64: return launch<T, 64>(c, st);
-        case 80: return launch<T, 80>(c, st);
-        case 96: return launch<T, 96>(c, st);
-        default: return launch<T, 128>(c, st);
+        case 64: return launch<T, 64>(c, boxes, st);
+        case 80: return launch<T, 80>(c, boxes, st);
+        case 96: return launch<T, 96>(c, boxes, st);
+        default: return launch<T, 128>(c, boxes, st);
     }
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encoder() {
+    static std::atomic<EncodeTiled> known{nullptr};
+    EncodeTiled f = known.load(std::memory_order_relaxed);
+    if (!f) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) return nullptr;
+        f = reinterpret_cast<EncodeTiled>(p);
+        known.store(f, std::memory_order_relaxed);
+    }
+    return f;
+}
+
+// False where the cache cannot be described so (strides of 2^40 bytes, no page): it is copied by 16 bytes then.
+bool describe(CUtensorMap* map, const char* base, bool bf16, int width, int tokens, const Pages& p, long long token, long long head, long long page) {
+    if (p.page == 1) token = 16;                 // (strides of what there is one of may be anything)
+    if (p.heads == 1) head = 16;
+    if (p.pages == 1) page = 16;
+    if (p.pages < 1 || token < 0 || head < 0 || page < 0 || token >= 1ll << 40 || head >= 1ll << 40 || page >= 1ll << 40) return false;
+    const EncodeTiled f = encoder();
+    if (!f) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)p.page, (cuuint64_t)p.heads, (cuuint64_t)p.pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)token, (cuuint64_t)head, (cuuint64_t)page};
+    const cuuint32_t box[4] = {64, (cuuint32_t)tokens, 1, 1}, ones[4] = {1, 1, 1, 1};
+    return f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<char*>(base), dims, strides, box, ones,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
 
 bool ardiff::launch_wide(const Call& c, int32_t dtype, int width, cudaStream_t st) {
-    return dtype == ARDIFF_F16 ? launch_width<__half>(c, width, st) : launch_width<__nv_bfloat16>(c, width, st);
+    Boxes boxes;
+    memset(&boxes, 0, sizeof(boxes));
+    int tokens = 1;
+    while (tokens < kWideKeys && c.cache.page % (2 * tokens) == 0) tokens *= 2;
+    const bool bf16 = dtype == ARDIFF_BF16;
+    if (tokens >= 8 && describe(&boxes.k, c.cache.k, bf16, width, tokens, c.cache, c.cache.k_token, c.cache.k_head, c.cache.k_page) &&
+        describe(&boxes.v, c.cache.v, bf16, width, tokens, c.cache, c.cache.v_token, c.cache.v_head, c.cache.v_page))
+        boxes.tokens = tokens;
+    return bf16 ? launch_width<__nv_bfloat16>(c, width, boxes, st) : launch_width<__half>(c, width, boxes, st);
 }
