@@ -574,7 +574,7 @@ int ardiff_rotary_append(const void* q, int64_t q_token, int64_t q_head, void* q
  *               (then the results of the requests that have it mean nothing)
  *   workspace   dev, 256-byte aligned, at least ardiff_attend_workspace(...) bytes, as for ardiff_pages_evict
  * Products take 16-bit operands with fp32 sums; weights are fp32 and rounded to dtype as operands of the second product, their sum is
- * that of the unrounded ones. The order of sums follows sizes and lengths: equal calls give equal bits. */
+ * that of the unrounded ones. The order of sums follows sizes, lengths and `most`: equal calls give equal bits. */
 int64_t ardiff_attend_workspace(int32_t requests, int32_t groups, int64_t tokens, int32_t q_heads, int32_t heads, int32_t head_width);
 int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype, const void* k_cache,
                         int64_t k_page, int64_t k_token, int64_t k_head, const void* v_cache, int64_t v_page, int64_t v_token,

@@ -4,11 +4,12 @@
 //   out = sum_p w_p v_p / sum_p w_p,   w_p = exp(scale q.k_p),   lse = ln sum_p w_p   over the keys p that the query sees.
 //
 // A sum over keys can be cut anywhere: a piece of it is its largest scale q.k, and sum and weighted values relative to that. So the shared tokens
-// and a request's own are different blocks of work, blocks are cut into tiles of 64 keys, and the tiles of all blocks and heads are dealt out
-// evenly, in one line, to as many CTAs as the GPU holds: one request of many keys keeps all SMs busy, and so do many requests of
+// and a request's own are different blocks of work, blocks are cut into tiles of keys, and the tiles of all blocks and heads are dealt out
+// evenly, in one line, to as many workers as the GPU holds: one request of many keys keeps all SMs busy, and so do many requests of
 // different lengths.
 //   plan_kernel     checks the call, forms the blocks (whole numbers, one CTA)
-//   narrow_kernel   up to 64 query rows a block
+//   wide_kernel     blocks of many query rows, on the tensor cores' own pace (attend_wide.cu)
+//   narrow_kernel   up to 16 or 32 query rows a block: bound by memory, a worker is a warp
 //   join_kernel     joins the pieces of cut blocks, and shared with own tokens
 #include <cuda_runtime.h>
 #include <math.h>
@@ -28,17 +29,15 @@ namespace {
 
 using namespace ardiff;
 
-constexpr int kMaxCtas = 512, kMaxWideCtas = 256;    // CTAs that have a place for pieces
+constexpr int kMaxSms = 256;                     // whose workers have places for pieces
 constexpr int kPlanThreads = 1024;
 // Fewer shared tokens are read by every request itself: a block of its own and the pieces to join cost more than they take.
 constexpr int kLeastShared = 64;
 
 // ---- the plan -----------------------------------------------------------------------------------
 // Blocks of a segment: of which list, how many.
-__device__ __forceinline__ bool is_wide(long long rows) { return rows > kNarrowRows; }
-__device__ __forceinline__ int blocks_of(long long rows) {
-    return (int)(is_wide(rows) ? (rows + kWideRows - 1) / kWideRows : (rows + kNarrowRows - 1) / kNarrowRows);
-}
+__device__ __forceinline__ bool is_wide(const Call& c, long long rows) { return rows > c.plan.narrow_rows; }
+__device__ __forceinline__ int blocks_of(const Call& c, long long rows) { return is_wide(c, rows) ? (int)((rows + kWideRows - 1) / kWideRows) : rows > 0; }
 
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
     __shared__ long long s_scan[32];
@@ -95,9 +94,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
                 token0 = c.offset[r0];
                 rows = keys > 0 ? (long long)(c.offset[r1] - token0) * G : 0;
             }
-            n = blocks_of(rows);
+            n = blocks_of(c, rows);
         }
-        const bool wide = is_wide(rows);
+        const bool wide = is_wide(c, rows);
         long long total;
         const long long packed = cta_scan((long long)(wide ? 0 : n) << 32 | (wide ? n : 0), s_scan, &total);
         const long long at = wide ? blocks[1] + (int)packed : blocks[0] + (packed >> 32);
@@ -138,9 +137,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
             len = c.length[r];
             share = c.plan.share[r];
             rows = (long long)news * G;
-            n = blocks_of(rows);
+            n = blocks_of(c, rows);
         }
-        const bool wide = is_wide(rows);
+        const bool wide = is_wide(c, rows);
         long long total;
         const long long packed = cta_scan((long long)(wide ? 0 : n) << 32 | (wide ? n : 0), s_scan, &total);
         const long long at = wide ? blocks[1] + (int)packed : blocks[0] + (packed >> 32);
@@ -189,297 +188,254 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
     }
 }
 
-// ---- up to 64 query rows ------------------------------------------------------------------------
-constexpr int kThreads = 128;
-constexpr int kStages = 3;
+// ---- few query rows -----------------------------------------------------------------------------
+constexpr int kWarps = 8;                        // of a CTA, one CTA an SM
+constexpr int kThreads = kWarps * 32;
 
-template <int D> constexpr int kTileBytes = kNarrowKeys * kPitch<D>;
-template <int D> constexpr int kNarrowShared = kStages * 2 * kTileBytes<D> + 16 * D * 4 + kStages * kNarrowKeys * 16 + 4 * 16 * 8;
+template <int D> constexpr int kPitch16 = 2 * D + 16;                     // bytes from row to row: an odd number of 16-byte places
+template <int D> constexpr int kStageBytes = 2 * kNarrowKeys * kPitch16<D>;
+template <int D> constexpr int kStages = 28400 / kStageBytes<D> < 6 ? 28400 / kStageBytes<D> : 6;
+template <int D> constexpr int kNarrowShared = kWarps * (kStages<D> * kStageBytes<D> + 64);
 
-// Four warps. Those that share 16 query rows (all four where the block has up to 16 rows, two up to 32) take turns at groups of 16 keys, each
-// with a running maximum, sum and weighted values of its own, joined in shared memory when the unit ends. Keys and values come by asynchronous copies,
-// two tiles ahead, through offsets that are looked up in the table a step before that.
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 2) narrow_kernel(const Call c) {
+// Every warp is a worker of its own: 16 keys of a kv head a step, as many steps under way as its part of shared memory holds (26 to 28 KB: with
+// eight warps some 200 KB an SM, more than memory's latency asks for), no meeting with other warps. A lane copies one key's row or one
+// value's (a bulk copy: rows lie 2 D + 16 bytes apart there, so that the eight rows of a matrix are in different banks), and looks up the place
+// of the next one meanwhile. Query rows are the left operand, 16 rows an instruction, or twice that (kTiles == 2): with few rows it is mostly
+// empty, but reading 512 bytes a key and head from memory takes longer than its products.
+template <typename T, int D, int kTiles>
+__global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
     extern __shared__ __align__(128) char smem[];
-    char* tiles = smem;
-    float* joined = reinterpret_cast<float*>(smem + kStages * 2 * kTileBytes<D>);
-    longlong2* place = reinterpret_cast<longlong2*>(joined + 16 * D);                // [stages][keys]
-    float2* part = reinterpret_cast<float2*>(place + kStages * kNarrowKeys);           // [warps][16]
     ardiff::begin_kernel();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const List& list = c.plan.narrow;
-    const long long steps = list.head->steps, each = steps_each(steps, list.ctas);
-    const long long begin = each * blockIdx.x;
+    const long long steps = list.head->steps, each = steps_each<false>(list);
+    const int worker = blockIdx.x * kWarps + warp;                                     // (neighbours read neighbouring keys)
+    const long long begin = each * worker;
     if (begin >= steps) return;
     const int n = (int)(min(steps, begin + each) - begin), own = list.head->own;
-    const uint32_t tiles_at = ptx::smem_u32(tiles);
+    const char* ring = smem + kWarps * 64 + warp * kStages<D> * kStageBytes<D>;
+    const uint32_t ring_at = ptx::smem_u32(ring), bars = ptx::smem_u32(smem) + warp * 64;
+    if (lane == 0) {
+        for (int s = 0; s < kStages<D>; ++s) ptx::mbar_init(bars + s * 8, 1);
+        ptx::fence_mbar_init();
+    }
+    __syncwarp();
 
     Cursor<false> now;
     now.start(c, find_last(list.steps, list.head->blocks, begin), begin);
     Cursor<false> load = now;                    // the step whose places are looked up next
-
-    auto fetch = [&](int step) {
-        if (step < n) {
-            const int stage = step % kStages;
-            const uint32_t k_to = tiles_at + stage * 2 * kTileBytes<D>, v_to = k_to + kTileBytes<D>;
-            constexpr int kChunks = D / 8;
-            for (int i = tid; i < kNarrowKeys * kChunks; i += kThreads) {
-                const int row = i / kChunks, ch = i - row * kChunks;
-                const longlong2 p = place[stage * kNarrowKeys + row];
-                cp_async16(k_to + chunk_at<D>(row, ch), c.cache.k + (p.x < 0 ? 0 : p.x + ch * 16), p.x < 0 ? 0 : 16);
-                cp_async16(v_to + chunk_at<D>(row, ch), c.cache.v + (p.x < 0 ? 0 : p.y + ch * 16), p.x < 0 ? 0 : 16);
-            }
-        }
-        cp_async_commit();
+    const bool v = lane >= 16;
+    const uint32_t row_to = ring_at + lane * kPitch16<D>;                              // 16 keys, then their values
+    // where this lane's row of the step at `load` lies, NULL for none
+    auto look_up = [&]() -> const char* {
+        const longlong2 p = place_of<false>(c, load, lane & 15);
+        return p.x < 0 ? nullptr : v ? c.cache.v + p.y : c.cache.k + p.x;
     };
-
-    // places of the first three steps, copies of the first two
-    for (int s = 0; s < kStages && s < n; ++s) {
-        if (tid < kNarrowKeys) place[s * kNarrowKeys + tid] = place_of<false>(c, load, tid);
+    auto fetch = [&](int step, const char* from) {
+        const int stage = step % kStages<D>;
+        const uint32_t there = __ballot_sync(0xffffffffu, from != nullptr);
+        if (lane == 0) ptx::mbar_arrive_expect_tx(bars + stage * 8, __popc(there) * 2 * D);
+        __syncwarp();
+        const uint32_t to = row_to + stage * kStageBytes<D>;
+        if (from) {
+            ptx::bulk_load(to, from, 2 * D, bars + stage * 8);
+        } else if (v) {                          // behind the last key: no value, rather than what was there
+            for (int j = 0; j < D / 8; ++j) ptx::sts_u4(to + j * 16, make_uint4(0u, 0u, 0u, 0u));
+            ptx::fence_proxy_async_smem();
+        }
+    };
+    for (int s = 0; s < kStages<D> && s < n; ++s) {
+        fetch(s, look_up());
         if (s + 1 < n) load.next(c);
     }
-    __syncthreads();
-    for (int s = 0; s < kStages - 1; ++s) fetch(s);
+    const char* found = n > kStages<D> ? look_up() : nullptr;
 
     const int G = c.x.G, quad = lane & 3, row8 = lane >> 2;
-    uint32_t q[D / 16][4];
-    float o[D / 8][4];
-    float m[2], l[2];
-    int lim[2];
-    int least = 0;                               // keys below this are seen by all rows of the block
-    int groups_m = 1, wm = 0, wk = 0, groups_k = 4;
-    bool fresh = true;
-    bool whole = now.tile == 0;
+    uint32_t q[kTiles][D / 16][4];
+    float o[kTiles][D / 8][4], m[kTiles][2], l[kTiles][2];
+    int lim[kTiles][2], least = 0;               // keys below `least` are seen by all rows of the block
+    bool fresh = true, whole = now.tile == 0;
+    uint32_t stage = 0, parity = 0;
 
     for (int i = 0; i < n; ++i) {
         if (fresh) {
             const Block& b = now.at;
-            groups_m = b.rows <= 16 ? 1 : b.rows <= 32 ? 2 : 4;
-            groups_k = 4 / groups_m;
-            wm = warp % groups_m;
-            wk = warp / groups_m;
             const int end = b.key0 + b.keys;
             least = min(end, b.limit + b.step * (b.row0 / G));
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int row = b.row0 + wm * 16 + row8 + 8 * u;
-                const bool there = row < b.row0 + b.rows;
-                const int tok = row / G, head = now.h * G + row - tok * G;
-                lim[u] = there ? min(end, b.limit + b.step * tok) : end;
-                const T* from = static_cast<const T*>(c.x.q) + (b.token0 + (long long)tok) * c.x.q_token + head * c.x.q_head;
+            for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    q[ks][u] = there ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2) : 0u;
-                    q[ks][u + 2] = there ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2 + 8) : 0u;
+                for (int u = 0; u < 2; ++u) {
+                    const int in = t * 16 + row8 + 8 * u, row = b.row0 + in;
+                    const bool there = in < b.rows;
+                    const int tok = c.x.by_G.quotient(row), head = now.h * G + row - tok * G;
+                    lim[t][u] = there ? min(end, b.limit + b.step * tok) : end;
+                    const T* from = static_cast<const T*>(c.x.q) + (b.token0 + (long long)tok) * c.x.q_token + head * c.x.q_head;
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        q[t][ks][u] = there ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2) : 0u;
+                        q[t][ks][u + 2] = there ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2 + 8) : 0u;
+                    }
+                    m[t][u] = -INFINITY;
+                    l[t][u] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < D / 8; ++j) o[t][j][2 * u] = o[t][j][2 * u + 1] = 0.f;
                 }
-                m[u] = -INFINITY;
-                l[u] = 0.f;
-            }
-#pragma unroll
-            for (int j = 0; j < D / 8; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
             fresh = false;
         }
-        cp_async_wait<kStages - 2>();
-        __syncthreads();
-        fetch(i + kStages - 1);
-        const int ahead = i + kStages;
-        longlong2 found;
-        if (ahead < n && tid < kNarrowKeys) found = place_of<false>(c, load, tid);
-
-        const uint32_t k_tile = tiles_at + (i % kStages) * 2 * kTileBytes<D>, v_tile = k_tile + kTileBytes<D>;
-        const int left = now.at.keys - now.tile * kNarrowKeys;
+        if (!wait_warp(bars + stage * 8, parity, c.status)) return;
+        const uint32_t k_tile = ring_at + stage * kStageBytes<D>, v_tile = k_tile + kNarrowKeys * kPitch16<D>;
         const int key0 = now.at.key0 + now.tile * kNarrowKeys;
-        for (int g = wk; g < kNarrowKeys / 16 && g * 16 < left; g += groups_k) {
-            float s[2][4];
+        const bool zone = key0 + kNarrowKeys > least;
+
+        float s[kTiles][2][4];
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+        for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[u][e] = 0.f;
-            const int k_row = g * 16 + (lane & 7) + ((lane >> 4) << 3), k_ch = (lane >> 3) & 1;
+            for (int e = 0; e < 4; ++e) s[t][0][e] = s[t][1][e] = 0.f;
+        const uint32_t k_row = k_tile + ((lane & 7) + ((lane >> 4) << 3)) * kPitch16<D> + ((lane >> 3) & 1) * 16;
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                uint32_t b[4];
-                ldmatrix_x4(b, k_tile + chunk_at<D>(k_row, ks * 2 + k_ch));
-                mma_16816(s[0], q[ks], b[0], b[1], T());
-                mma_16816(s[1], q[ks], b[2], b[3], T());
+        for (int ks = 0; ks < D / 16; ++ks) {
+            uint32_t b[4];
+            ldmatrix_x4(b, k_row + ks * 32);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                mma_16816(s[t][0], q[t][ks], b[0], b[1], T());
+                mma_16816(s[t][1], q[t][ks], b[2], b[3], T());
             }
-            const int key = key0 + g * 16 + quad * 2;
+        }
+        uint32_t p[kTiles][4];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
             float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[u][e] = key + u * 8 + (e & 1) < lim[e >> 1] ? s[u][e] * c.scale : -INFINITY;
-                    top[e >> 1] = fmaxf(top[e >> 1], s[u][e]);
+                    s[t][u][e] *= c.scale;
+                    if (zone && key0 + u * 8 + quad * 2 + (e & 1) >= lim[t][e >> 1]) s[t][u][e] = -INFINITY;
+                    top[e >> 1] = fmaxf(top[e >> 1], s[t][u][e]);
                 }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 1));
-                top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 2));
-            }
-            if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
-                float alpha[2];
+            // a higher maximum anywhere: all rows move to theirs
+            if (__any_sync(0xffffffffu, top[0] > m[t][0] || top[1] > m[t][1])) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const float higher = fmaxf(m[u], top[u]);
-                    alpha[u] = m[u] == higher ? 1.f : ex2(m[u] - higher);
-                    m[u] = higher;
-                    l[u] *= alpha[u];
-                }
+                    top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 1));
+                    top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 2));
+                    const float higher = fmaxf(m[t][u], top[u]), alpha = m[t][u] == higher ? 1.f : ex2(m[t][u] - higher);
+                    m[t][u] = higher;
+                    l[t][u] *= alpha;
 #pragma unroll
-                for (int j = 0; j < D / 8; ++j) {
-                    o[j][0] *= alpha[0]; o[j][1] *= alpha[0];
-                    o[j][2] *= alpha[1]; o[j][3] *= alpha[1];
+                    for (int j = 0; j < D / 8; ++j) { o[t][j][2 * u] *= alpha; o[t][j][2 * u + 1] *= alpha; }
                 }
             }
-            const float base[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+            const float base[2] = {m[t][0] == -INFINITY ? 0.f : m[t][0], m[t][1] == -INFINITY ? 0.f : m[t][1]};
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[u][e] = ex2(s[u][e] - base[e >> 1]);
-                    l[e >> 1] += s[u][e];
+                    s[t][u][e] = ex2(s[t][u][e] - base[e >> 1]);
+                    l[t][e >> 1] += s[t][u][e];
                 }
-            const uint32_t p[4] = {Pair<T>::pack(s[0][0], s[0][1]), Pair<T>::pack(s[0][2], s[0][3]), Pair<T>::pack(s[1][0], s[1][1]),
-                                   Pair<T>::pack(s[1][2], s[1][3])};
-            const int v_row = g * 16 + (lane & 15), v_ch = lane >> 4;
-            // Where some rows do not see all 16 keys, a value that is not finite must not reach them as 0 times it: such keys (there are none,
-            // as a rule) are added one by one.
-            bool odd = false;
-            if (key0 + g * 16 + 16 > least) {
-#pragma unroll
-                for (int j = 0; j < D / 8; j += 2) {
-                    uint32_t b[4];
-                    ldmatrix_x4_trans(b, v_tile + chunk_at<D>(v_row, j + v_ch));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) odd |= Pair<T>::not_finite(b[e]);
-                }
-                odd = __any_sync(0xffffffffu, odd);
-            }
-            if (odd) {
-                for (int n16 = 0; n16 < 16; ++n16) {
-                    const int from = (lane & 28) | ((n16 & 7) >> 1);
-                    const float a0 = n16 & 8 ? (n16 & 1 ? s[1][1] : s[1][0]) : (n16 & 1 ? s[0][1] : s[0][0]);
-                    const float a1 = n16 & 8 ? (n16 & 1 ? s[1][3] : s[1][2]) : (n16 & 1 ? s[0][3] : s[0][2]);
-                    const float w[2] = {Pair<T>::rounded(__shfl_sync(0xffffffffu, a0, from)), Pair<T>::rounded(__shfl_sync(0xffffffffu, a1, from))};
-                    const char* row = smem + (v_tile - tiles_at);
-#pragma unroll
-                    for (int j = 0; j < D / 8; ++j) {
-                        const T* v = reinterpret_cast<const T*>(row + chunk_at<D>(g * 16 + n16, j)) + quad * 2;
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-                            if (key0 + g * 16 + n16 < lim[u]) {
-                                o[j][2 * u] += w[u] * to_float(v[0]);
-                                o[j][2 * u + 1] += w[u] * to_float(v[1]);
-                            }
-                    }
-                }
-                continue;
-            }
+            p[t][0] = Pair<T>::pack(s[t][0][0], s[t][0][1]);
+            p[t][1] = Pair<T>::pack(s[t][0][2], s[t][0][3]);
+            p[t][2] = Pair<T>::pack(s[t][1][0], s[t][1][1]);
+            p[t][3] = Pair<T>::pack(s[t][1][2], s[t][1][3]);
+        }
+        // Where some rows do not see all 16 keys, a value that is not finite must not reach them as 0 times it: such keys (there are none,
+        // as a rule) are added one by one.
+        const uint32_t v_row = v_tile + (lane & 15) * kPitch16<D> + (lane >> 4) * 16;
+        bool odd = false;
+        if (zone) {
 #pragma unroll
             for (int j = 0; j < D / 8; j += 2) {
                 uint32_t b[4];
-                ldmatrix_x4_trans(b, v_tile + chunk_at<D>(v_row, j + v_ch));
-                mma_16816(o[j], p, b[0], b[1], T());
-                mma_16816(o[j + 1], p, b[2], b[3], T());
+                ldmatrix_x4_trans(b, v_row + j * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) odd |= Pair<T>::not_finite(b[e]);
+            }
+            odd = __any_sync(0xffffffffu, odd);
+        }
+        if (odd) {
+            for (int key = 0; key < kNarrowKeys; ++key) {
+                const int from = (lane & 28) | ((key & 7) >> 1);
+                const T* row = reinterpret_cast<const T*>(ring + (v_tile - ring_at) + key * kPitch16<D>) + quad * 2;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const float a = key & 8 ? (key & 1 ? s[t][1][2 * u + 1] : s[t][1][2 * u]) : (key & 1 ? s[t][0][2 * u + 1] : s[t][0][2 * u]);
+                        const float w = Pair<T>::rounded(__shfl_sync(0xffffffffu, a, from));
+                        if (key0 + key >= lim[t][u]) continue;
+#pragma unroll
+                        for (int j = 0; j < D / 8; ++j) {
+                            o[t][j][2 * u] += w * to_float(row[j * 8]);
+                            o[t][j][2 * u + 1] += w * to_float(row[j * 8 + 1]);
+                        }
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < D / 8; j += 2) {
+                uint32_t b[4];
+                ldmatrix_x4_trans(b, v_row + j * 16);
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    mma_16816(o[t][j], p[t], b[0], b[1], T());
+                    mma_16816(o[t][j + 1], p[t], b[2], b[3], T());
+                }
             }
         }
-        if (ahead < n && tid < kNarrowKeys) place[(ahead % kStages) * kNarrowKeys + tid] = found;
-        if (ahead + 1 < n) load.next(c);
+        __syncwarp();                            // the stage has been read
+        if (i + kStages<D> < n) {
+            fetch(i + kStages<D>, found);
+            if (i + kStages<D> + 1 < n) {
+                load.next(c);
+                found = look_up();
+            }
+        }
+        if (++stage == kStages<D>) { stage = 0; parity ^= 1; }
 
         const bool ends = now.tile + 1 == now.tiles;
         if (ends || i + 1 == n) {
-            // the unit's end, or this CTA's: join the warps that share rows, write
             const Block& b = now.at;
+            const long long unit = list.steps[now.b] + (long long)now.h * now.tiles;       // its first step
+            const bool direct = whole && ends && now.b >= own && c.plan.share[b.request].prefix < 0;
+            const long long at = direct ? 0 : piece_row<false>(c, now.b, b, now.h, worker, (int)(unit / each));
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                l[u] += __shfl_xor_sync(0xffffffffu, l[u], 1);
-                l[u] += __shfl_xor_sync(0xffffffffu, l[u], 2);
-            }
-            float all_m[2] = {m[0], m[1]}, all_l[2] = {l[0], l[1]};
-            if (groups_k > 1) {
-                if (quad == 0) {
-                    part[warp * 16 + row8] = make_float2(m[0], l[0]);
-                    part[warp * 16 + row8 + 8] = make_float2(m[1], l[1]);
-                }
-                __syncthreads();
+            for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    float top = -INFINITY, sum = 0.f;
-                    for (int w = wm; w < 4; w += groups_m) top = fmaxf(top, part[w * 16 + row8 + 8 * u].x);
-                    for (int w = wm; w < 4; w += groups_m) {
-                        const float2 p = part[w * 16 + row8 + 8 * u];
-                        if (p.x > -INFINITY) sum += p.y * ex2(p.x - top);
-                    }
-                    all_m[u] = top;
-                    all_l[u] = sum;
-                    const float f = m[u] > -INFINITY ? ex2(m[u] - top) : 0.f;
-#pragma unroll
-                    for (int j = 0; j < D / 8; ++j) { o[j][2 * u] *= f; o[j][2 * u + 1] *= f; }
-                }
-                // two row groups: one half of the values at a time, so that both fit
-                const int halves = groups_m;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    if (half >= halves) break;
-                    for (int w = 0; w < groups_k; ++w) {
-                        if (wk == w) {
-#pragma unroll
-                            for (int j = 0; j < D / 8; ++j) {
-                                if (halves == 2 && (j >= D / 16) != (half == 1)) continue;
-                                const int col = (halves == 2 ? j % (D / 16) : j) * 8 + quad * 2, pitch = halves == 2 ? D / 2 : D;
-#pragma unroll
-                                for (int u = 0; u < 2; ++u) {
-                                    float2* at = reinterpret_cast<float2*>(joined + (wm * 16 + row8 + 8 * u) * pitch + col);
-                                    float2 v = make_float2(o[j][2 * u], o[j][2 * u + 1]);
-                                    if (w > 0) { const float2 old = *at; v.x += old.x; v.y += old.y; }
-                                    if (w + 1 < groups_k) *at = v;
-                                    else { o[j][2 * u] = v.x; o[j][2 * u + 1] = v.y; }
-                                }
-                            }
-                        }
-                        __syncthreads();
-                    }
-                }
-            }
-            if (wk == groups_k - 1) {
-                const long long unit = list.steps[now.b] + (long long)now.h * now.tiles;       // its first step
-                const bool direct = whole && ends && now.b >= own && c.plan.share[b.request].prefix < 0;
-                const long long at = direct ? 0 : piece_row<false>(c, now.b, b, now.h, blockIdx.x, (int)(unit / each));
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int in = wm * 16 + row8 + 8 * u;
+                    float sum = l[t][u];
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                    const int in = t * 16 + row8 + 8 * u;
                     if (in >= b.rows) continue;
                     if (direct) {
-                        const int row = b.row0 + in, tok = row / G, head = now.h * G + row - tok * G;
-                        const float f = all_l[u] > 0.f ? 1.f / all_l[u] : all_l[u];
+                        const int row = b.row0 + in, tok = c.x.by_G.quotient(row), head = now.h * G + row - tok * G;
+                        const float f = sum > 0.f ? 1.f / sum : sum;
                         T* to = static_cast<T*>(c.x.out) + (b.token0 + (long long)tok) * c.x.out_token + head * c.x.out_head;
 #pragma unroll
                         for (int j = 0; j < D / 8; ++j)
-                            *reinterpret_cast<uint32_t*>(to + j * 8 + quad * 2) = Pair<T>::pack(o[j][2 * u] * f, o[j][2 * u + 1] * f);
-                        if (quad == 0)
-                            c.x.lse[(b.token0 + (long long)tok) * c.x.lse_token + head] = (all_m[u] + log2f(all_l[u])) * 0.6931471805599453f;
+                            *reinterpret_cast<uint32_t*>(to + j * 8 + quad * 2) = Pair<T>::pack(o[t][j][2 * u] * f, o[t][j][2 * u + 1] * f);
+                        if (quad == 0) c.x.lse[(b.token0 + (long long)tok) * c.x.lse_token + head] = (m[t][u] + log2f(sum)) * 0.6931471805599453f;
                     } else {
                         float* to = c.pieces.o + (at + in) * D;
 #pragma unroll
-                        for (int j = 0; j < D / 8; ++j) *reinterpret_cast<float2*>(to + j * 8 + quad * 2) = make_float2(o[j][2 * u], o[j][2 * u + 1]);
-                        if (quad == 0) c.pieces.ml[at + in] = make_float2(all_m[u], all_l[u]);
+                        for (int j = 0; j < D / 8; ++j)
+                            *reinterpret_cast<float2*>(to + j * 8 + quad * 2) = make_float2(o[t][j][2 * u], o[t][j][2 * u + 1]);
+                        if (quad == 0) c.pieces.ml[at + in] = make_float2(m[t][u], sum);
                     }
                 }
-            }
-            fresh = true;
-            whole = true;
+            fresh = whole = true;
         }
         if (i + 1 < n) now.next(c);
     }
-    cp_async_wait<0>();
 }
 
 // ---- pieces -------------------------------------------------------------------------------------
-// The pieces of a unit: of CTAs first .. first + count - 1.
+// The pieces of a unit: of workers first .. first + count - 1.
 struct Cut {
     int first, count;
 };
@@ -487,72 +443,81 @@ template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, int b
     const List& l = list_of<kWide>(c);
     const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
     if (tiles == 0) return Cut{0, 0};
-    const long long each = steps_each(l.head->steps, l.ctas), s0 = l.steps[b] + (long long)h * tiles;
+    const long long each = steps_each<kWide>(l), s0 = l.steps[b] + (long long)h * tiles;
     const int first = (int)(s0 / each);
     return Cut{first, (int)((s0 + tiles - 1) / each) - first + 1};
 }
 
-// A CTA a unit of the requests' own tokens, a warp a row: the pieces of the unit and those of the same row among its group's shared tokens.
+// A warp a row: its pieces among its request's own tokens and among its group's shared ones.
 template <typename T, int D, bool kWide>
-__device__ __forceinline__ void join_unit(const Call& c, int b, int h) {
+__device__ __forceinline__ void join_row(const Call& c, long long row_index, int h) {
     const int lane = threadIdx.x & 31, G = c.x.G;
-    const Block k = list_of<kWide>(c).block[b];
+    const List& list = list_of<kWide>(c);
+    const int b = find_last(list.rows, list.head->blocks, row_index), in = (int)(row_index - list.rows[b]);
+    const Block k = list.block[b];
     const Share share = c.plan.share[k.request];
     const Cut mine = cut_of<kWide>(c, b, k, h);
     if (mine.count == 1 && share.prefix < 0) return;                                // written already
-    for (int in = threadIdx.x >> 5; in < k.rows; in += 8) {
-        Cut theirs{0, 0};
-        Block p = k;
-        int pb = 0, p_in = 0;
-        if (share.prefix >= 0) {
-            const int row = share.row0 + k.row0 + in, per = share.wide ? kWideRows : kNarrowRows;
-            pb = share.prefix + row / per;
-            p_in = row % per;
-            p = (share.wide ? c.plan.wide : c.plan.narrow).block[pb];
-            theirs = share.wide ? cut_of<true>(c, pb, p, h) : cut_of<false>(c, pb, p, h);
-        }
-        auto row_of = [&](int i) -> long long {
-            if (i < mine.count) return piece_row<kWide>(c, b, k, h, mine.first + i, mine.first) + in;
-            const int cta = theirs.first + i - mine.count;
-            return (share.wide ? piece_row<true>(c, pb, p, h, cta, theirs.first) : piece_row<false>(c, pb, p, h, cta, theirs.first)) + p_in;
-        };
-        const int all = mine.count + theirs.count;
-        float top = -INFINITY;
-        for (int i = lane; i < all; i += 32) top = fmaxf(top, c.pieces.ml[row_of(i)].x);
-#pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float base = top == -INFINITY ? 0.f : top;
-        constexpr int kValues = (D + 31) / 32;
-        float acc[kValues], sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < kValues; ++j) acc[j] = 0.f;
-        for (int i0 = 0; i0 < all; i0 += 32) {
-            float w = 0.f;
-            long long at = 0;
-            if (i0 + lane < all) {
-                at = row_of(i0 + lane);
-                const float2 ml = c.pieces.ml[at];
-                w = ex2(ml.x - base);
-                sum += w * ml.y;
-            }
-            for (int i = 0; i < min(32, all - i0); ++i) {
-                const float f = __shfl_sync(0xffffffffu, w, i);
-                const float* from = c.pieces.o + __shfl_sync(0xffffffffu, at, i) * D;
-#pragma unroll
-                for (int j = 0; j < kValues; ++j)
-                    if (lane + 32 * j < D) acc[j] += f * from[lane + 32 * j];
-            }
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        const float f = sum > 0.f ? 1.f / sum : sum;                             // no key: 0, and lse -inf
-        const int row = k.row0 + in, tok = row / G, qh = h * G + row - tok * G;
-        T* to = static_cast<T*>(c.x.out) + (k.token0 + (long long)tok) * c.x.out_token + qh * c.x.out_head;
-#pragma unroll
-        for (int j = 0; j < kValues; ++j)
-            if (lane + 32 * j < D) to[lane + 32 * j] = from_float<T>(acc[j] * f);
-        if (lane == 0) c.x.lse[(k.token0 + (long long)tok) * c.x.lse_token + qh] = (base + log2f(sum)) * 0.6931471805599453f;
+    Cut theirs{0, 0};
+    Block p = k;
+    int pb = 0, p_in = 0;
+    if (share.prefix >= 0) {
+        const int row = share.row0 + k.row0 + in;
+        pb = share.wide ? share.prefix + row / kWideRows : share.prefix;
+        p_in = share.wide ? row % kWideRows : row;
+        p = (share.wide ? c.plan.wide : c.plan.narrow).block[pb];
+        theirs = share.wide ? cut_of<true>(c, pb, p, h) : cut_of<false>(c, pb, p, h);
     }
+    auto row_of = [&](int i) -> long long {
+        if (i < mine.count) return piece_row<kWide>(c, b, k, h, mine.first + i, mine.first) + in;
+        const int w = theirs.first + i - mine.count;
+        return (share.wide ? piece_row<true>(c, pb, p, h, w, theirs.first) : piece_row<false>(c, pb, p, h, w, theirs.first)) + p_in;
+    };
+    const int all = mine.count + theirs.count;
+    float top = -INFINITY;
+    for (int i = lane; i < all; i += 32) top = fmaxf(top, c.pieces.ml[row_of(i)].x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float base = top == -INFINITY ? 0.f : top;
+    constexpr int kValues = (D + 31) / 32;
+    float acc[kValues], sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < kValues; ++j) acc[j] = 0.f;
+    for (int i0 = 0; i0 < all; i0 += 32) {
+        float w = 0.f;
+        long long at = 0;
+        if (i0 + lane < all) {
+            at = row_of(i0 + lane);
+            const float2 ml = c.pieces.ml[at];
+            w = ex2(ml.x - base);
+            sum += w * ml.y;
+        }
+        const int here = min(32, all - i0);
+        for (int i = 0; i < here; i += 4) {
+            float x[4][kValues];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float* from = c.pieces.o + __shfl_sync(0xffffffffu, at, i + u) * D;
+#pragma unroll
+                for (int j = 0; j < kValues; ++j) x[u][j] = i + u < here && lane + 32 * j < D ? from[lane + 32 * j] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float f = __shfl_sync(0xffffffffu, w, i + u);
+#pragma unroll
+                for (int j = 0; j < kValues; ++j) acc[j] += f * x[u][j];
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float f = sum > 0.f ? 1.f / sum : sum;                                     // no key: 0, and lse -inf
+    const int row = k.row0 + in, tok = c.x.by_G.quotient(row), qh = h * G + row - tok * G;
+    T* to = static_cast<T*>(c.x.out) + (k.token0 + (long long)tok) * c.x.out_token + qh * c.x.out_head;
+#pragma unroll
+    for (int j = 0; j < kValues; ++j)
+        if (lane + 32 * j < D) to[lane + 32 * j] = from_float<T>(acc[j] * f);
+    if (lane == 0) c.x.lse[(k.token0 + (long long)tok) * c.x.lse_token + qh] = (base + log2f(sum)) * 0.6931471805599453f;
 }
 
 template <typename T, int D>
@@ -560,10 +525,13 @@ __global__ void __launch_bounds__(256) join_kernel(const Call c) {
     ardiff::begin_kernel();
     const int H = c.cache.heads;
     const PlanHead narrow = *c.plan.narrow.head, wide = *c.plan.wide.head;
-    const long long narrow_units = (long long)(narrow.blocks - narrow.own) * H, units = narrow_units + (long long)(wide.blocks - wide.own) * H;
-    for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        if (unit < narrow_units) join_unit<T, D, false>(c, narrow.own + (int)(unit / H), (int)(unit % H));
-        else join_unit<T, D, true>(c, wide.own + (int)((unit - narrow_units) / H), (int)((unit - narrow_units) % H));
+    const long long n0 = c.plan.narrow.rows[narrow.own], w0 = c.plan.wide.rows[wide.own];
+    const long long narrow_rows = (c.plan.narrow.rows[narrow.blocks] - n0) * H, all = narrow_rows + (c.plan.wide.rows[wide.blocks] - w0) * H;
+    for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += (long long)gridDim.x * 8) {
+        const long long j = i < narrow_rows ? i : i - narrow_rows;
+        const int h = (int)(j % H);
+        if (i < narrow_rows) join_row<T, D, false>(c, n0 + j / H, h);
+        else join_row<T, D, true>(c, w0 + j / H, h);
     }
 }
 
@@ -574,9 +542,9 @@ struct Layout {
 Layout layout(long long requests, long long groups, long long tokens, long long q_heads, long long heads, long long width) {
     Layout s;
     const long long rows = tokens * (q_heads / heads), parts = groups > 0 ? 2 : 1, ends = requests + (groups < requests ? groups : requests);
-    // narrow: a segment of 1 to 64 rows each; wide: the full blocks, and one for the end of every segment of more than 64 rows
+    // narrow: a segment each; wide: the full blocks, and one for the end of every segment of more than 16 rows
     s.narrow_blocks = (ends < parts * rows ? ends : parts * rows) + 1;
-    s.wide_blocks = parts * (rows / kWideRows + (rows / kNarrowRows < requests ? rows / kNarrowRows : requests)) + 1;
+    s.wide_blocks = parts * (rows / kWideRows + (rows / 16 < requests ? rows / 16 : requests)) + 1;
     s.main_rows = tokens * q_heads * parts;
     auto up = [](long long v) { return (v + 255) / 256 * 256; };
     long long at = 256;
@@ -587,25 +555,28 @@ Layout layout(long long requests, long long groups, long long tokens, long long 
         s.rows_at[i] = at; at = up(at + (blocks + 1) * 8);
     }
     s.share_at = at; at = up(at + requests * (long long)sizeof(Share));
-    const long long pieces = s.main_rows + (long long)kMaxCtas * kNarrowRows + (long long)kMaxWideCtas * kWideRows;
+    const long long pieces = s.main_rows + (long long)kMaxSms * (kWarps * kNarrowRows + kWideRows);
     s.ml_at = at; at = up(at + pieces * 8);
     s.o_at = at; at = up(at + pieces * width * 4);
     s.bytes = at;
     return s;
 }
 
-// Whether a block may have more than 64 rows: `most` and the number of tokens say what they can.
+// Whether a block may be wide: `most` and the number of tokens say what they can.
 bool may_be_wide(const Call& c, int most) {
     const long long news = most > 0 && most < c.x.tokens ? most : c.x.tokens;
-    return (c.groups > 0 ? c.x.tokens : news) * c.x.G > kNarrowRows;
+    return (c.groups > 0 ? c.x.tokens : news) * c.x.G > c.plan.narrow_rows;
 }
 
+template <typename T, int D, int kTiles> bool launch_narrow(const Call& c, cudaStream_t st) {
+    if (cudaFuncSetAttribute(narrow_kernel<T, D, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, kNarrowShared<D>) != cudaSuccess) return false;
+    return launch_early(narrow_kernel<T, D, kTiles>, c.plan.narrow.workers / kWarps, kThreads, 1, kNarrowShared<D>, st, c);
+}
 template <typename T, int D> bool launch(const Call& c, int32_t dtype, int most, int sms, cudaStream_t st) {
-    if (cudaFuncSetAttribute(narrow_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kNarrowShared<D>) != cudaSuccess) return false;
     const bool wide = may_be_wide(c, most);
     ardiff::set_launch_count(wide ? 4 : 3);
     return launch_early(plan_kernel, 1, kPlanThreads, 1, 0, st, c) && (!wide || launch_wide(c, dtype, D, st)) &&
-           launch_early(narrow_kernel<T, D>, c.plan.narrow.ctas, kThreads, 1, kNarrowShared<D>, st, c) &&
+           (c.plan.narrow_rows > 16 ? launch_narrow<T, D, 2>(c, st) : launch_narrow<T, D, 1>(c, st)) &&
            launch_early(join_kernel<T, D>, 8 * sms, 256, 1, 0, st, c);
 }
 template <typename T> bool launch_width(const Call& c, int32_t dtype, int width, int most, int sms, cudaStream_t st) {
@@ -679,13 +650,16 @@ extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_hea
         l.steps = reinterpret_cast<long long*>(w + s.steps_at[i]);
         l.rows = reinterpret_cast<long long*>(w + s.rows_at[i]);
     }
-    c.plan.narrow.ctas = 2 * sms < kMaxCtas ? 2 * sms : kMaxCtas;
-    c.plan.wide.ctas = sms < kMaxWideCtas ? sms : kMaxWideCtas;
+    c.plan.wide.workers = sms < kMaxSms ? sms : kMaxSms;
+    c.plan.narrow.workers = c.plan.wide.workers * kWarps;
+    // (a request's rows at most, or on average where that is not known: those of more go the wide way)
+    const int64_t news = most > 0 ? most : requests > 0 ? (tokens + requests - 1) / requests : 0;
+    c.plan.narrow_rows = news * c.x.G <= 16 ? 16 : 32;
     c.plan.share = reinterpret_cast<Share*>(w + s.share_at);
     c.pieces.ml = reinterpret_cast<float2*>(w + s.ml_at);
     c.pieces.o = reinterpret_cast<float*>(w + s.o_at);
     c.pieces.narrow_rows = s.main_rows;
-    c.pieces.wide_rows = s.main_rows + (long long)kMaxCtas * kNarrowRows;
+    c.pieces.wide_rows = s.main_rows + (long long)kMaxSms * kWarps * kNarrowRows;
     c.length = length; c.offset = offset; c.group = group; c.shared = shared; c.status = status;
     c.scale = scale * 1.4426950408889634f;
     c.requests = requests; c.groups = groups; c.causal = causal != 0;

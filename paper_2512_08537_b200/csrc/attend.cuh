@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "../../include/ardiff.h"
+#include "ptx.cuh"
 
 namespace ardiff {
 
@@ -18,8 +19,8 @@ struct Pages {                                   // strides in bytes
 };
 
 // Query rows that look at the same keys together. A segment is the new tokens of one request, or of a group of requests that share
-// their first tokens; row j of it is token token0 + j / G, query head h G + j % G (G: query heads a kv head). A block is some rows of a segment, 64 in
-// the list of narrow blocks, 256 in that of wide ones, and the keys that they see, key0 .. key0 + keys - 1. Its row j sees those from `low` on (wide
+// their first tokens; row j of it is token token0 + j / G, query head h G + j % G (G: query heads a kv head). A block is some rows of a segment, up to 16 or
+// 32 in the list of narrow blocks (a whole segment), 256 in that of wide ones, and the keys that they see, key0 .. key0 + keys - 1. Its row j sees those from `low` on (wide
 // blocks begin at a multiple of their tiles) and below limit + step * (j / G). Pages of keys all below `split` are found through row `front` of the table, the others through row `request`.
 struct Block {
     int token0, row0, rows, request, key0, keys, low, limit, step, split, front, pad;
@@ -37,7 +38,7 @@ struct Share {
     int prefix, wide, row0, shared, split, front, pad0, pad1;
 };
 
-constexpr int kNarrowRows = 64, kNarrowKeys = 64, kWideRows = 256, kWideKeys = 128;
+constexpr int kNarrowRows = 32, kNarrowKeys = 16, kWideRows = 256, kWideKeys = 128;
 template <bool kWide> struct Sizes {
     static constexpr int rows = kWide ? kWideRows : kNarrowRows, keys = kWide ? kWideKeys : kNarrowKeys;
 };
@@ -47,12 +48,13 @@ struct List {
     Block* block;
     long long* steps;                            // [blocks + 1]: steps of the blocks before
     long long* rows;                             // [blocks + 1]: rows of the blocks before
-    int ctas;                                    // that share its steps
+    int workers;                                 // that share its steps: CTAs of the wide kernel, warps of the narrow one
 };
 
 struct Plan {
     List narrow, wide;
     Share* share;                                // [requests]
+    int narrow_rows;                             // of a segment, at most, for it to be narrow: 16 or 32
 };
 
 // n / d for n < 2^31
@@ -77,12 +79,12 @@ struct Queries {                                 // strides in values
     Divide by_G;
 };
 
-// Results of a unit (a block and a kv head) in pieces: of the CTA that began it, in its rows' own place (narrow blocks' rows, then wide ones'), and
-// one of every CTA that went on with it, in that CTA's place behind all those. Values are relative to the piece's maximum, in powers of two.
+// Results of a unit (a block and a kv head) in pieces: of the worker that began it, in its rows' own place (narrow blocks' rows, then wide ones'), and
+// one of every worker that went on with it, in that one's place behind all those. Values are relative to the piece's maximum, in powers of two.
 struct Pieces {
     float* o;                                    // [rows][width]
     float2* ml;                                  // [rows]: maximum, sum
-    long long narrow_rows, wide_rows;            // where the CTAs' places begin
+    long long narrow_rows, wide_rows;            // where the workers' places begin
 };
 
 struct Call {
@@ -101,16 +103,19 @@ struct Call {
 
 template <bool kWide> __device__ __forceinline__ const List& list_of(const Call& c) { return kWide ? c.plan.wide : c.plan.narrow; }
 
-// The steps of a CTA: the same number for all but the last ones.
-__device__ __forceinline__ long long steps_each(long long steps, int ctas) { return max(1ll, (steps + ctas - 1) / ctas); }
+// The steps of a worker: the same number for all but the last ones. A narrow one (16 keys) has at least 8, so that there are not more pieces to join
+// than keys to read.
+template <bool kWide> __device__ __forceinline__ long long steps_each(const List& l) {
+    return max(kWide ? 1ll : 8ll, (l.head->steps + l.workers - 1) / l.workers);
+}
 
-template <bool kWide> __device__ __forceinline__ long long piece_row(const Call& c, int b, const Block& k, int h, int cta, int first) {
+template <bool kWide> __device__ __forceinline__ long long piece_row(const Call& c, int b, const Block& k, int h, int worker, int first) {
     const List& l = list_of<kWide>(c);
-    return cta != first ? (kWide ? c.pieces.wide_rows : c.pieces.narrow_rows) + (long long)cta * Sizes<kWide>::rows
+    return worker != first ? (kWide ? c.pieces.wide_rows : c.pieces.narrow_rows) + (long long)worker * Sizes<kWide>::rows
                         : (l.head->rows_before + l.rows[b]) * c.cache.heads + (long long)h * k.rows;
 }
 
-// Where a CTA is in the line of steps: block, head, tile of keys.
+// Where a worker is in the line of steps: block, head, tile of keys.
 template <bool kWide> struct Cursor {
     int b, h, tile, tiles;
     Block at;
@@ -153,7 +158,7 @@ template <bool kWide> __device__ __forceinline__ longlong2 place_of(const Call& 
                           id * c.cache.v_page + row * c.cache.v_token + load.h * c.cache.v_head);
 }
 
-// Blocks of more than 64 rows (attend_wide.cu).
+// The wide blocks (attend_wide.cu).
 bool launch_wide(const Call& c, int32_t dtype, int width, cudaStream_t st);
 
 // The last of n + 1 ascending numbers x[0] = 0 .. x[n] that is not above s < x[n]. All lanes of a warp call it with the same arguments.
@@ -211,6 +216,19 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// A wait with a limit of four seconds, after which the status says so. A warp's lanes get the same answer.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int32_t* status) {
+    if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
+    const unsigned long long t0 = ptx::globaltimer_ns();
+    for (int i = 0;; ++i) {
+        if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
+        if ((i & 63) == 63 && __any_sync(0xffffffffu, ptx::globaltimer_ns() - t0 > 4000000000ull)) {
+            *status = ARDIFF_ERR_TIMEOUT;
+            return false;
+        }
+    }
 }
 
 // 16-byte chunk c of row `row` of a tile of rows of D values: chunks change places with the row, or rows are a chunk longer than their values, so

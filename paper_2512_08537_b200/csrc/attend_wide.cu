@@ -1,4 +1,4 @@
-// Attention over pages for blocks of more than 64 query rows, on the tensor cores: a CTA takes 256 rows (two tiles of 128) through the
+// Attention over pages for blocks of many query rows, on the tensor cores: a CTA takes 256 rows (two tiles of 128) through the
 // tiles of 128 keys that are its share of the line of steps.
 //
 //   S_t = Q_t K^T          tcgen05, 128 x 128 in tensor memory, tile t = 0, 1
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
     const uint32_t bars = ptx::smem_u32(s_bar), at = ptx::smem_u32(smem);
     ardiff::begin_kernel();
     const List& list = c.plan.wide;
-    const long long steps = list.head->steps, each = steps_each(steps, list.ctas), begin = each * blockIdx.x;
+    const long long steps = list.head->steps, each = steps_each<true>(list), begin = each * blockIdx.x;
     if (begin >= steps) return;
     const int n = (int)(min(steps, begin + each) - begin), own = list.head->own, G = c.x.G;
     if (tid == 0) {
@@ -597,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
 
 template <typename T, int D> bool launch(const Call& c, const Boxes& boxes, cudaStream_t st) {
     if (cudaFuncSetAttribute(wide_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared<D>) != cudaSuccess) return false;
-    return launch_early(wide_kernel<T, D>, c.plan.wide.ctas, kThreads, 1, kShared<D>, st, c, boxes);
+    return launch_early(wide_kernel<T, D>, c.plan.wide.workers, kThreads, 1, kShared<D>, st, c, boxes);
 }
 template <typename T> bool launch_width(const Call& c, int width, const Boxes& boxes, cudaStream_t st) {
     switch (width) {
