@@ -566,7 +566,8 @@ int ardiff_rotary_append(const void* q, int64_t q_token, int64_t q_head, void* q
  *               [tokens][q_heads], rows lse_token apart.  tokens * q_heads < 2^31, q_heads <= ARDIFF_ROTARY_MAX_HEADS, a multiple of heads
  *   caches      as above, of the same type; head_width 64, 80, 96 or 128 (others: ERR_UNSUPPORTED). Pointers on 16-byte boundaries, strides
  *               multiples of 8 values, those of q and out too
- *   table       dev int32 [requests][width];  length  dev int32 [requests];  offset  dev int32 [requests + 1]
+ *   table       dev int32 [requests][width], width * page < 2^31, times heads < 2^34;  length  dev int32 [requests];  offset  dev
+ *               int32 [requests + 1]
  *   group       dev int32 [groups + 1], shared  dev int32 [groups]; groups == 0: NULL
  *   most        new tokens of a request at most, or 0 where that is not known: it only decides how the work is laid out
  *   status      dev int32 [1] out: ARDIFF_OK; ARDIFF_ERR_SHAPE where offsets descend or pass `tokens`, a length is negative or above

@@ -39,16 +39,30 @@ constexpr int kLeastShared = 64;
 __device__ __forceinline__ bool is_wide(const Call& c, long long rows) { return rows > c.plan.narrow_rows; }
 __device__ __forceinline__ int blocks_of(const Call& c, long long rows) { return is_wide(c, rows) ? (int)((rows + kWideRows - 1) / kWideRows) : rows > 0; }
 
+// Requests whose numbers fit here are read once; of more than that, again from memory.
+constexpr int kPlanKept = 1024;
+
+template <bool kKept>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
     __shared__ long long s_scan[32];
+    __shared__ int s_offset[kKept ? kPlanKept + 1 : 1], s_length[kKept ? kPlanKept : 1];
+    __shared__ Share s_share[kKept ? kPlanKept : 1];
     ardiff::begin_kernel();
     const int tid = threadIdx.x, lane = tid & 31, R = c.requests, G = c.x.G;
     const long long limit = (long long)c.cache.width * c.cache.page;
+    const int* offset = kKept ? s_offset : c.offset;
+    const int* length = kKept ? s_length : c.length;
+    Share* share = kKept ? s_share : c.plan.share;
     bool bad = false;
     for (int r = tid; r < R; r += kPlanThreads) {
         const int a = c.offset[r], b = c.offset[r + 1], len = c.length[r];
         bad |= a < 0 || b < a || b > c.x.tokens || len < 0 || len > limit;
-        c.plan.share[r] = Share{-1, 0, 0, 0, 0, r, 0, 0};
+        if (kKept) {
+            s_offset[r] = a;
+            if (r + 1 == R) s_offset[R] = b;
+            s_length[r] = len;
+        }
+        share[r] = Share{-1, 0, 0, 0, 0, r, 0, 0};
     }
     for (int g = tid; g < c.groups; g += kPlanThreads) {
         const int a = c.group[g], b = c.group[g + 1];
@@ -57,87 +71,90 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
     bad = __syncthreads_or(bad);
     if (tid == 0) *c.status = bad ? ARDIFF_ERR_SHAPE : ARDIFF_OK;
     if (bad) {
-        if (tid < 2) *(tid ? c.plan.wide : c.plan.narrow).head = PlanHead{0, 0, 0, 0};
+        if (tid < 2) *(tid ? c.plan.wide : c.plan.narrow).head = PlanHead{0, 0, 0, 0, 0, 0};
         return;
     }
-    // The tokens that all queries of a group see are found through its first row of the table, and read once for all, unless
-    // one request has queries, or all have so many that each fills its blocks of rows: then the same work is done, and there are no pieces to join.
-    for (int g = tid >> 5; g < c.groups; g += kPlanThreads / 32) {
-        const int r0 = c.group[g], r1 = c.group[g + 1];
-        int least = c.shared[g], active = 0, fewest = 0x7fffffff;
-        for (int r = r0 + lane; r < r1; r += 32) {
-            const int n = c.offset[r + 1] - c.offset[r];
-            if (n == 0) continue;
-            ++active;
-            fewest = min(fewest, n);
-            least = min(least, max(0, c.causal ? c.length[r] - n + 1 : c.length[r]));
-        }
-        least = __reduce_min_sync(0xffffffffu, least);
-        fewest = __reduce_min_sync(0xffffffffu, fewest);
-        active = __reduce_add_sync(0xffffffffu, active);
-        const bool once = active > 1 && least >= kLeastShared && (long long)fewest * G < kWideRows;
-        for (int r = r0 + lane; r < r1; r += 32) c.plan.share[r] = Share{-1, 0, 0, once ? least : 0, least, r0, 0, 0};
-    }
-    __syncthreads();
-
     long long blocks[2] = {0, 0};                // narrow, wide
-    // shared tokens: blocks of the group's rows
-    for (int g0 = 0; g0 < c.groups; g0 += kPlanThreads) {
-        const int g = g0 + tid;
-        int n = 0, r0 = 0, keys = 0, token0 = 0;
-        long long rows = 0;
-        if (g < c.groups) {
-            r0 = c.group[g];
-            const int r1 = c.group[g + 1];
-            if (r1 > r0) {
-                keys = c.plan.share[r0].shared;
-                token0 = c.offset[r0];
-                rows = keys > 0 ? (long long)(c.offset[r1] - token0) * G : 0;
+    if (c.groups > 0) {
+        // The tokens that all queries of a group see are found through its first row of the table, and read once for all, unless
+        // one request has queries, or all have so many that each fills its blocks of rows: then the same work is done, and there are no pieces to join.
+        for (int g = tid >> 5; g < c.groups; g += kPlanThreads / 32) {
+            const int r0 = c.group[g], r1 = c.group[g + 1];
+            int least = c.shared[g], active = 0, fewest = 0x7fffffff;
+            for (int r = r0 + lane; r < r1; r += 32) {
+                const int n = offset[r + 1] - offset[r];
+                if (n == 0) continue;
+                ++active;
+                fewest = min(fewest, n);
+                least = min(least, max(0, c.causal ? length[r] - n + 1 : length[r]));
             }
-            n = blocks_of(c, rows);
+            least = __reduce_min_sync(0xffffffffu, least);
+            fewest = __reduce_min_sync(0xffffffffu, fewest);
+            active = __reduce_add_sync(0xffffffffu, active);
+            const bool once = active > 1 && least >= kLeastShared && (long long)fewest * G < kWideRows;
+            for (int r = r0 + lane; r < r1; r += 32) share[r] = Share{-1, 0, 0, once ? least : 0, least, r0, 0, 0};
         }
-        const bool wide = is_wide(c, rows);
-        long long total;
-        const long long packed = cta_scan((long long)(wide ? 0 : n) << 32 | (wide ? n : 0), s_scan, &total);
-        const long long at = wide ? blocks[1] + (int)packed : blocks[0] + (packed >> 32);
-        const int per = wide ? kWideRows : kNarrowRows;
-        for (int j = 0; j < n; ++j) {
-            Block b;
-            b.token0 = token0; b.row0 = j * per; b.rows = (int)min((long long)per, rows - b.row0);
-            b.request = r0; b.key0 = b.low = 0; b.keys = keys; b.limit = keys; b.step = 0; b.split = 0; b.front = r0; b.pad = 0;
-            (wide ? c.plan.wide : c.plan.narrow).block[at + j] = b;
+        __syncthreads();
+        // shared tokens: blocks of the group's rows
+        for (int g0 = 0; g0 < c.groups; g0 += kPlanThreads) {
+            const int g = g0 + tid;
+            int n = 0, r0 = 0, keys = 0, token0 = 0;
+            long long rows = 0;
+            if (g < c.groups) {
+                r0 = c.group[g];
+                const int r1 = c.group[g + 1];
+                if (r1 > r0) {
+                    keys = share[r0].shared;
+                    token0 = offset[r0];
+                    rows = keys > 0 ? (long long)(offset[r1] - token0) * G : 0;
+                }
+                n = blocks_of(c, rows);
+            }
+            const bool wide = is_wide(c, rows);
+            long long total;
+            const long long packed = cta_scan((long long)(wide ? 0 : n) << 32 | (wide ? n : 0), s_scan, &total);
+            const long long at = wide ? blocks[1] + (int)packed : blocks[0] + (packed >> 32);
+            const int per = wide ? kWideRows : kNarrowRows;
+            for (int j = 0; j < n; ++j) {
+                Block b;
+                b.token0 = token0; b.row0 = j * per; b.rows = (int)min((long long)per, rows - b.row0);
+                b.request = r0; b.key0 = b.low = 0; b.keys = keys; b.limit = keys; b.step = 0; b.split = 0; b.front = r0; b.pad = 0;
+                (wide ? c.plan.wide : c.plan.narrow).block[at + j] = b;
+            }
+            if (n > 0) { share[r0].prefix = (int)at; share[r0].wide = wide; }
+            blocks[0] += total >> 32;
+            blocks[1] += (int)total;
         }
-        if (n > 0) { c.plan.share[r0].prefix = (int)at; c.plan.share[r0].wide = wide; }
-        blocks[0] += total >> 32;
-        blocks[1] += (int)total;
+        __syncthreads();
+        for (int g = tid >> 5; g < c.groups; g += kPlanThreads / 32) {
+            const int r0 = c.group[g], r1 = c.group[g + 1];
+            if (r0 == r1) continue;
+            const Share first = share[r0];
+            const int token0 = offset[r0];
+            __syncwarp();
+            for (int r = r0 + lane; r < r1 && first.prefix >= 0; r += 32) {
+                Share s = first;
+                s.row0 = (offset[r] - token0) * G;
+                share[r] = s;
+            }
+        }
     }
     const int own[2] = {(int)blocks[0], (int)blocks[1]};
-    __syncthreads();
-    for (int g = tid >> 5; g < c.groups; g += kPlanThreads / 32) {
-        const int r0 = c.group[g], r1 = c.group[g + 1];
-        if (r0 == r1) continue;
-        const Share first = c.plan.share[r0];
-        const int token0 = c.offset[r0];
-        __syncwarp();
-        for (int r = r0 + lane; r < r1 && first.prefix >= 0; r += 32) {
-            Share s = first;
-            s.row0 = (c.offset[r] - token0) * G;
-            c.plan.share[r] = s;
-        }
-    }
+    bool all_rows[2] = {false, false};
     __syncthreads();
     for (int first = 0; first < R; first += kPlanThreads) {
         const int r = first + tid;
         int n = 0, token0 = 0, len = 0, news = 0;
         long long rows = 0;
-        Share share{-1, 0, 0, 0, 0, 0, 0, 0};
+        Share mine{-1, 0, 0, 0, 0, 0, 0, 0};
         if (r < R) {
-            token0 = c.offset[r];
-            news = c.offset[r + 1] - token0;
-            len = c.length[r];
-            share = c.plan.share[r];
+            token0 = offset[r];
+            news = offset[r + 1] - token0;
+            len = length[r];
+            mine = share[r];
             rows = (long long)news * G;
             n = blocks_of(c, rows);
+            if (kKept) c.plan.share[r] = mine;
         }
         const bool wide = is_wide(c, rows);
         long long total;
@@ -147,18 +164,19 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
         for (int j = 0; j < n; ++j) {
             Block b;
             b.token0 = token0; b.row0 = j * per; b.rows = (int)min((long long)per, rows - b.row0);
-            b.request = r; b.low = share.shared; b.split = share.split; b.front = share.front; b.pad = 0;
+            b.request = r; b.low = mine.shared; b.split = mine.split; b.front = mine.front; b.pad = 0;
             b.key0 = wide ? b.low / kWideKeys * kWideKeys : b.low;
             b.step = c.causal ? 1 : 0;
             b.limit = c.causal ? len - news + 1 : len;
             const int last = min(len, b.limit + b.step * ((b.row0 + b.rows - 1) / G));
             b.keys = last > b.low ? last - b.key0 : 0;
+            all_rows[wide] |= b.keys == 0 || mine.prefix >= 0;
             (wide ? c.plan.wide : c.plan.narrow).block[at + j] = b;
         }
         blocks[0] += total >> 32;
         blocks[1] += (int)total;
     }
-    __syncthreads();
+    const int any = __syncthreads_or((all_rows[0] ? 1 : 0)) , any_wide = __syncthreads_or(all_rows[1] ? 1 : 0);
     long long before = 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -172,17 +190,17 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
                 s = (long long)((l.block[b].keys + keys - 1) / keys) * c.cache.heads;
                 w = l.block[b].rows;
             }
+            // (rows of 1024 blocks: up to 2^18; their steps: below 2^41)
             long long total;
-            const long long at = steps + cta_scan(s, s_scan, &total);
-            steps += total;
-            const long long rows_at = rows + cta_scan(w, s_scan, &total);
-            rows += total;
-            if (b < blocks[i]) { l.steps[b] = at; l.rows[b] = rows_at; }
+            const long long at = cta_scan(s << 19 | w, s_scan, &total);
+            if (b < blocks[i]) { l.steps[b] = steps + (at >> 19); l.rows[b] = rows + (at & 0x7ffff); }
+            steps += total >> 19;
+            rows += total & 0x7ffff;
         }
         if (tid == 0) {
             l.steps[blocks[i]] = steps;
             l.rows[blocks[i]] = rows;
-            *l.head = PlanHead{steps, before, (int)blocks[i], own[i]};
+            *l.head = PlanHead{steps, before, (int)blocks[i], own[i], i ? any_wide : any, 0};
         }
         before = rows;
     }
@@ -209,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const List& list = c.plan.narrow;
     const long long steps = list.head->steps, each = steps_each<false>(list);
-    const int worker = blockIdx.x * kWarps + warp;                                     // (neighbours read neighbouring keys)
+    const int worker = warp * gridDim.x + blockIdx.x;                                  // (few workers: on as many SMs)
     const long long begin = each * worker;
     if (begin >= steps) return;
     const int n = (int)(min(steps, begin + each) - begin), own = list.head->own;
@@ -450,11 +468,8 @@ template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, int b
 
 // A warp a row: its pieces among its request's own tokens and among its group's shared ones.
 template <typename T, int D, bool kWide>
-__device__ __forceinline__ void join_row(const Call& c, long long row_index, int h) {
+__device__ __forceinline__ void join_row(const Call& c, int b, const Block& k, int in, int h) {
     const int lane = threadIdx.x & 31, G = c.x.G;
-    const List& list = list_of<kWide>(c);
-    const int b = find_last(list.rows, list.head->blocks, row_index), in = (int)(row_index - list.rows[b]);
-    const Block k = list.block[b];
     const Share share = c.plan.share[k.request];
     const Cut mine = cut_of<kWide>(c, b, k, h);
     if (mine.count == 1 && share.prefix < 0) return;                                // written already
@@ -520,19 +535,42 @@ __device__ __forceinline__ void join_row(const Call& c, long long row_index, int
     if (lane == 0) c.x.lse[(k.token0 + (long long)tok) * c.x.lse_token + qh] = (base + log2f(sum)) * 0.6931471805599453f;
 }
 
+// The rows of a list: all of the requests' own, or, where nothing else is to be joined, those of units that a worker's first step cuts.
+template <typename T, int D, bool kWide>
+__device__ __forceinline__ void join_list(const Call& c) {
+    const List& list = list_of<kWide>(c);
+    const PlanHead head = *list.head;
+    const int H = c.cache.heads, warp = blockIdx.x * 8 + (threadIdx.x >> 5), warps = gridDim.x * 8;
+    if (head.all_rows) {
+        const long long first = list.rows[head.own], all = (list.rows[head.blocks] - first) * H;
+        for (long long i = warp; i < all; i += warps) {
+            const long long row = first + i / H;
+            const int b = find_last(list.rows, head.blocks, row);
+            join_row<T, D, kWide>(c, b, list.block[b], (int)(row - list.rows[b]), (int)(i % H));
+        }
+        return;
+    }
+    if (head.blocks == head.own) return;
+    const long long each = steps_each<kWide>(list);
+    const int cuts = (int)((head.steps - 1) / each), rows = kWide ? kWideRows : c.plan.narrow_rows;
+    for (int i = warp; i < cuts * rows; i += warps) {
+        const int row = i / cuts, worker = i - row * cuts + 1;
+        const long long step = each * worker;
+        const int b = find_last(list.steps, head.blocks, step);
+        const Block k = list.block[b];
+        if (row >= k.rows || b < head.own) continue;
+        const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys, h = (int)(step - list.steps[b]) / tiles;
+        const long long unit = list.steps[b] + (long long)h * tiles;
+        // (a unit that several workers cut is the first one's)
+        if (unit < step && unit >= step - each) join_row<T, D, kWide>(c, b, k, row, h);
+    }
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(256) join_kernel(const Call c) {
     ardiff::begin_kernel();
-    const int H = c.cache.heads;
-    const PlanHead narrow = *c.plan.narrow.head, wide = *c.plan.wide.head;
-    const long long n0 = c.plan.narrow.rows[narrow.own], w0 = c.plan.wide.rows[wide.own];
-    const long long narrow_rows = (c.plan.narrow.rows[narrow.blocks] - n0) * H, all = narrow_rows + (c.plan.wide.rows[wide.blocks] - w0) * H;
-    for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += (long long)gridDim.x * 8) {
-        const long long j = i < narrow_rows ? i : i - narrow_rows;
-        const int h = (int)(j % H);
-        if (i < narrow_rows) join_row<T, D, false>(c, n0 + j / H, h);
-        else join_row<T, D, true>(c, w0 + j / H, h);
-    }
+    join_list<T, D, false>(c);
+    join_list<T, D, true>(c);
 }
 
 // ---- the call -----------------------------------------------------------------------------------
@@ -575,7 +613,7 @@ template <typename T, int D, int kTiles> bool launch_narrow(const Call& c, cudaS
 template <typename T, int D> bool launch(const Call& c, int32_t dtype, int most, int sms, cudaStream_t st) {
     const bool wide = may_be_wide(c, most);
     ardiff::set_launch_count(wide ? 4 : 3);
-    return launch_early(plan_kernel, 1, kPlanThreads, 1, 0, st, c) && (!wide || launch_wide(c, dtype, D, st)) &&
+    return launch_early(c.requests <= kPlanKept ? plan_kernel<true> : plan_kernel<false>, 1, kPlanThreads, 1, 0, st, c) && (!wide || launch_wide(c, dtype, D, st)) &&
            (c.plan.narrow_rows > 16 ? launch_narrow<T, D, 2>(c, st) : launch_narrow<T, D, 1>(c, st)) &&
            launch_early(join_kernel<T, D>, 8 * sms, 256, 1, 0, st, c);
 }
@@ -618,8 +656,8 @@ extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_hea
                                    const int32_t* group, const int32_t* shared, int32_t most, float scale, int32_t causal, void* out,
                                    int64_t out_token, int64_t out_head, float* lse, int64_t lse_token, int32_t* status, void* workspace,
                                    int64_t workspace_bytes, void* stream) {
-    if (!shape(requests, groups, tokens, q_heads, heads) || pages < 0 || page < 1 || width < 0 || (int64_t)page * width >= (int64_t)1 << 31 || most < 0 ||
-        !isfinite(scale))
+    if (!shape(requests, groups, tokens, q_heads, heads) || pages < 0 || page < 1 || width < 0 || (int64_t)page * width >= (int64_t)1 << 31 ||
+        (int64_t)page * width * heads >= (int64_t)1 << 34 || most < 0 || !isfinite(scale))
         return ARDIFF_ERR_SHAPE;
     if ((dtype != ARDIFF_BF16 && dtype != ARDIFF_F16) || (head_width != 64 && head_width != 80 && head_width != 96 && head_width != 128))
         return ARDIFF_ERR_UNSUPPORTED;

@@ -30,6 +30,7 @@ struct PlanHead {
     long long steps;                             // of all blocks: key tiles times kv heads
     long long rows_before;                       // rows of the other list's blocks, in front of this one's among the pieces
     int blocks, own;                             // blocks [0, own): shared tokens; [own, blocks): the requests' own
+    int all_rows, pad;                           // whether there are rows to join beside those of units that are cut
 };
 
 // Of a request: the first block of its group's shared tokens (-1: none), in which list, and its first row there; how many shared tokens it does not read
@@ -103,10 +104,10 @@ struct Call {
 
 template <bool kWide> __device__ __forceinline__ const List& list_of(const Call& c) { return kWide ? c.plan.wide : c.plan.narrow; }
 
-// The steps of a worker: the same number for all but the last ones. A narrow one (16 keys) has at least 8, so that there are not more pieces to join
-// than keys to read.
+// The steps of a worker: the same number for all but the last ones. A narrow one (16 keys) has at least 4, so that joining the
+// pieces (a row of fp32 values each) does not take longer than reading the keys.
 template <bool kWide> __device__ __forceinline__ long long steps_each(const List& l) {
-    return max(kWide ? 1ll : 8ll, (l.head->steps + l.workers - 1) / l.workers);
+    return max(kWide ? 1ll : 4ll, (l.head->steps + l.workers - 1) / l.workers);
 }
 
 template <bool kWide> __device__ __forceinline__ long long piece_row(const Call& c, int b, const Block& k, int h, int worker, int first) {
