@@ -8,9 +8,12 @@
 // 10^5 turns and more, of which fp32 would keep no fraction; so turns are formed and reduced in fp64 (three operations a token and pair,
 // against 2 x 40 heads that use them) and only the fraction, at most half a turn, goes on in fp32. Rotations are fp32, rounded once.
 //
-// Bound by memory: every value is read once and written once. An item is a chunk of VEC pairs (two loads and two stores of up to 16 bytes),
-// or a chunk of VEC values that no pair covers. VEC is the widest that the alignment of rows, halves and pointers allows. Four items a
-// thread are under way at once.
+// Bound by memory: every value is read once and written once. Two kernels:
+//   rows_kernel    rows on 16-byte boundaries, of up to 512 bytes: a lane has one 16-byte chunk of a row, two to four rows a warp side by side, and the
+//                  cosines of that chunk in registers for all heads of the token; the other halves of pairs come by shuffles, whatever the number
+//                  of pairs (a window of two lanes' chunks, shifted). Four rows a lane under way.
+//   rotary_kernel  all others: an item is a chunk of VEC pairs (two loads and two stores) or of VEC values that no pair covers; VEC is the
+//                  widest that the alignment of rows, halves and pointers allows.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -23,6 +26,8 @@
 #include "rows.cuh"
 
 namespace {
+
+using namespace ardiff;
 
 constexpr int kThreads = 256;
 constexpr int kItems = 4;                        // items of a thread under way together
@@ -170,6 +175,170 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const Rotary a) {
     }
 }
 
+// ---- rows on 16-byte boundaries ----
+constexpr int kUnroll = 4;                       // rows of a lane under way together
+constexpr int kWarps = kThreads / 32;
+
+struct Words {
+    uint32_t w[4];
+};
+__device__ __forceinline__ Words shuffle(const uint4& x, int lane) {
+    return Words{{__shfl_sync(0xffffffffu, x.x, lane), __shfl_sync(0xffffffffu, x.y, lane), __shfl_sync(0xffffffffu, x.z, lane), __shfl_sync(0xffffffffu, x.w, lane)}};
+}
+
+// The 16 bytes from 2 s (s < 8) bytes into the chunk of lane `lane` on, the next lane's behind them.
+__device__ __forceinline__ Words window(const uint4& x, int lane, int s) {
+    const Words a = shuffle(x, lane), b = shuffle(x, lane + 1);
+    uint32_t w[8] = {a.w[0], a.w[1], a.w[2], a.w[3], b.w[0], b.w[1], b.w[2], b.w[3]};
+    if (s & 4) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (s & 2) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    if (s & 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    return Words{{w[0], w[1], w[2], w[3]}};
+}
+
+__device__ __forceinline__ uint4 to_chunk(const Words& w) { return make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]); }
+
+// kNeighbours: pairs 2 i, 2 i + 1. Else kAligned: the number of pairs fills whole chunks, so that a chunk's other halves are one other chunk.
+// `split` warps share a token.
+template <typename T, bool kNeighbours, bool kAligned, bool kAppend>
+__global__ void __launch_bounds__(kThreads) rows_kernel(const Rotary a, int lanes, int split) {
+    constexpr int N = Piece<T>::N;               // values of a chunk
+    extern __shared__ char smem[];
+    float2* cs = reinterpret_cast<float2*>(smem);                                   // [tokens][pairs]
+    ardiff::begin_kernel();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const long long t0 = (long long)blockIdx.x * a.tokens;
+    long long n = a.n;
+    if (kAppend && a.count) n = min(n, (long long)*a.count);
+    const int tokens = (int)max(0ll, min((long long)a.tokens, n - t0));
+    if (tokens == 0) return;
+    const int side = 32 / lanes, c = lane % lanes, sub = lane / lanes;              // rows side by side; chunk; which row
+    const bool mine = sub < side;
+    const int mt = warp / split;                 // of the CTA's tokens
+    const long long t = t0 + mt;
+    const int rows = a.q.heads + a.k.heads, step = side * split;
+    const T* q_in = static_cast<const T*>(a.q.in) + t * a.q.in_token + c * N;
+    const T* k_in = static_cast<const T*>(a.k.in) + t * a.k.in_token + c * N;
+    T* q_out = static_cast<T*>(a.q.out) + t * a.q.out_token + c * N;
+    T* k_out = static_cast<T*>(a.k.out) + c * N;
+    bool keys = true;                            // to be written
+    const bool there = mt < tokens;
+    if (kAppend) {
+        const long long slot = there ? a.slot[t] : -1;
+        keys = slot >= 0 && slot < a.slots;
+        if (keys) {
+            const long long pg = slot / a.page, in = slot - pg * a.page;
+            k_out += pg * a.k_page + in * a.k.out_token;
+            // values: copied as they are
+            const T* v_in = static_cast<const T*>(a.v.in) + t * a.v.in_token + c * N;
+            T* v_out = static_cast<T*>(a.v.out) + pg * a.v_page + in * a.v.out_token + c * N;
+            for (int r = (warp % split) * side + sub; mine && r < a.v.heads; r += kUnroll * step) {
+                uint4 x[kUnroll];
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u)
+                    if (r + u * step < a.v.heads) x[u] = *reinterpret_cast<const uint4*>(v_in + (long long)(r + u * step) * a.v.in_head);
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u)
+                    if (r + u * step < a.v.heads) *reinterpret_cast<uint4*>(v_out + (long long)(r + u * step) * a.v.out_head) = x[u];
+            }
+        }
+    } else {
+        k_out += t * a.k.out_token;
+    }
+    auto load = [&](int r) -> uint4 {
+        if (!mine || !there || r >= rows) return make_uint4(0u, 0u, 0u, 0u);
+        return *reinterpret_cast<const uint4*>(r < a.q.heads ? q_in + (long long)r * a.q.in_head : k_in + (long long)(r - a.q.heads) * a.k.in_head);
+    };
+    uint4 x[kUnroll];
+    const int first = (warp % split) * side + sub;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) x[u] = load(first + u * step);
+
+    for (uint32_t j = tid; j < (uint32_t)(tokens * a.pairs); j += kThreads) {
+        const uint32_t tok = quotient(j, a.by_token), i = j - tok * a.pairs;
+        const int axis = a.axis ? a.axis[i] : 0;
+        float s = 0.f, co = 1.f;                 // a pair of no axis stands still
+        if (axis >= 0 && axis < a.axes) {
+            double turns = (double)a.position[axis * a.position_ld + t0 + tok] * ((double)a.freq[i] * 0.15915494309189533577);
+            turns -= rint(turns);
+            sincospif(2.f * (float)turns, &s, &co);
+        }
+        cs[j] = make_float2(co, s * a.sign);
+    }
+    __syncthreads();
+    if (!there) return;
+
+    // out = x cos + y sin', y the pair's other value: masks say where it comes from a later place (up) or an earlier one (down), if at all
+    float co[N], si[N];
+    uint32_t up[4] = {0u, 0u, 0u, 0u}, down[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const int j = c * N + e;
+        const bool pair = j < 2 * a.pairs && mine, early = kNeighbours ? !(e & 1) : j < a.pairs;
+        const float2 w = pair ? cs[mt * a.pairs + (kNeighbours ? j >> 1 : early ? j : j - a.pairs)] : make_float2(1.f, 0.f);
+        co[e] = w.x;
+        si[e] = !pair ? -0.f : early ? -w.y : w.y;               // (x - 0 is x, whatever x is)
+        const uint32_t bits = N == 4 ? 0xffffffffu : e & 1 ? 0xffff0000u : 0xffffu;
+        if (pair && early) up[e * 4 / N] |= bits;
+        if (pair && !early) down[e * 4 / N] |= bits;
+    }
+    const int s = a.pairs % N, chunks = a.pairs / N, row_lane = lane - c;
+    const int half = c < chunks ? lane + chunks : lane - chunks;                    // (aligned) the other half's lane
+    for (int r0 = first; r0 - sub < rows; r0 += kUnroll * step) {
+        uint4 next[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) next[u] = load(r0 + (kUnroll + u) * step);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            Words y;
+            if (kNeighbours) {
+                y = N == 4 ? Words{{x[u].y, x[u].x, x[u].w, x[u].z}}
+                           : Words{{__funnelshift_r(x[u].x, x[u].x, 16), __funnelshift_r(x[u].y, x[u].y, 16), __funnelshift_r(x[u].z, x[u].z, 16), __funnelshift_r(x[u].w, x[u].w, 16)}};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y.w[i] &= up[i] | down[i];
+            } else if (kAligned) {
+                y = shuffle(x[u], half);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y.w[i] &= up[i] | down[i];
+            } else {
+                const int shift = N == 4 ? 2 * s : s;
+                const Words later = window(x[u], row_lane + c + chunks, shift), earlier = window(x[u], row_lane + c - chunks - 1, 8 - shift);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y.w[i] = (later.w[i] & up[i]) | (earlier.w[i] & down[i]);
+            }
+            const int r = r0 + u * step;
+            if (!mine || r >= rows || (kAppend && r >= a.q.heads && !keys)) continue;
+            float xs[N], ys[N];
+            unpack(x[u], xs, T());
+            unpack(to_chunk(y), ys, T());
+#pragma unroll
+            for (int e = 0; e < N; ++e) xs[e] = xs[e] * co[e] + ys[e] * si[e];
+            *reinterpret_cast<uint4*>(r < a.q.heads ? q_out + (long long)r * a.q.out_head : k_out + (long long)(r - a.q.heads) * a.k.out_head) = pack(xs, T());
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) x[u] = next[u];
+    }
+}
+
+template <typename T, bool kNeighbours, bool kAligned> bool launch_rows(const Rotary& a, bool append, unsigned grid, size_t smem, int lanes, int split, cudaStream_t st) {
+    return append ? ardiff::launch_early(rows_kernel<T, kNeighbours, kAligned, true>, grid, kThreads, 1, smem, st, a, lanes, split)
+                  : ardiff::launch_early(rows_kernel<T, kNeighbours, kAligned, false>, grid, kThreads, 1, smem, st, a, lanes, split);
+}
+template <typename T> bool launch_rows_of(const Rotary& a, bool neighbours, bool append, unsigned grid, size_t smem, int lanes, int split, cudaStream_t st) {
+    if (neighbours) return launch_rows<T, true, true>(a, append, grid, smem, lanes, split, st);
+    return a.pairs % Piece<T>::N ? launch_rows<T, false, false>(a, append, grid, smem, lanes, split, st)
+                                 : launch_rows<T, false, true>(a, append, grid, smem, lanes, split, st);
+}
+
 template <typename T, int VEC> bool launch(const Rotary& a, bool neighbours, bool append, unsigned grid, size_t smem, cudaStream_t st) {
     if (append) {
         return neighbours ? ardiff::launch_early(rotary_kernel<T, VEC, true, true>, grid, kThreads, 1, smem, st, a)
@@ -200,18 +369,35 @@ int rotary(Rotary& a, int32_t dtype, int32_t neighbours, bool append, cudaStream
     ardiff::set_launch_count(0);
     if (a.n == 0 || (a.q.heads == 0 && a.k.heads == 0)) return ARDIFF_OK;
     if (!a.position || (a.pairs > 0 && !a.freq) || (append && !a.slot)) return ARDIFF_ERR_NULL;
-    uint64_t bits = (uint64_t)a.width | (uint64_t)a.pairs;
+    uint64_t bits = (uint64_t)a.width | (uint64_t)a.pairs, bits_rows = 0;    // what a power of two divides where it divides all
     const Side* sides[3] = {&a.q, &a.k, &a.v};
     for (int i = 0; i < (append ? 3 : 2); ++i) {
         const Side& s = *sides[i];
         if (s.heads == 0) continue;
         if (!s.in || !s.out) return ARDIFF_ERR_NULL;
         if ((reinterpret_cast<uintptr_t>(s.in) | reinterpret_cast<uintptr_t>(s.out)) & (size - 1)) return ARDIFF_ERR_ALIGN;
-        bits |= places(s.in, size, s.in_token, s.heads > 1 ? s.in_head : 0) | places(s.out, size, s.out_token, s.heads > 1 ? s.out_head : 0);
+        bits_rows |= places(s.in, size, s.in_token, s.heads > 1 ? s.in_head : 0) | places(s.out, size, s.out_token, s.heads > 1 ? s.out_head : 0);
     }
-    if (append) bits |= (uint64_t)a.k_page | (uint64_t)a.v_page;
+    if (append) bits_rows |= (uint64_t)a.k_page | (uint64_t)a.v_page;
+    bits |= bits_rows;
     int vec = 16 / size;
     while (vec > 1 && (bits & (vec - 1))) vec >>= 1;
+    a.by_token = divide_by(a.pairs > 0 ? a.pairs : 1);
+    // rows of whole 16-byte chunks (neighbouring pairs never cross one)
+    const int lanes = a.width * size / 16;
+    if (lanes >= 1 && lanes <= 32 && !((bits_rows * size | (uint64_t)a.width * size) & 15)) {
+        // a warp a token; few tokens are shared by more, so that a warp's rows are few as well
+        int split = 1;
+        while (split < kWarps && a.n * split < 2368) split *= 2;
+        a.tokens = kWarps / split;
+        const unsigned grid = (unsigned)((a.n + a.tokens - 1) / a.tokens);
+        const size_t smem = (size_t)a.tokens * a.pairs * sizeof(float2);
+        const bool ok = dtype == ARDIFF_F32 ? launch_rows_of<float>(a, neighbours != 0, append, grid, smem, lanes, split, st)
+                      : dtype == ARDIFF_F16 ? launch_rows_of<__half>(a, neighbours != 0, append, grid, smem, lanes, split, st)
+                                            : launch_rows_of<__nv_bfloat16>(a, neighbours != 0, append, grid, smem, lanes, split, st);
+        ardiff::set_launch_count(1);
+        return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+    }
     const uint32_t chunks = a.pairs / vec + (a.width - 2 * a.pairs) / vec;
     const long long copies = append ? (long long)a.k.heads * (a.width / vec) : 0;
     const long long of_token = (long long)(a.q.heads + a.k.heads) * chunks + copies;
@@ -224,7 +410,6 @@ int rotary(Rotary& a, int32_t dtype, int32_t neighbours, bool append, cudaStream
     a.by_q = divide_by(a.q.heads > 0 ? a.q.heads : 1);
     a.by_k = divide_by(a.k.heads > 0 ? a.k.heads : 1);
     a.by_copies = divide_by((uint32_t)(a.width / vec));
-    a.by_token = divide_by(a.pairs > 0 ? a.pairs : 1);
     const size_t smem = (size_t)a.tokens * (a.pairs * sizeof(float2) + 16);
     const unsigned grid = (unsigned)((a.n + a.tokens - 1) / a.tokens);
     const bool ok = dtype == ARDIFF_F32 ? launch_type<float>(a, vec, neighbours != 0, append, grid, smem, st)
