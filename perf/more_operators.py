@@ -384,7 +384,7 @@ def _own_pass(s):
                                           lse=s["lse"], status=s["status"])
     if s["op"] == "weights":
         return ardiff.ardiff_attend_weights(s["q"], s["k_cache"], s["table"], s["length"], s["offset"], s["lse"], s["score"],
-                                            first=s["first"], most=s["most"], decay=s["decay"], scale=s["scale"], causal=s["causal"],
+                                            first=s["first"], decay=s["decay"], scale=s["scale"], causal=s["causal"],
                                             new_score=s["new_score"], status=s["status"])
     ardiff.ardiff_pages_evict(s["length"], s["budget"], s["score"], s["table"], s["k_cache"], s["v_cache"], first=s["first"],
                               position=s["position"], seen=s["seen"], recent=s["recent"], new_length=s["new_length"],
