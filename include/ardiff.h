@@ -598,7 +598,7 @@ int ardiff_attend_weights(const void* q, int64_t q_token, int64_t q_head, int32_
                           const void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head, int32_t pages, int32_t page,
                           int32_t heads, int32_t head_width, const int32_t* table, int32_t width, int32_t requests,
                           const int32_t* length, const int32_t* offset, const int32_t* first, const float* lse, int64_t lse_token,
-                          const float* score, int64_t ld, int32_t most, float scale, float decay, int32_t causal, float* new_score,
+                          const float* score, int64_t ld, float scale, float decay, int32_t causal, float* new_score,
                           int64_t new_ld, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Eviction. Of request r's length[r] tokens keep = min(length[r], max(budget[r], first[r])) stay: those at places below first[r], and of the

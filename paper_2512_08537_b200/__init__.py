@@ -142,7 +142,7 @@ def lib() -> ctypes.CDLL:
         L.ardiff_attend_weights_workspace.argtypes = [i32]
         L.ardiff_attend_weights.restype = ctypes.c_int
         L.ardiff_attend_weights.argtypes = [vp, i64, i64, i32, i64, i32, vp, i64, i64, i64, i32, i32, i32, i32, vp, i32, i32, vp, vp, vp,
-                                            vp, i64, vp, i64, i32, f32, f32, i32, vp, i64, vp, vp, i64, vp]
+                                            vp, i64, vp, i64, f32, f32, i32, vp, i64, vp, vp, i64, vp]
         L.ardiff_pages_evict_workspace.restype = i64
         L.ardiff_pages_evict_workspace.argtypes = [i32, i32, i32]
         L.ardiff_pages_evict.restype = ctypes.c_int
@@ -725,13 +725,13 @@ def _scores(x, R: int, index: int) -> int:
     return x.stride(0)
 
 
-def ardiff_attend_weights(q, k_cache, table, length, offset, lse, score, first=None, most=None, decay: float = 1.0, scale=None,
+def ardiff_attend_weights(q, k_cache, table, length, offset, lse, score, first=None, decay: float = 1.0, scale=None,
                           causal: bool = True, new_score=None, status=None, stream=None):
     """The attention weight that every token got from the new tokens' queries, added to decay * score (f32 [requests, places]): arguments as for
     ardiff_attend_pages, whose lse it takes. Places below first[r] (int32 [requests]) and from length[r] on are left as they are in new_score, which may
     be `score` (and is made without them being set if not given). Returns (new_score, status int32 [1])."""
     if stream is not None:
-        return _beside(ardiff_attend_weights, stream, q, k_cache, table, length, offset, lse, score, first, most, decay, scale, causal, new_score, status)
+        return _beside(ardiff_attend_weights, stream, q, k_cache, table, length, offset, lse, score, first, decay, scale, causal, new_score, status)
     index, R, width, pages, page, heads, D, T, dtype = _attend_args(q, k_cache, table, length, offset)
     qp, qt, qh, q_heads = _heads(q, index)
     _check_f32(lse, T * q_heads, index)
@@ -750,7 +750,7 @@ def ardiff_attend_weights(q, k_cache, table, length, offset, lse, score, first=N
     work = _workspace(size, "ardiff_attend_weights", q.device)
     _run(L.ardiff_attend_weights, "ardiff_attend_weights", index, qp, qt, qh, q_heads, T, dtype, *_cache_args(k_cache, q.dtype, index), pages, page,
          heads, D, table.data_ptr(), width, R, length.data_ptr(), offset.data_ptr(), _ptr(first), lse.data_ptr(), q_heads, score.data_ptr(), ld,
-         _most(most), D ** -0.5 if scale is None else scale, decay, 1 if causal else 0, new_score.data_ptr(), new_ld, status.data_ptr(),
+         D ** -0.5 if scale is None else scale, decay, 1 if causal else 0, new_score.data_ptr(), new_ld, status.data_ptr(),
          work.data_ptr(), size)
     return new_score, status
 

@@ -607,8 +607,9 @@ bool may_be_wide(const Call& c, int most) {
 }
 
 template <typename T, int D, int kTiles> bool launch_narrow(const Call& c, cudaStream_t st) {
-    if (cudaFuncSetAttribute(narrow_kernel<T, D, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, kNarrowShared<D>) != cudaSuccess) return false;
-    return launch_early(narrow_kernel<T, D, kTiles>, c.plan.narrow.workers / kWarps, kThreads, 1, kNarrowShared<D>, st, c);
+    static std::atomic<uint64_t> ready{0};
+    return shared_memory(narrow_kernel<T, D, kTiles>, kNarrowShared<D>, ready) &&
+           launch_early(narrow_kernel<T, D, kTiles>, c.plan.narrow.workers / kWarps, kThreads, 1, kNarrowShared<D>, st, c);
 }
 template <typename T, int D> bool launch(const Call& c, int32_t dtype, int most, int sms, cudaStream_t st) {
     const bool wide = may_be_wide(c, most);

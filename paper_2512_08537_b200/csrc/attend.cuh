@@ -1,5 +1,6 @@
 // What the kernels of attention over pages share: the cache, the plan of a call's work, the pieces of results that are joined.
 #pragma once
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -7,6 +8,7 @@
 
 #include "../../include/ardiff.h"
 #include "ptx.cuh"
+#include "rows.cuh"
 
 namespace ardiff {
 
@@ -219,13 +221,38 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// A wait with a limit of four seconds, after which the status says so. A warp's lanes get the same answer.
+constexpr unsigned long long kWaitLimit = 4000000000ull;   // ns
+
+// Waits give up after kWaitLimit, tell the status and make all others give up.
+struct Waits {
+    uint32_t bars;
+    volatile int* stop;
+    int32_t* status;
+    __device__ __forceinline__ bool operator()(int bar, uint32_t parity) const {
+        if (ptx::mbar_try_wait(bars + bar * 8, parity)) return true;
+        return slow(bar, parity);
+    }
+    __device__ __noinline__ bool slow(int bar, uint32_t parity) const {
+        const unsigned long long t0 = ptx::globaltimer_ns();
+        while (!*stop) {
+            for (int i = 0; i < 64; ++i)
+                if (ptx::mbar_try_wait(bars + bar * 8, parity)) return true;
+            if (ptx::globaltimer_ns() - t0 > kWaitLimit) {
+                *stop = 1;
+                *status = ARDIFF_ERR_TIMEOUT;
+            }
+        }
+        return false;
+    }
+};
+
+// A wait with the same limit, after which the status says so. A warp's lanes get the same answer.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int32_t* status) {
     if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
     const unsigned long long t0 = ptx::globaltimer_ns();
     for (int i = 0;; ++i) {
         if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
-        if ((i & 63) == 63 && __any_sync(0xffffffffu, ptx::globaltimer_ns() - t0 > 4000000000ull)) {
+        if ((i & 63) == 63 && __any_sync(0xffffffffu, ptx::globaltimer_ns() - t0 > kWaitLimit)) {
             *status = ARDIFF_ERR_TIMEOUT;
             return false;
         }
@@ -260,6 +287,29 @@ __device__ __forceinline__ long long cta_scan(long long v, long long* s, long lo
     const long long before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
     return inc - v + (warp ? before : 0);
 }
+
+// an arrival on the barrier once this thread's copies so far have landed
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// a b + c
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
+// byte of 16-byte chunk c of a row of D values, in tiles of blocks of 64 values
+__device__ __forceinline__ uint32_t swizzled(int row, int c) {
+    return (uint32_t)((c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+}
+
+// A cache as an array of four dimensions for TMA (tokens of a page, heads, pages), in boxes of `tokens` tokens and 64 values of a head, swizzled by
+// 128 bytes. False where it cannot be described so (strides of 2^40 bytes, no page): it is copied by 16 bytes then.
+bool describe(CUtensorMap* map, const char* base, bool bf16, int width, int tokens, const Pages& p, long long token, long long head, long long page);
+// The largest power of two of tokens, up to 128, that divides a page; 0 where it is below the 8 rows of a swizzled block.
+int box_tokens(int page);
 
 // The current device's SM count; 0 where that fails. Asked once a device.
 int device_sms();

@@ -38,7 +38,6 @@ constexpr int kPlaces = 4;                       // steps whose places are known
 constexpr int kRows = 128;                       // of a tile
 constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemColumns = 512;
 constexpr float kSlack = 8.f;
-constexpr unsigned long long kWaitLimit = 4000000000ull;   // ns
 
 template <int D> constexpr int kSub = (D + 63) / 64;                       // blocks of 64 values of a row
 template <int D> constexpr int kTile = kSub<D> * 128 * 128;                // bytes of 128 rows
@@ -47,41 +46,7 @@ template <int D> constexpr int kShared = 1024 + 6 * kTile<D> + kPlaces * kWideKe
 enum Bar { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + 2, kVFull = kKEmpty + 2, kVEmpty = kVFull + 2, kSFull = kVEmpty + 2, kPFull = kSFull + 2,
            kOFull = kPFull + 2, kVLanded = kOFull + 2, kDrained = kVLanded + 2, kPlaceFull, kPlaceEmpty = kPlaceFull + kPlaces, kBars = kPlaceEmpty + kPlaces };
 
-// Waits give up after kWaitLimit, tell the status and make all others give up.
-struct Waits {
-    uint32_t bars;
-    volatile int* stop;
-    int32_t* status;
-    __device__ __forceinline__ bool operator()(int bar, uint32_t parity) const {
-        if (ptx::mbar_try_wait(bars + bar * 8, parity)) return true;
-        return slow(bar, parity);
-    }
-    __device__ __noinline__ bool slow(int bar, uint32_t parity) const {
-        const unsigned long long t0 = ptx::globaltimer_ns();
-        while (!*stop) {
-            for (int i = 0; i < 64; ++i)
-                if (ptx::mbar_try_wait(bars + bar * 8, parity)) return true;
-            if (ptx::globaltimer_ns() - t0 > kWaitLimit) {
-                *stop = 1;
-                *status = ARDIFF_ERR_TIMEOUT;
-            }
-        }
-        return false;
-    }
-};
-
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-    Two r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-
-// byte of 16-byte chunk c of a row of D values, in tiles of blocks of 64 values
-__device__ __forceinline__ uint32_t swizzled(int row, int c) {
-    return (uint32_t)((c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
-}
-
-// The caches as arrays of four dimensions, copied by boxes of `tokens` tokens of a page and 64 values of a head; 0: not that way.
+// The two caches as TMA takes them; tokens 0: not that way.
 struct Boxes {
     CUtensorMap k, v;
     int tokens;
@@ -139,11 +104,6 @@ __device__ __forceinline__ void weights(uint32_t s_at, float scale, float base, 
     }
     sum = part[0] + part[1];
     top = max3(high[0], high[1], high[1]);
-}
-
-// an arrival on the barrier once this thread's copies so far have landed
-__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
 }
 
 // Keys below this are seen by all rows of a block.
@@ -596,8 +556,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
 }
 
 template <typename T, int D> bool launch(const Call& c, const Boxes& boxes, cudaStream_t st) {
-    if (cudaFuncSetAttribute(wide_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared<D>) != cudaSuccess) return false;
-    return launch_early(wide_kernel<T, D>, c.plan.wide.workers, kThreads, 1, kShared<D>, st, c, boxes);
+    static std::atomic<uint64_t> ready{0};
+    return shared_memory(wide_kernel<T, D>, kShared<D>, ready) &&
+           launch_early(wide_kernel<T, D>, c.plan.wide.workers, kThreads, 1, kShared<D>, st, c, boxes);
 }
 template <typename T> bool launch_width(const Call& c, int width, const Boxes& boxes, cudaStream_t st) {
     switch (width) {
@@ -607,6 +568,10 @@ template <typename T> bool launch_width(const Call& c, int width, const Boxes& b
         default: return launch<T, 128>(c, boxes, st);
     }
 }
+
+}  // namespace
+
+namespace {
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -623,8 +588,15 @@ EncodeTiled encoder() {
     return f;
 }
 
-// False where the cache cannot be described so (strides of 2^40 bytes, no page): it is copied by 16 bytes then.
-bool describe(CUtensorMap* map, const char* base, bool bf16, int width, int tokens, const Pages& p, long long token, long long head, long long page) {
+}  // namespace
+
+int ardiff::box_tokens(int page) {
+    int tokens = 1;
+    while (tokens < 128 && page % (2 * tokens) == 0) tokens *= 2;
+    return tokens >= 8 ? tokens : 0;
+}
+
+bool ardiff::describe(CUtensorMap* map, const char* base, bool bf16, int width, int tokens, const Pages& p, long long token, long long head, long long page) {
     if (p.page == 1) token = 16;                 // (strides of what there is one of may be anything)
     if (p.heads == 1) head = 16;
     if (p.pages == 1) page = 16;
@@ -638,15 +610,12 @@ bool describe(CUtensorMap* map, const char* base, bool bf16, int width, int toke
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-}  // namespace
-
 bool ardiff::launch_wide(const Call& c, int32_t dtype, int width, cudaStream_t st) {
     Boxes boxes;
     memset(&boxes, 0, sizeof(boxes));
-    int tokens = 1;
-    while (tokens < kWideKeys && c.cache.page % (2 * tokens) == 0) tokens *= 2;
+    const int tokens = box_tokens(c.cache.page);
     const bool bf16 = dtype == ARDIFF_BF16;
-    if (tokens >= 8 && describe(&boxes.k, c.cache.k, bf16, width, tokens, c.cache, c.cache.k_token, c.cache.k_head, c.cache.k_page) &&
+    if (tokens && describe(&boxes.k, c.cache.k, bf16, width, tokens, c.cache, c.cache.k_token, c.cache.k_head, c.cache.k_page) &&
         describe(&boxes.v, c.cache.v, bf16, width, tokens, c.cache, c.cache.v_token, c.cache.v_head, c.cache.v_page))
         boxes.tokens = tokens;
     return bf16 ? launch_width<__nv_bfloat16>(c, width, boxes, st) : launch_width<__half>(c, width, boxes, st);

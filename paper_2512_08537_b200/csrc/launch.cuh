@@ -1,7 +1,10 @@
 // Launches that may begin while the kernel before them on the stream ends, as far as it lets them.
 #pragma once
 #include <cuda_runtime.h>
+#include <stdint.h>
 #include <string.h>
+
+#include <atomic>
 
 namespace ardiff {
 
@@ -26,6 +29,17 @@ inline bool launch_early(K kernel, unsigned grid, unsigned threads, unsigned clu
     cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
     const bool ok = cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
     return cudaGetLastError() == cudaSuccess && ok;
+}
+
+// Grants a kernel `bytes` of dynamic shared memory on the current device, once a device (`ready` is the kernel's own: bits of the devices that
+// have granted it).
+template <typename K> inline bool shared_memory(K kernel, int bytes, std::atomic<uint64_t>& ready) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    if (dev < 64 && (ready.load(std::memory_order_relaxed) >> dev & 1)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    if (dev < 64) ready.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
+    return true;
 }
 
 }  // namespace ardiff

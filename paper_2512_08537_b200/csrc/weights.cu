@@ -2,10 +2,17 @@
 //
 //   new_score[r][p] = decay score[r][p] + sum over the request's new tokens i and query heads h of exp(scale q_ih.k_p - lse_ih)
 //
-// lse comes from the attention itself, so no maximum and no second pass is needed, and every key's sum stands alone: a CTA takes 64
-// keys of a request, goes through all kv heads (whose keys lie side by side in the cache), and writes each sum once. No atomics: equal calls
-// give equal bits. Keys are the left operand (a warp 16 of them) and query rows the columns, so that a sum over rows stays in a
-// thread's registers and four lanes.
+// lse comes from the attention itself, so no maximum and no second pass is needed, and every key's sum stands alone. Products are
+// transposed: 128 keys are the rows of the left operand, so that a sum over queries is one thread's (a lane of tensor memory), and up to 128
+// query rows of a head the columns, 16 at least. A CTA takes consecutive tiles of 128 keys of a request, up to 8 together, and goes through rows
+// and heads for all of them, so that queries are fetched once for 8 tiles; keys stream through four stages. Where there are fewer tiles than
+// SMs, the heads of a tile are split among CTAs, and the last of them adds the parts in their order. No atomics on sums: equal calls give equal bits.
+//
+// Bound by the keys' memory for few rows (512 bytes would be keys and values; here it is 256 a head of 128 values), by exponentials (16 a clock and SM)
+// from some 90 rows a kv head on.
+//
+// Warps: 0-3 and 4-7 sums, every other product each; 8 issues products; 9 copies keys (by TMA where pages allow, else by 16 bytes), 10 queries.
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -23,9 +30,11 @@ namespace {
 using namespace ardiff;
 
 constexpr int kPlanThreads = 1024;
-constexpr int kTileKeys = 64;
-constexpr int kThreads = 128;
-constexpr int kStages = 4;
+constexpr int kThreads = 11 * 32;
+constexpr int kKeys = 128, kRows = 128;          // of a product
+constexpr int kTogether = 8;                     // tiles of keys
+constexpr int kStages = 4, kScores = 4;          // keys in shared memory, products in tensor memory
+constexpr int kMaxSplit = 256;                   // CTAs, where heads are split among them
 
 struct Weights {
     Pages cache;
@@ -37,10 +46,20 @@ struct Weights {
     float* new_score;
     int32_t* status;
     long long* tiles;                            // [requests + 1]: tiles of the requests before
+    int* arrived;                                // [kMaxSplit]: parts of a tile that are there
+    float* part;                                 // [kMaxSplit][128]
     long long ld, new_ld, limit;
     float scale, decay;                          // scale: times log2 e
     int requests, causal;
 };
+
+struct KeyBoxes {
+    CUtensorMap k;
+    int tokens;                                  // of a box; 0: by 16 bytes
+};
+
+// The first key of a request's tiles: a multiple of 128, so that boxes of tokens do not cross pages.
+__device__ __forceinline__ int first_of(const Weights& c, int r) { return c.first ? max(0, c.first[r]) : 0; }
 
 __global__ void __launch_bounds__(kPlanThreads) tiles_kernel(const Weights c) {
     __shared__ long long s_scan[32];
@@ -54,8 +73,8 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_kernel(const Weights c) {
         if (r < R) {
             const int a = c.offset[r], b = c.offset[r + 1], len = c.length[r];
             bad |= a < 0 || b < a || b > c.x.tokens || len < 0 || len > c.limit;
-            const int first = c.first ? max(0, c.first[r]) : 0;
-            n = len > first ? (len - first + kTileKeys - 1) / kTileKeys : 0;
+            const int first = first_of(c, r);
+            n = len > first ? (len - first / kKeys * kKeys + kKeys - 1) / kKeys : 0;
         }
         long long total;
         const long long at = tiles + cta_scan(n, s_scan, &total);
@@ -63,132 +82,347 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_kernel(const Weights c) {
         tiles += total;
     }
     bad = __syncthreads_or(bad);
+    if (tid < kMaxSplit) c.arrived[tid] = 0;
     if (tid == 0) {
         *c.status = bad ? ARDIFF_ERR_SHAPE : ARDIFF_OK;
         c.tiles[R] = bad ? 0 : tiles;
     }
 }
 
-template <int D> constexpr int kTileBytes = kTileKeys * kPitch<D>;
-template <int D> constexpr int kShared = kStages * (kTileBytes<D> + kTileKeys * 8);
+// Consecutive tiles of one request that are worked on together.
+struct Segment {
+    int r, tiles, key0, keys;                    // keys: the end of the request's
+    int first, token0, news, rows, chunks;       // chunks of up to 128 of its rows
+};
+__device__ __forceinline__ Segment segment(const Weights& c, long long at, long long end) {
+    Segment s;
+    s.r = find_last(c.tiles, c.requests, at);
+    s.first = first_of(c, s.r);
+    s.key0 = s.first / kKeys * kKeys + (int)(at - c.tiles[s.r]) * kKeys;
+    s.keys = c.length[s.r];
+    s.tiles = (int)min(min(end, c.tiles[s.r + 1]) - at, (long long)kTogether);
+    s.token0 = c.offset[s.r];
+    s.news = c.offset[s.r + 1] - s.token0;
+    s.rows = s.news * c.x.G;
+    s.chunks = (s.rows + kRows - 1) / kRows;
+    return s;
+}
+
+template <int D> constexpr int kSub = (D + 63) / 64;                       // blocks of 64 values of a row
+template <int D> constexpr int kTile = kSub<D> * 128 * 128;                // bytes of 128 rows
+template <int D> constexpr int kShared = 1024 + (kStages + 2) * kTile<D> + 2 * kTogether * kKeys * 4 + kTogether * kKeys * 8 + 2 * kRows * 8;
+
+enum Bar { kKFull, kKEmpty = kKFull + kStages, kSFull = kKEmpty + kStages, kSEmpty = kSFull + kScores, kQFull = kSEmpty + kScores, kQEmpty = kQFull + 2,
+           kColFull = kQEmpty + 2, kColEmpty = kColFull + 2, kDrained = kColEmpty + 2, kBars };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) weights_kernel(const Weights c) {
-    extern __shared__ __align__(128) char smem[];
-    long long* place = reinterpret_cast<long long*>(smem + kStages * kTileBytes<D>);     // [stages][keys]
+__global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, const __grid_constant__ KeyBoxes boxes) {
+    extern __shared__ char raw[];
+    char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    constexpr int kQ = kStages * kTile<D>;
+    float* sums = reinterpret_cast<float*>(smem + kQ + 2 * kTile<D>);                 // [2][tiles][128]: every other product's
+    long long* place = reinterpret_cast<long long*>(sums + 2 * kTogether * kKeys);   // [tiles][128]: offsets of keys (odd: none), or of boxes
+    float2* column = reinterpret_cast<float2*>(place + kTogether * kKeys);           // [2][128]: -lse log2 e, keys that the row sees
+    __shared__ __align__(8) uint64_t s_bar[kBars];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_stop, s_last;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t bars = ptx::smem_u32(s_bar), smem_at = ptx::smem_u32(smem);
     ardiff::begin_kernel();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, row8 = lane >> 2;
-    const int R = c.requests, H = c.cache.heads, G = c.x.G;
-    const long long tiles = c.tiles[R];
-    const uint32_t at = ptx::smem_u32(smem);
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int r = find_last(c.tiles, R, tile);
-        const int token0 = c.offset[r], n = c.offset[r + 1] - token0, len = c.length[r];
-        const int key0 = (c.first ? max(0, c.first[r]) : 0) + (int)(tile - c.tiles[r]) * kTileKeys;
-        const int keys = min(kTileKeys, len - key0);
-        const int rows = n * G, limit = c.causal ? len - n + 1 : len;
-        __syncthreads();                         // the last tile's places have been read
-        if (tid < kTileKeys) {
-            long long p = -1;
-            if (tid < keys) {
-                const unsigned key = key0 + tid, pg = key / (unsigned)c.cache.page, in = key - pg * c.cache.page;
-                const int id = c.cache.table[(long long)r * c.cache.width + pg];
-                if (id >= 0 && id < c.cache.pages) p = id * c.cache.k_page + in * c.cache.k_token;
-                else *c.status = ARDIFF_ERR_SHAPE;
-            }
-            place[tid] = p;
+    const int H = c.cache.heads, G = c.x.G, workers = gridDim.x;
+    const long long tiles = c.tiles[c.requests];
+    if (tiles == 0) return;
+    // few tiles: `split` CTAs a tile, each some of its heads
+    const int split = tiles * 2 > workers ? 1 : min(H, (int)(workers / tiles));
+    const long long each = (tiles + workers - 1) / workers;
+    const long long begin = split > 1 ? blockIdx.x / split : each * blockIdx.x, end = split > 1 ? begin + 1 : min(tiles, begin + each);
+    if (begin >= tiles) return;
+    const int part = split > 1 ? blockIdx.x % split : 0, h0 = part * H / split, h1 = (part + 1) * H / split;
+    if (tid == 0) {
+        for (int i = 0; i < kBars; ++i) {
+            int count = 1;
+            if (i < kKEmpty) count = boxes.tokens ? 1 : 32;
+            else if (i >= kSEmpty && i < kQFull) count = 128;
+            else if ((i >= kQFull && i < kQEmpty) || (i >= kColFull && i < kColEmpty)) count = 32;
+            else if (i >= kColEmpty && i < kDrained) count = 256;
+            ptx::mbar_init(bars + i * 8, count);
         }
-        __syncthreads();
-        auto fetch = [&](int h) {
-            if (h < H && rows > 0) {
-                const uint32_t to = at + (h % kStages) * kTileBytes<D>;
-                constexpr int kChunks = D / 8;
-                for (int i = tid; i < kTileKeys * kChunks; i += kThreads) {
-                    const int row = i / kChunks, ch = i - row * kChunks;
-                    const long long p = place[row];
-                    cp_async16(to + chunk_at<D>(row, ch), c.cache.k + (p < 0 ? 0 : p + h * c.cache.k_head + ch * 16), p < 0 ? 0 : 16);
+        s_stop = 0;
+        ptx::fence_mbar_init();
+    }
+    if (warp == 8) {
+        ptx::tmem_alloc(ptx::smem_u32(&s_tmem), 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    const Waits wait{bars, &s_stop, c.status};
+    auto all = [](bool ok) { return __all_sync(0xffffffffu, ok) != 0; };     // a warp goes on or leaves as one
+    bool good = true;
+
+    if (warp == 9) {
+        // ---- keys
+        constexpr int kLanes = D / 8 <= 8 ? 8 : 16, kAtOnce = 32 / kLanes, kPeriod = 8 / kAtOnce;    // lanes a row, rows at once, before they repeat
+        const int ch = lane % kLanes, row0 = lane / kLanes, tokens = boxes.tokens;
+        const bool mine = ch < D / 8;
+        uint32_t to[kPeriod];
+#pragma unroll
+        for (int u = 0; u < kPeriod; ++u) to[u] = smem_at + swizzled(row0 + u * kAtOnce, ch);
+        uint32_t i = 0;
+        for (long long at = begin; at < end && good;) {
+            const Segment s = segment(c, at, end);
+            const int32_t* table = c.cache.table + (long long)s.r * c.cache.width;
+            const int step = tokens ? tokens : 1;
+            __syncwarp();
+            for (int j = lane; j < s.tiles * kKeys / step; j += 32) {
+                const int key = s.key0 + j * step;
+                long long p = 1;
+                if (key < s.keys) {
+                    const unsigned pg = (unsigned)key / (unsigned)c.cache.page, in = key - pg * c.cache.page;
+                    const int id = table[pg];
+                    if (id >= 0 && id < c.cache.pages) p = tokens ? (long long)id << 32 | in << 1 : id * c.cache.k_page + in * c.cache.k_token;
+                    else if (key + step > s.first) *c.status = ARDIFF_ERR_SHAPE;     // (tokens in front of the first one may lie anywhere)
                 }
+                place[j] = p;
             }
-            cp_async_commit();
-        };
-        for (int h = 0; h < kStages - 1; ++h) fetch(h);
-        float sum[2] = {0.f, 0.f};
-        for (int h = 0; h < H && rows > 0; ++h) {
-            cp_async_wait<kStages - 2>();
-            __syncthreads();
-            fetch(h + kStages - 1);
-            const uint32_t tile_at = at + (h % kStages) * kTileBytes<D>;
-            const int k_row = warp * 16 + (lane & 15), k_ch = lane >> 4;
-            uint32_t k[D / 16][4];
+            __syncwarp();
+            for (int chunk = 0; chunk < s.chunks && good; ++chunk)
+                for (int h = h0; h < h1 && good; ++h)
+                    for (int t = 0; t < s.tiles; ++t, ++i) {
+                        const int stage = i % kStages;
+                        good = all(wait(kKEmpty + stage, ((i / kStages) & 1) ^ 1));
+                        if (!good) break;
+                        const uint32_t bar = bars + (kKFull + stage) * 8;
+                        if (tokens) {
+                            const int of_tile = kKeys / tokens;
+                            const long long p = lane < of_tile ? place[t * of_tile + lane] : 1;
+                            const uint32_t there = __ballot_sync(0xffffffffu, !(p & 1));
+                            if (lane == 0) ptx::mbar_arrive_expect_tx(bar, __popc(there) * tokens * 128 * kSub<D>);
+                            __syncwarp();
+                            if (!(p & 1)) {
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) ldmatrix_x4(k[ks], tile_at + chunk_at<D>(k_row, ks * 2 + k_ch));
-            for (int row0 = 0; row0 < rows; row0 += 8) {
-                // column lane / 4 of the right operand; the result's columns are 2 quad and 2 quad + 1
-                const int row = row0 + row8, tok = row / G;
-                const T* from = static_cast<const T*>(c.x.q) + (token0 + (long long)tok) * c.x.q_token + (h * G + row - tok * G) * c.x.q_head;
-                float s[4] = {0.f, 0.f, 0.f, 0.f};
+                                for (int b = 0; b < kSub<D>; ++b)
+                                    ptx::tma_load_4d(smem_at + stage * kTile<D> + b * 16384 + lane * tokens * 128, &boxes.k, bar, b * 64, (int)(uint32_t)p >> 1, h,
+                                                     (int)(p >> 32));
+                            }
+                        } else {
+                            const long long* p = place + t * kKeys + row0;
+                            const char* from = c.cache.k + h * c.cache.k_head + ch * 16;
+#pragma unroll 1
+                            for (int j = 0; j < kKeys / kAtOnce; j += 16) {
+                                long long o[16];
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    const uint32_t b0 = row < rows ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2) : 0u;
-                    const uint32_t b1 = row < rows ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2 + 8) : 0u;
-                    mma_16816(s, k[ks], b0, b1, T());
-                }
+                                for (int u = 0; u < 16; ++u) o[u] = p[(j + u) * kAtOnce];
+                                const uint32_t base = stage * kTile<D> + (j / kPeriod) * 1024;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int col = row0 + quad * 2 + e, t = col / G;
-                    if (col >= rows) continue;
-                    const float lse = c.x.lse[(token0 + (long long)t) * c.x.lse_token + h * G + col - t * G];
-                    const float base = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f;      // a row without keys
-                    const int lim = limit + (c.causal ? t : 0), key = key0 + warp * 16 + row8;
-                    if (key < lim) sum[0] += ex2(s[e] * c.scale - base);
-                    if (key + 8 < lim) sum[1] += ex2(s[2 + e] * c.scale - base);
-                }
-            }
+                                for (int u = 0; u < 16; ++u)
+                                    if (mine) cp_async16(to[u % kPeriod] + base + (u / kPeriod) * 1024, from + (o[u] & 1 ? 0 : o[u]), o[u] & 1 ? 0 : 16);
+                            }
+                            cp_async_arrive(bar);
+                        }
+                    }
+            at += s.tiles;
         }
+        cp_async_commit();
         cp_async_wait<0>();
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 1);
-            sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 2);
-            const int in = warp * 16 + row8 + 8 * u;
-            if (quad == 0 && in < keys) {
-                const int p = key0 + in;
-                c.new_score[r * c.new_ld + p] = (p < len - n ? c.decay * c.score[r * c.ld + p] : 0.f) + sum[u];
-            }
+    } else if (warp == 10) {
+        // ---- queries, and what their columns need
+        constexpr int kLanes = D / 8 <= 8 ? 8 : 16;
+        const int ch = lane % kLanes;
+        const bool mine = ch < D / 8;
+        uint32_t u = 0;
+        for (long long at = begin; at < end && good;) {
+            const Segment s = segment(c, at, end);
+            const int limit = c.causal ? s.keys - s.news + 1 : s.keys;
+            for (int chunk = 0; chunk < s.chunks && good; ++chunk)
+                for (int h = h0; h < h1; ++h, ++u) {
+                    const int buf = u & 1, rows = min(kRows, s.rows - chunk * kRows);
+                    good = all(wait(kQEmpty + buf, ((u >> 1) & 1) ^ 1) && wait(kColEmpty + buf, ((u >> 1) & 1) ^ 1));
+                    if (!good) break;
+                    const T* base = static_cast<const T*>(c.x.q) + (long long)s.token0 * c.x.q_token + (long long)h * G * c.x.q_head + ch * 8;
+#pragma unroll 4
+                    for (int in = lane / kLanes; in < (rows + 15) / 16 * 16; in += 32 / kLanes) {
+                        const unsigned row = chunk * kRows + in, tok = c.x.by_G.quotient(row);
+                        const T* from = base + (in < rows ? tok * c.x.q_token + (row - tok * G) * c.x.q_head : 0);
+                        if (mine) cp_async16(smem_at + kQ + buf * kTile<D> + swizzled(in, ch), from, in < rows ? 16 : 0);
+                    }
+                    cp_async_arrive(bars + (kQFull + buf) * 8);
+                    for (int in = lane; in < (rows + 15) / 16 * 16; in += 32) {
+                        const unsigned row = chunk * kRows + in, tok = c.x.by_G.quotient(row);
+                        float2 v = make_float2(-INFINITY, 0.f);                        // no such row
+                        if (in < rows) {
+                            const float lse = c.x.lse[(s.token0 + (long long)tok) * c.x.lse_token + h * G + row - tok * G];
+                            v.x = lse == -INFINITY ? -INFINITY : lse * -1.4426950408889634f;      // a row without keys
+                            v.y = __int_as_float(limit + (c.causal ? (int)tok : 0));
+                        }
+                        column[buf * kRows + in] = v;
+                    }
+                    ptx::mbar_arrive(bars + (kColFull + buf) * 8);
+                }
+            at += s.tiles;
         }
+        cp_async_commit();
+        cp_async_wait<0>();
+    } else if (warp == 8) {
+        // ---- products
+        const uint64_t q_desc = ptx::smem_desc_sw128(smem_at + kQ), k_desc = ptx::smem_desc_sw128(smem_at);
+        uint32_t i = 0, u = 0;
+        for (long long at = begin; at < end && good;) {
+            const Segment s = segment(c, at, end);
+            for (int chunk = 0; chunk < s.chunks && good; ++chunk)
+                for (int h = h0; h < h1 && good; ++h, ++u) {
+                    const int rows = min(kRows, s.rows - chunk * kRows);
+                    const uint32_t idesc = ptx::idesc_16(Pair<T>::kBf16, kKeys, (rows + 15) / 16 * 16, false, false);
+                    const uint64_t b = q_desc + (u & 1) * (kTile<D> / 16);
+                    good = all(wait(kQFull + (u & 1), (u >> 1) & 1));
+                    for (int t = 0; t < s.tiles && good; ++t, ++i) {
+                        const int stage = i % kStages, to = i % kScores;
+                        good = all(wait(kKFull + stage, (i / kStages) & 1) && wait(kSEmpty + to, ((i / kScores) & 1) ^ 1));
+                        if (!good) break;
+                        ptx::fence_proxy_async_smem();
+                        ptx::tc_fence_after();
+                        const uint64_t a = k_desc + stage * (kTile<D> / 16);
+                        if (ptx::elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < D / 16; ++ks) {
+                                const uint32_t in = (ks >> 2) * 1024 + (ks & 3) * 2;
+                                ptx::mma_f16_ss(tmem + to * 128, a + in, b + in, idesc, ks > 0);
+                            }
+                            ptx::mma_commit(bars + (kSFull + to) * 8);
+                            ptx::mma_commit(bars + (kKEmpty + stage) * 8);
+                            if (t + 1 == s.tiles) ptx::mma_commit(bars + (kQEmpty + (u & 1)) * 8);
+                        }
+                        __syncwarp();
+                    }
+                }
+            at += s.tiles;
+        }
+        if (!good) {
+            // products in flight end before tensor memory is given back
+            if (ptx::elect_one()) ptx::mma_commit(bars + kDrained * 8);
+            __syncwarp();
+            for (int j = 0; j < 1 << 20 && !ptx::mbar_try_wait(bars + kDrained * 8, 0); ++j) {}
+        }
+        __syncwarp();
+    } else {
+        // ---- sums: a thread a key
+        const int side = warp >> 2, key = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
+        uint32_t i = 0, u = 0;
+        for (long long at = begin; at < end;) {
+            const Segment s = segment(c, at, end);
+            float* mine = sums + side * kTogether * kKeys + key;
+            for (int t = 0; t < s.tiles; ++t) mine[t * kKeys] = 0.f;
+            const int least = c.causal ? s.keys - s.news + 1 : s.keys;              // keys below are seen by all rows
+            for (int chunk = 0; chunk < s.chunks && good; ++chunk)
+                for (int h = h0; h < h1 && good; ++h, ++u) {
+                    const int groups = (min(kRows, s.rows - chunk * kRows) + 15) / 16;
+                    const float2* col = column + (u & 1) * kRows;
+                    good = all(wait(kColFull + (u & 1), (u >> 1) & 1));
+                    for (int t = 0; t < s.tiles && good; ++t, ++i) {
+                        if ((int)(i & 1) != side) continue;
+                        const int from = i % kScores;
+                        good = all(wait(kSFull + from, (i / kScores) & 1));
+                        if (!good) break;
+                        ptx::tc_fence_after();
+                        const int p = s.key0 + t * kKeys + key;
+                        const bool zone = s.key0 + (t + 1) * kKeys > least;
+                        float sum[2] = {0.f, 0.f};
+                        uint32_t x[2][16];
+                        ptx::tmem_ld_32x32b_x16(lanes + from * 128, x[0]);
+                        for (int g = 0; g < groups; g += 2) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                if (g + e >= groups) break;
+                                ptx::tmem_ld_wait_for(x[e]);
+                                if (g + e + 1 < groups) ptx::tmem_ld_32x32b_x16(lanes + from * 128 + (g + e + 1) * 16, x[e ^ 1]);
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) {
+                                    const float2 v = col[(g + e) * 16 + j];
+                                    const float w = ex2(fmaf(__uint_as_float(x[e][j]), c.scale, v.x));
+                                    sum[j & 1] += !zone || p < __float_as_int(v.y) ? w : 0.f;
+                                }
+                            }
+                        }
+                        ptx::tc_fence_before();
+                        ptx::mbar_arrive(bars + (kSEmpty + from) * 8);
+                        mine[t * kKeys] += sum[0] + sum[1];
+                    }
+                    ptx::mbar_arrive(bars + (kColEmpty + (u & 1)) * 8);
+                }
+            ptx::bar_sync(2, 256);               // (all eight warps come here for every segment, whether they gave up or not)
+            if (split == 1) {
+                for (int t = side; t < s.tiles; t += 2) {
+                    const int p = s.key0 + t * kKeys + key;
+                    if (p < s.first || p >= s.keys) continue;
+                    const float got = sums[t * kKeys + key] + sums[(kTogether + t) * kKeys + key];
+                    c.new_score[s.r * c.new_ld + p] = (p < s.keys - s.news ? c.decay * c.score[s.r * c.ld + p] : 0.f) + got;
+                }
+            } else {
+                float* parts = c.part + (long long)begin * split * kKeys;
+                if (side == 0) {
+                    parts[part * kKeys + key] = sums[key] + sums[kTogether * kKeys + key];
+                    __threadfence();
+                }
+                ptx::bar_sync(2, 256);
+                if (tid == 0) {
+                    s_last = atomicAdd(&c.arrived[begin], 1) == split - 1;
+                    __threadfence();
+                }
+                ptx::bar_sync(2, 256);
+                const int p = s.key0 + key;
+                if (s_last && side == 0 && p >= s.first && p < s.keys) {
+                    float got = 0.f;
+                    for (int j = 0; j < split; ++j) got += __ldcg(parts + j * kKeys + key);
+                    c.new_score[s.r * c.new_ld + p] = (p < s.keys - s.news ? c.decay * c.score[s.r * c.ld + p] : 0.f) + got;
+                }
+            }
+            ptx::bar_sync(2, 256);               // the sums have been read
+            at += s.tiles;
+        }
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 8) ptx::tmem_dealloc(tmem, 512);
+}
+
+template <typename T, int D> bool launch(const Weights& c, const KeyBoxes& boxes, int sms, cudaStream_t st) {
+    static std::atomic<uint64_t> ready{0};
+    return shared_memory(weights_kernel<T, D>, kShared<D>, ready) && launch_early(tiles_kernel, 1, kPlanThreads, 1, 0, st, c) &&
+           launch_early(weights_kernel<T, D>, sms < kMaxSplit ? sms : kMaxSplit, kThreads, 1, kShared<D>, st, c, boxes);
+}
+template <typename T> bool launch_width(const Weights& c, int width, const KeyBoxes& boxes, int sms, cudaStream_t st) {
+    switch (width) {
+        case 64: return launch<T, 64>(c, boxes, sms, st);
+        case 80: return launch<T, 80>(c, boxes, sms, st);
+        case 96: return launch<T, 96>(c, boxes, sms, st);
+        default: return launch<T, 128>(c, boxes, sms, st);
     }
 }
 
-template <typename T, int D> bool launch(const Weights& c, int sms, cudaStream_t st) {
-    if (cudaFuncSetAttribute(weights_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared<D>) != cudaSuccess) return false;
-    return launch_early(tiles_kernel, 1, kPlanThreads, 1, 0, st, c) && launch_early(weights_kernel<T, D>, 3 * sms, kThreads, 1, kShared<D>, st, c);
-}
-template <typename T> bool launch_width(const Weights& c, int width, int sms, cudaStream_t st) {
-    switch (width) {
-        case 64: return launch<T, 64>(c, sms, st);
-        case 80: return launch<T, 80>(c, sms, st);
-        case 96: return launch<T, 96>(c, sms, st);
-        default: return launch<T, 128>(c, sms, st);
-    }
-}
+// the numbers of tiles, the parts' counters, the parts
+int64_t arrived_at(int64_t requests) { return (requests + 1) * 8; }
+int64_t part_at(int64_t requests) { return (arrived_at(requests) + kMaxSplit * 4 + 255) / 256 * 256; }
 
 }  // namespace
 
 extern "C" int64_t ardiff_attend_weights_workspace(int32_t requests) {
     if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS) return ARDIFF_ERR_SHAPE;
-    return ((int64_t)requests + 1) * 8;
+    return part_at(requests) + (int64_t)kMaxSplit * kKeys * 4;
 }
 
 extern "C" int ardiff_attend_weights(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype,
                                      const void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head, int32_t pages, int32_t page,
                                      int32_t heads, int32_t head_width, const int32_t* table, int32_t width, int32_t requests,
                                      const int32_t* length, const int32_t* offset, const int32_t* first, const float* lse,
-                                     int64_t lse_token, const float* score, int64_t ld, int32_t most, float scale, float decay, int32_t causal,
+                                     int64_t lse_token, const float* score, int64_t ld, float scale, float decay, int32_t causal,
                                      float* new_score, int64_t new_ld, int32_t* status, void* workspace, int64_t workspace_bytes,
                                      void* stream) {
     if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || tokens < 0 || heads < 1 || q_heads < heads || q_heads % heads ||
         q_heads > ARDIFF_ROTARY_MAX_HEADS || tokens * q_heads >= (int64_t)1 << 31 || pages < 0 || page < 1 || width < 0 ||
-        (int64_t)page * width >= (int64_t)1 << 31 || most < 0 || ld < 0 || new_ld < 0 || !isfinite(scale) || !isfinite(decay))
+        (int64_t)page * width >= (int64_t)1 << 31 || ld < 0 || new_ld < 0 || !isfinite(scale) || !isfinite(decay))
         return ARDIFF_ERR_SHAPE;
     if ((dtype != ARDIFF_BF16 && dtype != ARDIFF_F16) || (head_width != 64 && head_width != 80 && head_width != 96 && head_width != 128))
         return ARDIFF_ERR_UNSUPPORTED;
@@ -205,16 +439,24 @@ extern "C" int ardiff_attend_weights(const void* q, int64_t q_token, int64_t q_h
     c.cache.k = static_cast<const char*>(k_cache); c.cache.k_page = k_page * 2; c.cache.k_token = k_token * 2; c.cache.k_head = k_head * 2;
     c.cache.table = table; c.cache.width = width; c.cache.page = page; c.cache.pages = pages; c.cache.heads = heads;
     c.x.q = q; c.x.lse = const_cast<float*>(lse); c.x.q_token = q_token; c.x.q_head = q_head; c.x.lse_token = lse_token;
-    c.x.heads = q_heads; c.x.G = q_heads / heads; c.x.tokens = tokens;
+    c.x.heads = q_heads; c.x.G = q_heads / heads; c.x.tokens = tokens; c.x.by_G = divide_by(q_heads / heads);
     c.length = length; c.offset = offset; c.first = first; c.score = score; c.new_score = new_score; c.status = status;
-    c.tiles = static_cast<long long*>(workspace);
+    char* w = static_cast<char*>(workspace);
+    c.tiles = reinterpret_cast<long long*>(w);
+    c.arrived = reinterpret_cast<int*>(w + arrived_at(requests));
+    c.part = reinterpret_cast<float*>(w + part_at(requests));
     c.ld = ld; c.new_ld = new_ld;
     const int64_t cap = (int64_t)page * width, rows = ld < new_ld ? ld : new_ld;
     c.limit = cap < rows ? cap : rows;
     c.scale = scale * 1.4426950408889634f; c.decay = decay;
     c.requests = requests; c.causal = causal != 0;
+    const bool bf16 = dtype == ARDIFF_BF16;
+    KeyBoxes boxes;
+    memset(&boxes, 0, sizeof(boxes));
+    const int box = box_tokens(page);
+    if (box && describe(&boxes.k, c.cache.k, bf16, head_width, box, c.cache, c.cache.k_token, c.cache.k_head, c.cache.k_page)) boxes.tokens = box;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool ok = dtype == ARDIFF_F16 ? launch_width<__half>(c, head_width, sms, st) : launch_width<__nv_bfloat16>(c, head_width, sms, st);
+    const bool ok = bf16 ? launch_width<__nv_bfloat16>(c, head_width, boxes, sms, st) : launch_width<__half>(c, head_width, boxes, sms, st);
     ardiff::set_launch_count(2);
     return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
 }

@@ -64,14 +64,14 @@ def attend():
 
 ATTEND = [(dict(requests=-1), SHAPE), (dict(requests=(1 << 20) + 1), SHAPE), (dict(tokens=-1), SHAPE), (dict(tokens=1 << 28), SHAPE), (dict(heads=0), SHAPE),
           (dict(q_heads=9), SHAPE), (dict(q_heads=1), SHAPE), (dict(q_heads=2048), SHAPE), (dict(pages=-1), SHAPE), (dict(page=0), SHAPE), (dict(width=-1), SHAPE),
-          (dict(page=1 << 16, width=1 << 15), SHAPE), (dict(most=-1), SHAPE), (dict(scale=math.inf), SHAPE), (dict(scale=math.nan), SHAPE),
+          (dict(page=1 << 16, width=1 << 15), SHAPE), (dict(scale=math.inf), SHAPE), (dict(scale=math.nan), SHAPE),
           (dict(dtype=ardiff.ARDIFF_F32), UNSUPPORTED), (dict(dtype=7), UNSUPPORTED), (dict(head_width=72), UNSUPPORTED), (dict(head_width=256), UNSUPPORTED),
           (dict(workspace_bytes=8), SHAPE), (dict(workspace_bytes=0), SHAPE), (dict(k_token=124), ALIGN), (dict(k_head=4), ALIGN), (dict(k_page=1), ALIGN),
           (dict(q_token=513), ALIGN), (dict(q_head=68), ALIGN), (dict(q=P + 8), ALIGN), (dict(k_cache=P + 8), ALIGN), (dict(workspace=P + 8), ALIGN)] + \
     [(dict([(name, None)]), NULL) for name in ("q", "k_cache", "table", "length", "offset", "lse", "status", "workspace")]
 
 
-@pytest.mark.parametrize("kw,code", ATTEND + [(dict(groups=-1), SHAPE), (dict(groups=(1 << 20) + 1), SHAPE), (dict(v_token=4), ALIGN), (dict(out_token=4), ALIGN),
+@pytest.mark.parametrize("kw,code", ATTEND + [(dict(most=-1), SHAPE), (dict(page=1 << 20, width=1 << 10, heads=16, q_heads=16), SHAPE), (dict(groups=-1), SHAPE), (dict(groups=(1 << 20) + 1), SHAPE), (dict(v_token=4), ALIGN), (dict(out_token=4), ALIGN),
                                               (dict(out_head=1), ALIGN), (dict(out=P + 2), ALIGN), (dict(v_cache=P + 2), ALIGN)] +
                          [(dict([(name, None)]), NULL) for name in ("v_cache", "out", "group", "shared")])
 def test_attend_refuses(kw, code):
@@ -80,7 +80,7 @@ def test_attend_refuses(kw, code):
 
 def weights():
     return dict(q=P, q_token=512, q_head=64, q_heads=8, tokens=4, dtype=ardiff.ARDIFF_BF16, **CACHE, pages=4, page=16, heads=2, head_width=64, table=P, width=4,
-                requests=2, length=P, offset=P, first=None, lse=P, lse_token=8, score=P, ld=64, most=1, scale=0.125, decay=1.0, causal=1, new_score=P, new_ld=64,
+                requests=2, length=P, offset=P, first=None, lse=P, lse_token=8, score=P, ld=64, scale=0.125, decay=1.0, causal=1, new_score=P, new_ld=64,
                 status=P, workspace=P, workspace_bytes=BIG, stream=None)
 
 

@@ -255,7 +255,7 @@ def test_weights(n, length, Hq, Hkv, page, D, dtype, layout):
         score = wide[:, :N]
         new = torch.full((R, N), -4.0, device=g.device)
         got, status = ardiff.ardiff_attend_weights(c.q, c.k, c.table, c.length, c.offset, lse, score.contiguous(), first=i32(first) if use_first else None,
-                                                   decay=0.75, causal=causal, new_score=new, most=max(n))
+                                                   decay=0.75, causal=causal, new_score=new)
         assert got is new and int(status) == 0
         for r in range(R):
             f = first[r] if use_first else 0
