@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
     bad = __syncthreads_or(bad);
     if (tid == 0) *c.status = bad ? ARDIFF_ERR_SHAPE : ARDIFF_OK;
     if (bad) {
-        if (tid < 2) *(tid ? c.plan.wide : c.plan.narrow).head = PlanHead{0, 0, 0, 0, 0, 0};
+        if (tid < 2) *(tid ? c.plan.wide : c.plan.narrow).head = PlanHead{0, 0, 0, 0, 0};
         return;
     }
     long long blocks[2] = {0, 0};                // narrow, wide
@@ -193,14 +193,16 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
             // (rows of 1024 blocks: up to 2^18; their steps: below 2^41)
             long long total;
             const long long at = cta_scan(s << 19 | w, s_scan, &total);
-            if (b < blocks[i]) { l.steps[b] = steps + (at >> 19); l.rows[b] = rows + (at & 0x7ffff); }
+            if (b < blocks[i]) {
+                l.steps[b] = l.block[b].first_step = steps + (at >> 19);
+                l.block[b].first_row = before + rows + (at & 0x7ffff);
+            }
             steps += total >> 19;
             rows += total & 0x7ffff;
         }
         if (tid == 0) {
             l.steps[blocks[i]] = steps;
-            l.rows[blocks[i]] = rows;
-            *l.head = PlanHead{steps, before, (int)blocks[i], own[i], i ? any_wide : any, 0};
+            *l.head = PlanHead{steps, (int)blocks[i], own[i], i ? any_wide : any, 0};
         }
         before = rows;
     }
@@ -226,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
     ardiff::begin_kernel();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const List& list = c.plan.narrow;
-    const long long steps = list.head->steps, each = steps_each<false>(list);
+    const long long steps = list.head->steps, each = steps_each<false>(steps, list.workers);
     const int worker = warp * gridDim.x + blockIdx.x;                                  // (few workers: on as many SMs)
     const long long begin = each * worker;
     if (begin >= steps) return;
@@ -418,9 +420,9 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
         const bool ends = now.tile + 1 == now.tiles;
         if (ends || i + 1 == n) {
             const Block& b = now.at;
-            const long long unit = list.steps[now.b] + (long long)now.h * now.tiles;       // its first step
+            const long long unit = now.at.first_step + (long long)now.h * now.tiles;       // its first step
             const bool direct = whole && ends && now.b >= own && c.plan.share[b.request].prefix < 0;
-            const long long at = direct ? 0 : piece_row<false>(c, now.b, b, now.h, worker, (int)(unit / each));
+            const long long at = direct ? 0 : piece_row<false>(c, b, now.h, worker, quotient_of(unit, each));
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -439,10 +441,9 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
                             *reinterpret_cast<uint32_t*>(to + j * 8 + quad * 2) = Pair<T>::pack(o[t][j][2 * u] * f, o[t][j][2 * u + 1] * f);
                         if (quad == 0) c.x.lse[(b.token0 + (long long)tok) * c.x.lse_token + head] = (m[t][u] + log2f(sum)) * 0.6931471805599453f;
                     } else {
-                        float* to = c.pieces.o + (at + in) * D;
 #pragma unroll
                         for (int j = 0; j < D / 8; ++j)
-                            *reinterpret_cast<float2*>(to + j * 8 + quad * 2) = make_float2(o[t][j][2 * u], o[t][j][2 * u + 1]);
+                            *reinterpret_cast<float2*>(piece_values(c, at, D, b.rows, in, j * 8 + quad * 2)) = make_float2(o[t][j][2 * u], o[t][j][2 * u + 1]);
                         if (quad == 0) c.pieces.ml[at + in] = make_float2(m[t][u], sum);
                     }
                 }
@@ -453,129 +454,156 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
 }
 
 // ---- pieces -------------------------------------------------------------------------------------
-// The pieces of a unit: of workers first .. first + count - 1.
+// The pieces of one row: of workers first .. first + count - 1, at row `main` of the pieces and, from the second on, at `others` + worker * cap; `rows`
+// of the block, the row's place `in` among them.
 struct Cut {
-    int first, count;
+    long long main, others;
+    int first, count, cap, rows, in;
+    __device__ __forceinline__ long long piece(int i) const { return i ? others + (long long)(first + i) * cap : main; }
 };
-template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, int b, const Block& k, int h) {
-    const List& l = list_of<kWide>(c);
+template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, long long steps, const Block& k, int h, int in) {
     const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
-    if (tiles == 0) return Cut{0, 0};
-    const long long each = steps_each<kWide>(l), s0 = l.steps[b] + (long long)h * tiles;
-    const int first = (int)(s0 / each);
-    return Cut{first, (int)((s0 + tiles - 1) / each) - first + 1};
+    Cut u;
+    u.rows = k.rows; u.in = in; u.cap = Sizes<kWide>::rows;
+    u.main = k.first_row * c.cache.heads + (long long)h * k.rows;
+    u.others = kWide ? c.pieces.wide_rows : c.pieces.narrow_rows;
+    u.first = u.count = 0;
+    if (tiles) {
+        const long long each = steps_each<kWide>(steps, list_of<kWide>(c).workers), s0 = k.first_step + (long long)h * tiles;
+        u.first = quotient_of(s0, each);
+        u.count = quotient_of(s0 + tiles - 1, each) - u.first + 1;
+    }
+    return u;
 }
 
-// A warp a row: its pieces among its request's own tokens and among its group's shared ones.
+// Eight rows of a unit and a kv head, by four warps: a lane has a row and every fourth of its groups of four values; a warp every fourth of the
+// row's pieces, those among its request's own tokens and those among its group's shared ones.
+constexpr int kJoinRows = 8, kJoinWarps = 4;
+
+template <int D> struct Joined {
+    float4 value[kJoinWarps][D / 4][kJoinRows];
+    float2 ml[kJoinWarps][kJoinRows];
+};
+
 template <typename T, int D, bool kWide>
-__device__ __forceinline__ void join_row(const Call& c, int b, const Block& k, int in, int h) {
-    const int lane = threadIdx.x & 31, G = c.x.G;
+__device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half, long long narrow_steps, long long wide_steps, const Block& k, int h, int first_row) {
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % kJoinWarps, G = c.x.G;
+    const int r = lane % kJoinRows, quarter = lane / kJoinRows, in = first_row + r;
     const Share share = c.plan.share[k.request];
-    const Cut mine = cut_of<kWide>(c, b, k, h);
+    const Cut mine = cut_of<kWide>(c, kWide ? wide_steps : narrow_steps, k, h, in);
     if (mine.count == 1 && share.prefix < 0) return;                                // written already
-    Cut theirs{0, 0};
-    Block p = k;
-    int pb = 0, p_in = 0;
-    if (share.prefix >= 0) {
+    const bool there = in < k.rows;
+    Cut theirs = mine;
+    theirs.count = 0;
+    if (share.prefix >= 0 && there) {
         const int row = share.row0 + k.row0 + in;
-        pb = share.wide ? share.prefix + row / kWideRows : share.prefix;
-        p_in = share.wide ? row % kWideRows : row;
-        p = (share.wide ? c.plan.wide : c.plan.narrow).block[pb];
-        theirs = share.wide ? cut_of<true>(c, pb, p, h) : cut_of<false>(c, pb, p, h);
+        theirs = share.wide ? cut_of<true>(c, wide_steps, c.plan.wide.block[share.prefix + row / kWideRows], h, row % kWideRows)
+                            : cut_of<false>(c, narrow_steps, c.plan.narrow.block[share.prefix], h, row);
     }
-    auto row_of = [&](int i) -> long long {
-        if (i < mine.count) return piece_row<kWide>(c, b, k, h, mine.first + i, mine.first) + in;
-        const int w = theirs.first + i - mine.count;
-        return (share.wide ? piece_row<true>(c, pb, p, h, w, theirs.first) : piece_row<false>(c, pb, p, h, w, theirs.first)) + p_in;
-    };
-    const int all = mine.count + theirs.count;
-    float top = -INFINITY;
-    for (int i = lane; i < all; i += 32) top = fmaxf(top, c.pieces.ml[row_of(i)].x);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const int all = there ? mine.count + theirs.count : 0;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll 4
+    for (int i = warp; i < all; i += kJoinWarps) {
+        const Cut& u = i < mine.count ? mine : theirs;
+        top = fmaxf(top, c.pieces.ml[u.piece(i < mine.count ? i : i - mine.count) + u.in].x);
+    }
     const float base = top == -INFINITY ? 0.f : top;
-    constexpr int kValues = (D + 31) / 32;
-    float acc[kValues], sum = 0.f;
+    float4 acc[D / 16];
 #pragma unroll
-    for (int j = 0; j < kValues; ++j) acc[j] = 0.f;
-    for (int i0 = 0; i0 < all; i0 += 32) {
-        float w = 0.f;
-        long long at = 0;
-        if (i0 + lane < all) {
-            at = row_of(i0 + lane);
-            const float2 ml = c.pieces.ml[at];
-            w = ex2(ml.x - base);
-            sum += w * ml.y;
-        }
-        const int here = min(32, all - i0);
-        for (int i = 0; i < here; i += 4) {
-            float x[4][kValues];
+    for (int j = 0; j < D / 16; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (int i = warp; i < all; i += kJoinWarps) {
+        const Cut& u = i < mine.count ? mine : theirs;
+        const long long at = u.piece(i < mine.count ? i : i - mine.count);
+        const float2 ml = c.pieces.ml[at + u.in];
+        const float* from = piece_values(c, at, D, u.rows, u.in, 4 * quarter);
+        const long long step = 16 * u.rows;
+        float4 x[D / 16];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float* from = c.pieces.o + __shfl_sync(0xffffffffu, at, i + u) * D;
+        for (int j = 0; j < D / 16; ++j) x[j] = *reinterpret_cast<const float4*>(from + j * step);
+        const float w = ex2(ml.x - base);
+        sum += w * ml.y;
 #pragma unroll
-                for (int j = 0; j < kValues; ++j) x[u][j] = i + u < here && lane + 32 * j < D ? from[lane + 32 * j] : 0.f;
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float f = __shfl_sync(0xffffffffu, w, i + u);
-#pragma unroll
-                for (int j = 0; j < kValues; ++j) acc[j] += f * x[u][j];
-            }
-        }
+        for (int j = 0; j < D / 16; ++j) { acc[j].x += w * x[j].x; acc[j].y += w * x[j].y; acc[j].z += w * x[j].z; acc[j].w += w * x[j].w; }
     }
 #pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    const float f = sum > 0.f ? 1.f / sum : sum;                                     // no key: 0, and lse -inf
+    for (int j = 0; j < D / 16; ++j) s.value[warp][4 * j + quarter][r] = acc[j];
+    if (quarter == 0) s.ml[warp][r] = make_float2(top, sum);
+    ptx::bar_sync(1 + half, 32 * kJoinWarps);
+    float all_top = -INFINITY, w[kJoinWarps];
+    float all_sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinWarps; ++i) all_top = fmaxf(all_top, s.ml[i][r].x);
+    const float all_base = all_top == -INFINITY ? 0.f : all_top;
+#pragma unroll
+    for (int i = 0; i < kJoinWarps; ++i) {
+        const float2 ml = s.ml[i][r];
+        w[i] = ml.x == -INFINITY ? 0.f : ex2(ml.x - all_base);
+        all_sum += w[i] * ml.y;
+    }
+    const float f = all_sum > 0.f ? 1.f / all_sum : all_sum;                         // no key: 0, and lse -inf
     const int row = k.row0 + in, tok = c.x.by_G.quotient(row), qh = h * G + row - tok * G;
     T* to = static_cast<T*>(c.x.out) + (k.token0 + (long long)tok) * c.x.out_token + qh * c.x.out_head;
+    for (int j = warp * 4 + quarter; there && j < D / 4; j += 4 * kJoinWarps) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < kValues; ++j)
-        if (lane + 32 * j < D) to[lane + 32 * j] = from_float<T>(acc[j] * f);
-    if (lane == 0) c.x.lse[(k.token0 + (long long)tok) * c.x.lse_token + qh] = (base + log2f(sum)) * 0.6931471805599453f;
+        for (int i = 0; i < kJoinWarps; ++i) {
+            const float4 x = s.value[i][j][r];
+            v.x += w[i] * x.x; v.y += w[i] * x.y; v.z += w[i] * x.z; v.w += w[i] * x.w;
+        }
+        *reinterpret_cast<uint2*>(to + 4 * j) = make_uint2(Pair<T>::pack(v.x * f, v.y * f), Pair<T>::pack(v.z * f, v.w * f));
+    }
+    if (there && warp == 0 && quarter == 0)
+        c.x.lse[(k.token0 + (long long)tok) * c.x.lse_token + qh] = (all_base + log2f(all_sum)) * 0.6931471805599453f;
+    ptx::bar_sync(1 + half, 32 * kJoinWarps);
 }
 
 // The rows of a list: all of the requests' own, or, where nothing else is to be joined, those of units that a worker's first step cuts.
 template <typename T, int D, bool kWide>
-__device__ __forceinline__ void join_list(const Call& c) {
+__device__ __forceinline__ void join_list(const Call& c, Joined<D>& s, int half, const PlanHead& narrow, const PlanHead& wide) {
     const List& list = list_of<kWide>(c);
-    const PlanHead head = *list.head;
-    const int H = c.cache.heads, warp = blockIdx.x * 8 + (threadIdx.x >> 5), warps = gridDim.x * 8;
+    const PlanHead& head = kWide ? wide : narrow;
+    const int H = c.cache.heads, parts = (kWide ? kWideRows : c.plan.narrow_rows) / kJoinRows;
+    const long long first = blockIdx.x * 2ll + half, step = gridDim.x * 2ll;
     if (head.all_rows) {
-        const long long first = list.rows[head.own], all = (list.rows[head.blocks] - first) * H;
-        for (long long i = warp; i < all; i += warps) {
-            const long long row = first + i / H;
-            const int b = find_last(list.rows, head.blocks, row);
-            join_row<T, D, kWide>(c, b, list.block[b], (int)(row - list.rows[b]), (int)(i % H));
+        const long long units = (long long)(head.blocks - head.own) * H;
+        for (long long i = first; i < units * parts; i += step) {
+            const long long unit = i / parts;
+            const int b = head.own + (int)(unit / H), row = (int)(i - unit * parts) * kJoinRows;
+            const Block k = list.block[b];
+            if (row < k.rows) join_rows<T, D, kWide>(c, s, half, narrow.steps, wide.steps, k, (int)(unit % H), row);
         }
         return;
     }
     if (head.blocks == head.own) return;
-    const long long each = steps_each<kWide>(list);
-    const int cuts = (int)((head.steps - 1) / each), rows = kWide ? kWideRows : c.plan.narrow_rows;
-    for (int i = warp; i < cuts * rows; i += warps) {
-        const int row = i / cuts, worker = i - row * cuts + 1;
-        const long long step = each * worker;
-        const int b = find_last(list.steps, head.blocks, step);
+    const long long each = steps_each<kWide>(head.steps, list.workers);
+    const int cuts = (int)((head.steps - 1) / each);
+    for (long long i = first; i < (long long)cuts * parts; i += step) {
+        const int row = (int)(i / cuts) * kJoinRows;
+        const long long at = each * (i % cuts + 1);
+        const int b = find_last(list.steps, head.blocks, at);
         const Block k = list.block[b];
         if (row >= k.rows || b < head.own) continue;
-        const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys, h = (int)(step - list.steps[b]) / tiles;
-        const long long unit = list.steps[b] + (long long)h * tiles;
+        const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys, h = (int)(at - k.first_step) / tiles;
+        const long long unit = k.first_step + (long long)h * tiles;
         // (a unit that several workers cut is the first one's)
-        if (unit < step && unit >= step - each) join_row<T, D, kWide>(c, b, k, row, h);
+        if (unit < at && unit >= at - each) join_rows<T, D, kWide>(c, s, half, narrow.steps, wide.steps, k, h, row);
     }
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256) join_kernel(const Call c) {
+    __shared__ Joined<D> s[2];
     ardiff::begin_kernel();
-    join_list<T, D, false>(c);
-    join_list<T, D, true>(c);
+    const int half = threadIdx.x >> 7;
+    const PlanHead narrow = *c.plan.narrow.head, wide = *c.plan.wide.head;
+    join_list<T, D, false>(c, s[half], half, narrow, wide);
+    join_list<T, D, true>(c, s[half], half, narrow, wide);
 }
 
 // ---- the call -----------------------------------------------------------------------------------
 struct Layout {
-    long long narrow_blocks, wide_blocks, main_rows, bytes, block_at[2], steps_at[2], rows_at[2], share_at, ml_at, o_at;
+    long long narrow_blocks, wide_blocks, main_rows, bytes, block_at[2], steps_at[2], share_at, ml_at, o_at;
 };
 Layout layout(long long requests, long long groups, long long tokens, long long q_heads, long long heads, long long width) {
     Layout s;
@@ -590,7 +618,6 @@ Layout layout(long long requests, long long groups, long long tokens, long long 
         const long long blocks = i ? s.wide_blocks : s.narrow_blocks;
         s.block_at[i] = at; at = up(at + blocks * (long long)sizeof(Block));
         s.steps_at[i] = at; at = up(at + (blocks + 1) * 8);
-        s.rows_at[i] = at; at = up(at + (blocks + 1) * 8);
     }
     s.share_at = at; at = up(at + requests * (long long)sizeof(Share));
     const long long pieces = s.main_rows + (long long)kMaxSms * (kWarps * kNarrowRows + kWideRows);
@@ -616,7 +643,7 @@ template <typename T, int D> bool launch(const Call& c, int32_t dtype, int most,
     ardiff::set_launch_count(wide ? 4 : 3);
     return launch_early(c.requests <= kPlanKept ? plan_kernel<true> : plan_kernel<false>, 1, kPlanThreads, 1, 0, st, c) && (!wide || launch_wide(c, dtype, D, st)) &&
            (c.plan.narrow_rows > 16 ? launch_narrow<T, D, 2>(c, st) : launch_narrow<T, D, 1>(c, st)) &&
-           launch_early(join_kernel<T, D>, 8 * sms, 256, 1, 0, st, c);
+           launch_early(join_kernel<T, D>, 4 * sms, 256, 1, 0, st, c);
 }
 template <typename T> bool launch_width(const Call& c, int32_t dtype, int width, int most, int sms, cudaStream_t st) {
     switch (width) {
@@ -687,7 +714,6 @@ extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_hea
         l.head = reinterpret_cast<PlanHead*>(w) + i;
         l.block = reinterpret_cast<Block*>(w + s.block_at[i]);
         l.steps = reinterpret_cast<long long*>(w + s.steps_at[i]);
-        l.rows = reinterpret_cast<long long*>(w + s.rows_at[i]);
     }
     c.plan.wide.workers = sms < kMaxSms ? sms : kMaxSms;
     c.plan.narrow.workers = c.plan.wide.workers * kWarps;

@@ -24,13 +24,13 @@ struct Pages {                                   // strides in bytes
 // their first tokens; row j of it is token token0 + j / G, query head h G + j % G (G: query heads a kv head). A block is some rows of a segment, up to 16 or
 // 32 in the list of narrow blocks (a whole segment), 256 in that of wide ones, and the keys that they see, key0 .. key0 + keys - 1. Its row j sees those from `low` on (wide
 // blocks begin at a multiple of their tiles) and below limit + step * (j / G). Pages of keys all below `split` are found through row `front` of the table, the others through row `request`.
-struct Block {
+struct alignas(16) Block {
     int token0, row0, rows, request, key0, keys, low, limit, step, split, front, pad;
+    long long first_step, first_row;             // steps of the list's blocks before; rows of all blocks before, the narrow list's first
 };
 
 struct PlanHead {
     long long steps;                             // of all blocks: key tiles times kv heads
-    long long rows_before;                       // rows of the other list's blocks, in front of this one's among the pieces
     int blocks, own;                             // blocks [0, own): shared tokens; [own, blocks): the requests' own
     int all_rows, pad;                           // whether there are rows to join beside those of units that are cut
 };
@@ -50,7 +50,6 @@ struct List {
     PlanHead* head;
     Block* block;
     long long* steps;                            // [blocks + 1]: steps of the blocks before
-    long long* rows;                             // [blocks + 1]: rows of the blocks before
     int workers;                                 // that share its steps: CTAs of the wide kernel, warps of the narrow one
 };
 
@@ -83,9 +82,10 @@ struct Queries {                                 // strides in values
 };
 
 // Results of a unit (a block and a kv head) in pieces: of the worker that began it, in its rows' own place (narrow blocks' rows, then wide ones'), and
-// one of every worker that went on with it, in that one's place behind all those. Values are relative to the piece's maximum, in powers of two.
+// one of every worker that went on with it, in that one's place behind all those. Values are relative to the piece's maximum, in powers of two, and lie
+// four of a row together, the rows of the block behind one another, so that threads with a row each write side by side.
 struct Pieces {
-    float* o;                                    // [rows][width]
+    float* o;                                    // a piece: [width / 4][rows of the block][4]
     float2* ml;                                  // [rows]: maximum, sum
     long long narrow_rows, wide_rows;            // where the workers' places begin
 };
@@ -108,14 +108,21 @@ template <bool kWide> __device__ __forceinline__ const List& list_of(const Call&
 
 // The steps of a worker: the same number for all but the last ones. A narrow one (16 keys) has at least 4, so that joining the
 // pieces (a row of fp32 values each) does not take longer than reading the keys.
-template <bool kWide> __device__ __forceinline__ long long steps_each(const List& l) {
-    return max(kWide ? 1ll : 4ll, (l.head->steps + l.workers - 1) / l.workers);
+template <bool kWide> __device__ __forceinline__ long long steps_each(long long steps, int workers) {
+    return max(kWide ? 1ll : 4ll, (steps + workers - 1) / workers);
+}
+// a / b for numbers that hardly ever need 64 bits
+__device__ __forceinline__ int quotient_of(long long a, long long b) {
+    return (a | b) >> 32 ? (int)(a / b) : (int)((uint32_t)a / (uint32_t)b);
 }
 
-template <bool kWide> __device__ __forceinline__ long long piece_row(const Call& c, int b, const Block& k, int h, int worker, int first) {
-    const List& l = list_of<kWide>(c);
+template <bool kWide> __device__ __forceinline__ long long piece_row(const Call& c, const Block& k, int h, int worker, int first) {
     return worker != first ? (kWide ? c.pieces.wide_rows : c.pieces.narrow_rows) + (long long)worker * Sizes<kWide>::rows
-                        : (l.head->rows_before + l.rows[b]) * c.cache.heads + (long long)h * k.rows;
+                           : k.first_row * c.cache.heads + (long long)h * k.rows;
+}
+
+__device__ __forceinline__ float* piece_values(const Call& c, long long piece, int width, int rows, int row, int value) {
+    return c.pieces.o + piece * width + ((long long)(value >> 2) * rows + row) * 4 + (value & 3);
 }
 
 // Where a worker is in the line of steps: block, head, tile of keys.
@@ -129,7 +136,7 @@ template <bool kWide> struct Cursor {
     __device__ __forceinline__ void start(const Call& c, int block, long long step) {
         b = block;
         enter(c);
-        const int in = (int)(step - list_of<kWide>(c).steps[b]);          // heads times tiles of a block: below 2^31
+        const int in = (int)(step - at.first_step);          // heads times tiles of a block: below 2^31
         h = in / tiles;
         tile = in - h * tiles;
     }

@@ -10,7 +10,7 @@
 // The maximum only moves when it would grow by more than 8 (a factor 256 that P and the sums hold easily): then O is rescaled in
 // tensor memory, which is rare; the product that last wrote O is done by then, since its successor S_t is issued after it.
 //
-// Warps: 0-3 and 4-7 the rows of tile 0 and 1 (a thread a row), 8 issues products, 9 copies keys, 10 values, 11 queries. Pages of a multiple of 8 tokens
+// Warps: 0-3 and 4-7 the rows of tile 0 and 1 (a thread a row), 8 issues products, 9 copies keys, 10 values (the rows' warps their queries). Pages of a multiple of 8 tokens
 // come by TMA, in boxes of the largest power of two of tokens that divides a page (a lane looks up and copies a box). Others come by asynchronous
 // 16-byte copies, 64 a lane and tile, into the same 128-byte-swizzled layout; their places warp 11 looks up, up to four steps ahead. Those
 // copies tell of themselves when they have landed, and the issuing warp puts the fence between the proxies.
@@ -43,7 +43,7 @@ template <int D> constexpr int kSub = (D + 63) / 64;                       // bl
 template <int D> constexpr int kTile = kSub<D> * 128 * 128;                // bytes of 128 rows
 template <int D> constexpr int kShared = 1024 + 6 * kTile<D> + kPlaces * kWideKeys * 16;
 
-enum Bar { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + 2, kVFull = kKEmpty + 2, kVEmpty = kVFull + 2, kSFull = kVEmpty + 2, kPFull = kSFull + 2,
+enum Bar { kQFull, kKFull = kQFull + 2, kKEmpty = kKFull + 2, kVFull = kKEmpty + 2, kVEmpty = kVFull + 2, kSFull = kVEmpty + 2, kPFull = kSFull + 2,
            kOFull = kPFull + 2, kVLanded = kOFull + 2, kDrained = kVLanded + 2, kPlaceFull, kPlaceEmpty = kPlaceFull + kPlaces, kBars = kPlaceEmpty + kPlaces };
 
 // The two caches as TMA takes them; tokens 0: not that way.
@@ -75,10 +75,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {              
     return r;
 }
 
-// A row's 128 scores from tensor memory: weights 2^(s scale - base), packed; their sum; the highest score (NaN if one is). Careful: only
-// those from `hidden` on and below `seen` count, and every exponential is the special-function unit's, infinities and NaN as they come.
-template <typename T, bool kCareful>
-__device__ __forceinline__ void weights(uint32_t s_at, float scale, float base, int hidden, int seen, uint32_t (&p)[64], Two& sum, float& top) {
+// A row's 128 scores from tensor memory: weights 2^(s scale - base), packed; their sum; the highest score (NaN if one is). A weight of a score that is
+// -inf is 2^-125 at the most, which no sum of any other weight notices; what is NaN is the caller's to see by the highest score.
+template <typename T> __device__ __forceinline__ void weights(uint32_t s_at, float scale, float base, uint32_t (&p)[64], float& sum, float& top) {
     const Two scale2 = two(scale, scale), base2 = two(-base, -base);
     uint32_t r[2][32];
     float high[2] = {-INFINITY, -INFINITY};
@@ -90,20 +89,37 @@ __device__ __forceinline__ void weights(uint32_t s_at, float scale, float base, 
         if (q < 3) ptx::tmem_ld_32x32b_x32(s_at + 32 * (q + 1), r[(q + 1) & 1]);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            float a = __uint_as_float(r[q & 1][2 * j]), b = __uint_as_float(r[q & 1][2 * j + 1]);
-            if (kCareful) {
-                a = 32 * q + 2 * j < seen && 32 * q + 2 * j >= hidden ? a : -INFINITY;
-                b = 32 * q + 2 * j + 1 < seen && 32 * q + 2 * j + 1 >= hidden ? b : -INFINITY;
-            }
+            const float a = __uint_as_float(r[q & 1][2 * j]), b = __uint_as_float(r[q & 1][2 * j + 1]);
             high[j & 1] = max3(high[j & 1], a, b);
             const float2 x = apart(fma2(two(a, b), scale2, base2));
-            const float2 w = !kCareful && (j & 3) == 3 ? exp2_by_products(x) : make_float2(ex2(x.x), ex2(x.y));
+            const float2 w = (j & 3) == 3 ? exp2_by_products(x) : make_float2(ex2(x.x), ex2(x.y));
             part[j & 1] = part[j & 1] + two(w.x, w.y);
             p[16 * q + j] = Pair<T>::pack(w.x, w.y);
         }
     }
-    sum = part[0] + part[1];
+    const float2 all = apart(part[0] + part[1]);
+    sum = all.x + all.y;
     top = max3(high[0], high[1], high[1]);
+}
+
+// The highest of a row's scores `hidden` <= key < seen (NaN if one is); the others become -inf, in tensor memory too where `hide` says so.
+__device__ __forceinline__ float highest_seen(uint32_t s_at, int hidden, int seen, bool hide) {
+    float high = -INFINITY;
+#pragma unroll 1
+    for (int q = 0; q < 128; q += 16) {
+        uint32_t r[16];
+        ptx::tmem_ld_32x32b_x16(s_at + q, r);
+        ptx::tmem_ld_wait_for(r);
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+            r[j] = q + j < seen && q + j >= hidden ? r[j] : 0xff800000u;
+            r[j + 1] = q + j + 1 < seen && q + j + 1 >= hidden ? r[j + 1] : 0xff800000u;
+            high = max3(high, __uint_as_float(r[j]), __uint_as_float(r[j + 1]));
+        }
+        if (hide) ptx::tmem_st_32x32b_x16(s_at + q, r);
+    }
+    if (hide) ptx::tmem_st_wait();
+    return high;
 }
 
 // Keys below this are seen by all rows of a block.
@@ -123,15 +139,14 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
     __shared__ int s_odd[2];                     // values of the stage that are not finite, where some row does not see them
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t bars = ptx::smem_u32(s_bar), at = ptx::smem_u32(smem);
-    ardiff::begin_kernel();
-    const List& list = c.plan.wide;
-    const long long steps = list.head->steps, each = steps_each<true>(list), begin = each * blockIdx.x;
-    if (begin >= steps) return;
-    const int n = (int)(min(steps, begin + each) - begin), own = list.head->own, G = c.x.G;
+    // (barriers and tensor memory do not wait for the kernels before)
     if (tid == 0) {
         for (int i = 0; i < kBars; ++i) {
-            const bool a_warp = i == kQFull || i == kKFull || i == kKFull + 1 || i == kVFull || i == kVFull + 1 || (i >= kPlaceFull && i < kPlaceEmpty);
-            ptx::mbar_init(bars + i * 8, a_warp ? (boxes.tokens && i != kQFull ? 1 : 32) : i >= kPlaceEmpty ? 2 : i == kPFull || i == kPFull + 1 ? 128 : 1);
+            int count = 1;
+            if (i == kKFull || i == kKFull + 1 || i == kVFull || i == kVFull + 1 || (i >= kPlaceFull && i < kPlaceEmpty)) count = boxes.tokens ? 1 : 32;
+            else if (i == kQFull || i == kQFull + 1 || i == kPFull || i == kPFull + 1) count = 128;
+            else if (i >= kPlaceEmpty) count = 2;
+            ptx::mbar_init(bars + i * 8, count);
         }
         s_stop = 0;
         ptx::fence_mbar_init();
@@ -144,22 +159,22 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
     __syncthreads();
     ptx::tc_fence_after();
     const uint32_t tmem = s_tmem;
+    ardiff::begin_kernel();
+    const List& list = c.plan.wide;
+    const long long steps = list.head->steps, each = steps_each<true>(steps, list.workers), begin = each * blockIdx.x;
+    const int n = (int)max(0ll, min(steps, begin + each) - begin), own = list.head->own, G = c.x.G;
     const Waits wait{bars, &s_stop, c.status};
     Cursor<true> now;
-    now.start(c, find_last(list.steps, list.head->blocks, begin), begin);
+    if (n > 0) now.start(c, find_last(list.steps, list.head->blocks, begin), begin);
 
-    if (warp == 11) {
-        // ---- places and queries
-        constexpr int kLanes = D / 8 <= 8 ? 8 : 16;                         // a row
-        const int ch = lane % kLanes;
-        const bool mine = ch < D / 8;
-        uint32_t unit = 0;
-        bool fresh = true;
-        for (int i = 0; i < n; ++i) {
+    if (n == 0) {
+        // nothing is left for this CTA
+    } else if (warp == 11) {
+        // ---- places
+        for (int i = 0; i < n && !boxes.tokens; ++i) {
             const int slot = i % kPlaces;
             longlong2 found[4];
             bool whole = true;
-            if (!boxes.tokens) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 found[u] = place_of<true>(c, now, u * 32 + lane);
@@ -174,26 +189,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
             }
             if (lane == 0) s_whole[slot] = whole;
             ptx::mbar_arrive(bars + (kPlaceFull + slot) * 8);
-            }
-            if (fresh) {
-                if (!__all_sync(0xffffffffu, wait(kQEmpty, (unit & 1) ^ 1))) break;
-                const int rows = now.at.rows > kRows ? 2 * kRows : kRows;
-                const T* base = static_cast<const T*>(c.x.q) + (long long)now.at.token0 * c.x.q_token + (long long)now.h * G * c.x.q_head + ch * 8;
-#pragma unroll 4
-                for (int in = lane / kLanes; in < rows; in += 32 / kLanes) {
-                    const bool there = in < now.at.rows;
-                    const unsigned row = now.at.row0 + in, tok = c.x.by_G.quotient(row);
-                    const T* from = base + (there ? tok * c.x.q_token + (row - tok * G) * c.x.q_head : 0);
-                    if (mine) cp_async16(at + kQ + (in >> 7) * kTile<D> + swizzled(in & 127, ch), from, there ? 16 : 0);
-                }
-                cp_async_arrive(bars + kQFull * 8);
-            }
-            fresh = now.tile + 1 == now.tiles;
-            if (fresh) ++unit;
             if (i + 1 < n) now.next(c);
         }
-        cp_async_commit();
-        cp_async_wait<0>();
     } else if (warp >= 9 && boxes.tokens) {
         // ---- keys or values, by boxes
         const bool v = warp == 10;
@@ -320,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
         const uint32_t idesc_o = ptx::idesc_16(Pair<T>::kBf16, 128, D, true, false);
         const uint64_t q_desc = ptx::smem_desc_sw128(at + kQ), k_desc = ptx::smem_desc_sw128(at + kK);
         const uint64_t v_desc = ptx::smem_desc_mn_sw128(at + kV, 16384, 1024);
-        uint32_t unit = 0, p_count[2] = {0, 0};
+        uint32_t units[2] = {0, 0}, p_count[2] = {0, 0};
         bool fresh = true, good = true;
         auto all = [](bool ok) { return __all_sync(0xffffffffu, ok) != 0; };
         auto commit = [&](int bar) {
@@ -355,14 +352,16 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
             const uint32_t parity = ((uint32_t)i >> 1) & 1;
             const bool two = now.at.rows > kRows, ends = now.tile + 1 == now.tiles || i + 1 == n;
             if (fresh) {
-                good = all(wait(kQFull, unit & 1) && wait(kKFull + stage, parity));
+                for (int tile = 0; tile < (two ? 2 : 1) && good; ++tile) {
+                    good = all(wait(kQFull + tile, units[tile] & 1) && wait(kKFull + stage, parity));
+                    ++units[tile];
+                    if (!good) break;
+                    ptx::fence_proxy_async_smem();
+                    ptx::tc_fence_after();
+                    scores(tile, stage);
+                }
                 if (!good) break;
-                ptx::fence_proxy_async_smem();
-                ptx::tc_fence_after();
-                scores(0, stage);
-                if (two) scores(1, stage);
                 commit(kKEmpty + stage);
-                if (ends) commit(kQEmpty);
             }
             const int stage1 = (i + 1) & 1;
             const uint32_t parity1 = ((uint32_t)(i + 1) >> 1) & 1;
@@ -392,12 +391,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                 }
             }
             if (!good) break;
-            if (!ends) {
-                commit(kKEmpty + stage1);
-                if (now.tile + 2 == now.tiles || i + 2 == n) commit(kQEmpty);
-            }
+            if (!ends) commit(kKEmpty + stage1);
             fresh = ends;
-            if (ends) ++unit;
             if (i + 1 < n) now.next(c);
         }
         if (!good) {
@@ -422,6 +417,17 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
             if (now.at.rows > tile * kRows) {
                 const int row = now.at.row0 + in, tok = row / G;
                 if (fresh) {
+                    // the warp's rows of queries (the last unit's products are done: its results have been read)
+                    constexpr int kLanes = D / 8 <= 8 ? 8 : 16;
+                    const T* base = static_cast<const T*>(c.x.q) + (long long)now.at.token0 * c.x.q_token + (long long)now.h * G * c.x.q_head + (lane % kLanes) * 8;
+#pragma unroll 4
+                    for (int u = lane / kLanes; u < 32; u += 32 / kLanes) {
+                        const int j = in - lane + u;
+                        const unsigned r = now.at.row0 + j, t = c.x.by_G.quotient(r);
+                        const T* from = base + (j < now.at.rows ? t * c.x.q_token + (r - t * G) * c.x.q_head : 0);
+                        if (lane % kLanes < D / 8) cp_async16(at + kQ + tile * kTile<D> + swizzled(j & 127, lane % kLanes), from, j < now.at.rows ? 16 : 0);
+                    }
+                    cp_async_arrive(bars + (kQFull + tile) * 8);
                     m = -INFINITY;
                     l = 0.f;
                     least = least_seen(now.at, G);
@@ -433,37 +439,38 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                 const int seen = lim - key0, hidden = now.at.low - key0;   // of the tile's keys
                 const bool masked = __any_sync(0xffffffffu, seen < kWideKeys || hidden > 0);
                 // Weights by the maximum so far, in the hope that it holds, and kept in registers until it is known to: S is still there for another
-                // try with a higher one (the first tile's always, later ones' rarely).
+                // try with a higher one. A unit's first tile, and tiles that some row does not see all of, are looked through before.
                 uint32_t p[64];
-                bool careful = masked;
-                for (bool again = false;;) {
-                    const float base = m == -INFINITY ? 0.f : m;
-                    Two sum = two(0.f, 0.f);
-                    float top = -INFINITY;
-                    if (careful) weights<T, true>(s_at, scale, base, hidden, seen, p, sum, top);
-                    else weights<T, false>(s_at, scale, base, hidden, seen, p, sum, top);
+                float top = 0.f;
+                bool look = fresh || masked;
+                if (look) top = highest_seen(s_at, hidden, seen, masked);
+                for (;;) {
                     const float highest = top * scale;
-                    const bool holds = highest <= m + kSlack || highest == -INFINITY;         // (not where it is NaN)
-                    if (again || __all_sync(0xffffffffu, holds)) {
-                        const float2 total = apart(sum);
-                        l += total.x + total.y;
-                        break;
-                    }
-                    const float higher = fmaxf(m, highest), alpha = m == higher ? 1.f : ex2(m - higher);
-                    m = higher;
-                    l *= alpha;
-                    if (!fresh) {
+                    if (look && __any_sync(0xffffffffu, highest > m + kSlack || (fresh && highest > m))) {
+                        const float higher = fmaxf(m, highest), alpha = m == higher ? 1.f : ex2(m - higher);
+                        m = higher;
+                        l *= alpha;
+                        if (!fresh) {
+#pragma unroll 1
+                            for (int q = 0; q < D; q += 16) {
+                                uint32_t o[16];
+                                ptx::tmem_ld_32x32b_x16(o_at + q, o);
+                                ptx::tmem_ld_wait_for(o);
 #pragma unroll
-                        for (int q = 0; q < D / 16; ++q) {
-                            uint32_t o[16];
-                            ptx::tmem_ld_32x32b_x16(o_at + 16 * q, o);
-                            ptx::tmem_ld_wait_for(o);
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-                            ptx::tmem_st_32x32b_x16(o_at + 16 * q, o);
+                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                                ptx::tmem_st_32x32b_x16(o_at + q, o);
+                            }
                         }
                     }
-                    careful = again = true;
+                    float sum;
+                    weights<T>(s_at, scale, m == -INFINITY ? 0.f : m, p, sum, top);
+                    // NaN and +inf have no weights: the row's results are NaN
+                    const bool lost = !(top * scale < INFINITY) && !(top == -INFINITY);
+                    if (look || __all_sync(0xffffffffu, lost || top * scale <= m + kSlack || top == -INFINITY)) {
+                        l += lost ? NAN : sum;
+                        break;
+                    }
+                    look = true;
                 }
                 bool odd = false;
                 if (now.at.key0 + (now.tile + 1) * kWideKeys > least) {
@@ -514,33 +521,34 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                 if (ends) {
                     if (!all(wait(kOFull + tile, o_count++ & 1))) break;
                     ptx::tc_fence_after();
-                    const long long unit = list.steps[now.b] + (long long)now.h * now.tiles;
+                    const long long unit = now.at.first_step + (long long)now.h * now.tiles;
                     const bool direct = whole && now.tile + 1 == now.tiles && now.b >= own && c.plan.share[now.at.request].prefix < 0;
                     const bool there = in < now.at.rows;
                     const int head = now.h * G + row - tok * G;
                     T* to = static_cast<T*>(c.x.out) + (there ? (now.at.token0 + (long long)tok) * c.x.out_token + head * c.x.out_head : 0);
-                    const long long piece = direct ? 0 : piece_row<true>(c, now.b, now.at, now.h, blockIdx.x, (int)(unit / each)) + in;
+                    const long long piece = direct ? 0 : piece_row<true>(c, now.at, now.h, blockIdx.x, quotient_of(unit, each));
+                    if (m == -INFINITY) l = l == l ? 0.f : l;                // no key was seen
                     const float f = l > 0.f ? 1.f / l : l;
-#pragma unroll
-                    for (int q = 0; q < D / 16; ++q) {
+#pragma unroll 1
+                    for (int q = 0; q < D; q += 16) {
                         uint32_t o[16];
-                        ptx::tmem_ld_32x32b_x16(o_at + 16 * q, o);
+                        ptx::tmem_ld_32x32b_x16(o_at + q, o);
                         ptx::tmem_ld_wait_for(o);
                         if (there && direct) {
                             uint32_t w[8];
 #pragma unroll
                             for (int j = 0; j < 8; ++j) w[j] = Pair<T>::pack(__uint_as_float(o[2 * j]) * f, __uint_as_float(o[2 * j + 1]) * f);
-                            *reinterpret_cast<uint4*>(to + 16 * q) = make_uint4(w[0], w[1], w[2], w[3]);
-                            *reinterpret_cast<uint4*>(to + 16 * q + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                            *reinterpret_cast<uint4*>(to + q) = make_uint4(w[0], w[1], w[2], w[3]);
+                            *reinterpret_cast<uint4*>(to + q + 8) = make_uint4(w[4], w[5], w[6], w[7]);
                         } else if (there) {
 #pragma unroll
                             for (int j = 0; j < 16; j += 4)
-                                *reinterpret_cast<uint4*>(c.pieces.o + piece * D + 16 * q + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                                *reinterpret_cast<uint4*>(piece_values(c, piece, D, now.at.rows, in, q + j)) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
                         }
                     }
                     if (there) {
                         if (direct) c.x.lse[(now.at.token0 + (long long)tok) * c.x.lse_token + head] = (m + log2f(l)) * 0.6931471805599453f;
-                        else c.pieces.ml[piece] = make_float2(m, l);
+                        else c.pieces.ml[piece + in] = make_float2(m, l);
                     }
                     ptx::tc_fence_before();
                 }
