@@ -486,13 +486,12 @@ template <int D> struct Joined {
 };
 
 template <typename T, int D, bool kWide>
-__device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half, long long narrow_steps, long long wide_steps, const Block& k, int h, int first_row) {
+__device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half, long long narrow_steps, long long wide_steps, const Block& k, const Share& share,
+                                          Cut mine, int h, int first_row) {
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % kJoinWarps, G = c.x.G;
     const int r = lane % kJoinRows, quarter = lane / kJoinRows, in = first_row + r;
-    const Share share = c.plan.share[k.request];
-    const Cut mine = cut_of<kWide>(c, kWide ? wide_steps : narrow_steps, k, h, in);
-    if (mine.count == 1 && share.prefix < 0) return;                                // written already
     const bool there = in < k.rows;
+    mine.in = in;
     Cut theirs = mine;
     theirs.count = 0;
     if (share.prefix >= 0 && there) {
@@ -558,36 +557,41 @@ __device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half,
     ptx::bar_sync(1 + half, 32 * kJoinWarps);
 }
 
-// The rows of a list: all of the requests' own, or, where nothing else is to be joined, those of units that a worker's first step cuts.
+// The rows of a list: all of the requests' own, or, where nothing else is to be joined, those of units that a worker's first step cuts. Four warps
+// take a narrow unit, or an eighth of a wide one.
 template <typename T, int D, bool kWide>
 __device__ __forceinline__ void join_list(const Call& c, Joined<D>& s, int half, const PlanHead& narrow, const PlanHead& wide) {
     const List& list = list_of<kWide>(c);
     const PlanHead& head = kWide ? wide : narrow;
-    const int H = c.cache.heads, parts = (kWide ? kWideRows : c.plan.narrow_rows) / kJoinRows;
-    const long long first = blockIdx.x * 2ll + half, step = gridDim.x * 2ll;
-    if (head.all_rows) {
-        const long long units = (long long)(head.blocks - head.own) * H;
-        for (long long i = first; i < units * parts; i += step) {
-            const long long unit = i / parts;
-            const int b = head.own + (int)(unit / H), row = (int)(i - unit * parts) * kJoinRows;
-            const Block k = list.block[b];
-            if (row < k.rows) join_rows<T, D, kWide>(c, s, half, narrow.steps, wide.steps, k, (int)(unit % H), row);
-        }
-        return;
-    }
     if (head.blocks == head.own) return;
+    const int H = c.cache.heads, kParts = kWide ? 8 : 1, rows = Sizes<kWide>::rows / kParts;
     const long long each = steps_each<kWide>(head.steps, list.workers);
-    const int cuts = (int)((head.steps - 1) / each);
-    for (long long i = first; i < (long long)cuts * parts; i += step) {
-        const int row = (int)(i / cuts) * kJoinRows;
-        const long long at = each * (i % cuts + 1);
-        const int b = find_last(list.steps, head.blocks, at);
+    const long long cuts = (head.steps - 1) / each, items = head.all_rows ? (long long)(head.blocks - head.own) * H : cuts;
+    for (long long i = blockIdx.x * 2 + half; i < items * kParts; i += gridDim.x * 2) {
+        const int item = quotient_of(i, kParts), row0 = (int)(i - (long long)item * kParts) * rows;
+        int b, h = 0;
+        if (head.all_rows) {
+            b = item / H;
+            h = item - b * H;
+            b += head.own;
+        } else {
+            b = find_last(list.steps, head.blocks, each * (item + 1));
+        }
         const Block k = list.block[b];
-        if (row >= k.rows || b < head.own) continue;
-        const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys, h = (int)(at - k.first_step) / tiles;
-        const long long unit = k.first_step + (long long)h * tiles;
-        // (a unit that several workers cut is the first one's)
-        if (unit < at && unit >= at - each) join_rows<T, D, kWide>(c, s, half, narrow.steps, wide.steps, k, h, row);
+        if (row0 >= k.rows) continue;
+        if (!head.all_rows) {
+            const long long at = each * (item + 1);
+            const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
+            h = (int)(at - k.first_step) / tiles;
+            const long long unit = k.first_step + (long long)h * tiles;
+            // (a unit that several workers cut is the first one's; shared tokens' units are joined with their requests' own)
+            if (b < head.own || unit >= at || unit < at - each) continue;
+        }
+        const Share share = c.plan.share[k.request];
+        const Cut mine = cut_of<kWide>(c, head.steps, k, h, 0);
+        if (mine.count == 1 && share.prefix < 0) continue;                              // written already
+        for (int row = row0; row < min(row0 + rows, k.rows); row += kJoinRows)
+            join_rows<T, D, kWide>(c, s, half, narrow.steps, wide.steps, k, share, mine, h, row);
     }
 }
 
