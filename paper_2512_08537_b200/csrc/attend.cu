@@ -215,13 +215,13 @@ constexpr int kThreads = kWarps * 32;
 template <int D> constexpr int kPitch16 = 2 * D + 16;                     // bytes from row to row: an odd number of 16-byte places
 template <int D> constexpr int kStageBytes = 2 * kNarrowKeys * kPitch16<D>;
 template <int D> constexpr int kStages = 28400 / kStageBytes<D> < 6 ? 28400 / kStageBytes<D> : 6;
-template <int D> constexpr int kNarrowShared = kWarps * (kStages<D> * kStageBytes<D> + 64);
+template <int D> constexpr int kNarrowShared = kWarps * (kStages<D> * kStageBytes<D> + kNarrowKeys * 16);
 
 // Every warp is a worker of its own: 16 keys of a kv head a step, as many steps under way as its part of shared memory holds (26 to 28 KB: with
-// eight warps some 200 KB an SM, more than memory's latency asks for), no meeting with other warps. A lane copies one key's row or one
-// value's (a bulk copy: rows lie 2 D + 16 bytes apart there, so that the eight rows of a matrix are in different banks), and looks up the place
-// of the next one meanwhile. Query rows are the left operand, 16 rows an instruction, or twice that (kTiles == 2): with few rows it is mostly
-// empty, but reading 512 bytes a key and head from memory takes longer than its products.
+// eight warps some 200 KB an SM, more than memory's latency asks for), no meeting with other warps. Lanes look up the places of the keys of the
+// step after the next one that is sent for, and copy 16 bytes each (bulk copies of single rows come at 15 clocks each: 2.9 TB/s with rows of 160 bytes).
+// Rows lie 2 D + 16 bytes apart, so that the eight rows of a matrix are in different banks. Query rows are the left operand, 16 rows an
+// instruction, or twice that (kTiles == 2): with few rows it is mostly empty, but reading 512 bytes a key and head from memory takes longer than its products.
 template <typename T, int D, int kTiles>
 __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
     extern __shared__ __align__(128) char smem[];
@@ -233,49 +233,46 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
     const long long begin = each * worker;
     if (begin >= steps) return;
     const int n = (int)(min(steps, begin + each) - begin), own = list.head->own;
-    const char* ring = smem + kWarps * 64 + warp * kStages<D> * kStageBytes<D>;
-    const uint32_t ring_at = ptx::smem_u32(ring), bars = ptx::smem_u32(smem) + warp * 64;
-    if (lane == 0) {
-        for (int s = 0; s < kStages<D>; ++s) ptx::mbar_init(bars + s * 8, 1);
-        ptx::fence_mbar_init();
-    }
-    __syncwarp();
+    const char* ring = smem + warp * kStages<D> * kStageBytes<D>;
+    longlong2* place = reinterpret_cast<longlong2*>(smem + kWarps * kStages<D> * kStageBytes<D>) + warp * kNarrowKeys;
+    const uint32_t ring_at = ptx::smem_u32(ring);
 
     Cursor<false> now;
     now.start(c, find_last(list.steps, list.head->blocks, begin), begin);
     Cursor<false> load = now;                    // the step whose places are looked up next
-    const bool v = lane >= 16;
-    const uint32_t row_to = ring_at + lane * kPitch16<D>;                              // 16 keys, then their values
-    // where this lane's row of the step at `load` lies, NULL for none
-    auto look_up = [&]() -> const char* {
-        const longlong2 p = place_of<false>(c, load, lane & 15);
-        return p.x < 0 ? nullptr : v ? c.cache.v + p.y : c.cache.k + p.x;
-    };
-    auto fetch = [&](int step, const char* from) {
-        const int stage = step % kStages<D>;
-        const uint32_t there = __ballot_sync(0xffffffffu, from != nullptr);
-        if (lane == 0) ptx::mbar_arrive_expect_tx(bars + stage * 8, __popc(there) * 2 * D);
+    auto look_up = [&]() -> longlong2 { return lane < kNarrowKeys ? place_of<false>(c, load, lane) : make_longlong2(-1, -1); };
+    // this lane's chunks of the 16 keys, and of their values
+    constexpr int kChunks = D / 8, kCopies = kNarrowKeys * kChunks / 32;
+    auto fetch = [&](int step, longlong2 found) {
+        if (lane < kNarrowKeys) place[lane] = found;
         __syncwarp();
-        const uint32_t to = row_to + stage * kStageBytes<D>;
-        if (from) {
-            ptx::bulk_load(to, from, 2 * D, bars + stage * 8);
-        } else if (v) {                          // behind the last key: no value, rather than what was there
-            for (int j = 0; j < D / 8; ++j) ptx::sts_u4(to + j * 16, make_uint4(0u, 0u, 0u, 0u));
-            ptx::fence_proxy_async_smem();
+        const uint32_t to = ring_at + (step % kStages<D>) * kStageBytes<D>;
+        longlong2 p[kCopies];
+#pragma unroll
+        for (int j = 0; j < kCopies; ++j) p[j] = place[(lane + 32 * j) / kChunks];
+#pragma unroll
+        for (int j = 0; j < kCopies; ++j) {
+            const int row = (lane + 32 * j) / kChunks, ch = lane + 32 * j - row * kChunks;
+            const uint32_t at = to + row * kPitch16<D> + ch * 16, bytes = p[j].x < 0 ? 0 : 16;       // (none: zeros)
+            cp_async16(at, c.cache.k + (bytes ? p[j].x + ch * 16 : 0), bytes);
+            cp_async16(at + kNarrowKeys * kPitch16<D>, c.cache.v + (bytes ? p[j].y + ch * 16 : 0), bytes);
         }
+        cp_async_commit();
+        __syncwarp();
     };
-    for (int s = 0; s < kStages<D> && s < n; ++s) {
-        fetch(s, look_up());
+    for (int s = 0; s < kStages<D>; ++s) {
+        if (s < n) fetch(s, look_up());
+        else cp_async_commit();
         if (s + 1 < n) load.next(c);
     }
-    const char* found = n > kStages<D> ? look_up() : nullptr;
+    longlong2 found = n > kStages<D> ? look_up() : make_longlong2(-1, -1);
 
     const int G = c.x.G, quad = lane & 3, row8 = lane >> 2;
     uint32_t q[kTiles][D / 16][4];
     float o[kTiles][D / 8][4], m[kTiles][2], l[kTiles][2];
     int lim[kTiles][2], least = 0;               // keys below `least` are seen by all rows of the block
     bool fresh = true, whole = now.tile == 0;
-    uint32_t stage = 0, parity = 0;
+    uint32_t stage = 0;
 
     for (int i = 0; i < n; ++i) {
         if (fresh) {
@@ -303,7 +300,8 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
                 }
             fresh = false;
         }
-        if (!wait_warp(bars + stage * 8, parity, c.status)) return;
+        cp_async_wait<kStages<D> - 1>();
+        __syncwarp();
         const uint32_t k_tile = ring_at + stage * kStageBytes<D>, v_tile = k_tile + kNarrowKeys * kPitch16<D>;
         const int key0 = now.at.key0 + now.tile * kNarrowKeys;
         const bool zone = key0 + kNarrowKeys > least;
@@ -414,8 +412,10 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
                 load.next(c);
                 found = look_up();
             }
+        } else {
+            cp_async_commit();                   // (one a step, so that the wait counts)
         }
-        if (++stage == kStages<D>) { stage = 0; parity ^= 1; }
+        if (++stage == kStages<D>) stage = 0;
 
         const bool ends = now.tile + 1 == now.tiles;
         if (ends || i + 1 == n) {

@@ -253,19 +253,6 @@ struct Waits {
     }
 };
 
-// A wait with the same limit, after which the status says so. A warp's lanes get the same answer.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int32_t* status) {
-    if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
-    const unsigned long long t0 = ptx::globaltimer_ns();
-    for (int i = 0;; ++i) {
-        if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
-        if ((i & 63) == 63 && __any_sync(0xffffffffu, ptx::globaltimer_ns() - t0 > kWaitLimit)) {
-            *status = ARDIFF_ERR_TIMEOUT;
-            return false;
-        }
-    }
-}
-
 // 16-byte chunk c of row `row` of a tile of rows of D values: chunks change places with the row, or rows are a chunk longer than their values, so
 // that the eight rows of a matrix lie in different banks.
 template <int D> constexpr int kPitch = D % 64 ? 2 * D + 16 : 2 * D;
