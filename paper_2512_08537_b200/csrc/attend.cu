@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
         for (int j = 0; j < n; ++j) {
             Block b;
             b.token0 = token0; b.row0 = j * per; b.rows = (int)min((long long)per, rows - b.row0);
-            b.request = r; b.low = mine.shared; b.split = mine.split; b.front = mine.front; b.pad = 0;
+            b.request = r; b.low = mine.shared; b.split = c.cache.by_page.quotient(mine.split); b.front = mine.front; b.pad = 0;
             b.key0 = wide ? b.low / kWideKeys * kWideKeys : b.low;
             b.step = c.causal ? 1 : 0;
             b.limit = c.causal ? len - news + 1 : len;
@@ -237,25 +237,77 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
     longlong2* place = reinterpret_cast<longlong2*>(smem + kWarps * kStages<D> * kStageBytes<D>) + warp * kNarrowKeys;
     const uint32_t ring_at = ptx::smem_u32(ring);
 
-    Cursor<false> now;
-    now.start(c, find_last(list.steps, list.head->blocks, begin), begin);
-    Cursor<false> load = now;                    // the step whose places are looked up next
-    auto look_up = [&]() -> longlong2 { return lane < kNarrowKeys ? place_of<false>(c, load, lane) : make_longlong2(-1, -1); };
+    // where this warp is in the line of steps, and what it needs of the block: of products, and of copies some steps ahead
+    struct Place {
+        int b, h, tile, tiles, key0, keys;
+        __device__ __forceinline__ void enter(const List& list) {
+            key0 = list.block[b].key0;
+            keys = list.block[b].keys;
+            tiles = (keys + kNarrowKeys - 1) / kNarrowKeys;
+            tile = 0;
+        }
+        // the next step; whether it is another block's (only called while there is one)
+        __device__ __forceinline__ bool next(const List& list, int heads) {
+            if (++tile < tiles) return false;
+            tile = 0;
+            if (++h < heads) return false;
+            h = 0;
+            do {
+                ++b;
+                enter(list);
+            } while (tiles == 0);
+            return true;
+        }
+    };
+    const int H = c.cache.heads;
+    Place now;
+    now.b = find_last(list.steps, list.head->blocks, begin);
+    now.enter(list);
+    {
+        const int in = (int)(begin - list.block[now.b].first_step);
+        now.h = in / now.tiles;
+        now.tile = in - now.h * now.tiles;
+    }
+    Place load = now;                            // the step whose places are looked up next
+    const int32_t *table, *front_table;
+    int split;
+    auto tables = [&]() {
+        const Block& b = list.block[load.b];
+        table = c.cache.table + (long long)b.request * c.cache.width;
+        front_table = c.cache.table + (long long)b.front * c.cache.width;
+        split = b.split;
+    };
+    tables();
+    auto look_up = [&]() -> longlong2 {
+        const int in = load.tile * kNarrowKeys + lane;
+        return lane < kNarrowKeys && in < load.keys ? place_of(c, table, front_table, split, load.key0 + in, load.h) : make_longlong2(-1, -1);
+    };
     // this lane's chunks of the 16 keys, and of their values
     constexpr int kChunks = D / 8, kCopies = kNarrowKeys * kChunks / 32;
     auto fetch = [&](int step, longlong2 found) {
         if (lane < kNarrowKeys) place[lane] = found;
+        const bool missing = __any_sync(0xffffffffu, lane < kNarrowKeys && found.x < 0);
         __syncwarp();
         const uint32_t to = ring_at + (step % kStages<D>) * kStageBytes<D>;
         longlong2 p[kCopies];
 #pragma unroll
         for (int j = 0; j < kCopies; ++j) p[j] = place[(lane + 32 * j) / kChunks];
+        if (!missing) {
 #pragma unroll
-        for (int j = 0; j < kCopies; ++j) {
-            const int row = (lane + 32 * j) / kChunks, ch = lane + 32 * j - row * kChunks;
-            const uint32_t at = to + row * kPitch16<D> + ch * 16, bytes = p[j].x < 0 ? 0 : 16;       // (none: zeros)
-            cp_async16(at, c.cache.k + (bytes ? p[j].x + ch * 16 : 0), bytes);
-            cp_async16(at + kNarrowKeys * kPitch16<D>, c.cache.v + (bytes ? p[j].y + ch * 16 : 0), bytes);
+            for (int j = 0; j < kCopies; ++j) {
+                const int row = (lane + 32 * j) / kChunks, ch = lane + 32 * j - row * kChunks;
+                const uint32_t at = to + row * kPitch16<D> + ch * 16;
+                cp_async16(at, c.cache.k + p[j].x + ch * 16, 16);
+                cp_async16(at + kNarrowKeys * kPitch16<D>, c.cache.v + p[j].y + ch * 16, 16);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kCopies; ++j) {
+                const int row = (lane + 32 * j) / kChunks, ch = lane + 32 * j - row * kChunks;
+                const uint32_t at = to + row * kPitch16<D> + ch * 16, bytes = p[j].x < 0 ? 0 : 16;       // (none: zeros)
+                cp_async16(at, c.cache.k + (bytes ? p[j].x + ch * 16 : 0), bytes);
+                cp_async16(at + kNarrowKeys * kPitch16<D>, c.cache.v + (bytes ? p[j].y + ch * 16 : 0), bytes);
+            }
         }
         cp_async_commit();
         __syncwarp();
@@ -263,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
     for (int s = 0; s < kStages<D>; ++s) {
         if (s < n) fetch(s, look_up());
         else cp_async_commit();
-        if (s + 1 < n) load.next(c);
+        if (s + 1 < n && load.next(list, H)) tables();
     }
     longlong2 found = n > kStages<D> ? look_up() : make_longlong2(-1, -1);
 
@@ -273,10 +325,12 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
     int lim[kTiles][2], least = 0;               // keys below `least` are seen by all rows of the block
     bool fresh = true, whole = now.tile == 0;
     uint32_t stage = 0;
+    const float scale = fabsf(c.scale);
+    const uint32_t signs = c.scale < 0.f ? 0x80008000u : 0u;
 
     for (int i = 0; i < n; ++i) {
         if (fresh) {
-            const Block& b = now.at;
+            const Block b = list.block[now.b];
             const int end = b.key0 + b.keys;
             least = min(end, b.limit + b.step * (b.row0 / G));
 #pragma unroll
@@ -290,8 +344,8 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
                     const T* from = static_cast<const T*>(c.x.q) + (b.token0 + (long long)tok) * c.x.q_token + head * c.x.q_head;
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks) {
-                        q[t][ks][u] = there ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2) : 0u;
-                        q[t][ks][u + 2] = there ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2 + 8) : 0u;
+                        q[t][ks][u] = (there ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2) : 0u) ^ signs;
+                        q[t][ks][u + 2] = (there ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2 + 8) : 0u) ^ signs;
                     }
                     m[t][u] = -INFINITY;
                     l[t][u] = 0.f;
@@ -303,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
         cp_async_wait<kStages<D> - 1>();
         __syncwarp();
         const uint32_t k_tile = ring_at + stage * kStageBytes<D>, v_tile = k_tile + kNarrowKeys * kPitch16<D>;
-        const int key0 = now.at.key0 + now.tile * kNarrowKeys;
+        const int key0 = now.key0 + now.tile * kNarrowKeys;
         const bool zone = key0 + kNarrowKeys > least;
 
         float s[kTiles][2][4];
@@ -325,17 +379,19 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
         uint32_t p[kTiles][4];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
-            float top[2] = {-INFINITY, -INFINITY};
+            if (zone) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key0 + u * 8 + quad * 2 + (e & 1) >= lim[t][e >> 1]) s[t][u][e] = -INFINITY;
+            }
+            float top[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[t][u][e] *= c.scale;
-                    if (zone && key0 + u * 8 + quad * 2 + (e & 1) >= lim[t][e >> 1]) s[t][u][e] = -INFINITY;
-                    top[e >> 1] = fmaxf(top[e >> 1], s[t][u][e]);
-                }
-            // a higher maximum anywhere: all rows move to theirs
-            if (__any_sync(0xffffffffu, top[0] > m[t][0] || top[1] > m[t][1])) {
+                top[u] = fmaxf(fmaxf(s[t][0][2 * u], s[t][0][2 * u + 1]), fmaxf(s[t][1][2 * u], s[t][1][2 * u + 1])) * scale;
+            // a maximum that would grow by more than 2^8 (which sums and weights hold) anywhere: all rows move to theirs
+            if (__any_sync(0xffffffffu, top[0] > m[t][0] + 8.f || top[1] > m[t][1] + 8.f)) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 1));
@@ -352,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[t][u][e] = ex2(s[t][u][e] - base[e >> 1]);
+                    s[t][u][e] = ex2(fmaf(s[t][u][e], scale, -base[e >> 1]));
                     l[t][e >> 1] += s[t][u][e];
                 }
             p[t][0] = Pair<T>::pack(s[t][0][0], s[t][0][1]);
@@ -409,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
         if (i + kStages<D> < n) {
             fetch(i + kStages<D>, found);
             if (i + kStages<D> + 1 < n) {
-                load.next(c);
+                if (load.next(list, H)) tables();
                 found = look_up();
             }
         } else {
@@ -419,8 +475,8 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
 
         const bool ends = now.tile + 1 == now.tiles;
         if (ends || i + 1 == n) {
-            const Block& b = now.at;
-            const long long unit = now.at.first_step + (long long)now.h * now.tiles;       // its first step
+            const Block b = list.block[now.b];
+            const long long unit = b.first_step + (long long)now.h * now.tiles;       // its first step
             const bool direct = whole && ends && now.b >= own && c.plan.share[b.request].prefix < 0;
             const long long at = direct ? 0 : piece_row<false>(c, b, now.h, worker, quotient_of(unit, each));
 #pragma unroll
@@ -449,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
                 }
             fresh = whole = true;
         }
-        if (i + 1 < n) now.next(c);
+        if (i + 1 < n) now.next(list, H);
     }
 }
 
@@ -707,8 +763,11 @@ extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_hea
     if (sms < 1) return ARDIFF_ERR_CUDA;
     Call c;
     memset(&c, 0, sizeof(c));
-    c.cache = Pages{static_cast<const char*>(k_cache), static_cast<const char*>(v_cache), k_page * 2, k_token * 2, k_head * 2, v_page * 2,
-                    v_token * 2, v_head * 2, table, width, page, pages, heads};
+    c.cache.k = static_cast<const char*>(k_cache); c.cache.v = static_cast<const char*>(v_cache);
+    c.cache.table = table; c.cache.width = width; c.cache.page = page; c.cache.pages = pages; c.cache.heads = heads; c.cache.by_page = divide_by(page);
+    if (!strides_of(k_page, k_token, k_head, c.cache, c.cache.k_page, c.cache.k_token, c.cache.k_head) ||
+        !strides_of(v_page, v_token, v_head, c.cache, c.cache.v_page, c.cache.v_token, c.cache.v_head))
+        return ARDIFF_ERR_SHAPE;
     c.x.q = q; c.x.out = out; c.x.lse = lse; c.x.q_token = q_token; c.x.q_head = q_head; c.x.out_token = out_token; c.x.out_head = out_head;
     c.x.lse_token = lse_token; c.x.heads = q_heads; c.x.G = q_heads / heads; c.x.tokens = tokens;
     c.x.by_G = divide_by(q_heads / heads);
@@ -731,6 +790,7 @@ extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_hea
     c.pieces.wide_rows = s.main_rows + (long long)kMaxSms * kWarps * kNarrowRows;
     c.length = length; c.offset = offset; c.group = group; c.shared = shared; c.status = status;
     c.scale = scale * 1.4426950408889634f;
+    if (fabsf(c.scale) < 1.2e-38f) c.scale = 1.2e-38f;       // (0 times the -inf of a key that is not seen would be NaN)
     c.requests = requests; c.groups = groups; c.causal = causal != 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool ok = dtype == ARDIFF_F16 ? launch_width<__half>(c, dtype, head_width, most, sms, st)

@@ -12,18 +12,37 @@
 
 namespace ardiff {
 
-struct Pages {                                   // strides in bytes
+// n / d for n < 2^31
+struct Divide {
+    uint32_t d, m, s;
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return d == 1 ? n : __umulhi(n, m) >> s; }
+};
+// m = 2^(32 + s) / d rounded up with 2^s < d <= 2^(s + 1): exact for n < 2^31, since m d - 2^(32 + s) < d <= 2^(s + 1)
+inline Divide divide_by(uint32_t d) {
+    uint32_t s = 0;
+    while (d > 1 && (2u << s) < d) ++s;
+    return Divide{d, d > 1 ? (uint32_t)((((uint64_t)1 << (32 + s)) + d - 1) / d) : 0u, s};
+}
+
+struct Pages {                                   // strides in 16 bytes
     const char* k;
     const char* v;
-    long long k_page, k_token, k_head, v_page, v_token, v_head;
+    uint32_t k_page, k_token, k_head, v_page, v_token, v_head;
     const int32_t* table;
     int width, page, pages, heads;
+    Divide by_page;
 };
+
+// A byte offset in a cache.
+__device__ __forceinline__ long long offset_of(uint32_t page_stride, uint32_t token_stride, uint32_t head_stride, int id, uint32_t row, int h) {
+    return (long long)(((unsigned long long)(uint32_t)id * page_stride + (unsigned long long)row * token_stride + (unsigned long long)(uint32_t)h * head_stride) << 4);
+}
 
 // Query rows that look at the same keys together. A segment is the new tokens of one request, or of a group of requests that share
 // their first tokens; row j of it is token token0 + j / G, query head h G + j % G (G: query heads a kv head). A block is some rows of a segment, up to 16 or
 // 32 in the list of narrow blocks (a whole segment), 256 in that of wide ones, and the keys that they see, key0 .. key0 + keys - 1. Its row j sees those from `low` on (wide
-// blocks begin at a multiple of their tiles) and below limit + step * (j / G). Pages of keys all below `split` are found through row `front` of the table, the others through row `request`.
+// blocks begin at a multiple of their tiles) and below limit + step * (j / G). The first `split` pages are found through row `front` of the table, the
+// others through row `request`.
 struct alignas(16) Block {
     int token0, row0, rows, request, key0, keys, low, limit, step, split, front, pad;
     long long first_step, first_row;             // steps of the list's blocks before; rows of all blocks before, the narrow list's first
@@ -36,7 +55,7 @@ struct PlanHead {
 };
 
 // Of a request: the first block of its group's shared tokens (-1: none), in which list, and its first row there; how many shared tokens it does not read
-// itself; how many it finds through another row of the table.
+// itself; how many pages it finds through another row of the table.
 struct Share {
     int prefix, wide, row0, shared, split, front, pad0, pad1;
 };
@@ -58,18 +77,6 @@ struct Plan {
     Share* share;                                // [requests]
     int narrow_rows;                             // of a segment, at most, for it to be narrow: 16 or 32
 };
-
-// n / d for n < 2^31
-struct Divide {
-    uint32_t d, m, s;
-    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return d == 1 ? n : __umulhi(n, m) >> s; }
-};
-// m = 2^(32 + s) / d rounded up with 2^s < d <= 2^(s + 1): exact for n < 2^31, since m d - 2^(32 + s) < d <= 2^(s + 1)
-inline Divide divide_by(uint32_t d) {
-    uint32_t s = 0;
-    while (d > 1 && (2u << s) < d) ++s;
-    return Divide{d, d > 1 ? (uint32_t)((((uint64_t)1 << (32 + s)) + d - 1) / d) : 0u, s};
-}
 
 struct Queries {                                 // strides in values
     const void* q;
@@ -153,19 +160,21 @@ template <bool kWide> struct Cursor {
     }
 };
 
-// The offsets of key `j` of the tile at `load` in the caches of keys and values, -1 for none.
-template <bool kWide> __device__ __forceinline__ longlong2 place_of(const Call& c, const Cursor<kWide>& load, int j) {
-    const int in = load.tile * Sizes<kWide>::keys + j;
-    if (in >= load.at.keys) return make_longlong2(-1, -1);
-    const unsigned key = load.at.key0 + in, pg = key / (unsigned)c.cache.page, row = key - pg * c.cache.page;
-    const int r = pg < (unsigned)load.at.split / (unsigned)c.cache.page ? load.at.front : load.at.request;
-    const int id = c.cache.table[(long long)r * c.cache.width + pg];
+// The offsets of key `key` of a head in the caches of keys and values, -1 for none.
+__device__ __forceinline__ longlong2 place_of(const Call& c, const int32_t* table, const int32_t* front_table, int split, unsigned key, int h) {
+    const unsigned pg = c.cache.by_page.quotient(key), row = key - pg * c.cache.page;
+    const int id = ((int)pg < split ? front_table : table)[pg];
     if (id < 0 || id >= c.cache.pages) {
         *c.status = ARDIFF_ERR_SHAPE;
         return make_longlong2(-1, -1);
     }
-    return make_longlong2(id * c.cache.k_page + row * c.cache.k_token + load.h * c.cache.k_head,
-                          id * c.cache.v_page + row * c.cache.v_token + load.h * c.cache.v_head);
+    return make_longlong2(offset_of(c.cache.k_page, c.cache.k_token, c.cache.k_head, id, row, h), offset_of(c.cache.v_page, c.cache.v_token, c.cache.v_head, id, row, h));
+}
+template <bool kWide> __device__ __forceinline__ longlong2 place_of(const Call& c, const Cursor<kWide>& load, int j) {
+    const int in = load.tile * Sizes<kWide>::keys + j;
+    if (in >= load.at.keys) return make_longlong2(-1, -1);
+    return place_of(c, c.cache.table + (long long)load.at.request * c.cache.width, c.cache.table + (long long)load.at.front * c.cache.width, load.at.split,
+                    load.at.key0 + in, load.h);
 }
 
 // The wide blocks (attend_wide.cu).
@@ -299,9 +308,19 @@ __device__ __forceinline__ uint32_t swizzled(int row, int c) {
     return (uint32_t)((c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
 }
 
+// The strides of a cache of 16-bit values in 16 bytes; false where one is negative or too large (those of what there is one of may be anything).
+inline bool strides_of(int64_t page, int64_t token, int64_t head, const Pages& p, uint32_t& to_page, uint32_t& to_token, uint32_t& to_head) {
+    if (p.pages <= 1) page = 0;
+    if (p.page == 1) token = 0;
+    if (p.heads == 1) head = 0;
+    if (page < 0 || token < 0 || head < 0 || (page | token | head) >> 35) return false;
+    to_page = (uint32_t)(page / 8); to_token = (uint32_t)(token / 8); to_head = (uint32_t)(head / 8);
+    return true;
+}
+
 // A cache as an array of four dimensions for TMA (tokens of a page, heads, pages), in boxes of `tokens` tokens and 64 values of a head, swizzled by
 // 128 bytes. False where it cannot be described so (strides of 2^40 bytes, no page): it is copied by 16 bytes then.
-bool describe(CUtensorMap* map, const char* base, bool bf16, int width, int tokens, const Pages& p, long long token, long long head, long long page);
+bool describe(CUtensorMap* map, const char* base, bool bf16, int width, int tokens, const Pages& p, uint32_t token, uint32_t head, uint32_t page);
 // The largest power of two of tokens, up to 128, that divides a page; 0 where it is below the 8 rows of a swizzled block.
 int box_tokens(int page);
 

@@ -204,9 +204,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
             next.id = -1;
             next.head = load.h;
             if (lane * tokens < kWideKeys && in < load.at.keys) {
-                const int pg = (unsigned)key / (unsigned)c.cache.page;
+                const int pg = c.cache.by_page.quotient(key);
                 next.row = key - pg * c.cache.page;
-                next.id = c.cache.table[(long long)(pg < load.at.split / c.cache.page ? load.at.front : load.at.request) * c.cache.width + pg];
+                next.id = c.cache.table[(long long)(pg < load.at.split ? load.at.front : load.at.request) * c.cache.width + pg];
                 if (next.id < 0 || next.id >= c.cache.pages) {
                     *c.status = ARDIFF_ERR_SHAPE;
                     next.id = -1;
@@ -604,15 +604,12 @@ int ardiff::box_tokens(int page) {
     return tokens >= 8 ? tokens : 0;
 }
 
-bool ardiff::describe(CUtensorMap* map, const char* base, bool bf16, int width, int tokens, const Pages& p, long long token, long long head, long long page) {
-    if (p.page == 1) token = 16;                 // (strides of what there is one of may be anything)
-    if (p.heads == 1) head = 16;
-    if (p.pages == 1) page = 16;
-    if (p.pages < 1 || token < 0 || head < 0 || page < 0 || token >= 1ll << 40 || head >= 1ll << 40 || page >= 1ll << 40) return false;
+bool ardiff::describe(CUtensorMap* map, const char* base, bool bf16, int width, int tokens, const Pages& p, uint32_t token, uint32_t head, uint32_t page) {
+    if (p.pages < 1) return false;
     const EncodeTiled f = encoder();
     if (!f) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)p.page, (cuuint64_t)p.heads, (cuuint64_t)p.pages};
-    const cuuint64_t strides[3] = {(cuuint64_t)token, (cuuint64_t)head, (cuuint64_t)page};
+    const cuuint64_t strides[3] = {16 * (cuuint64_t)(token ? token : 1), 16 * (cuuint64_t)(head ? head : 1), 16 * (cuuint64_t)(page ? page : 1)};
     const cuuint32_t box[4] = {64, (cuuint32_t)tokens, 1, 1}, ones[4] = {1, 1, 1, 1};
     return f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<char*>(base), dims, strides, box, ones,
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

@@ -180,9 +180,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
                 const int key = s.key0 + j * step;
                 long long p = 1;
                 if (key < s.keys) {
-                    const unsigned pg = (unsigned)key / (unsigned)c.cache.page, in = key - pg * c.cache.page;
+                    const unsigned pg = c.cache.by_page.quotient(key), in = key - pg * c.cache.page;
                     const int id = table[pg];
-                    if (id >= 0 && id < c.cache.pages) p = tokens ? (long long)id << 32 | in << 1 : id * c.cache.k_page + in * c.cache.k_token;
+                    if (id >= 0 && id < c.cache.pages) p = tokens ? (long long)id << 32 | in << 1 : offset_of(c.cache.k_page, c.cache.k_token, 0, id, in, 0);
                     else if (key + step > s.first) *c.status = ARDIFF_ERR_SHAPE;     // (tokens in front of the first one may lie anywhere)
                 }
                 place[j] = p;
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
                             }
                         } else {
                             const long long* p = place + t * kKeys + row0;
-                            const char* from = c.cache.k + h * c.cache.k_head + ch * 16;
+                            const char* from = c.cache.k + (long long)h * c.cache.k_head * 16 + ch * 16;
 #pragma unroll 1
                             for (int j = 0; j < kKeys / kAtOnce; j += 16) {
                                 long long o[16];
@@ -436,8 +436,9 @@ extern "C" int ardiff_attend_weights(const void* q, int64_t q_token, int64_t q_h
     if (sms < 1) return ARDIFF_ERR_CUDA;
     Weights c;
     memset(&c, 0, sizeof(c));
-    c.cache.k = static_cast<const char*>(k_cache); c.cache.k_page = k_page * 2; c.cache.k_token = k_token * 2; c.cache.k_head = k_head * 2;
-    c.cache.table = table; c.cache.width = width; c.cache.page = page; c.cache.pages = pages; c.cache.heads = heads;
+    c.cache.k = static_cast<const char*>(k_cache);
+    c.cache.table = table; c.cache.width = width; c.cache.page = page; c.cache.pages = pages; c.cache.heads = heads; c.cache.by_page = divide_by(page);
+    if (!strides_of(k_page, k_token, k_head, c.cache, c.cache.k_page, c.cache.k_token, c.cache.k_head)) return ARDIFF_ERR_SHAPE;
     c.x.q = q; c.x.lse = const_cast<float*>(lse); c.x.q_token = q_token; c.x.q_head = q_head; c.x.lse_token = lse_token;
     c.x.heads = q_heads; c.x.G = q_heads / heads; c.x.tokens = tokens; c.x.by_G = divide_by(q_heads / heads);
     c.length = length; c.offset = offset; c.first = first; c.score = score; c.new_score = new_score; c.status = status;

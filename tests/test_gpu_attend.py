@@ -155,6 +155,12 @@ def test_strides_and_scale():
     c.scale = -0.2
     out, lse, _ = c.attend(scale=-0.2)
     c.check(out, lse)
+    for n, length in (([5, 2], [64, 300]), ([150], [260])):
+        c = Case(n, length, 6, 2, 64, 16, "f16", seed=10)
+        for scale in (0.0, -0.3):
+            c.scale = scale
+            out, lse, _ = c.attend(scale=scale)
+            c.check(out, lse)
 
 
 def test_extreme_scores():
