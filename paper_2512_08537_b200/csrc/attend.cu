@@ -35,26 +35,99 @@ constexpr int kPlanThreads = 1024;
 constexpr int kLeastShared = 64;
 
 // ---- the plan -----------------------------------------------------------------------------------
-// Blocks of a segment: of which list, how many.
-__device__ __forceinline__ bool is_wide(const Call& c, long long rows) { return rows > c.plan.narrow_rows; }
-__device__ __forceinline__ int blocks_of(const Call& c, long long rows) { return is_wide(c, rows) ? (int)((rows + kWideRows - 1) / kWideRows) : rows > 0; }
+// What is summed over segments, for narrow and wide ones.
+struct Sums {
+    long long blocks, rows, steps[2];            // blocks, rows: the narrow ones in the upper half
+};
+// Exclusive sums over the CTA's threads, and the totals; `s` holds one of a warp each.
+__device__ __forceinline__ Sums cta_scan(Sums v, Sums* s, Sums* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    auto inclusive = [&](Sums x) {
+        x.blocks = warp_inclusive(x.blocks); x.rows = warp_inclusive(x.rows); x.steps[0] = warp_inclusive(x.steps[0]); x.steps[1] = warp_inclusive(x.steps[1]);
+        return x;
+    };
+    const Sums inc = inclusive(v);
+    __syncthreads();
+    if (lane == 31) s[warp] = inc;
+    __syncthreads();
+    Sums own{0, 0, {0, 0}};
+    if (lane < (int)(blockDim.x >> 5)) own = s[lane];
+    const Sums w = inclusive(own);
+    auto from = [&](long long x, int l) { return __shfl_sync(0xffffffffu, x, l); };
+    *total = Sums{from(w.blocks, 31), from(w.rows, 31), {from(w.steps[0], 31), from(w.steps[1], 31)}};
+    return Sums{inc.blocks - v.blocks + from(w.blocks - own.blocks, warp), inc.rows - v.rows + from(w.rows - own.rows, warp),
+                {inc.steps[0] - v.steps[0] + from(w.steps[0] - own.steps[0], warp), inc.steps[1] - v.steps[1] + from(w.steps[1] - own.steps[1], warp)}};
+}
+__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) {
+    return Sums{a.blocks + b.blocks, a.rows + b.rows, {a.steps[0] + b.steps[0], a.steps[1] + b.steps[1]}};
+}
+
+// A segment's blocks: `b` but for the rows' place and what follows from it. The keys that its rows see end at `length` for requests' own tokens.
+struct Segment {
+    Block b;
+    long long rows;
+    int length;
+    bool wide;
+    __device__ __forceinline__ int blocks() const { return rows <= 0 ? 0 : wide ? (int)((rows + kWideRows - 1) / kWideRows) : 1; }
+    __device__ __forceinline__ Block block(int j, const Call& c) const {
+        Block k = b;
+        const int per = wide ? kWideRows : kNarrowRows, tile = wide ? kWideKeys : kNarrowKeys;
+        k.row0 = j * per;
+        k.rows = (int)min((long long)per, rows - k.row0);
+        k.key0 = wide ? k.low / tile * tile : k.low;
+        const int last = min(length, k.limit + k.step * c.x.by_G.quotient(k.row0 + k.rows - 1));
+        k.keys = last > k.low ? last - k.key0 : 0;
+        return k;
+    }
+    __device__ __forceinline__ int steps(const Block& k, int heads) const {
+        const int tile = wide ? kWideKeys : kNarrowKeys;
+        return (k.keys + tile - 1) / tile * heads;
+    }
+    // what the segment adds
+    __device__ __forceinline__ Sums sums(const Call& c) const {
+        Sums v{0, 0, {0, 0}};
+        const int n = blocks(), up = wide ? 0 : 32;
+        v.blocks = (long long)n << up;
+        v.rows = rows > 0 ? rows << up : 0;
+        for (int j = 0; j < n; ++j) v.steps[wide] += steps(block(j, c), c.cache.heads);
+        return v;
+    }
+    // writes its blocks behind those of `before`; whether one of them has no key
+    __device__ __forceinline__ bool write(const Call& c, const Sums& before) const {
+        const List& l = wide ? c.plan.wide : c.plan.narrow;
+        const int at = wide ? (int)before.blocks : (int)(before.blocks >> 32), n = blocks();
+        long long step = before.steps[wide], row = wide ? (long long)(int)before.rows : before.rows >> 32;
+        bool empty = false;
+        for (int j = 0; j < n; ++j) {
+            Block k = block(j, c);
+            k.first_step = step;
+            k.first_row = row;
+            l.block[at + j] = k;
+            l.steps[at + j] = step;
+            step += steps(k, c.cache.heads);
+            row += k.rows;
+            empty |= k.keys == 0;
+        }
+        return empty;
+    }
+};
 
 // Requests whose numbers fit here are read once; of more than that, again from memory.
 constexpr int kPlanKept = 1024;
 
 template <bool kKept>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
-    __shared__ long long s_scan[32];
+    __shared__ Sums s_scan[32];
     __shared__ int s_offset[kKept ? kPlanKept + 1 : 1], s_length[kKept ? kPlanKept : 1];
     __shared__ Share s_share[kKept ? kPlanKept : 1];
     ardiff::begin_kernel();
-    const int tid = threadIdx.x, lane = tid & 31, R = c.requests, G = c.x.G;
+    const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x, R = c.requests, G = c.x.G;
     const long long limit = (long long)c.cache.width * c.cache.page;
     const int* offset = kKept ? s_offset : c.offset;
     const int* length = kKept ? s_length : c.length;
     Share* share = kKept ? s_share : c.plan.share;
     bool bad = false;
-    for (int r = tid; r < R; r += kPlanThreads) {
+    for (int r = tid; r < R; r += threads) {
         const int a = c.offset[r], b = c.offset[r + 1], len = c.length[r];
         bad |= a < 0 || b < a || b > c.x.tokens || len < 0 || len > limit;
         if (kKept) {
@@ -64,21 +137,21 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
         }
         share[r] = Share{-1, 0, 0, 0, 0, r, 0, 0};
     }
-    for (int g = tid; g < c.groups; g += kPlanThreads) {
+    for (int g = tid; g < c.groups; g += threads) {
         const int a = c.group[g], b = c.group[g + 1];
         bad |= a < 0 || b < a || b > R || c.shared[g] < 0;
     }
     bad = __syncthreads_or(bad);
     if (tid == 0) *c.status = bad ? ARDIFF_ERR_SHAPE : ARDIFF_OK;
     if (bad) {
-        if (tid < 2) *(tid ? c.plan.wide : c.plan.narrow).head = PlanHead{0, 0, 0, 0, 0};
+        if (tid < 2) *(tid ? c.plan.wide : c.plan.narrow).head = PlanHead{0, 0, 0, 0, 0, 0};
         return;
     }
-    long long blocks[2] = {0, 0};                // narrow, wide
+    Sums before{0, 0, {0, 0}};
     if (c.groups > 0) {
         // The tokens that all queries of a group see are found through its first row of the table, and read once for all, unless
         // one request has queries, or all have so many that each fills its blocks of rows: then the same work is done, and there are no pieces to join.
-        for (int g = tid >> 5; g < c.groups; g += kPlanThreads / 32) {
+        for (int g = tid >> 5; g < c.groups; g += threads / 32) {
             const int r0 = c.group[g], r1 = c.group[g + 1];
             int least = c.shared[g], active = 0, fewest = 0x7fffffff;
             for (int r = r0 + lane; r < r1; r += 32) {
@@ -95,38 +168,34 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
             for (int r = r0 + lane; r < r1; r += 32) share[r] = Share{-1, 0, 0, once ? least : 0, least, r0, 0, 0};
         }
         __syncthreads();
-        // shared tokens: blocks of the group's rows
-        for (int g0 = 0; g0 < c.groups; g0 += kPlanThreads) {
+        // shared tokens: the group's rows
+        for (int g0 = 0; g0 < c.groups; g0 += threads) {
             const int g = g0 + tid;
-            int n = 0, r0 = 0, keys = 0, token0 = 0;
-            long long rows = 0;
+            Segment x;
+            x.rows = 0;
+            x.wide = false;
+            int r0 = 0;
             if (g < c.groups) {
                 r0 = c.group[g];
-                const int r1 = c.group[g + 1];
-                if (r1 > r0) {
-                    keys = share[r0].shared;
-                    token0 = offset[r0];
-                    rows = keys > 0 ? (long long)(offset[r1] - token0) * G : 0;
+                const int r1 = c.group[g + 1], keys = r1 > r0 ? share[r0].shared : 0;
+                if (keys > 0) {
+                    x.b = Block{offset[r0], 0, 0, r0, 0, keys, 0, keys, 0, 0, r0, 0, 0, 0};
+                    x.rows = (long long)(offset[r1] - offset[r0]) * G;
+                    x.length = keys;
+                    x.wide = x.rows > c.plan.narrow_rows;
                 }
-                n = blocks_of(c, rows);
             }
-            const bool wide = is_wide(c, rows);
-            long long total;
-            const long long packed = cta_scan((long long)(wide ? 0 : n) << 32 | (wide ? n : 0), s_scan, &total);
-            const long long at = wide ? blocks[1] + (int)packed : blocks[0] + (packed >> 32);
-            const int per = wide ? kWideRows : kNarrowRows;
-            for (int j = 0; j < n; ++j) {
-                Block b;
-                b.token0 = token0; b.row0 = j * per; b.rows = (int)min((long long)per, rows - b.row0);
-                b.request = r0; b.key0 = b.low = 0; b.keys = keys; b.limit = keys; b.step = 0; b.split = 0; b.front = r0; b.pad = 0;
-                (wide ? c.plan.wide : c.plan.narrow).block[at + j] = b;
+            Sums total;
+            const Sums at = before + cta_scan(x.sums(c), s_scan, &total);
+            if (x.rows > 0) {
+                x.write(c, at);
+                share[r0].prefix = x.wide ? (int)at.blocks : (int)(at.blocks >> 32);
+                share[r0].wide = x.wide;
             }
-            if (n > 0) { share[r0].prefix = (int)at; share[r0].wide = wide; }
-            blocks[0] += total >> 32;
-            blocks[1] += (int)total;
+            before = before + total;
         }
         __syncthreads();
-        for (int g = tid >> 5; g < c.groups; g += kPlanThreads / 32) {
+        for (int g = tid >> 5; g < c.groups; g += threads / 32) {
             const int r0 = c.group[g], r1 = c.group[g + 1];
             if (r0 == r1) continue;
             const Share first = share[r0];
@@ -138,73 +207,42 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
                 share[r] = s;
             }
         }
+        __syncthreads();
     }
-    const int own[2] = {(int)blocks[0], (int)blocks[1]};
+    const int own[2] = {(int)(before.blocks >> 32), (int)before.blocks};
     bool all_rows[2] = {false, false};
-    __syncthreads();
-    for (int first = 0; first < R; first += kPlanThreads) {
+    for (int first = 0; first < R; first += threads) {
         const int r = first + tid;
-        int n = 0, token0 = 0, len = 0, news = 0;
-        long long rows = 0;
-        Share mine{-1, 0, 0, 0, 0, 0, 0, 0};
+        Segment x;
+        x.rows = 0;
+        x.wide = false;
+        bool joined = false;
         if (r < R) {
-            token0 = offset[r];
-            news = offset[r + 1] - token0;
-            len = length[r];
-            mine = share[r];
-            rows = (long long)news * G;
-            n = blocks_of(c, rows);
+            const Share mine = share[r];
+            const int token0 = offset[r], news = offset[r + 1] - token0, len = length[r];
             if (kKept) c.plan.share[r] = mine;
+            x.b = Block{token0, 0, 0, r, 0, 0, mine.shared, c.causal ? len - news + 1 : len, c.causal, (int)c.cache.by_page.quotient(mine.split), mine.front, 0, 0, 0};
+            x.rows = (long long)news * G;
+            x.length = len;
+            x.wide = x.rows > c.plan.narrow_rows;
+            joined = mine.prefix >= 0;
         }
-        const bool wide = is_wide(c, rows);
-        long long total;
-        const long long packed = cta_scan((long long)(wide ? 0 : n) << 32 | (wide ? n : 0), s_scan, &total);
-        const long long at = wide ? blocks[1] + (int)packed : blocks[0] + (packed >> 32);
-        const int per = wide ? kWideRows : kNarrowRows;
-        for (int j = 0; j < n; ++j) {
-            Block b;
-            b.token0 = token0; b.row0 = j * per; b.rows = (int)min((long long)per, rows - b.row0);
-            b.request = r; b.low = mine.shared; b.split = c.cache.by_page.quotient(mine.split); b.front = mine.front; b.pad = 0;
-            b.key0 = wide ? b.low / kWideKeys * kWideKeys : b.low;
-            b.step = c.causal ? 1 : 0;
-            b.limit = c.causal ? len - news + 1 : len;
-            const int last = min(len, b.limit + b.step * ((b.row0 + b.rows - 1) / G));
-            b.keys = last > b.low ? last - b.key0 : 0;
-            all_rows[wide] |= b.keys == 0 || mine.prefix >= 0;
-            (wide ? c.plan.wide : c.plan.narrow).block[at + j] = b;
+        Sums total;
+        const Sums at = before + cta_scan(x.sums(c), s_scan, &total);
+        if (x.rows > 0) {
+            const bool every = x.write(c, at) || joined;
+            all_rows[0] |= every && !x.wide;
+            all_rows[1] |= every && x.wide;
         }
-        blocks[0] += total >> 32;
-        blocks[1] += (int)total;
+        before = before + total;
     }
-    const int any = __syncthreads_or((all_rows[0] ? 1 : 0)) , any_wide = __syncthreads_or(all_rows[1] ? 1 : 0);
-    long long before = 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const List& l = i ? c.plan.wide : c.plan.narrow;
-        const int keys = i ? kWideKeys : kNarrowKeys;
-        long long steps = 0, rows = 0;
-        for (int first = 0; first < blocks[i]; first += kPlanThreads) {
-            const int b = first + tid;
-            long long s = 0, w = 0;
-            if (b < blocks[i]) {
-                s = (long long)((l.block[b].keys + keys - 1) / keys) * c.cache.heads;
-                w = l.block[b].rows;
-            }
-            // (rows of 1024 blocks: up to 2^18; their steps: below 2^41)
-            long long total;
-            const long long at = cta_scan(s << 19 | w, s_scan, &total);
-            if (b < blocks[i]) {
-                l.steps[b] = l.block[b].first_step = steps + (at >> 19);
-                l.block[b].first_row = before + rows + (at & 0x7ffff);
-            }
-            steps += total >> 19;
-            rows += total & 0x7ffff;
-        }
-        if (tid == 0) {
-            l.steps[blocks[i]] = steps;
-            *l.head = PlanHead{steps, (int)blocks[i], own[i], i ? any_wide : any, 0};
-        }
-        before = rows;
+    const int any[2] = {__syncthreads_or(all_rows[0]) != 0, __syncthreads_or(all_rows[1]) != 0};
+    if (tid < 2) {
+        const List& l = tid ? c.plan.wide : c.plan.narrow;
+        const int blocks = tid ? (int)before.blocks : (int)(before.blocks >> 32);
+        const long long steps = tid ? before.steps[1] : before.steps[0];
+        l.steps[blocks] = steps;
+        *l.head = PlanHead{steps, tid ? before.rows >> 32 : 0, blocks, tid ? own[1] : own[0], tid ? any[1] : any[0], 0};
     }
 }
 
@@ -278,15 +316,31 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
         split = b.split;
     };
     tables();
-    auto look_up = [&]() -> longlong2 {
+    // A lane's key of the step at `load`: its page, not looked at before it is copied a step later (it comes from memory), and where it is in there.
+    struct Key {
+        int id, row, h;                          // row -1: none
+    };
+    auto look_up = [&]() -> Key {
+        Key k{0, -1, load.h};
         const int in = load.tile * kNarrowKeys + lane;
-        return lane < kNarrowKeys && in < load.keys ? place_of(c, table, front_table, split, load.key0 + in, load.h) : make_longlong2(-1, -1);
+        if (lane < kNarrowKeys && in < load.keys) {
+            const unsigned key = load.key0 + in, pg = c.cache.by_page.quotient(key);
+            k.row = (int)(key - pg * c.cache.page);
+            k.id = ((int)pg < split ? front_table : table)[pg];
+        }
+        return k;
     };
     // this lane's chunks of the 16 keys, and of their values
     constexpr int kChunks = D / 8, kCopies = kNarrowKeys * kChunks / 32;
-    auto fetch = [&](int step, longlong2 found) {
-        if (lane < kNarrowKeys) place[lane] = found;
-        const bool missing = __any_sync(0xffffffffu, lane < kNarrowKeys && found.x < 0);
+    auto fetch = [&](int step, const Key& k) {
+        const bool there = k.row >= 0 && k.id >= 0 && k.id < c.cache.pages;
+        if (lane < kNarrowKeys) {
+            place[lane] = there ? make_longlong2(offset_of(c.cache.k_page, c.cache.k_token, c.cache.k_head, k.id, k.row, k.h),
+                                                 offset_of(c.cache.v_page, c.cache.v_token, c.cache.v_head, k.id, k.row, k.h))
+                                : make_longlong2(-1, -1);
+            if (k.row >= 0 && !there) *c.status = ARDIFF_ERR_SHAPE;
+        }
+        const bool missing = __any_sync(0xffffffffu, lane < kNarrowKeys && !there);
         __syncwarp();
         const uint32_t to = ring_at + (step % kStages<D>) * kStageBytes<D>;
         longlong2 p[kCopies];
@@ -317,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
         else cp_async_commit();
         if (s + 1 < n && load.next(list, H)) tables();
     }
-    longlong2 found = n > kStages<D> ? look_up() : make_longlong2(-1, -1);
+    Key found = look_up();
 
     const int G = c.x.G, quad = lane & 3, row8 = lane >> 2;
     uint32_t q[kTiles][D / 16][4];
@@ -478,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
             const Block b = list.block[now.b];
             const long long unit = b.first_step + (long long)now.h * now.tiles;       // its first step
             const bool direct = whole && ends && now.b >= own && c.plan.share[b.request].prefix < 0;
-            const long long at = direct ? 0 : piece_row<false>(c, b, now.h, worker, quotient_of(unit, each));
+            const long long at = direct ? 0 : piece_row<false>(c, 0, b, now.h, worker, quotient_of(unit, each));
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -517,15 +571,15 @@ struct Cut {
     int first, count, cap, rows, in;
     __device__ __forceinline__ long long piece(int i) const { return i ? others + (long long)(first + i) * cap : main; }
 };
-template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, long long steps, const Block& k, int h, int in) {
+template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, const PlanHead& head, const Block& k, int h, int in) {
     const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
     Cut u;
     u.rows = k.rows; u.in = in; u.cap = Sizes<kWide>::rows;
-    u.main = k.first_row * c.cache.heads + (long long)h * k.rows;
+    u.main = (head.rows_before + k.first_row) * c.cache.heads + (long long)h * k.rows;
     u.others = kWide ? c.pieces.wide_rows : c.pieces.narrow_rows;
     u.first = u.count = 0;
     if (tiles) {
-        const long long each = steps_each<kWide>(steps, list_of<kWide>(c).workers), s0 = k.first_step + (long long)h * tiles;
+        const long long each = steps_each<kWide>(head.steps, list_of<kWide>(c).workers), s0 = k.first_step + (long long)h * tiles;
         u.first = quotient_of(s0, each);
         u.count = quotient_of(s0 + tiles - 1, each) - u.first + 1;
     }
@@ -542,7 +596,7 @@ template <int D> struct Joined {
 };
 
 template <typename T, int D, bool kWide>
-__device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half, long long narrow_steps, long long wide_steps, const Block& k, const Share& share,
+__device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half, const PlanHead& narrow, const PlanHead& wide, const Block& k, const Share& share,
                                           Cut mine, int h, int first_row) {
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % kJoinWarps, G = c.x.G;
     const int r = lane % kJoinRows, quarter = lane / kJoinRows, in = first_row + r;
@@ -552,8 +606,8 @@ __device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half,
     theirs.count = 0;
     if (share.prefix >= 0 && there) {
         const int row = share.row0 + k.row0 + in;
-        theirs = share.wide ? cut_of<true>(c, wide_steps, c.plan.wide.block[share.prefix + row / kWideRows], h, row % kWideRows)
-                            : cut_of<false>(c, narrow_steps, c.plan.narrow.block[share.prefix], h, row);
+        theirs = share.wide ? cut_of<true>(c, wide, c.plan.wide.block[share.prefix + row / kWideRows], h, row % kWideRows)
+                            : cut_of<false>(c, narrow, c.plan.narrow.block[share.prefix], h, row);
     }
     const int all = there ? mine.count + theirs.count : 0;
     float top = -INFINITY, sum = 0.f;
@@ -644,10 +698,10 @@ __device__ __forceinline__ void join_list(const Call& c, Joined<D>& s, int half,
             if (b < head.own || unit >= at || unit < at - each) continue;
         }
         const Share share = c.plan.share[k.request];
-        const Cut mine = cut_of<kWide>(c, head.steps, k, h, 0);
+        const Cut mine = cut_of<kWide>(c, head, k, h, 0);
         if (mine.count == 1 && share.prefix < 0) continue;                              // written already
         for (int row = row0; row < min(row0 + rows, k.rows); row += kJoinRows)
-            join_rows<T, D, kWide>(c, s, half, narrow.steps, wide.steps, k, share, mine, h, row);
+            join_rows<T, D, kWide>(c, s, half, narrow, wide, k, share, mine, h, row);
     }
 }
 
@@ -701,7 +755,7 @@ template <typename T, int D, int kTiles> bool launch_narrow(const Call& c, cudaS
 template <typename T, int D> bool launch(const Call& c, int32_t dtype, int most, int sms, cudaStream_t st) {
     const bool wide = may_be_wide(c, most);
     ardiff::set_launch_count(wide ? 4 : 3);
-    return launch_early(c.requests <= kPlanKept ? plan_kernel<true> : plan_kernel<false>, 1, kPlanThreads, 1, 0, st, c) && (!wide || launch_wide(c, dtype, D, st)) &&
+    return launch_early(c.requests <= kPlanKept ? plan_kernel<true> : plan_kernel<false>, 1, c.requests <= 64 ? 64 : c.requests <= 256 ? 256 : kPlanThreads, 1, 0, st, c) && (!wide || launch_wide(c, dtype, D, st)) &&
            (c.plan.narrow_rows > 16 ? launch_narrow<T, D, 2>(c, st) : launch_narrow<T, D, 1>(c, st)) &&
            launch_early(join_kernel<T, D>, 4 * sms, 256, 1, 0, st, c);
 }

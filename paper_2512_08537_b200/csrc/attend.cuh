@@ -45,11 +45,12 @@ __device__ __forceinline__ long long offset_of(uint32_t page_stride, uint32_t to
 // others through row `request`.
 struct alignas(16) Block {
     int token0, row0, rows, request, key0, keys, low, limit, step, split, front, pad;
-    long long first_step, first_row;             // steps of the list's blocks before; rows of all blocks before, the narrow list's first
+    long long first_step, first_row;             // steps and rows of the list's blocks before
 };
 
 struct PlanHead {
     long long steps;                             // of all blocks: key tiles times kv heads
+    long long rows_before;                       // of the other list, in front of this one's among the pieces
     int blocks, own;                             // blocks [0, own): shared tokens; [own, blocks): the requests' own
     int all_rows, pad;                           // whether there are rows to join beside those of units that are cut
 };
@@ -123,22 +124,22 @@ __device__ __forceinline__ int quotient_of(long long a, long long b) {
     return (a | b) >> 32 ? (int)(a / b) : (int)((uint32_t)a / (uint32_t)b);
 }
 
-template <bool kWide> __device__ __forceinline__ long long piece_row(const Call& c, const Block& k, int h, int worker, int first) {
+template <bool kWide> __device__ __forceinline__ long long piece_row(const Call& c, long long rows_before, const Block& k, int h, int worker, int first) {
     return worker != first ? (kWide ? c.pieces.wide_rows : c.pieces.narrow_rows) + (long long)worker * Sizes<kWide>::rows
-                           : k.first_row * c.cache.heads + (long long)h * k.rows;
+                           : (rows_before + k.first_row) * c.cache.heads + (long long)h * k.rows;
 }
 
 __device__ __forceinline__ float* piece_values(const Call& c, long long piece, int width, int rows, int row, int value) {
     return c.pieces.o + piece * width + ((long long)(value >> 2) * rows + row) * 4 + (value & 3);
 }
 
-// Where a worker is in the line of steps: block, head, tile of keys.
-template <bool kWide> struct Cursor {
+// Where a wide worker is in the line of steps: block, head, tile of keys.
+struct Cursor {
     int b, h, tile, tiles;
     Block at;
     __device__ __forceinline__ void enter(const Call& c) {
-        at = list_of<kWide>(c).block[b];
-        tiles = (at.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
+        at = c.plan.wide.block[b];
+        tiles = (at.keys + kWideKeys - 1) / kWideKeys;
     }
     __device__ __forceinline__ void start(const Call& c, int block, long long step) {
         b = block;
@@ -160,21 +161,18 @@ template <bool kWide> struct Cursor {
     }
 };
 
-// The offsets of key `key` of a head in the caches of keys and values, -1 for none.
-__device__ __forceinline__ longlong2 place_of(const Call& c, const int32_t* table, const int32_t* front_table, int split, unsigned key, int h) {
-    const unsigned pg = c.cache.by_page.quotient(key), row = key - pg * c.cache.page;
-    const int id = ((int)pg < split ? front_table : table)[pg];
+// The offsets of key `j` of the tile at `load` in the caches of keys and values, -1 for none.
+__device__ __forceinline__ longlong2 place_of(const Call& c, const Cursor& load, int j) {
+    const int in = load.tile * kWideKeys + j;
+    if (in >= load.at.keys) return make_longlong2(-1, -1);
+    const unsigned key = load.at.key0 + in, pg = c.cache.by_page.quotient(key), row = key - pg * c.cache.page;
+    const int id = c.cache.table[(long long)((int)pg < load.at.split ? load.at.front : load.at.request) * c.cache.width + pg];
     if (id < 0 || id >= c.cache.pages) {
         *c.status = ARDIFF_ERR_SHAPE;
         return make_longlong2(-1, -1);
     }
-    return make_longlong2(offset_of(c.cache.k_page, c.cache.k_token, c.cache.k_head, id, row, h), offset_of(c.cache.v_page, c.cache.v_token, c.cache.v_head, id, row, h));
-}
-template <bool kWide> __device__ __forceinline__ longlong2 place_of(const Call& c, const Cursor<kWide>& load, int j) {
-    const int in = load.tile * Sizes<kWide>::keys + j;
-    if (in >= load.at.keys) return make_longlong2(-1, -1);
-    return place_of(c, c.cache.table + (long long)load.at.request * c.cache.width, c.cache.table + (long long)load.at.front * c.cache.width, load.at.split,
-                    load.at.key0 + in, load.h);
+    return make_longlong2(offset_of(c.cache.k_page, c.cache.k_token, c.cache.k_head, id, row, load.h),
+                          offset_of(c.cache.v_page, c.cache.v_token, c.cache.v_head, id, row, load.h));
 }
 
 // The wide blocks (attend_wide.cu).

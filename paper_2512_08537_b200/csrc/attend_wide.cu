@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
     const long long steps = list.head->steps, each = steps_each<true>(steps, list.workers), begin = each * blockIdx.x;
     const int n = (int)max(0ll, min(steps, begin + each) - begin), own = list.head->own, G = c.x.G;
     const Waits wait{bars, &s_stop, c.status};
-    Cursor<true> now;
+    Cursor now;
     if (n > 0) now.start(c, find_last(list.steps, list.head->blocks, begin), begin);
 
     if (n == 0) {
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
             bool whole = true;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                found[u] = place_of<true>(c, now, u * 32 + lane);
+                found[u] = place_of(c, now, u * 32 + lane);
                 whole &= found[u].x >= 0;
             }
             whole = __all_sync(0xffffffffu, whole);
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
         const int full = v ? kVFull : kKFull, empty = v ? kVEmpty : kKEmpty, tokens = boxes.tokens;
         const CUtensorMap* map = v ? &boxes.v : &boxes.k;
         const uint32_t to = at + (v ? kV : kK) + lane * tokens * 128;
-        Cursor<true> load = now;                 // of the box that is looked up next
+        Cursor load = now;                 // of the box that is looked up next
         struct Box { int id, row, head; } next;
         auto look_up = [&]() {
             const int in = load.tile * kWideKeys + lane * tokens, key = load.at.key0 + in;
@@ -526,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                     const bool there = in < now.at.rows;
                     const int head = now.h * G + row - tok * G;
                     T* to = static_cast<T*>(c.x.out) + (there ? (now.at.token0 + (long long)tok) * c.x.out_token + head * c.x.out_head : 0);
-                    const long long piece = direct ? 0 : piece_row<true>(c, now.at, now.h, blockIdx.x, quotient_of(unit, each));
+                    const long long piece = direct ? 0 : piece_row<true>(c, list.head->rows_before, now.at, now.h, blockIdx.x, quotient_of(unit, each));
                     if (m == -INFINITY) l = l == l ? 0.f : l;                // no key was seen
                     const float f = l > 0.f ? 1.f / l : l;
 #pragma unroll 1
