@@ -4,14 +4,16 @@
 //
 // lse comes from the attention itself, so no maximum and no second pass is needed, and every key's sum stands alone. Products are
 // transposed: 128 keys are the rows of the left operand, so that a sum over queries is one thread's (a lane of tensor memory), and up to 128
-// query rows of a head the columns, 16 at least. A CTA takes consecutive tiles of 128 keys of a request, up to 8 together, and goes through rows
-// and heads for all of them, so that queries are fetched once for 8 tiles; keys stream through four stages. Where there are fewer tiles than
+// query rows of a head the columns, 16 at least. A CTA takes consecutive tiles of 128 keys of a request, up to 8 together, and goes through heads
+// and rows for all of them, so that queries are fetched once for 8 tiles; up to 16 rows a head and 16 heads are fetched at once, and heads
+// follow one another inside a tile, as they lie in memory. Keys stream through four stages. Where there are fewer tiles than
 // SMs, the heads of a tile are split among CTAs, and the last of them adds the parts in their order. No atomics on sums: equal calls give equal bits.
 //
 // Bound by the keys' memory for few rows (512 bytes would be keys and values; here it is 256 a head of 128 values), by exponentials (16 a clock and SM)
 // from some 90 rows a kv head on.
 //
-// Warps: 0-3 and 4-7 sums, every other product each; 8 issues products; 9 copies keys (by TMA where pages allow, else by 16 bytes), 10 queries.
+// Warps: 0-3 and 4-7 sums, every other product each; 8 issues products; 9 copies keys (by TMA where pages allow, else by 16 bytes), 10 queries, 11 what is
+// known of their rows.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -30,9 +32,10 @@ namespace {
 using namespace ardiff;
 
 constexpr int kPlanThreads = 1024;
-constexpr int kThreads = 11 * 32;
+constexpr int kThreads = 12 * 32;
 constexpr int kKeys = 128, kRows = 128;          // of a product
 constexpr int kTogether = 8;                     // tiles of keys
+constexpr int kFew = 16;                         // rows of a head, and heads, that are fetched at once
 constexpr int kStages = 4, kScores = 4;          // keys in shared memory, products in tensor memory
 constexpr int kMaxSplit = 256;                   // CTAs, where heads are split among them
 
@@ -92,9 +95,12 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_kernel(const Weights c) {
 // Consecutive tiles of one request that are worked on together.
 struct Segment {
     int r, tiles, key0, keys;                    // keys: the end of the request's
-    int first, token0, news, rows, chunks;       // chunks of up to 128 of its rows
+    int first, token0, news, rows;
+    // what is gone through for every tile: `units` of queries (chunks of up to 128 rows of a head), or one of all heads (few)
+    int units, heads;                            // heads: of a unit
+    bool few;
 };
-__device__ __forceinline__ Segment segment(const Weights& c, long long at, long long end) {
+__device__ __forceinline__ Segment segment(const Weights& c, long long at, long long end, int heads) {
     Segment s;
     s.r = find_last(c.tiles, c.requests, at);
     s.first = first_of(c, s.r);
@@ -104,7 +110,9 @@ __device__ __forceinline__ Segment segment(const Weights& c, long long at, long 
     s.token0 = c.offset[s.r];
     s.news = c.offset[s.r + 1] - s.token0;
     s.rows = s.news * c.x.G;
-    s.chunks = (s.rows + kRows - 1) / kRows;
+    s.few = s.rows <= kFew && heads <= kFew;
+    s.heads = s.few ? heads : 1;
+    s.units = s.rows == 0 ? 0 : s.few ? 1 : (s.rows + kRows - 1) / kRows * heads;
     return s;
 }
 
@@ -115,6 +123,38 @@ template <int D> constexpr int kShared = 1024 + (kStages + 2) * kTile<D> + 2 * k
 enum Bar { kKFull, kKEmpty = kKFull + kStages, kSFull = kKEmpty + kStages, kSEmpty = kSFull + kScores, kQFull = kSEmpty + kScores, kQEmpty = kQFull + 2,
            kColFull = kQEmpty + 2, kColEmpty = kColFull + 2, kDrained = kColEmpty + 2, kBars };
 
+// The sum of a key's weights from `cols` scores in tensor memory; kSome: only rows that see the key.
+template <bool kSome> __device__ __forceinline__ float sum_of(uint32_t scores, const float* column, const int* seen, int cols, float scale, int key) {
+    const Two scale2 = two(scale, scale);
+    Two sum[2] = {two(0.f, 0.f), two(0.f, 0.f)};
+    const int groups = (cols + 15) / 16;
+    uint32_t x[2][16];
+    ptx::tmem_ld_32x32b_x16(scores, x[0]);
+    for (int g = 0; g < groups; g += 2) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if (g + e >= groups) break;
+            ptx::tmem_ld_wait_for(x[e]);
+            if (g + e + 1 < groups) ptx::tmem_ld_32x32b_x16(scores + (g + e + 1) * 16, x[e ^ 1]);
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                const float4 c = *reinterpret_cast<const float4*>(column + (g + e) * 16 + j);
+                const float2 a = apart(fma2(two(__uint_as_float(x[e][j]), __uint_as_float(x[e][j + 1])), scale2, two(c.x, c.y)));
+                const float2 b = apart(fma2(two(__uint_as_float(x[e][j + 2]), __uint_as_float(x[e][j + 3])), scale2, two(c.z, c.w)));
+                float2 p = make_float2(ex2(a.x), ex2(a.y)), q = make_float2(ex2(b.x), ex2(b.y));
+                if (kSome) {
+                    const int4 k = *reinterpret_cast<const int4*>(seen + (g + e) * 16 + j);
+                    p.x = key < k.x ? p.x : 0.f; p.y = key < k.y ? p.y : 0.f; q.x = key < k.z ? q.x : 0.f; q.y = key < k.w ? q.y : 0.f;
+                }
+                sum[0] = sum[0] + two(p.x, p.y);
+                sum[1] = sum[1] + two(q.x, q.y);
+            }
+        }
+    }
+    const float2 s = apart(sum[0] + sum[1]);
+    return s.x + s.y;
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, const __grid_constant__ KeyBoxes boxes) {
     extern __shared__ char raw[];
@@ -122,7 +162,9 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
     constexpr int kQ = kStages * kTile<D>;
     float* sums = reinterpret_cast<float*>(smem + kQ + 2 * kTile<D>);                 // [2][tiles][128]: every other product's
     long long* place = reinterpret_cast<long long*>(sums + 2 * kTogether * kKeys);   // [tiles][128]: offsets of keys (odd: none), or of boxes
-    float2* column = reinterpret_cast<float2*>(place + kTogether * kKeys);           // [2][128]: -lse log2 e, keys that the row sees
+    // of the rows of both buffers of queries (few: 16 a head, in both): -lse log2 e, keys that the row sees
+    float* column = reinterpret_cast<float*>(place + kTogether * kKeys);
+    int* seen = reinterpret_cast<int*>(column + 2 * kRows);
     __shared__ __align__(8) uint64_t s_bar[kBars];
     __shared__ uint32_t s_tmem;
     __shared__ int s_stop, s_last;
@@ -172,7 +214,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
         for (int u = 0; u < kPeriod; ++u) to[u] = smem_at + swizzled(row0 + u * kAtOnce, ch);
         uint32_t i = 0;
         for (long long at = begin; at < end && good;) {
-            const Segment s = segment(c, at, end);
+            const Segment s = segment(c, at, end, h1 - h0);
             const int32_t* table = c.cache.table + (long long)s.r * c.cache.width;
             const int step = tokens ? tokens : 1;
             __syncwarp();
@@ -188,10 +230,10 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
                 place[j] = p;
             }
             __syncwarp();
-            for (int chunk = 0; chunk < s.chunks && good; ++chunk)
-                for (int h = h0; h < h1 && good; ++h)
-                    for (int t = 0; t < s.tiles; ++t, ++i) {
-                        const int stage = i % kStages;
+            for (int v = 0; v < s.units && good; ++v)
+                for (int t = 0; t < s.tiles && good; ++t)
+                    for (int w = 0; w < s.heads; ++w, ++i) {
+                        const int stage = i % kStages, h = h0 + (s.few ? w : v % (h1 - h0));
                         good = all(wait(kKEmpty + stage, ((i / kStages) & 1) ^ 1));
                         if (!good) break;
                         const uint32_t bar = bars + (kKFull + stage) * 8;
@@ -228,75 +270,97 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
         cp_async_commit();
         cp_async_wait<0>();
     } else if (warp == 10) {
-        // ---- queries, and what their columns need
+        // ---- queries
         constexpr int kLanes = D / 8 <= 8 ? 8 : 16;
         const int ch = lane % kLanes;
         const bool mine = ch < D / 8;
         uint32_t u = 0;
+        bool few = false;                        // the unit before
         for (long long at = begin; at < end && good;) {
-            const Segment s = segment(c, at, end);
-            const int limit = c.causal ? s.keys - s.news + 1 : s.keys;
-            for (int chunk = 0; chunk < s.chunks && good; ++chunk)
-                for (int h = h0; h < h1; ++h, ++u) {
-                    const int buf = u & 1, rows = min(kRows, s.rows - chunk * kRows);
-                    good = all(wait(kQEmpty + buf, ((u >> 1) & 1) ^ 1) && wait(kColEmpty + buf, ((u >> 1) & 1) ^ 1));
-                    if (!good) break;
+            const Segment s = segment(c, at, end, h1 - h0);
+            for (int v = 0; v < s.units; ++v, ++u) {
+                const int buf = u & 1;
+                // (few: both buffers, when all units before are done with)
+                good = all(wait(kQEmpty + buf, ((u >> 1) & 1) ^ 1) && (!(s.few || few) || u == 0 || wait(kQEmpty + (buf ^ 1), ((u - 1) >> 1) & 1)));
+                if (!good) break;
+                few = s.few;
+                for (int w = 0; w < s.heads; ++w) {
+                    const int h = h0 + (s.few ? w : v % (h1 - h0)), row0 = s.few ? 0 : v / (h1 - h0) * kRows, rows = min(kRows, s.rows - row0);
+                    const uint32_t to = smem_at + kQ + (s.few ? w * kSub<D> * 2048 : buf * kTile<D>);
                     const T* base = static_cast<const T*>(c.x.q) + (long long)s.token0 * c.x.q_token + (long long)h * G * c.x.q_head + ch * 8;
-#pragma unroll 4
+#pragma unroll 8
                     for (int in = lane / kLanes; in < (rows + 15) / 16 * 16; in += 32 / kLanes) {
-                        const unsigned row = chunk * kRows + in, tok = c.x.by_G.quotient(row);
+                        const unsigned row = row0 + in, tok = c.x.by_G.quotient(row);
                         const T* from = base + (in < rows ? tok * c.x.q_token + (row - tok * G) * c.x.q_head : 0);
-                        if (mine) cp_async16(smem_at + kQ + buf * kTile<D> + swizzled(in, ch), from, in < rows ? 16 : 0);
+                        const uint32_t place_in = s.few ? (ch >> 3) * 2048 + in * 128 + (((ch & 7) ^ (in & 7)) << 4) : swizzled(in, ch);
+                        if (mine) cp_async16(to + place_in, from, in < rows ? 16 : 0);
                     }
-                    cp_async_arrive(bars + (kQFull + buf) * 8);
-                    for (int in = lane; in < (rows + 15) / 16 * 16; in += 32) {
-                        const unsigned row = chunk * kRows + in, tok = c.x.by_G.quotient(row);
-                        float2 v = make_float2(-INFINITY, 0.f);                        // no such row
-                        if (in < rows) {
-                            const float lse = c.x.lse[(s.token0 + (long long)tok) * c.x.lse_token + h * G + row - tok * G];
-                            v.x = lse == -INFINITY ? -INFINITY : lse * -1.4426950408889634f;      // a row without keys
-                            v.y = __int_as_float(limit + (c.causal ? (int)tok : 0));
-                        }
-                        column[buf * kRows + in] = v;
-                    }
-                    ptx::mbar_arrive(bars + (kColFull + buf) * 8);
                 }
+                cp_async_arrive(bars + (kQFull + buf) * 8);
+            }
             at += s.tiles;
         }
         cp_async_commit();
         cp_async_wait<0>();
+    } else if (warp == 11) {
+        // ---- what is known of their rows
+        uint32_t u = 0;
+        bool few = false;
+        for (long long at = begin; at < end && good;) {
+            const Segment s = segment(c, at, end, h1 - h0);
+            const int limit = c.causal ? s.keys - s.news + 1 : s.keys;
+            for (int v = 0; v < s.units; ++v, ++u) {
+                const int buf = u & 1;
+                good = all(wait(kColEmpty + buf, ((u >> 1) & 1) ^ 1) && (!(s.few || few) || u == 0 || wait(kColEmpty + (buf ^ 1), ((u - 1) >> 1) & 1)));
+                if (!good) break;
+                few = s.few;
+                for (int j = lane; j < (s.few ? s.heads * kFew : kRows); j += 32) {
+                    const int in = s.few ? j % kFew : j, h = h0 + (s.few ? j / kFew : v % (h1 - h0)), row = in + (s.few ? 0 : v / (h1 - h0) * kRows);
+                    float x = -INFINITY;                                               // no such row
+                    int y = 0;
+                    if (row < s.rows) {
+                        const unsigned tok = c.x.by_G.quotient(row);
+                        const float lse = c.x.lse[(s.token0 + (long long)tok) * c.x.lse_token + h * G + row - tok * G];
+                        x = lse == -INFINITY ? -INFINITY : lse * -1.4426950408889634f;            // a row without keys
+                        y = limit + (c.causal ? (int)tok : 0);
+                    }
+                    column[(s.few ? 0 : buf * kRows) + j] = x;
+                    seen[(s.few ? 0 : buf * kRows) + j] = y;
+                }
+                ptx::mbar_arrive(bars + (kColFull + buf) * 8);
+            }
+            at += s.tiles;
+        }
     } else if (warp == 8) {
         // ---- products
         const uint64_t q_desc = ptx::smem_desc_sw128(smem_at + kQ), k_desc = ptx::smem_desc_sw128(smem_at);
         uint32_t i = 0, u = 0;
         for (long long at = begin; at < end && good;) {
-            const Segment s = segment(c, at, end);
-            for (int chunk = 0; chunk < s.chunks && good; ++chunk)
-                for (int h = h0; h < h1 && good; ++h, ++u) {
-                    const int rows = min(kRows, s.rows - chunk * kRows);
-                    const uint32_t idesc = ptx::idesc_16(Pair<T>::kBf16, kKeys, (rows + 15) / 16 * 16, false, false);
-                    const uint64_t b = q_desc + (u & 1) * (kTile<D> / 16);
-                    good = all(wait(kQFull + (u & 1), (u >> 1) & 1));
-                    for (int t = 0; t < s.tiles && good; ++t, ++i) {
+            const Segment s = segment(c, at, end, h1 - h0);
+            for (int v = 0; v < s.units && good; ++v, ++u) {
+                const int rows = s.few ? kFew : min(kRows, s.rows - v / (h1 - h0) * kRows);
+                const uint32_t idesc = ptx::idesc_16(Pair<T>::kBf16, kKeys, (rows + 15) / 16 * 16, false, false);
+                const uint32_t next = s.few ? 128 : 1024;                              // blocks of 64 values of the queries, in 16 bytes
+                good = all(wait(kQFull + (u & 1), (u >> 1) & 1));
+                for (int t = 0; t < s.tiles && good; ++t)
+                    for (int w = 0; w < s.heads; ++w, ++i) {
                         const int stage = i % kStages, to = i % kScores;
                         good = all(wait(kKFull + stage, (i / kStages) & 1) && wait(kSEmpty + to, ((i / kScores) & 1) ^ 1));
                         if (!good) break;
                         ptx::fence_proxy_async_smem();
                         ptx::tc_fence_after();
-                        const uint64_t a = k_desc + stage * (kTile<D> / 16);
+                        const uint64_t a = k_desc + stage * (kTile<D> / 16), b = q_desc + (s.few ? w * kSub<D> * 128 : (u & 1) * (kTile<D> / 16));
                         if (ptx::elect_one()) {
 #pragma unroll
-                            for (int ks = 0; ks < D / 16; ++ks) {
-                                const uint32_t in = (ks >> 2) * 1024 + (ks & 3) * 2;
-                                ptx::mma_f16_ss(tmem + to * 128, a + in, b + in, idesc, ks > 0);
-                            }
+                            for (int ks = 0; ks < D / 16; ++ks)
+                                ptx::mma_f16_ss(tmem + to * 128, a + (ks >> 2) * 1024 + (ks & 3) * 2, b + (ks >> 2) * next + (ks & 3) * 2, idesc, ks > 0);
                             ptx::mma_commit(bars + (kSFull + to) * 8);
                             ptx::mma_commit(bars + (kKEmpty + stage) * 8);
-                            if (t + 1 == s.tiles) ptx::mma_commit(bars + (kQEmpty + (u & 1)) * 8);
+                            if (t + 1 == s.tiles && w + 1 == s.heads) ptx::mma_commit(bars + (kQEmpty + (u & 1)) * 8);
                         }
                         __syncwarp();
                     }
-                }
+            }
             at += s.tiles;
         }
         if (!good) {
@@ -312,46 +376,29 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
         uint32_t i = 0, u = 0;
         for (long long at = begin; at < end;) {
-            const Segment s = segment(c, at, end);
+            const Segment s = segment(c, at, end, h1 - h0);
             float* mine = sums + side * kTogether * kKeys + key;
             for (int t = 0; t < s.tiles; ++t) mine[t * kKeys] = 0.f;
             const int least = c.causal ? s.keys - s.news + 1 : s.keys;              // keys below are seen by all rows
-            for (int chunk = 0; chunk < s.chunks && good; ++chunk)
-                for (int h = h0; h < h1 && good; ++h, ++u) {
-                    const int groups = (min(kRows, s.rows - chunk * kRows) + 15) / 16;
-                    const float2* col = column + (u & 1) * kRows;
-                    good = all(wait(kColFull + (u & 1), (u >> 1) & 1));
-                    for (int t = 0; t < s.tiles && good; ++t, ++i) {
+            for (int v = 0; v < s.units && good; ++v, ++u) {
+                const int cols = s.few ? s.rows : min(kRows, s.rows - v / (h1 - h0) * kRows);
+                good = all(wait(kColFull + (u & 1), (u >> 1) & 1));
+                for (int t = 0; t < s.tiles && good; ++t)
+                    for (int w = 0; w < s.heads; ++w, ++i) {
                         if ((int)(i & 1) != side) continue;
-                        const int from = i % kScores;
+                        const int from = i % kScores, at_col = s.few ? w * kFew : (u & 1) * kRows;
                         good = all(wait(kSFull + from, (i / kScores) & 1));
                         if (!good) break;
                         ptx::tc_fence_after();
-                        const int p = s.key0 + t * kKeys + key;
-                        const bool zone = s.key0 + (t + 1) * kKeys > least;
-                        float sum[2] = {0.f, 0.f};
-                        uint32_t x[2][16];
-                        ptx::tmem_ld_32x32b_x16(lanes + from * 128, x[0]);
-                        for (int g = 0; g < groups; g += 2) {
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                if (g + e >= groups) break;
-                                ptx::tmem_ld_wait_for(x[e]);
-                                if (g + e + 1 < groups) ptx::tmem_ld_32x32b_x16(lanes + from * 128 + (g + e + 1) * 16, x[e ^ 1]);
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) {
-                                    const float2 v = col[(g + e) * 16 + j];
-                                    const float w = ex2(fmaf(__uint_as_float(x[e][j]), c.scale, v.x));
-                                    sum[j & 1] += !zone || p < __float_as_int(v.y) ? w : 0.f;
-                                }
-                            }
-                        }
+                        const uint32_t scores = lanes + from * 128;
+                        mine[t * kKeys] += s.key0 + (t + 1) * kKeys > least
+                                               ? sum_of<true>(scores, column + at_col, seen + at_col, cols, c.scale, s.key0 + t * kKeys + key)
+                                               : sum_of<false>(scores, column + at_col, seen + at_col, cols, c.scale, 0);
                         ptx::tc_fence_before();
                         ptx::mbar_arrive(bars + (kSEmpty + from) * 8);
-                        mine[t * kKeys] += sum[0] + sum[1];
                     }
-                    ptx::mbar_arrive(bars + (kColEmpty + (u & 1)) * 8);
-                }
+                ptx::mbar_arrive(bars + (kColEmpty + (u & 1)) * 8);
+            }
             ptx::bar_sync(2, 256);               // (all eight warps come here for every segment, whether they gave up or not)
             if (split == 1) {
                 for (int t = side; t < s.tiles; t += 2) {
