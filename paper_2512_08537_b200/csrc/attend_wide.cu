@@ -615,6 +615,17 @@ bool ardiff::describe(CUtensorMap* map, const char* base, bool bf16, int width, 
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool ardiff::describe_queries(CUtensorMap* map, const Queries& x, bool bf16, int width, int rows) {
+    if (x.tokens < 1 || rows % x.G || x.q_token < 0 || x.q_head < 0 || (x.q_token | x.q_head) >> 38) return false;
+    const EncodeTiled f = encoder();
+    if (!f) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)x.heads, (cuuint64_t)x.tokens};
+    const cuuint64_t strides[2] = {x.heads > 1 && x.q_head ? 2 * (cuuint64_t)x.q_head : 16, x.tokens > 1 && x.q_token ? 2 * (cuuint64_t)x.q_token : 16};
+    const cuuint32_t box[3] = {64, (cuuint32_t)x.G, (cuuint32_t)(rows / x.G)}, ones[3] = {1, 1, 1};
+    return f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(x.q), dims, strides, box, ones,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool ardiff::launch_wide(const Call& c, int32_t dtype, int width, cudaStream_t st) {
     Boxes boxes;
     memset(&boxes, 0, sizeof(boxes));

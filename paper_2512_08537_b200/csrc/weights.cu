@@ -57,8 +57,9 @@ struct Weights {
 };
 
 struct KeyBoxes {
-    CUtensorMap k;
-    int tokens;                                  // of a box; 0: by 16 bytes
+    CUtensorMap k, q, few;                       // few: boxes of 16 rows of queries
+    int tokens;                                  // of a box of keys; 0: by 16 bytes
+    bool queries;                                // by boxes
 };
 
 // The first key of a request's tiles: a multiple of 128, so that boxes of tokens do not cross pages.
@@ -185,7 +186,8 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
             int count = 1;
             if (i < kKEmpty) count = boxes.tokens ? 1 : 32;
             else if (i >= kSEmpty && i < kQFull) count = 128;
-            else if ((i >= kQFull && i < kQEmpty) || (i >= kColFull && i < kColEmpty)) count = 32;
+            else if (i >= kQFull && i < kQEmpty) count = boxes.queries ? 1 : 32;
+            else if (i >= kColFull && i < kColEmpty) count = 32;
             else if (i >= kColEmpty && i < kDrained) count = 256;
             ptx::mbar_init(bars + i * 8, count);
         }
@@ -284,6 +286,18 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
                 good = all(wait(kQEmpty + buf, ((u >> 1) & 1) ^ 1) && (!(s.few || few) || u == 0 || wait(kQEmpty + (buf ^ 1), ((u - 1) >> 1) & 1)));
                 if (!good) break;
                 few = s.few;
+                if (boxes.queries) {
+                    const uint32_t bar = bars + (kQFull + buf) * 8;
+                    if (lane == 0) ptx::mbar_arrive_expect_tx(bar, s.few ? s.heads * kSub<D> * kFew * 128 : kTile<D>);
+                    __syncwarp();
+                    // (rows of other requests behind this one's are no rows of its columns)
+                    for (int j = lane; j < s.heads * kSub<D>; j += 32) {
+                        const int w = j / kSub<D>, x = j - w * kSub<D>, h = h0 + (s.few ? w : v % (h1 - h0));
+                        if (s.few) ptx::tma_load_3d(smem_at + kQ + j * kFew * 128, &boxes.few, bar, x * 64, h * G, s.token0);
+                        else ptx::tma_load_3d(smem_at + kQ + buf * kTile<D> + x * 16384, &boxes.q, bar, x * 64, h * G, s.token0 + v / (h1 - h0) * (kRows / G));
+                    }
+                    continue;
+                }
                 for (int w = 0; w < s.heads; ++w) {
                     const int h = h0 + (s.few ? w : v % (h1 - h0)), row0 = s.few ? 0 : v / (h1 - h0) * kRows, rows = min(kRows, s.rows - row0);
                     const uint32_t to = smem_at + kQ + (s.few ? w * kSub<D> * 2048 : buf * kTile<D>);
@@ -391,7 +405,8 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
                         if (!good) break;
                         ptx::tc_fence_after();
                         const uint32_t scores = lanes + from * 128;
-                        mine[t * kKeys] += s.key0 + (t + 1) * kKeys > least
+                        // (a column that is no row of the request may hold anything)
+                        mine[t * kKeys] += s.key0 + (t + 1) * kKeys > least || (cols & 15)
                                                ? sum_of<true>(scores, column + at_col, seen + at_col, cols, c.scale, s.key0 + t * kKeys + key)
                                                : sum_of<false>(scores, column + at_col, seen + at_col, cols, c.scale, 0);
                         ptx::tc_fence_before();
@@ -503,6 +518,7 @@ extern "C" int ardiff_attend_weights(const void* q, int64_t q_token, int64_t q_h
     memset(&boxes, 0, sizeof(boxes));
     const int box = box_tokens(page);
     if (box && describe(&boxes.k, c.cache.k, bf16, head_width, box, c.cache, c.cache.k_token, c.cache.k_head, c.cache.k_page)) boxes.tokens = box;
+    boxes.queries = describe_queries(&boxes.q, c.x, bf16, head_width, kRows) && describe_queries(&boxes.few, c.x, bf16, head_width, kFew);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool ok = bf16 ? launch_width<__nv_bfloat16>(c, head_width, boxes, sms, st) : launch_width<__half>(c, head_width, boxes, sms, st);
     ardiff::set_launch_count(2);
