@@ -325,7 +325,4 @@ bool describe_queries(CUtensorMap* map, const Queries& x, bool bf16, int width, 
 // The largest power of two of tokens, up to 128, that divides a page; 0 where it is below the 8 rows of a swizzled block.
 int box_tokens(int page);
 
-// The current device's SM count; 0 where that fails. Asked once a device.
-int device_sms();
-
 }  // namespace ardiff

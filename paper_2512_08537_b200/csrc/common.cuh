@@ -30,6 +30,9 @@ int write_zero_count(int32_t* count, cudaStream_t st);
 void gate_load_kernels();
 void load_prefix_kernel();
 
+// the current device's SM count; 0 where that fails. Asked once a device
+int device_sms();
+
 // shape of a head (for callers that must match their buffers to it)
 const ardiff_head_desc* head_desc(const ardiff_head* head);
 

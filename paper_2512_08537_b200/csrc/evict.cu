@@ -6,9 +6,10 @@
 // became free. So as many rows move as leave a place free below the new end, not the whole cache, and sources (>= keep) and
 // destinations (< keep) are apart: all moves run at once, in place.
 //
-// Two kernels. The first finds, by CTA a request, the keep-th largest weight by three counts of 11 bits each over whole numbers that order as
-// the weights do, then walks the places once more with a running count of heavier and equal ones: the number kept in front of a place p is
-// heavier(p) + min(equal(p), equal ones needed), which gives every hole and every token behind the end its rank. The second copies the rows.
+// Two kernels. The first finds, by CTA a request (or a cluster of eight, where there are few requests of many tokens), the keep-th largest weight by three
+// counts of 11, 11 and 10 bits over whole numbers that order as the weights do, then walks the places once more with a running count of heavier and
+// equal ones: the number kept in front of a place p is heavier(p) + min(equal(p), equal ones needed), which gives every hole and every token
+// behind the end its rank. CTAs of a cluster have a stretch of places each and read one another's counts. The second kernel copies the rows.
 // Bound by the latency of those passes where few rows move, by memory where many do.
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -19,6 +20,7 @@
 #include "../../include/ardiff.h"
 #include "common.cuh"
 #include "launch.cuh"
+#include "ptx.cuh"
 #include "rows.cuh"
 
 namespace {
@@ -26,7 +28,8 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kBins = 2048;
 constexpr int kPer = 4;                          // places of a thread, consecutive, in the last walk
-constexpr int kKept = 40960;                     // keys that shared memory holds; more are worked out again in every pass
+constexpr int kKept = 40960;                     // keys that a CTA's shared memory holds; more are worked out again in every pass
+constexpr int kCluster = 8;
 
 struct Evict {
     const int32_t* length;
@@ -83,23 +86,50 @@ __device__ __forceinline__ uint2 cta_scan(uint2 v, uint2* s, uint2* total) {
     return make_uint2(inc.x - v.x + __shfl_sync(0xffffffffu, w.x, warp), inc.y - v.y + __shfl_sync(0xffffffffu, w.y, warp));
 }
 
+__device__ __forceinline__ uint32_t peer(const uint32_t* p, int cta) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(ptx::map_peer(ptx::smem_u32(p), cta)) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void add_to_peer(const uint32_t* p, int cta, uint32_t v) {
+    asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(ptx::map_peer(ptx::smem_u32(p), cta)), "r"(v) : "memory");
+}
+
+// kParts CTAs (a cluster) a request.
+template <int kParts>
 __global__ void __launch_bounds__(kThreads) select_kernel(const Evict a) {
     extern __shared__ uint32_t s_key[];
-    __shared__ uint32_t s_bin[kBins];
+    __shared__ uint32_t s_bin[kBins], s_all[kParts > 1 ? 2 : 1][kParts > 1 ? kBins : 1], s_counts[4];      // heavier, equal: of the stretch, and of its part in front of the new end
     __shared__ uint2 s_scan[32];
-    __shared__ uint32_t s_prefix, s_rest, s_inside;
+    __shared__ uint32_t s_prefix, s_rest;
     ardiff::begin_kernel();
-    const int tid = threadIdx.x, r = blockIdx.x;
-    if (r == 0) {
+    const int tid = threadIdx.x, r = blockIdx.x / kParts, rank = blockIdx.x % kParts;
+    auto meet = [&]() {
+        if (kParts > 1) ptx::cluster_sync_all();
+        else __syncthreads();
+    };
+    auto sum_of = [&](const uint32_t* p, int parts) {
+        uint32_t v = 0;
+        if constexpr (kParts == 1) {
+            v = parts ? *p : 0u;
+        } else {
+            for (int i = 0; i < parts; ++i) v += peer(p, i);
+        }
+        return v;
+    };
+    if (kParts > 1)
+        for (int b = tid; b < kBins; b += kThreads) s_all[0][b] = 0;
+    if (blockIdx.x == 0) {
         bool bad = false;
         for (int i = tid; i < a.requests; i += kThreads) bad |= a.length[i] < 0 || (long long)a.length[i] > a.limit;
         bad = __syncthreads_or(bad);
         if (tid == 0) *a.status = bad ? ARDIFF_ERR_SHAPE : ARDIFF_OK;
     }
     const int length = a.length[r];
-    __syncthreads();                             // new_length may be the length itself
+    meet();                                      // new_length may be the length itself
     if (length < 0 || (long long)length > a.limit) {         // left as it is
-        if (tid == 0) { a.new_length[r] = length; a.moves[r] = 0; }
+        if (tid == 0 && rank == 0) { a.new_length[r] = length; a.moves[r] = 0; }
         return;
     }
     const int first = a.first ? min(max(a.first[r], 0), length) : 0;
@@ -110,14 +140,16 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const Evict a) {
     float* new_score = a.new_score + r * a.new_ld;
     int32_t* new_position = a.new_position ? a.new_position + r * a.new_ld : nullptr;
     int32_t* source = a.source ? a.source + r * a.new_ld : nullptr;
-    if (tid == 0) a.new_length[r] = keep;
+    meet();                                      // (seen, first or budget may be the same array, too)
+    if (tid == 0 && rank == 0) a.new_length[r] = keep;
+    auto stay = [&](int p) {
+        new_score[p] = score[p];
+        if (new_position) new_position[p] = position ? position[p] : p;
+        if (source) source[p] = p;
+    };
     if (keep == length) {
-        if (tid == 0) a.moves[r] = 0;
-        for (int p = tid; p < length; p += kThreads) {
-            new_score[p] = score[p];
-            if (new_position) new_position[p] = position ? position[p] : p;
-            if (source) source[p] = p;
-        }
+        if (tid == 0 && rank == 0) a.moves[r] = 0;
+        for (int p = rank * kThreads + tid; p < length; p += kParts * kThreads) stay(p);
         return;
     }
 
@@ -125,33 +157,48 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const Evict a) {
         const long long pos = position ? position[p] : p;
         return pos >= recent_from ? kInfinite : ordered(score[p]);
     };
-    const int n = length - first;
-    auto key = [&](int i) -> uint32_t { return i < kKept ? s_key[i] : work_out(first + i); };
-    for (int i = tid; i < min(n, kKept); i += kThreads) s_key[i] = work_out(first + i);
+    const int n = length - first, stretch = ((n + kParts - 1) / kParts + kPer - 1) / kPer * kPer;
+    const int lo = min(n, rank * stretch), hi = min(n, lo + stretch), end = keep - first;     // of this CTA; the new end
+    auto key = [&](int i) -> uint32_t { return i - lo < kKept ? s_key[i - lo] : work_out(first + i); };
+    for (int i = lo + tid; i < min(hi, lo + kKept); i += kThreads) s_key[i - lo] = work_out(first + i);
 
     // the need-th largest key, by its highest 11 bits, the next 11, the last 10
-    uint32_t prefix = 0, need = keep - first;
+    uint32_t prefix = 0, need = end;
     constexpr int shift[3] = {21, 10, 0}, above[3] = {32, 21, 10};
     if (need > 0) {
 #pragma unroll
         for (int round = 0; round < 3; ++round) {
-            for (int b = tid; b < kBins; b += kThreads) s_bin[b] = 0;
+            // (two lots of sums: the next round's is cleared while this one's is not yet complete)
+            for (int b = tid; b < kBins; b += kThreads) {
+                s_bin[b] = 0;
+                if (kParts > 1) s_all[kParts > 1 ? (round + 1) & 1 : 0][b] = 0;
+            }
             __syncthreads();
             const uint32_t mask = round == 2 ? 1023u : 2047u;
-            for (int i = tid; i < n; i += kThreads) {
+            for (int i = lo + tid; i < hi; i += kThreads) {
                 const uint32_t k = key(i);
                 if (round == 0 || (k >> above[round]) == (prefix >> above[round])) atomicAdd(&s_bin[(k >> shift[round]) & mask], 1u);
             }
             __syncthreads();
+            const uint32_t* bin = s_bin;
+            if (kParts > 1) {
+                // every CTA adds its few bins that are not empty to everyone's sums
+                uint32_t* sums = s_all[kParts > 1 ? round & 1 : 0];
+                for (int b = tid; b < kBins; b += kThreads)
+                    if (s_bin[b])
+                        for (int i = 0; i < kParts; ++i) add_to_peer(sums + b, i, s_bin[b]);
+                meet();
+                bin = sums;
+            }
             // bins from the top: thread t has the two from kBins - 1 - 2 t down
             const int top = kBins - 1 - 2 * tid;
-            const uint32_t hi = s_bin[top], lo = s_bin[top - 1];
+            const uint32_t upper = bin[top], lower = bin[top - 1];
             uint2 total;
-            const uint32_t before = cta_scan(make_uint2(hi + lo, 0u), s_scan, &total).x;
-            if (before < need && need <= before + hi + lo) {
-                const bool second = need > before + hi;
+            const uint32_t before = cta_scan(make_uint2(upper + lower, 0u), s_scan, &total).x;
+            if (before < need && need <= before + upper + lower) {
+                const bool second = need > before + upper;
                 s_prefix = prefix | ((uint32_t)(second ? top - 1 : top) << shift[round]);
-                s_rest = need - before - (second ? hi : 0u);
+                s_rest = need - before - (second ? upper : 0u);
             }
             __syncthreads();
             prefix = s_prefix;
@@ -160,50 +207,52 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const Evict a) {
         }
     } else {
         prefix = 0xffffffffu;                    // nothing is heavier or as heavy
+        __syncthreads();
     }
     const uint32_t border = prefix, equal = need;
 
-    // places in order: what is kept, its rank; holes below keep, tokens behind it
-    int2* move = a.move + (long long)r * a.capacity;
+    // heavier and equal ones in front of this CTA's places, and of all in front of the new end
     uint2 carry = make_uint2(0u, 0u);
-    uint32_t inside = 0;                         // kept ones of first .. keep - 1
-    for (int base = 0; base < n; base += kThreads * kPer) {
+    uint32_t inside;
+    {
+        uint2 all = make_uint2(0u, 0u), front = make_uint2(0u, 0u);
+        for (int i = lo + tid; i < hi; i += kThreads) {
+            const uint32_t k = key(i);
+            all.x += k > border; all.y += k == border;
+            if (i < end) { front.x += k > border; front.y += k == border; }
+        }
+        uint2 sum_all, sum_front;
+        cta_scan(all, s_scan, &sum_all);
+        cta_scan(front, s_scan, &sum_front);
+        if (tid == 0) { s_counts[0] = sum_all.x; s_counts[1] = sum_all.y; s_counts[2] = sum_front.x; s_counts[3] = sum_front.y; }
+        meet();
+        if (kParts > 1) carry = make_uint2(sum_of(&s_counts[0], rank), sum_of(&s_counts[1], rank));
+        inside = sum_of(&s_counts[2], kParts) + min(sum_of(&s_counts[3], kParts), equal);
+    }
+
+    // places in order: what is kept, its rank; holes in front of the new end, tokens behind it
+    int2* move = a.move + (long long)r * a.capacity;
+    for (int base = lo; base < hi; base += kThreads * kPer) {
         uint32_t k[kPer];
         uint2 mine = make_uint2(0u, 0u);
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
             const int i = base + tid * kPer + u;
-            k[u] = i < n ? key(i) : 0u;
-            if (i < n) { mine.x += k[u] > border; mine.y += k[u] == border; }
+            k[u] = i < hi ? key(i) : 0u;
+            if (i < hi) { mine.x += k[u] > border; mine.y += k[u] == border; }
         }
         uint2 total;
         uint2 at = cta_scan(mine, s_scan, &total);
         at.x += carry.x; at.y += carry.y;
-        if (base <= keep - first && keep - first < base + kThreads * kPer) {
-            uint2 c = at;
-#pragma unroll
-            for (int u = 0; u < kPer; ++u) {
-                const int i = base + tid * kPer + u;
-                if (i == keep - first) s_inside = c.x + min(c.y, equal);
-                c.x += k[u] > border; c.y += k[u] == border;
-            }
-            __syncthreads();
-            inside = s_inside;
-        }
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
             const int i = base + tid * kPer + u, p = first + i;
-            if (i < n) {
+            if (i < hi) {
                 const uint32_t before = at.x + min(at.y, equal);
                 const bool stays = k[u] > border || (k[u] == border && at.y < equal);
                 if (p < keep) {
-                    if (!stays) {
-                        move[i - before].x = p;
-                    } else {
-                        new_score[p] = score[p];
-                        if (new_position) new_position[p] = position ? position[p] : p;
-                        if (source) source[p] = p;
-                    }
+                    if (stays) stay(p);
+                    else move[i - before].x = p;
                 } else if (stays) {
                     move[before - inside].y = p;
                 }
@@ -212,15 +261,11 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const Evict a) {
         }
         carry.x += total.x; carry.y += total.y;
     }
-    for (int p = tid; p < first; p += kThreads) {
-        new_score[p] = score[p];
-        if (new_position) new_position[p] = position ? position[p] : p;
-        if (source) source[p] = p;
-    }
-    const int moves = keep - first - (int)inside;
-    if (tid == 0) a.moves[r] = moves;
-    __syncthreads();
-    for (int j = tid; j < moves; j += kThreads) {
+    for (int p = rank * kThreads + tid; p < first; p += kParts * kThreads) stay(p);
+    const int moves = end - (int)inside;
+    if (tid == 0 && rank == 0) a.moves[r] = moves;
+    meet();
+    for (int j = rank * kThreads + tid; j < moves; j += kParts * kThreads) {
         const int2 m = move[j];
         new_score[m.x] = score[m.y];
         if (new_position) new_position[m.x] = position ? position[m.y] : m.y;
@@ -272,16 +317,6 @@ __global__ void __launch_bounds__(256) move_kernel(const Evict a, int split) {
     }
 }
 
-bool prepare_device() {
-    static std::atomic<bool> known[64] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return false;
-    if (dev < 64 && known[dev].load(std::memory_order_relaxed)) return true;
-    if (cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKept * 4) != cudaSuccess) return false;
-    if (dev < 64) known[dev].store(true, std::memory_order_relaxed);
-    return true;
-}
-
 // moves of a request: as many as there are holes below the new end and tokens behind it
 int64_t move_capacity(int64_t limit) { return limit / 2 + 1; }
 
@@ -314,7 +349,6 @@ extern "C" int ardiff_pages_evict(int32_t requests, const int32_t* length, const
     const int64_t limit = (int64_t)page * width;
     if (workspace_bytes < ardiff_pages_evict_workspace(requests, page, width) && requests > 0) return ARDIFF_ERR_SHAPE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (!prepare_device()) return ARDIFF_ERR_CUDA;
     Evict a;
     memset(&a, 0, sizeof(a));
     a.length = length; a.budget = budget; a.first = first; a.score = score; a.position = position; a.seen = seen; a.table = table;
@@ -334,9 +368,18 @@ extern "C" int ardiff_pages_evict(int32_t requests, const int32_t* length, const
         ardiff::set_launch_count(0);
         return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
     }
-    const int64_t keys = limit < kKept ? limit : kKept;
+    const int sms = ardiff::device_sms();
+    if (sms < 1) return ARDIFF_ERR_CUDA;
+    // A cluster a request where that fills no more than two rounds of the SMs and a CTA has 512 places or more of the longest one (8 requests of 16384:
+    // 38 us with a CTA each, 13 with eight).
+    const bool clusters = requests * kCluster <= 2 * sms && limit >= kCluster * 512;
+    const int64_t places = clusters ? (limit + kCluster - 1) / kCluster + kPer : limit, keys = places < kKept ? places : kKept;
     const int split = requests >= 592 ? 1 : (592 + requests - 1) / requests;
-    const bool ok = ardiff::launch_early(select_kernel, (unsigned)requests, kThreads, 1, (size_t)keys * 4, st, a) &&
+    static std::atomic<uint64_t> ready[2] = {};
+    const bool ok = (clusters ? ardiff::shared_memory(select_kernel<kCluster>, kKept * 4, ready[1]) &&
+                                    ardiff::launch_early(select_kernel<kCluster>, (unsigned)requests * kCluster, kThreads, kCluster, (size_t)keys * 4, st, a)
+                              : ardiff::shared_memory(select_kernel<1>, kKept * 4, ready[0]) &&
+                                    ardiff::launch_early(select_kernel<1>, (unsigned)requests, kThreads, 1, (size_t)keys * 4, st, a)) &&
                     ardiff::launch_early(move_kernel, (unsigned)(requests * split), 256, 1, 0, st, a, split);
     ardiff::set_launch_count(2);
     return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
