@@ -210,7 +210,7 @@ __device__ __forceinline__ uint4 to_chunk(const Words& w) { return make_uint4(w.
 // kNeighbours: pairs 2 i, 2 i + 1. Else kAligned: the number of pairs fills whole chunks, so that a chunk's other halves are one other chunk.
 // `split` warps share a token.
 template <typename T, bool kNeighbours, bool kAligned, bool kAppend>
-__global__ void __launch_bounds__(kThreads) rows_kernel(const Rotary a, int lanes, int split) {
+__global__ void __launch_bounds__(kThreads, 3) rows_kernel(const Rotary a, int lanes, int split) {
     constexpr int N = Piece<T>::N;               // values of a chunk
     extern __shared__ char smem[];
     float2* cs = reinterpret_cast<float2*>(smem);                                   // [tokens][pairs]
