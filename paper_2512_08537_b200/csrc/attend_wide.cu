@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                 if (tile == 1 && !two) break;
                 if (tile == 0) {
                     good = all(wait(kVFull + stage, parity));
-                    ptx::fence_proxy_async_smem();
+                    if (!boxes.tokens) ptx::fence_proxy_async_smem();          // (TMA writes where products read)
                 }
                 good = good && all(wait(kPFull + tile, p_count[tile] & 1));
                 ++p_count[tile];
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                     if (tile == 0) {
                         good = all(wait(kKFull + stage1, parity1));
                         if (!good) break;
-                        ptx::fence_proxy_async_smem();
+                        if (!boxes.tokens) ptx::fence_proxy_async_smem();
                         ptx::tc_fence_after();
                     }
                     scores(tile, stage1);
