@@ -366,10 +366,16 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
         cp_async_commit();
         __syncwarp();
     };
+    Key first[kStages<D>];                       // (all sent for before one is looked at)
+#pragma unroll
     for (int s = 0; s < kStages<D>; ++s) {
-        if (s < n) fetch(s, look_up());
-        else cp_async_commit();
+        if (s < n) first[s] = look_up();
         if (s + 1 < n && load.next(list, H)) tables();
+    }
+#pragma unroll
+    for (int s = 0; s < kStages<D>; ++s) {
+        if (s < n) fetch(s, first[s]);
+        else cp_async_commit();
     }
     Key found = look_up();
 
