@@ -536,23 +536,45 @@ int ardiff_distill_topk_step(const void* logits, int32_t dtype, int64_t n, int32
  *   count       dev int32 [1], or NULL: tokens from *count on (a padded batch: offset[requests] of the extension) are not touched */
 #define ARDIFF_ROTARY_MAX_WIDTH 512
 #define ARDIFF_ROTARY_MAX_HEADS 1024
-int ardiff_rotary(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head,
-                  int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, void* k_out, int64_t k_out_token,
-                  int64_t k_out_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width, const int32_t* position,
-                  int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs, int32_t neighbours,
-                  void* stream);
-int ardiff_rotary_backward(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head,
-                           int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, void* k_out, int64_t k_out_token,
-                           int64_t k_out_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width, const int32_t* position,
-                           int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs,
-                           int32_t neighbours, void* stream);
-int ardiff_rotary_append(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head,
-                         int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, const void* v, int64_t v_token,
-                         int64_t v_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width, const int32_t* position,
-                         int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs,
-                         int32_t neighbours, const int64_t* slot, const int32_t* count, void* k_cache, int64_t k_cache_page,
-                         int64_t k_cache_token, int64_t k_cache_head, void* v_cache, int64_t v_cache_page, int64_t v_cache_token,
-                         int64_t v_cache_head, int32_t pages, int32_t page, void* stream);
+typedef struct {
+    const void* q;
+    int64_t q_token, q_head;
+    void* q_out;
+    int64_t q_out_token, q_out_head, q_heads;
+    const void* k;
+    int64_t k_token, k_head;
+    void* k_out;
+    int64_t k_out_token, k_out_head, k_heads, dtype, n, width;
+    const int32_t* position;
+    int64_t position_ld, axes;
+    const float* freq;
+    const int32_t* axis;
+    int64_t pairs, neighbours;
+} ardiff_rotary_call;
+int ardiff_rotary(const ardiff_rotary_call* call, void* stream);
+int ardiff_rotary_backward(const ardiff_rotary_call* call, void* stream);
+typedef struct {
+    const void* q;
+    int64_t q_token, q_head;
+    void* q_out;
+    int64_t q_out_token, q_out_head, q_heads;
+    const void* k;
+    int64_t k_token, k_head;
+    const void* v;
+    int64_t v_token, v_head, k_heads, dtype, n, width;
+    const int32_t* position;
+    int64_t position_ld, axes;
+    const float* freq;
+    const int32_t* axis;
+    int64_t pairs, neighbours;
+    const int64_t* slot;
+    const int32_t* count;
+    void* k_cache;
+    int64_t k_cache_page, k_cache_token, k_cache_head;
+    void* v_cache;
+    int64_t v_cache_page, v_cache_token, v_cache_head, pages, page;
+} ardiff_rotary_append_call;
+int ardiff_rotary_append(const ardiff_rotary_append_call* call, void* stream);
 
 /* Attention of new tokens over pages. Request r's new tokens are rows offset[r] .. offset[r + 1] - 1 of q, its length[r] tokens (the new
  * ones among them, at its end) lie in the pages of its row of the table. With G = q_heads / heads, query head h looks at head h / G:
@@ -577,13 +599,30 @@ int ardiff_rotary_append(const void* q, int64_t q_token, int64_t q_head, void* q
  * Products take 16-bit operands with fp32 sums; weights are fp32 and rounded to dtype as operands of the second product, their sum is
  * that of the unrounded ones. The order of sums follows sizes, lengths and `most`: equal calls give equal bits. */
 int64_t ardiff_attend_workspace(int32_t requests, int32_t groups, int64_t tokens, int32_t q_heads, int32_t heads, int32_t head_width);
-int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype, const void* k_cache,
-                        int64_t k_page, int64_t k_token, int64_t k_head, const void* v_cache, int64_t v_page, int64_t v_token,
-                        int64_t v_head, int32_t pages, int32_t page, int32_t heads, int32_t head_width, const int32_t* table,
-                        int32_t width, int32_t requests, const int32_t* length, const int32_t* offset, int32_t groups,
-                        const int32_t* group, const int32_t* shared, int32_t most, float scale, int32_t causal, void* out,
-                        int64_t out_token, int64_t out_head, float* lse, int64_t lse_token, int32_t* status, void* workspace,
-                        int64_t workspace_bytes, void* stream);
+typedef struct {
+    const void* q;
+    int64_t q_token, q_head, q_heads, tokens, dtype;
+    const void* k_cache;
+    int64_t k_page, k_token, k_head;
+    const void* v_cache;
+    int64_t v_page, v_token, v_head, pages, page, heads, head_width;
+    const int32_t* table;
+    int64_t width, requests;
+    const int32_t* length, *offset;
+    int64_t groups;
+    const int32_t* group, *shared;
+    int64_t most;
+    double scale;
+    int64_t causal;
+    void* out;
+    int64_t out_token, out_head;
+    float* lse;
+    int64_t lse_token;
+    int32_t* status;
+    void* workspace;
+    int64_t workspace_bytes;
+} ardiff_attend_pages_call;
+int ardiff_attend_pages(const ardiff_attend_pages_call* call, void* stream);
 
 /* The weight that every token got, added up (what eviction goes by):
  *   new_score[r][p] = (p < length[r] - n ? decay * score[r][p] : 0) + sum over the n new tokens that see p and all query heads of
@@ -594,12 +633,27 @@ int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_head, int32_t 
  *   score, new_score  dev float [requests], rows ld and new_ld apart (lengths may not pass either); may be the same
  *   status      as above;  workspace  16-byte aligned, at least ardiff_attend_weights_workspace(requests) bytes */
 int64_t ardiff_attend_weights_workspace(int32_t requests);
-int ardiff_attend_weights(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype,
-                          const void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head, int32_t pages, int32_t page,
-                          int32_t heads, int32_t head_width, const int32_t* table, int32_t width, int32_t requests,
-                          const int32_t* length, const int32_t* offset, const int32_t* first, const float* lse, int64_t lse_token,
-                          const float* score, int64_t ld, float scale, float decay, int32_t causal, float* new_score,
-                          int64_t new_ld, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
+typedef struct {
+    const void* q;
+    int64_t q_token, q_head, q_heads, tokens, dtype;
+    const void* k_cache;
+    int64_t k_page, k_token, k_head, pages, page, heads, head_width;
+    const int32_t* table;
+    int64_t width, requests;
+    const int32_t* length, *offset, *first;
+    const float* lse;
+    int64_t lse_token;
+    const float* score;
+    int64_t ld;
+    double scale, decay;
+    int64_t causal;
+    float* new_score;
+    int64_t new_ld;
+    int32_t* status;
+    void* workspace;
+    int64_t workspace_bytes;
+} ardiff_attend_weights_call;
+int ardiff_attend_weights(const ardiff_attend_weights_call* call, void* stream);
 
 /* Eviction. Of request r's length[r] tokens keep = min(length[r], max(budget[r], first[r])) stay: those at places below first[r], and of the
  * others those of largest score, the lowest place first where equal. Tokens whose position is at or above seen[r] - recent count as
@@ -620,13 +674,28 @@ int ardiff_attend_weights(const void* q, int64_t q_token, int64_t q_head, int32_
  *   workspace   dev, 16-byte aligned, at least ardiff_pages_evict_workspace(requests, page, width) bytes; nothing is kept in it between
  *               calls, but calls that may run at the same time need their own */
 int64_t ardiff_pages_evict_workspace(int32_t requests, int32_t page, int32_t width);
-int ardiff_pages_evict(int32_t requests, const int32_t* length, const int32_t* budget, const int32_t* first, const float* score,
-                       int64_t ld, const int32_t* position, const int32_t* seen, int32_t recent, const int32_t* table,
-                       int32_t width, int32_t dtype, void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head,
-                       void* v_cache, int64_t v_page, int64_t v_token, int64_t v_head, int32_t pages, int32_t page,
-                       int32_t heads, int32_t head_width, int32_t* new_length, float* new_score, int32_t* new_position,
-                       int32_t* source, int64_t new_ld, int32_t* status, void* workspace, int64_t workspace_bytes,
-                       void* stream);
+typedef struct {
+    int64_t requests;
+    const int32_t* length, *budget, *first;
+    const float* score;
+    int64_t ld;
+    const int32_t* position, *seen;
+    int64_t recent;
+    const int32_t* table;
+    int64_t width, dtype;
+    void* k_cache;
+    int64_t k_page, k_token, k_head;
+    void* v_cache;
+    int64_t v_page, v_token, v_head, pages, page, heads, head_width;
+    int32_t* new_length;
+    float* new_score;
+    int32_t* new_position, *source;
+    int64_t new_ld;
+    int32_t* status;
+    void* workspace;
+    int64_t workspace_bytes;
+} ardiff_pages_evict_call;
+int ardiff_pages_evict(const ardiff_pages_evict_call* call, void* stream);
 
 /* Number of kernel launches the last call of the gate, the head, the cache's pages or the rows of logits on this
  * thread enqueued (for launch accounting by benchmarks). */

@@ -15,6 +15,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 from typing import Dict, Optional
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -125,29 +126,16 @@ def lib() -> ctypes.CDLL:
         L.ardiff_distill_topk_backward.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, i32, f32, vp, vp, vp, i64, vp]
         L.ardiff_distill_topk_step.restype = ctypes.c_int
         L.ardiff_distill_topk_step.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, i32, f32, vp, vp, vp, vp, i64, vp]
-        turn = [vp, i64, i64, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, i32, i32, i64, i32, vp, i64, i32, vp, vp, i32, i32, vp]
-        L.ardiff_rotary.restype = ctypes.c_int
-        L.ardiff_rotary.argtypes = turn
-        L.ardiff_rotary_backward.restype = ctypes.c_int
-        L.ardiff_rotary_backward.argtypes = turn
-        L.ardiff_rotary_append.restype = ctypes.c_int
-        L.ardiff_rotary_append.argtypes = [vp, i64, i64, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, i32, i32, i64, i32, vp, i64, i32,
-                                           vp, vp, i32, i32, vp, vp, vp, i64, i64, i64, vp, i64, i64, i64, i32, i32, vp]
+        for fn in (L.ardiff_rotary, L.ardiff_rotary_backward, L.ardiff_rotary_append, L.ardiff_attend_pages, L.ardiff_attend_weights,
+                   L.ardiff_pages_evict):
+            fn.restype = ctypes.c_int
+            fn.argtypes = [ctypes.c_char_p, vp]                # a packed structure, the stream
         L.ardiff_attend_workspace.restype = i64
         L.ardiff_attend_workspace.argtypes = [i32, i32, i64, i32, i32, i32]
-        L.ardiff_attend_pages.restype = ctypes.c_int
-        L.ardiff_attend_pages.argtypes = [vp, i64, i64, i32, i64, i32, vp, i64, i64, i64, vp, i64, i64, i64, i32, i32, i32, i32, vp, i32,
-                                          i32, vp, vp, i32, vp, vp, i32, f32, i32, vp, i64, i64, vp, i64, vp, vp, i64, vp]
         L.ardiff_attend_weights_workspace.restype = i64
         L.ardiff_attend_weights_workspace.argtypes = [i32]
-        L.ardiff_attend_weights.restype = ctypes.c_int
-        L.ardiff_attend_weights.argtypes = [vp, i64, i64, i32, i64, i32, vp, i64, i64, i64, i32, i32, i32, i32, vp, i32, i32, vp, vp, vp,
-                                            vp, i64, vp, i64, f32, f32, i32, vp, i64, vp, vp, i64, vp]
         L.ardiff_pages_evict_workspace.restype = i64
         L.ardiff_pages_evict_workspace.argtypes = [i32, i32, i32]
-        L.ardiff_pages_evict.restype = ctypes.c_int
-        L.ardiff_pages_evict.argtypes = [i32, vp, vp, vp, vp, i64, vp, vp, i32, vp, i32, i32, vp, i64, i64, i64, vp, i64, i64, i64, i32,
-                                         i32, i32, i32, vp, vp, vp, vp, i64, vp, vp, i64, vp]
         _lib = L
     return _lib
 
@@ -556,12 +544,20 @@ def ardiff_distill_topk_step(logits, teacher, ids, weight, temperature: float = 
     return loss, stats, grad
 
 
+# The structures that these calls take, all of 64-bit fields: packed at once, where ctypes takes a tenth of a microsecond an argument.
+_ROTARY, _APPEND = struct.Struct("24q"), struct.Struct("36q")
+_ATTEND, _WEIGHTS, _EVICT = struct.Struct("27qd9q"), struct.Struct("24q2d6q"), struct.Struct("32q")
+
+
+def _at(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
 def _heads(x, index: int):
     """Address, strides of tokens and heads, and heads of a tensor [n, heads, width] whose rows are contiguous."""
     n, heads, width = x.shape
-    assert x.get_device() == index and heads < _SIZES and width < _SIZES, f"a tensor on cuda:{index} expected, of sizes within 32 bits"
     token, head, one = x.stride()
-    assert width <= 1 or one == 1, "rows must be contiguous"
+    assert x.get_device() == index and (one == 1 or width <= 1), f"a tensor on cuda:{index} with contiguous rows expected"
     return x.data_ptr(), token, head, heads
 
 
@@ -569,9 +565,10 @@ def _out_heads(x, like, index: int):
     """The same without the number of heads, for results of the shape and type of `like`. They must not overlap themselves."""
     assert x.dtype is like.dtype and x.shape == like.shape, f"{like.dtype} {tuple(like.shape)} expected, got {x.dtype} {tuple(x.shape)}"
     n, heads, width = x.shape
-    token, head = x.stride()[:2]
+    token, head, one = x.stride()
+    assert x.get_device() == index and (one == 1 or width <= 1), f"a tensor on cuda:{index} with contiguous rows expected"
     assert (heads <= 1 or head >= width) and (n <= 1 or token >= width), "rows of results must not overlap"
-    return _heads(x, index)[:3]
+    return x.data_ptr(), token, head
 
 
 def _rotary_args(q, k, position, freq, axis):
@@ -585,11 +582,10 @@ def _rotary_args(q, k, position, freq, axis):
     assert position.dtype is t.i32 and position.get_device() == index and position.shape[1] == n and (n <= 1 or position.stride(1) == 1), \
         f"int32 positions [axes, {n}] on cuda:{index} expected"
     pairs = freq.numel()
-    assert n < _SIZES and pairs < _SIZES and axes < _SIZES, _TOO_LARGE
     _check_f32(freq, pairs, index)
     if axis is not None:
         _check_i32(axis, pairs, index)
-    return index, t.types.get(q.dtype, -1), n, width, (position.data_ptr(), position.stride(0) if axes > 1 else 0, axes, freq.data_ptr(), _ptr(axis), pairs)
+    return index, t.types.get(q.dtype, -1), n, width, (position.data_ptr(), position.stride(0) if axes > 1 else 0, axes, freq.data_ptr(), _at(axis), pairs)
 
 
 def _turned(fn, where, q, k, position, freq, axis, neighbours, q_out, k_out):
@@ -600,8 +596,8 @@ def _turned(fn, where, q, k, position, freq, axis, neighbours, q_out, k_out):
         k_out = _torch.empty(k.shape, dtype=k.dtype, device=k.device)
     qp, qt, qh, q_heads = _heads(q, index)
     kp, kt, kh, k_heads = _heads(k, index)
-    _run(fn, where, index, qp, qt, qh, *_out_heads(q_out, q, index), q_heads, kp, kt, kh, *_out_heads(k_out, k, index), k_heads, dtype, n,
-         width, *angles, 1 if neighbours else 0)
+    _run(fn, where, index, _ROTARY.pack(qp, qt, qh, *_out_heads(q_out, q, index), q_heads, kp, kt, kh, *_out_heads(k_out, k, index), k_heads,
+                                        dtype, n, width, *angles, 1 if neighbours else 0))
     return q_out, k_out
 
 
@@ -624,11 +620,9 @@ def ardiff_rotary_backward(grad_q, grad_k, position, freq, axis=None, neighbours
 
 def _cache_args(cache, dtype, index: int):
     """Address and strides of pages, tokens and heads of a cache [pages, page, heads, width] whose rows are contiguous."""
-    assert cache.dtype is dtype and cache.get_device() == index, f"a cache of {dtype} on cuda:{index} expected"
-    pages, page, heads, width = cache.shape
-    assert pages < _SIZES and page < _SIZES and heads < _SIZES and width < _SIZES, _TOO_LARGE
     a, b, c, d = cache.stride()
-    assert width <= 1 or d == 1, "rows must be contiguous"
+    assert cache.dtype is dtype and cache.get_device() == index and (d == 1 or cache.shape[3] <= 1), \
+        f"a cache of {dtype} on cuda:{index} with contiguous rows expected"
     return cache.data_ptr(), a, b, c
 
 
@@ -650,9 +644,10 @@ def ardiff_rotary_append(q, k, v, position, freq, slot, k_cache, v_cache, axis=N
     assert k_cache.shape == v_cache.shape and k_cache.shape[2] == k.shape[1] and k_cache.shape[3] == width, "caches [pages, page, kv heads, width] expected"
     qp, qt, qh, q_heads = _heads(q, index)
     kp, kt, kh, k_heads = _heads(k, index)
-    _run(lib().ardiff_rotary_append, "ardiff_rotary_append", index, qp, qt, qh, *_out_heads(q_out, q, index), q_heads, kp, kt, kh,
-         *_heads(v, index)[:3], k_heads, dtype, n, width, *angles, 1 if neighbours else 0, slot.data_ptr(), _ptr(count),
-         *_cache_args(k_cache, k.dtype, index), *_cache_args(v_cache, k.dtype, index), pages, page)
+    _run(lib().ardiff_rotary_append, "ardiff_rotary_append", index,
+         _APPEND.pack(qp, qt, qh, *_out_heads(q_out, q, index), q_heads, kp, kt, kh, *_heads(v, index)[:3], k_heads, dtype, n, width, *angles,
+                      1 if neighbours else 0, slot.data_ptr(), _at(count), *_cache_args(k_cache, k.dtype, index),
+                      *_cache_args(v_cache, k.dtype, index), pages, page))
     return q_out
 
 
@@ -661,7 +656,7 @@ def _attend_args(q, k_cache, table, length, offset):
     R, width = table.shape
     pages, page, heads, D = k_cache.shape
     T, q_heads, _ = q.shape
-    assert R < _SIZES and width < _SIZES and T < _SIZES, _TOO_LARGE
+    assert R < _SIZES and T < _SIZES and q_heads < _SIZES and heads < _SIZES and D < _SIZES, _TOO_LARGE
     index = q.get_device()
     assert index >= 0 and q.shape[2] == D, "queries and keys of the same width expected"
     _check_i32(table, R * width, index)
@@ -674,12 +669,6 @@ def _workspace(size: int, where: str, device):
     if size < 0:
         raise ArdiffError(size, where)
     return _torch.empty((size,), dtype=_torch.u8, device=device)
-
-
-def _most(most) -> int:
-    most = 0 if most is None else most
-    assert 0 <= most < _SIZES, _TOO_LARGE
-    return most
 
 
 def ardiff_attend_pages(q, k_cache, v_cache, table, length, offset, group=None, shared=None, most=None, scale=None, causal: bool = True,
@@ -708,10 +697,11 @@ def ardiff_attend_pages(q, k_cache, v_cache, table, length, offset, group=None, 
     L = lib()
     size = L.ardiff_attend_workspace(R, groups, T, q_heads, heads, D)
     work = _workspace(size, "ardiff_attend_pages", q.device)
-    _run(L.ardiff_attend_pages, "ardiff_attend_pages", index, qp, qt, qh, q_heads, T, dtype, *_cache_args(k_cache, q.dtype, index),
-         *_cache_args(v_cache, q.dtype, index), pages, page, heads, D, table.data_ptr(), width, R, length.data_ptr(), offset.data_ptr(), groups,
-         _ptr(group), _ptr(shared), _most(most), D ** -0.5 if scale is None else scale, 1 if causal else 0, *_out_heads(out, q, index),
-         lse.data_ptr(), q_heads, status.data_ptr(), work.data_ptr(), size)
+    _run(L.ardiff_attend_pages, "ardiff_attend_pages", index,
+         _ATTEND.pack(qp, qt, qh, q_heads, T, dtype, *_cache_args(k_cache, q.dtype, index), *_cache_args(v_cache, q.dtype, index), pages, page,
+                      heads, D, table.data_ptr(), width, R, length.data_ptr(), offset.data_ptr(), groups, _at(group), _at(shared),
+                      0 if most is None else most, D ** -0.5 if scale is None else scale, 1 if causal else 0, *_out_heads(out, q, index),
+                      lse.data_ptr(), q_heads, status.data_ptr(), work.data_ptr(), size))
     return out, lse, status
 
 
@@ -748,10 +738,11 @@ def ardiff_attend_weights(q, k_cache, table, length, offset, lse, score, first=N
     L = lib()
     size = L.ardiff_attend_weights_workspace(R)
     work = _workspace(size, "ardiff_attend_weights", q.device)
-    _run(L.ardiff_attend_weights, "ardiff_attend_weights", index, qp, qt, qh, q_heads, T, dtype, *_cache_args(k_cache, q.dtype, index), pages, page,
-         heads, D, table.data_ptr(), width, R, length.data_ptr(), offset.data_ptr(), _ptr(first), lse.data_ptr(), q_heads, score.data_ptr(), ld,
-         D ** -0.5 if scale is None else scale, decay, 1 if causal else 0, new_score.data_ptr(), new_ld, status.data_ptr(),
-         work.data_ptr(), size)
+    _run(L.ardiff_attend_weights, "ardiff_attend_weights", index,
+         _WEIGHTS.pack(qp, qt, qh, q_heads, T, dtype, *_cache_args(k_cache, q.dtype, index), pages, page, heads, D, table.data_ptr(), width, R,
+                       length.data_ptr(), offset.data_ptr(), _at(first), lse.data_ptr(), q_heads, score.data_ptr(), ld,
+                       D ** -0.5 if scale is None else scale, decay, 1 if causal else 0, new_score.data_ptr(), new_ld, status.data_ptr(),
+                       work.data_ptr(), size))
     return new_score, status
 
 
@@ -768,7 +759,7 @@ def ardiff_pages_evict(length, budget, score, table, k_cache, v_cache, first=Non
     t = _t()
     R, width = table.shape
     pages, page, heads, D = k_cache.shape
-    assert R < _SIZES and width < _SIZES and 0 <= recent < _SIZES, _TOO_LARGE
+    assert R < _SIZES and width < _SIZES and page < _SIZES, _TOO_LARGE
     index = length.get_device()
     assert index >= 0 and k_cache.shape == v_cache.shape, "caches of the same shape expected"
     _check_i32(table, R * width, index)
@@ -792,10 +783,11 @@ def ardiff_pages_evict(length, budget, score, table, k_cache, v_cache, first=Non
     L = lib()
     size = L.ardiff_pages_evict_workspace(R, page, width)
     work = _workspace(size, "ardiff_pages_evict", length.device)
-    _run(L.ardiff_pages_evict, "ardiff_pages_evict", index, R, length.data_ptr(), budget.data_ptr(), _ptr(first), score.data_ptr(), ld, _ptr(position),
-         _ptr(seen), recent, table.data_ptr(), width, t.types.get(k_cache.dtype, -1), *_cache_args(k_cache, k_cache.dtype, index),
-         *_cache_args(v_cache, k_cache.dtype, index), pages, page, heads, D, new_length.data_ptr(), new_score.data_ptr(), _ptr(new_position),
-         _ptr(source), new_ld, status.data_ptr(), work.data_ptr(), size)
+    _run(L.ardiff_pages_evict, "ardiff_pages_evict", index,
+         _EVICT.pack(R, length.data_ptr(), budget.data_ptr(), _at(first), score.data_ptr(), ld, _at(position), _at(seen), recent,
+                     table.data_ptr(), width, t.types.get(k_cache.dtype, -1), *_cache_args(k_cache, k_cache.dtype, index),
+                     *_cache_args(v_cache, k_cache.dtype, index), pages, page, heads, D, new_length.data_ptr(), new_score.data_ptr(),
+                     _at(new_position), _at(source), new_ld, status.data_ptr(), work.data_ptr(), size))
     return new_length, new_score, new_position, status
 
 

@@ -797,7 +797,7 @@ extern "C" int64_t ardiff_attend_workspace(int32_t requests, int32_t groups, int
     return layout(requests, groups, tokens, q_heads, heads, head_width).bytes;
 }
 
-extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype, const void* k_cache,
+static int attend_pages_checked(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype, const void* k_cache,
                                    int64_t k_page, int64_t k_token, int64_t k_head, const void* v_cache, int64_t v_page, int64_t v_token,
                                    int64_t v_head, int32_t pages, int32_t page, int32_t heads, int32_t head_width, const int32_t* table,
                                    int32_t width, int32_t requests, const int32_t* length, const int32_t* offset, int32_t groups,
@@ -856,4 +856,15 @@ extern "C" int ardiff_attend_pages(const void* q, int64_t q_token, int64_t q_hea
     const bool ok = dtype == ARDIFF_F16 ? launch_width<__half>(c, dtype, head_width, most, sms, st)
                                         : launch_width<__nv_bfloat16>(c, dtype, head_width, most, sms, st);
     return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+}
+
+extern "C" int ardiff_attend_pages(const ardiff_attend_pages_call* a, void* stream) {
+    if (!a) return ARDIFF_ERR_NULL;
+    if (!ardiff::in_32_bits({a->q_heads, a->dtype, a->pages, a->page, a->heads, a->head_width, a->width, a->requests, a->groups, a->most,
+        a->causal})) return ARDIFF_ERR_SHAPE;
+    return attend_pages_checked(a->q, a->q_token, a->q_head, (int32_t)a->q_heads, a->tokens, (int32_t)a->dtype, a->k_cache, a->k_page,
+        a->k_token, a->k_head, a->v_cache, a->v_page, a->v_token, a->v_head, (int32_t)a->pages, (int32_t)a->page, (int32_t)a->heads,
+        (int32_t)a->head_width, a->table, (int32_t)a->width, (int32_t)a->requests, a->length, a->offset, (int32_t)a->groups, a->group,
+        a->shared, (int32_t)a->most, (float)a->scale, (int32_t)a->causal, a->out, a->out_token, a->out_head, a->lse, a->lse_token,
+        a->status, a->workspace, a->workspace_bytes, stream);
 }

@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "../../include/ardiff.h"
 
 namespace ardiff {
@@ -29,6 +31,13 @@ int write_zero_count(int32_t* count, cudaStream_t st);
 // load the gate's kernels on the current device, ahead of their first use
 void gate_load_kernels();
 void load_prefix_kernel();
+
+// whether sizes that calls take as 64 bits fit the 32 that kernels take
+inline bool in_32_bits(std::initializer_list<int64_t> sizes) {
+    for (int64_t x : sizes)
+        if (x != (int32_t)x) return false;
+    return true;
+}
 
 // the current device's SM count; 0 where that fails. Asked once a device
 int device_sms();

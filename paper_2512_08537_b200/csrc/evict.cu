@@ -328,7 +328,7 @@ extern "C" int64_t ardiff_pages_evict_workspace(int32_t requests, int32_t page, 
     return (int64_t)requests * (8 * move_capacity((int64_t)page * width) + 4) + 16;
 }
 
-extern "C" int ardiff_pages_evict(int32_t requests, const int32_t* length, const int32_t* budget, const int32_t* first, const float* score,
+static int pages_evict_checked(int32_t requests, const int32_t* length, const int32_t* budget, const int32_t* first, const float* score,
                                   int64_t ld, const int32_t* position, const int32_t* seen, int32_t recent, const int32_t* table,
                                   int32_t width, int32_t dtype, void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head,
                                   void* v_cache, int64_t v_page, int64_t v_token, int64_t v_head, int32_t pages, int32_t page,
@@ -383,4 +383,14 @@ extern "C" int ardiff_pages_evict(int32_t requests, const int32_t* length, const
                     ardiff::launch_early(move_kernel, (unsigned)(requests * split), 256, 1, 0, st, a, split);
     ardiff::set_launch_count(2);
     return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+}
+
+extern "C" int ardiff_pages_evict(const ardiff_pages_evict_call* a, void* stream) {
+    if (!a) return ARDIFF_ERR_NULL;
+    if (!ardiff::in_32_bits({a->requests, a->recent, a->width, a->dtype, a->pages, a->page, a->heads,
+        a->head_width})) return ARDIFF_ERR_SHAPE;
+    return pages_evict_checked((int32_t)a->requests, a->length, a->budget, a->first, a->score, a->ld, a->position, a->seen,
+        (int32_t)a->recent, a->table, (int32_t)a->width, (int32_t)a->dtype, a->k_cache, a->k_page, a->k_token, a->k_head, a->v_cache,
+        a->v_page, a->v_token, a->v_head, (int32_t)a->pages, (int32_t)a->page, (int32_t)a->heads, (int32_t)a->head_width, a->new_length,
+        a->new_score, a->new_position, a->source, a->new_ld, a->status, a->workspace, a->workspace_bytes, stream);
 }

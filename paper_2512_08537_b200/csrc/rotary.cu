@@ -433,7 +433,7 @@ Rotary arguments(const void* q, int64_t q_token, int64_t q_head, void* q_out, in
 
 }  // namespace
 
-extern "C" int ardiff_rotary(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head,
+static int rotary_checked(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head,
                              int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, void* k_out, int64_t k_out_token,
                              int64_t k_out_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width, const int32_t* position,
                              int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs,
@@ -444,7 +444,15 @@ extern "C" int ardiff_rotary(const void* q, int64_t q_token, int64_t q_head, voi
     return rotary(a, dtype, neighbours, false, static_cast<cudaStream_t>(stream));
 }
 
-extern "C" int ardiff_rotary_backward(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token,
+extern "C" int ardiff_rotary(const ardiff_rotary_call* a, void* stream) {
+    if (!a) return ARDIFF_ERR_NULL;
+    if (!ardiff::in_32_bits({a->q_heads, a->k_heads, a->dtype, a->width, a->axes, a->pairs, a->neighbours})) return ARDIFF_ERR_SHAPE;
+    return rotary_checked(a->q, a->q_token, a->q_head, a->q_out, a->q_out_token, a->q_out_head, (int32_t)a->q_heads, a->k, a->k_token,
+        a->k_head, a->k_out, a->k_out_token, a->k_out_head, (int32_t)a->k_heads, (int32_t)a->dtype, a->n, (int32_t)a->width, a->position,
+        a->position_ld, (int32_t)a->axes, a->freq, a->axis, (int32_t)a->pairs, (int32_t)a->neighbours, stream);
+}
+
+static int rotary_backward_checked(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token,
                                       int64_t q_out_head, int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, void* k_out,
                                       int64_t k_out_token, int64_t k_out_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width,
                                       const int32_t* position, int64_t position_ld, int32_t axes, const float* freq,
@@ -456,7 +464,15 @@ extern "C" int ardiff_rotary_backward(const void* q, int64_t q_token, int64_t q_
     return rotary(a, dtype, neighbours, false, static_cast<cudaStream_t>(stream));
 }
 
-extern "C" int ardiff_rotary_append(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token,
+extern "C" int ardiff_rotary_backward(const ardiff_rotary_call* a, void* stream) {
+    if (!a) return ARDIFF_ERR_NULL;
+    if (!ardiff::in_32_bits({a->q_heads, a->k_heads, a->dtype, a->width, a->axes, a->pairs, a->neighbours})) return ARDIFF_ERR_SHAPE;
+    return rotary_backward_checked(a->q, a->q_token, a->q_head, a->q_out, a->q_out_token, a->q_out_head, (int32_t)a->q_heads, a->k,
+        a->k_token, a->k_head, a->k_out, a->k_out_token, a->k_out_head, (int32_t)a->k_heads, (int32_t)a->dtype, a->n, (int32_t)a->width,
+        a->position, a->position_ld, (int32_t)a->axes, a->freq, a->axis, (int32_t)a->pairs, (int32_t)a->neighbours, stream);
+}
+
+static int rotary_append_checked(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token,
                                     int64_t q_out_head, int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, const void* v,
                                     int64_t v_token, int64_t v_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width,
                                     const int32_t* position, int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis,
@@ -472,4 +488,15 @@ extern "C" int ardiff_rotary_append(const void* q, int64_t q_token, int64_t q_he
     a.v_page = v_cache_page;
     a.slot = slot; a.count = count; a.page = page; a.slots = (long long)pages * page;
     return rotary(a, dtype, neighbours, true, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int ardiff_rotary_append(const ardiff_rotary_append_call* a, void* stream) {
+    if (!a) return ARDIFF_ERR_NULL;
+    if (!ardiff::in_32_bits({a->q_heads, a->k_heads, a->dtype, a->width, a->axes, a->pairs, a->neighbours, a->pages,
+        a->page})) return ARDIFF_ERR_SHAPE;
+    return rotary_append_checked(a->q, a->q_token, a->q_head, a->q_out, a->q_out_token, a->q_out_head, (int32_t)a->q_heads, a->k,
+        a->k_token, a->k_head, a->v, a->v_token, a->v_head, (int32_t)a->k_heads, (int32_t)a->dtype, a->n, (int32_t)a->width, a->position,
+        a->position_ld, (int32_t)a->axes, a->freq, a->axis, (int32_t)a->pairs, (int32_t)a->neighbours, a->slot, a->count, a->k_cache,
+        a->k_cache_page, a->k_cache_token, a->k_cache_head, a->v_cache, a->v_cache_page, a->v_cache_token, a->v_cache_head,
+        (int32_t)a->pages, (int32_t)a->page, stream);
 }

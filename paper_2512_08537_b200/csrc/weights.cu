@@ -475,7 +475,7 @@ extern "C" int64_t ardiff_attend_weights_workspace(int32_t requests) {
     return part_at(requests) + (int64_t)kMaxSplit * kKeys * 4;
 }
 
-extern "C" int ardiff_attend_weights(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype,
+static int attend_weights_checked(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype,
                                      const void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head, int32_t pages, int32_t page,
                                      int32_t heads, int32_t head_width, const int32_t* table, int32_t width, int32_t requests,
                                      const int32_t* length, const int32_t* offset, const int32_t* first, const float* lse,
@@ -523,4 +523,14 @@ extern "C" int ardiff_attend_weights(const void* q, int64_t q_token, int64_t q_h
     const bool ok = bf16 ? launch_width<__nv_bfloat16>(c, head_width, boxes, sms, st) : launch_width<__half>(c, head_width, boxes, sms, st);
     ardiff::set_launch_count(2);
     return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
+}
+
+extern "C" int ardiff_attend_weights(const ardiff_attend_weights_call* a, void* stream) {
+    if (!a) return ARDIFF_ERR_NULL;
+    if (!ardiff::in_32_bits({a->q_heads, a->dtype, a->pages, a->page, a->heads, a->head_width, a->width, a->requests,
+        a->causal})) return ARDIFF_ERR_SHAPE;
+    return attend_weights_checked(a->q, a->q_token, a->q_head, (int32_t)a->q_heads, a->tokens, (int32_t)a->dtype, a->k_cache, a->k_page,
+        a->k_token, a->k_head, (int32_t)a->pages, (int32_t)a->page, (int32_t)a->heads, (int32_t)a->head_width, a->table, (int32_t)a->width,
+        (int32_t)a->requests, a->length, a->offset, a->first, a->lse, a->lse_token, a->score, a->ld, (float)a->scale, (float)a->decay,
+        (int32_t)a->causal, a->new_score, a->new_ld, a->status, a->workspace, a->workspace_bytes, stream);
 }

@@ -1,5 +1,6 @@
 """Refusals of the operators around a draft model's cache: every one is made before anything is launched, so they need no GPU."""
 import math
+import struct
 
 import pytest
 
@@ -12,8 +13,31 @@ BIG = 1 << 40
 
 
 def call(name, defaults, kw):
+    """The call with a structure of these fields, in their order."""
     assert set(kw) <= set(defaults), kw
-    return getattr(ardiff.lib(), name)(*{**defaults, **kw}.values())
+    fields = {**defaults, **kw}
+    stream = fields.pop("stream")
+    form = "".join("d" if k in ("scale", "decay") else "q" for k in fields)
+    return getattr(ardiff.lib(), name)(struct.pack(form, *(0 if v is None else v for v in fields.values())), stream)
+
+
+@pytest.mark.parametrize("name", ["ardiff_rotary", "ardiff_rotary_backward", "ardiff_rotary_append", "ardiff_attend_pages",
+                                  "ardiff_attend_weights", "ardiff_pages_evict"])
+def test_no_structure(name):
+    assert getattr(ardiff.lib(), name)(None, None) == NULL
+
+
+@pytest.mark.parametrize("name,fields", [("ardiff_rotary", ["q_heads", "k_heads", "dtype", "width", "axes", "pairs"]),
+                                         ("ardiff_rotary_append", ["q_heads", "k_heads", "width", "axes", "pairs", "pages", "page"]),
+                                         ("ardiff_attend_pages", ["q_heads", "heads", "pages", "page", "head_width", "width", "requests", "groups", "most"]),
+                                         ("ardiff_attend_weights", ["q_heads", "heads", "pages", "page", "head_width", "width", "requests"]),
+                                         ("ardiff_pages_evict", ["requests", "recent", "width", "pages", "page", "heads", "head_width"])])
+def test_what_32_bits_do_not_hold(name, fields):
+    made = {"ardiff_rotary": turn, "ardiff_rotary_append": append, "ardiff_attend_pages": attend, "ardiff_attend_weights": weights,
+            "ardiff_pages_evict": evict}[name]()
+    for f in fields:
+        for off in (1 << 32, -(1 << 32), 1 << 62):
+            assert call(name, made, {f: made[f] + off}) == SHAPE, f
 
 
 def turn(**kw):
@@ -114,14 +138,3 @@ def test_workspaces():
     small, large = L.ardiff_attend_workspace(1, 0, 1, 8, 2, 64), L.ardiff_attend_workspace(500, 3, 4000, 8, 2, 64)
     assert 0 < small < large
     assert L.ardiff_pages_evict_workspace(3, 16, 5) > 0 and L.ardiff_attend_weights_workspace(3) >= 32
-
-
-def test_what_32_bits_do_not_hold_is_refused_before_the_call():
-    """The binding checks what ctypes would cut off (tensors without memory of their own stand in for the sizes)."""
-    import torch
-    with pytest.raises(AssertionError):
-        ardiff.ardiff_attend_pages(torch.zeros(1, 1, 64), torch.zeros(1, 1, 1, 64), torch.zeros(1, 1, 1, 64), torch.zeros((1, 1), dtype=torch.int32),
-                                   torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), most=1 << 32)
-    with pytest.raises(AssertionError):
-        ardiff.ardiff_pages_evict(torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1), torch.zeros((1, 1), dtype=torch.int32),
-                                  torch.zeros(1, 1, 1, 64), torch.zeros(1, 1, 1, 64), recent=1 << 33)
