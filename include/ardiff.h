@@ -583,7 +583,8 @@ int ardiff_rotary_append(const ardiff_rotary_append_call* call, void* stream);
  * no key has out 0 and lse -inf. Rows of q behind offset[requests] are not read, those of out and lse left as they were.
  * Shared tokens: the requests group[g] .. group[g + 1] - 1 (g < groups) have their first shared[g] tokens in common, so these are read
  * once for all of them, and whole pages of them through the table's row group[g] alone. (The page in which they end is every request's own
- * and holds the same. Where a query of the group does not see all of them, only those that all see are taken as shared.)
+ * and holds the same. Where a query of the group does not see all of them, or request group[g] has fewer, only those that all see and
+ * it has are taken as shared.)
  *   q, out      dev [tokens][q_heads][head_width] of type dtype, ARDIFF_BF16 or ARDIFF_F16, strides in values; lse  dev float
  *               [tokens][q_heads], rows lse_token apart.  tokens * q_heads < 2^31, q_heads <= ARDIFF_ROTARY_MAX_HEADS, a multiple of heads
  *   caches      as above, of the same type; head_width 64, 80, 96 or 128 (others: ERR_UNSUPPORTED). Pointers on 16-byte boundaries, strides
@@ -591,8 +592,8 @@ int ardiff_rotary_append(const ardiff_rotary_append_call* call, void* stream);
  *   table       dev int32 [requests][width], width * page < 2^31, times heads < 2^34;  length  dev int32 [requests];  offset  dev
  *               int32 [requests + 1]
  *   group       dev int32 [groups + 1], shared  dev int32 [groups]; groups == 0: NULL
- *   most        new tokens of a request at most, or 0 where that is not known: it only decides how the work is laid out
- *   status      dev int32 [1] out: ARDIFF_OK; ARDIFF_ERR_SHAPE where offsets descend or pass `tokens`, a length is negative or above
+ *   most        new tokens of a request at most, or 0 where that is not known: it decides how the work is laid out
+ *   status      dev int32 [1] out: ARDIFF_OK; ARDIFF_ERR_SHAPE where offsets descend or pass `tokens`, a request has more than `most`, a length is negative or above
  *               width * page, groups descend or pass `requests`, or shared is negative (then nothing is computed), or where a page outside 0 .. pages - 1 was met
  *               (then the results of the requests that have it mean nothing)
  *   workspace   dev, 256-byte aligned, at least ardiff_attend_workspace(...) bytes, as for ardiff_pages_evict

@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
     bool bad = false;
     for (int r = tid; r < R; r += threads) {
         const int a = c.offset[r], b = c.offset[r + 1], len = c.length[r];
-        bad |= a < 0 || b < a || b > c.x.tokens || len < 0 || len > limit;
+        bad |= a < 0 || b < a || b > c.x.tokens || len < 0 || len > limit || (c.most > 0 && b - a > c.most);
         if (kKept) {
             s_offset[r] = a;
             if (r + 1 == R) s_offset[R] = b;
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Call c) {
         // one request has queries, or all have so many that each fills its blocks of rows: then the same work is done, and there are no pieces to join.
         for (int g = tid >> 5; g < c.groups; g += threads / 32) {
             const int r0 = c.group[g], r1 = c.group[g + 1];
-            int least = c.shared[g], active = 0, fewest = 0x7fffffff;
+            int least = r0 < r1 ? min(c.shared[g], length[r0]) : 0, active = 0, fewest = 0x7fffffff;    // (its row holds no more)
             for (int r = r0 + lane; r < r1; r += 32) {
                 const int n = offset[r + 1] - offset[r];
                 if (n == 0) continue;
@@ -851,7 +851,7 @@ static int attend_pages_checked(const void* q, int64_t q_token, int64_t q_head, 
     c.length = length; c.offset = offset; c.group = group; c.shared = shared; c.status = status;
     c.scale = scale * 1.4426950408889634f;
     if (fabsf(c.scale) < 1.2e-38f) c.scale = 1.2e-38f;       // (0 times the -inf of a key that is not seen would be NaN)
-    c.requests = requests; c.groups = groups; c.causal = causal != 0;
+    c.requests = requests; c.groups = groups; c.causal = causal != 0; c.most = most;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool ok = dtype == ARDIFF_F16 ? launch_width<__half>(c, dtype, head_width, most, sms, st)
                                         : launch_width<__nv_bfloat16>(c, dtype, head_width, most, sms, st);

@@ -109,7 +109,7 @@ struct Call {
     const int32_t* shared;
     int32_t* status;
     float scale;                                 // times log2 e
-    int requests, groups, causal;
+    int requests, groups, causal, most;          // most: new tokens of a request, 0: not known
 };
 
 template <bool kWide> __device__ __forceinline__ const List& list_of(const Call& c) { return kWide ? c.plan.wide : c.plan.narrow; }

@@ -194,7 +194,7 @@ def test_what_is_not_finite_stays_with_the_queries_that_see_it():
                 assert not bool(torch.isfinite(out[[2, 3]].float()).all(-1).any())
 
 
-@pytest.mark.parametrize("what", ["offset", "tokens", "negative", "length", "group", "shared"])
+@pytest.mark.parametrize("what", ["offset", "tokens", "negative", "length", "group", "shared", "most"])
 def test_plans_that_are_out_of_range_compute_nothing(what):
     c = Case([2, 3], [50, 60], 4, 2, 64, 16, groups=[0, 2], shared=[32], seed=4)
     if what == "offset":
@@ -207,10 +207,10 @@ def test_plans_that_are_out_of_range_compute_nothing(what):
         c.length = i32([50, 16 * c.table.shape[1] + 1])
     elif what == "group":
         c.group = i32([0, 3])
-    else:
+    elif what == "shared":
         c.shared = i32([-1])
     out, lse = torch.full_like(c.q, 3.0, memory_format=torch.contiguous_format), torch.full((5, 4), 3.0, device=c.q.device)
-    got = c.attend(out=out, lse=lse)
+    got = c.attend(out=out, lse=lse, most=2 if what == "most" else None)
     assert int(got[2]) == SHAPE and bool((out == 3.0).all()) and bool((lse == 3.0).all())
 
 
@@ -487,6 +487,88 @@ def test_a_round_from_extension_to_eviction_captured():
             tokens[r] = [byp[p] for p in there]
         used = sum(-(-int(x) // page) for x in eager["length"])
         assert int(eager["count"]) == R * width - used == int(graphed["count"])
+
+
+def test_a_cache_beyond_32_bits_and_keys_and_values_side_by_side():
+    """Pages at the end of a pool of 9 GB whose keys and values lie side by side: tokens are rotated into it, attended to by few and by many rows, weighed,
+    evicted; pages of 64 tokens (boxes) and of 60."""
+    dev = require_cuda()
+    for page in (64, 60):
+        H, D, per = 1, 64, 2 * page * 64 * 2
+        pages = (9 << 30) // per
+        pool = torch.empty((pages, 2, page, H, D), dtype=torch.float16, device=dev)
+        k, v = pool[:, 0], pool[:, 1]
+        R, L, new, width = 3, 400, 20, 8
+        table = (pages - 1 - torch.arange(R * width, device=dev, dtype=torch.int32)).view(R, width).contiguous()
+        assert int(table.min()) * per > 1 << 32
+        g = torch.Generator(device=dev).manual_seed(page)
+        T = R * L
+        x = torch.randn((T, 6, D), device=dev, generator=g).half()
+        p = torch.arange(L, device=dev)
+        slot = (table.long()[:, p // page] * page + p % page).reshape(-1)
+        freq = torch.zeros((32,), device=dev)                              # (turned by nothing)
+        q = ardiff.ardiff_rotary_append(x[:, :4], x[:, 4:5], x[:, 5:6], torch.zeros((1, T), dtype=torch.int32, device=dev), freq, slot, k, v)
+        assert torch.equal(q, x[:, :4])
+        for n in (2, new):                                                 # 8 rows, 80 rows
+            rows = torch.cat([q.view(R, L, 4, D)[r, L - n:] for r in range(R)])
+            offset, length = i32([n * r for r in range(R + 1)]), i32([L] * R)
+            out, lse, status = ardiff.ardiff_attend_pages(rows, k, v, table, length, offset, most=n)
+            score, status2 = ardiff.ardiff_attend_weights(rows, k, table, length, offset, lse, torch.zeros((R, width * page), device=dev))
+            assert int(status) == 0 and int(status2) == 0
+            for r in range(R):
+                K, V = x.view(R, L, 6, D)[r, :, 4].double(), x.view(R, L, 6, D)[r, :, 5].double()
+                s = torch.einsum("nhd,ld->nhl", rows[n * r:n * (r + 1)].double(), K) / 8.0
+                s = s.masked_fill(torch.arange(L, device=dev)[None, None, :] > (L - n + torch.arange(n, device=dev))[:, None, None], -math.inf)
+                w = torch.softmax(s, -1)
+                want = torch.einsum("nhl,ld->nhd", w, V)
+                # the weight and the result rounded to f16, values up to about 4
+                assert float((out[n * r:n * (r + 1)].double() - want).abs().max()) <= 2.0 ** -11 * 2 * 4.5 + 2.0 ** -12
+                assert float((score[r, :L].double() - w.sum((0, 1))).abs().max()) <= 2.0 ** -11
+        before = torch.stack([k[table[1].long()[p // page], p % page], v[table[1].long()[p // page], p % page]]).clone()
+        src = torch.zeros((R, width * page), dtype=torch.int32, device=dev)
+        new_length, _, _, status = ardiff.ardiff_pages_evict(i32([L] * R), i32([50] * R), score, table, k, v, source=src)
+        assert int(status) == 0 and new_length.tolist() == [50] * R
+        at = src[1, :50].long()
+        after = torch.stack([k[table[1].long()[p // page], p % page], v[table[1].long()[p // page], p % page]])
+        assert torch.equal(after[:, :50], before[:, at]) and torch.equal(after[:, 50:], before[:, 50:])
+        del pool, k, v
+
+
+def test_many_requests_and_many_groups():
+    """More requests than the plan keeps, a group a request or two, one after the other."""
+    R = 1500
+    n, length = [r % 3 for r in range(R)], [(r * 37) % 200 + r % 3 for r in range(R)]
+    groups = list(range(0, R, 2)) + [R]
+    shared = [80 if g % 2 else 0 for g in range(len(groups) - 1)]
+    c = Case(n, length, 2, 1, 64, 16, groups=groups, shared=shared, seed=2)
+    out, lse, status = c.attend()
+    assert int(status) == 0
+    c.check(out, lse)
+    plain = c.attend(group=None, shared=None)
+    c.check(plain[0], plain[1])
+
+
+def test_two_graphs_and_an_eager_call_at_once():
+    """Two captured calls share nothing; replayed beside each other, and beside an eager one."""
+    c, d = Case([1] * 20, [500 + 9 * i for i in range(20)], 8, 2, 128, 16, seed=5), Case([100], [900], 8, 2, 128, 16, seed=6)
+    want = [x.attend() for x in (c, d)]
+    torch.cuda.synchronize()
+    graphs, held = [], []
+    for x in (c, d):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held.append(x.attend())
+        graphs.append(graph)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(5):
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        eager = c.attend()
+        torch.cuda.synchronize()
+        for w, x in zip(want, held):
+            assert torch.equal(w[0], x[0]) and torch.equal(w[1], x[1])
+        assert torch.equal(eager[0], want[0][0])
 
 
 def test_calls_at_once_on_two_streams():
