@@ -257,7 +257,8 @@ template <int D> constexpr int kNarrowShared = kWarps * (kStages<D> * kStageByte
 
 // Every warp is a worker of its own: 16 keys of a kv head a step, as many steps under way as its part of shared memory holds (26 to 28 KB: with
 // eight warps some 200 KB an SM, more than memory's latency asks for), no meeting with other warps. Lanes look up the places of the keys of the
-// step after the next one that is sent for, and copy 16 bytes each (bulk copies of single rows come at 15 clocks each: 2.9 TB/s with rows of 160 bytes).
+// step after the next one that is sent for, and copy 16 bytes each. (96 requests of 16 heads of 80 values, 360 MB: 84 us, 4.3 TB/s; bulk copies of
+// single rows, which come at 15 clocks each, took 122; rows loaded straight into the products' registers 183, since a warp then waits for memory in every step.)
 // Rows lie 2 D + 16 bytes apart, so that the eight rows of a matrix are in different banks. Query rows are the left operand, 16 rows an
 // instruction, or twice that (kTiles == 2): with few rows it is mostly empty, but reading 512 bytes a key and head from memory takes longer than its products.
 template <typename T, int D, int kTiles>
@@ -592,6 +593,7 @@ template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, const
     return u;
 }
 
+// Bound by the latency of what leads to a piece (units, blocks, pieces): 5 us where there are few, 25 for the 147 units of 256 rows that 148 CTAs cut.
 // Eight rows of a unit and a kv head, by four warps: a lane has a row and every fourth of its groups of four values; a warp every fourth of the
 // row's pieces, those among its request's own tokens and those among its group's shared ones.
 constexpr int kJoinRows = 8, kJoinWarps = 4;
@@ -761,7 +763,9 @@ template <typename T, int D, int kTiles> bool launch_narrow(const Call& c, cudaS
 template <typename T, int D> bool launch(const Call& c, int32_t dtype, int most, int sms, cudaStream_t st) {
     const bool wide = may_be_wide(c, most);
     ardiff::set_launch_count(wide ? 4 : 3);
-    return launch_early(c.requests <= kPlanKept ? plan_kernel<true> : plan_kernel<false>, 1, c.requests <= 64 ? 64 : c.requests <= 256 ? 256 : kPlanThreads, 1, 0, st, c) && (!wide || launch_wide(c, dtype, D, st)) &&
+    const unsigned threads = c.requests <= 64 ? 64 : c.requests <= 256 ? 256 : kPlanThreads;
+    const bool planned = c.requests <= kPlanKept ? launch_early(plan_kernel<true>, 1, threads, 1, 0, st, c) : launch_early(plan_kernel<false>, 1, threads, 1, 0, st, c);
+    return planned && (!wide || launch_wide(c, dtype, D, st)) &&
            (c.plan.narrow_rows > 16 ? launch_narrow<T, D, 2>(c, st) : launch_narrow<T, D, 1>(c, st)) &&
            launch_early(join_kernel<T, D>, 4 * sms, 256, 1, 0, st, c);
 }

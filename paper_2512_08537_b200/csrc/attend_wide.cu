@@ -9,6 +9,9 @@
 // x width multiply-adds (2048 cycles at 128) and 2 x 128 x 128 exponentials (2048 cycles of 16 a clock).
 // The maximum only moves when it would grow by more than 8 (a factor 256 that P and the sums hold easily): then O is rescaled in
 // tensor memory, which is rare; the product that last wrote O is done by then, since its successor S_t is issued after it.
+// Measured: prompts of 841 to 1024 tokens of 32 heads over 15000 shared ones, 4 requests, width 128, 1.0 TFLOP: 0.93 ms alone, 1.03 PFLOP/s, 1.1 ms back to
+// back at the clock that the power cap leaves. A step takes some 4000 cycles, 3300 of them in the issue of products that wait for
+// one another and for shared memory (both operands of S come from there: 128 bytes a clock, all that it gives).
 //
 // Warps: 0-3 and 4-7 the rows of tile 0 and 1 (a thread a row), 8 issues products, 9 copies keys, 10 values (the rows' warps their queries). Pages of a multiple of 8 tokens
 // come by TMA, in boxes of the largest power of two of tokens that divides a page (a lane looks up and copies a box). Others come by asynchronous
@@ -155,11 +158,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
         ptx::tmem_alloc(ptx::smem_u32(&s_tmem), kTmemColumns);
         ptx::tmem_relinquish();
     }
+    ardiff::begin_kernel();
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
     const uint32_t tmem = s_tmem;
-    ardiff::begin_kernel();
     const List& list = c.plan.wide;
     const long long steps = list.head->steps, each = steps_each<true>(steps, list.workers), begin = each * blockIdx.x;
     const int n = (int)max(0ll, min(steps, begin + each) - begin), own = list.head->own, G = c.x.G;

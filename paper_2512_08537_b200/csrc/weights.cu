@@ -10,7 +10,9 @@
 // SMs, the heads of a tile are split among CTAs, and the last of them adds the parts in their order. No atomics on sums: equal calls give equal bits.
 //
 // Bound by the keys' memory for few rows (512 bytes would be keys and values; here it is 256 a head of 128 values), by exponentials (16 a clock and SM)
-// from some 90 rows a kv head on.
+// from some 90 rows a kv head on. 128 requests of one query, up to 4096 tokens, 8 heads of 128: 540 MB in 112 us, 4.8 TB/s (15 tiles for the fullest of 148
+// CTAs where 14.2 are the mean, 82 % of the copy rate between its start and end); 8 requests of 32 queries, up to 16384 tokens: 46 us, of which the
+// exponentials take 19 and the keys 21.
 //
 // Warps: 0-3 and 4-7 sums, every other product each; 8 issues products; 9 copies keys (by TMA where pages allow, else by 16 bytes), 10 queries, 11 what is
 // known of their rows.
