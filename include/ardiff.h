@@ -517,7 +517,9 @@ int ardiff_distill_topk_step(const void* logits, int32_t dtype, int64_t n, int32
  *
  * A cache here is two pools, of keys and of values: value (pg, i, h, d) of a pool lies at pg * page_stride + i * token_stride +
  * h * head_stride + d values, for 0 <= pg < pages, 0 <= i < page, 0 <= h < heads, 0 <= d < width (so the tokens of a page, or its
- * heads, may lie next to each other). Tables, lengths, offsets and slots are those of ardiff_pages_extend.
+ * heads, may lie next to each other). Tables, lengths, offsets and slots are those of ardiff_pages_extend. Strides are not negative.
+ *
+ * The calls take a structure; all its fields are 64 bits wide, sizes have to fit 32 (ERR_SHAPE), pointers are NULL where an argument is left out.
  * ------------------------------------------------------------------------------------- */
 
 /* Rotary positions. Token t turns pair i of every head by angle = position[axis[i]][t] * freq[i]:
@@ -595,7 +597,8 @@ int ardiff_rotary_append(const ardiff_rotary_append_call* call, void* stream);
  *   most        new tokens of a request at most, or 0 where that is not known: it decides how the work is laid out
  *   status      dev int32 [1] out: ARDIFF_OK; ARDIFF_ERR_SHAPE where offsets descend or pass `tokens`, a request has more than `most`, a length is negative or above
  *               width * page, groups descend or pass `requests`, or shared is negative (then nothing is computed), or where a page outside 0 .. pages - 1 was met
- *               (then the results of the requests that have it mean nothing)
+ *               (then the results of the requests that have it mean nothing);
+ *               ARDIFF_ERR_TIMEOUT where a bounded wait ran out (results mean nothing)
  *   workspace   dev, 256-byte aligned, at least ardiff_attend_workspace(...) bytes, as for ardiff_pages_evict
  * Products take 16-bit operands with fp32 sums; weights are fp32 and rounded to dtype as operands of the second product, their sum is
  * that of the unrounded ones. The order of sums follows sizes, lengths and `most`: equal calls give equal bits. */
@@ -698,7 +701,7 @@ typedef struct {
 } ardiff_pages_evict_call;
 int ardiff_pages_evict(const ardiff_pages_evict_call* call, void* stream);
 
-/* Number of kernel launches the last call of the gate, the head, the cache's pages or the rows of logits on this
+/* Number of kernel launches the last call of the gate, the head, the cache or the rows of logits on this
  * thread enqueued (for launch accounting by benchmarks). */
 int ardiff_last_launch_count(void);
 
