@@ -317,7 +317,7 @@ inline bool strides_of(int64_t page, int64_t token, int64_t head, const Pages& p
 }
 
 // A cache as an array of four dimensions for TMA (tokens of a page, heads, pages), in boxes of `tokens` tokens and 64 values of a head, swizzled by
-// 128 bytes. False where it cannot be described so (strides of 2^40 bytes, no page): it is copied by 16 bytes then.
+// 128 bytes. False where it cannot be described so (strides of 2^40 bytes or 0, no page): it is copied by 16 bytes then.
 bool describe(CUtensorMap* map, const char* base, bool bf16, int width, int tokens, const Pages& p, uint32_t token, uint32_t head, uint32_t page);
 // Queries as an array of three dimensions (heads, tokens), in boxes of the G heads of a kv head, of `rows` / G tokens and of 64 values: `rows` rows in the
 // order of the blocks. False where G does not divide `rows` or the strides do not fit.

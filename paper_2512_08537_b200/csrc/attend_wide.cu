@@ -608,7 +608,8 @@ int ardiff::box_tokens(int page) {
 }
 
 bool ardiff::describe(CUtensorMap* map, const char* base, bool bf16, int width, int tokens, const Pages& p, uint32_t token, uint32_t head, uint32_t page) {
-    if (p.pages < 1) return false;
+    // (a stride of 0 where there is more than one: the same rows under several names)
+    if (p.pages < 1 || (!token && p.page > 1) || (!head && p.heads > 1) || (!page && p.pages > 1)) return false;
     const EncodeTiled f = encoder();
     if (!f) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)p.page, (cuuint64_t)p.heads, (cuuint64_t)p.pages};
@@ -620,10 +621,11 @@ bool ardiff::describe(CUtensorMap* map, const char* base, bool bf16, int width, 
 
 bool ardiff::describe_queries(CUtensorMap* map, const Queries& x, bool bf16, int width, int rows) {
     if (x.tokens < 1 || rows % x.G || x.q_token < 0 || x.q_head < 0 || (x.q_token | x.q_head) >> 38) return false;
+    if ((!x.q_token && x.tokens > 1) || (!x.q_head && x.heads > 1)) return false;
     const EncodeTiled f = encoder();
     if (!f) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)x.heads, (cuuint64_t)x.tokens};
-    const cuuint64_t strides[2] = {x.heads > 1 && x.q_head ? 2 * (cuuint64_t)x.q_head : 16, x.tokens > 1 && x.q_token ? 2 * (cuuint64_t)x.q_token : 16};
+    const cuuint64_t strides[2] = {x.heads > 1 ? 2 * (cuuint64_t)x.q_head : 16, x.tokens > 1 ? 2 * (cuuint64_t)x.q_token : 16};
     const cuuint32_t box[3] = {64, (cuuint32_t)x.G, (cuuint32_t)(rows / x.G)}, ones[3] = {1, 1, 1};
     return f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(x.q), dims, strides, box, ones,
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

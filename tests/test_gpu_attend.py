@@ -583,3 +583,23 @@ def test_calls_at_once_on_two_streams():
     for pair in got:
         for w, x in zip(want, pair):
             assert torch.equal(w[0], x[0]) and torch.equal(w[1], x[1])
+
+
+@pytest.mark.parametrize("page,n,length", [(64, [300, 40, 1], [700, 333, 500]), (25, [300, 1], [420, 90]), (16, [1, 2], [300, 40])])
+def test_rows_that_lie_in_memory_once(page, n, length):
+    """Caches whose heads or pages, and queries whose heads or tokens, are one another's: strides of 0."""
+    c = Case(n, length, 8, 4, 128, page, seed=12)
+    q, k, v = c.q, torch.nan_to_num(c.k), torch.nan_to_num(c.v)
+
+    def results(q, k, v):
+        out, lse, status = ardiff.ardiff_attend_pages(q, k, v, c.table, c.length, c.offset)
+        score = torch.ones((len(n), c.table.shape[1] * page), device=q.device)
+        score, status2 = ardiff.ardiff_attend_weights(q, k, c.table, c.length, c.offset, lse, score, new_score=score)
+        assert int(status) == 0 and int(status2) == 0
+        return out, lse, score
+
+    for qs, ks in ((q[:, :1].expand_as(q), k), (q[:1].expand_as(q), k), (q, k[:, :, :1].expand_as(k)), (q, k[:1].expand_as(k)), (q, k[:, :1].expand_as(k))):
+        vs = v if ks is k else v[:, :, 1:2].expand_as(v)
+        same, apart = results(qs, ks, vs), results(qs.contiguous(), ks.contiguous(), vs.contiguous())
+        for a, b in zip(same, apart):                  # (queries by boxes or by rows: the same sums)
+            assert torch.equal(a, b)
