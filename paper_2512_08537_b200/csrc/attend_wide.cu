@@ -57,9 +57,10 @@ struct Boxes {
 
 // 2^x of two numbers, x <= 8, by the nearest whole number and a polynomial for the rest f, |f| <= 1/2 (fitted to 2^f for the least relative
 // error, 2.1e-7 in fp32): a quarter of the exponentials go this way, through pipes that have room, so that the special-function unit's 16 a
-// clock are not the bound. Numbers below -125 count as that; NaN and infinities are not taken here.
+// clock are not the bound. Numbers below -127 count as that, and 2^-127 comes out as 2^-149 (the lowest exponent has no leading one), which is 0 in 16
+// bits: a key that is not seen adds nothing, however large its value. NaN and infinities are not taken here.
 __device__ __forceinline__ float2 exp2_by_products(float2 x) {
-    const Two y = two(fmaxf(x.x, -125.f), fmaxf(x.y, -125.f));
+    const Two y = two(fmaxf(x.x, -127.f), fmaxf(x.y, -127.f));
     const Two t = y + two(12582912.f, 12582912.f);             // 1.5 2^23: the whole number in the low bits
     const Two f = fma2(t + two(-12582912.f, -12582912.f), two(-1.f, -1.f), y);
     Two v = fma2(two(1.32764725e-3f, 1.32764725e-3f), f, two(9.67554096e-3f, 9.67554096e-3f));
@@ -79,7 +80,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {              
 }
 
 // A row's 128 scores from tensor memory: weights 2^(s scale - base), packed; their sum; the highest score (NaN if one is). A weight of a score that is
-// -inf is 2^-125 at the most, which no sum of any other weight notices; what is NaN is the caller's to see by the highest score.
+// -inf is 2^-149 at the most, which no sum of any other weight notices; what is NaN is the caller's to see by the highest score.
 template <typename T> __device__ __forceinline__ void weights(uint32_t s_at, float scale, float base, uint32_t (&p)[64], float& sum, float& top) {
     const Two scale2 = two(scale, scale), base2 = two(-base, -base);
     uint32_t r[2][32];

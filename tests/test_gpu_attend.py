@@ -603,3 +603,14 @@ def test_rows_that_lie_in_memory_once(page, n, length):
         same, apart = results(qs, ks, vs), results(qs.contiguous(), ks.contiguous(), vs.contiguous())
         for a, b in zip(same, apart):                  # (queries by boxes or by rows: the same sums)
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,largest", [("bf16", 3e38), ("f16", 6e4)])
+@pytest.mark.parametrize("n,page", [(300, 64), (300, 25), (12, 16)])
+def test_the_largest_values_stay_with_the_queries_that_see_them(dtype, largest, n, page):
+    c = Case([n], [n + 140], 2, 2, 64, page, dtype, seed=13)
+    want = c.attend()
+    last = torch.arange(n + 132, n + 140, device=c.q.device)          # seen by the last eight queries alone
+    c.v[c.table[0].long()[last // page], last % page] = largest
+    got = c.attend()
+    assert torch.equal(got[0][:n - 8], want[0][:n - 8]) and torch.equal(got[1], want[1])
