@@ -590,7 +590,7 @@ int ardiff_rotary_append(const ardiff_rotary_append_call* call, void* stream);
  *   q, out      dev [tokens][q_heads][head_width] of type dtype, ARDIFF_BF16 or ARDIFF_F16, strides in values; lse  dev float
  *               [tokens][q_heads], rows lse_token apart.  tokens * q_heads < 2^31, q_heads <= ARDIFF_ROTARY_MAX_HEADS, a multiple of heads
  *   caches      as above, of the same type; head_width 64, 80, 96 or 128 (others: ERR_UNSUPPORTED). Pointers on 16-byte boundaries, strides
- *               multiples of 8 values, those of q and out too
+ *               multiples of 8 values, those of q and out too. scale * log2 e is a finite float
  *   table       dev int32 [requests][width], width * page < 2^31, times heads < 2^34;  length  dev int32 [requests];  offset  dev
  *               int32 [requests + 1]
  *   group       dev int32 [groups + 1], shared  dev int32 [groups]; groups == 0: NULL

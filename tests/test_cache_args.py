@@ -138,3 +138,9 @@ def test_workspaces():
     small, large = L.ardiff_attend_workspace(1, 0, 1, 8, 2, 64), L.ardiff_attend_workspace(500, 3, 4000, 8, 2, 64)
     assert 0 < small < large
     assert L.ardiff_pages_evict_workspace(3, 16, 5) > 0 and L.ardiff_attend_weights_workspace(3) >= 32
+
+
+@pytest.mark.parametrize("scale", [math.inf, -math.inf, math.nan, 1e39, 3e38, -3e38])
+def test_scales_that_are_not_finite_in_powers_of_two(scale):
+    assert call("ardiff_attend_pages", attend(), dict(scale=scale)) == SHAPE
+    assert call("ardiff_attend_weights", weights(), dict(scale=scale)) == SHAPE
