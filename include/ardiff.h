@@ -528,7 +528,7 @@ int ardiff_distill_topk_step(const void* logits, int32_t dtype, int64_t n, int32
  * returned become those of its inputs. Turns are formed in fp64, rotations in fp32 and rounded once.
  *   q, k        dev [n][heads][width] of type dtype (ARDIFF_BF16, ARDIFF_F16 or ARDIFF_F32), width contiguous, strides in
  *               values, at multiples of the value's size (16-byte boundaries are fastest); either may have 0 heads
- *   q_out, k_out  the same shape; may be the inputs themselves (same strides), must not overlap them otherwise
+ *   q_out, k_out  the same shape; may be the inputs themselves (same strides, else ERR_UNSUPPORTED), must not overlap them otherwise
  *   n           0 <= n < 2^31;  heads <= ARDIFF_ROTARY_MAX_HEADS;  1 <= width <= ARDIFF_ROTARY_MAX_WIDTH;  0 <= 2 * pairs <= width
  *   position    dev int32 [axes][n], rows position_ld apart: any numbers
  *   freq        dev float [pairs];  axis  dev int32 [pairs], or NULL: 0. A pair of an axis outside 0 .. axes - 1 stands still
@@ -587,7 +587,7 @@ int ardiff_rotary_append(const ardiff_rotary_append_call* call, void* stream);
  * once for all of them, and whole pages of them through the table's row group[g] alone. (The page in which they end is every request's own
  * and holds the same. Where a query of the group does not see all of them, or request group[g] has fewer, only those that all see and
  * it has are taken as shared.)
- *   q, out      dev [tokens][q_heads][head_width] of type dtype, ARDIFF_BF16 or ARDIFF_F16, strides in values; lse  dev float
+ *   q, out      dev [tokens][q_heads][head_width] of type dtype, ARDIFF_BF16 or ARDIFF_F16, strides in values, apart (q == out: ERR_UNSUPPORTED); lse  dev float
  *               [tokens][q_heads], rows lse_token apart.  tokens * q_heads < 2^31, q_heads <= ARDIFF_ROTARY_MAX_HEADS, a multiple of heads
  *   caches      as above, of the same type; head_width 64, 80, 96 or 128 (others: ERR_UNSUPPORTED). Pointers on 16-byte boundaries, strides
  *               multiples of 8 values, those of q and out too. scale * log2 e is a finite float
@@ -634,7 +634,7 @@ int ardiff_attend_pages(const ardiff_attend_pages_call* call, void* stream);
  * Arguments as for ardiff_attend_pages, whose lse this takes (a row with lse -inf adds nothing); q may be the last queries of a
  * prompt alone. A request without new tokens has its scores multiplied by decay.
  *   first       dev int32 [requests], or NULL: 0 (e.g. behind shared tokens, which are not one request's to evict)
- *   score, new_score  dev float [requests], rows ld and new_ld apart (lengths may not pass either); may be the same
+ *   score, new_score  dev float [requests], rows ld and new_ld apart (lengths may not pass either); may be the same (same distance)
  *   status      as above;  workspace  16-byte aligned, at least ardiff_attend_weights_workspace(requests) bytes */
 int64_t ardiff_attend_weights_workspace(int32_t requests);
 typedef struct {

@@ -823,6 +823,7 @@ static int attend_pages_checked(const void* q, int64_t q_token, int64_t q_head, 
         return ARDIFF_ERR_ALIGN;
     const Layout s = layout(requests, groups, tokens, q_heads, heads, head_width);
     if (workspace_bytes < s.bytes) return ARDIFF_ERR_SHAPE;
+    if (tokens > 0 && q == out) return ARDIFF_ERR_UNSUPPORTED;         // (blocks of other workers still read them)
     const int sms = device_sms();
     if (sms < 1) return ARDIFF_ERR_CUDA;
     Call c;

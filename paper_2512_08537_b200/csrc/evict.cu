@@ -359,6 +359,7 @@ static int pages_evict_checked(int32_t requests, const int32_t* length, const in
         return ARDIFF_ERR_ALIGN;
     const int64_t limit = (int64_t)page * width;
     if (workspace_bytes < ardiff_pages_evict_workspace(requests, page, width) && requests > 0) return ARDIFF_ERR_SHAPE;
+    if (requests > 1 && ld != new_ld && (score == new_score || (position && position == new_position))) return ARDIFF_ERR_SHAPE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     Evict a;
     memset(&a, 0, sizeof(a));

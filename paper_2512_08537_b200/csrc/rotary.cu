@@ -379,6 +379,7 @@ int rotary(Rotary& a, int32_t dtype, int32_t neighbours, bool append, cudaStream
         if (s.heads == 0) continue;
         if (!s.in || !s.out) return ARDIFF_ERR_NULL;
         if ((reinterpret_cast<uintptr_t>(s.in) | reinterpret_cast<uintptr_t>(s.out)) & (size - 1)) return ARDIFF_ERR_ALIGN;
+        if (s.in == s.out && ((a.n > 1 && s.in_token != s.out_token) || (s.heads > 1 && s.in_head != s.out_head))) return ARDIFF_ERR_UNSUPPORTED;
         bits_rows |= places(s.in, size, s.in_token, s.heads > 1 ? s.in_head : 0) | places(s.out, size, s.out_token, s.heads > 1 ? s.out_head : 0);
     }
     if (append) bits_rows |= (uint64_t)a.k_page | (uint64_t)a.v_page;

@@ -496,6 +496,7 @@ static int attend_weights_checked(const void* q, int64_t q_token, int64_t q_head
     auto low = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
     if (((low(q) | low(k_cache)) & 15u) || (low(workspace) & 15u) || ((q_token | q_head | k_page | k_token | k_head) & 7)) return ARDIFF_ERR_ALIGN;
     if (workspace_bytes < ardiff_attend_weights_workspace(requests)) return ARDIFF_ERR_SHAPE;
+    if (score == new_score && requests > 1 && ld != new_ld) return ARDIFF_ERR_SHAPE;
     const int sms = device_sms();
     if (sms < 1) return ARDIFF_ERR_CUDA;
     Weights c;

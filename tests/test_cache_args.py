@@ -144,3 +144,14 @@ def test_workspaces():
 def test_scales_that_are_not_finite_in_powers_of_two(scale):
     assert call("ardiff_attend_pages", attend(), dict(scale=scale)) == SHAPE
     assert call("ardiff_attend_weights", weights(), dict(scale=scale)) == SHAPE
+
+
+def test_results_where_inputs_are():
+    """Only in place: at the same distances, and not where other blocks still read them."""
+    assert call("ardiff_attend_pages", attend(), {}) == UNSUPPORTED                   # q and out are both at P
+    for name in ("ardiff_rotary", "ardiff_rotary_backward"):
+        for kw in (dict(q_out_token=1024), dict(q_out_head=128), dict(k_out_token=256), dict(k_out_head=1024)):
+            assert call(name, turn(), kw) == UNSUPPORTED, kw
+    assert call("ardiff_attend_weights", weights(), dict(new_ld=80)) == SHAPE
+    assert call("ardiff_pages_evict", evict(), dict(new_ld=80)) == SHAPE
+    assert call("ardiff_pages_evict", evict(), dict(new_ld=80, new_score=2 * P, position=P, new_position=P)) == SHAPE
