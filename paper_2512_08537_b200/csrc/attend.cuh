@@ -260,6 +260,13 @@ struct Waits {
     }
 };
 
+// Copies that a warp which gave up has sent for: they land before shared memory is given back. Copy i is step i's, into stage i % stages; `sent`
+// have been sent. Bounded, as all waits.
+__device__ __forceinline__ void wait_for_copies(uint32_t bars, int full, uint32_t sent, uint32_t stages) {
+    for (uint32_t i = sent > stages ? sent - stages : 0; i < sent; ++i)
+        for (int j = 0; j < 1 << 20 && !ptx::mbar_try_wait(bars + (full + i % stages) * 8, (i / stages) & 1); ++j) {}
+}
+
 // 16-byte chunk c of row `row` of a tile of rows of D values: chunks change places with the row, or rows are a chunk longer than their values, so
 // that the eight rows of a matrix lie in different banks.
 template <int D> constexpr int kPitch = D % 64 ? 2 * D + 16 : 2 * D;

@@ -219,10 +219,13 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
         };
         look_up();
         uint32_t landed[2] = {0, 0};
-        for (int i = 0; i < n; ++i) {
+        bool good = true;
+        int i = 0;
+        for (; i < n; ++i) {
             const int stage = i & 1;
             const Box box = next;
-            if (!__all_sync(0xffffffffu, wait(empty + stage, ((i >> 1) & 1) ^ 1))) break;
+            good = __all_sync(0xffffffffu, wait(empty + stage, ((i >> 1) & 1) ^ 1));
+            if (!good) break;
             const bool zone = v && now.at.key0 + (now.tile + 1) * kWideKeys > least_seen(now.at, G);
             const uint32_t bar = bars + ((zone ? kVLanded : full) + stage) * 8;
             const uint32_t there = __ballot_sync(0xffffffffu, box.id >= 0);
@@ -240,7 +243,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
             if (zone) {
                 // keys that some row of the block does not see must not reach it as 0 times a value that is not finite; those behind the
                 // last one, whatever they are, become zeros
-                if (!__all_sync(0xffffffffu, wait(kVLanded + stage, landed[stage]++ & 1))) break;
+                good = __all_sync(0xffffffffu, wait(kVLanded + stage, landed[stage]++ & 1));
+                if (!good) {
+                    for (int j = 0; j < 1 << 20 && !ptx::mbar_try_wait(bars + (kVLanded + stage) * 8, (landed[stage] - 1) & 1); ++j) {}
+                    break;
+                }
                 const int left = now.at.keys - now.tile * kWideKeys;
                 bool odd = false;
                 for (int j = lane; j < kWideKeys * 8 * kSub<D>; j += 32) {
@@ -259,6 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
             }
             if (i + 1 < n) now.next(c);
         }
+        if (!good) wait_for_copies(bars, full, i, 2);
     } else if (warp >= 9) {
         // ---- keys or values, by 16 bytes
         const bool v = warp == 10;

@@ -273,6 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
         }
         cp_async_commit();
         cp_async_wait<0>();
+        if (!good) wait_for_copies(bars, kKFull, i, kStages);
     } else if (warp == 10) {
         // ---- queries
         constexpr int kLanes = D / 8 <= 8 ? 8 : 16;
@@ -318,6 +319,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
         }
         cp_async_commit();
         cp_async_wait<0>();
+        if (!good) wait_for_copies(bars, kQFull, u, 2);
     } else if (warp == 11) {
         // ---- what is known of their rows
         uint32_t u = 0;
