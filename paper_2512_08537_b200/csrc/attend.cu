@@ -79,9 +79,9 @@ struct Segment {
         k.keys = last > k.low ? last - k.key0 : 0;
         return k;
     }
-    __device__ __forceinline__ int steps(const Block& k, int heads) const {
+    __device__ __forceinline__ int steps(const Block& k, const Call& c) const {
         const int tile = wide ? kWideKeys : kNarrowKeys;
-        return (k.keys + tile - 1) / tile * heads;
+        return (k.keys + tile - 1) / tile * (wide ? c.cache.heads : c.cache.heads / c.plan.team);
     }
     // what the segment adds
     __device__ __forceinline__ Sums sums(const Call& c) const {
@@ -89,7 +89,7 @@ struct Segment {
         const int n = blocks(), up = wide ? 0 : 32;
         v.blocks = (long long)n << up;
         v.rows = rows > 0 ? rows << up : 0;
-        for (int j = 0; j < n; ++j) v.steps[wide] += steps(block(j, c), c.cache.heads);
+        for (int j = 0; j < n; ++j) v.steps[wide] += steps(block(j, c), c);
         return v;
     }
     // writes its blocks behind those of `before`; whether one of them has no key
@@ -104,7 +104,7 @@ struct Segment {
             k.first_row = row;
             l.block[at + j] = k;
             l.steps[at + j] = step;
-            step += steps(k, c.cache.heads);
+            step += steps(k, c);
             row += k.rows;
             empty |= k.keys == 0;
         }
@@ -255,7 +255,7 @@ template <int D> constexpr int kStageBytes = 2 * kNarrowKeys * kPitch16<D>;
 template <int D> constexpr int kStages = 28400 / kStageBytes<D> < 6 ? 28400 / kStageBytes<D> : 6;
 template <int D> constexpr int kNarrowShared = kWarps * (kStages<D> * kStageBytes<D> + kNarrowKeys * 16);
 
-// Every warp is a worker of its own: 16 keys of a kv head a step, as many steps under way as its part of shared memory holds (26 to 28 KB: with
+// Every warp goes its own way (teams: through the same keys as its neighbours): 16 keys of a kv head a step, as many steps under way as its part of shared memory holds (26 to 28 KB: with
 // eight warps some 200 KB an SM, more than memory's latency asks for), no meeting with other warps. Lanes look up the places of the keys of the
 // step after the next one that is sent for, and copy 16 bytes each. (96 requests of 16 heads of 80 values, 360 MB: 84 us, 4.3 TB/s; bulk copies of
 // single rows, which come at 15 clocks each, took 122; rows loaded straight into the products' registers 183, since a warp then waits for memory in every step.)
@@ -268,7 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const List& list = c.plan.narrow;
     const long long steps = list.head->steps, each = steps_each<false>(steps, list.workers);
-    const int worker = warp * gridDim.x + blockIdx.x;                                  // (few workers: on as many SMs)
+    const int team = D % 64 ? c.plan.team : 1;                                         // (known where rows are whole lines)
+    const int worker = warp / team * gridDim.x + blockIdx.x;                    // (few workers: on as many SMs)
     const long long begin = each * worker;
     if (begin >= steps) return;
     const int n = (int)(min(steps, begin + each) - begin), own = list.head->own;
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
 
     // where this warp is in the line of steps, and what it needs of the block: of products, and of copies some steps ahead
     struct Place {
-        int b, h, tile, tiles, key0, keys;
+        int b, h, tile, tiles, key0, keys;       // h: this warp's of the team's heads
         __device__ __forceinline__ void enter(const List& list) {
             key0 = list.block[b].key0;
             keys = list.block[b].keys;
@@ -286,11 +287,12 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
             tile = 0;
         }
         // the next step; whether it is another block's (only called while there is one)
-        __device__ __forceinline__ bool next(const List& list, int heads) {
+        __device__ __forceinline__ bool next(const List& list, int heads, int team) {
             if (++tile < tiles) return false;
             tile = 0;
-            if (++h < heads) return false;
-            h = 0;
+            h += team;
+            if (h < heads) return false;
+            h &= team - 1;
             do {
                 ++b;
                 enter(list);
@@ -298,14 +300,14 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
             return true;
         }
     };
-    const int H = c.cache.heads;
     Place now;
     now.b = find_last(list.steps, list.head->blocks, begin);
     now.enter(list);
     {
         const int in = (int)(begin - list.block[now.b].first_step);
-        now.h = in / now.tiles;
-        now.tile = in - now.h * now.tiles;
+        const int group = in / now.tiles;
+        now.tile = in - group * now.tiles;
+        now.h = group * team + warp % team;
     }
     Place load = now;                            // the step whose places are looked up next
     const int32_t *table, *front_table;
@@ -371,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
 #pragma unroll
     for (int s = 0; s < kStages<D>; ++s) {
         if (s < n) first[s] = look_up();
-        if (s + 1 < n && load.next(list, H)) tables();
+        if (s + 1 < n && load.next(list, c.cache.heads, team)) tables();
     }
 #pragma unroll
     for (int s = 0; s < kStages<D>; ++s) {
@@ -526,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
         if (i + kStages<D> < n) {
             fetch(i + kStages<D>, found);
             if (i + kStages<D> + 1 < n) {
-                if (load.next(list, H)) tables();
+                if (load.next(list, c.cache.heads, team)) tables();
                 found = look_up();
             }
         } else {
@@ -537,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
         const bool ends = now.tile + 1 == now.tiles;
         if (ends || i + 1 == n) {
             const Block b = list.block[now.b];
-            const long long unit = b.first_step + (long long)now.h * now.tiles;       // its first step
+            const long long unit = b.first_step + (long long)(now.h / team) * now.tiles;       // its first step
             const bool direct = whole && ends && now.b >= own && c.plan.share[b.request].prefix < 0;
             const long long at = direct ? 0 : piece_row<false>(c, 0, b, now.h, worker, quotient_of(unit, each));
 #pragma unroll
@@ -566,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
                 }
             fresh = whole = true;
         }
-        if (i + 1 < n) now.next(list, H);
+        if (i + 1 < n) now.next(list, c.cache.heads, team);
     }
 }
 
@@ -581,12 +583,13 @@ struct Cut {
 template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, const PlanHead& head, const Block& k, int h, int in) {
     const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
     Cut u;
-    u.rows = k.rows; u.in = in; u.cap = Sizes<kWide>::rows;
+    const int team = kWide ? 1 : c.plan.team;
+    u.rows = k.rows; u.in = in; u.cap = Sizes<kWide>::rows * team;
     u.main = (head.rows_before + k.first_row) * c.cache.heads + (long long)h * k.rows;
-    u.others = kWide ? c.pieces.wide_rows : c.pieces.narrow_rows;
+    u.others = kWide ? c.pieces.wide_rows : c.pieces.narrow_rows + h % team * kNarrowRows;
     u.first = u.count = 0;
     if (tiles) {
-        const long long each = steps_each<kWide>(head.steps, list_of<kWide>(c).workers), s0 = k.first_step + (long long)h * tiles;
+        const long long each = steps_each<kWide>(head.steps, list_of<kWide>(c).workers), s0 = k.first_step + (long long)(h / team) * tiles;
         u.first = quotient_of(s0, each);
         u.count = quotient_of(s0 + tiles - 1, each) - u.first + 1;
     }
@@ -682,9 +685,9 @@ __device__ __forceinline__ void join_list(const Call& c, Joined<D>& s, int half,
     const List& list = list_of<kWide>(c);
     const PlanHead& head = kWide ? wide : narrow;
     if (head.blocks == head.own) return;
-    const int H = c.cache.heads, kParts = kWide ? 8 : 1, rows = Sizes<kWide>::rows / kParts;
+    const int H = c.cache.heads, team = kWide ? 1 : c.plan.team, kParts = kWide ? 8 : 1, rows = Sizes<kWide>::rows / kParts;
     const long long each = steps_each<kWide>(head.steps, list.workers);
-    const long long cuts = (head.steps - 1) / each, items = head.all_rows ? (long long)(head.blocks - head.own) * H : cuts;
+    const long long cuts = (head.steps - 1) / each, items = head.all_rows ? (long long)(head.blocks - head.own) * H : cuts * team;
     for (long long i = blockIdx.x * 2 + half; i < items * kParts; i += gridDim.x * 2) {
         const int item = quotient_of(i, kParts), row0 = (int)(i - (long long)item * kParts) * rows;
         int b, h = 0;
@@ -693,15 +696,16 @@ __device__ __forceinline__ void join_list(const Call& c, Joined<D>& s, int half,
             h = item - b * H;
             b += head.own;
         } else {
-            b = find_last(list.steps, head.blocks, each * (item + 1));
+            b = find_last(list.steps, head.blocks, each * (item / team + 1));
         }
         const Block k = list.block[b];
         if (row0 >= k.rows) continue;
         if (!head.all_rows) {
-            const long long at = each * (item + 1);
+            const long long at = each * (item / team + 1);
             const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
             h = (int)(at - k.first_step) / tiles;
             const long long unit = k.first_step + (long long)h * tiles;
+            h = h * team + item % team;
             // (a unit that several workers cut is the first one's; shared tokens' units are joined with their requests' own)
             if (b < head.own || unit >= at || unit < at - each) continue;
         }
@@ -758,7 +762,7 @@ bool may_be_wide(const Call& c, int most) {
 template <typename T, int D, int kTiles> bool launch_narrow(const Call& c, cudaStream_t st) {
     static std::atomic<uint64_t> ready{0};
     return shared_memory(narrow_kernel<T, D, kTiles>, kNarrowShared<D>, ready) &&
-           launch_early(narrow_kernel<T, D, kTiles>, c.plan.narrow.workers / kWarps, kThreads, 1, kNarrowShared<D>, st, c);
+           launch_early(narrow_kernel<T, D, kTiles>, c.plan.wide.workers, kThreads, 1, kNarrowShared<D>, st, c);
 }
 template <typename T, int D> bool launch(const Call& c, int32_t dtype, int most, int sms, cudaStream_t st) {
     const bool wide = may_be_wide(c, most);
@@ -844,7 +848,13 @@ static int attend_pages_checked(const void* q, int64_t q_token, int64_t q_head, 
         l.steps = reinterpret_cast<long long*>(w + s.steps_at[i]);
     }
     c.plan.wide.workers = sms < kMaxSms ? sms : kMaxSms;
-    c.plan.narrow.workers = c.plan.wide.workers * kWarps;
+    // Memory is read in lines of 128 bytes. Where rows of neighbouring heads share them, warps of a CTA go through the same keys of
+    // several heads, so that what one does not want is in L2 for the next (96 requests of 3500 tokens, 16 heads of 80 values side by side, 1.7 GB:
+    // 313 us, 472 without).
+    c.plan.team = 1;
+    if (head_width % 64 && k_head < k_token && k_head % 64)
+        while (c.plan.team < kWarps && heads % (2 * c.plan.team) == 0) c.plan.team *= 2;
+    c.plan.narrow.workers = c.plan.wide.workers * kWarps / c.plan.team;
     // (a request's rows at most, or on average where that is not known: those of more go the wide way)
     const int64_t news = most > 0 ? most : requests > 0 ? (tokens + requests - 1) / requests : 0;
     c.plan.narrow_rows = news * c.x.G <= 16 ? 16 : 32;

@@ -49,7 +49,7 @@ struct alignas(16) Block {
 };
 
 struct PlanHead {
-    long long steps;                             // of all blocks: key tiles times kv heads
+    long long steps;                             // of all blocks: key tiles times kv heads (narrow: times teams of heads)
     long long rows_before;                       // of the other list, in front of this one's among the pieces
     int blocks, own;                             // blocks [0, own): shared tokens; [own, blocks): the requests' own
     int all_rows, pad;                           // whether there are rows to join beside those of units that are cut
@@ -70,13 +70,14 @@ struct List {
     PlanHead* head;
     Block* block;
     long long* steps;                            // [blocks + 1]: steps of the blocks before
-    int workers;                                 // that share its steps: CTAs of the wide kernel, warps of the narrow one
+    int workers;                                 // that share its steps: CTAs of the wide kernel, teams of the narrow one
 };
 
 struct Plan {
     List narrow, wide;
     Share* share;                                // [requests]
     int narrow_rows;                             // of a segment, at most, for it to be narrow: 16 or 32
+    int team;                                    // warps of the narrow kernel, a kv head each, that go through the same keys: 1, 2, 4 or 8
 };
 
 struct Queries {                                 // strides in values
@@ -125,7 +126,8 @@ __device__ __forceinline__ int quotient_of(long long a, long long b) {
 }
 
 template <bool kWide> __device__ __forceinline__ long long piece_row(const Call& c, long long rows_before, const Block& k, int h, int worker, int first) {
-    return worker != first ? (kWide ? c.pieces.wide_rows : c.pieces.narrow_rows) + (long long)worker * Sizes<kWide>::rows
+    return worker != first ? (kWide ? c.pieces.wide_rows + (long long)worker * kWideRows
+                                    : c.pieces.narrow_rows + ((long long)worker * c.plan.team + h % c.plan.team) * kNarrowRows)
                            : (rows_before + k.first_row) * c.cache.heads + (long long)h * k.rows;
 }
 

@@ -614,3 +614,16 @@ def test_the_largest_values_stay_with_the_queries_that_see_them(dtype, largest, 
     c.v[c.table[0].long()[last // page], last % page] = largest
     got = c.attend()
     assert torch.equal(got[0][:n - 8], want[0][:n - 8]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("n,length,Hq,Hkv,page,groups,shared", [
+    ([1] * 7, [3, 900, 65, 64, 1, 0, 2000], 16, 16, 25, None, None), ([2, 4, 1], [700, 4, 1500], 32, 8, 16, None, None),
+    ([1, 5, 3], [333, 1200, 90], 12, 6, 32, None, None), ([1, 1], [5000, 17], 12, 12, 64, None, None), ([1, 2], [900, 40], 3, 3, 7, None, None),
+    ([2, 3, 1, 1], [800, 777, 900, 40], 16, 8, 25, [0, 3], [700]), ([1], [40], 16, 16, 1, None, None)])
+@pytest.mark.parametrize("D,dtype,layout", [(80, "bf16", "nhd"), (96, "f16", "nhd"), (80, "f16", "hnd")])
+def test_few_rows_of_heads_that_share_lines_of_memory(n, length, Hq, Hkv, page, groups, shared, D, dtype, layout):
+    c = Case(n, length, Hq, Hkv, D, page, dtype, layout, groups, shared, pad=1, seed=len(n) * D)
+    for most in (None, max(n)):
+        out, lse, status = c.attend(most=most)
+        assert int(status) == 0
+        c.check(out, lse)
