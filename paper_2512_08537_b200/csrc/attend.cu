@@ -596,20 +596,23 @@ template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, const
     return u;
 }
 
+// Eight rows of a unit and a kv head, by four warps, or eight where there are not too many such: a lane has a row and every fourth of its groups of four
+// values; a warp every fourth (eighth) of the row's pieces, those among its request's own tokens and those among its group's shared ones, by the maximum
+// so far (one pass: maxima come with the values). One request of 8000 tokens, 8 heads, in pieces of 64 keys: 15 us with 32 rows a head, 10 with 4; with
+// half a CTA for all rows of a unit, and two passes, it was 71 and 19. Several pieces of a warp at once cost registers, and so CTAs an SM.
 // Bound by the latency of what leads to a piece (units, blocks, pieces): 5 us where there are few, 25 for the 147 units of 256 rows that 148 CTAs cut.
-// Eight rows of a unit and a kv head, by four warps: a lane has a row and every fourth of its groups of four values; a warp every fourth of the
-// row's pieces, those among its request's own tokens and those among its group's shared ones.
-constexpr int kJoinRows = 8, kJoinWarps = 4;
+constexpr int kJoinRows = 8, kJoinWarps = 8;
 
 template <int D> struct Joined {
     float4 value[kJoinWarps][D / 4][kJoinRows];
     float2 ml[kJoinWarps][kJoinRows];
 };
 
-template <typename T, int D, bool kWide>
+// By W warps; with four of them, `half` says which of the CTA's.
+template <typename T, int D, bool kWide, int W>
 __device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half, const PlanHead& narrow, const PlanHead& wide, const Block& k, const Share& share,
                                           Cut mine, int h, int first_row) {
-    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % kJoinWarps, G = c.x.G;
+    const int lane = threadIdx.x & 31, place = threadIdx.x >> 5, warp = place % W, place0 = place - warp, G = c.x.G;
     const int r = lane % kJoinRows, quarter = lane / kJoinRows, in = first_row + r;
     const bool there = in < k.rows;
     mine.in = in;
@@ -622,17 +625,11 @@ __device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half,
     }
     const int all = there ? mine.count + theirs.count : 0;
     float top = -INFINITY, sum = 0.f;
-#pragma unroll 4
-    for (int i = warp; i < all; i += kJoinWarps) {
-        const Cut& u = i < mine.count ? mine : theirs;
-        top = fmaxf(top, c.pieces.ml[u.piece(i < mine.count ? i : i - mine.count) + u.in].x);
-    }
-    const float base = top == -INFINITY ? 0.f : top;
     float4 acc[D / 16];
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-    for (int i = warp; i < all; i += kJoinWarps) {
+#pragma unroll 1
+    for (int i = warp; i < all; i += W) {
         const Cut& u = i < mine.count ? mine : theirs;
         const long long at = u.piece(i < mine.count ? i : i - mine.count);
         const float2 ml = c.pieces.ml[at + u.in];
@@ -641,57 +638,61 @@ __device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half,
         float4 x[D / 16];
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) x[j] = *reinterpret_cast<const float4*>(from + j * step);
-        const float w = ex2(ml.x - base);
-        sum += w * ml.y;
+        const float higher = fmaxf(top, ml.x), base = higher == -INFINITY ? 0.f : higher;
+        const float old = top == higher ? 1.f : ex2(top - base), w = ex2(ml.x - base);
+        top = higher;
+        sum = sum * old + w * ml.y;
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) { acc[j].x += w * x[j].x; acc[j].y += w * x[j].y; acc[j].z += w * x[j].z; acc[j].w += w * x[j].w; }
+        for (int j = 0; j < D / 16; ++j) {
+            acc[j].x = acc[j].x * old + w * x[j].x; acc[j].y = acc[j].y * old + w * x[j].y;
+            acc[j].z = acc[j].z * old + w * x[j].z; acc[j].w = acc[j].w * old + w * x[j].w;
+        }
     }
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) s.value[warp][4 * j + quarter][r] = acc[j];
-    if (quarter == 0) s.ml[warp][r] = make_float2(top, sum);
-    ptx::bar_sync(1 + half, 32 * kJoinWarps);
-    float all_top = -INFINITY, w[kJoinWarps];
+    for (int j = 0; j < D / 16; ++j) s.value[place][4 * j + quarter][r] = acc[j];
+    if (quarter == 0) s.ml[place][r] = make_float2(top, sum);
+    ptx::bar_sync(1 + half, 32 * W);
+    float all_top = -INFINITY, w[W];
     float all_sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < kJoinWarps; ++i) all_top = fmaxf(all_top, s.ml[i][r].x);
+    for (int i = 0; i < W; ++i) all_top = fmaxf(all_top, s.ml[place0 + i][r].x);
     const float all_base = all_top == -INFINITY ? 0.f : all_top;
 #pragma unroll
-    for (int i = 0; i < kJoinWarps; ++i) {
-        const float2 ml = s.ml[i][r];
+    for (int i = 0; i < W; ++i) {
+        const float2 ml = s.ml[place0 + i][r];
         w[i] = ml.x == -INFINITY ? 0.f : ex2(ml.x - all_base);
         all_sum += w[i] * ml.y;
     }
     const float f = all_sum > 0.f ? 1.f / all_sum : all_sum;                         // no key: 0, and lse -inf
     const int row = k.row0 + in, tok = c.x.by_G.quotient(row), qh = h * G + row - tok * G;
     T* to = static_cast<T*>(c.x.out) + (k.token0 + (long long)tok) * c.x.out_token + qh * c.x.out_head;
-    for (int j = warp * 4 + quarter; there && j < D / 4; j += 4 * kJoinWarps) {
+    for (int j = warp * 4 + quarter; there && j < D / 4; j += 4 * W) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < kJoinWarps; ++i) {
-            const float4 x = s.value[i][j][r];
+        for (int i = 0; i < W; ++i) {
+            const float4 x = s.value[place0 + i][j][r];
             v.x += w[i] * x.x; v.y += w[i] * x.y; v.z += w[i] * x.z; v.w += w[i] * x.w;
         }
         *reinterpret_cast<uint2*>(to + 4 * j) = make_uint2(Pair<T>::pack(v.x * f, v.y * f), Pair<T>::pack(v.z * f, v.w * f));
     }
     if (there && warp == 0 && quarter == 0)
         c.x.lse[(k.token0 + (long long)tok) * c.x.lse_token + qh] = (all_base + log2f(all_sum)) * 0.6931471805599453f;
-    ptx::bar_sync(1 + half, 32 * kJoinWarps);
+    ptx::bar_sync(1 + half, 32 * W);
 }
 
-// The rows of a list: all of the requests' own, or, where nothing else is to be joined, those of units that a worker's first step cuts. Four warps
-// take a narrow unit, or an eighth of a wide one.
-template <typename T, int D, bool kWide>
-__device__ __forceinline__ void join_list(const Call& c, Joined<D>& s, int half, const PlanHead& narrow, const PlanHead& wide) {
+// The rows of a list: all of the requests' own, or, where nothing else is to be joined, those of units that are cut: all units are looked at, or
+// those that a worker's first step cuts, whatever is less. With W == 8 a CTA takes eight rows of a unit, else half a CTA a narrow unit or an eighth of a wide one.
+template <typename T, int D, bool kWide, int W>
+__device__ __forceinline__ void join_parts(const Call& c, Joined<D>& s, int half, const PlanHead& narrow, const PlanHead& wide, long long items, bool by_unit) {
     const List& list = list_of<kWide>(c);
     const PlanHead& head = kWide ? wide : narrow;
-    if (head.blocks == head.own) return;
-    const int H = c.cache.heads, team = kWide ? 1 : c.plan.team, kParts = kWide ? 8 : 1, rows = Sizes<kWide>::rows / kParts;
+    constexpr int kParts = W == kJoinWarps ? Sizes<kWide>::rows / kJoinRows : kWide ? 8 : 1, kRows = Sizes<kWide>::rows / kParts;
+    const int H = c.cache.heads, team = kWide ? 1 : c.plan.team;
     const long long each = steps_each<kWide>(head.steps, list.workers);
-    const long long cuts = (head.steps - 1) / each, items = head.all_rows ? (long long)(head.blocks - head.own) * H : cuts * team;
-    for (long long i = blockIdx.x * 2 + half; i < items * kParts; i += gridDim.x * 2) {
-        const int item = quotient_of(i, kParts), row0 = (int)(i - (long long)item * kParts) * rows;
+    for (long long i = W == kJoinWarps ? blockIdx.x : blockIdx.x * 2 + half; i < items * kParts; i += gridDim.x * (kJoinWarps / W)) {
+        const int item = quotient_of(i, kParts), row0 = (int)(i - (long long)item * kParts) * kRows;
         int b, h = 0;
-        if (head.all_rows) {
+        if (by_unit) {
             b = item / H;
             h = item - b * H;
             b += head.own;
@@ -700,7 +701,7 @@ __device__ __forceinline__ void join_list(const Call& c, Joined<D>& s, int half,
         }
         const Block k = list.block[b];
         if (row0 >= k.rows) continue;
-        if (!head.all_rows) {
+        if (!by_unit) {
             const long long at = each * (item / team + 1);
             const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
             h = (int)(at - k.first_step) / tiles;
@@ -712,19 +713,31 @@ __device__ __forceinline__ void join_list(const Call& c, Joined<D>& s, int half,
         const Share share = c.plan.share[k.request];
         const Cut mine = cut_of<kWide>(c, head, k, h, 0);
         if (mine.count == 1 && share.prefix < 0) continue;                              // written already
-        for (int row = row0; row < min(row0 + rows, k.rows); row += kJoinRows)
-            join_rows<T, D, kWide>(c, s, half, narrow, wide, k, share, mine, h, row);
+        for (int row = row0; row < min(row0 + kRows, k.rows); row += kJoinRows)
+            join_rows<T, D, kWide, W>(c, s, half, narrow, wide, k, share, mine, h, row);
     }
+}
+template <typename T, int D, bool kWide>
+__device__ __forceinline__ void join_list(const Call& c, Joined<D>& s, int half, const PlanHead& narrow, const PlanHead& wide) {
+    const List& list = list_of<kWide>(c);
+    const PlanHead& head = kWide ? wide : narrow;
+    if (head.blocks == head.own) return;
+    const long long cuts = (head.steps - 1) / steps_each<kWide>(head.steps, list.workers) * (kWide ? 1 : c.plan.team);
+    const long long units = (long long)(head.blocks - head.own) * c.cache.heads;
+    const bool by_unit = head.all_rows || units <= cuts;
+    const long long items = by_unit ? units : cuts;
+    if (items * (Sizes<kWide>::rows / kJoinRows) <= gridDim.x) join_parts<T, D, kWide, kJoinWarps>(c, s, 0, narrow, wide, items, by_unit);
+    else join_parts<T, D, kWide, kJoinWarps / 2>(c, s, half, narrow, wide, items, by_unit);
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(256) join_kernel(const Call c) {
-    __shared__ Joined<D> s[2];
+__global__ void __launch_bounds__(256, 2) join_kernel(const Call c) {
+    __shared__ Joined<D> s;
     ardiff::begin_kernel();
     const int half = threadIdx.x >> 7;
     const PlanHead narrow = *c.plan.narrow.head, wide = *c.plan.wide.head;
-    join_list<T, D, false>(c, s[half], half, narrow, wide);
-    join_list<T, D, true>(c, s[half], half, narrow, wide);
+    join_list<T, D, false>(c, s, half, narrow, wide);
+    join_list<T, D, true>(c, s, half, narrow, wide);
 }
 
 // ---- the call -----------------------------------------------------------------------------------

@@ -627,3 +627,12 @@ def test_few_rows_of_heads_that_share_lines_of_memory(n, length, Hq, Hkv, page, 
         out, lse, status = c.attend(most=most)
         assert int(status) == 0
         c.check(out, lse)
+
+
+@pytest.mark.parametrize("D,dtype", [(64, "f16"), (96, "bf16"), (128, "bf16")])
+@pytest.mark.parametrize("n,Hq,Hkv", [(8, 32, 8), (1, 8, 8), (3, 4, 1)])
+def test_one_request_cut_into_many_pieces(n, Hq, Hkv, D, dtype):
+    c = Case([n], [8000], Hq, Hkv, D, 64, dtype, seed=n)
+    out, lse, status = c.attend(most=n)
+    assert int(status) == 0
+    c.check(out, lse)
