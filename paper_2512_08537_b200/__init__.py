@@ -325,7 +325,7 @@ class _Torch:
         self.i32, self.i64, self.f32 = torch.int32, torch.int64, torch.float32
         self.types = {torch.bfloat16: ARDIFF_BF16, torch.float16: ARDIFF_F16, torch.float32: ARDIFF_F32}
         self.u8 = torch.uint8
-        self.empty, self.device = torch.empty, torch.cuda.device
+        self.empty, self.empty_like, self.device = torch.empty, torch.empty_like, torch.cuda.device
         self.current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
 
@@ -553,6 +553,11 @@ def _at(t) -> int:
     return 0 if t is None else t.data_ptr()
 
 
+def _made_like(x):
+    """A contiguous result of x's shape and type (empty_like takes half the time of empty, but keeps the order of strides)."""
+    return _torch.empty_like(x) if x.is_contiguous() else _torch.empty(x.shape, dtype=x.dtype, device=x.device)
+
+
 def _heads(x, index: int):
     """Address, strides of tokens and heads, and heads of a tensor [n, heads, width] whose rows are contiguous."""
     n, heads, width = x.shape
@@ -592,9 +597,9 @@ def _rotary_args(q, k, position, freq, axis):
 def _turned(fn, where, q, k, position, freq, axis, neighbours, q_out, k_out):
     index, dtype, n, width, angles = _rotary_args(q, k, position, freq, axis)
     if q_out is None:
-        q_out = _torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _made_like(q)
     if k_out is None:
-        k_out = _torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        k_out = _made_like(k)
     qp, qt, qh, q_heads = _heads(q, index)
     kp, kt, kh, k_heads = _heads(k, index)
     _run(fn, where, index, _ROTARY.pack(qp, qt, qh, *_out_heads(q_out, q, index), q_heads, kp, kt, kh, *_out_heads(k_out, k, index), k_heads,
@@ -636,7 +641,7 @@ def ardiff_rotary_append(q, k, v, position, freq, slot, k_cache, v_cache, axis=N
         return _beside(ardiff_rotary_append, stream, q, k, v, position, freq, slot, k_cache, v_cache, axis, count, neighbours, q_out)
     index, dtype, n, width, angles = _rotary_args(q, k, position, freq, axis)
     if q_out is None:
-        q_out = _torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _made_like(q)
     assert v.shape == k.shape and v.dtype is k.dtype, "keys and values of the same shape and type expected"
     assert slot.dtype is _torch.i64 and slot.numel() == n and slot.get_device() == index and slot.is_contiguous(), f"int64 slots [{n}] on cuda:{index} expected"
     if count is not None:
@@ -691,7 +696,7 @@ def ardiff_attend_pages(q, k_cache, v_cache, table, length, offset, group=None, 
         _check_i32(group, groups + 1, index)
         _check_i32(shared, groups, index)
     if out is None:
-        out = _torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _made_like(q)
     qp, qt, qh, q_heads = _heads(q, index)
     lse = _made_f32(lse, (T, q_heads), T * q_heads, q)
     status = _made_i32(status, 1, length)
