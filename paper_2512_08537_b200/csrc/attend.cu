@@ -257,7 +257,8 @@ template <int D> constexpr int kNarrowShared = kWarps * (kStages<D> * kStageByte
 
 // Every warp goes its own way (teams: through the same keys as its neighbours): 16 keys of a kv head a step, as many steps under way as its part of shared memory holds (26 to 28 KB: with
 // eight warps some 200 KB an SM, more than memory's latency asks for), no meeting with other warps. Lanes look up the places of the keys of the
-// step after the next one that is sent for, and copy 16 bytes each. (96 requests of 16 heads of 80 values, 360 MB: 84 us, 4.3 TB/s; bulk copies of
+// step after the next one that is sent for, and copy 16 bytes each. (128 requests of 4096 tokens of 8 heads of 128 values,
+// 2.1 GB: 380 us, 5.6 TB/s; 96 short requests of 16 heads of 80, 360 MB: 84 us, 4.3 TB/s; bulk copies of
 // single rows, which come at 15 clocks each, took 122; rows loaded straight into the products' registers 183, since a warp then waits for memory in every step.)
 // Rows lie 2 D + 16 bytes apart, so that the eight rows of a matrix are in different banks. Query rows are the left operand, 16 rows an
 // instruction, or twice that (kTiles == 2): with few rows it is mostly empty, but reading 512 bytes a key and head from memory takes longer than its products.
