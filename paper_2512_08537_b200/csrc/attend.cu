@@ -609,11 +609,13 @@ template <int D> struct Joined {
     float2 ml[kJoinWarps][kJoinRows];
 };
 
-// By W warps; with four of them, `half` says which of the CTA's.
+// By W warps; with four of them, `half` says which of the CTA's. A barrier's number belongs to one number of threads: halves of a CTA may be in different
+// lists, one with W == 4 and the next with W == 8.
 template <typename T, int D, bool kWide, int W>
 __device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half, const PlanHead& narrow, const PlanHead& wide, const Block& k, const Share& share,
                                           Cut mine, int h, int first_row) {
     const int lane = threadIdx.x & 31, place = threadIdx.x >> 5, warp = place % W, place0 = place - warp, G = c.x.G;
+    const int bar = W == kJoinWarps ? 3 : 1 + half;
     const int r = lane % kJoinRows, quarter = lane / kJoinRows, in = first_row + r;
     const bool there = in < k.rows;
     mine.in = in;
@@ -652,7 +654,7 @@ __device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half,
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) s.value[place][4 * j + quarter][r] = acc[j];
     if (quarter == 0) s.ml[place][r] = make_float2(top, sum);
-    ptx::bar_sync(1 + half, 32 * W);
+    ptx::bar_sync(bar, 32 * W);
     float all_top = -INFINITY, w[W];
     float all_sum = 0.f;
 #pragma unroll
@@ -678,7 +680,7 @@ __device__ __forceinline__ void join_rows(const Call& c, Joined<D>& s, int half,
     }
     if (there && warp == 0 && quarter == 0)
         c.x.lse[(k.token0 + (long long)tok) * c.x.lse_token + qh] = (all_base + log2f(all_sum)) * 0.6931471805599453f;
-    ptx::bar_sync(1 + half, 32 * W);
+    ptx::bar_sync(bar, 32 * W);
 }
 
 // The rows of a list: all of the requests' own, or, where nothing else is to be joined, those of units that are cut: all units are looked at, or

@@ -636,3 +636,17 @@ def test_one_request_cut_into_many_pieces(n, Hq, Hkv, D, dtype):
     out, lse, status = c.attend(most=n)
     assert int(status) == 0
     c.check(out, lse)
+
+
+@pytest.mark.parametrize("decoding,chunks,Hq,Hkv,D,page", [(40, [64], 32, 8, 128, 16), (64, [300, 9], 16, 4, 64, 64), (200, [33, 64], 8, 2, 80, 25), (30, [120], 16, 8, 128, 32)])
+def test_decoding_and_prompts_in_one_batch(decoding, chunks, Hq, Hkv, D, page):
+    """Many units of few rows and few of many: joined by half CTAs and by whole ones, in one call."""
+    n = [1] * decoding + chunks
+    length = [2000 - 13 * r for r in range(decoding // 2)] + [700 + r for r in range(decoding - decoding // 2)] + [1000 + x for x in chunks]
+    c = Case(n, length, Hq, Hkv, D, page, seed=decoding)
+    want = c.attend()
+    assert int(want[2]) == 0
+    c.check(want[0], want[1])
+    for _ in range(20):
+        got = c.attend()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
