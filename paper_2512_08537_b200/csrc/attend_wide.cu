@@ -472,6 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                                 for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
                                 ptx::tmem_st_32x32b_x16(o_at + q, o);
                             }
+                            ptx::tmem_st_wait();               // (the product key by key reads them again)
                         }
                     }
                     float sum;

@@ -650,3 +650,25 @@ def test_decoding_and_prompts_in_one_batch(decoding, chunks, Hq, Hkv, D, page):
     for _ in range(20):
         got = c.attend()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("D,dtype,page", [(64, "bf16", 16), (80, "f16", 25), (128, "bf16", 64)])
+def test_what_is_not_finite_where_the_maximum_rises(D, dtype, page):
+    """300 new tokens behind 20000: several tiles a CTA, and scores that rise far above the first ones' in the tiles that hold a value that is not finite."""
+    c = Case([300], [20300], 8, 8, D, page, dtype, seed=D)
+    p = torch.arange(20000, 20300, device=c.q.device)
+    c.keys[0][20000:] *= 8
+    c.k[c.table[0].long()[p // page], p % page] = c.keys[0][20000:]
+    want, want_lse, _ = c.attend()
+    c.check(want, want_lse)
+    for at_new in (40, 200, 299):
+        at = int(c.table[0, (20000 + at_new) // page]), (20000 + at_new) % page
+        for bad in (math.nan, math.inf):
+            old = c.v[at].clone()
+            c.v[at] = bad
+            out, lse, status = c.attend()
+            c.v[at] = old
+            assert int(status) == 0 and torch.equal(lse, want_lse)
+            assert not bool(torch.isfinite(out[at_new:].float()).any())
+            out[at_new:] = want[at_new:]
+            c.check(out, lse)
