@@ -454,13 +454,13 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
                 top[u] = fmaxf(fmaxf(s[t][0][2 * u], s[t][0][2 * u + 1]), fmaxf(s[t][1][2 * u], s[t][1][2 * u + 1])) * scale;
-            // a maximum that would grow by more than 2^8 (which sums and weights hold) anywhere: all rows move to theirs
-            if (__any_sync(0xffffffffu, top[0] > m[t][0] + 8.f || top[1] > m[t][1] + 8.f)) {
+            // m is the base of the weights so far. A maximum that would pass it by more than sums and weights hold, anywhere: all rows move to theirs
+            if (__any_sync(0xffffffffu, top[0] > m[t][0] + Pair<T>::kSlack || top[1] > m[t][1] + Pair<T>::kSlack)) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 1));
                     top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 2));
-                    const float higher = fmaxf(m[t][u], top[u]), alpha = m[t][u] == higher ? 1.f : ex2(m[t][u] - higher);
+                    const float higher = fmaxf(m[t][u], top[u] - Pair<T>::kLift), alpha = m[t][u] == higher ? 1.f : ex2(m[t][u] - higher);
                     m[t][u] = higher;
                     l[t][u] *= alpha;
 #pragma unroll

@@ -91,11 +91,11 @@ struct Queries {                                 // strides in values
 };
 
 // Results of a unit (a block and a kv head) in pieces: of the worker that began it, in its rows' own place (narrow blocks' rows, then wide ones'), and
-// one of every worker that went on with it, in that one's place behind all those. Values are relative to the piece's maximum, in powers of two, and lie
+// one of every worker that went on with it, in that one's place behind all those. Values are relative to the piece's base, in powers of two (its maximum, or somewhat less), and lie
 // four of a row together, the rows of the block behind one another, so that threads with a row each write side by side.
 struct Pieces {
     float* o;                                    // a piece: [width / 4][rows of the block][4]
-    float2* ml;                                  // [rows]: maximum, sum
+    float2* ml;                                  // [rows]: base, sum
     long long narrow_rows, wide_rows;            // where the workers' places begin
 };
 
@@ -196,9 +196,13 @@ __device__ __forceinline__ int find_last(const long long* x, int n, long long s)
     return lo;
 }
 
+// Pairs of 16-bit values. Weights are relative to 2^kLift below the highest score so far, which may be passed by 2^kSlack in all before it moves: in f16, whose
+// largest number is 2^16, weights of 2^7 for the highest score and up to 2^15, so that keys 2^21 lighter than the heaviest still have all their bits as operands
+// (with weights of 1 for the highest those of 2^-14 and less, which can be many behind one heavy key, lost theirs). bf16 has the range of fp32.
 template <typename T> struct Pair;
 template <> struct Pair<__nv_bfloat16> {
     static constexpr bool kBf16 = true;
+    static constexpr float kLift = 0.f, kSlack = 8.f;
     static __device__ __forceinline__ uint32_t pack(float a, float b) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);
@@ -208,6 +212,7 @@ template <> struct Pair<__nv_bfloat16> {
 };
 template <> struct Pair<__half> {
     static constexpr bool kBf16 = false;
+    static constexpr float kLift = 7.f, kSlack = 15.f;
     static __device__ __forceinline__ uint32_t pack(float a, float b) {
         const __half2 h = __floats2half2_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);

@@ -2,12 +2,12 @@
 // tiles of 128 keys that are its share of the line of steps.
 //
 //   S_t = Q_t K^T          tcgen05, 128 x 128 in tensor memory, tile t = 0, 1
-//   P_t = 2^(S_t scale - m_t), m_t a running maximum of every row
+//   P_t = 2^(S_t scale - m_t), m_t a base of every row, by its running maximum (f16: 2^7 below it)
 //   O_t = O_t + P_t V      tcgen05, P_t from tensor memory (16-bit, over S_t's first columns), V as it lies in the cache (keys are rows: N-major)
 //
 // While one tile's rows go through the exponentials the tensor cores work on the other's products, so both pipes stay busy: per step 4 x 128 x 128
 // x width multiply-adds (2048 cycles at 128) and 2 x 128 x 128 exponentials (2048 cycles of 16 a clock).
-// The maximum only moves when it would grow by more than 8 (a factor 256 that P and the sums hold easily): then O is rescaled in
+// The base only moves when the maximum would grow by more than 8 (a factor 256 that P and the sums hold easily): then O is rescaled in
 // tensor memory, which is rare; the product that last wrote O is done by then, since its successor S_t is issued after it.
 // Measured: prompts of 841 to 1024 tokens of 32 heads over 15000 shared ones, 4 requests, width 128, 1.0 TFLOP: 0.93 ms alone, 1.03 PFLOP/s, 1.1 ms back to
 // back at the clock that the power cap leaves. A step takes some 4000 cycles, 3300 of them in the issue of products that wait for
@@ -40,7 +40,6 @@ constexpr int kThreads = 12 * 32;               // three warps a quarter of the 
 constexpr int kPlaces = 4;                       // steps whose places are known
 constexpr int kRows = 128;                       // of a tile
 constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemColumns = 512;
-constexpr float kSlack = 8.f;
 
 template <int D> constexpr int kSub = (D + 63) / 64;                       // blocks of 64 values of a row
 template <int D> constexpr int kTile = kSub<D> * 128 * 128;                // bytes of 128 rows
@@ -55,7 +54,7 @@ struct Boxes {
     int tokens;
 };
 
-// 2^x of two numbers, x <= 8, by the nearest whole number and a polynomial for the rest f, |f| <= 1/2 (fitted to 2^f for the least relative
+// 2^x of two numbers, x <= 15, by the nearest whole number and a polynomial for the rest f, |f| <= 1/2 (fitted to 2^f for the least relative
 // error, 2.1e-7 in fp32): a quarter of the exponentials go this way, through pipes that have room, so that the special-function unit's 16 a
 // clock are not the bound. Numbers below -127 count as that, and 2^-127 comes out as 2^-149 (the lowest exponent has no leading one), which is 0 in 16
 // bits: a key that is not seen adds nothing, however large its value. NaN and infinities are not taken here.
@@ -458,8 +457,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                 if (look) top = highest_seen(s_at, hidden, seen, masked);
                 for (;;) {
                     const float highest = top * scale;
-                    if (look && __any_sync(0xffffffffu, highest > m + kSlack || (fresh && highest > m))) {
-                        const float higher = fmaxf(m, highest), alpha = m == higher ? 1.f : ex2(m - higher);
+                    if (look && __any_sync(0xffffffffu, highest > m + Pair<T>::kSlack || (fresh && highest > m))) {
+                        const float higher = fmaxf(m, highest - Pair<T>::kLift), alpha = m == higher ? 1.f : ex2(m - higher);
                         m = higher;
                         l *= alpha;
                         if (!fresh) {
@@ -479,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                     weights<T>(s_at, scale, m == -INFINITY ? 0.f : m, p, sum, top);
                     // NaN and +inf have no weights: the row's results are NaN
                     const bool lost = !(top * scale < INFINITY) && !(top == -INFINITY);
-                    if (look || __all_sync(0xffffffffu, lost || top * scale <= m + kSlack || top == -INFINITY)) {
+                    if (look || __all_sync(0xffffffffu, lost || top * scale <= m + Pair<T>::kSlack || top == -INFINITY)) {
                         l += lost ? NAN : sum;
                         break;
                     }

@@ -672,3 +672,40 @@ def test_what_is_not_finite_where_the_maximum_rises(D, dtype, page):
             assert not bool(torch.isfinite(out[at_new:].float()).any())
             out[at_new:] = want[at_new:]
             c.check(out, lse)
+
+
+def heavy_and_light(dtype, R, n, G, causal, D, page):
+    """One key has most of the weight and a value of 0; 16383 others, 2^19 to 2^20.6 times lighter each and all alike, so that their roundings add up, make
+    the result; in front of R requests, that look at the same pages, so that a worker goes through all of them behind the heavy one. Results by heads, and
+    the same in 64 bits."""
+    dev, dt, H, L = require_cuda(), TYPES[dtype], 8, 16384
+    g = torch.Generator(device=dev).manual_seed(D + n)
+    pages = -(-L // page)
+    k, v = torch.zeros((pages * page, H, D), device=dev), torch.zeros((pages * page, H, D), device=dev)
+    k[1:L, :, 0] = -math.log(2.0) * (19.0 + 0.23 * torch.arange(H, device=dev))
+    v[1:L] = 0.5 + torch.rand((L - 1, H, D), device=dev, generator=g)
+    k, v = k.to(dt).view(pages, page, H, D), v.to(dt).view(pages, page, H, D)
+    q = torch.zeros((R * n, H * G, D), dtype=dt, device=dev)
+    q[..., 0] = 1
+    table = torch.arange(pages, device=dev, dtype=torch.int32).repeat(R, 1)
+    out, lse, status = ardiff.ardiff_attend_pages(q, k, v, table, i32([L] * R), i32([n * r for r in range(R + 1)]), most=n, scale=1.0, causal=causal)
+    assert int(status) == 0
+    w = torch.exp(k.reshape(-1, H, D)[:L, :, 0].double())
+    want = torch.einsum("lh,lhd->hd", w, v.reshape(-1, H, D)[:L].double()) / w.sum(0)[:, None]
+    return out.view(R * n, H, G, D).double(), lse.view(R * n, H, G).double(), want[None, :, None], torch.log(w.sum(0))[None, :, None]
+
+
+HEAVY = [(160, 1, 1, True), (160, 4, 2, False), (20, 64, 4, False)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("R,n,G,causal", HEAVY)
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 25)])
+def test_light_keys_behind_a_heavy_one_keep_their_bits(dtype, R, n, G, causal, D, page):
+    out, _, want, _ = heavy_and_light(dtype, R, n, G, causal, D, page)
+    # all values are positive, so errors are relative: the weight as an operand and the result, half a step each; an exponential of 2^-22 whose argument, up to
+    # 2^5, is off by 2^-23 of it; sums in 32 bits of at most 2^14 weights, which are 2^-5 of the row's: all together below 2^-11.5 of the result in the sum that
+    # it is divided by, and 2^-14 in its own, of 2^10 products of 16 keys
+    eps = torch.finfo(TYPES[dtype]).eps / 2
+    err = ((out - want) / want).abs()
+    assert float(err.max()) <= 2 * eps + eps * eps + 2.0 ** -11.5, float(err.max())
