@@ -601,7 +601,7 @@ int ardiff_rotary_append(const ardiff_rotary_append_call* call, void* stream);
  *               ARDIFF_ERR_TIMEOUT where a bounded wait ran out (results mean nothing)
  *   workspace   dev, 256-byte aligned, at least ardiff_attend_workspace(...) bytes, as for ardiff_pages_evict
  * Products take 16-bit operands with fp32 sums; weights are fp32 and rounded to dtype as operands of the second product (in f16 those of keys down to
- * 2^-21 of the row's heaviest keep all its bits, those below 2^-32 count as 0), their sum is that of the unrounded ones. The order of sums follows sizes, lengths and `most`: equal calls give equal bits. */
+ * 2^-21 of the row's heaviest keep all its bits, those below 2^-32 of it may count as 0), their sum is that of the unrounded ones. The order of sums follows sizes, lengths and `most`: equal calls give equal bits. */
 int64_t ardiff_attend_workspace(int32_t requests, int32_t groups, int64_t tokens, int32_t q_heads, int32_t heads, int32_t head_width);
 typedef struct {
     const void* q;

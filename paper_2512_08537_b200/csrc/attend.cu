@@ -253,7 +253,7 @@ constexpr int kThreads = kWarps * 32;
 template <int D> constexpr int kPitch16 = 2 * D + 16;                     // bytes from row to row: an odd number of 16-byte places
 template <int D> constexpr int kStageBytes = 2 * kNarrowKeys * kPitch16<D>;
 template <int D> constexpr int kStages = 28400 / kStageBytes<D> < 6 ? 28400 / kStageBytes<D> : 6;
-template <int D> constexpr int kNarrowShared = kWarps * (kStages<D> * kStageBytes<D> + kNarrowKeys * 16);
+template <int D> constexpr int kNarrowShared = kWarps * (kStages<D> * kStageBytes<D> + kNarrowKeys * 16 + 4 * 32 * 4);
 
 // Every warp goes its own way (teams: through the same keys as its neighbours): 16 keys of a kv head a step, as many steps under way as its part of shared memory holds (26 to 28 KB: with
 // eight warps some 200 KB an SM, more than memory's latency asks for), no meeting with other warps. Lanes look up the places of the keys of the
@@ -276,6 +276,8 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
     const int n = (int)(min(steps, begin + each) - begin), own = list.head->own;
     const char* ring = smem + warp * kStages<D> * kStageBytes<D>;
     longlong2* place = reinterpret_cast<longlong2*>(smem + kWarps * kStages<D> * kStageBytes<D>) + warp * kNarrowKeys;
+    // this lane's sums of weights but for the last 32 steps': four rows, a lane beside the other
+    float* sums = reinterpret_cast<float*>(smem + kWarps * (kStages<D> * kStageBytes<D> + kNarrowKeys * 16)) + warp * 4 * 32 + lane;
     const uint32_t ring_at = ptx::smem_u32(ring);
 
     // where this warp is in the line of steps, and what it needs of the block: of products, and of copies some steps ahead
@@ -385,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
 
     const int G = c.x.G, quad = lane & 3, row8 = lane >> 2;
     uint32_t q[kTiles][D / 16][4];
-    float o[kTiles][D / 8][4], m[kTiles][2], l[kTiles][2];
+    float o[kTiles][D / 8][4], m[kTiles][2], l[kTiles][2];        // l: the last steps' sum of weights
     int lim[kTiles][2], least = 0;               // keys below `least` are seen by all rows of the block
     bool fresh = true, whole = now.tile == 0;
     uint32_t stage = 0;
@@ -412,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
                         q[t][ks][u + 2] = (there ? *reinterpret_cast<const uint32_t*>(from + ks * 16 + quad * 2 + 8) : 0u) ^ signs;
                     }
                     m[t][u] = -INFINITY;
-                    l[t][u] = 0.f;
+                    l[t][u] = sums[(t * 2 + u) * 32] = 0.f;
 #pragma unroll
                     for (int j = 0; j < D / 8; ++j) o[t][j][2 * u] = o[t][j][2 * u + 1] = 0.f;
                 }
@@ -463,6 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
                     const float higher = fmaxf(m[t][u], top[u] - Pair<T>::kLift), alpha = m[t][u] == higher ? 1.f : ex2(m[t][u] - higher);
                     m[t][u] = higher;
                     l[t][u] *= alpha;
+                    sums[(t * 2 + u) * 32] *= alpha;
 #pragma unroll
                     for (int j = 0; j < D / 8; ++j) { o[t][j][2 * u] *= alpha; o[t][j][2 * u + 1] *= alpha; }
                 }
@@ -471,10 +474,11 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[t][u][e] = ex2(fmaf(s[t][u][e], scale, -base[e >> 1]));
-                    l[t][e >> 1] += s[t][u][e];
-                }
+                for (int e = 0; e < 4; ++e) s[t][u][e] = ex2(fmaf(s[t][u][e], scale, -base[e >> 1]));
+            // A sum of N weights one by one is off by N steps of 2^-24 where they are alike and behind a heavy one (2.4e-4 for 16384 keys); by four,
+            // steps and groups of 32 steps it is by 32 and N / 2048 of them.
+#pragma unroll
+            for (int u = 0; u < 2; ++u) l[t][u] += (s[t][0][2 * u] + s[t][0][2 * u + 1]) + (s[t][1][2 * u] + s[t][1][2 * u + 1]);
             p[t][0] = Pair<T>::pack(s[t][0][0], s[t][0][1]);
             p[t][1] = Pair<T>::pack(s[t][0][2], s[t][0][3]);
             p[t][2] = Pair<T>::pack(s[t][1][0], s[t][1][1]);
@@ -538,6 +542,12 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
         if (++stage == kStages<D>) stage = 0;
 
         const bool ends = now.tile + 1 == now.tiles;
+        if ((i & 31) == 31) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) { sums[(t * 2 + u) * 32] += l[t][u]; l[t][u] = 0.f; }
+        }
         if (ends || i + 1 == n) {
             const Block b = list.block[now.b];
             const long long unit = b.first_step + (long long)(now.h / team) * now.tiles;       // its first step
@@ -547,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    float sum = l[t][u];
+                    float sum = l[t][u] + sums[(t * 2 + u) * 32];
                     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
                     const int in = t * 16 + row8 + 8 * u;

@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
         const float scale = fabsf(c.scale);
         uint32_t s_count = 0, o_count = 0;
         bool fresh = true, whole = now.tile == 0;
-        float m = -INFINITY, l = 0.f;
+        float m = -INFINITY, l = 0.f, recent = 0.f;                        // sums of weights, of the last 32 tiles apart: roundings add up less
         int lim = 0, least = 0;
         auto all = [](bool ok) { return __all_sync(0xffffffffu, ok) != 0; };     // a warp goes on or leaves as one
         for (int i = 0; i < n; ++i) {
@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                     }
                     cp_async_arrive(bars + (kQFull + tile) * 8);
                     m = -INFINITY;
-                    l = 0.f;
+                    l = recent = 0.f;
                     least = least_seen(now.at, G);
                     lim = in < now.at.rows ? min(now.at.key0 + now.at.keys, now.at.limit + now.at.step * tok) : now.at.key0 + now.at.keys;
                 }
@@ -461,6 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                         const float higher = fmaxf(m, highest - Pair<T>::kLift), alpha = m == higher ? 1.f : ex2(m - higher);
                         m = higher;
                         l *= alpha;
+                        recent *= alpha;
                         if (!fresh) {
 #pragma unroll 1
                             for (int q = 0; q < D; q += 16) {
@@ -479,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                     // NaN and +inf have no weights: the row's results are NaN
                     const bool lost = !(top * scale < INFINITY) && !(top == -INFINITY);
                     if (look || __all_sync(0xffffffffu, lost || top * scale <= m + Pair<T>::kSlack || top == -INFINITY)) {
-                        l += lost ? NAN : sum;
+                        recent += lost ? NAN : sum;
                         break;
                     }
                     look = true;
@@ -530,6 +531,10 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before();
                 ptx::mbar_arrive(bars + (kPFull + tile) * 8);
+                if (ends || (i & 31) == 31) {
+                    l += recent;
+                    recent = 0.f;
+                }
                 if (ends) {
                     if (!all(wait(kOFull + tile, o_count++ & 1))) break;
                     ptx::tc_fence_after();

@@ -709,3 +709,13 @@ def test_light_keys_behind_a_heavy_one_keep_their_bits(dtype, R, n, G, causal, D
     eps = torch.finfo(TYPES[dtype]).eps / 2
     err = ((out - want) / want).abs()
     assert float(err.max()) <= 2 * eps + eps * eps + 2.0 ** -11.5, float(err.max())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("R,n,G,causal", HEAVY)
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 25)])
+def test_sums_of_weights_do_not_add_up_roundings(dtype, R, n, G, causal, D, page):
+    _, lse, _, want = heavy_and_light(dtype, R, n, G, causal, D, page)
+    # roundings of 2^-24 of the sum each: up to 32 in a tile or a group of steps, 32 of groups or 128 of tiles, 16 where parts are joined: 192 at the most; the heavy
+    # key's exponential 2^-22, those of the light ones, 2^-5 of the sum, 2^-18; a logarithm of 2^-22 and lse's own rounding
+    assert float((lse - want).abs().max()) <= 192 * 2.0 ** -24 + 2.0 ** -19
