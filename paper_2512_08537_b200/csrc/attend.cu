@@ -475,8 +475,8 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const Call c) {
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[t][u][e] = ex2(fmaf(s[t][u][e], scale, -base[e >> 1]));
-            // A sum of N weights one by one is off by N steps of 2^-24 where they are alike and behind a heavy one (2.4e-4 for 16384 keys); by four,
-            // steps and groups of 32 steps it is by 32 and N / 2048 of them.
+            // A lane's sum of weights of N keys one by one is off by N / 4 steps of 2^-24 where they are alike and behind a heavy one (2.4e-4 for 16384
+            // keys); by four, steps and groups of 32 steps it is by 32 and N / 512 of them.
 #pragma unroll
             for (int u = 0; u < 2; ++u) l[t][u] += (s[t][0][2 * u] + s[t][0][2 * u + 1]) + (s[t][1][2 * u] + s[t][1][2 * u + 1]);
             p[t][0] = Pair<T>::pack(s[t][0][0], s[t][0][1]);

@@ -125,8 +125,11 @@ __device__ __forceinline__ float highest_seen(uint32_t s_at, int hidden, int see
     return high;
 }
 
-// Keys below this are seen by all rows of a block.
-__device__ __forceinline__ int least_seen(const Block& b, int G) { return min(b.key0 + b.keys, b.limit + b.step * (b.row0 / G)); }
+// Whether some row of the block does not see all keys of a tile: keys from the first row's limit on, and those in front of the block's first key.
+__device__ __forceinline__ bool some_unseen(const Block& b, int tile, const Divide& by_G) {
+    const int key0 = b.key0 + tile * kWideKeys;
+    return key0 < b.low || key0 + kWideKeys > min(b.key0 + b.keys, b.limit + b.step * (int)by_G.quotient(b.row0));
+}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const __grid_constant__ Boxes boxes) {
@@ -225,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
             const Box box = next;
             good = __all_sync(0xffffffffu, wait(empty + stage, ((i >> 1) & 1) ^ 1));
             if (!good) break;
-            const bool zone = v && now.at.key0 + (now.tile + 1) * kWideKeys > least_seen(now.at, G);
+            const bool zone = v && some_unseen(now.at, now.tile, c.x.by_G);
             const uint32_t bar = bars + ((zone ? kVLanded : full) + stage) * 8;
             const uint32_t there = __ballot_sync(0xffffffffu, box.id >= 0);
             if (lane == 0) ptx::mbar_arrive_expect_tx(bar, __popc(there) * tokens * 128 * kSub<D>);
@@ -300,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                         if (mine) cp_async16(to[u % kPeriod] + base + (u / kPeriod) * 1024, from + (o[u] & 1 ? 0 : o[u]), o[u] & 1 ? 0 : 16);
                 }
             }
-            if (v && now.at.key0 + (now.tile + 1) * kWideKeys > least_seen(now.at, G)) {
+            if (v && some_unseen(now.at, now.tile, c.x.by_G)) {
                 // keys that some row of the block does not see must not reach it as 0 times a value that is not finite
                 cp_async_commit();
                 cp_async_wait<0>();
@@ -376,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
             }
             const int stage1 = (i + 1) & 1;
             const uint32_t parity1 = ((uint32_t)(i + 1) >> 1) & 1;
-            const bool zone = now.at.key0 + (now.tile + 1) * kWideKeys > least_seen(now.at, G);
+            const bool zone = some_unseen(now.at, now.tile, c.x.by_G);
 #pragma unroll
             for (int tile = 0; tile < 2; ++tile) {
                 if (tile == 1 && !two) break;
@@ -421,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
         uint32_t s_count = 0, o_count = 0;
         bool fresh = true, whole = now.tile == 0;
         float m = -INFINITY, l = 0.f, recent = 0.f;                        // sums of weights, of the last 32 tiles apart: roundings add up less
-        int lim = 0, least = 0;
+        int lim = 0;
         auto all = [](bool ok) { return __all_sync(0xffffffffu, ok) != 0; };     // a warp goes on or leaves as one
         for (int i = 0; i < n; ++i) {
             const bool ends = now.tile + 1 == now.tiles || i + 1 == n;
@@ -441,7 +444,6 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                     cp_async_arrive(bars + (kQFull + tile) * 8);
                     m = -INFINITY;
                     l = recent = 0.f;
-                    least = least_seen(now.at, G);
                     lim = in < now.at.rows ? min(now.at.key0 + now.at.keys, now.at.limit + now.at.step * tok) : now.at.key0 + now.at.keys;
                 }
                 if (!all(wait(kSFull + tile, s_count++ & 1))) break;
@@ -486,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const Call c, const _
                     look = true;
                 }
                 bool odd = false;
-                if (now.at.key0 + (now.tile + 1) * kWideKeys > least) {
+                if (some_unseen(now.at, now.tile, c.x.by_G)) {
                     if (!all(wait(kVFull + (i & 1), ((uint32_t)i >> 1) & 1))) break;
                     odd = *(volatile int*)&s_odd[i & 1] != 0;
                 }

@@ -719,3 +719,23 @@ def test_sums_of_weights_do_not_add_up_roundings(dtype, R, n, G, causal, D, page
     # roundings of 2^-24 of the sum each: up to 32 in a tile or a group of steps, 32 of groups or 128 of tiles, 16 where parts are joined: 192 at the most; the heavy
     # key's exponential 2^-22, those of the light ones, 2^-5 of the sum, 2^-18; a logarithm of 2^-22 and lse's own rounding
     assert float((lse - want).abs().max()) <= 192 * 2.0 ** -24 + 2.0 ** -19
+
+
+@pytest.mark.parametrize("D,dtype,page", [(64, "bf16", 16), (80, "f16", 25), (128, "bf16", 64), (128, "f16", 1)])
+@pytest.mark.parametrize("shared", [200, 256, 333])
+def test_what_is_not_finite_among_shared_tokens(D, dtype, page, shared):
+    """Every query sees the shared tokens: a value that is +inf makes its column +inf, wherever the shared tokens end inside a tile of the own ones."""
+    n = [40, 50, 20]
+    c = Case(n, [700, 900, 1210], 4, 1, D, page, dtype, groups=[0, 3], shared=[shared], seed=shared, spread=0.3)
+    want, want_lse, _ = c.attend()
+    c.check(want, want_lse)
+    for p in (shared - 1, shared - 60, 3):
+        at = c.table[:, p // page].long()
+        old = c.v[at, p % page].clone()
+        c.v[at, p % page, :, 5] = math.inf
+        for kw in ({}, dict(group=None, shared=None)):
+            out, lse, status = c.attend(**kw)
+            assert int(status) == 0 and bool(torch.isposinf(out[..., 5]).all())
+            out[..., 5] = want[..., 5]
+            c.check(out, lse)
+        c.v[at, p % page] = old
