@@ -573,7 +573,7 @@ def _out_heads(x, like, index: int):
     token, head, one = x.stride()
     assert x.get_device() == index and (one == 1 or width <= 1), f"a tensor on cuda:{index} with contiguous rows expected"
     assert (heads <= 1 or head >= width) and (n <= 1 or token >= width) and \
-        (heads <= 1 or n <= 1 or (token > (heads - 1) * head if token >= head else head > (n - 1) * token)), "rows of results must not overlap"
+        (heads <= 1 or n <= 1 or (token >= (heads - 1) * head + width if token >= head else head >= (n - 1) * token + width)), "rows of results must not overlap"
     return x.data_ptr(), token, head
 
 

@@ -155,3 +155,21 @@ def test_results_where_inputs_are():
     assert call("ardiff_attend_weights", weights(), dict(new_ld=80)) == SHAPE
     assert call("ardiff_pages_evict", evict(), dict(new_ld=80)) == SHAPE
     assert call("ardiff_pages_evict", evict(), dict(new_ld=80, new_score=2 * P, position=P, new_position=P)) == SHAPE
+
+
+@pytest.mark.parametrize("n,heads,width,token,head,good", [
+    (3, 2, 64, 128, 64, True), (3, 2, 64, 127, 64, False), (3, 2, 64, 72, 64, False), (3, 2, 64, 136, 72, True), (3, 2, 64, 135, 72, False), (3, 2, 64, 64, 192, True),
+    (3, 2, 64, 64, 191, False), (3, 2, 64, 64, 136, False), (3, 2, 64, 72, 208, True), (3, 2, 64, 72, 207, False), (1, 2, 64, 8, 64, True), (3, 1, 64, 64, 8, True),
+    (3, 1, 64, 56, 8, False), (1, 2, 64, 8, 56, False), (0, 2, 64, 0, 64, True), (2, 2, 1, 2, 1, True), (2, 2, 1, 1, 1, False), (2, 2, 64, 64, 64, False)])
+def test_results_whose_rows_overlap_are_refused(n, heads, width, token, head, good):
+    import torch
+    ardiff._t()
+    like = torch.empty((n, heads, width), dtype=torch.float16)
+    x = torch.empty((4096,), dtype=torch.float16).as_strided((n, heads, width), (token, head, 1))
+    places = [t * token + h * head + d for t in range(n) for h in range(heads) for d in range(width)]
+    assert (len(set(places)) == len(places)) == good
+    if good:
+        assert ardiff._out_heads(x, like, -1) == (x.data_ptr(), token, head)
+    else:
+        with pytest.raises(AssertionError, match="overlap"):
+            ardiff._out_heads(x, like, -1)
