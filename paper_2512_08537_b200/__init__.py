@@ -632,6 +632,14 @@ def _cache_args(cache, dtype, index: int):
     return cache.data_ptr(), a, b, c
 
 
+def _written_cache_args(cache, dtype, index: int):
+    """The same for a cache that is written: no two of its rows may be one (torch refuses to write to those, too)."""
+    args = _cache_args(cache, dtype, index)
+    if 0 in args[1:]:
+        assert all(s or n <= 1 for s, n in zip(args[1:], cache.shape)), "rows of a cache that is written must not be one another's"
+    return args
+
+
 def ardiff_rotary_append(q, k, v, position, freq, slot, k_cache, v_cache, axis=None, count=None, neighbours: bool = False, q_out=None,
                          stream=None):
     """Queries turned as by ardiff_rotary (into q_out), keys turned and written with their values into a cache (k_cache, v_cache [pages, page,
@@ -652,8 +660,8 @@ def ardiff_rotary_append(q, k, v, position, freq, slot, k_cache, v_cache, axis=N
     kp, kt, kh, k_heads = _heads(k, index)
     _run(lib().ardiff_rotary_append, "ardiff_rotary_append", index,
          _APPEND.pack(qp, qt, qh, *_out_heads(q_out, q, index), q_heads, kp, kt, kh, *_heads(v, index)[:3], k_heads, dtype, n, width, *angles,
-                      1 if neighbours else 0, slot.data_ptr(), _at(count), *_cache_args(k_cache, k.dtype, index),
-                      *_cache_args(v_cache, k.dtype, index), pages, page))
+                      1 if neighbours else 0, slot.data_ptr(), _at(count), *_written_cache_args(k_cache, k.dtype, index),
+                      *_written_cache_args(v_cache, k.dtype, index), pages, page))
     return q_out
 
 
@@ -791,8 +799,8 @@ def ardiff_pages_evict(length, budget, score, table, k_cache, v_cache, first=Non
     work = _workspace(size, "ardiff_pages_evict", length.device)
     _run(L.ardiff_pages_evict, "ardiff_pages_evict", index,
          _EVICT.pack(R, length.data_ptr(), budget.data_ptr(), _at(first), score.data_ptr(), ld, _at(position), _at(seen), recent,
-                     table.data_ptr(), width, t.types.get(k_cache.dtype, -1), *_cache_args(k_cache, k_cache.dtype, index),
-                     *_cache_args(v_cache, k_cache.dtype, index), pages, page, heads, D, new_length.data_ptr(), new_score.data_ptr(),
+                     table.data_ptr(), width, t.types.get(k_cache.dtype, -1), *_written_cache_args(k_cache, k_cache.dtype, index),
+                     *_written_cache_args(v_cache, k_cache.dtype, index), pages, page, heads, D, new_length.data_ptr(), new_score.data_ptr(),
                      _at(new_position), _at(source), new_ld, status.data_ptr(), work.data_ptr(), size))
     return new_length, new_score, new_position, status
 

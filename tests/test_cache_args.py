@@ -173,3 +173,16 @@ def test_results_whose_rows_overlap_are_refused(n, heads, width, token, head, go
     else:
         with pytest.raises(AssertionError, match="overlap"):
             ardiff._out_heads(x, like, -1)
+
+
+def test_caches_whose_rows_are_one_another_s_are_not_written():
+    import torch
+    cache = torch.empty((3, 4, 2, 64), dtype=torch.float16)
+    assert ardiff._written_cache_args(cache, torch.float16, -1) == (cache.data_ptr(), 512, 128, 64)
+    assert ardiff._written_cache_args(cache.transpose(1, 2), torch.float16, -1) == (cache.data_ptr(), 512, 64, 128)
+    for x in (cache[:1].expand(3, 4, 2, 64), cache[:, :1].expand(3, 4, 2, 64), cache[:, :, :1].expand(3, 4, 2, 64)):
+        assert 0 in ardiff._cache_args(x, torch.float16, -1)[1:]
+        with pytest.raises(AssertionError, match="written"):
+            ardiff._written_cache_args(x, torch.float16, -1)
+    one = torch.empty((1, 1, 1, 64), dtype=torch.float16).as_strided((1, 1, 1, 64), (0, 0, 0, 1))
+    assert ardiff._written_cache_args(one, torch.float16, -1) == (one.data_ptr(), 0, 0, 0)
