@@ -519,8 +519,12 @@ int ardiff_distill_topk_step(const void* logits, int32_t dtype, int64_t n, int32
  * h * head_stride + d values, for 0 <= pg < pages, 0 <= i < page, 0 <= h < heads, 0 <= d < width (so the tokens of a page, or its
  * heads, may lie next to each other). Tables, lengths, offsets and slots are those of ardiff_pages_extend. Strides are not negative.
  *
+ * A row of the table names ARDIFF_CACHE_MAX_PLACES places at most, 2^31 - 2^14 (places are counted in 32 bits, some thousand at once).
+ *
  * The calls take a structure; all its fields are 64 bits wide, sizes have to fit 32 (ERR_SHAPE), pointers are NULL where an argument is left out.
  * ------------------------------------------------------------------------------------- */
+
+#define ARDIFF_CACHE_MAX_PLACES 2147467264
 
 /* Rotary positions. Token t turns pair i of every head by angle = position[axis[i]][t] * freq[i]:
  *   (a, b) -> (a cos - b sin, a sin + b cos),   values i and i + pairs of the row, or 2 i and 2 i + 1 (`neighbours` != 0);
@@ -591,7 +595,7 @@ int ardiff_rotary_append(const ardiff_rotary_append_call* call, void* stream);
  *               [tokens][q_heads], rows lse_token apart.  tokens * q_heads < 2^31, q_heads <= ARDIFF_ROTARY_MAX_HEADS, a multiple of heads
  *   caches      as above, of the same type; head_width 64, 80, 96 or 128 (others: ERR_UNSUPPORTED). Pointers on 16-byte boundaries, strides
  *               multiples of 8 values, those of q and out too. scale * log2 e is a finite float
- *   table       dev int32 [requests][width], width * page < 2^31, times heads < 2^34;  length  dev int32 [requests];  offset  dev
+ *   table       dev int32 [requests][width], width * page <= ARDIFF_CACHE_MAX_PLACES, times heads < 2^34;  length  dev int32 [requests];  offset  dev
  *               int32 [requests + 1]
  *   group       dev int32 [groups + 1], shared  dev int32 [groups]; groups == 0: NULL
  *   most        new tokens of a request at most, or 0 where that is not known: it decides how the work is laid out
@@ -664,7 +668,8 @@ int ardiff_attend_weights(const ardiff_attend_weights_call* call, void* stream);
  * infinitely heavy, NaN as -inf. Tokens that stay keep their place where it is below keep; the others move, in order, into the places
  * below keep that became free, and what is known of them with them. (Attention does not depend on the order of its keys, except for
  * new ones that must not see each other; ardiff_pages_truncate with new_length as the target gives the pages back.)
- *   requests    0 <= requests <= ARDIFF_PAGES_MAX_REQUESTS;  page >= 1, width >= 0 pages a row of the table, page * width < 2^31
+ *   requests    0 <= requests <= ARDIFF_PAGES_MAX_REQUESTS;  page >= 1, width >= 0 pages a row of the table, page * width <=
+ *               ARDIFF_CACHE_MAX_PLACES
  *   length, budget, first   dev int32 [requests]; first may be NULL (0). Budgets below 0 are 0
  *   score       dev float [requests], rows ld apart: what ardiff_attend_weights adds up
  *   position    dev int32, the same shape, or NULL: the place.  seen  dev int32 [requests], or NULL: the length

@@ -838,7 +838,7 @@ static int attend_pages_checked(const void* q, int64_t q_token, int64_t q_head, 
                                    const int32_t* group, const int32_t* shared, int32_t most, float scale, int32_t causal, void* out,
                                    int64_t out_token, int64_t out_head, float* lse, int64_t lse_token, int32_t* status, void* workspace,
                                    int64_t workspace_bytes, void* stream) {
-    if (!shape(requests, groups, tokens, q_heads, heads) || pages < 0 || page < 1 || width < 0 || (int64_t)page * width >= (int64_t)1 << 31 ||
+    if (!shape(requests, groups, tokens, q_heads, heads) || pages < 0 || page < 1 || width < 0 || (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES ||
         (int64_t)page * width * heads >= (int64_t)1 << 34 || most < 0 || !isfinite(scale * 1.4426950408889634f))
         return ARDIFF_ERR_SHAPE;
     if ((dtype != ARDIFF_BF16 && dtype != ARDIFF_F16) || (head_width != 64 && head_width != 80 && head_width != 96 && head_width != 128))

@@ -334,7 +334,7 @@ int64_t move_capacity(int64_t limit) { return limit / 2 + 1; }
 }  // namespace
 
 extern "C" int64_t ardiff_pages_evict_workspace(int32_t requests, int32_t page, int32_t width) {
-    if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || page < 1 || width < 0 || (int64_t)page * width >= (int64_t)1 << 31)
+    if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || page < 1 || width < 0 || (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES)
         return ARDIFF_ERR_SHAPE;
     return (int64_t)requests * (8 * move_capacity((int64_t)page * width) + 4) + 16;
 }
@@ -348,7 +348,7 @@ static int pages_evict_checked(int32_t requests, const int32_t* length, const in
                                   void* stream) {
     const int size = ardiff::value_size(dtype);
     if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || page < 1 || width < 0 || pages < 0 || heads < 1 || heads > 65535 ||
-        head_width < 1 || head_width > ARDIFF_ROTARY_MAX_WIDTH || recent < 0 || ld < 0 || new_ld < 0 || (int64_t)page * width >= (int64_t)1 << 31)
+        head_width < 1 || head_width > ARDIFF_ROTARY_MAX_WIDTH || recent < 0 || ld < 0 || new_ld < 0 || (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES)
         return ARDIFF_ERR_SHAPE;
     if (!size || head_width * size % 16) return ARDIFF_ERR_UNSUPPORTED;
     if (!status) return ARDIFF_ERR_NULL;

@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1) weights_kernel(const Weights c, c
                             if (!(p & 1)) {
 #pragma unroll
                                 for (int b = 0; b < kSub<D>; ++b)
-                                    ptx::tma_load_4d(smem_at + stage * kTile<D> + b * 16384 + lane * tokens * 128, &boxes.k, bar, b * 64, (int)(uint32_t)p >> 1, h,
+                                    ptx::tma_load_4d(smem_at + stage * kTile<D> + b * 16384 + lane * tokens * 128, &boxes.k, bar, b * 64, (int)((uint32_t)p >> 1), h,
                                                      (int)(p >> 32));
                             }
                         } else {
@@ -488,7 +488,7 @@ static int attend_weights_checked(const void* q, int64_t q_token, int64_t q_head
                                      void* stream) {
     if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || tokens < 0 || heads < 1 || q_heads < heads || q_heads % heads ||
         q_heads > ARDIFF_ROTARY_MAX_HEADS || tokens * q_heads >= (int64_t)1 << 31 || pages < 0 || page < 1 || width < 0 ||
-        (int64_t)page * width >= (int64_t)1 << 31 || ld < 0 || new_ld < 0 || !isfinite(scale * 1.4426950408889634f) || !isfinite(decay))
+        (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES || ld < 0 || new_ld < 0 || !isfinite(scale * 1.4426950408889634f) || !isfinite(decay))
         return ARDIFF_ERR_SHAPE;
     if ((dtype != ARDIFF_BF16 && dtype != ARDIFF_F16) || (head_width != 64 && head_width != 80 && head_width != 96 && head_width != 128))
         return ARDIFF_ERR_UNSUPPORTED;

@@ -186,3 +186,13 @@ def test_caches_whose_rows_are_one_another_s_are_not_written():
             ardiff._written_cache_args(x, torch.float16, -1)
     one = torch.empty((1, 1, 1, 64), dtype=torch.float16).as_strided((1, 1, 1, 64), (0, 0, 0, 1))
     assert ardiff._written_cache_args(one, torch.float16, -1) == (one.data_ptr(), 0, 0, 0)
+
+
+@pytest.mark.parametrize("page,width", [(1, (1 << 31) - 1), (1, (1 << 31) - (1 << 14) + 1), (127, 16909320), ((1 << 31) - 1, 1)])
+def test_places_whose_numbers_come_close_to_2_31_are_refused(page, width):
+    """Kernels step through them by thousands at once, in 32 bits."""
+    assert call("ardiff_attend_pages", attend(), dict(page=page, width=width)) == SHAPE
+    assert call("ardiff_attend_weights", weights(), dict(page=page, width=width)) == SHAPE
+    assert call("ardiff_pages_evict", evict(), dict(page=page, width=width)) == SHAPE
+    assert ardiff.lib().ardiff_pages_evict_workspace(1, page, width) == SHAPE
+    assert ardiff.lib().ardiff_pages_evict_workspace(1, 1, (1 << 31) - (1 << 14)) > 1 << 32
