@@ -34,6 +34,7 @@ using namespace ardiff;
 
 constexpr int kThreads = 256;
 constexpr int kItems = 4;                        // items of a thread under way together
+constexpr float kStill = 2.f;                    // in the place of a cosine: a pair of no axis stands still, whatever its values are (0 times an infinity would be NaN)
 
 // n / d for n * d < 2^32, by the number 2^32 / d rounded up (here n < 2^20, since a CTA has at most 2048 items or one token's, and d <= 1024)
 struct Divide {
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const Rotary a) {
     for (uint32_t j = threadIdx.x; j < (uint32_t)(tokens * a.pairs); j += kThreads) {
         const uint32_t t = quotient(j, a.by_token), i = j - t * a.pairs;
         const int axis = a.axis ? a.axis[i] : 0;
-        float s = 0.f, c = 1.f;                  // a pair of no axis stands still
+        float s = 0.f, c = kStill;
         if (axis >= 0 && axis < a.axes) {
             double turns = (double)a.position[axis * a.position_ld + t0 + t] * ((double)a.freq[i] * 0.15915494309189533577);
             turns -= rint(turns);
@@ -163,8 +164,8 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const Rotary a) {
                     T &a0 = kNeighbours ? (2 * e < VEC ? lo[u].x[2 * e < VEC ? 2 * e : 0] : hi[u].x[2 * e >= VEC ? 2 * e - VEC : 0]) : lo[u].x[e];
                     T &b0 = kNeighbours ? (2 * e + 1 < VEC ? lo[u].x[2 * e + 1 < VEC ? 2 * e + 1 : 0] : hi[u].x[2 * e + 1 >= VEC ? 2 * e + 1 - VEC : 0]) : hi[u].x[e];
                     const float x = ardiff::to_float(a0), y = ardiff::to_float(b0);
-                    v[2 * e] = ardiff::from_float<T>(x * w.x - y * w.y);
-                    v[2 * e + 1] = ardiff::from_float<T>(x * w.y + y * w.x);
+                    v[2 * e] = w.x == kStill ? a0 : ardiff::from_float<T>(x * w.x - y * w.y);
+                    v[2 * e + 1] = w.x == kStill ? b0 : ardiff::from_float<T>(x * w.y + y * w.x);
                 }
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
@@ -269,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, 3) rows_kernel(const Rotary a, int l
     for (uint32_t j = tid; j < (uint32_t)(tokens * a.pairs); j += kThreads) {
         const uint32_t tok = quotient(j, a.by_token), i = j - tok * a.pairs;
         const int axis = a.axis ? a.axis[i] : 0;
-        float s = 0.f, co = 1.f;                 // a pair of no axis stands still
+        float s = 0.f, co = kStill;
         if (axis >= 0 && axis < a.axes) {
             double turns = (double)a.position[axis * a.position_ld + t0 + tok] * ((double)a.freq[i] * 0.15915494309189533577);
             turns -= rint(turns);
@@ -286,9 +287,10 @@ __global__ void __launch_bounds__(kThreads, 3) rows_kernel(const Rotary a, int l
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         const int j = c * N + e;
-        const bool pair = j < 2 * a.pairs && mine, early = kNeighbours ? !(e & 1) : j < a.pairs;
-        const float2 w = pair ? cs[mt * a.pairs + (kNeighbours ? j >> 1 : early ? j : j - a.pairs)] : make_float2(1.f, 0.f);
-        co[e] = w.x;
+        const bool early = kNeighbours ? !(e & 1) : j < a.pairs;
+        const float2 w = j < 2 * a.pairs && mine ? cs[mt * a.pairs + (kNeighbours ? j >> 1 : early ? j : j - a.pairs)] : make_float2(kStill, 0.f);
+        const bool pair = w.x != kStill;
+        co[e] = pair ? w.x : 1.f;
         si[e] = !pair ? -0.f : early ? -w.y : w.y;               // (x - 0 is x, whatever x is)
         const uint32_t bits = N == 4 ? 0xffffffffu : e & 1 ? 0xffff0000u : 0xffffu;
         if (pair && early) up[e * 4 / N] |= bits;

@@ -163,3 +163,27 @@ def test_on_another_stream_and_captured():
     # there and back: two roundings of values that a rotation cannot make larger than sqrt 2 times the pair's larger one
     assert float((back[0].float() - q.float()).abs().max()) <= float(q.float().abs().max()) * 2.0 ** -8 * 4
     assert math.isfinite(float(back[1].float().sum()))
+
+
+@pytest.mark.parametrize("D,P,pad", [(64, 32, 0), (80, 35, 0), (64, 20, 5), (66, 33, 2), (128, 64, 0)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_pairs_of_no_axis_stand_still_whatever_they_hold(D, P, pad, dtype, neighbours):
+    q, k, _, position, freq, axis = inputs(90, 3, 2, D, P, 2, dtype, 99, D + P, pad)
+    q, k = q.clone(memory_format=torch.preserve_format), k.clone(memory_format=torch.preserve_format)
+    axis[::2] = -1
+    axis[4::6] = 2 ** 31 - 1
+    still = ((axis < 0) | (axis >= 2)).nonzero()[:, 0]
+    one, other = (2 * still, 2 * still + 1) if neighbours else (still, still + P)
+    q[3::4, :, one] = math.inf
+    q[2::4, :, other] = -math.inf
+    k[::2, :, other] = math.nan
+    k[:, :, one[1:]] = -0.0
+    for fn, sign in ((ardiff.ardiff_rotary, 1.0), (ardiff.ardiff_rotary_backward, -1.0)):
+        for x, y in zip((q, k), fn(q, k, position, freq, axis=axis, neighbours=neighbours)):
+            kept = torch.cat([one, other])
+            assert torch.equal(torch.nan_to_num(y[..., kept], nan=77.0), torch.nan_to_num(x[..., kept], nan=77.0))
+            assert torch.equal(torch.signbit(y[..., kept]), torch.signbit(x[..., kept]))
+            want, size = turned(torch.nan_to_num(x.float(), nan=0.0, posinf=0.0, neginf=0.0), position, freq, axis, neighbours, sign)
+            rest = [i for i in range(D) if i not in set(kept.tolist())]
+            near(y[..., rest], want[..., rest], size[..., rest])
