@@ -29,7 +29,7 @@ namespace {
 
 using namespace ardiff;
 
-constexpr int kMaxSms = 256;                     // whose workers have places for pieces
+constexpr int kMaxSms = 160;                     // whose workers have places for pieces
 constexpr int kPlanThreads = 1024;
 // Fewer shared tokens are read by every request itself: a block of its own and the pieces to join cost more than they take.
 constexpr int kLeastShared = 64;
@@ -595,15 +595,15 @@ template <bool kWide> __device__ __forceinline__ Cut cut_of(const Call& c, const
     const int tiles = (k.keys + Sizes<kWide>::keys - 1) / Sizes<kWide>::keys;
     Cut u;
     const int team = kWide ? 1 : c.plan.team;
-    u.rows = k.rows; u.in = in; u.cap = Sizes<kWide>::rows * team;
-    u.main = (head.rows_before + k.first_row) * c.cache.heads + (long long)h * k.rows;
-    u.others = kWide ? c.pieces.wide_rows : c.pieces.narrow_rows + h % team * kNarrowRows;
+    u.rows = k.rows; u.in = in; u.cap = (kWide ? c.pieces.wide_cap : c.pieces.narrow_cap) * team;
+    u.others = place_row<kWide>(c, h, 0);
     u.first = u.count = 0;
     if (tiles) {
         const long long each = steps_each<kWide>(head.steps, list_of<kWide>(c).workers), s0 = k.first_step + (long long)(h / team) * tiles;
         u.first = quotient_of(s0, each);
         u.count = quotient_of(s0 + tiles - 1, each) - u.first + 1;
     }
+    u.main = first_row<kWide>(c, head.rows_before, k, h, u.first);
     return u;
 }
 
@@ -755,7 +755,8 @@ __global__ void __launch_bounds__(256, 2) join_kernel(const Call c) {
 
 // ---- the call -----------------------------------------------------------------------------------
 struct Layout {
-    long long narrow_blocks, wide_blocks, main_rows, bytes, block_at[2], steps_at[2], share_at, ml_at, o_at;
+    long long narrow_blocks, wide_blocks, first_rows, narrow_cap, wide_cap, bytes, block_at[2], steps_at[2], share_at, ml_at, o_at;
+    bool begun;
 };
 Layout layout(long long requests, long long groups, long long tokens, long long q_heads, long long heads, long long width) {
     Layout s;
@@ -763,7 +764,11 @@ Layout layout(long long requests, long long groups, long long tokens, long long 
     // narrow: a segment each; wide: the full blocks, and one for the end of every segment of more than 16 rows
     s.narrow_blocks = (ends < parts * rows ? ends : parts * rows) + 1;
     s.wide_blocks = parts * (rows / kWideRows + (rows / 16 < requests ? rows / 16 : requests)) + 1;
-    s.main_rows = tokens * q_heads * parts;
+    s.narrow_cap = rows < 1 ? 1 : rows < kNarrowRows ? rows : kNarrowRows;
+    s.wide_cap = rows <= 16 ? 0 : rows < kWideRows ? rows : kWideRows;
+    const long long places = kMaxSms * (kWarps * s.narrow_cap + s.wide_cap);
+    s.begun = groups == 0 && places < tokens * q_heads;
+    s.first_rows = s.begun ? places : tokens * q_heads * parts;
     auto up = [](long long v) { return (v + 255) / 256 * 256; };
     long long at = 256;
     for (int i = 0; i < 2; ++i) {
@@ -772,7 +777,7 @@ Layout layout(long long requests, long long groups, long long tokens, long long 
         s.steps_at[i] = at; at = up(at + (blocks + 1) * 8);
     }
     s.share_at = at; at = up(at + requests * (long long)sizeof(Share));
-    const long long pieces = s.main_rows + (long long)kMaxSms * (kWarps * kNarrowRows + kWideRows);
+    const long long pieces = s.first_rows + places;
     s.ml_at = at; at = up(at + pieces * 8);
     s.o_at = at; at = up(at + pieces * width * 4);
     s.bytes = at;
@@ -887,8 +892,9 @@ static int attend_pages_checked(const void* q, int64_t q_token, int64_t q_head, 
     c.plan.share = reinterpret_cast<Share*>(w + s.share_at);
     c.pieces.ml = reinterpret_cast<float2*>(w + s.ml_at);
     c.pieces.o = reinterpret_cast<float*>(w + s.o_at);
-    c.pieces.narrow_rows = s.main_rows;
-    c.pieces.wide_rows = s.main_rows + (long long)kMaxSms * kWarps * kNarrowRows;
+    c.pieces.narrow_rows = s.first_rows;
+    c.pieces.wide_rows = s.first_rows + kMaxSms * kWarps * s.narrow_cap;
+    c.pieces.narrow_cap = (int)s.narrow_cap; c.pieces.wide_cap = (int)s.wide_cap; c.pieces.begun = s.begun;
     c.length = length; c.offset = offset; c.group = group; c.shared = shared; c.status = status;
     c.scale = scale * 1.4426950408889634f;
     if (fabsf(c.scale) < 1.2e-38f) c.scale = 1.2e-38f;       // (0 times the -inf of a key that is not seen would be NaN)

@@ -90,13 +90,16 @@ struct Queries {                                 // strides in values
     Divide by_G;
 };
 
-// Results of a unit (a block and a kv head) in pieces: of the worker that began it, in its rows' own place (narrow blocks' rows, then wide ones'), and
-// one of every worker that went on with it, in that one's place behind all those. Values are relative to the piece's base, in powers of two (its maximum, or somewhat less), and lie
+// Results of a unit (a block and a kv head) in pieces: one of every worker that went on with it, in that worker's place, and in front of all those the piece of
+// the worker that began it: in its rows' own place (narrow blocks' rows, then wide ones'), or, where no units are joined with others' and there are more rows
+// than that takes, in a second place of the worker, which leaves at most one unit unfinished. Values are relative to the piece's base, in powers of two (its maximum, or somewhat less), and lie
 // four of a row together, the rows of the block behind one another, so that threads with a row each write side by side.
 struct Pieces {
     float* o;                                    // a piece: [width / 4][rows of the block][4]
     float2* ml;                                  // [rows]: base, sum
     long long narrow_rows, wide_rows;            // where the workers' places begin
+    int narrow_cap, wide_cap;                    // rows of a place: of a block, at most
+    int begun;                                   // whether workers have a second place, as many rows in front
 };
 
 struct Call {
@@ -125,10 +128,17 @@ __device__ __forceinline__ int quotient_of(long long a, long long b) {
     return (a | b) >> 32 ? (int)(a / b) : (int)((uint32_t)a / (uint32_t)b);
 }
 
+// A worker's place for kv head h (a team of narrow workers has as many).
+template <bool kWide> __device__ __forceinline__ long long place_row(const Call& c, int h, int worker) {
+    return kWide ? c.pieces.wide_rows + (long long)worker * c.pieces.wide_cap
+                 : c.pieces.narrow_rows + ((long long)worker * c.plan.team + h % c.plan.team) * c.pieces.narrow_cap;
+}
+// Where the piece of the worker that began a unit lies.
+template <bool kWide> __device__ __forceinline__ long long first_row(const Call& c, long long rows_before, const Block& k, int h, int worker) {
+    return c.pieces.begun ? place_row<kWide>(c, h, worker) - c.pieces.narrow_rows : (rows_before + k.first_row) * c.cache.heads + (long long)h * k.rows;
+}
 template <bool kWide> __device__ __forceinline__ long long piece_row(const Call& c, long long rows_before, const Block& k, int h, int worker, int first) {
-    return worker != first ? (kWide ? c.pieces.wide_rows + (long long)worker * kWideRows
-                                    : c.pieces.narrow_rows + ((long long)worker * c.plan.team + h % c.plan.team) * kNarrowRows)
-                           : (rows_before + k.first_row) * c.cache.heads + (long long)h * k.rows;
+    return worker != first ? place_row<kWide>(c, h, worker) : first_row<kWide>(c, rows_before, k, h, worker);
 }
 
 __device__ __forceinline__ float* piece_values(const Call& c, long long piece, int width, int rows, int row, int value) {

@@ -196,3 +196,16 @@ def test_places_whose_numbers_come_close_to_2_31_are_refused(page, width):
     assert call("ardiff_pages_evict", evict(), dict(page=page, width=width)) == SHAPE
     assert ardiff.lib().ardiff_pages_evict_workspace(1, page, width) == SHAPE
     assert ardiff.lib().ardiff_pages_evict_workspace(1, 1, (1 << 31) - (1 << 14)) > 1 << 32
+
+
+def test_workspace_of_attention_holds_what_its_pieces_need():
+    L = ardiff.lib()
+    # one token of one request, 32 heads: a place of 4 rows for each of 160 x 8 warps
+    assert L.ardiff_attend_workspace(1, 0, 1, 32, 8, 128) < 4 << 20
+    # without groups two places a worker at the most, however many tokens: 2 x 160 x (8 x 32 + 256) rows of 128 values, and the list of blocks
+    for tokens in (20000, 65536):
+        assert L.ardiff_attend_workspace(64, 0, tokens, 32, 8, 128) < 90 << 20
+    # with groups every row may be joined, in both lists
+    assert 2 * 65536 * 32 * 128 * 4 < L.ardiff_attend_workspace(64, 1, 65536, 32, 8, 128) < 2 * 65536 * 32 * 130 * 4 + (50 << 20)
+    for args in ((1, 8, 1, 64), (3, 8, 2, 64), (17, 1, 1, 128)):
+        assert 0 < L.ardiff_attend_workspace(2, 0, *args) <= L.ardiff_attend_workspace(2, 1, *args)

@@ -202,3 +202,26 @@ def test_eviction_in_place(kind):
             for old, new in ((k, k2), (v, v2)):
                 rows = old[where]
                 assert torch.equal(new[where][:m], rows[at]) and torch.equal(new[where][m:], rows[m:])
+
+
+@pytest.mark.parametrize("n,length,Hq,Hkv,D,groups,shared", [
+    ([1], [5000], 4, 4, 64, None, None), ([1], [300], 8, 2, 128, None, None), ([3, 1], [4000, 77], 12, 4, 80, None, None), ([17], [3000], 1, 1, 64, None, None),
+    ([300], [9000], 8, 8, 128, None, None), ([40, 700, 1, 9], [900, 3000, 8000, 4000], 16, 4, 96, None, None), ([1] * 300, list(range(500, 2000, 5)), 16, 4, 64, None, None),
+    ([1200], [1200], 32, 8, 128, None, None), ([1] * 700, [900 + r for r in range(700)], 16, 16, 80, None, None), ([4, 9, 2], [900, 800, 850], 4, 2, 64, [0, 3], [700]),
+    ([80, 1, 70], [900, 800, 850], 8, 2, 128, [0, 2], [500])])
+def test_attention_stays_inside_its_workspace(monkeypatch, n, length, Hq, Hkv, D, groups, shared):
+    """What lies in front of the workspace and behind it keeps its bytes; what lay in it before does not matter."""
+    c = Case(n, length, Hq, Hkv, D, 16, seed=D, groups=groups, shared=shared)
+    made = []
+
+    def workspace(size, where, device):
+        made.append((torch.full((size + 8192,), 0xFF, dtype=torch.uint8, device=device), size))
+        return made[-1][0][4096:4096 + size]
+
+    monkeypatch.setattr(ardiff, "_workspace", workspace)
+    for most in (None, max(n)):
+        out, lse, status = c.attend(most=most)
+        assert int(status) == 0
+        c.check(out, lse)
+        x, size = made.pop()
+        assert bool((x[:4096] == 0xFF).all()) and bool((x[4096 + size:] == 0xFF).all())
