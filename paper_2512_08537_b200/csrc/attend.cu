@@ -836,82 +836,72 @@ extern "C" int64_t ardiff_attend_workspace(int32_t requests, int32_t groups, int
     return layout(requests, groups, tokens, q_heads, heads, head_width).bytes;
 }
 
-static int attend_pages_checked(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype, const void* k_cache,
-                                   int64_t k_page, int64_t k_token, int64_t k_head, const void* v_cache, int64_t v_page, int64_t v_token,
-                                   int64_t v_head, int32_t pages, int32_t page, int32_t heads, int32_t head_width, const int32_t* table,
-                                   int32_t width, int32_t requests, const int32_t* length, const int32_t* offset, int32_t groups,
-                                   const int32_t* group, const int32_t* shared, int32_t most, float scale, int32_t causal, void* out,
-                                   int64_t out_token, int64_t out_head, float* lse, int64_t lse_token, int32_t* status, void* workspace,
-                                   int64_t workspace_bytes, void* stream) {
-    if (!shape(requests, groups, tokens, q_heads, heads) || pages < 0 || page < 1 || width < 0 || (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES ||
+extern "C" int ardiff_attend_pages(const ardiff_attend_pages_call* call, void* stream) {
+    if (!call) return ARDIFF_ERR_NULL;
+    const ardiff_attend_pages_call& c = *call;
+    if (!ardiff::in_32_bits({c.q_heads, c.dtype, c.pages, c.page, c.heads, c.head_width, c.width, c.requests, c.groups, c.most, c.causal})) return ARDIFF_ERR_SHAPE;
+    const int requests = (int)c.requests, groups = (int)c.groups, q_heads = (int)c.q_heads, heads = (int)c.heads, head_width = (int)c.head_width;
+    const int page = (int)c.page, width = (int)c.width, most = (int)c.most, dtype = (int)c.dtype;
+    const int64_t tokens = c.tokens;
+    const float scale = (float)c.scale;
+    if (!shape(requests, groups, tokens, q_heads, heads) || c.pages < 0 || page < 1 || width < 0 || (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES ||
         (int64_t)page * width * heads >= (int64_t)1 << 34 || most < 0 || !isfinite(scale * 1.4426950408889634f))
         return ARDIFF_ERR_SHAPE;
     if ((dtype != ARDIFF_BF16 && dtype != ARDIFF_F16) || (head_width != 64 && head_width != 80 && head_width != 96 && head_width != 128))
         return ARDIFF_ERR_UNSUPPORTED;
-    if (!status || !offset || !workspace) return ARDIFF_ERR_NULL;
-    if (requests > 0 && (!length || (width > 0 && !table) || !k_cache || !v_cache)) return ARDIFF_ERR_NULL;
-    if (tokens > 0 && (!q || !out || !lse)) return ARDIFF_ERR_NULL;
-    if (groups > 0 && (!group || !shared)) return ARDIFF_ERR_NULL;
+    if (!c.status || !c.offset || !c.workspace) return ARDIFF_ERR_NULL;
+    if (requests > 0 && (!c.length || (width > 0 && !c.table) || !c.k_cache || !c.v_cache)) return ARDIFF_ERR_NULL;
+    if (tokens > 0 && (!c.q || !c.out || !c.lse)) return ARDIFF_ERR_NULL;
+    if (groups > 0 && (!c.group || !c.shared)) return ARDIFF_ERR_NULL;
     auto low = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
-    if (((low(q) | low(out) | low(k_cache) | low(v_cache)) & 15u) || (low(workspace) & 255u) ||
-        ((q_token | q_head | out_token | out_head | k_page | k_token | k_head | v_page | v_token | v_head) & 7))
+    if (((low(c.q) | low(c.out) | low(c.k_cache) | low(c.v_cache)) & 15u) || (low(c.workspace) & 255u) ||
+        ((c.q_token | c.q_head | c.out_token | c.out_head | c.k_page | c.k_token | c.k_head | c.v_page | c.v_token | c.v_head) & 7))
         return ARDIFF_ERR_ALIGN;
     const Layout s = layout(requests, groups, tokens, q_heads, heads, head_width);
-    if (workspace_bytes < s.bytes) return ARDIFF_ERR_SHAPE;
-    if (tokens > 0 && q == out) return ARDIFF_ERR_UNSUPPORTED;         // (blocks of other workers still read them)
+    if (c.workspace_bytes < s.bytes) return ARDIFF_ERR_SHAPE;
+    if (tokens > 0 && c.q == c.out) return ARDIFF_ERR_UNSUPPORTED;         // (blocks of other workers still read them)
     const int sms = device_sms();
     if (sms < 1) return ARDIFF_ERR_CUDA;
-    Call c;
-    memset(&c, 0, sizeof(c));
-    c.cache.k = static_cast<const char*>(k_cache); c.cache.v = static_cast<const char*>(v_cache);
-    c.cache.table = table; c.cache.width = width; c.cache.page = page; c.cache.pages = pages; c.cache.heads = heads; c.cache.by_page = divide_by(page);
-    if (!strides_of(k_page, k_token, k_head, c.cache, c.cache.k_page, c.cache.k_token, c.cache.k_head) ||
-        !strides_of(v_page, v_token, v_head, c.cache, c.cache.v_page, c.cache.v_token, c.cache.v_head))
+    Call a;
+    memset(&a, 0, sizeof(a));
+    a.cache.k = static_cast<const char*>(c.k_cache); a.cache.v = static_cast<const char*>(c.v_cache);
+    a.cache.table = c.table; a.cache.width = width; a.cache.page = page; a.cache.pages = c.pages; a.cache.heads = heads; a.cache.by_page = divide_by(page);
+    if (!strides_of(c.k_page, c.k_token, c.k_head, a.cache, a.cache.k_page, a.cache.k_token, a.cache.k_head) ||
+        !strides_of(c.v_page, c.v_token, c.v_head, a.cache, a.cache.v_page, a.cache.v_token, a.cache.v_head))
         return ARDIFF_ERR_SHAPE;
-    c.x.q = q; c.x.out = out; c.x.lse = lse; c.x.q_token = q_token; c.x.q_head = q_head; c.x.out_token = out_token; c.x.out_head = out_head;
-    c.x.lse_token = lse_token; c.x.heads = q_heads; c.x.G = q_heads / heads; c.x.tokens = tokens;
-    c.x.by_G = divide_by(q_heads / heads);
-    char* w = static_cast<char*>(workspace);
+    a.x.q = c.q; a.x.out = c.out; a.x.lse = c.lse; a.x.q_token = c.q_token; a.x.q_head = c.q_head; a.x.out_token = c.out_token; a.x.out_head = c.out_head;
+    a.x.lse_token = c.lse_token; a.x.heads = q_heads; a.x.G = q_heads / heads; a.x.tokens = tokens;
+    a.x.by_G = divide_by(q_heads / heads);
+    char* w = static_cast<char*>(c.workspace);
     for (int i = 0; i < 2; ++i) {
-        List& l = i ? c.plan.wide : c.plan.narrow;
+        List& l = i ? a.plan.wide : a.plan.narrow;
         l.head = reinterpret_cast<PlanHead*>(w) + i;
         l.block = reinterpret_cast<Block*>(w + s.block_at[i]);
         l.steps = reinterpret_cast<long long*>(w + s.steps_at[i]);
     }
-    c.plan.wide.workers = sms < kMaxSms ? sms : kMaxSms;
+    a.plan.wide.workers = sms < kMaxSms ? sms : kMaxSms;
     // Memory is read in lines of 128 bytes. Where rows of neighbouring heads share them, warps of a CTA go through the same keys of
     // several heads, so that what one does not want is in L2 for the next (96 requests of 3500 tokens, 16 heads of 80 values side by side, 1.7 GB:
     // 313 us, 472 without).
-    c.plan.team = 1;
-    if (head_width % 64 && k_head < k_token && k_head % 64)
-        while (c.plan.team < kWarps && heads % (2 * c.plan.team) == 0) c.plan.team *= 2;
-    c.plan.narrow.workers = c.plan.wide.workers * kWarps / c.plan.team;
+    a.plan.team = 1;
+    if (head_width % 64 && c.k_head < c.k_token && c.k_head % 64)
+        while (a.plan.team < kWarps && heads % (2 * a.plan.team) == 0) a.plan.team *= 2;
+    a.plan.narrow.workers = a.plan.wide.workers * kWarps / a.plan.team;
     // (a request's rows at most, or on average where that is not known: those of more go the wide way)
     const int64_t news = most > 0 ? most : requests > 0 ? (tokens + requests - 1) / requests : 0;
-    c.plan.narrow_rows = news * c.x.G <= 16 ? 16 : 32;
-    c.plan.share = reinterpret_cast<Share*>(w + s.share_at);
-    c.pieces.ml = reinterpret_cast<float2*>(w + s.ml_at);
-    c.pieces.o = reinterpret_cast<float*>(w + s.o_at);
-    c.pieces.narrow_rows = s.first_rows;
-    c.pieces.wide_rows = s.first_rows + kMaxSms * kWarps * s.narrow_cap;
-    c.pieces.narrow_cap = (int)s.narrow_cap; c.pieces.wide_cap = (int)s.wide_cap; c.pieces.begun = s.begun;
-    c.length = length; c.offset = offset; c.group = group; c.shared = shared; c.status = status;
-    c.scale = scale * 1.4426950408889634f;
-    if (fabsf(c.scale) < 1.2e-38f) c.scale = 1.2e-38f;       // (0 times the -inf of a key that is not seen would be NaN)
-    c.requests = requests; c.groups = groups; c.causal = causal != 0; c.most = most;
+    a.plan.narrow_rows = news * a.x.G <= 16 ? 16 : 32;
+    a.plan.share = reinterpret_cast<Share*>(w + s.share_at);
+    a.pieces.ml = reinterpret_cast<float2*>(w + s.ml_at);
+    a.pieces.o = reinterpret_cast<float*>(w + s.o_at);
+    a.pieces.narrow_rows = s.first_rows;
+    a.pieces.wide_rows = s.first_rows + kMaxSms * kWarps * s.narrow_cap;
+    a.pieces.narrow_cap = (int)s.narrow_cap; a.pieces.wide_cap = (int)s.wide_cap; a.pieces.begun = s.begun;
+    a.length = c.length; a.offset = c.offset; a.group = c.group; a.shared = c.shared; a.status = c.status;
+    a.scale = scale * 1.4426950408889634f;
+    if (fabsf(a.scale) < 1.2e-38f) a.scale = 1.2e-38f;       // (0 times the -inf of a key that is not seen would be NaN)
+    a.requests = requests; a.groups = groups; a.causal = c.causal != 0; a.most = most;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool ok = dtype == ARDIFF_F16 ? launch_width<__half>(c, dtype, head_width, most, sms, st)
-                                        : launch_width<__nv_bfloat16>(c, dtype, head_width, most, sms, st);
+    const bool ok = dtype == ARDIFF_F16 ? launch_width<__half>(a, dtype, head_width, most, sms, st)
+                                        : launch_width<__nv_bfloat16>(a, dtype, head_width, most, sms, st);
     return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
-}
-
-extern "C" int ardiff_attend_pages(const ardiff_attend_pages_call* a, void* stream) {
-    if (!a) return ARDIFF_ERR_NULL;
-    if (!ardiff::in_32_bits({a->q_heads, a->dtype, a->pages, a->page, a->heads, a->head_width, a->width, a->requests, a->groups, a->most,
-        a->causal})) return ARDIFF_ERR_SHAPE;
-    return attend_pages_checked(a->q, a->q_token, a->q_head, (int32_t)a->q_heads, a->tokens, (int32_t)a->dtype, a->k_cache, a->k_page,
-        a->k_token, a->k_head, a->v_cache, a->v_page, a->v_token, a->v_head, (int32_t)a->pages, (int32_t)a->page, (int32_t)a->heads,
-        (int32_t)a->head_width, a->table, (int32_t)a->width, (int32_t)a->requests, a->length, a->offset, (int32_t)a->groups, a->group,
-        a->shared, (int32_t)a->most, (float)a->scale, (int32_t)a->causal, a->out, a->out_token, a->out_head, a->lse, a->lse_token,
-        a->status, a->workspace, a->workspace_bytes, stream);
 }

@@ -339,44 +339,41 @@ extern "C" int64_t ardiff_pages_evict_workspace(int32_t requests, int32_t page, 
     return (int64_t)requests * (8 * move_capacity((int64_t)page * width) + 4) + 16;
 }
 
-static int pages_evict_checked(int32_t requests, const int32_t* length, const int32_t* budget, const int32_t* first, const float* score,
-                                  int64_t ld, const int32_t* position, const int32_t* seen, int32_t recent, const int32_t* table,
-                                  int32_t width, int32_t dtype, void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head,
-                                  void* v_cache, int64_t v_page, int64_t v_token, int64_t v_head, int32_t pages, int32_t page,
-                                  int32_t heads, int32_t head_width, int32_t* new_length, float* new_score, int32_t* new_position,
-                                  int32_t* source, int64_t new_ld, int32_t* status, void* workspace, int64_t workspace_bytes,
-                                  void* stream) {
-    const int size = ardiff::value_size(dtype);
-    if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || page < 1 || width < 0 || pages < 0 || heads < 1 || heads > 65535 ||
-        head_width < 1 || head_width > ARDIFF_ROTARY_MAX_WIDTH || recent < 0 || ld < 0 || new_ld < 0 || (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES)
+extern "C" int ardiff_pages_evict(const ardiff_pages_evict_call* call, void* stream) {
+    if (!call) return ARDIFF_ERR_NULL;
+    const ardiff_pages_evict_call& c = *call;
+    if (!ardiff::in_32_bits({c.requests, c.recent, c.width, c.dtype, c.pages, c.page, c.heads, c.head_width})) return ARDIFF_ERR_SHAPE;
+    const int requests = (int)c.requests, page = (int)c.page, width = (int)c.width, size = ardiff::value_size((int32_t)c.dtype);
+    if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || page < 1 || width < 0 || c.pages < 0 || c.heads < 1 || c.heads > 65535 ||
+        c.head_width < 1 || c.head_width > ARDIFF_ROTARY_MAX_WIDTH || c.recent < 0 || c.ld < 0 || c.new_ld < 0 || (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES)
         return ARDIFF_ERR_SHAPE;
-    if (!size || head_width * size % 16) return ARDIFF_ERR_UNSUPPORTED;
-    if (!status) return ARDIFF_ERR_NULL;
-    if (requests > 0 && (!length || !budget || !score || !new_length || !new_score || !workspace || (width > 0 && !table) || !k_cache || !v_cache))
+    if (!size || c.head_width * size % 16) return ARDIFF_ERR_UNSUPPORTED;
+    if (!c.status) return ARDIFF_ERR_NULL;
+    if (requests > 0 && (!c.length || !c.budget || !c.score || !c.new_length || !c.new_score || !c.workspace || (width > 0 && !c.table) || !c.k_cache || !c.v_cache))
         return ARDIFF_ERR_NULL;
-    if (((reinterpret_cast<uintptr_t>(k_cache) | reinterpret_cast<uintptr_t>(v_cache)) & 15u) ||
-        ((k_page | k_token | k_head | v_page | v_token | v_head) * size & 15) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
+    if (((reinterpret_cast<uintptr_t>(c.k_cache) | reinterpret_cast<uintptr_t>(c.v_cache)) & 15u) ||
+        ((c.k_page | c.k_token | c.k_head | c.v_page | c.v_token | c.v_head) * size & 15) || (reinterpret_cast<uintptr_t>(c.workspace) & 15u))
         return ARDIFF_ERR_ALIGN;
     const int64_t limit = (int64_t)page * width;
-    if (workspace_bytes < ardiff_pages_evict_workspace(requests, page, width) && requests > 0) return ARDIFF_ERR_SHAPE;
-    if (requests > 1 && ld != new_ld && (score == new_score || (position && position == new_position))) return ARDIFF_ERR_SHAPE;
+    if (c.workspace_bytes < ardiff_pages_evict_workspace(requests, page, width) && requests > 0) return ARDIFF_ERR_SHAPE;
+    if (requests > 1 && c.ld != c.new_ld && (c.score == c.new_score || (c.position && c.position == c.new_position))) return ARDIFF_ERR_SHAPE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     Evict a;
     memset(&a, 0, sizeof(a));
-    a.length = length; a.budget = budget; a.first = first; a.score = score; a.position = position; a.seen = seen; a.table = table;
-    a.k = static_cast<char*>(k_cache); a.v = static_cast<char*>(v_cache);
-    a.new_length = new_length; a.new_score = new_score; a.new_position = new_position; a.source = source; a.status = status;
+    a.length = c.length; a.budget = c.budget; a.first = c.first; a.score = c.score; a.position = c.position; a.seen = c.seen; a.table = c.table;
+    a.k = static_cast<char*>(c.k_cache); a.v = static_cast<char*>(c.v_cache);
+    a.new_length = c.new_length; a.new_score = c.new_score; a.new_position = c.new_position; a.source = c.source; a.status = c.status;
     a.capacity = (int)move_capacity(limit);
-    a.move = static_cast<int2*>(workspace);
+    a.move = static_cast<int2*>(c.workspace);
     a.moves = reinterpret_cast<int32_t*>(a.move + (int64_t)requests * a.capacity);
-    a.ld = ld; a.new_ld = new_ld;
-    a.limit = limit < ld ? limit : ld;
-    a.limit = a.limit < new_ld ? a.limit : new_ld;
-    a.k_page = k_page * size; a.k_token = k_token * size; a.k_head = k_head * size;
-    a.v_page = v_page * size; a.v_token = v_token * size; a.v_head = v_head * size;
-    a.requests = requests; a.recent = recent; a.page = page; a.width = width; a.pages = pages; a.heads = heads; a.row = head_width * size;
+    a.ld = c.ld; a.new_ld = c.new_ld;
+    a.limit = limit < c.ld ? limit : c.ld;
+    a.limit = a.limit < c.new_ld ? a.limit : c.new_ld;
+    a.k_page = c.k_page * size; a.k_token = c.k_token * size; a.k_head = c.k_head * size;
+    a.v_page = c.v_page * size; a.v_token = c.v_token * size; a.v_head = c.v_head * size;
+    a.requests = requests; a.recent = c.recent; a.page = page; a.width = width; a.pages = c.pages; a.heads = c.heads; a.row = c.head_width * size;
     if (requests == 0) {
-        const bool ok = cudaMemsetAsync(status, 0, 4, st) == cudaSuccess;
+        const bool ok = cudaMemsetAsync(c.status, 0, 4, st) == cudaSuccess;
         ardiff::set_launch_count(0);
         return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
     }
@@ -395,14 +392,4 @@ static int pages_evict_checked(int32_t requests, const int32_t* length, const in
                     ardiff::launch_early(move_kernel, (unsigned)(requests * split), 256, 1, 0, st, a, split);
     ardiff::set_launch_count(2);
     return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
-}
-
-extern "C" int ardiff_pages_evict(const ardiff_pages_evict_call* a, void* stream) {
-    if (!a) return ARDIFF_ERR_NULL;
-    if (!ardiff::in_32_bits({a->requests, a->recent, a->width, a->dtype, a->pages, a->page, a->heads,
-        a->head_width})) return ARDIFF_ERR_SHAPE;
-    return pages_evict_checked((int32_t)a->requests, a->length, a->budget, a->first, a->score, a->ld, a->position, a->seen,
-        (int32_t)a->recent, a->table, (int32_t)a->width, (int32_t)a->dtype, a->k_cache, a->k_page, a->k_token, a->k_head, a->v_cache,
-        a->v_page, a->v_token, a->v_head, (int32_t)a->pages, (int32_t)a->page, (int32_t)a->heads, (int32_t)a->head_width, a->new_length,
-        a->new_score, a->new_position, a->source, a->new_ld, a->status, a->workspace, a->workspace_bytes, stream);
 }

@@ -425,84 +425,42 @@ int rotary(Rotary& a, int32_t dtype, int32_t neighbours, bool append, cudaStream
     return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
 }
 
-Rotary arguments(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head, int32_t q_heads,
-                 const void* k, int64_t k_token, int64_t k_head, int32_t k_heads, int64_t n, int32_t width, const int32_t* position,
-                 int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs) {
+// What both structures say, of queries, keys and angles.
+template <typename C> Rotary arguments(const C& c, float sign) {
     Rotary a;
     memset(&a, 0, sizeof(a));
-    a.q = Side{q, q_out, q_token, q_head, q_out_token, q_out_head, q_heads};
-    a.k.in = k; a.k.in_token = k_token; a.k.in_head = k_head; a.k.heads = k_heads;
-    a.n = n; a.width = width; a.position = position; a.position_ld = position_ld; a.axes = axes; a.freq = freq; a.axis = axis;
-    a.pairs = pairs; a.sign = 1.f;
+    a.q.in = c.q; a.q.in_token = c.q_token; a.q.in_head = c.q_head; a.q.heads = (int)c.q_heads;
+    a.q.out = c.q_out; a.q.out_token = c.q_out_token; a.q.out_head = c.q_out_head;
+    a.k.in = c.k; a.k.in_token = c.k_token; a.k.in_head = c.k_head; a.k.heads = (int)c.k_heads;
+    a.n = c.n; a.width = (int)c.width; a.position = c.position; a.position_ld = c.position_ld; a.axes = (int)c.axes; a.freq = c.freq; a.axis = c.axis;
+    a.pairs = (int)c.pairs; a.sign = sign;
     return a;
+}
+
+int turned(const ardiff_rotary_call* call, float sign, void* stream) {
+    if (!call) return ARDIFF_ERR_NULL;
+    const ardiff_rotary_call& c = *call;
+    if (!ardiff::in_32_bits({c.q_heads, c.k_heads, c.dtype, c.width, c.axes, c.pairs, c.neighbours})) return ARDIFF_ERR_SHAPE;
+    Rotary a = arguments(c, sign);
+    a.k.out = c.k_out; a.k.out_token = c.k_out_token; a.k.out_head = c.k_out_head;
+    return rotary(a, (int32_t)c.dtype, (int32_t)c.neighbours, false, static_cast<cudaStream_t>(stream));
 }
 
 }  // namespace
 
-static int rotary_checked(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token, int64_t q_out_head,
-                             int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, void* k_out, int64_t k_out_token,
-                             int64_t k_out_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width, const int32_t* position,
-                             int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis, int32_t pairs,
-                             int32_t neighbours, void* stream) {
-    Rotary a = arguments(q, q_token, q_head, q_out, q_out_token, q_out_head, q_heads, k, k_token, k_head, k_heads, n, width, position,
-                         position_ld, axes, freq, axis, pairs);
-    a.k.out = k_out; a.k.out_token = k_out_token; a.k.out_head = k_out_head;
-    return rotary(a, dtype, neighbours, false, static_cast<cudaStream_t>(stream));
-}
+extern "C" int ardiff_rotary(const ardiff_rotary_call* call, void* stream) { return turned(call, 1.f, stream); }
 
-extern "C" int ardiff_rotary(const ardiff_rotary_call* a, void* stream) {
-    if (!a) return ARDIFF_ERR_NULL;
-    if (!ardiff::in_32_bits({a->q_heads, a->k_heads, a->dtype, a->width, a->axes, a->pairs, a->neighbours})) return ARDIFF_ERR_SHAPE;
-    return rotary_checked(a->q, a->q_token, a->q_head, a->q_out, a->q_out_token, a->q_out_head, (int32_t)a->q_heads, a->k, a->k_token,
-        a->k_head, a->k_out, a->k_out_token, a->k_out_head, (int32_t)a->k_heads, (int32_t)a->dtype, a->n, (int32_t)a->width, a->position,
-        a->position_ld, (int32_t)a->axes, a->freq, a->axis, (int32_t)a->pairs, (int32_t)a->neighbours, stream);
-}
+extern "C" int ardiff_rotary_backward(const ardiff_rotary_call* call, void* stream) { return turned(call, -1.f, stream); }
 
-static int rotary_backward_checked(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token,
-                                      int64_t q_out_head, int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, void* k_out,
-                                      int64_t k_out_token, int64_t k_out_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width,
-                                      const int32_t* position, int64_t position_ld, int32_t axes, const float* freq,
-                                      const int32_t* axis, int32_t pairs, int32_t neighbours, void* stream) {
-    Rotary a = arguments(q, q_token, q_head, q_out, q_out_token, q_out_head, q_heads, k, k_token, k_head, k_heads, n, width, position,
-                         position_ld, axes, freq, axis, pairs);
-    a.k.out = k_out; a.k.out_token = k_out_token; a.k.out_head = k_out_head;
-    a.sign = -1.f;
-    return rotary(a, dtype, neighbours, false, static_cast<cudaStream_t>(stream));
-}
-
-extern "C" int ardiff_rotary_backward(const ardiff_rotary_call* a, void* stream) {
-    if (!a) return ARDIFF_ERR_NULL;
-    if (!ardiff::in_32_bits({a->q_heads, a->k_heads, a->dtype, a->width, a->axes, a->pairs, a->neighbours})) return ARDIFF_ERR_SHAPE;
-    return rotary_backward_checked(a->q, a->q_token, a->q_head, a->q_out, a->q_out_token, a->q_out_head, (int32_t)a->q_heads, a->k,
-        a->k_token, a->k_head, a->k_out, a->k_out_token, a->k_out_head, (int32_t)a->k_heads, (int32_t)a->dtype, a->n, (int32_t)a->width,
-        a->position, a->position_ld, (int32_t)a->axes, a->freq, a->axis, (int32_t)a->pairs, (int32_t)a->neighbours, stream);
-}
-
-static int rotary_append_checked(const void* q, int64_t q_token, int64_t q_head, void* q_out, int64_t q_out_token,
-                                    int64_t q_out_head, int32_t q_heads, const void* k, int64_t k_token, int64_t k_head, const void* v,
-                                    int64_t v_token, int64_t v_head, int32_t k_heads, int32_t dtype, int64_t n, int32_t width,
-                                    const int32_t* position, int64_t position_ld, int32_t axes, const float* freq, const int32_t* axis,
-                                    int32_t pairs, int32_t neighbours, const int64_t* slot, const int32_t* count, void* k_cache,
-                                    int64_t k_cache_page, int64_t k_cache_token, int64_t k_cache_head, void* v_cache,
-                                    int64_t v_cache_page, int64_t v_cache_token, int64_t v_cache_head, int32_t pages, int32_t page,
-                                    void* stream) {
-    if (pages < 0 || page < 1) return ARDIFF_ERR_SHAPE;
-    Rotary a = arguments(q, q_token, q_head, q_out, q_out_token, q_out_head, q_heads, k, k_token, k_head, k_heads, n, width, position,
-                         position_ld, axes, freq, axis, pairs);
-    a.k.out = k_cache; a.k.out_token = k_cache_token; a.k.out_head = k_cache_head; a.k_page = k_cache_page;
-    a.v = Side{v, v_cache, v_token, v_head, v_cache_token, v_cache_head, k_heads};
-    a.v_page = v_cache_page;
-    a.slot = slot; a.count = count; a.page = page; a.slots = (long long)pages * page;
-    return rotary(a, dtype, neighbours, true, static_cast<cudaStream_t>(stream));
-}
-
-extern "C" int ardiff_rotary_append(const ardiff_rotary_append_call* a, void* stream) {
-    if (!a) return ARDIFF_ERR_NULL;
-    if (!ardiff::in_32_bits({a->q_heads, a->k_heads, a->dtype, a->width, a->axes, a->pairs, a->neighbours, a->pages,
-        a->page})) return ARDIFF_ERR_SHAPE;
-    return rotary_append_checked(a->q, a->q_token, a->q_head, a->q_out, a->q_out_token, a->q_out_head, (int32_t)a->q_heads, a->k,
-        a->k_token, a->k_head, a->v, a->v_token, a->v_head, (int32_t)a->k_heads, (int32_t)a->dtype, a->n, (int32_t)a->width, a->position,
-        a->position_ld, (int32_t)a->axes, a->freq, a->axis, (int32_t)a->pairs, (int32_t)a->neighbours, a->slot, a->count, a->k_cache,
-        a->k_cache_page, a->k_cache_token, a->k_cache_head, a->v_cache, a->v_cache_page, a->v_cache_token, a->v_cache_head,
-        (int32_t)a->pages, (int32_t)a->page, stream);
+extern "C" int ardiff_rotary_append(const ardiff_rotary_append_call* call, void* stream) {
+    if (!call) return ARDIFF_ERR_NULL;
+    const ardiff_rotary_append_call& c = *call;
+    if (!ardiff::in_32_bits({c.q_heads, c.k_heads, c.dtype, c.width, c.axes, c.pairs, c.neighbours, c.pages, c.page})) return ARDIFF_ERR_SHAPE;
+    if (c.pages < 0 || c.page < 1) return ARDIFF_ERR_SHAPE;
+    Rotary a = arguments(c, 1.f);
+    a.k.out = c.k_cache; a.k.out_token = c.k_cache_token; a.k.out_head = c.k_cache_head; a.k_page = c.k_cache_page;
+    a.v.in = c.v; a.v.in_token = c.v_token; a.v.in_head = c.v_head; a.v.heads = a.k.heads;
+    a.v.out = c.v_cache; a.v.out_token = c.v_cache_token; a.v.out_head = c.v_cache_head; a.v_page = c.v_cache_page;
+    a.slot = c.slot; a.count = c.count; a.page = (int)c.page; a.slots = (long long)c.pages * c.page;
+    return rotary(a, (int32_t)c.dtype, (int32_t)c.neighbours, true, static_cast<cudaStream_t>(stream));
 }

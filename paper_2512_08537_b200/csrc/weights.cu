@@ -479,63 +479,54 @@ extern "C" int64_t ardiff_attend_weights_workspace(int32_t requests) {
     return part_at(requests) + (int64_t)kMaxSplit * kKeys * 4;
 }
 
-static int attend_weights_checked(const void* q, int64_t q_token, int64_t q_head, int32_t q_heads, int64_t tokens, int32_t dtype,
-                                     const void* k_cache, int64_t k_page, int64_t k_token, int64_t k_head, int32_t pages, int32_t page,
-                                     int32_t heads, int32_t head_width, const int32_t* table, int32_t width, int32_t requests,
-                                     const int32_t* length, const int32_t* offset, const int32_t* first, const float* lse,
-                                     int64_t lse_token, const float* score, int64_t ld, float scale, float decay, int32_t causal,
-                                     float* new_score, int64_t new_ld, int32_t* status, void* workspace, int64_t workspace_bytes,
-                                     void* stream) {
+extern "C" int ardiff_attend_weights(const ardiff_attend_weights_call* call, void* stream) {
+    if (!call) return ARDIFF_ERR_NULL;
+    const ardiff_attend_weights_call& c = *call;
+    if (!ardiff::in_32_bits({c.q_heads, c.dtype, c.pages, c.page, c.heads, c.head_width, c.width, c.requests, c.causal})) return ARDIFF_ERR_SHAPE;
+    const int requests = (int)c.requests, q_heads = (int)c.q_heads, heads = (int)c.heads, head_width = (int)c.head_width, page = (int)c.page;
+    const int width = (int)c.width, dtype = (int)c.dtype;
+    const int64_t tokens = c.tokens;
+    const float scale = (float)c.scale, decay = (float)c.decay;
     if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || tokens < 0 || heads < 1 || q_heads < heads || q_heads % heads ||
-        q_heads > ARDIFF_ROTARY_MAX_HEADS || tokens * q_heads >= (int64_t)1 << 31 || pages < 0 || page < 1 || width < 0 ||
-        (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES || ld < 0 || new_ld < 0 || !isfinite(scale * 1.4426950408889634f) || !isfinite(decay))
+        q_heads > ARDIFF_ROTARY_MAX_HEADS || tokens * q_heads >= (int64_t)1 << 31 || c.pages < 0 || page < 1 || width < 0 ||
+        (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES || c.ld < 0 || c.new_ld < 0 || !isfinite(scale * 1.4426950408889634f) || !isfinite(decay))
         return ARDIFF_ERR_SHAPE;
     if ((dtype != ARDIFF_BF16 && dtype != ARDIFF_F16) || (head_width != 64 && head_width != 80 && head_width != 96 && head_width != 128))
         return ARDIFF_ERR_UNSUPPORTED;
-    if (!status || !offset || !workspace) return ARDIFF_ERR_NULL;
-    if (requests > 0 && (!length || (width > 0 && !table) || !k_cache || !score || !new_score)) return ARDIFF_ERR_NULL;
-    if (tokens > 0 && (!q || !lse)) return ARDIFF_ERR_NULL;
+    if (!c.status || !c.offset || !c.workspace) return ARDIFF_ERR_NULL;
+    if (requests > 0 && (!c.length || (width > 0 && !c.table) || !c.k_cache || !c.score || !c.new_score)) return ARDIFF_ERR_NULL;
+    if (tokens > 0 && (!c.q || !c.lse)) return ARDIFF_ERR_NULL;
     auto low = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
-    if (((low(q) | low(k_cache)) & 15u) || (low(workspace) & 15u) || ((q_token | q_head | k_page | k_token | k_head) & 7)) return ARDIFF_ERR_ALIGN;
-    if (workspace_bytes < ardiff_attend_weights_workspace(requests)) return ARDIFF_ERR_SHAPE;
-    if (score == new_score && requests > 1 && ld != new_ld) return ARDIFF_ERR_SHAPE;
+    if (((low(c.q) | low(c.k_cache)) & 15u) || (low(c.workspace) & 15u) || ((c.q_token | c.q_head | c.k_page | c.k_token | c.k_head) & 7)) return ARDIFF_ERR_ALIGN;
+    if (c.workspace_bytes < ardiff_attend_weights_workspace(requests)) return ARDIFF_ERR_SHAPE;
+    if (c.score == c.new_score && requests > 1 && c.ld != c.new_ld) return ARDIFF_ERR_SHAPE;
     const int sms = device_sms();
     if (sms < 1) return ARDIFF_ERR_CUDA;
-    Weights c;
-    memset(&c, 0, sizeof(c));
-    c.cache.k = static_cast<const char*>(k_cache);
-    c.cache.table = table; c.cache.width = width; c.cache.page = page; c.cache.pages = pages; c.cache.heads = heads; c.cache.by_page = divide_by(page);
-    if (!strides_of(k_page, k_token, k_head, c.cache, c.cache.k_page, c.cache.k_token, c.cache.k_head)) return ARDIFF_ERR_SHAPE;
-    c.x.q = q; c.x.lse = const_cast<float*>(lse); c.x.q_token = q_token; c.x.q_head = q_head; c.x.lse_token = lse_token;
-    c.x.heads = q_heads; c.x.G = q_heads / heads; c.x.tokens = tokens; c.x.by_G = divide_by(q_heads / heads);
-    c.length = length; c.offset = offset; c.first = first; c.score = score; c.new_score = new_score; c.status = status;
-    char* w = static_cast<char*>(workspace);
-    c.tiles = reinterpret_cast<long long*>(w);
-    c.arrived = reinterpret_cast<int*>(w + arrived_at(requests));
-    c.part = reinterpret_cast<float*>(w + part_at(requests));
-    c.ld = ld; c.new_ld = new_ld;
-    const int64_t cap = (int64_t)page * width, rows = ld < new_ld ? ld : new_ld;
-    c.limit = cap < rows ? cap : rows;
-    c.scale = scale * 1.4426950408889634f; c.decay = decay;
-    c.requests = requests; c.causal = causal != 0;
+    Weights a;
+    memset(&a, 0, sizeof(a));
+    a.cache.k = static_cast<const char*>(c.k_cache);
+    a.cache.table = c.table; a.cache.width = width; a.cache.page = page; a.cache.pages = c.pages; a.cache.heads = heads; a.cache.by_page = divide_by(page);
+    if (!strides_of(c.k_page, c.k_token, c.k_head, a.cache, a.cache.k_page, a.cache.k_token, a.cache.k_head)) return ARDIFF_ERR_SHAPE;
+    a.x.q = c.q; a.x.lse = const_cast<float*>(c.lse); a.x.q_token = c.q_token; a.x.q_head = c.q_head; a.x.lse_token = c.lse_token;
+    a.x.heads = q_heads; a.x.G = q_heads / heads; a.x.tokens = tokens; a.x.by_G = divide_by(q_heads / heads);
+    a.length = c.length; a.offset = c.offset; a.first = c.first; a.score = c.score; a.new_score = c.new_score; a.status = c.status;
+    char* w = static_cast<char*>(c.workspace);
+    a.tiles = reinterpret_cast<long long*>(w);
+    a.arrived = reinterpret_cast<int*>(w + arrived_at(requests));
+    a.part = reinterpret_cast<float*>(w + part_at(requests));
+    a.ld = c.ld; a.new_ld = c.new_ld;
+    const int64_t cap = (int64_t)page * width, rows = c.ld < c.new_ld ? c.ld : c.new_ld;
+    a.limit = cap < rows ? cap : rows;
+    a.scale = scale * 1.4426950408889634f; a.decay = decay;
+    a.requests = requests; a.causal = c.causal != 0;
     const bool bf16 = dtype == ARDIFF_BF16;
     KeyBoxes boxes;
     memset(&boxes, 0, sizeof(boxes));
     const int box = box_tokens(page);
-    if (box && describe(&boxes.k, c.cache.k, bf16, head_width, box, c.cache, c.cache.k_token, c.cache.k_head, c.cache.k_page)) boxes.tokens = box;
-    boxes.queries = describe_queries(&boxes.q, c.x, bf16, head_width, kRows) && describe_queries(&boxes.few, c.x, bf16, head_width, kFew);
+    if (box && describe(&boxes.k, a.cache.k, bf16, head_width, box, a.cache, a.cache.k_token, a.cache.k_head, a.cache.k_page)) boxes.tokens = box;
+    boxes.queries = describe_queries(&boxes.q, a.x, bf16, head_width, kRows) && describe_queries(&boxes.few, a.x, bf16, head_width, kFew);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool ok = bf16 ? launch_width<__nv_bfloat16>(c, head_width, boxes, sms, st) : launch_width<__half>(c, head_width, boxes, sms, st);
+    const bool ok = bf16 ? launch_width<__nv_bfloat16>(a, head_width, boxes, sms, st) : launch_width<__half>(a, head_width, boxes, sms, st);
     ardiff::set_launch_count(2);
     return ok ? ARDIFF_OK : ARDIFF_ERR_CUDA;
-}
-
-extern "C" int ardiff_attend_weights(const ardiff_attend_weights_call* a, void* stream) {
-    if (!a) return ARDIFF_ERR_NULL;
-    if (!ardiff::in_32_bits({a->q_heads, a->dtype, a->pages, a->page, a->heads, a->head_width, a->width, a->requests,
-        a->causal})) return ARDIFF_ERR_SHAPE;
-    return attend_weights_checked(a->q, a->q_token, a->q_head, (int32_t)a->q_heads, a->tokens, (int32_t)a->dtype, a->k_cache, a->k_page,
-        a->k_token, a->k_head, (int32_t)a->pages, (int32_t)a->page, (int32_t)a->heads, (int32_t)a->head_width, a->table, (int32_t)a->width,
-        (int32_t)a->requests, a->length, a->offset, a->first, a->lse, a->lse_token, a->score, a->ld, (float)a->scale, (float)a->decay,
-        (int32_t)a->causal, a->new_score, a->new_ld, a->status, a->workspace, a->workspace_bytes, stream);
 }
