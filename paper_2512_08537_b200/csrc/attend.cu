@@ -814,7 +814,7 @@ template <typename T> bool launch_width(const Call& c, int32_t dtype, int width,
 }
 
 bool shape(int64_t requests, int64_t groups, int64_t tokens, int64_t q_heads, int64_t heads) {
-    return requests >= 0 && requests <= ARDIFF_PAGES_MAX_REQUESTS && groups >= 0 && groups <= ARDIFF_PAGES_MAX_REQUESTS && tokens >= 0 && heads >= 1 &&
+    return requests >= 0 && requests <= ARDIFF_PAGES_MAX_REQUESTS && groups >= 0 && groups <= ARDIFF_PAGES_MAX_REQUESTS && tokens >= 0 && tokens < (int64_t)1 << 31 && heads >= 1 &&
            q_heads >= heads && q_heads % heads == 0 && q_heads <= ARDIFF_ROTARY_MAX_HEADS && tokens * q_heads < (int64_t)1 << 31;
 }
 

@@ -487,7 +487,7 @@ extern "C" int ardiff_attend_weights(const ardiff_attend_weights_call* call, voi
     const int width = (int)c.width, dtype = (int)c.dtype;
     const int64_t tokens = c.tokens;
     const float scale = (float)c.scale, decay = (float)c.decay;
-    if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || tokens < 0 || heads < 1 || q_heads < heads || q_heads % heads ||
+    if (requests < 0 || requests > ARDIFF_PAGES_MAX_REQUESTS || tokens < 0 || tokens >= (int64_t)1 << 31 || heads < 1 || q_heads < heads || q_heads % heads ||
         q_heads > ARDIFF_ROTARY_MAX_HEADS || tokens * q_heads >= (int64_t)1 << 31 || c.pages < 0 || page < 1 || width < 0 ||
         (int64_t)page * width > ARDIFF_CACHE_MAX_PLACES || c.ld < 0 || c.new_ld < 0 || !isfinite(scale * 1.4426950408889634f) || !isfinite(decay))
         return ARDIFF_ERR_SHAPE;

@@ -209,3 +209,11 @@ def test_workspace_of_attention_holds_what_its_pieces_need():
     assert 2 * 65536 * 32 * 128 * 4 < L.ardiff_attend_workspace(64, 1, 65536, 32, 8, 128) < 2 * 65536 * 32 * 130 * 4 + (50 << 20)
     for args in ((1, 8, 1, 64), (3, 8, 2, 64), (17, 1, 1, 128)):
         assert 0 < L.ardiff_attend_workspace(2, 0, *args) <= L.ardiff_attend_workspace(2, 1, *args)
+
+
+@pytest.mark.parametrize("tokens,q_heads,heads", [(1 << 61, 8, 2), (1 << 62, 4, 2), (1 << 60, 16, 16), ((1 << 61) + 1, 8, 8), (1 << 54, 1024, 1)])
+def test_numbers_of_tokens_whose_products_wrap(tokens, q_heads, heads):
+    assert ardiff.lib().ardiff_attend_workspace(2, 0, tokens, q_heads, heads, 64) == SHAPE
+    kw = dict(tokens=tokens, q_heads=q_heads, heads=heads, workspace_bytes=(1 << 63) - 1)
+    assert call("ardiff_attend_pages", attend(), dict(kw, out=2 * P)) == SHAPE
+    assert call("ardiff_attend_weights", weights(), kw) == SHAPE
